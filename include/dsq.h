@@ -51,12 +51,13 @@ typedef enum {
   DS_ERR_UNSUPPORTED = -6
 } ds_status;
 
-/* dev_status is four words.  Word 0 holds flags: */
+/* dev_status is four words (the calls on single matrices below take a pointer to the first one alone).  Word 0 holds flags: */
 #define DS_DEV_TOPK_INCONSISTENT 0x1u /* top-k selection counted a number of entries other than k */
 /* Words 1 and 2 count top-k selections (one per vector and pass) by the route they took: with the
  * threshold band predicted from the previous steps ("predicted": v is read once), or through the
  * full histogram after a missing or wrong prediction ("full": v is read three times).  Both routes
  * give the same result; the counters are for tests and tuning.  Word 3 is reserved. */
+#define DS_DEV_MMA_TIMEOUT 0x2u       /* a tensor-core product gave up waiting (about a second): its outputs are not valid */
 #define DS_DEV_WORD_FLAGS 0
 #define DS_DEV_WORD_TOPK_PREDICTED 1
 #define DS_DEV_WORD_TOPK_FULL 2
@@ -357,6 +358,82 @@ int ds_step_host(ds_handle h, const float* g_host, float* g_dev, uint32_t step, 
 #define DS_STATIC_TOPK_MAX_D (1u << 23)
 int ds_topk_worker_static(const float* g, float* delta, uint64_t d, uint64_t k, uint32_t* idx, float* val,
                           uint32_t* dev_status, void* cuda_stream);
+
+/*
+ * ---- What produces a gradient and what is done with Q[v]: operators on matrices ----
+ *
+ * These calls stand beside the step above and share its rules: device memory and workspaces are the caller's, work is only
+ * enqueued, everything returns a ds_status.  dev_status: device uint32, zero-filled by the caller once (DS_DEV_MMA_TIMEOUT).
+ */
+typedef enum { DS_F32 = 0, DS_BF16 = 1, DS_F16 = 2 } ds_dtype;
+
+/*
+ * Matrix products in 8-bit integers with one scale per row of either operand ("per token and channel").
+ *
+ * ds_i8_quantize: x [rows, cols], `ld` elements between rows, becomes
+ *     q  [rows, ldq]   codes by rows:     scale_r   = max_c |x_rc| * fl(1/127),  q_rc  = round(x_rc * fl(1/scale_r))
+ *     qt [cols, ldqt]  codes by columns, transposed:  scale_t_c = max_r |x_rc| * fl(1/127),  qt_cr = round(x_rc * fl(1/scale_t_c))
+ *     col_sum [cols]   sum over the rows (the gradient of a bias), in 32 bits
+ *   Each of (q, scale), (qt, scale_t), col_sum may be NULL; x is read once for the rows alone, else twice.  Rounding is to
+ *   nearest even.  A line of zeros (or one whose scale would be subnormal) has scale 0 and codes 0; a line that holds an
+ *   inf or a NaN has scale NaN and codes 0, so that products with it are NaN.  Codes between the line's end and the next
+ *   multiple of 16 may be overwritten (with 0 by rows).  q, qt: 16-byte aligned, ldq and ldqt multiples of 16.
+ *   workspace (16-byte aligned, ds_i8_quantize_workspace bytes) is needed unless q alone is asked for.
+ * ds_i8_matmul:  out_mn = (sum_k a_mk b_nk) * sa_m * sb_n + bias_n  with a [m, k], b [n, k]; the sum is exact, the rest is
+ *   done from left to right in 32 bits.  bias may be NULL.  out [m, n], `ldo` elements between rows, of type out_dtype.  k <= DS_I8_MAX_K, else DS_ERR_UNSUPPORTED.
+ *   k = 0 gives the bias.
+ * ds_i8_linear:  the two together for a linear layer whose weights w [n, k] were quantised before (rows = output
+ *   channels): x [rows, k] is quantised by rows into the workspace (ds_i8_linear_workspace bytes, 16-byte aligned).
+ * Training takes the same calls: forward  a = rows of x, b = rows of W;  gradient of inputs  a = rows of dY, b = columns
+ *   of W (qt);  gradient of weights  a = columns of dY, b = columns of x.
+ */
+#define DS_I8_MAX_K 131072u
+uint64_t ds_i8_quantize_workspace(uint64_t rows, uint64_t cols, int with_col_sum);
+int ds_i8_quantize(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ld, int8_t* q, uint64_t ldq, float* scale,
+                   int8_t* qt, uint64_t ldqt, float* scale_t, float* col_sum, void* workspace, size_t workspace_bytes,
+                   void* cuda_stream);
+int ds_i8_matmul(const int8_t* a, uint64_t lda, const float* sa, const int8_t* b, uint64_t ldb, const float* sb, const float* bias,
+                 uint64_t m, uint64_t n, uint64_t k, void* out, int out_dtype, uint64_t ldo, uint32_t* dev_status, void* cuda_stream);
+uint64_t ds_i8_linear_workspace(uint64_t rows, uint64_t k);
+int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t ldx, const int8_t* w, uint64_t ldw, const float* sw,
+                 const float* bias, uint64_t n, void* out, int out_dtype, uint64_t ldo, void* workspace, size_t workspace_bytes,
+                 uint32_t* dev_status, void* cuda_stream);
+
+/*
+ * Orthogonalised update of matrices (momentum and Newton-Schulz products):
+ *
+ *     buf = momentum * buf + g;   u = g + momentum * buf (DS_ORTH_NESTEROV) or buf;   X = u / (||u||_F + eps)
+ *     `steps` times:  A = X X^T,  X = a X + (b A + c A A) X      (X^T where the matrix is taller than wide)
+ *     out = X,  and / or  x = x (1 - gamma decay) - gamma scale X
+ *
+ * for `batch` matrices [rows, cols], each row-major and contiguous, `stride` elements apart in g, buf and x (0: rows * cols),
+ * so that they can be slices of the flat gradient and model of the step above; out is contiguous.  buf is float and updated
+ * in place (NULL: u = g).  g: DS_F32, DS_BF16 or DS_F16; out: DS_F32 or DS_BF16.  buf and u are formed in 32 bits exactly as
+ * written (each operation rounded); the products run on 16-bit floats with 32-bit sums: X is within about 1e-3 of exact
+ * arithmetic (Frobenius norm, relative).  Singular values of X must stay below 8 (they do for the usual coefficients).  An
+ * update of zeros gives zeros; one that holds an inf or a NaN gives NaN.
+ *
+ * ds_orth_create: with workspace == NULL fills *workspace_bytes and returns DS_NEED_BUFFERS; else makes a handle on that
+ * workspace (256-byte aligned, zero-filled once by the caller).  Host-only.  One handle on one stream at a time.
+ */
+#define DS_ORTH_NESTEROV 0x1u
+typedef struct {
+  uint32_t rows, cols;   /* 1 .. 2^20 each */
+  uint32_t batch;        /* 1 .. 65535 */
+  uint32_t steps;        /* 1 .. 32 */
+  float a, b, c;         /* coefficients of the step */
+  float momentum;
+  float eps;             /* >= 0 */
+  float scale;           /* factor of the model update */
+  uint32_t flags;        /* DS_ORTH_NESTEROV or 0 */
+  uint32_t reserved;     /* 0 */
+  uint64_t stride;
+} ds_orth_config;
+typedef struct ds_orth_ctx* ds_orth_handle;
+int ds_orth_create(const ds_orth_config* cfg, void* workspace, size_t* workspace_bytes, uint32_t* dev_status, ds_orth_handle* out);
+int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum, void* out, int out_dtype, float* x, float gamma,
+                   float decay, void* cuda_stream);
+int ds_orth_destroy(ds_orth_handle h);
 
 /* Text of the most recent CUDA error seen by this thread's calls ("" if none). */
 const char* ds_last_error(void);

@@ -26,7 +26,13 @@ EXPORTS = ("ds_get_layout", "ds_create", "ds_worker_compress", "ds_server_aggreg
            "ds_apply_update", "ds_destroy", "ds_step_host", "ds_last_error", "ds_version",
            "ds_kernel_launches", "ds_topk_worker_static", "ds_worker_compress_rows",
            "ds_server_aggregate_compress_slice", "ds_apply_update_slice", "ds_server_topk_slice_begin",
-           "ds_server_topk_slice_digit", "ds_server_topk_slice_emit", "ds_apply_update_sparse_range")
+           "ds_server_topk_slice_digit", "ds_server_topk_slice_emit", "ds_apply_update_sparse_range",
+           "ds_i8_quantize_workspace", "ds_i8_quantize", "ds_i8_matmul", "ds_i8_linear_workspace", "ds_i8_linear",
+           "ds_orth_create", "ds_orth_update", "ds_orth_destroy")
+DS_DEV_MMA_TIMEOUT = 2
+DS_F32, DS_BF16, DS_F16 = 0, 1, 2
+DS_I8_MAX_K = 131072
+DS_ORTH_NESTEROV = 1
 DS_SLICE_ALIGN = 8192
 
 
@@ -51,6 +57,12 @@ class ds_buffers(C.Structure):
 
 class ds_payload_layout(C.Structure):
     _fields_ = [("stride", C.c_uint64), ("off", C.c_uint64 * 3), ("count", C.c_uint64 * 3)]
+
+
+class ds_orth_config(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("cols", C.c_uint32), ("batch", C.c_uint32), ("steps", C.c_uint32),
+                ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("momentum", C.c_float), ("eps", C.c_float),
+                ("scale", C.c_float), ("flags", C.c_uint32), ("reserved", C.c_uint32), ("stride", C.c_uint64)]
 
 
 class DsqError(RuntimeError):
@@ -87,8 +99,18 @@ def load_library() -> C.CDLL:
     L.ds_server_topk_slice_digit.argtypes = [vp, C.c_int, C.c_uint64, C.c_uint64, vp, vp, vp]
     L.ds_server_topk_slice_emit.argtypes = [vp, C.c_uint64, C.c_uint64, u32, u32, C.c_uint64, u32, vp]
     L.ds_apply_update_sparse_range.argtypes = [vp, C.c_uint64, C.c_uint64, vp]
+    u64, size = C.c_uint64, C.c_size_t
+    L.ds_i8_quantize_workspace.argtypes = [u64, u64, C.c_int]
+    L.ds_i8_quantize.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, vp, vp, u64, vp, vp, vp, size, vp]
+    L.ds_i8_matmul.argtypes = [vp, u64, vp, vp, u64, vp, vp, u64, u64, u64, vp, C.c_int, u64, vp, vp]
+    L.ds_i8_linear_workspace.argtypes = [u64, u64]
+    L.ds_i8_linear.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, vp, vp, u64, vp, C.c_int, u64, vp, size, vp, vp]
+    L.ds_orth_create.argtypes = [C.POINTER(ds_orth_config), vp, C.POINTER(size), vp, C.POINTER(vp)]
+    L.ds_orth_update.argtypes = [vp, vp, C.c_int, vp, vp, C.c_int, vp, C.c_float, C.c_float, vp]
+    L.ds_orth_destroy.argtypes = [vp]
     for name in EXPORTS:
         getattr(L, name).restype = C.c_int
+    L.ds_i8_quantize_workspace.restype = L.ds_i8_linear_workspace.restype = u64
     L.ds_last_error.restype = C.c_char_p
     L.ds_kernel_launches.restype = C.c_uint64
     _lib = L

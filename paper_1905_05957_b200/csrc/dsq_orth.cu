@@ -1,0 +1,596 @@
+// Orthogonalised update: momentum, then Newton-Schulz products that bring the singular values of the update near one.
+//
+//   buf = mu buf + g;   u = g + mu buf (Nesterov) or buf;   X = u / (||u||_F + eps)
+//   `steps` times:  A = X X^T,  B = b A + c A A,  X = a X + B X         (over the shorter side: X is [m, n], m <= n)
+//   out = X;  optionally x = (1 - gamma decay) x - gamma scale X
+//
+// Numbers.  Products run on 16-bit floats with 11 bits of significand (same rate as the 8-bit-significand format, whose error
+// would be eight times as large) and add up in 32 bits.  The entries of X, A and B are bounded (|X| <= 1.3, |A| <= 1.5, |B| <= 8 for
+// the usual coefficients), so they are held times 2^10, which keeps small entries out of the subnormals.  Two things
+// would otherwise lose bits that later steps multiply by a = 3.4 each:
+//  - X is carried in two halves (hi + lo, 22 bits).  The term aX takes both; the products take hi.  With hi alone, updates
+//    whose energy sits in few directions came out 0.6 % to 2 % off; with both, 0.02 % to 0.05 %.
+//  - The diagonals of A and B, which hold most of their size when rows are nearly orthogonal, stay in 32 bits: A = D + O and
+//    B = E + F with F off-diagonal:  F = b O + c (O O)_off + c (d_i + d_j) O_ij,  E_ii = b d_i + c d_i^2 + c (O O)_ii,
+//    X = (a + E) X + F X.  Row scalings cost nothing in the epilogues.  (0.1 % to 0.2 % off without it on such inputs.)
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "dsq_mma.cuh"
+
+using namespace dsq;
+
+namespace {
+
+constexpr float kUp = 1024.f, kDown = 1.f / 1024.f;   // the fixed scale of the 16-bit matrices
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+
+__device__ __forceinline__ void load4(float (&o)[4], const float* p) {
+  const float4 v = *reinterpret_cast<const float4*>(p);
+  o[0] = v.x, o[1] = v.y, o[2] = v.z, o[3] = v.w;
+}
+template <class T16>
+__device__ __forceinline__ void load4(float (&o)[4], const T16* p) {
+  const uint2 v = *reinterpret_cast<const uint2*>(p);
+  const T16* e = reinterpret_cast<const T16*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = to_f32(e[i]);
+}
+
+struct Momentum {
+  const void* g;
+  float* buf;        // NULL: u = g
+  uint64_t stride;   // elements between matrices of g and buf
+  float mu;
+  int nesterov;
+  __device__ __forceinline__ float update(float g, float b) const {   // the new buf
+    return __fadd_rn(__fmul_rn(mu, b), g);
+  }
+  __device__ __forceinline__ float direction(float g, float b) const {   // u from the new buf
+    return nesterov ? __fadd_rn(g, __fmul_rn(mu, b)) : b;
+  }
+};
+
+// ---- momentum and norm: one pass over g and buf ----
+// Bound by memory: 4 (or 2) + 4 bytes read and 4 written an entry.  Squares add up in 64 bits, each thread over its own
+// entries, then in a fixed order; the CTA of a matrix that ends last adds the CTAs' sums, in order, and leaves
+// 2^10 / (norm + eps).
+constexpr int kNormCtas = 512;
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_orth_momentum(const Momentum mo, uint64_t count, int vec, float eps, double* partial,
+                                                            uint32_t* ticket, float* inv) {
+  pdl_prologue();
+  const uint64_t off = (uint64_t)blockIdx.y * mo.stride;
+  const T* g = static_cast<const T*>(mo.g) + off;
+  float* buf = mo.buf ? mo.buf + off : nullptr;
+  double sum = 0;
+  const uint64_t first = (uint64_t)blockIdx.x * kThreads + threadIdx.x, step = (uint64_t)gridDim.x * kThreads;
+  if (vec) {
+    for (uint64_t i = first * 4; i < count; i += step * 4) {
+      float gv[4], bv[4], u[4];
+      load4(gv, g + i);
+      if (buf) {
+        load4(bv, buf + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bv[j] = mo.update(gv[j], bv[j]), u[j] = mo.direction(gv[j], bv[j]);
+        *reinterpret_cast<float4*>(buf + i) = make_float4(bv[0], bv[1], bv[2], bv[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = gv[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += (double)u[j] * (double)u[j];
+    }
+  } else {
+    for (uint64_t i = first; i < count; i += step) {
+      const float gv = to_f32(g[i]);
+      float u = gv;
+      if (buf) {
+        const float bv = mo.update(gv, buf[i]);
+        buf[i] = bv;
+        u = mo.direction(gv, bv);
+      }
+      sum += (double)u * (double)u;
+    }
+  }
+  __shared__ double warp_sum[kThreads / 32];
+  __shared__ uint32_t last;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0;
+    for (int i = 0; i < kThreads / 32; ++i) s += warp_sum[i];
+    partial[(uint64_t)blockIdx.y * kNormCtas + blockIdx.x] = s;
+    __threadfence();
+    last = atomicAdd(ticket + blockIdx.y, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last || threadIdx.x >= 32) return;
+  __threadfence();
+  double s = 0;
+  for (uint32_t i = threadIdx.x; i < gridDim.x; i += 32) s += __ldcg(partial + (uint64_t)blockIdx.y * kNormCtas + i);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  if (threadIdx.x == 0) {
+    inv[blockIdx.y] = kUp / ((float)sqrt(s) + eps);
+    ticket[blockIdx.y] = 0;
+  }
+}
+
+// ---- X = u / norm in two halves, transposed where the matrix is taller than wide ----
+// 64 x 64 tiles; the tile goes through shared memory when it is transposed.
+struct Halves {
+  __half *hi, *lo;
+  uint32_t ld;       // elements between rows (a multiple of 8)
+  uint64_t stride;   // elements between matrices
+};
+
+template <class T, bool TALL>
+__global__ void __launch_bounds__(kThreads) k_orth_split(const Momentum mo, uint32_t rows, uint32_t cols, int vec, const float* inv,
+                                                         const Halves x) {
+  pdl_prologue();
+  __shared__ float tile[TALL ? 64 : 1][TALL ? 65 : 1];
+  const uint32_t b = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+  const uint64_t off = (uint64_t)b * mo.stride;
+  const T* g = static_cast<const T*>(mo.g) + off;
+  const float* buf = mo.buf ? mo.buf + off : nullptr;
+  const float f = inv[b];
+  auto put = [&](uint32_t r, uint32_t c, const float (&v)[4]) {   // c a multiple of 4 below ld
+    __half h[4], l[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h[j] = __float2half_rn(v[j]), l[j] = __float2half_rn(v[j] - __half2float(h[j]));
+    const uint64_t at = (uint64_t)b * x.stride + (uint64_t)r * x.ld + c;
+    *reinterpret_cast<uint2*>(x.hi + at) = *reinterpret_cast<uint2*>(h);
+    *reinterpret_cast<uint2*>(x.lo + at) = *reinterpret_cast<uint2*>(l);
+  };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lr = threadIdx.x / 16 + 16 * i, lc = threadIdx.x % 16 * 4, r = r0 + lr, c = c0 + lc;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (r < rows && c < cols) {
+      const uint64_t at = (uint64_t)r * cols + c;
+      float gv[4] = {0.f, 0.f, 0.f, 0.f}, bv[4] = {0.f, 0.f, 0.f, 0.f};
+      if (vec) {
+        load4(gv, g + at);
+        if (buf) load4(bv, buf + at);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c + j < cols) {
+            gv[j] = to_f32(g[at + j]);
+            if (buf) bv[j] = buf[at + j];
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = __fmul_rn(buf ? mo.direction(gv[j], bv[j]) : gv[j], f);
+    }
+    if constexpr (TALL) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) tile[lr][lc + j] = v[j];
+    } else {
+      if (r < rows && c < x.ld) put(r, c, v);
+    }
+  }
+  if constexpr (TALL) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lr = threadIdx.x / 16 + 16 * i, lc = threadIdx.x % 16 * 4, r = c0 + lr, c = r0 + lc;   // of X = u^T
+      float v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = tile[lc + j][lr];
+      if (r < cols && c < x.ld) put(r, c, v);
+    }
+  }
+}
+
+// ---- epilogues of the three products ----
+
+struct Half32 {   // 32 consecutive entries of a row
+  uint4 q[4];
+};
+__device__ __forceinline__ Half32 load_half32(const __half* row, uint32_t col0, uint32_t ld) {
+  Half32 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    v.q[i] = col0 + 8 * i < ld ? *reinterpret_cast<const uint4*>(row + col0 + 8 * i) : make_uint4(0, 0, 0, 0);
+  return v;
+}
+__device__ __forceinline__ void store_half32(__half* row, uint32_t col0, uint32_t ld, const Half32& v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (col0 + 8 * i < ld) *reinterpret_cast<uint4*>(row + col0 + 8 * i) = v.q[i];
+}
+__device__ __forceinline__ float half_at(const Half32& v, int j) { return __half2float(reinterpret_cast<const __half*>(&v)[j]); }
+
+// A symmetric matrix in 16 bits without its diagonal, which is held apart.
+struct SymOut {
+  __half* off;
+  float* diag;
+  uint32_t m, ld;
+  uint64_t stride, diag_stride;
+  // The block (row, col0..col0+31) and its mirror image.  Lanes hold consecutive rows, so a column of the block is 64
+  // consecutive bytes of the mirrored row.
+  __device__ __forceinline__ void put(const Half32& v, uint32_t row, uint32_t col0, uint32_t b) const {
+    if (row >= m) return;
+    __half* base = off + b * stride;
+    store_half32(base + (uint64_t)row * ld, col0, ld, v);
+    if (col0 > row) {
+      const __half* e = reinterpret_cast<const __half*>(&v);
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (col0 + j < m) base[(uint64_t)(col0 + j) * ld + row] = e[j];
+    }
+  }
+};
+
+struct EpiGram {   // A = X X^T
+  struct Pre {};
+  SymOut a;
+  __device__ __forceinline__ Pre load(uint32_t, uint32_t, uint32_t) const { return {}; }
+  __device__ __forceinline__ void apply(const Pre&, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b) const {
+    Half32 v;
+    __half* e = reinterpret_cast<__half*>(&v);
+    float d = 0.f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float s = __uint_as_float(acc[j]);
+      const bool on = col0 + j == row;
+      if (on) d = s;
+      e[j] = __float2half_rn(on ? 0.f : s * kDown);
+    }
+    if (row >= col0 && row < col0 + 32 && row < a.m) a.diag[b * a.diag_stride + row] = d * (kDown * kDown);
+    a.put(v, row, col0, b);
+  }
+};
+
+struct EpiPoly {   // B = b A + c A A, the accumulator being O O
+  struct Pre {
+    Half32 o;
+    float d;
+  };
+  SymOut a, out;
+  float b1, c1;
+  __device__ __forceinline__ Pre load(uint32_t row, uint32_t col0, uint32_t b) const {
+    Pre p{};
+    if (row < a.m) {
+      p.o = load_half32(a.off + b * a.stride + (uint64_t)row * a.ld, col0, a.ld);
+      p.d = a.diag[b * a.diag_stride + row];
+    }
+    return p;
+  }
+  __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b) const {
+    Half32 v;
+    __half* e = reinterpret_cast<__half*>(&v);
+    const float* dj = a.diag + b * a.diag_stride + col0;   // padded to a multiple of 32 entries
+    float d = 0.f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float s = __uint_as_float(acc[j]), o = half_at(p.o, j);
+      const bool on = col0 + j == row;
+      if (on) d = s;
+      e[j] = __float2half_rn(on || col0 + j >= a.m ? 0.f : fmaf(c1, fmaf(s, kDown, (p.d + dj[j]) * o), b1 * o));
+    }
+    if (row >= col0 && row < col0 + 32 && row < a.m)
+      out.diag[b * a.diag_stride + row] = fmaf(c1, fmaf(d, kDown * kDown, p.d * p.d), b1 * p.d);
+    out.put(v, row, col0, b);
+  }
+};
+
+struct EpiX {   // X = (a + E) X + F X
+  struct Pre {
+    Half32 hi, lo;
+    float e;
+  };
+  const __half *hi, *lo;     // X, both halves
+  const float* diag;         // E
+  uint64_t stride, diag_stride;
+  uint32_t m, n, ld;
+  float a1;
+  __half *hi_out, *lo_out;   // the next X; NULL on the last step, which writes:
+  void* out;                 //   out (may be NULL), contiguous, in the orientation of the gradient
+  int out_dtype, tall, vec;
+  float* x;                  //   x (may be NULL)
+  uint64_t x_stride;
+  float keep, rate;          //   x = keep x - rate X
+  __device__ __forceinline__ Pre load(uint32_t row, uint32_t col0, uint32_t b) const {
+    Pre p{};
+    if (row < m) {
+      const uint64_t at = b * stride + (uint64_t)row * ld;
+      p.hi = load_half32(hi + at, col0, ld);
+      p.lo = load_half32(lo + at, col0, ld);
+      p.e = diag[b * diag_stride + row];
+    }
+    return p;
+  }
+  __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b) const {
+    if (row >= m) return;
+    const float f = a1 + p.e;
+    float v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = fmaf(f, half_at(p.hi, j) + half_at(p.lo, j), __uint_as_float(acc[j]) * kDown);
+    if (hi_out) {
+      Half32 h, l;
+      __half *eh = reinterpret_cast<__half*>(&h), *el = reinterpret_cast<__half*>(&l);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        eh[j] = __float2half_rn(v[j]);
+        el[j] = __float2half_rn(v[j] - __half2float(eh[j]));
+      }
+      const uint64_t at = b * stride + (uint64_t)row * ld;
+      store_half32(hi_out + at, col0, ld, h);
+      store_half32(lo_out + at, col0, ld, l);
+      return;
+    }
+    // The last step leaves the workspace.  Tall matrices come back transposed: lanes then hold consecutive entries.
+    const uint64_t step = tall ? m : 1;
+    const uint64_t first = tall ? (uint64_t)col0 * m + row : (uint64_t)row * n + col0, each = (uint64_t)m * n;
+    const bool whole = vec && !tall && col0 + 32 <= n;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] *= kDown;
+    if (out) {
+      const uint64_t at = b * each + first;
+      if (out_dtype == DS_BF16) {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(out) + at;
+        if (whole) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            __nv_bfloat16 t[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] = __float2bfloat16_rn(v[8 * q + j]);
+            *reinterpret_cast<uint4*>(o + 8 * q) = *reinterpret_cast<uint4*>(t);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (col0 + j < n) o[j * step] = __float2bfloat16_rn(v[j]);
+        }
+      } else {
+        float* o = static_cast<float*>(out) + at;
+        if (whole) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) *reinterpret_cast<float4*>(o + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (col0 + j < n) o[j * step] = v[j];
+        }
+      }
+    }
+    if (x) {
+      float* px = x + b * x_stride + first;
+      if (whole) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          float4 t = *reinterpret_cast<float4*>(px + 4 * q);
+          t.x = __fsub_rn(__fmul_rn(keep, t.x), __fmul_rn(rate, v[4 * q]));
+          t.y = __fsub_rn(__fmul_rn(keep, t.y), __fmul_rn(rate, v[4 * q + 1]));
+          t.z = __fsub_rn(__fmul_rn(keep, t.z), __fmul_rn(rate, v[4 * q + 2]));
+          t.w = __fsub_rn(__fmul_rn(keep, t.w), __fmul_rn(rate, v[4 * q + 3]));
+          *reinterpret_cast<float4*>(px + 4 * q) = t;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (col0 + j < n) px[j * step] = __fsub_rn(__fmul_rn(keep, px[j * step]), __fmul_rn(rate, v[j]));
+      }
+    }
+  }
+};
+
+template <bool B_ACROSS, class Epi>
+cudaError_t launch_f16(int bn, const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
+  switch (bn) {
+    case 256: return launch_mma_bn<kMmaF16, 256, B_ACROSS>(a, b, s, epi, st);
+    case 192: return launch_mma_bn<kMmaF16, 192, B_ACROSS>(a, b, s, epi, st);
+    case 128: return launch_mma_bn<kMmaF16, 128, B_ACROSS>(a, b, s, epi, st);
+    default: return launch_mma_bn<kMmaF16, 64, B_ACROSS>(a, b, s, epi, st);
+  }
+}
+
+inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
+
+bool orth_config_ok(const ds_orth_config* c) {
+  if (!c || c->rows < 1 || c->cols < 1 || c->batch < 1 || c->batch > 65535 || c->rows > (1u << 20) || c->cols > (1u << 20)) return false;
+  if (c->steps < 1 || c->steps > 32 || (c->flags & ~DS_ORTH_NESTEROV)) return false;
+  if (c->stride && c->stride < (uint64_t)c->rows * c->cols) return false;
+  for (float v : {c->a, c->b, c->c, c->momentum, c->eps, c->scale})
+    if (!std::isfinite(v)) return false;
+  return c->eps >= 0.f;
+}
+
+}  // namespace
+
+struct ds_orth_ctx {
+  ds_orth_config cfg;
+  uint32_t m, n, ldx, ldm;
+  uint64_t xs, ms, ds;            // elements between matrices of X, of A and B, of the diagonals
+  __half *hi[2], *lo[2];
+  SymOut a, b;
+  double* partial;
+  float* inv;
+  uint32_t* ticket;
+  uint32_t* dev_status;
+  bool mapped;                    // the tensor maps below are made (on the first update: the driver makes them)
+  int bn_gram, bn_poly, bn_x;
+  CUtensorMap x_rows[2], x_cols_gram[2], x_across[2], a_rows, a_cols, b_rows;
+};
+
+namespace {
+
+// Carves the workspace; returns its size.
+uint64_t orth_plan(ds_orth_ctx* h, uint8_t* ws) {
+  const ds_orth_config& c = h->cfg;
+  h->m = c.rows < c.cols ? c.rows : c.cols;
+  h->n = c.rows < c.cols ? c.cols : c.rows;
+  h->ldx = (uint32_t)round_up(h->n, 8);
+  h->ldm = (uint32_t)round_up(h->m, 8);
+  h->xs = (uint64_t)h->m * h->ldx;
+  h->ms = (uint64_t)h->m * h->ldm;
+  h->ds = round_up(h->m, 32);
+  uint64_t pos = 0;
+  auto take = [&](uint64_t bytes) {
+    uint8_t* p = ws ? ws + pos : nullptr;
+    pos += round_up(bytes, 256);
+    return p;
+  };
+  h->ticket = reinterpret_cast<uint32_t*>(take(4ull * c.batch));
+  h->inv = reinterpret_cast<float*>(take(4ull * c.batch));
+  h->partial = reinterpret_cast<double*>(take(8ull * kNormCtas * c.batch));
+  for (int i = 0; i < 2; ++i) {
+    h->hi[i] = reinterpret_cast<__half*>(take(2 * h->xs * c.batch));
+    h->lo[i] = reinterpret_cast<__half*>(take(2 * h->xs * c.batch));
+  }
+  for (SymOut* s : {&h->a, &h->b}) {
+    s->off = reinterpret_cast<__half*>(take(2 * h->ms * c.batch));
+    s->diag = reinterpret_cast<float*>(take(4 * h->ds * c.batch));
+    s->m = h->m;
+    s->ld = h->ldm;
+    s->stride = h->ms;
+    s->diag_stride = h->ds;
+  }
+  return pos;
+}
+
+cudaError_t orth_maps(ds_orth_ctx* h) {
+  const uint32_t batch = h->cfg.batch;
+  const int sms = sm_count();
+  h->bn_gram = pick_bn({h->m, h->m, h->n, batch, 1, nullptr}, sms);
+  h->bn_poly = pick_bn({h->m, h->m, h->m, batch, 1, nullptr}, sms);
+  h->bn_x = pick_bn({h->m, h->n, h->m, batch, 0, nullptr}, sms);
+  cudaError_t e = cudaSuccess;
+  auto add = [&](CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t ld, uint64_t stride, uint32_t box_rows) {
+    if (e == cudaSuccess) e = make_tensor_map(map, kMmaF16, base, cols, rows, batch, ld, stride, 64, box_rows);
+  };
+  for (int i = 0; i < 2; ++i) {
+    add(&h->x_rows[i], h->hi[i], h->n, h->m, h->ldx, h->xs, kMmaRows);
+    add(&h->x_cols_gram[i], h->hi[i], h->n, h->m, h->ldx, h->xs, h->bn_gram);
+    add(&h->x_across[i], h->hi[i], h->n, h->m, h->ldx, h->xs, 64);
+  }
+  add(&h->a_rows, h->a.off, h->m, h->m, h->ldm, h->ms, kMmaRows);
+  add(&h->a_cols, h->a.off, h->m, h->m, h->ldm, h->ms, h->bn_poly);
+  add(&h->b_rows, h->b.off, h->m, h->m, h->ldm, h->ms, kMmaRows);
+  h->mapped = e == cudaSuccess;
+  return e;
+}
+
+template <class T>
+cudaError_t launch_prepare(const ds_orth_ctx* h, const Momentum& mo, int vec, cudaStream_t st) {
+  const ds_orth_config& c = h->cfg;
+  const uint64_t count = (uint64_t)c.rows * c.cols;
+  const uint64_t want = (count + 16ull * kThreads - 1) / (16ull * kThreads);
+  const uint32_t ctas = (uint32_t)(want < kNormCtas ? want : kNormCtas);
+  launch_pdl(k_orth_momentum<T>, dim3(ctas, c.batch), dim3(kThreads), st, mo, count, vec, c.eps, h->partial, h->ticket, h->inv);
+  const Halves x{h->hi[0], h->lo[0], h->ldx, h->xs};
+  const dim3 grid((c.cols + 63) / 64, (c.rows + 63) / 64, c.batch);
+  if (c.rows > c.cols)
+    launch_pdl(k_orth_split<T, true>, grid, dim3(kThreads), st, mo, c.rows, c.cols, vec, (const float*)h->inv, x);
+  else
+    launch_pdl(k_orth_split<T, false>, grid, dim3(kThreads), st, mo, c.rows, c.cols, vec, (const float*)h->inv, x);
+  count_launches(2);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+extern "C" {
+
+int ds_orth_create(const ds_orth_config* cfg, void* workspace, size_t* workspace_bytes, uint32_t* dev_status, ds_orth_handle* out) {
+  if (!orth_config_ok(cfg) || !workspace_bytes) return DS_ERR_INVALID_ARG;
+  ds_orth_ctx tmp;
+  memset(&tmp, 0, sizeof tmp);
+  tmp.cfg = *cfg;
+  const uint64_t need = orth_plan(&tmp, static_cast<uint8_t*>(workspace));
+  if (!workspace) {
+    *workspace_bytes = need;
+    return DS_NEED_BUFFERS;
+  }
+  if (!dev_status || !out) return DS_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255u) || (reinterpret_cast<uintptr_t>(dev_status) & 3u)) return DS_ERR_ALIGN;
+  if (*workspace_bytes < need) return DS_ERR_BUFFER_TOO_SMALL;
+  tmp.dev_status = dev_status;
+  ds_orth_ctx* h = new (std::nothrow) ds_orth_ctx(tmp);
+  if (!h) return DS_ERR_INVALID_ARG;
+  *out = h;
+  return DS_OK;
+}
+
+int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum, void* out, int out_dtype, float* x, float gamma,
+                   float decay, void* cuda_stream) {
+  if (!h || !g || (!out && !x)) return DS_ERR_INVALID_ARG;
+  if (g_dtype != DS_F32 && g_dtype != DS_BF16 && g_dtype != DS_F16) return DS_ERR_INVALID_ARG;
+  if (out && out_dtype != DS_F32 && out_dtype != DS_BF16) return DS_ERR_INVALID_ARG;
+  if (x && (!std::isfinite(gamma) || !std::isfinite(decay))) return DS_ERR_INVALID_ARG;
+  const ds_orth_config& c = h->cfg;
+  const uintptr_t gp = reinterpret_cast<uintptr_t>(g), bp = reinterpret_cast<uintptr_t>(momentum), op = reinterpret_cast<uintptr_t>(out),
+                  xp = reinterpret_cast<uintptr_t>(x);
+  const uint32_t g_size = g_dtype == DS_F32 ? 4 : 2, out_size = out_dtype == DS_F32 ? 4 : 2;
+  if ((gp & (g_size - 1)) || ((bp | xp) & 3u) || (out && (op & (out_size - 1)))) return DS_ERR_ALIGN;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (!h->mapped) {
+    const cudaError_t e = orth_maps(h);
+    if (e != cudaSuccess) return cuda_fail(e, "tensor maps");
+  }
+  Momentum mo;
+  mo.g = g;
+  mo.buf = momentum;
+  mo.stride = c.stride ? c.stride : (uint64_t)c.rows * c.cols;
+  mo.mu = c.momentum;
+  mo.nesterov = (c.flags & DS_ORTH_NESTEROV) ? 1 : 0;
+  // four entries at a time where every matrix, and every row of it, starts on a boundary of four
+  const int vec = c.cols % 4 == 0 && mo.stride % 4 == 0 && (gp & (4 * g_size - 1)) == 0 && (bp & 15u) == 0;
+  cudaError_t e = g_dtype == DS_F32    ? launch_prepare<float>(h, mo, vec, st)
+                  : g_dtype == DS_BF16 ? launch_prepare<__nv_bfloat16>(h, mo, vec, st)
+                                       : launch_prepare<__half>(h, mo, vec, st);
+  const MmaShape gram{h->m, h->m, h->n, c.batch, 1, h->dev_status}, poly{h->m, h->m, h->m, c.batch, 1, h->dev_status},
+      full{h->m, h->n, h->m, c.batch, 0, h->dev_status};
+  int cur = 0;
+  for (uint32_t s = 0; s < c.steps && e == cudaSuccess; ++s, cur ^= 1) {
+    e = launch_f16<false>(h->bn_gram, h->x_rows[cur], h->x_cols_gram[cur], gram, EpiGram{h->a}, st);
+    if (e == cudaSuccess) e = launch_f16<false>(h->bn_poly, h->a_rows, h->a_cols, poly, EpiPoly{h->a, h->b, c.b, c.c}, st);
+    EpiX ex;
+    memset(&ex, 0, sizeof ex);
+    ex.hi = h->hi[cur];
+    ex.lo = h->lo[cur];
+    ex.diag = h->b.diag;
+    ex.stride = h->xs;
+    ex.diag_stride = h->ds;
+    ex.m = h->m;
+    ex.n = h->n;
+    ex.ld = h->ldx;
+    ex.a1 = c.a;
+    if (s + 1 < c.steps) {
+      ex.hi_out = h->hi[cur ^ 1];
+      ex.lo_out = h->lo[cur ^ 1];
+    } else {
+      ex.out = out;
+      ex.out_dtype = out_dtype;
+      ex.tall = c.rows > c.cols;
+      ex.x = x;
+      ex.x_stride = mo.stride;
+      ex.keep = 1.f - gamma * decay;
+      ex.rate = gamma * c.scale;
+      ex.vec = c.cols % 8 == 0 && (op & 15u) == 0 && (xp & 15u) == 0 && mo.stride % 4 == 0;
+    }
+    if (e == cudaSuccess) e = launch_f16<true>(h->bn_x, h->b_rows, h->x_across[cur], full, ex, st);
+  }
+  return e == cudaSuccess ? DS_OK : cuda_fail(e, "orthogonalised update");
+}
+
+int ds_orth_destroy(ds_orth_handle h) {
+  if (!h) return DS_ERR_INVALID_ARG;
+  delete h;
+  return DS_OK;
+}
+
+}  // extern "C"
