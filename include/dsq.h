@@ -383,7 +383,8 @@ typedef enum { DS_F32 = 0, DS_BF16 = 1, DS_F16 = 2 } ds_dtype;
  *   done from left to right in 32 bits.  bias may be NULL.  out [m, n], `ldo` elements between rows, of type out_dtype.  k <= DS_I8_MAX_K, else DS_ERR_UNSUPPORTED.
  *   k = 0 gives the bias.
  * ds_i8_linear:  the two together for a linear layer whose weights w [n, k] were quantised before (rows = output
- *   channels): x [rows, k] is quantised by rows into the workspace (ds_i8_linear_workspace bytes, 16-byte aligned).
+ *   channels): x [rows, k] is quantised by rows into the workspace (ds_i8_linear_workspace bytes, 16-byte aligned;
+ *   none where that is 0: a few short rows, which are one launch).
  * Training takes the same calls: forward  a = rows of x, b = rows of W;  gradient of inputs  a = rows of dY, b = columns
  *   of W (qt);  gradient of weights  a = columns of dY, b = columns of x.
  */
@@ -394,7 +395,7 @@ int ds_i8_quantize(const void* x, int dtype, uint64_t rows, uint64_t cols, uint6
                    void* cuda_stream);
 int ds_i8_matmul(const int8_t* a, uint64_t lda, const float* sa, const int8_t* b, uint64_t ldb, const float* sb, const float* bias,
                  uint64_t m, uint64_t n, uint64_t k, void* out, int out_dtype, uint64_t ldo, uint32_t* dev_status, void* cuda_stream);
-uint64_t ds_i8_linear_workspace(uint64_t rows, uint64_t k);
+uint64_t ds_i8_linear_workspace(uint64_t rows, uint64_t k, uint64_t n);
 int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t ldx, const int8_t* w, uint64_t ldw, const float* sw,
                  const float* bias, uint64_t n, void* out, int out_dtype, uint64_t ldo, void* workspace, size_t workspace_bytes,
                  uint32_t* dev_status, void* cuda_stream);

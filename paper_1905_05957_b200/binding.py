@@ -6,6 +6,7 @@ library's kernels.  There is no CPU fallback: a missing library or device raises
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 
 import torch
@@ -103,7 +104,7 @@ def load_library() -> C.CDLL:
     L.ds_i8_quantize_workspace.argtypes = [u64, u64, C.c_int]
     L.ds_i8_quantize.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, vp, vp, u64, vp, vp, vp, size, vp]
     L.ds_i8_matmul.argtypes = [vp, u64, vp, vp, u64, vp, vp, u64, u64, u64, vp, C.c_int, u64, vp, vp]
-    L.ds_i8_linear_workspace.argtypes = [u64, u64]
+    L.ds_i8_linear_workspace.argtypes = [u64, u64, u64]
     L.ds_i8_linear.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, vp, vp, u64, vp, C.c_int, u64, vp, size, vp, vp]
     L.ds_orth_create.argtypes = [C.POINTER(ds_orth_config), vp, C.POINTER(size), vp, C.POINTER(vp)]
     L.ds_orth_update.argtypes = [vp, vp, C.c_int, vp, vp, C.c_int, vp, C.c_float, C.c_float, vp]
@@ -115,6 +116,26 @@ def load_library() -> C.CDLL:
     L.ds_kernel_launches.restype = C.c_uint64
     _lib = L
     return L
+
+
+_call = None
+
+
+def fast_call():
+    """(call, addresses): call(addresses[name], *integers) calls a function of the ABI whose arguments are all pointers or
+    integers, without ctypes (csrc/dsq_call.c)."""
+    global _call
+    if _call is None:
+        lib = load_library()
+        path = os.path.join(_HERE, "csrc", "dsq_call.so")
+        spec = importlib.util.spec_from_file_location("dsq_call", path)
+        if not os.path.exists(path) or spec is None:
+            raise RuntimeError(f"{path} is missing: run `python -m paper_1905_05957_b200.build`")
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _call = module.call, {name: C.cast(getattr(lib, name), C.c_void_p).value
+                              for name in ("ds_i8_quantize", "ds_i8_matmul", "ds_i8_linear")}
+    return _call
 
 
 def _qspec(q: Q) -> ds_qspec:

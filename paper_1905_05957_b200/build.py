@@ -4,16 +4,19 @@ Every translation unit is compiled to an object file on its own (side by side), 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(CSRC, "build")
 LIB = os.path.join(CSRC, "libdsq.so")
+CALL_SRC = os.path.join(CSRC, "dsq_call.c")
+CALL_LIB = os.path.join(CSRC, "dsq_call.so")      # the Python extension through which the short calls go
 SOURCES = ["dsq_api.cu", "dsq_chunked.cu", "dsq_chunked_sign.cu", "dsq_chunked_sign_l2.cu", "dsq_chunked_qsgd.cu", "dsq_chunked_qsgd_window.cu",
            "dsq_elementwise.cu", "dsq_topk.cu", "dsq_static.cu", "dsq_whole.cu",
-           "dsq_mma.cu", "dsq_orth.cu", "dsq_int8.cu"]
-HEADERS = ["dsq_common.cuh", "dsq_chunked.cuh", "dsq_mma.cuh", "dsq_internal.h", os.path.join("..", "..", "include", "dsq.h")]
+           "dsq_mma.cu", "dsq_orth.cu", "dsq_orth_small.cu", "dsq_int8.cu"]
+HEADERS = ["dsq_common.cuh", "dsq_chunked.cuh", "dsq_mma.cuh", "dsq_orth.cuh", "dsq_internal.h", os.path.join("..", "..", "include", "dsq.h")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -23,7 +26,7 @@ NVCC_FLAGS = [
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALL_LIB) or os.path.getmtime(CALL_SRC) > os.path.getmtime(CALL_LIB):
         return True
     t = os.path.getmtime(LIB)
     return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
@@ -45,6 +48,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
         objs = list(pool.map(compile_one, SOURCES))
     subprocess.run([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", LIB + ".tmp"] + objs, check=True)
     os.replace(LIB + ".tmp", LIB)
+    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], CALL_SRC, "-o",
+                    CALL_LIB + ".tmp"], check=True)
+    os.replace(CALL_LIB + ".tmp", CALL_LIB)
     return LIB
 
 

@@ -10,6 +10,7 @@
 #include <cuda_fp16.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "dsq_mma.cuh"
 
@@ -274,6 +275,20 @@ __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float
 __device__ __forceinline__ void store1(__half* p, float v) { *p = __float2half_rn(v); }
 
 template <class T>
+__device__ __forceinline__ void pack4f(uint32_t* w, float a, float b, float c, float d) {
+  if constexpr (sizeof(T) == 4) {
+    w[0] = __float_as_uint(a), w[1] = __float_as_uint(b), w[2] = __float_as_uint(c), w[3] = __float_as_uint(d);
+  } else if constexpr (std::is_same<T, __half>::value) {
+    const __half2 x = __floats2half2_rn(a, b), y = __floats2half2_rn(c, d);
+    w[0] = *reinterpret_cast<const uint32_t*>(&x), w[1] = *reinterpret_cast<const uint32_t*>(&y);
+  } else {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b), y = __floats2bfloat162_rn(c, d);
+    w[0] = *reinterpret_cast<const uint32_t*>(&x), w[1] = *reinterpret_cast<const uint32_t*>(&y);
+  }
+}
+
+// Rows of out start on 32-byte boundaries, sb and bias on 16.
+template <class T>
 struct EpiScale {
   struct Pre {
     float s;
@@ -282,26 +297,26 @@ struct EpiScale {
   T* out;
   uint64_t ld;
   uint32_t m, n;
-  int vec;   // rows of out, sb and bias start on 16-byte boundaries
   __device__ __forceinline__ Pre load(uint32_t row, uint32_t, uint32_t) const { return {row < m ? __ldg(sa + row) : 0.f}; }
   __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t) const {
     if (row >= m) return;
     T* o = out + row * ld + col0;
-    if (vec && col0 + 32 <= n) {
+    if (col0 + 32 <= n) {
 #pragma unroll
-      for (int i = 0; i < 32; i += 16 / sizeof(T)) {
-        T t[16 / sizeof(T)];
+      for (int i = 0; i < 32; i += 32 / sizeof(T)) {
+        uint32_t piece[8];
 #pragma unroll
-        for (int j = 0; j < 16 / (int)sizeof(T); j += 4) {
+        for (int j = 0; j < 32 / (int)sizeof(T); j += 4) {
           const float4 s = __ldg(reinterpret_cast<const float4*>(sb + col0 + i + j));
           float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
           if (bias) c = __ldg(reinterpret_cast<const float4*>(bias + col0 + i + j));
-          store1(t + j, __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j], p.s), s.x), c.x));
-          store1(t + j + 1, __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j + 1], p.s), s.y), c.y));
-          store1(t + j + 2, __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j + 2], p.s), s.z), c.z));
-          store1(t + j + 3, __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j + 3], p.s), s.w), c.w));
+          const float v0 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j], p.s), s.x), c.x);
+          const float v1 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j + 1], p.s), s.y), c.y);
+          const float v2 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j + 2], p.s), s.z), c.z);
+          const float v3 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j + 3], p.s), s.w), c.w);
+          pack4f<T>(piece + j * sizeof(T) / 4, v0, v1, v2, v3);
         }
-        *reinterpret_cast<uint4*>(o + i) = *reinterpret_cast<uint4*>(t);
+        st_b32(o + i, piece);
       }
     } else {
 #pragma unroll
@@ -312,6 +327,29 @@ struct EpiScale {
   }
 };
 
+// The same with the operands' places exchanged: rows of the product are output channels, its columns tokens.  Lanes hold
+// consecutive channels, so a token's outputs leave as 64 or 128 consecutive bytes.
+template <class T>
+struct EpiScaleTurned {
+  struct Pre {
+    float s, c;
+  };
+  const float *sa, *sb, *bias;   // of tokens, of channels
+  T* out;
+  uint64_t ld;
+  uint32_t m, n;                 // channels, tokens
+  __device__ __forceinline__ Pre load(uint32_t row, uint32_t, uint32_t) const {
+    return row < m ? Pre{__ldg(sb + row), bias ? __ldg(bias + row) : 0.f} : Pre{0.f, 0.f};
+  }
+  __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t) const {
+    if (row >= m) return;
+    T* o = out + col0 * ld + row;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (col0 + j < n) store1(o + j * ld, __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[j], __ldg(sa + col0 + j)), p.s), p.c));
+  }
+};
+
 // An empty sum (K = 0): the bias alone.
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_i8_empty(T* out, uint64_t ld, uint32_t n, const float* bias) {
@@ -319,11 +357,257 @@ __global__ void __launch_bounds__(kThreads) k_i8_empty(T* out, uint64_t ld, uint
   for (uint32_t c = threadIdx.x; c < n; c += kThreads) store1(out + blockIdx.x * ld + c, bias ? bias[c] : 0.f);
 }
 
+// ---- few tokens ----
+// The weights' bytes are all that counts.  A CTA takes 16 or 32 rows of W; each of its eight warps has an eighth of K, which it
+// reads in chunks of 64 codes a row, four chunks ahead, straight into the registers of m16n8k32 instructions (tokens are the 8
+// columns; the warp instruction is enough, the loop waits for memory).  A sum of whole numbers may be taken in any order, so
+// k is dealt to the instructions' places as it arrives: lane t of a group of four loads 16 consecutive codes of its rows and
+// tokens and feeds them as two instructions' worth.  The warps' sums meet in shared memory.
+//
+// Short inputs of up to 8 tokens are quantised within, by every CTA for itself, under the first loads of W (x stays in L2): a
+// decode step is then one launch.  Above kFewCodes codes of W a launch of TMA-fed tiles is faster than this one.
+constexpr uint32_t kFewFusedEntries = 16384;   // entries of x up to which it is quantised within
+constexpr uint32_t kFewMost = 16;              // tokens
+constexpr uint64_t kFewCodes = 48u << 20;
+
+struct FewParams {
+  const void* x;          // tokens: values of type T, or codes
+  uint64_t ldx;
+  const float* sx;        // scales of the tokens (codes only)
+  const int8_t* w;
+  uint64_t ldw;
+  const float *sw, *bias;
+  void* out;
+  uint64_t ldo;
+  uint32_t m, n, k;
+  int vec;                // rows of x start on 16-byte boundaries
+};
+
+// 16 codes from k0 on; behind the end of a row nothing is read and zeros stand.  (The end is rare: kept small, since the
+// loops' length in instructions counts where a warp lives for a few microseconds.)
+__device__ __forceinline__ uint4 load_codes16(const int8_t* row, uint32_t k0, uint32_t k) {
+  if (k0 + 16 <= k) return __ldg(reinterpret_cast<const uint4*>(row + k0));
+  unsigned long long v[2] = {0, 0};
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll 1
+    for (uint32_t i = k0 + 8 * h; i < k && i < k0 + 8 * h + 8; ++i) v[h] |= (unsigned long long)(uint8_t)row[i] << (8 * (i & 7));
+  return make_uint4((uint32_t)v[0], (uint32_t)(v[0] >> 32), (uint32_t)v[1], (uint32_t)(v[1] >> 32));
+}
+
+__device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 16 values of one token from k0 on, as codes.
+template <class T>
+__device__ __forceinline__ uint4 encode16(const T* row, uint32_t k0, uint32_t k, float inv, int vec) {
+  if (vec && k0 + 16 <= k) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 16 / Vec<T>::kN; ++i) {
+      Vec<T> v;
+      v.raw = __ldg(reinterpret_cast<const uint4*>(row + k0) + i);
+#pragma unroll
+      for (int j = 0; j < Vec<T>::kN / 4; ++j)
+        w[i * (Vec<T>::kN / 4) + j] =
+            pack4(code_of(v.at(4 * j), inv), code_of(v.at(4 * j + 1), inv), code_of(v.at(4 * j + 2), inv), code_of(v.at(4 * j + 3), inv));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  unsigned long long v[2] = {0, 0};
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll 1
+    for (uint32_t i = k0 + 8 * h; i < k && i < k0 + 8 * h + 8; ++i)
+      v[h] |= (unsigned long long)(uint8_t)code_of(to_f32(row[i]), inv) << (8 * (i & 7));
+  return make_uint4((uint32_t)v[0], (uint32_t)(v[0] >> 32), (uint32_t)v[1], (uint32_t)(v[1] >> 32));
+}
+
+// Bytes between tokens in shared memory: whole chunks, and an odd number of 64 bytes, which spreads a quarter warp's 16-byte
+// reads (two tokens, 64 bytes of each) over all banks.
+__host__ __device__ inline uint32_t few_pitch(uint32_t k) {
+  const uint32_t c = (k + 63) / 64;
+  return 64 * (c | 1);
+}
+
+// X: type of x (int8_t: codes), O: type of out, NT: groups of 8 tokens, RB: blocks of 16 rows of W.
+template <class X, class O, int NT, int RB>
+__global__ void __launch_bounds__(256, 2) k_i8_few(const FewParams p) {
+  constexpr bool kCodes = sizeof(X) == 1;
+  constexpr int kAhead = 4;
+  extern __shared__ __align__(16) uint8_t xs[];     // the codes of tokens that are quantised here
+  __shared__ int part[8][RB * 16][NT * 8 + 1];
+  __shared__ uint32_t tops[8];
+  __shared__ float scale[NT * 8], inverse[8];
+  pdl_prologue();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t row0 = blockIdx.x * (16 * RB);
+  const uint32_t chunks = p.k / 64, per = (chunks + 7) / 8, pitch = few_pitch(p.k);
+  const uint32_t first = warp * per, end = min(first + per, chunks);
+  const int8_t *wrow[2 * RB], *xrow[NT];            // rows and tokens past the end: one that is there, not stored
+#pragma unroll
+  for (int i = 0; i < 2 * RB; ++i) wrow[i] = p.w + (uint64_t)min(row0 + g + 8 * i, p.n - 1) * p.ldw;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const uint32_t token = min(8u * j + g, p.m - 1);
+    xrow[j] = kCodes ? static_cast<const int8_t*>(p.x) + token * p.ldx : reinterpret_cast<const int8_t*>(xs) + token * pitch;
+  }
+  // whole chunks in a loop without a branch but its own; the rest of K, if any, is the last warp's
+  uint4 w[kAhead][2 * RB], xc[kAhead][NT];
+  auto fetch = [&](uint32_t c, uint4 (&to)[2 * RB], uint4 (&xt)[NT]) {
+    if (c >= end) return;
+    const uint32_t k0 = c * 64 + t * 16;
+#pragma unroll
+    for (int i = 0; i < 2 * RB; ++i) to[i] = __ldg(reinterpret_cast<const uint4*>(wrow[i] + k0));
+    if constexpr (kCodes) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) xt[j] = __ldg(reinterpret_cast<const uint4*>(xrow[j] + k0));
+    }
+  };
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a) fetch(first + a, w[a], xc[a]);
+
+  if constexpr (!kCodes) {
+    // scales: 8 / 2^ceil(log2 m) warps to a token
+    const int shift = p.m <= 1 ? 3 : p.m <= 2 ? 2 : p.m <= 4 ? 1 : 0;
+    const uint32_t token = warp >> shift, share = warp & ((1 << shift) - 1), lanes = 32u << shift;
+    uint32_t top = 0;
+    if (token < p.m) {
+      const X* row = static_cast<const X*>(p.x) + token * p.ldx;
+      const uint32_t at = share * 32 + lane;
+      constexpr int N = Vec<X>::kN;
+      const uint32_t nv = p.vec ? p.k / N : 0;
+#pragma unroll 4
+      for (uint32_t v = at; v < nv; v += lanes) {
+        Vec<X> r;
+        r.raw = __ldg(reinterpret_cast<const uint4*>(row) + v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) top = max(top, mag_bits(r.at(i)));
+      }
+#pragma unroll 1
+      for (uint32_t k = nv * N + at; k < p.k; k += lanes) top = max(top, mag_bits(to_f32(row[k])));
+    }
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    if (lane == 0) tops[warp] = top;
+    __syncthreads();
+    if (threadIdx.x < 8) {
+      const uint32_t tok = threadIdx.x;
+      uint32_t m = 0;
+      for (uint32_t i = 0; i < (1u << shift); ++i)
+        if ((tok << shift) + i < 8) m = max(m, tops[(tok << shift) + i]);
+      float s, v;
+      scale_of(m, s, v);
+      scale[tok] = s;
+      inverse[tok] = v;
+    }
+    __syncthreads();
+    const uint32_t pieces = (p.k + 15) / 16;
+    for (uint32_t i = threadIdx.x; i < p.m * pieces; i += 256) {
+      const uint32_t tok = i / pieces, k0 = (i - tok * pieces) * 16;
+      *reinterpret_cast<uint4*>(xs + tok * pitch + k0) =
+          encode16(static_cast<const X*>(p.x) + tok * p.ldx, k0, p.k, inverse[tok], p.vec);
+    }
+    __syncthreads();
+  } else {
+    if (threadIdx.x < NT * 8) scale[threadIdx.x] = threadIdx.x < p.m ? p.sx[threadIdx.x] : 0.f;
+  }
+
+  int acc[RB][NT][4];
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[r][j][i] = 0;
+  auto multiply = [&](const uint4 (&wc)[2 * RB], const uint4 (&x)[NT]) {
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      const uint4 lo = wc[2 * r], hi = wc[2 * r + 1];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        mma_s8(acc[r][j], lo.x, hi.x, lo.y, hi.y, x[j].x, x[j].y);
+        mma_s8(acc[r][j], lo.z, hi.z, lo.w, hi.w, x[j].z, x[j].w);
+      }
+    }
+  };
+  for (uint32_t c0 = first; c0 < end; c0 += kAhead) {
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const uint32_t c = c0 + a;
+      if (c >= end) break;
+      if constexpr (!kCodes) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) xc[a][j] = *reinterpret_cast<const uint4*>(xrow[j] + c * 64 + t * 16);
+      }
+      multiply(w[a], xc[a]);
+      fetch(c + kAhead, w[a], xc[a]);
+    }
+  }
+  if (warp == 7 && (p.k & 63)) {
+    const uint32_t k0 = chunks * 64 + t * 16;
+    uint4 we[2 * RB], xe[NT];
+#pragma unroll
+    for (int i = 0; i < 2 * RB; ++i) we[i] = load_codes16(wrow[i], k0, p.k);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      if constexpr (kCodes)
+        xe[j] = load_codes16(xrow[j], k0, p.k);
+      else
+        xe[j] = k0 < p.k ? *reinterpret_cast<const uint4*>(xrow[j] + k0) : make_uint4(0, 0, 0, 0);
+    }
+    multiply(we, xe);
+  }
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) part[warp][16 * r + g + 8 * (i >> 1)][8 * j + 2 * t + (i & 1)] = acc[r][j][i];
+  __syncthreads();
+  for (uint32_t o = threadIdx.x; o < RB * 16 * p.m; o += 256) {
+    const uint32_t token = o / (RB * 16), r = o % (RB * 16), row = row0 + r;
+    int s = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s += part[q][r][token];
+    if (row < p.n)
+      store1(static_cast<O*>(p.out) + token * p.ldo + row,
+             __fadd_rn(__fmul_rn(__fmul_rn((float)s, scale[token]), __ldg(p.sw + row)), p.bias ? __ldg(p.bias + row) : 0.f));
+  }
+}
+
+template <class X, class O, int NT>
+cudaError_t launch_few(const FewParams& p, cudaStream_t st) {
+  // 32 rows a CTA halve what the tokens' codes cost; where that leaves SMs without a CTA, 16
+  const size_t smem = sizeof(X) > 1 ? (size_t)p.m * few_pitch(p.k) : 0;
+  if ((p.n + 31) / 32 >= 2 * (uint32_t)sm_count())
+    launch_pdl_dyn(k_i8_few<X, O, NT, 2>, dim3((p.n + 31) / 32), dim3(256), smem, st, p);
+  else
+    launch_pdl_dyn(k_i8_few<X, O, NT, 1>, dim3((p.n + 15) / 16), dim3(256), smem, st, p);
+  count_launches(1);
+  return cudaGetLastError();
+}
+template <class X>
+cudaError_t launch_few_fused(const FewParams& p, int out_dtype, cudaStream_t st) {
+  return out_dtype == DS_F32 ? launch_few<X, float, 1>(p, st) : out_dtype == DS_BF16 ? launch_few<X, __nv_bfloat16, 1>(p, st) : launch_few<X, __half, 1>(p, st);
+}
+inline bool few_fused(uint64_t rows, uint64_t n, uint64_t k) { return rows <= 8 && rows * k <= kFewFusedEntries && n * k <= kFewCodes; }
+
 inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 inline bool aligned(const void* p, uint64_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 inline uint32_t size_of(int dtype) { return dtype == DS_F32 ? 4 : 2; }
 inline bool dtype_ok(int t) { return t == DS_F32 || t == DS_BF16 || t == DS_F16; }
 constexpr uint64_t kMaxLen = 1ull << 30;
+constexpr uint32_t kTurnedMost = 64;
+
+// CTAs that share a tile's K, for few tokens: as many as run at once with at least four steps each.
+inline uint32_t few_parts(uint32_t tiles, uint32_t k) {
+  uint32_t p = 1;
+  while (p < 8 && tiles <= (uint32_t)cluster_count(2 * p) && (k + 127) / 128 >= 8 * p) p *= 2;
+  return p;
+}
 
 template <class T>
 cudaError_t product(const int8_t* a, uint64_t lda, const float* sa, const int8_t* b, uint64_t ldb, const float* sb, const float* bias,
@@ -333,20 +617,40 @@ cudaError_t product(const int8_t* a, uint64_t lda, const float* sa, const int8_t
     count_launches(1);
     return cudaGetLastError();
   }
-  const MmaShape s{m, n, k, 1, 0, dev_status};
-  const EpiScale<T> epi{sa, sb, bias, out, ldo, m, n,
-                        aligned(out, 16) && ldo * sizeof(T) % 16 == 0 && aligned(sb, 16) && (!bias || aligned(bias, 16))};
-  const int bn = pick_bn(s, sm_count());
+  if (m <= kFewMost && (uint64_t)n * k <= kFewCodes) {
+    const FewParams p{a, lda, sa, b, ldb, sb, bias, out, ldo, m, n, k, 1};
+    return m <= 8 ? launch_few<int8_t, T, 1>(p, st) : launch_few<int8_t, T, 2>(p, st);
+  }
+  // Turned: tiles of 128 output channels by so many tokens.  For few tokens, so that shared memory fills with weights and not
+  // with rows that are not there; and where rows of out are on no boundary, since lanes then hold consecutive entries.
+  const bool vec = aligned(out, 32) && ldo * sizeof(T) % 32 == 0 && aligned(sb, 16) && (!bias || aligned(bias, 16));
+  if (m <= kTurnedMost || !vec) {
+    const MmaShape s{n, m, k, 1, 1, 0, dev_status};
+    const EpiScaleTurned<T> epi{sa, sb, bias, out, ldo, n, m};
+    const bool narrow = m <= 32;
+    MmaPlan plan = plan_mma(s);
+    if (narrow) {
+      plan.pair = false;
+      plan.bn = 32;
+      const TileWalk w(s, 32);
+      plan.parts = few_parts(w.total, k);
+    }
+    CUtensorMap mw, mx;
+    cudaError_t e = make_tensor_map(&mw, kMmaI8, b, k, n, 1, ldb, ldb * n, 128, kMmaRows);
+    if (e == cudaSuccess) e = make_tensor_map(&mx, kMmaI8, a, k, m, 1, lda, lda * m, 128, plan.box_rows());
+    if (e != cudaSuccess) return e;
+    if (!narrow) return launch_mma<kMmaI8, false>(plan, mw, mx, s, epi, st);
+    return plan.parts > 1 ? launch_mma_split<kMmaI8, 32, false>(plan.parts, mw, mx, s, epi, st)
+                          : launch_mma_bn<kMmaI8, 32, false>(mw, mx, s, epi, st);
+  }
+  const MmaShape s{m, n, k, 1, 1, 0, dev_status};
+  const EpiScale<T> epi{sa, sb, bias, out, ldo, m, n};
+  const MmaPlan plan = plan_mma(s);
   CUtensorMap ma, mb;
   cudaError_t e = make_tensor_map(&ma, kMmaI8, a, k, m, 1, lda, lda * m, 128, kMmaRows);
-  if (e == cudaSuccess) e = make_tensor_map(&mb, kMmaI8, b, k, n, 1, ldb, ldb * n, 128, bn);
+  if (e == cudaSuccess) e = make_tensor_map(&mb, kMmaI8, b, k, n, 1, ldb, ldb * n, 128, plan.box_rows());
   if (e != cudaSuccess) return e;
-  switch (bn) {
-    case 256: return launch_mma_bn<kMmaI8, 256, false>(ma, mb, s, epi, st);
-    case 192: return launch_mma_bn<kMmaI8, 192, false>(ma, mb, s, epi, st);
-    case 128: return launch_mma_bn<kMmaI8, 128, false>(ma, mb, s, epi, st);
-    default: return launch_mma_bn<kMmaI8, 64, false>(ma, mb, s, epi, st);
-  }
+  return launch_mma<kMmaI8, false>(plan, ma, mb, s, epi, st);
 }
 
 template <class T>
@@ -451,16 +755,34 @@ int ds_i8_matmul(const int8_t* a, uint64_t lda, const float* sa, const int8_t* b
   return e == cudaSuccess ? DS_OK : cuda_fail(e, "8-bit product");
 }
 
-uint64_t ds_i8_linear_workspace(uint64_t rows, uint64_t k) { return rows * round_up(k, 16) + 4 * round_up(rows, 64); }
+uint64_t ds_i8_linear_workspace(uint64_t rows, uint64_t k, uint64_t n) {
+  return few_fused(rows, n, k) ? 0 : rows * round_up(k, 16) + 4 * round_up(rows, 64);
+}
 
 int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t ldx, const int8_t* w, uint64_t ldw, const float* sw,
                  const float* bias, uint64_t n, void* out, int out_dtype, uint64_t ldo, void* workspace, size_t workspace_bytes,
                  uint32_t* dev_status, void* cuda_stream) {
   if (rows > kMaxLen || k > DS_I8_MAX_K) return rows > kMaxLen ? DS_ERR_INVALID_ARG : DS_ERR_UNSUPPORTED;
   if (rows == 0 || n == 0) return dtype_ok(dtype) && dtype_ok(out_dtype) ? DS_OK : DS_ERR_INVALID_ARG;
+  if (k == 0)
+    return dtype_ok(dtype) ? ds_i8_matmul(nullptr, 0, sw, nullptr, 0, sw, bias, rows, n, 0, out, out_dtype, ldo, dev_status, cuda_stream)
+                           : DS_ERR_INVALID_ARG;
+  if (few_fused(rows, n, k)) {
+    if (!dtype_ok(dtype) || !dtype_ok(out_dtype) || n > kMaxLen || ldx < k || ldo < n || !x || !sw || !out) return DS_ERR_INVALID_ARG;
+    const int rc = check_codes(w, ldw, k);
+    if (rc != DS_OK) return rc;
+    if (!aligned(x, size_of(dtype)) || !aligned(sw, 4) || !aligned(bias, 4) || !aligned(out, size_of(out_dtype))) return DS_ERR_ALIGN;
+    const FewParams p{x, ldx, nullptr, w, ldw, sw, bias, out, ldo, (uint32_t)rows, (uint32_t)n, (uint32_t)k,
+                      aligned(x, 16) && ldx * size_of(dtype) % 16 == 0};
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = dtype == DS_F32    ? launch_few_fused<float>(p, out_dtype, st)
+                          : dtype == DS_BF16 ? launch_few_fused<__nv_bfloat16>(p, out_dtype, st)
+                                             : launch_few_fused<__half>(p, out_dtype, st);
+    return e == cudaSuccess ? DS_OK : cuda_fail(e, "8-bit product");
+  }
   if (!workspace) return DS_ERR_INVALID_ARG;
   if (!aligned(workspace, 16)) return DS_ERR_ALIGN;
-  if (workspace_bytes < ds_i8_linear_workspace(rows, k)) return DS_ERR_BUFFER_TOO_SMALL;
+  if (workspace_bytes < ds_i8_linear_workspace(rows, k, n)) return DS_ERR_BUFFER_TOO_SMALL;
   const uint64_t ldq = round_up(k, 16);
   float* s = static_cast<float*>(workspace);
   int8_t* q = static_cast<int8_t*>(workspace) + 4 * round_up(rows, 64);

@@ -35,6 +35,37 @@ int sm_count() {
   return n;
 }
 
+namespace {
+__global__ void __launch_bounds__(kMmaThreads, 1) k_cluster_probe() {}   // never launched: asked about
+}
+
+int cluster_count(uint32_t size) {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<int> known[kMaxDevices][9];
+  int dev = 0, n = 0;
+  if (size < 2 || size > 8 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+  n = known[dev][size].load(std::memory_order_relaxed);
+  if (!n) {
+    (void)cudaFuncSetAttribute(k_cluster_probe, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPairSmem);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(size * (sm_count() / size));
+    cfg.blockDim = dim3(kMmaThreads);
+    cfg.dynamicSmemBytes = kPairSmem;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = size;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, k_cluster_probe, &cfg) != cudaSuccess || n < 1) {
+      (void)cudaGetLastError();
+      n = sm_count() / (int)size;
+    }
+    known[dev][size].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
 cudaError_t make_tensor_map(CUtensorMap* map, int kind, const void* base, uint64_t cols, uint64_t rows, uint64_t batch, uint64_t ld,
                             uint64_t batch_stride, uint32_t box_cols, uint32_t box_rows) {
   const EncodeFn fn = encoder();

@@ -48,16 +48,16 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Waits until the phase of the given parity has completed.  False: another role gave up, or the limit ran out (which
+// Waits until the phase of the given parity has completed (a whole warp together).  False: another role gave up, or the limit ran out (which
 // makes the others give up too).
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-  if (mbar_try(bar, parity)) return true;
+  if (__all_sync(0xFFFFFFFFu, mbar_try(bar, parity))) return true;
   const long long t0 = clock64();
   while (true) {
     for (int i = 0; i < 16; ++i)
-      if (mbar_try(bar, parity)) return true;
-    if (*gave_up) return false;
-    if (clock64() - t0 > kWaitCycles) {
+      if (__all_sync(0xFFFFFFFFu, mbar_try(bar, parity))) return true;
+    if (__any_sync(0xFFFFFFFFu, *gave_up != 0)) return false;
+    if (__any_sync(0xFFFFFFFFu, clock64() - t0 > kWaitCycles)) {
       *gave_up = 1;
       return false;
     }
@@ -110,7 +110,28 @@ __device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t addr) {
         "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
 }
+// 32 bytes at once (a whole sector: a row's piece written 16 bytes at a time costs twice the transactions), 32-byte aligned.
+__device__ __forceinline__ void ld_b32(uint32_t* w, const void* p) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(p)
+               : "memory");
+}
+__device__ __forceinline__ void st_b32(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+               "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// One lane of a converged warp.  The loops around TMA and matrix instructions are run by whole warps, whose loop values the
+// compiler can then keep in the uniform registers that these instructions take, and only their issue by one lane: run by a
+// single lane altogether, a step of K cost 520 cycles whatever the tile's width.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+  return ok != 0;
+}
 
 // Shared-memory descriptor of an operand tile whose rows are 128 bytes, swizzled by 128 bytes (atoms of 8 rows, 1024
 // bytes).  Laid out along K: `stride` = bytes between groups of eight rows.  Laid out across K: `stride` = bytes between
@@ -131,6 +152,7 @@ __host__ __device__ constexpr uint32_t mma_idesc() {
 struct MmaShape {
   uint32_t m, n, k;        // C is [m, n] per matrix of the batch
   uint32_t batch;
+  uint32_t elem;           // bytes of an operand's element
   uint32_t sym;            // 1: C is symmetric; only 32 x 32 blocks on or above the diagonal are handed to the epilogue
   uint32_t* dev_status;
 };
@@ -138,7 +160,7 @@ struct MmaShape {
 template <int BN>
 struct MmaTile {
   static constexpr int kStageBytes = (kMmaRows + BN) * 128;
-  static constexpr int kStages = BN == 256 ? 4 : BN == 192 ? 5 : BN == 128 ? 6 : 8;
+  static constexpr int kStages = BN == 256 ? 4 : BN == 192 ? 5 : BN == 128 ? 6 : BN == 64 ? 8 : 10;
   static constexpr int kTmemCols = BN == 192 ? 512 : 2 * BN;
   static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024;
 };
@@ -196,7 +218,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t ring = (smem_u32(dyn) + 1023u) & ~1023u;
   const uint32_t full = smem_u32(bars), empty = full + 8 * T::kStages, tfull = empty + 8 * T::kStages, tempty = tfull + 16,
                  drain = tempty + 16;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     tma_prefetch_map(&map_a);
@@ -218,7 +240,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_slot, 0);
   // Only now may the next kernel's CTAs come in: one that took this SM's tensor memory before this CTA had its share would
   // wait for this kernel while this kernel waits for it.
   asm volatile("griddepcontrol.launch_dependents;");
@@ -227,7 +249,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const TileWalk walk(shape, BN);
   const uint32_t nk = (shape.k + kBK - 1) / kBK;
 
-  if (warp == 0 && lane == 0) {
+  if (warp == 0) {
+    const bool one = elect_one();
     asm volatile("fence.proxy.async.global;" ::: "memory");
     uint32_t stage = 0, phase = 0, issued = 0;
     bool ok = true;
@@ -237,15 +260,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       for (uint32_t kb = 0; kb < nk; ++kb) {
         if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, &gave_up))) break;
         const uint32_t dst = ring + stage * T::kStageBytes;
-        mbar_expect_tx(full + 8 * stage, T::kStageBytes);
-        tma_load_3d(dst, &map_a, (int)(kb * kBK), (int)(i * kMmaRows), (int)b, full + 8 * stage);
-        if constexpr (B_ACROSS) {
+        if (one) {
+          mbar_expect_tx(full + 8 * stage, T::kStageBytes);
+          tma_load_3d(dst, &map_a, (int)(kb * kBK), (int)(i * kMmaRows), (int)b, full + 8 * stage);
+          if constexpr (B_ACROSS) {
 #pragma unroll
-          for (int c = 0; c < BN / 64; ++c)
-            tma_load_3d(dst + kMmaRows * 128 + c * (kBK * 128), &map_b, (int)(j * BN + c * 64), (int)(kb * kBK), (int)b, full + 8 * stage);
-        } else {
-          tma_load_3d(dst + kMmaRows * 128, &map_b, (int)(kb * kBK), (int)(j * BN), (int)b, full + 8 * stage);
+            for (int c = 0; c < BN / 64; ++c)
+              tma_load_3d(dst + kMmaRows * 128 + c * (kBK * 128), &map_b, (int)(j * BN + c * 64), (int)(kb * kBK), (int)b, full + 8 * stage);
+          } else {
+            tma_load_3d(dst + kMmaRows * 128, &map_b, (int)(kb * kBK), (int)(j * BN), (int)b, full + 8 * stage);
+          }
         }
+        __syncwarp();
         ++issued;
         if (++stage == T::kStages) {
           stage = 0;
@@ -263,7 +289,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         }
       }
     }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1) {
+    const bool one = elect_one();
     constexpr uint32_t idesc = mma_idesc<KIND, BN, B_ACROSS>();
     uint32_t stage = 0, phase = 0, at = 0, aphase = 0;
     bool ok = true;
@@ -274,28 +301,32 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       for (uint32_t kb = 0; kb < nk; ++kb) {
         if (!(ok = mbar_wait(full + 8 * stage, phase, &gave_up))) break;
         tc_fence_after();
-        const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128;
+        if (one) {
+          const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {   // four instructions of 32 bytes of K
-          const uint64_t da = smem_desc(sa + 32 * q, 16, 1024);
-          const uint64_t db = B_ACROSS ? smem_desc(sb + 2048 * q, kBK * 128, 1024) : smem_desc(sb + 32 * q, 16, 1024);
-          tc_mma<KIND>(d, da, db, idesc, (kb | q) != 0);
+          for (int q = 0; q < 4; ++q) {   // four instructions of 32 bytes of K
+            const uint64_t da = smem_desc(sa + 32 * q, 16, 1024);
+            const uint64_t db = B_ACROSS ? smem_desc(sb + 2048 * q, kBK * 128, 1024) : smem_desc(sb + 32 * q, 16, 1024);
+            tc_mma<KIND>(d, da, db, idesc, (kb | q) != 0);
+          }
+          tc_commit(empty + 8 * stage);
         }
-        tc_commit(empty + 8 * stage);
+        __syncwarp();
         if (++stage == T::kStages) {
           stage = 0;
           phase ^= 1;
         }
       }
       if (!ok) break;
-      tc_commit(tfull + 8 * at);
+      if (one) tc_commit(tfull + 8 * at);
+      __syncwarp();
       if (++at == 2) {
         at = 0;
         aphase ^= 1;
       }
     }
     if (!ok) {   // products in flight must have ended before the tensor memory is freed
-      tc_commit(drain);
+      if (one) tc_commit(drain);
       const long long t0 = clock64();
       while (!mbar_try(drain, 0) && clock64() - t0 < kWaitCycles) {
       }
@@ -318,8 +349,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       while (c < kBlocks && !wanted(c)) c += 2;
       typename Epi::Pre pre{};
       if (c < kBlocks) pre = epi.load(row, c_first + 32 * c, b);
-      const bool ok = mbar_wait(tfull + 8 * at, aphase, &gave_up);
-      if (!__all_sync(0xFFFFFFFFu, ok)) break;
+      if (!mbar_wait(tfull + 8 * at, aphase, &gave_up)) break;
       tc_fence_after();
       while (c < kBlocks) {
         uint32_t acc[32];
@@ -354,6 +384,460 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   if (threadIdx.x == 0 && gave_up && shape.dev_status) atomicOr(shape.dev_status + DS_DEV_WORD_FLAGS, DS_DEV_MMA_TIMEOUT);
 }
 
+// ---- the same product by pairs of CTAs ----
+// Two CTAs of a cluster work on one 256 x 256 tile (cta_group::2): each fetches 128 rows of A and half of B's rows, each
+// tensor core reads both halves of B, and each CTA keeps the accumulator of its own 128 rows.  Per product that is two thirds of
+// the shared-memory and L2 traffic of a 128 x 256 tile of one CTA, which is what bounds large products (a 4096^3 product:
+// 118 us by single CTAs; the design doc has the table).  The first CTA of the pair issues all matrix instructions.
+//
+// An item of work is a tile or half of one (256 x 128): the tiles left over after whole rounds are halved where both halves
+// of all of them fit into one round.
+struct PairWalk {
+  uint32_t mt, nt, per, total, whole, items, sym;
+  __host__ __device__ PairWalk(const MmaShape& s, uint32_t pairs) : sym(s.sym) {
+    mt = (s.m + 255) / 256;
+    nt = (s.n + 255) / 256;
+    per = sym ? mt * (mt + 1) / 2 : mt * nt;
+    total = per * s.batch;
+    const uint32_t rest = total % pairs;
+    whole = 2 * rest <= pairs ? total - rest : total;
+    items = whole + 2 * (total - whole);
+  }
+  // item -> matrix b, first row of the tile, first column and width of the item
+  __host__ __device__ void at(uint32_t t, uint32_t& b, uint32_t& row, uint32_t& col, uint32_t& width) const {
+    uint32_t half = 0;
+    width = 256;
+    if (t >= whole) {
+      half = (t - whole) & 1;
+      t = whole + ((t - whole) >> 1);
+      width = 128;
+    }
+    b = t / per;
+    t -= b * per;
+    uint32_t i, j;
+    if (sym) {   // columns of the upper triangle one after the other: column j holds the tiles 0..j
+      j = (uint32_t)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+      while (j * (j + 1) / 2 > t) --j;
+      while ((j + 1) * (j + 2) / 2 <= t) ++j;
+      i = t - j * (j + 1) / 2;
+    } else {
+      const uint32_t band = 4 * nt, g = t / band, r = t - g * band;
+      const uint32_t h = mt - 4 * g < 4 ? mt - 4 * g : 4;
+      j = r / h;
+      i = 4 * g + r - j * h;
+    }
+    row = i * 256;
+    col = j * 256 + half * 128;
+  }
+};
+
+constexpr int kPairStages = 6;
+constexpr int kPairStageBytes = 2 * kMmaRows * 128;   // per CTA: 128 rows of A, 128 of B
+constexpr size_t kPairSmem = (size_t)kPairStages * kPairStageBytes + 1024;
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {   // the same place in a CTA of the cluster
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {   // arrives at this place in both CTAs
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
+               : "memory");
+}
+template <int KIND>
+__device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (KIND == kMmaF16)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+template <int KIND, bool B_ACROSS, class Epi>
+__global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
+    k_mma_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const Epi epi) {
+  constexpr int kBK = KIND == kMmaF16 ? 64 : 128;
+  extern __shared__ uint8_t dyn[];
+  __shared__ uint64_t bars[2 * kPairStages + 5];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int gave_up;
+  const uint32_t ring = (smem_u32(dyn) + 1023u) & ~1023u;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * kPairStages, tfull = empty + 8 * kPairStages, tempty = tfull + 16,
+                 drain = tempty + 16;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+
+  if (threadIdx.x == 0) {
+    tma_prefetch_map(&map_a);
+    tma_prefetch_map(&map_b);
+    for (int i = 0; i < kPairStages; ++i) {
+      mbar_init(full + 8 * i, 1);
+      mbar_init(empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(tfull + 8 * i, 1);
+      mbar_init(tempty + 8 * i, 16);   // the epilogue warps of both CTAs
+    }
+    mbar_init(drain, 1);
+    gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  }
+  tc_fence_before();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_slot, 0);
+  asm volatile("griddepcontrol.launch_dependents;");   // after the allocation, as above
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const PairWalk walk(shape, pairs);
+  const uint32_t nk = (shape.k + kBK - 1) / kBK;
+  // an item of which nothing is wanted (outside C, or below the diagonal): every role passes over it
+  auto skip = [&](uint32_t row, uint32_t col, uint32_t width) { return col >= shape.n || (shape.sym && col + width <= row); };
+
+  if (warp == 0) {
+    const bool one = elect_one();
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+    uint32_t stage = 0, phase = 0, issued = 0;
+    bool ok = true;
+    for (uint32_t t = pair; ok && t < walk.items; t += pairs) {
+      uint32_t b, row, col, width;
+      walk.at(t, b, row, col, width);
+      if (skip(row, col, width)) continue;
+      const uint32_t mine = width / 2;                 // rows of B that this CTA fetches
+      for (uint32_t kb = 0; kb < nk; ++kb) {
+        if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, &gave_up))) break;
+        const uint32_t dst = ring + stage * kPairStageBytes, bar = in_cta(full + 8 * stage, 0);
+        if (one) {
+          if (rank == 0) mbar_expect_tx(full + 8 * stage, 2 * (kMmaRows + mine) * 128);
+          tma_load_3d_pair(dst, &map_a, (int)(kb * kBK), (int)(row + rank * kMmaRows), (int)b, bar);
+          for (uint32_t c = 0; c < mine; c += 64) {
+            const uint32_t to = dst + kMmaRows * 128 + c * 128, n0 = col + rank * mine + c;
+            if constexpr (B_ACROSS)
+              tma_load_3d_pair(to, &map_b, (int)n0, (int)(kb * kBK), (int)b, bar);
+            else
+              tma_load_3d_pair(to, &map_b, (int)(kb * kBK), (int)n0, (int)b, bar);
+          }
+        }
+        __syncwarp();
+        ++issued;
+        if (++stage == kPairStages) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
+    }
+    if (!ok && rank == 0) {   // copies in flight land before shared memory is given away (their bytes count in this CTA)
+      const uint32_t last = issued < (uint32_t)kPairStages ? issued : (uint32_t)kPairStages;
+      for (uint32_t q = 0; q < last; ++q) {
+        stage = stage ? stage - 1 : kPairStages - 1;
+        const uint32_t use = (issued - 1 - q) / kPairStages;
+        const long long t0 = clock64();
+        while (!mbar_try(full + 8 * stage, use & 1) && clock64() - t0 < kWaitCycles) {
+        }
+      }
+    }
+  } else if (warp == 1 && rank == 0) {
+    const bool one = elect_one();
+    constexpr uint32_t types = (KIND == kMmaF16 ? (1u << 4) : ((2u << 4) | (1u << 7) | (1u << 10))) | (B_ACROSS ? 1u << 16 : 0u) |
+                               ((uint32_t)(2 * kMmaRows >> 4) << 24);
+    uint32_t stage = 0, phase = 0, at = 0, aphase = 0;
+    bool ok = true;
+    for (uint32_t t = pair; ok && t < walk.items; t += pairs) {
+      uint32_t b, row, col, width;
+      walk.at(t, b, row, col, width);
+      if (skip(row, col, width)) continue;
+      const uint32_t idesc = types | (width >> 3 << 17);
+      if (!(ok = mbar_wait(tempty + 8 * at, aphase ^ 1, &gave_up))) break;
+      tc_fence_after();
+      const uint32_t d = tmem + at * 256;
+      for (uint32_t kb = 0; kb < nk; ++kb) {
+        if (!(ok = mbar_wait(full + 8 * stage, phase, &gave_up))) break;
+        tc_fence_after();
+        if (one) {
+          const uint32_t sa = ring + stage * kPairStageBytes, sb = sa + kMmaRows * 128;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint64_t da = smem_desc(sa + 32 * q, 16, 1024);
+            const uint64_t db = B_ACROSS ? smem_desc(sb + 2048 * q, kBK * 128, 1024) : smem_desc(sb + 32 * q, 16, 1024);
+            tc_mma_pair<KIND>(d, da, db, idesc, (kb | q) != 0);
+          }
+          tc_commit_pair(empty + 8 * stage);
+        }
+        __syncwarp();
+        if (++stage == kPairStages) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
+      if (!ok) break;
+      if (one) tc_commit_pair(tfull + 8 * at);
+      __syncwarp();
+      if (++at == 2) {
+        at = 0;
+        aphase ^= 1;
+      }
+    }
+    if (!ok) {
+      if (one) tc_commit_pair(drain);
+      const long long t0 = clock64();
+      while (!mbar_try(drain, 0) && clock64() - t0 < kWaitCycles) {
+      }
+    }
+  } else if (warp >= 4) {
+    const uint32_t quarter = warp & 3, group = (warp - 4) >> 2;
+    uint32_t at = 0, aphase = 0;
+    for (uint32_t t = pair; t < walk.items; t += pairs) {
+      uint32_t b, row_t, col, width;
+      walk.at(t, b, row_t, col, width);
+      if (skip(row_t, col, width)) continue;
+      const uint32_t row0 = row_t + rank * kMmaRows + quarter * 32, row = row0 + lane;
+      const int blocks = (int)(width >> 5);
+      auto wanted = [&](int c) {
+        const uint32_t col0 = col + 32 * c;
+        return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >= row0);
+      };
+      int c = (int)group;
+      while (c < blocks && !wanted(c)) c += 2;
+      typename Epi::Pre pre{};
+      if (c < blocks) pre = epi.load(row, col + 32 * c, b);
+      if (!mbar_wait(tfull + 8 * at, aphase, &gave_up)) break;
+      tc_fence_after();
+      while (c < blocks) {
+        uint32_t acc[32];
+        tmem_load32(acc, tmem + at * 256 + 32 * c + (quarter << 21));
+        int cn = c + 2;
+        while (cn < blocks && !wanted(cn)) cn += 2;
+        typename Epi::Pre nxt{};
+        if (cn < blocks) nxt = epi.load(row, col + 32 * cn, b);
+        tmem_load_wait();
+        epi.apply(pre, acc, row, col + 32 * c, b);
+        pre = nxt;
+        c = cn;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(in_cta(tempty + 8 * at, 0));
+      if (++at == 2) {
+        at = 0;
+        aphase ^= 1;
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync();   // the other CTA's arrivals and commits name this CTA's shared memory until here
+  tc_fence_after();
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+  if (threadIdx.x == 0 && gave_up && shape.dev_status) atomicOr(shape.dev_status + DS_DEV_WORD_FLAGS, DS_DEV_MMA_TIMEOUT);
+}
+
+// ---- a long K and few tiles: one tile by a cluster, K split over its CTAs ----
+// Each CTA of the cluster sums its share of K; then every 32 x 32 block of the tile gets an owner, the other CTAs write their
+// sums of it into the owner's shared memory (the ring, which is idle by then), and the owner adds them in the order of the
+// CTAs' ranks, so that results do not depend on timing.  512 x 512 x 4608 by single CTAs: 15.5 us of which 12 are the 72 steps
+// of K in a row; on a third of the SMs.
+template <int KIND, int BN, bool B_ACROSS, class Epi>
+__global__ void __launch_bounds__(kMmaThreads, 1)
+    k_mma_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const Epi epi,
+                const uint32_t parts) {
+  using T = MmaTile<BN>;
+  constexpr int kBK = KIND == kMmaF16 ? 64 : 128;
+  constexpr int kTmem = BN < 32 ? 32 : BN == 192 ? 256 : BN;
+  constexpr int kBlocks = BN / 32;
+  extern __shared__ uint8_t dyn[];
+  __shared__ uint64_t bars[2 * T::kStages + 1];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int gave_up;
+  const uint32_t ring = (smem_u32(dyn) + 1023u) & ~1023u;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * T::kStages, done = empty + 8 * T::kStages;
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+
+  if (threadIdx.x == 0) {
+    tma_prefetch_map(&map_a);
+    tma_prefetch_map(&map_b);
+    for (int i = 0; i < T::kStages; ++i) {
+      mbar_init(full + 8 * i, 1);
+      mbar_init(empty + 8 * i, 1);
+    }
+    mbar_init(done, 1);
+    gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), kTmem);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_slot, 0);
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  const TileWalk walk(shape, BN);
+  uint32_t b, ti, tj;
+  walk.at(blockIdx.x / parts, b, ti, tj);
+  const uint32_t nk_all = (shape.k + kBK - 1) / kBK, share = (nk_all + parts - 1) / parts;
+  const uint32_t k_first = min(rank * share, nk_all), nk = min(share, nk_all - k_first);
+
+  const uint32_t quarter = warp & 3, group = (warp - 4) >> 2;   // epilogue warps
+  const uint32_t row0 = ti * kMmaRows + quarter * 32, row = row0 + lane, c_first = tj * BN;
+  auto wanted = [&](int c) {
+    const uint32_t col0 = c_first + 32 * c;
+    return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >= row0);
+  };
+  auto owner = [&](int c) { return (uint32_t)(c * 4 + quarter) % parts; };
+  // where in an owner's ring the sums of block (c, quarter) from CTA r lie: 4 KB
+  auto slot = [&](int c, uint32_t r) { return ring + (((c * 4 + quarter) / parts) * parts + r) * 4096u; };
+
+  if (warp == 0) {
+    const bool one = elect_one();
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+    uint32_t stage = 0, phase = 0, issued = 0;
+    bool ok = true;
+    for (uint32_t kb = k_first; kb < k_first + nk; ++kb) {
+      if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, &gave_up))) break;
+      const uint32_t dst = ring + stage * T::kStageBytes;
+      if (one) {
+        mbar_expect_tx(full + 8 * stage, T::kStageBytes);
+        tma_load_3d(dst, &map_a, (int)(kb * kBK), (int)(ti * kMmaRows), (int)b, full + 8 * stage);
+        if constexpr (B_ACROSS) {
+#pragma unroll
+          for (int c = 0; c < BN / 64; ++c)
+            tma_load_3d(dst + kMmaRows * 128 + c * (kBK * 128), &map_b, (int)(c_first + c * 64), (int)(kb * kBK), (int)b, full + 8 * stage);
+        } else {
+          tma_load_3d(dst + kMmaRows * 128, &map_b, (int)(kb * kBK), (int)c_first, (int)b, full + 8 * stage);
+        }
+      }
+      __syncwarp();
+      ++issued;
+      if (++stage == T::kStages) {
+        stage = 0;
+        phase ^= 1;
+      }
+    }
+    if (!ok) {
+      const uint32_t last = issued < (uint32_t)T::kStages ? issued : (uint32_t)T::kStages;
+      for (uint32_t q = 0; q < last; ++q) {
+        stage = stage ? stage - 1 : T::kStages - 1;
+        const uint32_t use = (issued - 1 - q) / T::kStages;
+        const long long t0 = clock64();
+        while (!mbar_try(full + 8 * stage, use & 1) && clock64() - t0 < kWaitCycles) {
+        }
+      }
+    }
+  } else if (warp == 1) {
+    const bool one = elect_one();
+    constexpr uint32_t idesc = mma_idesc<KIND, BN, B_ACROSS>();
+    uint32_t stage = 0, phase = 0;
+    for (uint32_t kb = 0; kb < nk; ++kb) {
+      if (!mbar_wait(full + 8 * stage, phase, &gave_up)) break;
+      tc_fence_after();
+      if (one) {
+        const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint64_t da = smem_desc(sa + 32 * q, 16, 1024);
+          const uint64_t db = B_ACROSS ? smem_desc(sb + 2048 * q, kBK * 128, 1024) : smem_desc(sb + 32 * q, 16, 1024);
+          tc_mma<KIND>(tmem, da, db, idesc, (kb | q) != 0);
+        }
+        tc_commit(empty + 8 * stage);
+      }
+      __syncwarp();
+      if (++stage == T::kStages) {
+        stage = 0;
+        phase ^= 1;
+      }
+    }
+    if (one) tc_commit(done);   // after a wait that ran out, too: it tells that the products in flight have ended
+    __syncwarp();
+  }
+  // every role: this CTA's products have ended, its ring is idle
+  (void)mbar_wait(done, 0, &gave_up);
+  tc_fence_after();
+  cluster_sync();
+  if (warp >= 4) {
+    for (int c = (int)group; c < kBlocks; c += 2) {
+      if (!wanted(c) || owner(c) == rank) continue;
+      uint32_t acc[32];
+      tmem_load32(acc, tmem + 32 * c + (quarter << 21));
+      tmem_load_wait();
+      const uint32_t to = in_cta(slot(c, rank), owner(c)) + lane * 16;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + 512 * j), "r"(nk ? acc[4 * j] : 0u),
+                     "r"(nk ? acc[4 * j + 1] : 0u), "r"(nk ? acc[4 * j + 2] : 0u), "r"(nk ? acc[4 * j + 3] : 0u)
+                     : "memory");
+    }
+  }
+  __syncwarp();
+  cluster_sync();
+  if (warp >= 4) {
+    for (int c = (int)group; c < kBlocks; c += 2) {
+      if (!wanted(c) || owner(c) != rank) continue;
+      const typename Epi::Pre pre = epi.load(row, c_first + 32 * c, b);
+      uint32_t acc[32], own[32];
+      tmem_load32(own, tmem + 32 * c + (quarter << 21));
+      tmem_load_wait();
+#pragma unroll
+      for (int j = 0; j < 32; ++j) acc[j] = 0;
+      for (uint32_t r = 0; r < parts; ++r) {
+        const uint32_t from = slot(c, r) + lane * 16;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          uint32_t v[4];
+          if (r != rank)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(from + 512 * j) : "memory");
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x = r != rank ? v[i] : nk ? own[4 * j + i] : 0u;
+            if constexpr (KIND == kMmaI8)
+              acc[4 * j + i] += x;
+            else
+              acc[4 * j + i] = __float_as_uint(__fadd_rn(__uint_as_float(acc[4 * j + i]), __uint_as_float(x)));
+          }
+        }
+      }
+      epi.apply(pre, acc, row, c_first + 32 * c, b);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 2) tmem_free(tmem, kTmem);
+  if (threadIdx.x == 0 && gave_up && shape.dev_status) atomicOr(shape.dev_status + DS_DEV_WORD_FLAGS, DS_DEV_MMA_TIMEOUT);
+}
+
 // ---- host side ------------------------------------------------------------------------------------------
 
 // A map over `batch` matrices of `rows` rows of `cols` elements (2-byte floats or bytes), `ld` elements apart, read in
@@ -363,23 +847,78 @@ cudaError_t make_tensor_map(CUtensorMap* map, int kind, const void* base, uint64
 
 int sm_count();
 
-// The width of a tile that ends first: CTAs go through the tiles in rounds, and a round lasts as long as its tile is wide
-// plus what a tile costs whatever its width (its first operands and the end of its epilogue, about 24 columns' worth).
-inline int pick_bn(const MmaShape& s, int sms) {
-  int best = 64;
-  double least = 1e300;
-  for (int bn : {256, 192, 128, 64}) {
-    const TileWalk w(s, bn);
-    const double rounds = (double)((w.total + sms - 1) / sms);
-    // a tile narrower than 192 columns is held up by shared memory: 128 + bn rows are read for 128 x bn products
-    const double width = bn >= 192 ? bn : (128 + bn) * 0.6;
-    const double cost = rounds * (width + 24);
-    if (cost < least * 0.999) {
-      least = cost;
-      best = bn;
-    }
+// Clusters of `size` (2, 4 or 8) such CTAs that run at once on this device (a cluster stays within a part of the device, which
+// may leave SMs over).
+int cluster_count(uint32_t size);
+inline int pair_count() { return cluster_count(2); }
+
+// How a product is taken.
+struct MmaPlan {
+  bool pair;
+  int bn;             // width of a tile (single CTAs and clusters)
+  uint32_t parts;     // CTAs that share a tile's K: 1, or a cluster of 2, 4 or 8
+  uint32_t box_rows() const { return pair ? 64 : (uint32_t)bn; }   // rows of a box of B
+};
+
+// Which form ends first, from times measured on a B200 in us: `steps` of 128 bytes of K; what a launch costs whatever its size
+// (single CTAs 4, pairs 6, clusters that split K 8); a tile's step by its width, with few SMs busy and with all of them (when
+// L2 and power bound it); a tile's epilogue, which the next tile's products hide.  Measured and modelled, 16-bit operands:
+//   4096^3: 64 columns 162 / 165, 128 116 / 127, 192 107 / 114, 256 116 / 118, pairs 98 / 98
+//   2048^3: 38 / 29, 25 / 24, 30 / 28, 22 / 22, 24 / 23;   1024^3: 8.5 / 8.2, 9.9 / 9.0, 11.7 / 11, 14 / 13, 12 / 11
+constexpr double kTileEpilogue = 1.0;      // per 64 columns
+inline double step_time(int bn, double busy) {
+  const double few = bn == 256 ? 0.30 : bn == 192 ? 0.25 : bn == 128 ? 0.18 : 0.16;
+  const double all = bn == 256 ? 0.43 : bn == 192 ? 0.335 : bn == 128 ? 0.27 : 0.18;
+  return busy >= 1 ? all : busy <= 0.4 ? few : few + (all - few) * (busy - 0.4) / 0.6;
+}
+inline double rounds_time(double rounds, double main, double epilogue) {
+  return rounds <= 0 ? 0 : main + (rounds - 1) * (main > epilogue ? main : epilogue) + epilogue;
+}
+inline double single_time(const MmaShape& s, int sms, int bn) {
+  const TileWalk w(s, bn);
+  return 4 + rounds_time((double)((w.total + sms - 1) / sms), step_time(bn, (double)w.total / sms) * (s.k * (double)s.elem / 128),
+                         kTileEpilogue * bn / 64);
+}
+inline double split_time(const MmaShape& s, int sms, int bn, uint32_t parts) {
+  const TileWalk w(s, bn);
+  if (w.total > (uint32_t)cluster_count(parts) || bn > 128) return 1e300;   // one round: a CTA keeps one tile
+  return 8 + step_time(bn, (double)w.total * parts / sms) * (s.k * (double)s.elem / 128) / parts + kTileEpilogue * bn / 64;
+}
+inline double pair_time(const MmaShape& s, int pairs) {
+  const PairWalk w(s, pairs);
+  const double rounds = w.whole / pairs + (w.whole % pairs != 0), steps = s.k * (double)s.elem / 128, epi = 4 * kTileEpilogue;
+  const double main = 0.40 * steps;
+  double t = 6 + rounds_time(rounds, main, epi);
+  if (w.items > w.whole) t += rounds > 0 ? (0.5 * main > epi ? 0.5 * main : epi) - 0.5 * epi : 0.5 * (main + epi);
+  return t;
+}
+inline MmaPlan plan_mma(const MmaShape& s) {
+  const int sms = sm_count();
+  MmaPlan p{false, 64, 1};
+  double least = single_time(s, sms, 64);
+  for (int bn : {128, 192, 256}) {
+    const double t = single_time(s, sms, bn);
+    if (t < least) least = t, p = MmaPlan{false, bn, 1};
   }
-  return best;
+  for (int bn : {64, 128})
+    for (uint32_t parts : {2u, 4u, 8u}) {
+      const double t = split_time(s, sms, bn, parts);
+      if (t < least) least = t, p = MmaPlan{false, bn, parts};
+    }
+  if (pair_time(s, pair_count()) < least) p = MmaPlan{true, 256, 1};
+  return p;
+}
+
+// Shared memory beyond 48 KB is asked for once per kernel and device.
+template <auto KERNEL>
+inline void allow_smem_for(size_t bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  (void)cudaGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (done.load(std::memory_order_relaxed) & bit) return;
+  if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess)
+    done.fetch_or(bit, std::memory_order_relaxed);
 }
 
 template <int KIND, int BN, bool B_ACROSS, class Epi>
@@ -387,9 +926,55 @@ cudaError_t launch_mma_bn(const CUtensorMap& a, const CUtensorMap& b, const MmaS
   const TileWalk w(s, BN);
   const uint32_t grid = w.total < (uint32_t)sm_count() ? w.total : (uint32_t)sm_count();
   if (!grid) return cudaSuccess;
-  launch_pdl_smem(k_mma<KIND, BN, B_ACROSS, Epi>, dim3(grid), dim3(kMmaThreads), MmaTile<BN>::kSmem, st, a, b, s, epi);
+  allow_smem_for<k_mma<KIND, BN, B_ACROSS, Epi>>(MmaTile<BN>::kSmem);
+  launch_pdl_dyn(k_mma<KIND, BN, B_ACROSS, Epi>, dim3(grid), dim3(kMmaThreads), MmaTile<BN>::kSmem, st, a, b, s, epi);
   count_launches(1);
   return cudaGetLastError();
+}
+
+template <int KIND, int BN, bool B_ACROSS, class Epi>
+cudaError_t launch_mma_split(uint32_t parts, const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
+  const TileWalk w(s, BN);
+  if (!w.total) return cudaSuccess;
+  allow_smem_for<k_mma_split<KIND, BN, B_ACROSS, Epi>>(MmaTile<BN>::kSmem);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(w.total * parts);
+  cfg.blockDim = dim3(kMmaThreads);
+  cfg.dynamicSmemBytes = MmaTile<BN>::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = parts;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  (void)cudaLaunchKernelEx(&cfg, k_mma_split<KIND, BN, B_ACROSS, Epi>, a, b, s, epi, parts);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+template <int KIND, bool B_ACROSS, class Epi>
+cudaError_t launch_mma(const MmaPlan& plan, const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
+  if (plan.pair) {
+    const PairWalk w(s, pair_count());
+    const uint32_t pairs = w.items < (uint32_t)pair_count() ? w.items : (uint32_t)pair_count();
+    if (!pairs) return cudaSuccess;
+    allow_smem_for<k_mma_pair<KIND, B_ACROSS, Epi>>(kPairSmem);
+    launch_pdl_dyn(k_mma_pair<KIND, B_ACROSS, Epi>, dim3(2 * pairs), dim3(kMmaThreads), kPairSmem, st, a, b, s, epi);
+    count_launches(1);
+    return cudaGetLastError();
+  }
+  if (plan.parts > 1)
+    return plan.bn == 128 ? launch_mma_split<KIND, 128, B_ACROSS>(plan.parts, a, b, s, epi, st)
+                          : launch_mma_split<KIND, 64, B_ACROSS>(plan.parts, a, b, s, epi, st);
+  switch (plan.bn) {
+    case 256: return launch_mma_bn<KIND, 256, B_ACROSS>(a, b, s, epi, st);
+    case 192: return launch_mma_bn<KIND, 192, B_ACROSS>(a, b, s, epi, st);
+    case 128: return launch_mma_bn<KIND, 128, B_ACROSS>(a, b, s, epi, st);
+    default: return launch_mma_bn<KIND, 64, B_ACROSS>(a, b, s, epi, st);
+  }
 }
 
 }  // namespace dsq

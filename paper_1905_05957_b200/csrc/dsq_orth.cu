@@ -13,50 +13,16 @@
 //  - The diagonals of A and B, which hold most of their size when rows are nearly orthogonal, stay in 32 bits: A = D + O and
 //    B = E + F with F off-diagonal:  F = b O + c (O O)_off + c (d_i + d_j) O_ij,  E_ii = b d_i + c d_i^2 + c (O O)_ii,
 //    X = (a + E) X + F X.  Row scalings cost nothing in the epilogues.  (0.1 % to 0.2 % off without it on such inputs.)
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <cmath>
 #include <cstring>
 #include <new>
 
 #include "dsq_mma.cuh"
+#include "dsq_orth.cuh"
 
 using namespace dsq;
 
 namespace {
-
-constexpr float kUp = 1024.f, kDown = 1.f / 1024.f;   // the fixed scale of the 16-bit matrices
-
-__device__ __forceinline__ float to_f32(float v) { return v; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
-
-__device__ __forceinline__ void load4(float (&o)[4], const float* p) {
-  const float4 v = *reinterpret_cast<const float4*>(p);
-  o[0] = v.x, o[1] = v.y, o[2] = v.z, o[3] = v.w;
-}
-template <class T16>
-__device__ __forceinline__ void load4(float (&o)[4], const T16* p) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p);
-  const T16* e = reinterpret_cast<const T16*>(&v);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = to_f32(e[i]);
-}
-
-struct Momentum {
-  const void* g;
-  float* buf;        // NULL: u = g
-  uint64_t stride;   // elements between matrices of g and buf
-  float mu;
-  int nesterov;
-  __device__ __forceinline__ float update(float g, float b) const {   // the new buf
-    return __fadd_rn(__fmul_rn(mu, b), g);
-  }
-  __device__ __forceinline__ float direction(float g, float b) const {   // u from the new buf
-    return nesterov ? __fadd_rn(g, __fmul_rn(mu, b)) : b;
-  }
-};
 
 // ---- momentum and norm: one pass over g and buf ----
 // Bound by memory: 4 (or 2) + 4 bytes read and 4 written an entry.  Squares add up in 64 bits, each thread over its own
@@ -131,7 +97,7 @@ __global__ void __launch_bounds__(kThreads) k_orth_momentum(const Momentum mo, u
 // 64 x 64 tiles; the tile goes through shared memory when it is transposed.
 struct Halves {
   __half *hi, *lo;
-  uint32_t ld;       // elements between rows (a multiple of 8)
+  uint32_t ld;       // elements between rows (a multiple of 16)
   uint64_t stride;   // elements between matrices
 };
 
@@ -140,7 +106,8 @@ __global__ void __launch_bounds__(kThreads) k_orth_split(const Momentum mo, uint
                                                          const Halves x) {
   pdl_prologue();
   __shared__ float tile[TALL ? 64 : 1][TALL ? 65 : 1];
-  const uint32_t b = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+  // from the end: what the pass before touched last is still in L2
+  const uint32_t b = gridDim.z - 1 - blockIdx.z, r0 = (gridDim.y - 1 - blockIdx.y) * 64, c0 = (gridDim.x - 1 - blockIdx.x) * 64;
   const uint64_t off = (uint64_t)b * mo.stride;
   const T* g = static_cast<const T*>(mo.g) + off;
   const float* buf = mo.buf ? mo.buf + off : nullptr;
@@ -196,22 +163,28 @@ __global__ void __launch_bounds__(kThreads) k_orth_split(const Momentum mo, uint
 
 // ---- epilogues of the three products ----
 
-struct Half32 {   // 32 consecutive entries of a row
-  uint4 q[4];
+struct Half32 {   // 32 consecutive entries of a row, two to a word
+  uint32_t w[16];
+  __device__ __forceinline__ float2 two(int j) const {   // entries 2j and 2j + 1
+    return __half22float2(*reinterpret_cast<const __half2*>(w + j));
+  }
+  __device__ __forceinline__ void set(int j, float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    w[j] = *reinterpret_cast<const uint32_t*>(&h);
+  }
 };
 __device__ __forceinline__ Half32 load_half32(const __half* row, uint32_t col0, uint32_t ld) {
   Half32 v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    v.q[i] = col0 + 8 * i < ld ? *reinterpret_cast<const uint4*>(row + col0 + 8 * i) : make_uint4(0, 0, 0, 0);
+  for (int i = 0; i < 16; ++i) v.w[i] = 0;
+  if (col0 < ld) ld_b32(v.w, row + col0);
+  if (col0 + 16 < ld) ld_b32(v.w + 8, row + col0 + 16);
   return v;
 }
 __device__ __forceinline__ void store_half32(__half* row, uint32_t col0, uint32_t ld, const Half32& v) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (col0 + 8 * i < ld) *reinterpret_cast<uint4*>(row + col0 + 8 * i) = v.q[i];
+  if (col0 < ld) st_b32(row + col0, v.w);
+  if (col0 + 16 < ld) st_b32(row + col0 + 16, v.w + 8);
 }
-__device__ __forceinline__ float half_at(const Half32& v, int j) { return __half2float(reinterpret_cast<const __half*>(&v)[j]); }
 
 // A symmetric matrix in 16 bits without its diagonal, which is held apart.
 struct SymOut {
@@ -226,10 +199,10 @@ struct SymOut {
     __half* base = off + b * stride;
     store_half32(base + (uint64_t)row * ld, col0, ld, v);
     if (col0 > row) {
-      const __half* e = reinterpret_cast<const __half*>(&v);
+      uint16_t* to = reinterpret_cast<uint16_t*>(base + (uint64_t)col0 * ld + row);
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        if (col0 + j < m) base[(uint64_t)(col0 + j) * ld + row] = e[j];
+        if (col0 + j < m) to[(uint64_t)j * ld] = (uint16_t)(v.w[j / 2] >> (16 * (j & 1)));
     }
   }
 };
@@ -240,16 +213,15 @@ struct EpiGram {   // A = X X^T
   __device__ __forceinline__ Pre load(uint32_t, uint32_t, uint32_t) const { return {}; }
   __device__ __forceinline__ void apply(const Pre&, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b) const {
     Half32 v;
-    __half* e = reinterpret_cast<__half*>(&v);
-    float d = 0.f;
+    float d = 0.f, s[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
-      const float s = __uint_as_float(acc[j]);
-      const bool on = col0 + j == row;
-      if (on) d = s;
-      e[j] = __float2half_rn(on ? 0.f : s * kDown);
+      s[j] = __uint_as_float(acc[j]) * kDown;
+      if (col0 + j == row) d = s[j], s[j] = 0.f;
     }
-    if (row >= col0 && row < col0 + 32 && row < a.m) a.diag[b * a.diag_stride + row] = d * (kDown * kDown);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v.set(j, s[2 * j], s[2 * j + 1]);
+    if (row >= col0 && row < col0 + 32 && row < a.m) a.diag[b * a.diag_stride + row] = d * kDown;
     a.put(v, row, col0, b);
   }
 };
@@ -271,16 +243,24 @@ struct EpiPoly {   // B = b A + c A A, the accumulator being O O
   }
   __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b) const {
     Half32 v;
-    __half* e = reinterpret_cast<__half*>(&v);
-    const float* dj = a.diag + b * a.diag_stride + col0;   // padded to a multiple of 32 entries
-    float d = 0.f;
+    const float4* dj = reinterpret_cast<const float4*>(a.diag + b * a.diag_stride + col0);   // padded to a multiple of 32 entries
+    float d = 0.f, e[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      const float s = __uint_as_float(acc[j]), o = half_at(p.o, j);
-      const bool on = col0 + j == row;
-      if (on) d = s;
-      e[j] = __float2half_rn(on || col0 + j >= a.m ? 0.f : fmaf(c1, fmaf(s, kDown, (p.d + dj[j]) * o), b1 * o));
+    for (int q = 0; q < 8; ++q) {
+      const float4 t = __ldg(dj + q);
+      const float2 o0 = p.o.two(2 * q), o1 = p.o.two(2 * q + 1);
+      const float dd[4] = {t.x, t.y, t.z, t.w}, o[4] = {o0.x, o0.y, o1.x, o1.y};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = 4 * q + i;
+        const float s = __uint_as_float(acc[j]);
+        const bool on = col0 + j == row;
+        if (on) d = s;
+        e[j] = on || col0 + j >= a.m ? 0.f : fmaf(c1, fmaf(s, kDown, (p.d + dd[i]) * o[i]), b1 * o[i]);
+      }
     }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v.set(j, e[2 * j], e[2 * j + 1]);
     if (row >= col0 && row < col0 + 32 && row < a.m)
       out.diag[b * a.diag_stride + row] = fmaf(c1, fmaf(d, kDown * kDown, p.d * p.d), b1 * p.d);
     out.put(v, row, col0, b);
@@ -298,11 +278,8 @@ struct EpiX {   // X = (a + E) X + F X
   uint32_t m, n, ld;
   float a1;
   __half *hi_out, *lo_out;   // the next X; NULL on the last step, which writes:
-  void* out;                 //   out (may be NULL), contiguous, in the orientation of the gradient
-  int out_dtype, tall, vec;
-  float* x;                  //   x (may be NULL)
-  uint64_t x_stride;
-  float keep, rate;          //   x = keep x - rate X
+  OrthOut to;                //   in the orientation of the gradient
+  int tall, vec;
   __device__ __forceinline__ Pre load(uint32_t row, uint32_t col0, uint32_t b) const {
     Pre p{};
     if (row < m) {
@@ -318,14 +295,18 @@ struct EpiX {   // X = (a + E) X + F X
     const float f = a1 + p.e;
     float v[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = fmaf(f, half_at(p.hi, j) + half_at(p.lo, j), __uint_as_float(acc[j]) * kDown);
+    for (int j = 0; j < 16; ++j) {
+      const float2 h = p.hi.two(j), l = p.lo.two(j);
+      v[2 * j] = fmaf(f, h.x + l.x, __uint_as_float(acc[2 * j]) * kDown);
+      v[2 * j + 1] = fmaf(f, h.y + l.y, __uint_as_float(acc[2 * j + 1]) * kDown);
+    }
     if (hi_out) {
       Half32 h, l;
-      __half *eh = reinterpret_cast<__half*>(&h), *el = reinterpret_cast<__half*>(&l);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        eh[j] = __float2half_rn(v[j]);
-        el[j] = __float2half_rn(v[j] - __half2float(eh[j]));
+      for (int j = 0; j < 16; ++j) {
+        h.set(j, v[2 * j], v[2 * j + 1]);
+        const float2 r = h.two(j);
+        l.set(j, v[2 * j] - r.x, v[2 * j + 1] - r.y);
       }
       const uint64_t at = b * stride + (uint64_t)row * ld;
       store_half32(hi_out + at, col0, ld, h);
@@ -338,17 +319,20 @@ struct EpiX {   // X = (a + E) X + F X
     const bool whole = vec && !tall && col0 + 32 <= n;
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] *= kDown;
-    if (out) {
+    if (to.out) {
       const uint64_t at = b * each + first;
-      if (out_dtype == DS_BF16) {
-        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(out) + at;
+      if (to.dtype == DS_BF16) {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(to.out) + at;
         if (whole) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            __nv_bfloat16 t[8];
+          for (int q = 0; q < 2; ++q) {
+            uint32_t t[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] = __float2bfloat16_rn(v[8 * q + j]);
-            *reinterpret_cast<uint4*>(o + 8 * q) = *reinterpret_cast<uint4*>(t);
+            for (int j = 0; j < 8; ++j) {
+              const __nv_bfloat162 h = __floats2bfloat162_rn(v[16 * q + 2 * j], v[16 * q + 2 * j + 1]);
+              t[j] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            st_b32(o + 16 * q, t);
           }
         } else {
 #pragma unroll
@@ -356,7 +340,7 @@ struct EpiX {   // X = (a + E) X + F X
             if (col0 + j < n) o[j * step] = __float2bfloat16_rn(v[j]);
         }
       } else {
-        float* o = static_cast<float*>(out) + at;
+        float* o = static_cast<float*>(to.out) + at;
         if (whole) {
 #pragma unroll
           for (int q = 0; q < 8; ++q) *reinterpret_cast<float4*>(o + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
@@ -367,36 +351,26 @@ struct EpiX {   // X = (a + E) X + F X
         }
       }
     }
-    if (x) {
-      float* px = x + b * x_stride + first;
+    if (to.x) {
+      float* px = to.x + b * to.x_stride + first;
       if (whole) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           float4 t = *reinterpret_cast<float4*>(px + 4 * q);
-          t.x = __fsub_rn(__fmul_rn(keep, t.x), __fmul_rn(rate, v[4 * q]));
-          t.y = __fsub_rn(__fmul_rn(keep, t.y), __fmul_rn(rate, v[4 * q + 1]));
-          t.z = __fsub_rn(__fmul_rn(keep, t.z), __fmul_rn(rate, v[4 * q + 2]));
-          t.w = __fsub_rn(__fmul_rn(keep, t.w), __fmul_rn(rate, v[4 * q + 3]));
+          t.x = __fsub_rn(__fmul_rn(to.keep, t.x), __fmul_rn(to.rate, v[4 * q]));
+          t.y = __fsub_rn(__fmul_rn(to.keep, t.y), __fmul_rn(to.rate, v[4 * q + 1]));
+          t.z = __fsub_rn(__fmul_rn(to.keep, t.z), __fmul_rn(to.rate, v[4 * q + 2]));
+          t.w = __fsub_rn(__fmul_rn(to.keep, t.w), __fmul_rn(to.rate, v[4 * q + 3]));
           *reinterpret_cast<float4*>(px + 4 * q) = t;
         }
       } else {
 #pragma unroll
         for (int j = 0; j < 32; ++j)
-          if (col0 + j < n) px[j * step] = __fsub_rn(__fmul_rn(keep, px[j * step]), __fmul_rn(rate, v[j]));
+          if (col0 + j < n) px[j * step] = __fsub_rn(__fmul_rn(to.keep, px[j * step]), __fmul_rn(to.rate, v[j]));
       }
     }
   }
 };
-
-template <bool B_ACROSS, class Epi>
-cudaError_t launch_f16(int bn, const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
-  switch (bn) {
-    case 256: return launch_mma_bn<kMmaF16, 256, B_ACROSS>(a, b, s, epi, st);
-    case 192: return launch_mma_bn<kMmaF16, 192, B_ACROSS>(a, b, s, epi, st);
-    case 128: return launch_mma_bn<kMmaF16, 128, B_ACROSS>(a, b, s, epi, st);
-    default: return launch_mma_bn<kMmaF16, 64, B_ACROSS>(a, b, s, epi, st);
-  }
-}
 
 inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
@@ -414,6 +388,7 @@ bool orth_config_ok(const ds_orth_config* c) {
 struct ds_orth_ctx {
   ds_orth_config cfg;
   uint32_t m, n, ldx, ldm;
+  uint32_t small;                 // CTAs a matrix takes in the form for small matrices, 0: the products below
   uint64_t xs, ms, ds;            // elements between matrices of X, of A and B, of the diagonals
   __half *hi[2], *lo[2];
   SymOut a, b;
@@ -422,7 +397,7 @@ struct ds_orth_ctx {
   uint32_t* ticket;
   uint32_t* dev_status;
   bool mapped;                    // the tensor maps below are made (on the first update: the driver makes them)
-  int bn_gram, bn_poly, bn_x;
+  MmaPlan p_gram, p_poly, p_x;
   CUtensorMap x_rows[2], x_cols_gram[2], x_across[2], a_rows, a_cols, b_rows;
 };
 
@@ -433,11 +408,13 @@ uint64_t orth_plan(ds_orth_ctx* h, uint8_t* ws) {
   const ds_orth_config& c = h->cfg;
   h->m = c.rows < c.cols ? c.rows : c.cols;
   h->n = c.rows < c.cols ? c.cols : c.rows;
-  h->ldx = (uint32_t)round_up(h->n, 8);
-  h->ldm = (uint32_t)round_up(h->m, 8);
+  h->ldx = (uint32_t)round_up(h->n, 16);
+  h->ldm = (uint32_t)round_up(h->m, 16);
   h->xs = (uint64_t)h->m * h->ldx;
   h->ms = (uint64_t)h->m * h->ldm;
   h->ds = round_up(h->m, 32);
+  h->small = orth_small_ctas(h->m, h->n, c.batch);
+  if (h->small) return 256;   // works in shared memory
   uint64_t pos = 0;
   auto take = [&](uint64_t bytes) {
     uint8_t* p = ws ? ws + pos : nullptr;
@@ -464,21 +441,20 @@ uint64_t orth_plan(ds_orth_ctx* h, uint8_t* ws) {
 
 cudaError_t orth_maps(ds_orth_ctx* h) {
   const uint32_t batch = h->cfg.batch;
-  const int sms = sm_count();
-  h->bn_gram = pick_bn({h->m, h->m, h->n, batch, 1, nullptr}, sms);
-  h->bn_poly = pick_bn({h->m, h->m, h->m, batch, 1, nullptr}, sms);
-  h->bn_x = pick_bn({h->m, h->n, h->m, batch, 0, nullptr}, sms);
+  h->p_gram = plan_mma({h->m, h->m, h->n, batch, 2, 1, nullptr});
+  h->p_poly = plan_mma({h->m, h->m, h->m, batch, 2, 1, nullptr});
+  h->p_x = plan_mma({h->m, h->n, h->m, batch, 2, 0, nullptr});
   cudaError_t e = cudaSuccess;
   auto add = [&](CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t ld, uint64_t stride, uint32_t box_rows) {
     if (e == cudaSuccess) e = make_tensor_map(map, kMmaF16, base, cols, rows, batch, ld, stride, 64, box_rows);
   };
   for (int i = 0; i < 2; ++i) {
     add(&h->x_rows[i], h->hi[i], h->n, h->m, h->ldx, h->xs, kMmaRows);
-    add(&h->x_cols_gram[i], h->hi[i], h->n, h->m, h->ldx, h->xs, h->bn_gram);
+    add(&h->x_cols_gram[i], h->hi[i], h->n, h->m, h->ldx, h->xs, h->p_gram.box_rows());
     add(&h->x_across[i], h->hi[i], h->n, h->m, h->ldx, h->xs, 64);
   }
   add(&h->a_rows, h->a.off, h->m, h->m, h->ldm, h->ms, kMmaRows);
-  add(&h->a_cols, h->a.off, h->m, h->m, h->ldm, h->ms, h->bn_poly);
+  add(&h->a_cols, h->a.off, h->m, h->m, h->ldm, h->ms, h->p_poly.box_rows());
   add(&h->b_rows, h->b.off, h->m, h->m, h->ldm, h->ms, kMmaRows);
   h->mapped = e == cudaSuccess;
   return e;
@@ -537,27 +513,32 @@ int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum
   const uint32_t g_size = g_dtype == DS_F32 ? 4 : 2, out_size = out_dtype == DS_F32 ? 4 : 2;
   if ((gp & (g_size - 1)) || ((bp | xp) & 3u) || (out && (op & (out_size - 1)))) return DS_ERR_ALIGN;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (!h->mapped) {
-    const cudaError_t e = orth_maps(h);
-    if (e != cudaSuccess) return cuda_fail(e, "tensor maps");
-  }
   Momentum mo;
   mo.g = g;
   mo.buf = momentum;
   mo.stride = c.stride ? c.stride : (uint64_t)c.rows * c.cols;
   mo.mu = c.momentum;
   mo.nesterov = (c.flags & DS_ORTH_NESTEROV) ? 1 : 0;
+  const OrthOut where{out, out_dtype, x, mo.stride, 1.f - gamma * decay, gamma * c.scale};
+  if (h->small) {
+    const cudaError_t e = launch_orth_small(c, h->small, mo, g_dtype, where, st);
+    return e == cudaSuccess ? DS_OK : cuda_fail(e, "orthogonalised update");
+  }
+  if (!h->mapped) {
+    const cudaError_t e = orth_maps(h);
+    if (e != cudaSuccess) return cuda_fail(e, "tensor maps");
+  }
   // four entries at a time where every matrix, and every row of it, starts on a boundary of four
   const int vec = c.cols % 4 == 0 && mo.stride % 4 == 0 && (gp & (4 * g_size - 1)) == 0 && (bp & 15u) == 0;
   cudaError_t e = g_dtype == DS_F32    ? launch_prepare<float>(h, mo, vec, st)
                   : g_dtype == DS_BF16 ? launch_prepare<__nv_bfloat16>(h, mo, vec, st)
                                        : launch_prepare<__half>(h, mo, vec, st);
-  const MmaShape gram{h->m, h->m, h->n, c.batch, 1, h->dev_status}, poly{h->m, h->m, h->m, c.batch, 1, h->dev_status},
-      full{h->m, h->n, h->m, c.batch, 0, h->dev_status};
+  const MmaShape gram{h->m, h->m, h->n, c.batch, 2, 1, h->dev_status}, poly{h->m, h->m, h->m, c.batch, 2, 1, h->dev_status},
+      full{h->m, h->n, h->m, c.batch, 2, 0, h->dev_status};
   int cur = 0;
   for (uint32_t s = 0; s < c.steps && e == cudaSuccess; ++s, cur ^= 1) {
-    e = launch_f16<false>(h->bn_gram, h->x_rows[cur], h->x_cols_gram[cur], gram, EpiGram{h->a}, st);
-    if (e == cudaSuccess) e = launch_f16<false>(h->bn_poly, h->a_rows, h->a_cols, poly, EpiPoly{h->a, h->b, c.b, c.c}, st);
+    e = launch_mma<kMmaF16, false>(h->p_gram, h->x_rows[cur], h->x_cols_gram[cur], gram, EpiGram{h->a}, st);
+    if (e == cudaSuccess) e = launch_mma<kMmaF16, false>(h->p_poly, h->a_rows, h->a_cols, poly, EpiPoly{h->a, h->b, c.b, c.c}, st);
     EpiX ex;
     memset(&ex, 0, sizeof ex);
     ex.hi = h->hi[cur];
@@ -573,16 +554,11 @@ int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum
       ex.hi_out = h->hi[cur ^ 1];
       ex.lo_out = h->lo[cur ^ 1];
     } else {
-      ex.out = out;
-      ex.out_dtype = out_dtype;
+      ex.to = where;
       ex.tall = c.rows > c.cols;
-      ex.x = x;
-      ex.x_stride = mo.stride;
-      ex.keep = 1.f - gamma * decay;
-      ex.rate = gamma * c.scale;
-      ex.vec = c.cols % 8 == 0 && (op & 15u) == 0 && (xp & 15u) == 0 && mo.stride % 4 == 0;
+      ex.vec = c.cols % 16 == 0 && (op & 31u) == 0 && (xp & 15u) == 0 && mo.stride % 4 == 0;
     }
-    if (e == cudaSuccess) e = launch_f16<true>(h->bn_x, h->b_rows, h->x_across[cur], full, ex, st);
+    if (e == cudaSuccess) e = launch_mma<kMmaF16, true>(h->p_x, h->b_rows, h->x_across[cur], full, ex, st);
   }
   return e == cudaSuccess ? DS_OK : cuda_fail(e, "orthogonalised update");
 }

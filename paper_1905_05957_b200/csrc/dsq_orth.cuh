@@ -1,0 +1,56 @@
+// Shared pieces of the orthogonalised update: its numbers' scale, the momentum, and the form for small matrices.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "dsq_internal.h"
+
+namespace dsq {
+
+constexpr float kUp = 1024.f, kDown = 1.f / 1024.f;   // the fixed scale of the 16-bit matrices
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+
+__device__ __forceinline__ void load4(float (&o)[4], const float* p) {
+  const float4 v = *reinterpret_cast<const float4*>(p);
+  o[0] = v.x, o[1] = v.y, o[2] = v.z, o[3] = v.w;
+}
+template <class T16>
+__device__ __forceinline__ void load4(float (&o)[4], const T16* p) {
+  const uint2 v = *reinterpret_cast<const uint2*>(p);
+  const T16* e = reinterpret_cast<const T16*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = to_f32(e[i]);
+}
+
+struct Momentum {
+  const void* g;
+  float* buf;        // NULL: u = g
+  uint64_t stride;   // elements between matrices of g and buf
+  float mu;
+  int nesterov;
+  __device__ __forceinline__ float update(float g, float b) const {   // the new buf
+    return __fadd_rn(__fmul_rn(mu, b), g);
+  }
+  __device__ __forceinline__ float direction(float g, float b) const {   // u from the new buf
+    return nesterov ? __fadd_rn(g, __fmul_rn(mu, b)) : b;
+  }
+};
+
+// Where a finished update goes.
+struct OrthOut {
+  void* out;          // NULL or contiguous [batch, rows, cols]
+  int dtype;          // DS_F32 or DS_BF16
+  float* x;           // NULL or the model: x = keep x - rate X
+  uint64_t x_stride;
+  float keep, rate;
+};
+
+// Matrices whose shorter side is at most 128 and whose longer side fits: one cluster of CTAs a matrix, everything in one launch
+// (dsq_orth_small.cu).  Returns the CTAs a matrix takes, 0 where it does not fit.
+uint32_t orth_small_ctas(uint32_t m, uint32_t n, uint32_t batch);
+cudaError_t launch_orth_small(const ds_orth_config& c, uint32_t ctas, const Momentum& mo, int g_dtype, const OrthOut& o, cudaStream_t st);
+
+}  // namespace dsq

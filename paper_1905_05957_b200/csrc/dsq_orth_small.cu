@@ -1,0 +1,369 @@
+// The orthogonalised update of small matrices in one launch: X is [m, n], m <= 128, and a cluster of CTAs keeps it in shared
+// memory for all steps, each CTA a slice of columns.  Of a step  A = X X^T,  B = b A + c A A,  X = a X + B X  only A needs the
+// other slices: the CTAs' sums are added through distributed shared memory, every CTA a share of the rows, and handed to all;
+// B is computed by every CTA for itself.  The same goes for the norm.
+//
+// A launch of the general form costs 4 to 5 us whatever its size, and an update has seventeen of them; here four 64 x 576
+// matrices take the time of their sums alone.  Since the tensor cores are idle most of that time, the products are taken in
+// two halves of either operand (hi hi + hi lo + lo hi on 16-bit floats: 22 bits), which small matrices need: their roundings do
+// not average out.  The warp instruction m16n8k16 is used; the operands are far too small for tiles of 128 rows to pay.
+#include "dsq_mma.cuh"
+#include "dsq_orth.cuh"
+
+using namespace dsq;
+
+namespace {
+
+constexpr int kSmallThreads = 256;
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_cluster2(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ void st_cluster_f64(uint32_t addr, double v) {
+  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
+}
+
+// Two floats as hi and lo halves.
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  const __half2 h = __floats2half2_rn(a, b);
+  const float2 r = __half22float2(h);
+  const __half2 l = __floats2half2_rn(a - r.x, b - r.y);
+  hi = *reinterpret_cast<const uint32_t*>(&h);
+  lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+__device__ __forceinline__ float2 join2(uint32_t hi, uint32_t lo) {
+  const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi)), l = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+  return make_float2(h.x + l.x, h.y + l.y);
+}
+
+// Shared memory of a CTA, in bytes: X hi, X lo [MP][w + 8] halves; A hi, A lo [MP][MP + 8]; and one block that is the CTA's share
+// of A in floats [MP][MP + 4], then B hi, B lo.  (Rows 16 bytes longer than a multiple of 32 spread ldmatrix over all banks.)
+template <int MP>
+struct SmallLayout {
+  uint32_t w, pitch;      // columns of a slice (a multiple of 16), bytes between rows of X
+  static constexpr uint32_t kPitchA = (MP + 8) * 2, kHalfA = MP * kPitchA, kPitchP = (MP + 4) * 4;
+  __host__ __device__ explicit SmallLayout(uint32_t w_) : w(w_), pitch((w_ + 8) * 2) {}
+  __host__ __device__ uint32_t x_half() const { return MP * pitch; }
+  __host__ __device__ uint32_t at_a() const { return 2 * x_half(); }
+  __host__ __device__ uint32_t at_p() const { return at_a() + 2 * kHalfA; }
+  __host__ __device__ uint32_t bytes() const { return at_p() + 2 * kHalfA; }
+};
+
+struct SmallArgs {
+  Momentum mo;
+  OrthOut to;
+  uint32_t rows, cols, m, n, steps, w;
+  int tall;
+  float a, b, c, eps;
+};
+
+template <class T, int MP>
+__global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs p) {
+  constexpr int kRowTiles = MP / 16, kHalves = 8 / kRowTiles, kCols = MP / kHalves, kTiles = kCols / 8;
+  constexpr int kChunk = 64, kChunkTiles = kChunk / kHalves / 8;
+  extern __shared__ __align__(16) uint8_t dyn[];
+  __shared__ double sums[kMaxCluster], warp_sum[kSmallThreads / 32];
+  pdl_prologue();
+  const SmallLayout<MP> L(p.w);
+  const uint32_t base = smem_u32(dyn), xh = base, xl = base + L.x_half(), ah = base + L.at_a(), al = ah + L.kHalfA, ps = base + L.at_p(),
+                 bh = ps, bl = ps + L.kHalfA;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint32_t ctas;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
+  const uint32_t rank = cluster_rank(), matrix = blockIdx.x / ctas;
+  const uint32_t c0 = rank * p.w, mine = c0 >= p.n ? 0 : min(p.w, p.n - c0);    // columns of X in this slice
+  const uint64_t off = (uint64_t)matrix * p.mo.stride;
+  const T* g = static_cast<const T*>(p.mo.g) + off;
+  float* buf = p.mo.buf ? p.mo.buf + off : nullptr;
+
+  // Entry e of the slice: where it is in the matrix, and in X.  Consecutive entries are consecutive in memory.
+  const uint32_t total = p.m * mine;
+  auto place = [&](uint32_t e, uint64_t& at, uint32_t& r, uint32_t& c) {
+    if (p.tall) {          // X = u^T: the slice is rows c0.. of u, all of their m entries
+      c = e / p.m;
+      r = e - c * p.m;
+      at = (uint64_t)(c0 + c) * p.m + r;
+    } else {
+      r = e / mine;
+      c = e - r * mine;
+      at = (uint64_t)r * p.n + c0 + c;
+    }
+  };
+
+  // momentum and norm
+  double sum = 0;
+  for (uint32_t e = tid; e < total; e += kSmallThreads) {
+    uint64_t at;
+    uint32_t r, c;
+    place(e, at, r, c);
+    float u = to_f32(g[at]);
+    if (buf) {
+      const float v = p.mo.update(u, buf[at]);
+      buf[at] = v;
+      u = p.mo.direction(u, v);
+    }
+    sum += (double)u * (double)u;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  if (lane == 0) warp_sum[warp] = sum;
+  // X starts as zeros: rows and columns past the end stay so
+  for (uint32_t i = tid; i < L.at_a() / 16; i += kSmallThreads) reinterpret_cast<uint4*>(dyn)[i] = make_uint4(0, 0, 0, 0);
+  cluster_sync();          // every CTA of the cluster runs: its shared memory may be written
+  if (tid < (int)ctas) {
+    double s = 0;
+    for (int i = 0; i < kSmallThreads / 32; ++i) s += warp_sum[i];
+    st_cluster_f64(in_cta(smem_u32(&sums[rank]), tid), s);
+  }
+  cluster_sync();
+  double norm2 = 0;
+  for (uint32_t i = 0; i < ctas; ++i) norm2 += sums[i];
+  const float scale = kUp / ((float)sqrt(norm2) + p.eps);
+  for (uint32_t e = tid; e < total; e += kSmallThreads) {
+    uint64_t at;
+    uint32_t r, c;
+    place(e, at, r, c);
+    float u = to_f32(g[at]);
+    if (buf) u = p.mo.direction(u, buf[at]);
+    const float v = __fmul_rn(u, scale);
+    const __half h = __float2half_rn(v);
+    *reinterpret_cast<__half*>(dyn + r * L.pitch + 2 * c) = h;
+    *reinterpret_cast<__half*>(dyn + L.x_half() + r * L.pitch + 2 * c) = __float2half_rn(v - __half2float(h));
+  }
+  __syncthreads();
+
+  const int rt = warp % kRowTiles, half = warp / kRowTiles;
+  const uint32_t a_row = rt * 16 + (lane & 15), a_k = (lane >> 4) * 8;                       // ldmatrix places: an operand's rows
+  const uint32_t b_row = (lane & 7) + ((lane >> 4) << 3), b_k = ((lane >> 3) & 1) * 8;       // the other's, laid out along K
+  const uint32_t t_k = lane & 15, t_n = (lane >> 4) * 8;                                     // the other's, across K
+  const int er = lane >> 2, ec = 2 * (lane & 3);                                             // accumulators: rows er, er + 8
+
+  for (uint32_t step = 0; step < p.steps; ++step) {
+    {   // this slice's share of A = X X^T
+      float acc[kTiles][4] = {};
+      for (uint32_t k = 0; k < p.w; k += 16) {
+        uint32_t fh[4], fl[4];
+        ldsm(fh, xh + a_row * L.pitch + 2 * (k + a_k));
+        ldsm(fl, xl + a_row * L.pitch + 2 * (k + a_k));
+#pragma unroll
+        for (int j = 0; j < kTiles; j += 2) {
+          uint32_t gh[4], gl[4];
+          const uint32_t at = (half * kCols + j * 8 + b_row) * L.pitch + 2 * (k + b_k);
+          ldsm(gh, xh + at);
+          ldsm(gl, xl + at);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            mma_f16(acc[j + q], fl, gh[2 * q], gh[2 * q + 1]);
+            mma_f16(acc[j + q], fh, gl[2 * q], gl[2 * q + 1]);
+            mma_f16(acc[j + q], fh, gh[2 * q], gh[2 * q + 1]);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j) {
+        float* to = reinterpret_cast<float*>(dyn + L.at_p() + (rt * 16 + er) * L.kPitchP) + half * kCols + j * 8 + ec;
+        *reinterpret_cast<float2*>(to) = make_float2(acc[j][0], acc[j][1]);
+        *reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(to) + 8 * L.kPitchP) = make_float2(acc[j][2], acc[j][3]);
+      }
+    }
+    cluster_sync();
+    {   // rows rank, rank + ctas, ... of the sum, in the order of the ranks, to every CTA
+      const uint32_t share = (MP - rank + ctas - 1) / ctas;
+      for (uint32_t i = tid; i < share * (MP / 4); i += kSmallThreads) {
+        const uint32_t r = rank + (i / (MP / 4)) * ctas, c = i % (MP / 4) * 4, from = ps + r * L.kPitchP + 4 * c;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint32_t q = 0; q < ctas; ++q) {
+          const float4 v = ld_cluster4(in_cta(from, q));
+          s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+        }
+        uint32_t h0, h1, l0, l1;
+        split2(s.x * kDown, s.y * kDown, h0, l0);
+        split2(s.z * kDown, s.w * kDown, h1, l1);
+        const uint32_t to = ah + r * L.kPitchA + 2 * c;
+        for (uint32_t q = 0; q < ctas; ++q) {
+          st_cluster2(in_cta(to, q), h0, h1);
+          st_cluster2(in_cta(to + L.kHalfA, q), l0, l1);
+        }
+      }
+    }
+    cluster_sync();
+    {   // B = b A + c A A
+      float acc[kTiles][4] = {};
+#pragma unroll 2
+      for (uint32_t k = 0; k < MP; k += 16) {
+        uint32_t fh[4], fl[4];
+        ldsm(fh, ah + a_row * L.kPitchA + 2 * (k + a_k));
+        ldsm(fl, al + a_row * L.kPitchA + 2 * (k + a_k));
+#pragma unroll
+        for (int j = 0; j < kTiles; j += 2) {
+          uint32_t gh[4], gl[4];
+          const uint32_t at = (half * kCols + j * 8 + b_row) * L.kPitchA + 2 * (k + b_k);
+          ldsm(gh, ah + at);
+          ldsm(gl, al + at);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            mma_f16(acc[j + q], fl, gh[2 * q], gh[2 * q + 1]);
+            mma_f16(acc[j + q], fh, gl[2 * q], gl[2 * q + 1]);
+            mma_f16(acc[j + q], fh, gh[2 * q], gh[2 * q + 1]);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const uint32_t at = (rt * 16 + er + 8 * q) * L.kPitchA + 2 * (half * kCols + j * 8 + ec);
+          const float2 v = join2(*reinterpret_cast<const uint32_t*>(dyn + L.at_a() + at), *reinterpret_cast<const uint32_t*>(dyn + L.at_a() + L.kHalfA + at));
+          uint32_t h, l;
+          split2(fmaf(p.c, acc[j][2 * q] * kDown, p.b * v.x), fmaf(p.c, acc[j][2 * q + 1] * kDown, p.b * v.y), h, l);
+          *reinterpret_cast<uint32_t*>(dyn + L.at_p() + at) = h;
+          *reinterpret_cast<uint32_t*>(dyn + L.at_p() + L.kHalfA + at) = l;
+        }
+    }
+    __syncthreads();
+    // X = a X + B X, 64 columns at a time: they depend on themselves alone
+    for (uint32_t c1 = 0; c1 < p.w; c1 += kChunk) {
+      const uint32_t first = c1 + half * (kChunkTiles * 8);
+      float acc[kChunkTiles][4] = {};
+      if (first < p.w) {
+#pragma unroll 2
+        for (uint32_t k = 0; k < MP; k += 16) {
+          uint32_t fh[4], fl[4];
+          ldsm(fh, bh + a_row * L.kPitchA + 2 * (k + a_k));
+          ldsm(fl, bl + a_row * L.kPitchA + 2 * (k + a_k));
+#pragma unroll
+          for (int j = 0; j < kChunkTiles; j += 2) {
+            if (first + 8 * j >= p.w) continue;       // w is a multiple of 16: both tiles or none
+            uint32_t gh[4], gl[4];
+            const uint32_t at = (k + t_k) * L.pitch + 2 * (first + 8 * j + t_n);
+            ldsm_t(gh, xh + at);
+            ldsm_t(gl, xl + at);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              mma_f16(acc[j + q], fl, gh[2 * q], gh[2 * q + 1]);
+              mma_f16(acc[j + q], fh, gl[2 * q], gl[2 * q + 1]);
+              mma_f16(acc[j + q], fh, gh[2 * q], gh[2 * q + 1]);
+            }
+          }
+        }
+      }
+      __syncthreads();     // everybody has read these columns
+#pragma unroll
+      for (int j = 0; j < kChunkTiles; ++j) {
+        if (first + 8 * j >= p.w) continue;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const uint32_t at = (rt * 16 + er + 8 * q) * L.pitch + 2 * (first + 8 * j + ec);
+          uint32_t* ph = reinterpret_cast<uint32_t*>(dyn + at);
+          uint32_t* pl = reinterpret_cast<uint32_t*>(dyn + L.x_half() + at);
+          const float2 v = join2(*ph, *pl);
+          split2(fmaf(p.a, v.x, acc[j][2 * q] * kDown), fmaf(p.a, v.y, acc[j][2 * q + 1] * kDown), *ph, *pl);
+        }
+      }
+    }
+    __syncthreads();
+  }
+
+  for (uint32_t e = tid; e < total; e += kSmallThreads) {
+    uint64_t at;
+    uint32_t r, c;
+    place(e, at, r, c);
+    const float v = (__half2float(*reinterpret_cast<const __half*>(dyn + r * L.pitch + 2 * c)) +
+                     __half2float(*reinterpret_cast<const __half*>(dyn + L.x_half() + r * L.pitch + 2 * c))) * kDown;
+    if (p.to.out) {
+      const uint64_t o = (uint64_t)matrix * p.rows * p.cols + at;
+      if (p.to.dtype == DS_BF16)
+        static_cast<__nv_bfloat16*>(p.to.out)[o] = __float2bfloat16_rn(v);
+      else
+        static_cast<float*>(p.to.out)[o] = v;
+    }
+    if (p.to.x) {
+      float* x = p.to.x + (uint64_t)matrix * p.to.x_stride + at;
+      *x = __fsub_rn(__fmul_rn(p.to.keep, *x), __fmul_rn(p.to.rate, v));
+    }
+  }
+}
+
+uint32_t slice(uint32_t n, uint32_t ctas) { return ((n + ctas - 1) / ctas + 15) / 16 * 16; }
+constexpr uint32_t kSmallSmem = 225 * 1024;
+uint32_t small_bytes(uint32_t m, uint32_t w) { return m <= 64 ? SmallLayout<64>(w).bytes() : SmallLayout<128>(w).bytes(); }
+
+template <class T, int MP>
+cudaError_t launch(const SmallArgs& a, uint32_t ctas, uint32_t batch, cudaStream_t st) {
+  allow_smem_for<k_orth_small<T, MP>>(kSmallSmem);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(ctas * batch);
+  cfg.blockDim = dim3(kSmallThreads);
+  cfg.dynamicSmemBytes = SmallLayout<MP>(a.w).bytes();
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  (void)cudaLaunchKernelEx(&cfg, k_orth_small<T, MP>, a);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+namespace dsq {
+
+uint32_t orth_small_ctas(uint32_t m, uint32_t n, uint32_t batch) {
+  if (m > 128) return 0;
+  // slices of about 64 columns: narrower ones leave a CTA less work than the exchange costs
+  uint32_t c = 1;
+  while (c < kMaxCluster && n > 64 * c) c *= 2;
+  while (c < kMaxCluster && small_bytes(m, slice(n, c)) > kSmallSmem) c *= 2;
+  if (small_bytes(m, slice(n, c)) > kSmallSmem) return 0;
+  // many matrices fill the SMs with fewer CTAs each
+  while (c > 1 && (uint64_t)batch * c > (uint64_t)sm_count() && small_bytes(m, slice(n, c / 2)) <= kSmallSmem) c /= 2;
+  return c;
+}
+
+cudaError_t launch_orth_small(const ds_orth_config& c, uint32_t ctas, const Momentum& mo, int g_dtype, const OrthOut& o, cudaStream_t st) {
+  SmallArgs a{};
+  a.mo = mo;
+  a.to = o;
+  a.rows = c.rows;
+  a.cols = c.cols;
+  a.tall = c.rows > c.cols;
+  a.m = a.tall ? c.cols : c.rows;
+  a.n = a.tall ? c.rows : c.cols;
+  a.steps = c.steps;
+  a.w = slice(a.n, ctas);
+  a.a = c.a;
+  a.b = c.b;
+  a.c = c.c;
+  a.eps = c.eps;
+  if (a.m <= 64)
+    return g_dtype == DS_F32    ? launch<float, 64>(a, ctas, c.batch, st)
+           : g_dtype == DS_BF16 ? launch<__nv_bfloat16, 64>(a, ctas, c.batch, st)
+                                : launch<__half, 64>(a, ctas, c.batch, st);
+  return g_dtype == DS_F32    ? launch<float, 128>(a, ctas, c.batch, st)
+         : g_dtype == DS_BF16 ? launch<__nv_bfloat16, 128>(a, ctas, c.batch, st)
+                              : launch<__half, 128>(a, ctas, c.batch, st);
+}
+
+}  // namespace dsq

@@ -10,15 +10,18 @@ import math
 import torch
 
 from .binding import (DS_BF16, DS_DEV_MMA_TIMEOUT, DS_F16, DS_F32, DS_NEED_BUFFERS, DS_OK, DS_ORTH_NESTEROV, DsqError, ds_orth_config,
+                      fast_call,
                       load_library)
 
 _DTYPES = {torch.float32: DS_F32, torch.bfloat16: DS_BF16, torch.float16: DS_F16}
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _dtype(t: torch.dtype, what: str) -> int:
-    if t not in _DTYPES:
+    code = _DTYPES.get(t)
+    if code is None:
         raise TypeError(f"{what}: float32, bfloat16 or float16 expected, got {t}")
-    return _DTYPES[t]
+    return code
 
 
 def _check(rc: int, what: str):
@@ -26,40 +29,51 @@ def _check(rc: int, what: str):
         raise DsqError(rc, what, load_library().ds_last_error().decode())
 
 
-def _stream(t: torch.Tensor, stream) -> int:
-    return (stream if stream is not None else torch.cuda.current_stream(t.device)).cuda_stream
-
-
-def _need_cuda(*tensors):
+def _same_device(device: torch.device, *tensors):
     for t in tensors:
-        if t is not None and not t.is_cuda:
-            raise ValueError("CUDA tensors expected: there is no CPU path")
-        if t is not None and t.device != tensors[0].device:
-            raise ValueError("tensors on different devices")
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on different devices: {device} and {t.device}")
 
 
-def _matrix(x: torch.Tensor, what: str) -> tuple[torch.Tensor, int]:
-    """x as rows of consecutive entries, and the distance between rows."""
-    if x.dim() != 2:
-        raise ValueError(f"{what}: a matrix expected, got {x.dim()} dimensions")
-    if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+def _matrix(x: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int, torch.device]:
+    """x as rows of consecutive entries; rows, columns, the distance between rows, the device."""
+    device = x.device
+    if device.type != "cuda":
+        raise ValueError(f"{what}: a CUDA tensor expected: there is no CPU path")
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"{what}: a matrix expected, got {len(shape)} dimensions")
+    r, c = shape
+    ld, step = x.stride()
+    if (c > 1 and step != 1) or (r > 1 and ld < c):
         x = x.contiguous()
-    return x, (x.stride(0) if x.shape[0] > 1 else x.shape[1])
+        ld = c
+    return x, r, c, (ld if r > 1 else c), device
 
 
-def _vector(v: torch.Tensor | None, n: int, what: str):
-    if v is not None and (v.dtype != torch.float32 or v.shape != (n,) or not v.is_contiguous()):
+def _vector(v: torch.Tensor | None, n: int, what: str) -> int | None:
+    """The address of n contiguous float32 values, or None."""
+    if v is None:
+        return None
+    if v.dtype is not torch.float32 or v.dim() != 1 or v.shape[0] != n or not v.is_contiguous():
         raise ValueError(f"{what}: {n} contiguous float32 values expected, got {v.dtype} {tuple(v.shape)}")
+    return v.data_ptr()
 
 
-_status: dict = {}
+def _stream_of(device: torch.device, stream) -> int:
+    return _raw_stream(device.index) if stream is None else stream.cuda_stream
 
 
-def _dev_status(device: torch.device) -> torch.Tensor:
-    """The device word in which products report waits that ran out (one per device, kept)."""
-    if device not in _status:
-        _status[device] = torch.zeros(1, dtype=torch.int32, device=device)
-    return _status[device]
+_status: dict = {}     # device -> (word in which products report waits that ran out, its address)
+
+
+def _dev_status(device: torch.device) -> int:
+    entry = _status.get(device)
+    if entry is None:
+        word = torch.zeros(1, dtype=torch.int32, device=device)
+        torch.cuda.synchronize(device)          # cleared before any stream's product may set it
+        entry = _status[device] = (word, word.data_ptr())
+    return entry[1]
 
 
 def device_status(device: str | torch.device = "cuda") -> int:
@@ -67,44 +81,69 @@ def device_status(device: str | torch.device = "cuda") -> int:
     device = torch.device(device)
     if device.index is None:
         device = torch.device(device.type, torch.cuda.current_device())
-    return int(_dev_status(device).item())
+    _dev_status(device)
+    return int(_status[device][0].item())
+
+
+def _up(v: int, to: int) -> int:
+    return (v + to - 1) // to * to
 
 
 class Int8Matrix:
     """Codes [rows, cols] (int8) with one float32 scale per row: row r stands for codes[r] * scale[r].
     Rows must start on 16-byte boundaries (int8_quantize gives such; pack() copies into such)."""
 
-    __slots__ = ("codes", "scale")
+    __slots__ = ("rows", "cols", "ld", "device", "codes_ptr", "scale_ptr", "_codes", "_scale")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor):
-        if codes.dtype != torch.int8 or codes.dim() != 2 or (codes.shape[1] > 1 and codes.stride(1) != 1):
+        device = codes.device
+        if codes.dtype is not torch.int8 or codes.dim() != 2:
             raise ValueError("codes: a row-major int8 matrix expected")
-        _vector(scale, codes.shape[0], "scale")
-        _need_cuda(codes, scale)
-        self.codes, self.scale = codes, scale
+        self.rows, self.cols = r, c = codes.shape
+        ld, step = codes.stride()
+        if c > 1 and step != 1:
+            raise ValueError("codes: a row-major int8 matrix expected")
+        if device.type != "cuda" or scale.device != device:
+            raise ValueError("CUDA tensors on one device expected: there is no CPU path")
+        self.ld = ld if r > 1 else _up(c, 16)
+        self.device = device
+        self._codes, self._scale = codes, scale
+        self.codes_ptr, self.scale_ptr = codes.data_ptr(), _vector(scale, r, "scale")
+
+    @classmethod
+    def _within(cls, buf: torch.Tensor, base: int, at: int, scale_at: int, rows: int, cols: int, ld: int, device) -> "Int8Matrix":
+        """Codes and scales at two offsets of one byte buffer whose address is `base`; views are made when asked for."""
+        m = cls.__new__(cls)
+        m.rows, m.cols, m.ld, m.device = rows, cols, ld, device
+        m.codes_ptr, m.scale_ptr = base + at, base + scale_at
+        m._codes, m._scale = (buf, at), (buf, scale_at)
+        return m
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if isinstance(self._codes, tuple):
+            buf, at = self._codes
+            self._codes = buf.view(torch.int8).as_strided((self.rows, self.cols), (self.ld, 1), at)
+        return self._codes
+
+    @property
+    def scale(self) -> torch.Tensor:
+        if isinstance(self._scale, tuple):
+            buf, at = self._scale
+            self._scale = buf[at:at + 4 * self.rows].view(torch.float32)
+        return self._scale
 
     @property
     def shape(self):
-        return self.codes.shape
-
-    @property
-    def ld(self) -> int:
-        r, c = self.codes.shape
-        return self.codes.stride(0) if r > 1 else (c + 15) // 16 * 16
-
-    @classmethod
-    def empty(cls, rows: int, cols: int, device) -> "Int8Matrix":
-        pitch = max(16, (cols + 15) // 16 * 16)
-        return cls(torch.empty(rows, pitch, dtype=torch.int8, device=device)[:, :cols],
-                   torch.empty(rows, dtype=torch.float32, device=device))
+        return torch.Size((self.rows, self.cols))
 
     @classmethod
     def pack(cls, codes: torch.Tensor, scale: torch.Tensor) -> "Int8Matrix":
         """A copy of any int8 matrix with its rows on 16-byte boundaries."""
-        m = cls.empty(*codes.shape, codes.device)
-        m.codes.copy_(codes)
-        m.scale.copy_(scale)
-        return m
+        r, c = codes.shape
+        out = torch.empty(r, max(16, _up(c, 16)), dtype=torch.int8, device=codes.device)[:, :c]
+        out.copy_(codes)
+        return cls(out, scale.to(torch.float32, copy=True))
 
     def dequantize(self) -> torch.Tensor:
         return self.codes.float() * self.scale[:, None]
@@ -115,68 +154,77 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
     sums, in that order; one thing asked for is returned by itself, several as a tuple."""
     if not (rows or cols or col_sum):
         raise ValueError("nothing to compute")
-    _need_cuda(x)
     dt = _dtype(x.dtype, "x")
-    x, ld = _matrix(x, "x")
-    r, c = x.shape
-    lib = load_library()
-    by_r = Int8Matrix.empty(r, c, x.device) if rows else None
-    by_c = Int8Matrix.empty(c, r, x.device) if cols else None
-    total = torch.empty(c, dtype=torch.float32, device=x.device) if col_sum else None
-    ws = None
-    if cols or col_sum:
-        ws = torch.empty(lib.ds_i8_quantize_workspace(r, c, int(col_sum)), dtype=torch.uint8, device=x.device)
-    _check(lib.ds_i8_quantize(x.data_ptr(), dt, r, c, ld,
-                              by_r.codes.data_ptr() if rows else None, by_r.ld if rows else 0, by_r.scale.data_ptr() if rows else None,
-                              by_c.codes.data_ptr() if cols else None, by_c.ld if cols else 0, by_c.scale.data_ptr() if cols else None,
-                              None if total is None else total.data_ptr(), None if ws is None else ws.data_ptr(),
-                              0 if ws is None else ws.numel(), _stream(x, stream)), "ds_i8_quantize")
-    got = [v for v in (by_r, by_c, total) if v is not None]
+    x, r, c, ld, device = _matrix(x, "x")
+    call, address = fast_call()
+    # one buffer: codes, scales, sums, and at its end what only the call itself uses
+    ldr, ldc = max(16, _up(c, 16)), max(16, _up(r, 16))
+    at_c = r * ldr if rows else 0
+    at_rs = at_c + (c * ldc if cols else 0)
+    at_cs = at_rs + (_up(4 * r, 16) if rows else 0)
+    at_sum = at_cs + (_up(4 * c, 16) if cols else 0)
+    at_ws = at_sum + (_up(4 * c, 16) if col_sum else 0)
+    ws = load_library().ds_i8_quantize_workspace(r, c, 1 if col_sum else 0) if cols or col_sum else 0
+    buf = torch.empty(at_ws + ws + 16, dtype=torch.uint8, device=device)
+    base = buf.data_ptr()
+    _check(call(address["ds_i8_quantize"], x.data_ptr(), dt, r, c, ld, base if rows else 0, ldr, base + at_rs if rows else 0,
+                base + at_c if cols else 0, ldc, base + at_cs if cols else 0, base + at_sum if col_sum else 0,
+                base + at_ws if ws else 0, ws, _stream_of(device, stream)), "ds_i8_quantize")
+    got = []
+    if rows:
+        got.append(Int8Matrix._within(buf, base, 0, at_rs, r, c, ldr, device))
+    if cols:
+        got.append(Int8Matrix._within(buf, base, at_c, at_cs, c, r, ldc, device))
+    if col_sum:
+        got.append(buf[at_sum:at_sum + 4 * c].view(torch.float32))
     return got[0] if len(got) == 1 else tuple(got)
 
 
-def _out(out, shape, dtype, device):
+def _out(out: torch.Tensor | None, m: int, n: int, dtype: torch.dtype, device) -> tuple[torch.Tensor, int, int]:
+    """The output, its type, the distance between its rows."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(shape) or (out.shape[1] > 1 and out.stride(1) != 1) or (out.shape[0] > 1 and out.stride(0) < out.shape[1]):
-        raise ValueError(f"out: a row-major matrix {tuple(shape)} expected, got {tuple(out.shape)}")
-    return out
+        return torch.empty((m, n), dtype=dtype, device=device), _dtype(dtype, "out"), n
+    if out.shape != (m, n) or out.device != device:
+        raise ValueError(f"out: a matrix {(m, n)} on {device} expected, got {tuple(out.shape)} on {out.device}")
+    ld, step = out.stride()
+    if (n > 1 and step != 1) or (m > 1 and ld < n):
+        raise ValueError("out: rows of consecutive entries expected")
+    return out, _dtype(out.dtype, "out"), (ld if m > 1 else n)
 
 
 def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """a b^T (+ bias): [a rows, b rows], the sums exact in 32-bit integers."""
-    if a.shape[1] != b.shape[1]:
-        raise ValueError(f"lengths differ: {a.shape[1]} and {b.shape[1]}")
-    m, n, k = a.shape[0], b.shape[0], a.shape[1]
-    _vector(bias, n, "bias")
-    _need_cuda(a.codes, b.codes, bias, out)
-    out = _out(out, (m, n), out_dtype, a.codes.device)
-    ldo = out.stride(0) if m > 1 else n
-    _check(load_library().ds_i8_matmul(a.codes.data_ptr(), a.ld, a.scale.data_ptr(), b.codes.data_ptr(), b.ld, b.scale.data_ptr(),
-                                       None if bias is None else bias.data_ptr(), m, n, k, out.data_ptr(), _dtype(out.dtype, "out"), ldo,
-                                       _dev_status(out.device).data_ptr(), _stream(out, stream)), "ds_i8_matmul")
+    if a.cols != b.cols:
+        raise ValueError(f"lengths differ: {a.cols} and {b.cols}")
+    device = a.device
+    bp = _vector(bias, b.rows, "bias")
+    if b.device != device or (bias is not None and bias.device != device):
+        raise ValueError("tensors on different devices")
+    out, odt, ldo = _out(out, a.rows, b.rows, out_dtype, device)
+    call, address = fast_call()
+    _check(call(address["ds_i8_matmul"], a.codes_ptr, a.ld, a.scale_ptr, b.codes_ptr, b.ld, b.scale_ptr, bp, a.rows, b.rows, a.cols,
+                out.data_ptr(), odt, ldo, _dev_status(device), _stream_of(device, stream)), "ds_i8_matmul")
     return out
 
 
 def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """x W^T (+ bias) for weights quantised before: x [tokens, k] is quantised by rows on the way."""
-    _need_cuda(x, w.codes, bias, out)
     dt = _dtype(x.dtype, "x")
-    x, ld = _matrix(x, "x")
-    m, k = x.shape
-    n = w.shape[0]
-    if w.shape[1] != k:
-        raise ValueError(f"x has {k} columns, the weights {w.shape[1]}")
-    _vector(bias, n, "bias")
-    out = _out(out, (m, n), out_dtype or x.dtype, x.device)
-    lib = load_library()
-    ws = torch.empty(max(16, lib.ds_i8_linear_workspace(m, k)), dtype=torch.uint8, device=x.device)
-    _check(lib.ds_i8_linear(x.data_ptr(), dt, m, k, ld, w.codes.data_ptr(), w.ld, w.scale.data_ptr(),
-                            None if bias is None else bias.data_ptr(), n, out.data_ptr(), _dtype(out.dtype, "out"),
-                            out.stride(0) if m > 1 else n, ws.data_ptr(), ws.numel(), _dev_status(x.device).data_ptr(),
-                            _stream(x, stream)), "ds_i8_linear")
+    x, m, k, ld, device = _matrix(x, "x")
+    n = w.rows
+    if w.cols != k:
+        raise ValueError(f"x has {k} columns, the weights {w.cols}")
+    bp = _vector(bias, n, "bias")
+    if w.device != device or (bias is not None and bias.device != device):
+        raise ValueError("tensors on different devices")
+    out, odt, ldo = _out(out, m, n, out_dtype or x.dtype, device)
+    call, address = fast_call()
+    size = load_library().ds_i8_linear_workspace(m, k, n)
+    ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+    _check(call(address["ds_i8_linear"], x.data_ptr(), dt, m, k, ld, w.codes_ptr, w.ld, w.scale_ptr, bp, n, out.data_ptr(), odt, ldo,
+                None if ws is None else ws.data_ptr(), size, _dev_status(device), _stream_of(device, stream)), "ds_i8_linear")
     return out
 
 
@@ -210,8 +258,8 @@ class Int8Linear:
         a gradient row of DoubleSqueeze."""
         if self._x_cols is None or self.by_cols is None:
             raise RuntimeError("backward needs a forward with training=True before it")
-        if dy.dim() != 2 or dy.shape != (self._x_cols.shape[1], self.by_rows.shape[0]):
-            raise ValueError(f"dy: {(self._x_cols.shape[1], self.by_rows.shape[0])} expected, got {tuple(dy.shape)}")
+        if dy.dim() != 2 or dy.shape != (self._x_cols.cols, self.by_rows.rows):
+            raise ValueError(f"dy: {(self._x_cols.cols, self.by_rows.rows)} expected, got {tuple(dy.shape)}")
         got = int8_quantize(dy, rows=True, cols=True, col_sum=self.bias is not None, stream=stream)
         dx = int8_matmul(got[0], self.by_cols, out_dtype=dx_dtype or dy.dtype, stream=stream)
         dw = int8_matmul(got[1], self._x_cols, out_dtype=dw_dtype, out=dw, stream=stream)
@@ -271,7 +319,7 @@ class OrthUpdate:
         xp = self._span(x, "x", (torch.float32,))
         _check(self.lib.ds_orth_update(self.handle, gp, _DTYPES[g.dtype], mp, None if out is None else out.data_ptr(),
                                        DS_F32 if out is None else _DTYPES[out.dtype], xp, gamma, decay,
-                                       _stream(g, stream)), "ds_orth_update")
+                                       _stream_of(self.device, stream)), "ds_orth_update")
         return out
 
     def timed_out(self) -> bool:

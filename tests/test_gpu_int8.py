@@ -307,7 +307,7 @@ def test_refusals():
     assert lib.ds_i8_linear(p + 2, 0, 8, 64, 64, *args) == binding.DS_ERR_ALIGN
     assert lib.ds_i8_linear(p, 0, 8, big, big, *args) == binding.DS_ERR_UNSUPPORTED
     small = args[:9] + (16, None, None)
-    assert lib.ds_i8_linear(p, 0, 8, 64, 64, *small) == binding.DS_ERR_BUFFER_TOO_SMALL
+    assert lib.ds_i8_linear(p, 0, 64, 64, 64, *small) == binding.DS_ERR_BUFFER_TOO_SMALL
     q = torch.zeros(8, 64, dtype=torch.int8, device="cuda")
     assert lib.ds_i8_quantize(p, 0, 8, 64, 64, q.data_ptr(), 64, None, None, 0, None, None, None, 0, None) == binding.DS_ERR_INVALID_ARG
     assert lib.ds_i8_quantize(p, 0, 8, 64, 64, q.data_ptr(), 72, p, None, 0, None, None, None, 0, None) == binding.DS_ERR_ALIGN
