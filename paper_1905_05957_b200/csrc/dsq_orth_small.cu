@@ -14,8 +14,10 @@ using namespace dsq;
 
 namespace {
 
-constexpr int kSmallThreads = 256;
+constexpr int kSmallThreads = 512, kSmallWarps = kSmallThreads / 32;
 constexpr int kMaxCluster = 8;
+// (Loops here are unrolled no further than they are written: the whole kernel runs in some ten thousand cycles, and fetching its
+// instructions for the first time is a good part of them.  A form with everything unrolled took twice as long.)
 
 __device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -24,7 +26,7 @@ __device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -76,10 +78,10 @@ struct SmallArgs {
 
 template <class T, int MP>
 __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs p) {
-  constexpr int kRowTiles = MP / 16, kHalves = 8 / kRowTiles, kCols = MP / kHalves, kTiles = kCols / 8;
-  constexpr int kChunk = 64, kChunkTiles = kChunk / kHalves / 8;
+  constexpr int kRowTiles = MP / 16, kHalves = kSmallWarps / kRowTiles, kCols = MP / kHalves, kTiles = kCols / 8;
+  constexpr int kChunkTiles = MP == 64 ? 4 : 8, kChunk = kHalves * kChunkTiles * 8;    // 128 columns at a time
   extern __shared__ __align__(16) uint8_t dyn[];
-  __shared__ double sums[kMaxCluster], warp_sum[kSmallThreads / 32];
+  __shared__ double sums[kMaxCluster], warp_sum[kSmallWarps];
   pdl_prologue();
   const SmallLayout<MP> L(p.w);
   const uint32_t base = smem_u32(dyn), xh = base, xl = base + L.x_half(), ah = base + L.at_a(), al = ah + L.kHalfA, ps = base + L.at_p(),
@@ -93,34 +95,42 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs
   const T* g = static_cast<const T*>(p.mo.g) + off;
   float* buf = p.mo.buf ? p.mo.buf + off : nullptr;
 
-  // Entry e of the slice: where it is in the matrix, and in X.  Consecutive entries are consecutive in memory.
-  const uint32_t total = p.m * mine;
-  auto place = [&](uint32_t e, uint64_t& at, uint32_t& r, uint32_t& c) {
-    if (p.tall) {          // X = u^T: the slice is rows c0.. of u, all of their m entries
-      c = e / p.m;
-      r = e - c * p.m;
-      at = (uint64_t)(c0 + c) * p.m + r;
-    } else {
-      r = e / mine;
-      c = e - r * mine;
-      at = (uint64_t)r * p.n + c0 + c;
-    }
+  // The slice is `lines` runs of `run` consecutive entries in memory, `apart` entries from one to the next: pieces of the rows of X, or,
+  // where X = u^T, whole rows of u, each a column of X.
+  const uint32_t lines = p.tall ? mine : p.m, run = p.tall ? p.m : mine, apart = p.tall ? p.m : p.n;
+  const uint64_t start = p.tall ? (uint64_t)c0 * p.m : c0;
+  const uint32_t x_line = p.tall ? 2 : L.pitch, x_entry = p.tall ? L.pitch : 2;       // bytes between the same in X
+  // visits (line, entry) pairs: a warp takes four lines at a time, so that their loads run together
+  auto visit = [&](auto&& load, auto&& use) {
+#pragma unroll 1
+    for (uint32_t l0 = warp * 4; l0 < lines; l0 += kSmallWarps * 4)
+#pragma unroll 1
+      for (uint32_t i = lane; i < run; i += 32) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (l0 + q < lines) load(q, start + (uint64_t)(l0 + q) * apart + i);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (l0 + q < lines) use(q, start + (uint64_t)(l0 + q) * apart + i, (l0 + q) * x_line + i * x_entry);
+      }
   };
 
   // momentum and norm
   double sum = 0;
-  for (uint32_t e = tid; e < total; e += kSmallThreads) {
-    uint64_t at;
-    uint32_t r, c;
-    place(e, at, r, c);
-    float u = to_f32(g[at]);
+  float gv[4], bv[4];
+  auto load = [&](int q, uint64_t at) {
+    gv[q] = to_f32(g[at]);
+    if (buf) bv[q] = buf[at];
+  };
+  visit(load, [&](int q, uint64_t at, uint32_t) {
+    float u = gv[q];
     if (buf) {
-      const float v = p.mo.update(u, buf[at]);
+      const float v = p.mo.update(u, bv[q]);
       buf[at] = v;
       u = p.mo.direction(u, v);
     }
     sum += (double)u * (double)u;
-  }
+  });
 #pragma unroll
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
   if (lane == 0) warp_sum[warp] = sum;
@@ -129,24 +139,19 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs
   cluster_sync();          // every CTA of the cluster runs: its shared memory may be written
   if (tid < (int)ctas) {
     double s = 0;
-    for (int i = 0; i < kSmallThreads / 32; ++i) s += warp_sum[i];
+    for (int i = 0; i < kSmallWarps; ++i) s += warp_sum[i];
     st_cluster_f64(in_cta(smem_u32(&sums[rank]), tid), s);
   }
   cluster_sync();
   double norm2 = 0;
   for (uint32_t i = 0; i < ctas; ++i) norm2 += sums[i];
   const float scale = kUp / ((float)sqrt(norm2) + p.eps);
-  for (uint32_t e = tid; e < total; e += kSmallThreads) {
-    uint64_t at;
-    uint32_t r, c;
-    place(e, at, r, c);
-    float u = to_f32(g[at]);
-    if (buf) u = p.mo.direction(u, buf[at]);
-    const float v = __fmul_rn(u, scale);
+  visit(load, [&](int q, uint64_t, uint32_t at_x) {
+    const float v = __fmul_rn(buf ? p.mo.direction(gv[q], bv[q]) : gv[q], scale);
     const __half h = __float2half_rn(v);
-    *reinterpret_cast<__half*>(dyn + r * L.pitch + 2 * c) = h;
-    *reinterpret_cast<__half*>(dyn + L.x_half() + r * L.pitch + 2 * c) = __float2half_rn(v - __half2float(h));
-  }
+    *reinterpret_cast<__half*>(dyn + at_x) = h;
+    *reinterpret_cast<__half*>(dyn + L.x_half() + at_x) = __float2half_rn(v - __half2float(h));
+  });
   __syncthreads();
 
   const int rt = warp % kRowTiles, half = warp / kRowTiles;
@@ -155,26 +160,46 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs
   const uint32_t t_k = lane & 15, t_n = (lane >> 4) * 8;                                     // the other's, across K
   const int er = lane >> 2, ec = 2 * (lane & 3);                                             // accumulators: rows er, er + 8
 
+#pragma unroll 1
   for (uint32_t step = 0; step < p.steps; ++step) {
-    {   // this slice's share of A = X X^T
+    // first this slice's share of A = X X^T, then A A: the same sums over other rows
+#pragma unroll 1
+    for (int second = 0; second < 2; ++second) {
+      const uint32_t oh = second ? ah : xh, ol = second ? al : xl, pitch = second ? L.kPitchA : L.pitch, len = second ? MP : p.w;
       float acc[kTiles][4] = {};
-      for (uint32_t k = 0; k < p.w; k += 16) {
+#pragma unroll 1
+      for (uint32_t k = 0; k < len; k += 16) {
         uint32_t fh[4], fl[4];
-        ldsm(fh, xh + a_row * L.pitch + 2 * (k + a_k));
-        ldsm(fl, xl + a_row * L.pitch + 2 * (k + a_k));
+        ldsm(fh, oh + a_row * pitch + 2 * (k + a_k));
+        ldsm(fl, ol + a_row * pitch + 2 * (k + a_k));
 #pragma unroll
         for (int j = 0; j < kTiles; j += 2) {
           uint32_t gh[4], gl[4];
-          const uint32_t at = (half * kCols + j * 8 + b_row) * L.pitch + 2 * (k + b_k);
-          ldsm(gh, xh + at);
-          ldsm(gl, xl + at);
+          const uint32_t at = (half * kCols + j * 8 + b_row) * pitch + 2 * (k + b_k);
+          ldsm(gh, oh + at);
+          ldsm(gl, ol + at);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) mma_f16(acc[j + q], fl, gh[2 * q], gh[2 * q + 1]);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) mma_f16(acc[j + q], fh, gl[2 * q], gl[2 * q + 1]);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) mma_f16(acc[j + q], fh, gh[2 * q], gh[2 * q + 1]);
+        }
+      }
+      if (second) {   // B = b A + c A A
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j)
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
-            mma_f16(acc[j + q], fl, gh[2 * q], gh[2 * q + 1]);
-            mma_f16(acc[j + q], fh, gl[2 * q], gl[2 * q + 1]);
-            mma_f16(acc[j + q], fh, gh[2 * q], gh[2 * q + 1]);
+            const uint32_t at = (rt * 16 + er + 8 * q) * L.kPitchA + 2 * (half * kCols + j * 8 + ec);
+            const float2 v = join2(*reinterpret_cast<const uint32_t*>(dyn + L.at_a() + at), *reinterpret_cast<const uint32_t*>(dyn + L.at_a() + L.kHalfA + at));
+            uint32_t h, l;
+            split2(fmaf(p.c, acc[j][2 * q] * kDown, p.b * v.x), fmaf(p.c, acc[j][2 * q + 1] * kDown, p.b * v.y), h, l);
+            *reinterpret_cast<uint32_t*>(dyn + L.at_p() + at) = h;
+            *reinterpret_cast<uint32_t*>(dyn + L.at_p() + L.kHalfA + at) = l;
           }
-        }
+        __syncthreads();
+        break;
       }
 #pragma unroll
       for (int j = 0; j < kTiles; ++j) {
@@ -182,68 +207,38 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs
         *reinterpret_cast<float2*>(to) = make_float2(acc[j][0], acc[j][1]);
         *reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(to) + 8 * L.kPitchP) = make_float2(acc[j][2], acc[j][3]);
       }
-    }
-    cluster_sync();
-    {   // rows rank, rank + ctas, ... of the sum, in the order of the ranks, to every CTA
+      cluster_sync();
+      // rows rank, rank + ctas, ... of the sum, in the order of the ranks, to every CTA
       const uint32_t share = (MP - rank + ctas - 1) / ctas;
+#pragma unroll 1
       for (uint32_t i = tid; i < share * (MP / 4); i += kSmallThreads) {
         const uint32_t r = rank + (i / (MP / 4)) * ctas, c = i % (MP / 4) * 4, from = ps + r * L.kPitchP + 4 * c;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (uint32_t q = 0; q < ctas; ++q) {
-          const float4 v = ld_cluster4(in_cta(from, q));
-          s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-        }
+        float4 v[kMaxCluster], s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (uint32_t q = 0; q < kMaxCluster; ++q)
+          if (q < ctas) v[q] = ld_cluster4(in_cta(from, q));
+#pragma unroll
+        for (uint32_t q = 0; q < kMaxCluster; ++q)
+          if (q < ctas) s.x += v[q].x, s.y += v[q].y, s.z += v[q].z, s.w += v[q].w;
         uint32_t h0, h1, l0, l1;
         split2(s.x * kDown, s.y * kDown, h0, l0);
         split2(s.z * kDown, s.w * kDown, h1, l1);
         const uint32_t to = ah + r * L.kPitchA + 2 * c;
+#pragma unroll 1
         for (uint32_t q = 0; q < ctas; ++q) {
           st_cluster2(in_cta(to, q), h0, h1);
           st_cluster2(in_cta(to + L.kHalfA, q), l0, l1);
         }
       }
+      cluster_sync();
     }
-    cluster_sync();
-    {   // B = b A + c A A
-      float acc[kTiles][4] = {};
-#pragma unroll 2
-      for (uint32_t k = 0; k < MP; k += 16) {
-        uint32_t fh[4], fl[4];
-        ldsm(fh, ah + a_row * L.kPitchA + 2 * (k + a_k));
-        ldsm(fl, al + a_row * L.kPitchA + 2 * (k + a_k));
-#pragma unroll
-        for (int j = 0; j < kTiles; j += 2) {
-          uint32_t gh[4], gl[4];
-          const uint32_t at = (half * kCols + j * 8 + b_row) * L.kPitchA + 2 * (k + b_k);
-          ldsm(gh, ah + at);
-          ldsm(gl, al + at);
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            mma_f16(acc[j + q], fl, gh[2 * q], gh[2 * q + 1]);
-            mma_f16(acc[j + q], fh, gl[2 * q], gl[2 * q + 1]);
-            mma_f16(acc[j + q], fh, gh[2 * q], gh[2 * q + 1]);
-          }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kTiles; ++j)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const uint32_t at = (rt * 16 + er + 8 * q) * L.kPitchA + 2 * (half * kCols + j * 8 + ec);
-          const float2 v = join2(*reinterpret_cast<const uint32_t*>(dyn + L.at_a() + at), *reinterpret_cast<const uint32_t*>(dyn + L.at_a() + L.kHalfA + at));
-          uint32_t h, l;
-          split2(fmaf(p.c, acc[j][2 * q] * kDown, p.b * v.x), fmaf(p.c, acc[j][2 * q + 1] * kDown, p.b * v.y), h, l);
-          *reinterpret_cast<uint32_t*>(dyn + L.at_p() + at) = h;
-          *reinterpret_cast<uint32_t*>(dyn + L.at_p() + L.kHalfA + at) = l;
-        }
-    }
-    __syncthreads();
-    // X = a X + B X, 64 columns at a time: they depend on themselves alone
+    // X = a X + B X, some columns at a time: they depend on themselves alone
+#pragma unroll 1
     for (uint32_t c1 = 0; c1 < p.w; c1 += kChunk) {
       const uint32_t first = c1 + half * (kChunkTiles * 8);
       float acc[kChunkTiles][4] = {};
       if (first < p.w) {
-#pragma unroll 2
+#pragma unroll 1
         for (uint32_t k = 0; k < MP; k += 16) {
           uint32_t fh[4], fl[4];
           ldsm(fh, bh + a_row * L.kPitchA + 2 * (k + a_k));
@@ -256,11 +251,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs
             ldsm_t(gh, xh + at);
             ldsm_t(gl, xl + at);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              mma_f16(acc[j + q], fl, gh[2 * q], gh[2 * q + 1]);
-              mma_f16(acc[j + q], fh, gl[2 * q], gl[2 * q + 1]);
-              mma_f16(acc[j + q], fh, gh[2 * q], gh[2 * q + 1]);
-            }
+            for (int q = 0; q < 2; ++q) mma_f16(acc[j + q], fl, gh[2 * q], gh[2 * q + 1]);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) mma_f16(acc[j + q], fh, gl[2 * q], gl[2 * q + 1]);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) mma_f16(acc[j + q], fh, gh[2 * q], gh[2 * q + 1]);
           }
         }
       }
@@ -281,24 +276,20 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs
     __syncthreads();
   }
 
-  for (uint32_t e = tid; e < total; e += kSmallThreads) {
-    uint64_t at;
-    uint32_t r, c;
-    place(e, at, r, c);
-    const float v = (__half2float(*reinterpret_cast<const __half*>(dyn + r * L.pitch + 2 * c)) +
-                     __half2float(*reinterpret_cast<const __half*>(dyn + L.x_half() + r * L.pitch + 2 * c))) * kDown;
-    if (p.to.out) {
-      const uint64_t o = (uint64_t)matrix * p.rows * p.cols + at;
-      if (p.to.dtype == DS_BF16)
-        static_cast<__nv_bfloat16*>(p.to.out)[o] = __float2bfloat16_rn(v);
-      else
-        static_cast<float*>(p.to.out)[o] = v;
-    }
-    if (p.to.x) {
-      float* x = p.to.x + (uint64_t)matrix * p.to.x_stride + at;
-      *x = __fsub_rn(__fmul_rn(p.to.keep, *x), __fmul_rn(p.to.rate, v));
-    }
-  }
+  float xv[4];
+  visit([&](int q, uint64_t at) { xv[q] = p.to.x ? p.to.x[(uint64_t)matrix * p.to.x_stride + at] : 0.f; },
+        [&](int q, uint64_t at, uint32_t at_x) {
+          const float v = (__half2float(*reinterpret_cast<const __half*>(dyn + at_x)) +
+                           __half2float(*reinterpret_cast<const __half*>(dyn + L.x_half() + at_x))) * kDown;
+          const uint64_t o = (uint64_t)matrix * p.rows * p.cols + at;
+          if (p.to.out) {
+            if (p.to.dtype == DS_BF16)
+              static_cast<__nv_bfloat16*>(p.to.out)[o] = __float2bfloat16_rn(v);
+            else
+              static_cast<float*>(p.to.out)[o] = v;
+          }
+          if (p.to.x) p.to.x[(uint64_t)matrix * p.to.x_stride + at] = __fsub_rn(__fmul_rn(p.to.keep, xv[q]), __fmul_rn(p.to.rate, v));
+        });
 }
 
 uint32_t slice(uint32_t n, uint32_t ctas) { return ((n + ctas - 1) / ctas + 15) / 16 * 16; }
