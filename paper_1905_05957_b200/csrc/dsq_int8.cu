@@ -290,6 +290,7 @@ __device__ __forceinline__ void pack4f(uint32_t* w, float a, float b, float c, f
 // Rows of out start on 32-byte boundaries, sb and bias on 16.
 template <class T>
 struct EpiScale {
+  static constexpr int kIn = 0, kOut = 0;
   struct Pre {
     float s;
   };
@@ -331,6 +332,7 @@ struct EpiScale {
 // consecutive channels, so a token's outputs leave as 64 or 128 consecutive bytes.
 template <class T>
 struct EpiScaleTurned {
+  static constexpr int kIn = 0, kOut = 0;
   struct Pre {
     float s, c;
   };

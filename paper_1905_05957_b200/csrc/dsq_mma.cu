@@ -36,6 +36,7 @@ int sm_count() {
 }
 
 namespace {
+constexpr size_t kProbeSmem = 226 * 1024;     // about what the kernels take: one CTA an SM
 __global__ void __launch_bounds__(kMmaThreads, 1) k_cluster_probe() {}   // never launched: asked about
 }
 
@@ -46,11 +47,11 @@ int cluster_count(uint32_t size) {
   if (size < 2 || size > 8 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
   n = known[dev][size].load(std::memory_order_relaxed);
   if (!n) {
-    (void)cudaFuncSetAttribute(k_cluster_probe, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPairSmem);
+    (void)cudaFuncSetAttribute(k_cluster_probe, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kProbeSmem);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(size * (sm_count() / size));
     cfg.blockDim = dim3(kMmaThreads);
-    cfg.dynamicSmemBytes = kPairSmem;
+    cfg.dynamicSmemBytes = kProbeSmem;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = size;
@@ -67,7 +68,7 @@ int cluster_count(uint32_t size) {
 }
 
 cudaError_t make_tensor_map(CUtensorMap* map, int kind, const void* base, uint64_t cols, uint64_t rows, uint64_t batch, uint64_t ld,
-                            uint64_t batch_stride, uint32_t box_cols, uint32_t box_rows) {
+                            uint64_t batch_stride, uint32_t box_cols, uint32_t box_rows, bool block) {
   const EncodeFn fn = encoder();
   if (!fn) return cudaErrorNotSupported;
   const uint64_t size = kind == kMmaF16 ? 2 : 1;
@@ -77,7 +78,7 @@ cudaError_t make_tensor_map(CUtensorMap* map, int kind, const void* base, uint64
   const cuuint32_t step[3] = {1, 1, 1};
   const CUresult r = fn(map, kind == kMmaF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 3,
                         const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                        block ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 

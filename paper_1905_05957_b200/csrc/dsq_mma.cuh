@@ -122,7 +122,17 @@ __device__ __forceinline__ void st_b32(void* p, const uint32_t* w) {
                "r"(w[5]), "r"(w[6]), "r"(w[7])
                : "memory");
 }
-__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Ends when the loads before have arrived.  The registers pass through it, so that nothing that uses them can be moved ahead.
+__device__ __forceinline__ void tmem_load_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+                 "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+                 "+r"(r[28]), "+r"(r[29])
+               :
+               : "memory");
+  asm volatile("" : "+r"(r[30]), "+r"(r[31])::"memory");
+}
 
 // One lane of a converged warp.  The loops around TMA and matrix instructions are run by whole warps, whose loop values the
 // compiler can then keep in the uniform registers that these instructions take, and only their issue by one lane: run by a
@@ -157,12 +167,156 @@ struct MmaShape {
   uint32_t* dev_status;
 };
 
-template <int BN>
+// Epilogues.  A warp hands over blocks of 32 x 32 of C, a row to a lane:
+//   struct Pre;  Pre load(row, col0, batch) const;   what it reads from global memory for its row (row may be out of range)
+//   void apply(pre, acc, row, col0, batch) const;    acc: 32 raw accumulators of the row
+// and, with kIn or kOut above 0, blocks of 32 x 32 halves that pass through shared memory: kIn of them are fetched by TMA, two
+// blocks ahead, and kOut are stored by TMA.  A row read or written straight from a lane touches 32 lines an instruction; that
+// alone was most of the epilogue of X = a X + B X (1536 x 4608 x 512: 17.6 us, 7.1 without reads and writes).
+//   const CUtensorMap* in(i) const;  const CUtensorMap* out(i) const;     (out: NULL where nothing is stored)
+//   void apply(pre, acc, row, col0, batch, smem) const;                   smem: this lane's row of the first block (see row_chunk)
+constexpr uint32_t kBlockBytes = 2048;     // 32 rows of 64 bytes, 64-byte swizzle
+// The 16-byte piece q of a lane's row: pieces are exchanged within a row by the row's number, as TMA lays them.
+__device__ __forceinline__ uint32_t row_chunk(uint32_t block, int lane, int q) { return block + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4); }
+
+template <class Epi>
+struct Staged {
+  static constexpr int kBlocks = Epi::kIn > Epi::kOut ? Epi::kIn : Epi::kOut;
+  static constexpr uint32_t kSlot = kBlocks * kBlockBytes;      // a warp has two
+  static constexpr uint32_t kBytes = 8 * 2 * kSlot;
+};
+
+template <int BN, class Epi>
 struct MmaTile {
   static constexpr int kStageBytes = (kMmaRows + BN) * 128;
-  static constexpr int kStages = BN == 256 ? 4 : BN == 192 ? 5 : BN == 128 ? 6 : BN == 64 ? 8 : 10;
+  static constexpr int kFit = (int)((225 * 1024 - Staged<Epi>::kBytes) / kStageBytes);
+  static constexpr int kStages = kFit < 10 ? kFit : 10;
   static constexpr int kTmemCols = BN == 192 ? 512 : 2 * BN;
-  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024;
+  static constexpr uint32_t kRing = kStages * kStageBytes;
+  static constexpr size_t kSmem = kRing + Staged<Epi>::kBytes + 1024;
+};
+
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src)
+               : "memory");
+}
+
+// The epilogue of one warp: its two slots of shared memory, and the barriers on which their loads arrive.
+template <class Epi>
+struct EpilogueWarp {
+  uint32_t slots, bars;      // addresses
+  uint32_t slot = 0, phases = 0;
+  int lane;
+  volatile int* gave_up;
+
+  __device__ __forceinline__ uint32_t at(uint32_t which) const { return slots + which * Staged<Epi>::kSlot; }
+  __device__ __forceinline__ void fetch(const Epi& epi, uint32_t which, uint32_t row0, uint32_t col0, uint32_t b) {
+    if constexpr (Epi::kIn > 0) {
+      if (lane == 0) {
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");    // what this slot last held has left it
+        mbar_expect_tx(bars + 8 * which, Epi::kIn * kBlockBytes);
+#pragma unroll
+        for (int i = 0; i < Epi::kIn; ++i) tma_load_3d(at(which) + i * kBlockBytes, epi.in(i), (int)col0, (int)row0, (int)b, bars + 8 * which);
+      }
+      __syncwarp();
+    }
+  }
+  // One block.  False: a wait ran out.
+  template <class LoadNext>
+  __device__ __forceinline__ bool block(const Epi& epi, const typename Epi::Pre& pre, uint32_t tmem_addr, bool empty, uint32_t row0, uint32_t col0,
+                                        uint32_t b, LoadNext&& load_next) {
+    uint32_t acc[32];
+    tmem_load32(acc, tmem_addr);
+    load_next();
+    tmem_load_wait(acc);
+    if (empty) {      // an empty sum: nothing was written to the accumulator
+#pragma unroll
+      for (int q = 0; q < 32; ++q) acc[q] = 0;
+    }
+    return finish(epi, pre, acc, row0, col0, b);
+  }
+  __device__ __forceinline__ bool finish(const Epi& epi, const typename Epi::Pre& pre, const uint32_t (&acc)[32], uint32_t row0, uint32_t col0, uint32_t b) {
+    if constexpr (Epi::kIn > 0) {
+      if (!mbar_wait(bars + 8 * slot, (phases >> slot) & 1, gave_up)) return false;
+      phases ^= 1u << slot;
+    } else if constexpr (Epi::kOut > 0) {
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+      __syncwarp();
+    }
+    if constexpr (Epi::kIn + Epi::kOut > 0) {
+      epi.apply(pre, acc, row0 + lane, col0, b, at(slot), lane);
+      if constexpr (Epi::kOut > 0) {
+        if (epi.out(0)) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+#pragma unroll
+            for (int i = 0; i < Epi::kOut; ++i) tma_store_3d(epi.out(i), (int)col0, (int)row0, (int)b, at(slot) + i * kBlockBytes);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        }
+      }
+      __syncwarp();
+      slot ^= 1;
+    } else {
+      epi.apply(pre, acc, row0 + lane, col0, b);
+    }
+    return true;
+  }
+  __device__ __forceinline__ void drain() const {      // stores have been made
+    if constexpr (Epi::kOut > 0) {
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+      __syncwarp();
+    }
+  }
+  // What is still on its way into this warp's slots when it gives up lands first (`fetched`: loads asked for and not waited for).
+  __device__ __forceinline__ void abandon(int fetched) {
+    if constexpr (Epi::kIn > 0) {
+      for (int i = 0; i < fetched; ++i) {
+        const uint32_t which = (slot + i) & 1;
+        const long long t0 = clock64();
+        while (!mbar_try(bars + 8 * which, (phases >> which) & 1) && clock64() - t0 < kWaitCycles) {
+        }
+      }
+    }
+  }
+  // All blocks of this warp's part of a tile.  `ready` waits for the accumulator.
+  template <class Wanted, class Ready>
+  __device__ __forceinline__ bool tile(const Epi& epi, int group, int blocks, uint32_t row0, uint32_t col, uint32_t b, uint32_t tmem_at, bool empty,
+                                       Wanted&& wanted, Ready&& ready) {
+    auto next = [&](int c) {
+      c += 2;
+      while (c < blocks && !wanted(c)) c += 2;
+      return c;
+    };
+    int c = next(group - 2), cn = next(c);
+    typename Epi::Pre pre{};
+    if (c < blocks) {
+      fetch(epi, slot, row0, col + 32 * c, b);
+      pre = epi.load(row0 + lane, col + 32 * c, b);
+    }
+    if (cn < blocks) fetch(epi, slot ^ 1, row0, col + 32 * cn, b);
+    if (!ready()) {
+      abandon((c < blocks) + (cn < blocks));
+      return false;
+    }
+    tc_fence_after();
+    while (c < blocks) {
+      const int nn = next(cn);
+      const uint32_t used = slot;
+      typename Epi::Pre after{};
+      if (!block(epi, pre, tmem_at + 32 * c, empty, row0, col + 32 * c, b,
+                 [&] { if (cn < blocks) after = epi.load(row0 + lane, col + 32 * cn, b); })) {
+        abandon(1 + (cn < blocks));
+        return false;
+      }
+      if (nn < blocks) fetch(epi, used, row0, col + 32 * nn, b);
+      pre = after;
+      c = cn;
+      cn = nn;
+    }
+    return true;
+  }
 };
 
 // Tiles of C in the order in which CTAs take them.
@@ -202,22 +356,18 @@ struct TileWalk {
   }
 };
 
-// Epi: struct with
-//   struct Pre                                      what it reads from global memory for one block of 32 columns
-//   Pre load(row, col0, batch) const               (row may be out of range)
-//   void apply(pre, acc, row, col0, batch) const   acc: 32 raw accumulators of one row
 template <int KIND, int BN, bool B_ACROSS, class Epi>
 __global__ void __launch_bounds__(kMmaThreads, 1)
-    k_mma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const Epi epi) {
-  using T = MmaTile<BN>;
+    k_mma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const __grid_constant__ Epi epi) {
+  using T = MmaTile<BN, Epi>;
   constexpr int kBK = KIND == kMmaF16 ? 64 : 128;    // elements of K per stage: 128 bytes
   extern __shared__ uint8_t dyn[];
-  __shared__ uint64_t bars[2 * T::kStages + 5];
+  __shared__ uint64_t bars[2 * T::kStages + 5 + 16];
   __shared__ uint32_t tmem_slot;
   __shared__ int gave_up;
   const uint32_t ring = (smem_u32(dyn) + 1023u) & ~1023u;
   const uint32_t full = smem_u32(bars), empty = full + 8 * T::kStages, tfull = empty + 8 * T::kStages, tempty = tfull + 16,
-                 drain = tempty + 16;
+                 drain = tempty + 16, staged = drain + 8;
   const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -232,6 +382,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       mbar_init(tempty + 8 * i, 8);
     }
     mbar_init(drain, 1);
+    for (int i = 0; i < 16; ++i) mbar_init(staged + 8 * i, 1);
     gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -245,13 +396,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   // wait for this kernel while this kernel waits for it.
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("fence.proxy.async.global;" ::: "memory");   // what earlier kernels stored is about to be read by TMA
 
   const TileWalk walk(shape, BN);
   const uint32_t nk = (shape.k + kBK - 1) / kBK;
 
   if (warp == 0) {
     const bool one = elect_one();
-    asm volatile("fence.proxy.async.global;" ::: "memory");
     uint32_t stage = 0, phase = 0, issued = 0;
     bool ok = true;
     for (uint32_t t = blockIdx.x; ok && t < walk.total; t += gridDim.x) {
@@ -334,39 +485,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   } else if (warp >= 4) {
     // two groups of four warps; a warp reads the 32 lanes that its rank in the group names
     const uint32_t quarter = warp & 3, group = (warp - 4) >> 2;
+    EpilogueWarp<Epi> ew{ring + T::kRing + (warp - 4) * 2 * Staged<Epi>::kSlot, staged + 16 * (warp - 4), 0, 0, lane, &gave_up};
     uint32_t at = 0, aphase = 0;
     for (uint32_t t = blockIdx.x; t < walk.total; t += gridDim.x) {
       uint32_t b, i, j;
       walk.at(t, b, i, j);
-      const uint32_t row0 = i * kMmaRows + quarter * 32, row = row0 + lane;
-      constexpr int kBlocks = BN / 32;
-      const uint32_t c_first = j * BN;
+      const uint32_t row0 = i * kMmaRows + quarter * 32, col = j * BN;
       auto wanted = [&](int c) {
-        const uint32_t col0 = c_first + 32 * c;
+        const uint32_t col0 = col + 32 * c;
         return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >= row0);
       };
-      int c = (int)group;
-      while (c < kBlocks && !wanted(c)) c += 2;
-      typename Epi::Pre pre{};
-      if (c < kBlocks) pre = epi.load(row, c_first + 32 * c, b);
-      if (!mbar_wait(tfull + 8 * at, aphase, &gave_up)) break;
-      tc_fence_after();
-      while (c < kBlocks) {
-        uint32_t acc[32];
-        tmem_load32(acc, tmem + at * BN + 32 * c + (quarter << 21));
-        int cn = c + 2;
-        while (cn < kBlocks && !wanted(cn)) cn += 2;
-        typename Epi::Pre nxt{};
-        if (cn < kBlocks) nxt = epi.load(row, c_first + 32 * cn, b);
-        tmem_load_wait();
-        if (nk == 0) {   // an empty sum: nothing was written to the accumulator
-#pragma unroll
-          for (int q = 0; q < 32; ++q) acc[q] = 0;
-        }
-        epi.apply(pre, acc, row, c_first + 32 * c, b);
-        pre = nxt;
-        c = cn;
-      }
+      if (!ew.tile(epi, (int)group, BN / 32, row0, col, b, tmem + at * BN + (quarter << 21), nk == 0, wanted,
+                   [&] { return mbar_wait(tfull + 8 * at, aphase, &gave_up); }))
+        break;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(tempty + 8 * at);
@@ -375,6 +506,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         aphase ^= 1;
       }
     }
+    ew.drain();
   }
   __syncwarp();
   tc_fence_before();
@@ -431,9 +563,13 @@ struct PairWalk {
   }
 };
 
-constexpr int kPairStages = 6;
 constexpr int kPairStageBytes = 2 * kMmaRows * 128;   // per CTA: 128 rows of A, 128 of B
-constexpr size_t kPairSmem = (size_t)kPairStages * kPairStageBytes + 1024;
+template <class Epi>
+struct PairTile {
+  static constexpr int kStages = (int)((225 * 1024 - Staged<Epi>::kBytes) / kPairStageBytes);
+  static constexpr uint32_t kRing = kStages * kPairStageBytes;
+  static constexpr size_t kSmem = kRing + Staged<Epi>::kBytes + 1024;
+};
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -479,15 +615,16 @@ __device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t a_desc, ui
 
 template <int KIND, bool B_ACROSS, class Epi>
 __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
-    k_mma_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const Epi epi) {
+    k_mma_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const __grid_constant__ Epi epi) {
+  constexpr int kPairStages = PairTile<Epi>::kStages;
   constexpr int kBK = KIND == kMmaF16 ? 64 : 128;
   extern __shared__ uint8_t dyn[];
-  __shared__ uint64_t bars[2 * kPairStages + 5];
+  __shared__ uint64_t bars[2 * kPairStages + 5 + 16];
   __shared__ uint32_t tmem_slot;
   __shared__ int gave_up;
   const uint32_t ring = (smem_u32(dyn) + 1023u) & ~1023u;
   const uint32_t full = smem_u32(bars), empty = full + 8 * kPairStages, tfull = empty + 8 * kPairStages, tempty = tfull + 16,
-                 drain = tempty + 16;
+                 drain = tempty + 16, staged = drain + 8;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
 
@@ -503,6 +640,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
       mbar_init(tempty + 8 * i, 16);   // the epilogue warps of both CTAs
     }
     mbar_init(drain, 1);
+    for (int i = 0; i < 16; ++i) mbar_init(staged + 8 * i, 1);
     gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -517,6 +655,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_slot, 0);
   asm volatile("griddepcontrol.launch_dependents;");   // after the allocation, as above
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("fence.proxy.async.global;" ::: "memory");   // what earlier kernels stored is about to be read by TMA
 
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const PairWalk walk(shape, pairs);
@@ -526,7 +665,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
 
   if (warp == 0) {
     const bool one = elect_one();
-    asm volatile("fence.proxy.async.global;" ::: "memory");
     uint32_t stage = 0, phase = 0, issued = 0;
     bool ok = true;
     for (uint32_t t = pair; ok && t < walk.items; t += pairs) {
@@ -615,35 +753,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
     }
   } else if (warp >= 4) {
     const uint32_t quarter = warp & 3, group = (warp - 4) >> 2;
+    EpilogueWarp<Epi> ew{ring + PairTile<Epi>::kRing + (warp - 4) * 2 * Staged<Epi>::kSlot, staged + 16 * (warp - 4), 0, 0, lane, &gave_up};
     uint32_t at = 0, aphase = 0;
     for (uint32_t t = pair; t < walk.items; t += pairs) {
       uint32_t b, row_t, col, width;
       walk.at(t, b, row_t, col, width);
       if (skip(row_t, col, width)) continue;
-      const uint32_t row0 = row_t + rank * kMmaRows + quarter * 32, row = row0 + lane;
-      const int blocks = (int)(width >> 5);
+      const uint32_t row0 = row_t + rank * kMmaRows + quarter * 32;
       auto wanted = [&](int c) {
         const uint32_t col0 = col + 32 * c;
         return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >= row0);
       };
-      int c = (int)group;
-      while (c < blocks && !wanted(c)) c += 2;
-      typename Epi::Pre pre{};
-      if (c < blocks) pre = epi.load(row, col + 32 * c, b);
-      if (!mbar_wait(tfull + 8 * at, aphase, &gave_up)) break;
-      tc_fence_after();
-      while (c < blocks) {
-        uint32_t acc[32];
-        tmem_load32(acc, tmem + at * 256 + 32 * c + (quarter << 21));
-        int cn = c + 2;
-        while (cn < blocks && !wanted(cn)) cn += 2;
-        typename Epi::Pre nxt{};
-        if (cn < blocks) nxt = epi.load(row, col + 32 * cn, b);
-        tmem_load_wait();
-        epi.apply(pre, acc, row, col + 32 * c, b);
-        pre = nxt;
-        c = cn;
-      }
+      if (!ew.tile(epi, (int)group, (int)(width >> 5), row0, col, b, tmem + at * 256 + (quarter << 21), false, wanted,
+                   [&] { return mbar_wait(tfull + 8 * at, aphase, &gave_up); }))
+        break;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(in_cta(tempty + 8 * at, 0));
@@ -652,6 +775,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
         aphase ^= 1;
       }
     }
+    ew.drain();
   }
   __syncwarp();
   tc_fence_before();
@@ -668,18 +792,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
 // of K in a row; on a third of the SMs.
 template <int KIND, int BN, bool B_ACROSS, class Epi>
 __global__ void __launch_bounds__(kMmaThreads, 1)
-    k_mma_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const Epi epi,
+    k_mma_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const __grid_constant__ Epi epi,
                 const uint32_t parts) {
-  using T = MmaTile<BN>;
+  using T = MmaTile<BN, Epi>;
   constexpr int kBK = KIND == kMmaF16 ? 64 : 128;
   constexpr int kTmem = BN < 32 ? 32 : BN == 192 ? 256 : BN;
   constexpr int kBlocks = BN / 32;
   extern __shared__ uint8_t dyn[];
-  __shared__ uint64_t bars[2 * T::kStages + 1];
+  __shared__ uint64_t bars[2 * T::kStages + 1 + 16];
   __shared__ uint32_t tmem_slot;
   __shared__ int gave_up;
   const uint32_t ring = (smem_u32(dyn) + 1023u) & ~1023u;
-  const uint32_t full = smem_u32(bars), empty = full + 8 * T::kStages, done = empty + 8 * T::kStages;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * T::kStages, done = empty + 8 * T::kStages,
+                 staged = done + 8;
   const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
 
@@ -691,6 +816,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       mbar_init(empty + 8 * i, 1);
     }
     mbar_init(done, 1);
+    for (int i = 0; i < 16; ++i) mbar_init(staged + 8 * i, 1);
     gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -702,6 +828,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_slot, 0);
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("fence.proxy.async.global;" ::: "memory");   // what earlier kernels stored is about to be read by TMA
 
   const TileWalk walk(shape, BN);
   uint32_t b, ti, tj;
@@ -710,7 +837,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t k_first = min(rank * share, nk_all), nk = min(share, nk_all - k_first);
 
   const uint32_t quarter = warp & 3, group = (warp - 4) >> 2;   // epilogue warps
-  const uint32_t row0 = ti * kMmaRows + quarter * 32, row = row0 + lane, c_first = tj * BN;
+  const uint32_t row0 = ti * kMmaRows + quarter * 32, c_first = tj * BN;
   auto wanted = [&](int c) {
     const uint32_t col0 = c_first + 32 * c;
     return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >= row0);
@@ -721,7 +848,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 
   if (warp == 0) {
     const bool one = elect_one();
-    asm volatile("fence.proxy.async.global;" ::: "memory");
     uint32_t stage = 0, phase = 0, issued = 0;
     bool ok = true;
     for (uint32_t kb = k_first; kb < k_first + nk; ++kb) {
@@ -790,7 +916,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       if (!wanted(c) || owner(c) == rank) continue;
       uint32_t acc[32];
       tmem_load32(acc, tmem + 32 * c + (quarter << 21));
-      tmem_load_wait();
+      tmem_load_wait(acc);
       const uint32_t to = in_cta(slot(c, rank), owner(c)) + lane * 16;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -802,12 +928,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   __syncwarp();
   cluster_sync();
   if (warp >= 4) {
+    EpilogueWarp<Epi> ew{ring + T::kRing + (warp - 4) * 2 * Staged<Epi>::kSlot, staged + 16 * (warp - 4), 0, 0, lane, &gave_up};
     for (int c = (int)group; c < kBlocks; c += 2) {
       if (!wanted(c) || owner(c) != rank) continue;
-      const typename Epi::Pre pre = epi.load(row, c_first + 32 * c, b);
+      ew.fetch(epi, ew.slot, row0, c_first + 32 * c, b);
+      const typename Epi::Pre pre = epi.load(row0 + lane, c_first + 32 * c, b);
       uint32_t acc[32], own[32];
       tmem_load32(own, tmem + 32 * c + (quarter << 21));
-      tmem_load_wait();
+      tmem_load_wait(own);
 #pragma unroll
       for (int j = 0; j < 32; ++j) acc[j] = 0;
       for (uint32_t r = 0; r < parts; ++r) {
@@ -827,8 +955,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           }
         }
       }
-      epi.apply(pre, acc, row, c_first + 32 * c, b);
+      if (!ew.finish(epi, pre, acc, row0, c_first + 32 * c, b)) {
+        ew.abandon(1);
+        break;
+      }
     }
+    ew.drain();
   }
   __syncwarp();
   tc_fence_before();
@@ -841,9 +973,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 // ---- host side ------------------------------------------------------------------------------------------
 
 // A map over `batch` matrices of `rows` rows of `cols` elements (2-byte floats or bytes), `ld` elements apart, read in
-// boxes of box_cols x box_rows with 128-byte swizzle; entries outside read as zero.
+// boxes of box_cols x box_rows with 128-byte swizzle (blocks of an epilogue, 64 bytes wide: 64-byte swizzle); entries outside
+// read as zero and are not written.
 cudaError_t make_tensor_map(CUtensorMap* map, int kind, const void* base, uint64_t cols, uint64_t rows, uint64_t batch, uint64_t ld,
-                            uint64_t batch_stride, uint32_t box_cols, uint32_t box_rows);
+                            uint64_t batch_stride, uint32_t box_cols, uint32_t box_rows, bool block = false);
 
 int sm_count();
 
@@ -926,8 +1059,8 @@ cudaError_t launch_mma_bn(const CUtensorMap& a, const CUtensorMap& b, const MmaS
   const TileWalk w(s, BN);
   const uint32_t grid = w.total < (uint32_t)sm_count() ? w.total : (uint32_t)sm_count();
   if (!grid) return cudaSuccess;
-  allow_smem_for<k_mma<KIND, BN, B_ACROSS, Epi>>(MmaTile<BN>::kSmem);
-  launch_pdl_dyn(k_mma<KIND, BN, B_ACROSS, Epi>, dim3(grid), dim3(kMmaThreads), MmaTile<BN>::kSmem, st, a, b, s, epi);
+  allow_smem_for<k_mma<KIND, BN, B_ACROSS, Epi>>(MmaTile<BN, Epi>::kSmem);
+  launch_pdl_dyn(k_mma<KIND, BN, B_ACROSS, Epi>, dim3(grid), dim3(kMmaThreads), MmaTile<BN, Epi>::kSmem, st, a, b, s, epi);
   count_launches(1);
   return cudaGetLastError();
 }
@@ -936,11 +1069,11 @@ template <int KIND, int BN, bool B_ACROSS, class Epi>
 cudaError_t launch_mma_split(uint32_t parts, const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
   const TileWalk w(s, BN);
   if (!w.total) return cudaSuccess;
-  allow_smem_for<k_mma_split<KIND, BN, B_ACROSS, Epi>>(MmaTile<BN>::kSmem);
+  allow_smem_for<k_mma_split<KIND, BN, B_ACROSS, Epi>>(MmaTile<BN, Epi>::kSmem);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(w.total * parts);
   cfg.blockDim = dim3(kMmaThreads);
-  cfg.dynamicSmemBytes = MmaTile<BN>::kSmem;
+  cfg.dynamicSmemBytes = MmaTile<BN, Epi>::kSmem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -961,8 +1094,8 @@ cudaError_t launch_mma(const MmaPlan& plan, const CUtensorMap& a, const CUtensor
     const PairWalk w(s, pair_count());
     const uint32_t pairs = w.items < (uint32_t)pair_count() ? w.items : (uint32_t)pair_count();
     if (!pairs) return cudaSuccess;
-    allow_smem_for<k_mma_pair<KIND, B_ACROSS, Epi>>(kPairSmem);
-    launch_pdl_dyn(k_mma_pair<KIND, B_ACROSS, Epi>, dim3(2 * pairs), dim3(kMmaThreads), kPairSmem, st, a, b, s, epi);
+    allow_smem_for<k_mma_pair<KIND, B_ACROSS, Epi>>(PairTile<Epi>::kSmem);
+    launch_pdl_dyn(k_mma_pair<KIND, B_ACROSS, Epi>, dim3(2 * pairs), dim3(kMmaThreads), PairTile<Epi>::kSmem, st, a, b, s, epi);
     count_launches(1);
     return cudaGetLastError();
   }

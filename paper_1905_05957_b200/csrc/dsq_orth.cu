@@ -172,34 +172,35 @@ struct Half32 {   // 32 consecutive entries of a row, two to a word
     const __half2 h = __floats2half2_rn(a, b);
     w[j] = *reinterpret_cast<const uint32_t*>(&h);
   }
-};
-__device__ __forceinline__ Half32 load_half32(const __half* row, uint32_t col0, uint32_t ld) {
-  Half32 v;
+  // this lane's row of a block in shared memory
+  __device__ __forceinline__ void get(uint32_t block, int lane) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v.w[i] = 0;
-  if (col0 < ld) ld_b32(v.w, row + col0);
-  if (col0 + 16 < ld) ld_b32(v.w + 8, row + col0 + 16);
-  return v;
-}
-__device__ __forceinline__ void store_half32(__half* row, uint32_t col0, uint32_t ld, const Half32& v) {
-  if (col0 < ld) st_b32(row + col0, v.w);
-  if (col0 + 16 < ld) st_b32(row + col0 + 16, v.w + 8);
-}
+    for (int q = 0; q < 4; ++q)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[4 * q]), "=r"(w[4 * q + 1]), "=r"(w[4 * q + 2]), "=r"(w[4 * q + 3])
+                   : "r"(row_chunk(block, lane, q))
+                   : "memory");
+  }
+  __device__ __forceinline__ void put(uint32_t block, int lane) const {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row_chunk(block, lane, q)), "r"(w[4 * q]), "r"(w[4 * q + 1]), "r"(w[4 * q + 2]),
+                   "r"(w[4 * q + 3])
+                   : "memory");
+  }
+};
 
-// A symmetric matrix in 16 bits without its diagonal, which is held apart.
+// A symmetric matrix in 16 bits without its diagonal, which is held apart.  A block goes out through shared memory; its mirror
+// image straight: lanes hold consecutive rows, so a column of the block is 64 consecutive bytes of the mirrored row.
 struct SymOut {
   __half* off;
   float* diag;
   uint32_t m, ld;
   uint64_t stride, diag_stride;
-  // The block (row, col0..col0+31) and its mirror image.  Lanes hold consecutive rows, so a column of the block is 64
-  // consecutive bytes of the mirrored row.
-  __device__ __forceinline__ void put(const Half32& v, uint32_t row, uint32_t col0, uint32_t b) const {
-    if (row >= m) return;
-    __half* base = off + b * stride;
-    store_half32(base + (uint64_t)row * ld, col0, ld, v);
-    if (col0 > row) {
-      uint16_t* to = reinterpret_cast<uint16_t*>(base + (uint64_t)col0 * ld + row);
+  __device__ __forceinline__ void put(const Half32& v, uint32_t row, uint32_t col0, uint32_t b, uint32_t block, int lane) const {
+    v.put(block, lane);
+    if (row < m && col0 > row) {
+      uint16_t* to = reinterpret_cast<uint16_t*>(off + b * stride + (uint64_t)col0 * ld + row);
 #pragma unroll
       for (int j = 0; j < 32; ++j)
         if (col0 + j < m) to[(uint64_t)j * ld] = (uint16_t)(v.w[j / 2] >> (16 * (j & 1)));
@@ -208,10 +209,14 @@ struct SymOut {
 };
 
 struct EpiGram {   // A = X X^T
+  static constexpr int kIn = 0, kOut = 1;
   struct Pre {};
+  CUtensorMap a_blocks;
   SymOut a;
+  __device__ __forceinline__ const CUtensorMap* in(int) const { return nullptr; }
+  __device__ __forceinline__ const CUtensorMap* out(int) const { return &a_blocks; }
   __device__ __forceinline__ Pre load(uint32_t, uint32_t, uint32_t) const { return {}; }
-  __device__ __forceinline__ void apply(const Pre&, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b) const {
+  __device__ __forceinline__ void apply(const Pre&, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b, uint32_t block, int lane) const {
     Half32 v;
     float d = 0.f, s[32];
 #pragma unroll
@@ -222,97 +227,89 @@ struct EpiGram {   // A = X X^T
 #pragma unroll
     for (int j = 0; j < 16; ++j) v.set(j, s[2 * j], s[2 * j + 1]);
     if (row >= col0 && row < col0 + 32 && row < a.m) a.diag[b * a.diag_stride + row] = d * kDown;
-    a.put(v, row, col0, b);
+    a.put(v, row, col0, b, block, lane);
   }
 };
 
 struct EpiPoly {   // B = b A + c A A, the accumulator being O O
+  static constexpr int kIn = 1, kOut = 1;
   struct Pre {
-    Half32 o;
     float d;
   };
-  SymOut a, out;
+  CUtensorMap a_blocks, b_blocks;
+  SymOut a, b;
   float b1, c1;
-  __device__ __forceinline__ Pre load(uint32_t row, uint32_t col0, uint32_t b) const {
-    Pre p{};
-    if (row < a.m) {
-      p.o = load_half32(a.off + b * a.stride + (uint64_t)row * a.ld, col0, a.ld);
-      p.d = a.diag[b * a.diag_stride + row];
-    }
-    return p;
-  }
-  __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b) const {
+  __device__ __forceinline__ const CUtensorMap* in(int) const { return &a_blocks; }
+  __device__ __forceinline__ const CUtensorMap* out(int) const { return &b_blocks; }
+  __device__ __forceinline__ Pre load(uint32_t row, uint32_t, uint32_t z) const { return {row < a.m ? a.diag[z * a.diag_stride + row] : 0.f}; }
+  __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t z, uint32_t block, int lane) const {
     Half32 v;
-    const float4* dj = reinterpret_cast<const float4*>(a.diag + b * a.diag_stride + col0);   // padded to a multiple of 32 entries
-    float d = 0.f, e[32];
+    v.get(block, lane);
+    const float4* dj = reinterpret_cast<const float4*>(a.diag + z * a.diag_stride + col0);   // padded to a multiple of 32 entries
+    float d = 0.f;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       const float4 t = __ldg(dj + q);
-      const float2 o0 = p.o.two(2 * q), o1 = p.o.two(2 * q + 1);
+      const float2 o0 = v.two(2 * q), o1 = v.two(2 * q + 1);
       const float dd[4] = {t.x, t.y, t.z, t.w}, o[4] = {o0.x, o0.y, o1.x, o1.y};
+      float e[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int j = 4 * q + i;
         const float s = __uint_as_float(acc[j]);
         const bool on = col0 + j == row;
         if (on) d = s;
-        e[j] = on || col0 + j >= a.m ? 0.f : fmaf(c1, fmaf(s, kDown, (p.d + dd[i]) * o[i]), b1 * o[i]);
+        e[i] = on || col0 + j >= a.m ? 0.f : fmaf(c1, fmaf(s, kDown, (p.d + dd[i]) * o[i]), b1 * o[i]);
       }
+      v.set(2 * q, e[0], e[1]);
+      v.set(2 * q + 1, e[2], e[3]);
     }
-#pragma unroll
-    for (int j = 0; j < 16; ++j) v.set(j, e[2 * j], e[2 * j + 1]);
     if (row >= col0 && row < col0 + 32 && row < a.m)
-      out.diag[b * a.diag_stride + row] = fmaf(c1, fmaf(d, kDown * kDown, p.d * p.d), b1 * p.d);
-    out.put(v, row, col0, b);
+      b.diag[z * a.diag_stride + row] = fmaf(c1, fmaf(d, kDown * kDown, p.d * p.d), b1 * p.d);
+    b.put(v, row, col0, z, block, lane);
   }
 };
 
 struct EpiX {   // X = (a + E) X + F X
+  static constexpr int kIn = 2, kOut = 2;
   struct Pre {
-    Half32 hi, lo;
     float e;
   };
-  const __half *hi, *lo;     // X, both halves
-  const float* diag;         // E
-  uint64_t stride, diag_stride;
-  uint32_t m, n, ld;
+  CUtensorMap blocks[2], next[2];   // X and the next X, hi and lo
+  const float* diag;                // E
+  uint64_t diag_stride;
+  uint32_t m, n;
   float a1;
-  __half *hi_out, *lo_out;   // the next X; NULL on the last step, which writes:
-  OrthOut to;                //   in the orientation of the gradient
+  int last;                         // the last step writes:
+  OrthOut to;                       //   in the orientation of the gradient
   int tall, vec;
-  __device__ __forceinline__ Pre load(uint32_t row, uint32_t col0, uint32_t b) const {
-    Pre p{};
-    if (row < m) {
-      const uint64_t at = b * stride + (uint64_t)row * ld;
-      p.hi = load_half32(hi + at, col0, ld);
-      p.lo = load_half32(lo + at, col0, ld);
-      p.e = diag[b * diag_stride + row];
-    }
-    return p;
-  }
-  __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b) const {
-    if (row >= m) return;
+  __device__ __forceinline__ const CUtensorMap* in(int i) const { return blocks + i; }
+  __device__ __forceinline__ const CUtensorMap* out(int i) const { return last ? nullptr : next + i; }
+  __device__ __forceinline__ Pre load(uint32_t row, uint32_t, uint32_t b) const { return {row < m ? diag[b * diag_stride + row] : 0.f}; }
+  __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b, uint32_t block, int lane) const {
     const float f = a1 + p.e;
     float v[32];
+    Half32 h, l;
+    h.get(block, lane);
+    l.get(block + kBlockBytes, lane);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      const float2 h = p.hi.two(j), l = p.lo.two(j);
-      v[2 * j] = fmaf(f, h.x + l.x, __uint_as_float(acc[2 * j]) * kDown);
-      v[2 * j + 1] = fmaf(f, h.y + l.y, __uint_as_float(acc[2 * j + 1]) * kDown);
+      const float2 x = h.two(j), y = l.two(j);
+      v[2 * j] = fmaf(f, x.x + y.x, __uint_as_float(acc[2 * j]) * kDown);
+      v[2 * j + 1] = fmaf(f, x.y + y.y, __uint_as_float(acc[2 * j + 1]) * kDown);
     }
-    if (hi_out) {
-      Half32 h, l;
+    if (!last) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
         h.set(j, v[2 * j], v[2 * j + 1]);
         const float2 r = h.two(j);
         l.set(j, v[2 * j] - r.x, v[2 * j + 1] - r.y);
       }
-      const uint64_t at = b * stride + (uint64_t)row * ld;
-      store_half32(hi_out + at, col0, ld, h);
-      store_half32(lo_out + at, col0, ld, l);
+      h.put(block, lane);
+      l.put(block + kBlockBytes, lane);
       return;
     }
+    if (row >= m) return;
     // The last step leaves the workspace.  Tall matrices come back transposed: lanes then hold consecutive entries.
     const uint64_t step = tall ? m : 1;
     const uint64_t first = tall ? (uint64_t)col0 * m + row : (uint64_t)row * n + col0, each = (uint64_t)m * n;
@@ -399,6 +396,7 @@ struct ds_orth_ctx {
   bool mapped;                    // the tensor maps below are made (on the first update: the driver makes them)
   MmaPlan p_gram, p_poly, p_x;
   CUtensorMap x_rows[2], x_cols_gram[2], x_across[2], a_rows, a_cols, b_rows;
+  CUtensorMap hi_blocks[2], lo_blocks[2], a_blocks, b_blocks;
 };
 
 namespace {
@@ -456,6 +454,15 @@ cudaError_t orth_maps(ds_orth_ctx* h) {
   add(&h->a_rows, h->a.off, h->m, h->m, h->ldm, h->ms, kMmaRows);
   add(&h->a_cols, h->a.off, h->m, h->m, h->ldm, h->ms, h->p_poly.box_rows());
   add(&h->b_rows, h->b.off, h->m, h->m, h->ldm, h->ms, kMmaRows);
+  auto add_blocks = [&](CUtensorMap* map, const void* base, uint64_t cols, uint64_t ld, uint64_t stride) {
+    if (e == cudaSuccess) e = make_tensor_map(map, kMmaF16, base, cols, h->m, batch, ld, stride, 32, 32, true);
+  };
+  for (int i = 0; i < 2; ++i) {
+    add_blocks(&h->hi_blocks[i], h->hi[i], h->n, h->ldx, h->xs);
+    add_blocks(&h->lo_blocks[i], h->lo[i], h->n, h->ldx, h->xs);
+  }
+  add_blocks(&h->a_blocks, h->a.off, h->m, h->ldm, h->ms);
+  add_blocks(&h->b_blocks, h->b.off, h->m, h->ldm, h->ms);
   h->mapped = e == cudaSuccess;
   return e;
 }
@@ -537,23 +544,22 @@ int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum
       full{h->m, h->n, h->m, c.batch, 2, 0, h->dev_status};
   int cur = 0;
   for (uint32_t s = 0; s < c.steps && e == cudaSuccess; ++s, cur ^= 1) {
-    e = launch_mma<kMmaF16, false>(h->p_gram, h->x_rows[cur], h->x_cols_gram[cur], gram, EpiGram{h->a}, st);
-    if (e == cudaSuccess) e = launch_mma<kMmaF16, false>(h->p_poly, h->a_rows, h->a_cols, poly, EpiPoly{h->a, h->b, c.b, c.c}, st);
+    e = launch_mma<kMmaF16, false>(h->p_gram, h->x_rows[cur], h->x_cols_gram[cur], gram, EpiGram{h->a_blocks, h->a}, st);
+    if (e == cudaSuccess)
+      e = launch_mma<kMmaF16, false>(h->p_poly, h->a_rows, h->a_cols, poly, EpiPoly{h->a_blocks, h->b_blocks, h->a, h->b, c.b, c.c}, st);
     EpiX ex;
     memset(&ex, 0, sizeof ex);
-    ex.hi = h->hi[cur];
-    ex.lo = h->lo[cur];
+    ex.blocks[0] = h->hi_blocks[cur];
+    ex.blocks[1] = h->lo_blocks[cur];
+    ex.next[0] = h->hi_blocks[cur ^ 1];
+    ex.next[1] = h->lo_blocks[cur ^ 1];
     ex.diag = h->b.diag;
-    ex.stride = h->xs;
     ex.diag_stride = h->ds;
     ex.m = h->m;
     ex.n = h->n;
-    ex.ld = h->ldx;
     ex.a1 = c.a;
-    if (s + 1 < c.steps) {
-      ex.hi_out = h->hi[cur ^ 1];
-      ex.lo_out = h->lo[cur ^ 1];
-    } else {
+    ex.last = s + 1 == c.steps;
+    if (ex.last) {
       ex.to = where;
       ex.tall = c.rows > c.cols;
       ex.vec = c.cols % 16 == 0 && (op & 31u) == 0 && (xp & 15u) == 0 && mo.stride % 4 == 0;
