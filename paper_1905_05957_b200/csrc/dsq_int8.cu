@@ -33,10 +33,16 @@ __device__ __forceinline__ void scale_of(uint32_t amax_bits, float& s, float& in
   else
     inv = __frcp_rn(s);
 }
-__device__ __forceinline__ int code_of(float v, float inv) { return __float2int_rn(__fmul_rn(v, inv)); }   // a NaN gives 0
+// round(v * inv) in the low byte: adding 1.5 * 2^23 rounds to the nearest whole number, ties to even, and leaves it in the low
+// bits (conversions run at a fraction of the rate of additions).  Of a line with inv = 0 the codes are masked: v may be inf or NaN.
+__device__ __forceinline__ uint32_t code_of(float v, float inv) { return __float_as_uint(__fadd_rn(__fmul_rn(v, inv), 12582912.f)); }
+__device__ __forceinline__ uint32_t mask_of(float inv) { return inv != 0.f ? 0xFFFFFFFFu : 0u; }
 __device__ __forceinline__ uint32_t mag_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-__device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
+__device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+  return pack4(code_of(a, inv), code_of(b, inv), code_of(c, inv), code_of(d, inv)) & mask_of(inv);
 }
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
@@ -49,50 +55,37 @@ struct Vec {
   static constexpr int kN = 16 / sizeof(T);
   uint4 raw;
   __device__ __forceinline__ float at(int i) const { return to_f32(reinterpret_cast<const T*>(&raw)[i]); }
+  __device__ __forceinline__ void set(int i, T t) { reinterpret_cast<T*>(&raw)[i] = t; }
 };
 
 // ---- by rows: one CTA a row, one reading ----
-// The row stays in registers between its maximum and its codes (up to kKeep vectors a thread; the rest of a longer row is read
-// again, from cache).  Codes from `cols` up to the next multiple of 16 are written as 0.
-constexpr int kKeep = 4;
+// WHOLE: the row is whole vectors of 16 bytes on 16-byte boundaries, at most kKeep of them a thread: they are fetched together
+// and stay in registers between the row's maximum and its codes.  Else entry by entry, from cache the second time.  Codes from
+// `cols` up to the next multiple of 16 are written as 0.
+constexpr int kKeep = 8;
 
-template <class T, bool VEC>
+template <class T, bool WHOLE>
 __global__ void __launch_bounds__(256) k_i8_rows(const T* x, uint64_t ld, uint32_t cols, int8_t* q, uint64_t ldq, float* scale) {
   pdl_prologue();
-  constexpr int N = VEC ? Vec<T>::kN : 4;
+  constexpr int N = Vec<T>::kN;
   const T* row = x + (uint64_t)blockIdx.x * ld;
   int8_t* out = q + (uint64_t)blockIdx.x * ldq;
-  const uint32_t nv = (cols + N - 1) / N, nv_out = (cols + 15) / 16 * 16 / N;
-  auto fetch = [&](uint32_t v, float (&f)[N]) {
-    if (VEC && (v + 1) * N <= cols) {
-      Vec<T> r;
-      r.raw = *reinterpret_cast<const uint4*>(row + (uint64_t)v * N);
-#pragma unroll
-      for (int i = 0; i < N; ++i) f[i] = r.at(i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) f[i] = v * N + i < cols ? to_f32(row[(uint64_t)v * N + i]) : 0.f;
-    }
-  };
-  float keep[kKeep][N];
+  const uint32_t nv = cols / N;
+  Vec<T> keep[WHOLE ? kKeep : 1];
   uint32_t top = 0;
+  if constexpr (WHOLE) {
 #pragma unroll
-  for (int k = 0; k < kKeep; ++k) {
-    const uint32_t v = threadIdx.x + k * blockDim.x;
-    if (v < nv) {
-      fetch(v, keep[k]);
-#pragma unroll
-      for (int i = 0; i < N; ++i) top = max(top, mag_bits(keep[k][i]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) keep[k][i] = 0.f;
+    for (int k = 0; k < kKeep; ++k) {
+      const uint32_t v = threadIdx.x + k * blockDim.x;
+      keep[k].raw = v < nv ? __ldg(reinterpret_cast<const uint4*>(row) + v) : make_uint4(0, 0, 0, 0);
     }
-  }
-  for (uint32_t v = threadIdx.x + kKeep * blockDim.x; v < nv; v += blockDim.x) {
-    float f[N];
-    fetch(v, f);
 #pragma unroll
-    for (int i = 0; i < N; ++i) top = max(top, mag_bits(f[i]));
+    for (int k = 0; k < kKeep; ++k)
+#pragma unroll
+      for (int i = 0; i < N; ++i) top = max(top, mag_bits(keep[k].at(i)));
+  } else {
+#pragma unroll 4
+    for (uint32_t c = threadIdx.x; c < cols; c += blockDim.x) top = max(top, mag_bits(to_f32(row[c])));
   }
   __shared__ uint32_t tops[8];
   top = __reduce_max_sync(0xFFFFFFFFu, top);
@@ -102,25 +95,29 @@ __global__ void __launch_bounds__(256) k_i8_rows(const T* x, uint64_t ld, uint32
   float s, inv;
   scale_of(top, s, inv);
   if (threadIdx.x == 0) scale[blockIdx.x] = s;
-  auto emit = [&](uint32_t v, const float (&f)[N]) {
-    uint32_t w[N / 4];
+  if constexpr (WHOLE) {
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i)
-      w[i] = pack4(code_of(f[4 * i], inv), code_of(f[4 * i + 1], inv), code_of(f[4 * i + 2], inv), code_of(f[4 * i + 3], inv));
-    if constexpr (N == 8)
-      *reinterpret_cast<uint2*>(out + v * N) = make_uint2(w[0], w[1]);
-    else
-      *reinterpret_cast<uint32_t*>(out + v * N) = w[0];
-  };
+    for (int k = 0; k < kKeep; ++k) {
+      const uint32_t v = threadIdx.x + k * blockDim.x;
+      if (v >= nv) break;
+      uint32_t w[N / 4];
 #pragma unroll
-  for (int k = 0; k < kKeep; ++k) {
-    const uint32_t v = threadIdx.x + k * blockDim.x;
-    if (v < nv_out) emit(v, keep[k]);
-  }
-  for (uint32_t v = threadIdx.x + kKeep * blockDim.x; v < nv_out; v += blockDim.x) {
-    float f[N];
-    fetch(v, f);
-    emit(v, f);
+      for (int i = 0; i < N / 4; ++i)
+        w[i] = codes4(keep[k].at(4 * i), keep[k].at(4 * i + 1), keep[k].at(4 * i + 2), keep[k].at(4 * i + 3), inv);
+      if constexpr (N == 8)
+        *reinterpret_cast<uint2*>(out + v * N) = make_uint2(w[0], w[1]);
+      else
+        *reinterpret_cast<uint32_t*>(out + v * N) = w[0];
+    }
+    if (threadIdx.x < 16 && cols + threadIdx.x < (cols + 15) / 16 * 16) out[cols + threadIdx.x] = 0;
+  } else {
+#pragma unroll 2
+    for (uint32_t c = threadIdx.x * 4; c < (cols + 15) / 16 * 16; c += blockDim.x * 4) {
+      float f[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = c + i < cols ? to_f32(row[c + i]) : 0.f;
+      *reinterpret_cast<uint32_t*>(out + c) = codes4(f[0], f[1], f[2], f[3], inv);
+    }
   }
 }
 
@@ -129,142 +126,157 @@ __global__ void __launch_bounds__(256) k_i8_rows(const T* x, uint64_t ld, uint32
 // for the gradient of a bias, the column sums of each block of kAmaxRows rows.
 constexpr int kAmaxRows = 64;
 
-template <class T, bool VEC>
+template <class T, bool VEC, bool SUMS>
 __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t* row_top,
                                                  uint32_t* col_top, float* sums) {
   pdl_prologue();
-  constexpr int N = Vec<T>::kN;
+  constexpr int N = Vec<T>::kN, kRows = kAmaxRows / 8;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t c = (blockIdx.x * 32 + lane) * N, r0 = blockIdx.y * kAmaxRows;
   uint32_t top[N];
   float sum[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) top[i] = 0, sum[i] = 0.f;
-#pragma unroll
-  for (int k = 0; k < kAmaxRows / 8; ++k) {
-    const uint32_t r = r0 + warp + 8 * k;
+  auto take = [&](const Vec<T>& v, uint32_t r) {
     uint32_t mine = 0;
-    if (r < rows && c < cols) {
-      float f[N];
-      if (VEC && c + N <= cols) {
-        Vec<T> v;
-        v.raw = __ldg(reinterpret_cast<const uint4*>(x + r * ld + c));
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = v.at(i);
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = c + i < cols ? to_f32(x[r * ld + c + i]) : 0.f;
-      }
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const uint32_t b = mag_bits(f[i]);
-        mine = max(mine, b);
-        top[i] = max(top[i], b);
-        sum[i] += f[i];
-      }
+    for (int i = 0; i < N; ++i) {
+      const float f = v.at(i);
+      const uint32_t b = mag_bits(f);
+      mine = max(mine, b);
+      top[i] = max(top[i], b);
+      if constexpr (SUMS) sum[i] += f;
     }
-    mine = __reduce_max_sync(0xFFFFFFFFu, mine);
-    if (row_top && lane == 0 && r < rows && mine) atomicMax(row_top + r, mine);
+    if (row_top) {
+      mine = __reduce_max_sync(0xFFFFFFFFu, mine);
+      if (lane == 0 && r < rows && mine) atomicMax(row_top + r, mine);
+    }
+  };
+  if (VEC && (blockIdx.x + 1) * 32 * N <= cols && r0 + kAmaxRows <= rows) {   // inside: all loads together
+    Vec<T> v[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) v[k].raw = __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)(r0 + warp + 8 * k) * ld + c));
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) take(v[k], r0 + warp + 8 * k);
+  } else {
+#pragma unroll 1
+    for (int k = 0; k < kRows; ++k) {
+      const uint32_t r = r0 + warp + 8 * k;
+      Vec<T> v;
+      v.raw = make_uint4(0, 0, 0, 0);
+      if (r < rows)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (c + i < cols) v.set(i, x[(uint64_t)r * ld + c + i]);
+      take(v, r);
+    }
   }
   __shared__ uint32_t tops[8][32 * N];
-  __shared__ float part[8][32 * N];
+  __shared__ float part[SUMS ? 8 : 1][SUMS ? 32 * N : 1];
 #pragma unroll
-  for (int i = 0; i < N; ++i) tops[warp][lane + 32 * i] = top[i], part[warp][lane + 32 * i] = sum[i];
+  for (int i = 0; i < N; ++i) {
+    tops[warp][lane + 32 * i] = top[i];
+    if constexpr (SUMS) part[warp][lane + 32 * i] = sum[i];
+  }
   __syncthreads();
   for (int t = threadIdx.x; t < 32 * N; t += 256) {
     uint32_t m = 0;
-    float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) m = max(m, tops[w][t]), s += part[w][t];
+    for (int w = 0; w < 8; ++w) m = max(m, tops[w][t]);
     const uint32_t col = (blockIdx.x * 32 + t % 32) * N + t / 32;
     if (col < cols) {
       if (col_top && m) atomicMax(col_top + col, m);
-      if (sums) sums[(uint64_t)blockIdx.y * cols + col] = s;
+      if constexpr (SUMS) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) s += part[w][t];
+        sums[(uint64_t)blockIdx.y * cols + col] = s;
+      }
     }
   }
 }
 
-// Second reading: the codes.  A tile is 128 rows x 64 columns; a thread takes blocks of 4 x 4, writes their rows straight and
+// Second reading: the codes.  A tile is 128 x 128; a thread takes blocks of 4 rows x 8 columns, writes their rows straight and
 // their columns through shared memory, so that a column's 128 codes leave as one line.
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256)
     k_i8_codes(const T* x, uint64_t ld, uint32_t rows, uint32_t cols, const uint32_t* row_top, const uint32_t* col_top, const float* sums,
                int8_t* q, uint64_t ldq, float* scale, int8_t* qt, uint64_t ldqt, float* scale_t, float* col_sum) {
   pdl_prologue();
-  __shared__ float rinv[128], cinv[64];
-  __shared__ uint32_t turned[64][33];
-  const uint32_t r0 = blockIdx.y * 128, c0 = blockIdx.x * 64, tid = threadIdx.x;
+  constexpr int N = Vec<T>::kN, V = 8 / N;     // vectors of 16 bytes in 8 columns
+  __shared__ float rinv[128], cinv[128];
+  __shared__ uint32_t turned[128][33];
+  const uint32_t r0 = blockIdx.y * 128, c0 = blockIdx.x * 128, tid = threadIdx.x;
+  const bool inside = VEC && r0 + 128 <= rows && c0 + 128 <= cols;
+  const uint32_t lc = tid % 16 * 8, c = c0 + lc;
+  Vec<T> v[4][V];
+  auto fetch = [&](int half) {
+    const uint32_t r = r0 + (tid / 16 + 16 * half) * 4;
+    if (inside) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[i][j].raw = __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)(r + i) * ld + c) + j);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (j % N == 0) v[i][j / N].raw = make_uint4(0, 0, 0, 0);
+          if (r + i < rows && c + j < cols) v[i][j / N].set(j % N, x[(uint64_t)(r + i) * ld + c + j]);
+        }
+    }
+  };
+  fetch(0);
   if (tid < 128) {
     const uint32_t r = r0 + tid;
+    float s = 0.f, inv = 0.f;
     if (q && r < rows) {
-      float s, inv;
       scale_of(row_top[r], s, inv);
-      rinv[tid] = inv;
       if (blockIdx.x == 0) scale[r] = s;
     }
-  } else if (tid < 192) {
-    const uint32_t c = c0 + tid - 128;
-    if (c < cols) {
-      if (qt) {
-        float s, inv;
-        scale_of(col_top[c], s, inv);
-        cinv[tid - 128] = inv;
-        if (blockIdx.y == 0) scale_t[c] = s;
-      }
-      if (col_sum && blockIdx.y == 0) {
-        float s = 0.f;
-        for (uint32_t k = 0; k < (rows + kAmaxRows - 1) / kAmaxRows; ++k) s += sums[(uint64_t)k * cols + c];
-        col_sum[c] = s;
-      }
+    rinv[tid] = inv;
+  } else {
+    const uint32_t k = c0 + tid - 128;
+    float s = 0.f, inv = 0.f;
+    if (qt && k < cols) {
+      scale_of(col_top[k], s, inv);
+      if (blockIdx.y == 0) scale_t[k] = s;
+    }
+    cinv[tid - 128] = inv;
+    if (col_sum && blockIdx.y == 0 && k < cols) {
+      float t = 0.f;
+#pragma unroll 4
+      for (uint32_t b = 0; b < (rows + kAmaxRows - 1) / kAmaxRows; ++b) t += sums[(uint64_t)b * cols + k];
+      col_sum[k] = t;
     }
   }
   __syncthreads();
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    const uint32_t lc = tid % 16 * 4, lr = (tid / 16 + 16 * half) * 4, c = c0 + lc;
-    float f[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t r = r0 + lr + i;
-      const T* p = x + r * ld + c;
-      if (VEC && r < rows && c + 4 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-          const float4 v = __ldg(reinterpret_cast<const float4*>(p));
-          f[i][0] = v.x, f[i][1] = v.y, f[i][2] = v.z, f[i][3] = v.w;
-        } else {
-          const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) f[i][j] = to_f32(reinterpret_cast<const T*>(&v)[j]);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) f[i][j] = r < rows && c + j < cols ? to_f32(p[j]) : 0.f;
-      }
-    }
+    const uint32_t lr = (tid / 16 + 16 * half) * 4;
+    if (half) fetch(1);
+    auto at = [&](int i, int j) { return v[i][j / N].at(j % N); };
     if (q) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t r = r0 + lr + i;
-        const float v = rinv[lr + i];
-        if (r < rows && c < ldq)
-          *reinterpret_cast<uint32_t*>(q + r * ldq + c) =
-              pack4(code_of(f[i][0], v), code_of(f[i][1], v), code_of(f[i][2], v), code_of(f[i][3], v));
+        const float f = rinv[lr + i];
+        const uint32_t w0 = codes4(at(i, 0), at(i, 1), at(i, 2), at(i, 3), f), w1 = codes4(at(i, 4), at(i, 5), at(i, 6), at(i, 7), f);
+        if (r < rows && c < ldq) *reinterpret_cast<uint2*>(q + (uint64_t)r * ldq + c) = make_uint2(w0, w1);
       }
     }
     if (qt) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float v = c + j < cols ? cinv[lc + j] : 0.f;
-        turned[lc + j][lr / 4] = pack4(code_of(f[0][j], v), code_of(f[1][j], v), code_of(f[2][j], v), code_of(f[3][j], v));
-      }
+      for (int j = 0; j < 8; ++j) turned[lc + j][lr / 4] = codes4(at(0, j), at(1, j), at(2, j), at(3, j), cinv[lc + j]);
     }
   }
   if (!qt) return;
   __syncthreads();
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const uint32_t lc = tid / 32 + 8 * k, w = tid % 32;
-    if (c0 + lc < cols && r0 + 4 * w < ldqt) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + lc) * ldqt + r0 + 4 * w) = turned[lc][w];
+#pragma unroll 4
+  for (int k = 0; k < 16; ++k) {
+    const uint32_t l = tid / 32 + 8 * k, w = tid % 32;
+    if (c0 + l < cols && r0 + 4 * w < ldqt) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
   }
 }
 
@@ -415,7 +427,7 @@ __device__ __forceinline__ uint4 encode16(const T* row, uint32_t k0, uint32_t k,
 #pragma unroll
       for (int j = 0; j < Vec<T>::kN / 4; ++j)
         w[i * (Vec<T>::kN / 4) + j] =
-            pack4(code_of(v.at(4 * j), inv), code_of(v.at(4 * j + 1), inv), code_of(v.at(4 * j + 2), inv), code_of(v.at(4 * j + 3), inv));
+            codes4(v.at(4 * j), v.at(4 * j + 1), v.at(4 * j + 2), v.at(4 * j + 3), inv);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
@@ -424,7 +436,7 @@ __device__ __forceinline__ uint4 encode16(const T* row, uint32_t k0, uint32_t k,
   for (int h = 0; h < 2; ++h)
 #pragma unroll 1
     for (uint32_t i = k0 + 8 * h; i < k && i < k0 + 8 * h + 8; ++i)
-      v[h] |= (unsigned long long)(uint8_t)code_of(to_f32(row[i]), inv) << (8 * (i & 7));
+      v[h] |= (unsigned long long)(code_of(to_f32(row[i]), inv) & mask_of(inv) & 0xFFu) << (8 * (i & 7));
   return make_uint4((uint32_t)v[0], (uint32_t)(v[0] >> 32), (uint32_t)v[1], (uint32_t)(v[1] >> 32));
 }
 
@@ -660,13 +672,16 @@ cudaError_t quantize(const T* x, uint32_t rows, uint32_t cols, uint64_t ld, int8
                      float* scale_t, float* col_sum, uint8_t* ws, cudaStream_t st) {
   const bool vec = aligned(x, 16) && ld * sizeof(T) % 16 == 0;
   if (!qt && !col_sum) {
-    // as many threads as the row has vectors for two each, at most 256
-    const uint32_t nv = (cols + 15) / 16 * 16 / (vec ? Vec<T>::kN : 4);
-    const uint32_t want = (uint32_t)round_up((nv + 1) / 2, 32), bs = want < 32 ? 32 : want > 256 ? 256 : want;
-    if (vec)
+    const uint32_t nv = cols / Vec<T>::kN;
+    if (vec && cols % Vec<T>::kN == 0 && nv <= 256 * kKeep) {
+      // With rows enough to fill the device, as many vectors a thread as it can keep (8192 rows of 16 KB: 46 us with four, 40 with
+      // eight); with few rows, two: the row's latency is what counts.
+      const uint32_t each = rows >= 8 * (uint32_t)sm_count() ? kKeep : 2;
+      const uint32_t want = (uint32_t)round_up((nv + each - 1) / each, 32), bs = want < 32 ? 32 : want > 256 ? 256 : want;
       launch_pdl(k_i8_rows<T, true>, dim3(rows), dim3(bs), st, x, ld, cols, q, ldq, scale);
-    else
-      launch_pdl(k_i8_rows<T, false>, dim3(rows), dim3(bs), st, x, ld, cols, q, ldq, scale);
+    } else {
+      launch_pdl(k_i8_rows<T, false>, dim3(rows), dim3(256), st, x, ld, cols, q, ldq, scale);
+    }
     count_launches(1);
     return cudaGetLastError();
   }
@@ -675,17 +690,18 @@ cudaError_t quantize(const T* x, uint32_t rows, uint32_t cols, uint64_t ld, int8
   float* sums = col_sum ? reinterpret_cast<float*>(col_top + round_up(cols, 64)) : nullptr;
   cudaError_t e = cudaMemsetAsync(ws, 0, 4 * (round_up(rows, 64) + round_up(cols, 64)), st);
   if (e != cudaSuccess) return e;
-  const dim3 g1((cols + 32 * Vec<T>::kN - 1) / (32 * Vec<T>::kN), (rows + kAmaxRows - 1) / kAmaxRows), g2((cols + 63) / 64, (rows + 127) / 128);
+  const dim3 g1((cols + 32 * Vec<T>::kN - 1) / (32 * Vec<T>::kN), (rows + kAmaxRows - 1) / kAmaxRows), g2((cols + 127) / 128, (rows + 127) / 128);
   uint32_t *rt = q ? row_top : nullptr, *ct = qt ? col_top : nullptr;
-  if (vec) {
-    launch_pdl(k_i8_amax<T, true>, g1, dim3(256), st, x, ld, rows, cols, rt, ct, sums);
-    launch_pdl(k_i8_codes<T, true>, g2, dim3(256), st, x, ld, rows, cols, (const uint32_t*)rt, (const uint32_t*)ct, (const float*)sums, q,
-               ldq, scale, qt, ldqt, scale_t, col_sum);
-  } else {
-    launch_pdl(k_i8_amax<T, false>, g1, dim3(256), st, x, ld, rows, cols, rt, ct, sums);
-    launch_pdl(k_i8_codes<T, false>, g2, dim3(256), st, x, ld, rows, cols, (const uint32_t*)rt, (const uint32_t*)ct, (const float*)sums, q,
-               ldq, scale, qt, ldqt, scale_t, col_sum);
-  }
+  auto amax = [&](auto kernel) { launch_pdl(kernel, g1, dim3(256), st, x, ld, rows, cols, rt, ct, sums); };
+  if (sums)
+    vec ? amax(k_i8_amax<T, true, true>) : amax(k_i8_amax<T, false, true>);
+  else
+    vec ? amax(k_i8_amax<T, true, false>) : amax(k_i8_amax<T, false, false>);
+  auto codes = [&](auto kernel) {
+    launch_pdl(kernel, g2, dim3(256), st, x, ld, rows, cols, (const uint32_t*)rt, (const uint32_t*)ct, (const float*)sums, q, ldq, scale, qt, ldqt,
+               scale_t, col_sum);
+  };
+  vec ? codes(k_i8_codes<T, true>) : codes(k_i8_codes<T, false>);
   count_launches(2);
   return cudaGetLastError();
 }

@@ -15,6 +15,17 @@ from .binding import (DS_BF16, DS_DEV_MMA_TIMEOUT, DS_F16, DS_F32, DS_NEED_BUFFE
 
 _DTYPES = {torch.float32: DS_F32, torch.bfloat16: DS_BF16, torch.float16: DS_F16}
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_empty = torch.empty
+_call = _quantize_at = _matmul_at = _linear_at = _quantize_ws = _linear_ws = None
+
+
+def _load():
+    """Looks the library's functions up once: the calls below are short enough for every look-up to show."""
+    global _call, _quantize_at, _matmul_at, _linear_at, _quantize_ws, _linear_ws
+    lib = load_library()
+    _call, address = fast_call()
+    _quantize_at, _matmul_at, _linear_at = (address[n] for n in ("ds_i8_quantize", "ds_i8_matmul", "ds_i8_linear"))
+    _quantize_ws, _linear_ws = lib.ds_i8_quantize_workspace, lib.ds_i8_linear_workspace
 
 
 def _dtype(t: torch.dtype, what: str) -> int:
@@ -29,16 +40,9 @@ def _check(rc: int, what: str):
         raise DsqError(rc, what, load_library().ds_last_error().decode())
 
 
-def _same_device(device: torch.device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors on different devices: {device} and {t.device}")
-
-
 def _matrix(x: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int, torch.device]:
     """x as rows of consecutive entries; rows, columns, the distance between rows, the device."""
-    device = x.device
-    if device.type != "cuda":
+    if not x.is_cuda:
         raise ValueError(f"{what}: a CUDA tensor expected: there is no CPU path")
     shape = x.shape
     if len(shape) != 2:
@@ -48,45 +52,38 @@ def _matrix(x: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int, to
     if (c > 1 and step != 1) or (r > 1 and ld < c):
         x = x.contiguous()
         ld = c
-    return x, r, c, (ld if r > 1 else c), device
+    return x, r, c, (ld if r > 1 else c), x.device
 
 
-def _vector(v: torch.Tensor | None, n: int, what: str) -> int | None:
-    """The address of n contiguous float32 values, or None."""
+def _vector(v: torch.Tensor | None, n: int, what: str, device) -> int | None:
+    """The address of n contiguous float32 values on `device`, or None."""
     if v is None:
         return None
-    if v.dtype is not torch.float32 or v.dim() != 1 or v.shape[0] != n or not v.is_contiguous():
+    if v.dtype is not torch.float32 or v.shape != (n,) or not v.is_contiguous():
         raise ValueError(f"{what}: {n} contiguous float32 values expected, got {v.dtype} {tuple(v.shape)}")
+    if v.device != device:
+        raise ValueError(f"{what}: on {v.device}, the others on {device}")
     return v.data_ptr()
 
 
-def _stream_of(device: torch.device, stream) -> int:
-    return _raw_stream(device.index) if stream is None else stream.cuda_stream
+_status: dict = {}     # device index -> (word in which products report waits that ran out, its address)
 
 
-_status: dict = {}     # device -> (word in which products report waits that ran out, its address)
-
-
-def _dev_status(device: torch.device) -> int:
-    entry = _status.get(device)
+def _dev_status(index: int) -> int:
+    entry = _status.get(index)
     if entry is None:
-        word = torch.zeros(1, dtype=torch.int32, device=device)
-        torch.cuda.synchronize(device)          # cleared before any stream's product may set it
-        entry = _status[device] = (word, word.data_ptr())
+        word = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", index))
+        torch.cuda.synchronize(index)          # cleared before any stream's product may set it
+        entry = _status[index] = (word, word.data_ptr())
     return entry[1]
 
 
 def device_status(device: str | torch.device = "cuda") -> int:
     """DS_DEV_* flags of the matrix operators on a device; 0 unless one of them failed.  Waits for the device."""
     device = torch.device(device)
-    if device.index is None:
-        device = torch.device(device.type, torch.cuda.current_device())
-    _dev_status(device)
-    return int(_status[device][0].item())
-
-
-def _up(v: int, to: int) -> int:
-    return (v + to - 1) // to * to
+    index = torch.cuda.current_device() if device.index is None else device.index
+    _dev_status(index)
+    return int(_status[index][0].item())
 
 
 class Int8Matrix:
@@ -96,19 +93,16 @@ class Int8Matrix:
     __slots__ = ("rows", "cols", "ld", "device", "codes_ptr", "scale_ptr", "_codes", "_scale")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor):
-        device = codes.device
-        if codes.dtype is not torch.int8 or codes.dim() != 2:
-            raise ValueError("codes: a row-major int8 matrix expected")
-        self.rows, self.cols = r, c = codes.shape
+        if codes.dtype is not torch.int8 or not codes.is_cuda:
+            raise ValueError("codes: a row-major int8 matrix on a CUDA device expected: there is no CPU path")
+        r, c = codes.shape
         ld, step = codes.stride()
         if c > 1 and step != 1:
             raise ValueError("codes: a row-major int8 matrix expected")
-        if device.type != "cuda" or scale.device != device:
-            raise ValueError("CUDA tensors on one device expected: there is no CPU path")
-        self.ld = ld if r > 1 else _up(c, 16)
-        self.device = device
+        self.rows, self.cols, self.device = r, c, codes.device
+        self.ld = ld if r > 1 else (c + 15) // 16 * 16
         self._codes, self._scale = codes, scale
-        self.codes_ptr, self.scale_ptr = codes.data_ptr(), _vector(scale, r, "scale")
+        self.codes_ptr, self.scale_ptr = codes.data_ptr(), _vector(scale, r, "scale", self.device)
 
     @classmethod
     def _within(cls, buf: torch.Tensor, base: int, at: int, scale_at: int, rows: int, cols: int, ld: int, device) -> "Int8Matrix":
@@ -141,7 +135,7 @@ class Int8Matrix:
     def pack(cls, codes: torch.Tensor, scale: torch.Tensor) -> "Int8Matrix":
         """A copy of any int8 matrix with its rows on 16-byte boundaries."""
         r, c = codes.shape
-        out = torch.empty(r, max(16, _up(c, 16)), dtype=torch.int8, device=codes.device)[:, :c]
+        out = _empty(r, max(16, (c + 15) // 16 * 16), dtype=torch.int8, device=codes.device)[:, :c]
         out.copy_(codes)
         return cls(out, scale.to(torch.float32, copy=True))
 
@@ -154,22 +148,25 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
     sums, in that order; one thing asked for is returned by itself, several as a tuple."""
     if not (rows or cols or col_sum):
         raise ValueError("nothing to compute")
+    if _call is None:
+        _load()
     dt = _dtype(x.dtype, "x")
     x, r, c, ld, device = _matrix(x, "x")
-    call, address = fast_call()
     # one buffer: codes, scales, sums, and at its end what only the call itself uses
-    ldr, ldc = max(16, _up(c, 16)), max(16, _up(r, 16))
+    ldr, ldc = (c + 15) // 16 * 16 or 16, (r + 15) // 16 * 16 or 16
     at_c = r * ldr if rows else 0
     at_rs = at_c + (c * ldc if cols else 0)
-    at_cs = at_rs + (_up(4 * r, 16) if rows else 0)
-    at_sum = at_cs + (_up(4 * c, 16) if cols else 0)
-    at_ws = at_sum + (_up(4 * c, 16) if col_sum else 0)
-    ws = load_library().ds_i8_quantize_workspace(r, c, 1 if col_sum else 0) if cols or col_sum else 0
-    buf = torch.empty(at_ws + ws + 16, dtype=torch.uint8, device=device)
+    at_cs = at_rs + (4 * ldc if rows else 0)
+    at_sum = at_cs + (4 * ldr if cols else 0)
+    at_ws = at_sum + (4 * ldr if col_sum else 0)
+    ws = _quantize_ws(r, c, 1 if col_sum else 0) if cols or col_sum else 0
+    buf = _empty(at_ws + ws + 16, dtype=torch.uint8, device=device)
     base = buf.data_ptr()
-    _check(call(address["ds_i8_quantize"], x.data_ptr(), dt, r, c, ld, base if rows else 0, ldr, base + at_rs if rows else 0,
-                base + at_c if cols else 0, ldc, base + at_cs if cols else 0, base + at_sum if col_sum else 0,
-                base + at_ws if ws else 0, ws, _stream_of(device, stream)), "ds_i8_quantize")
+    rc = _call(_quantize_at, x.data_ptr(), dt, r, c, ld, base if rows else 0, ldr, base + at_rs if rows else 0,
+               base + at_c if cols else 0, ldc, base + at_cs if cols else 0, base + at_sum if col_sum else 0,
+               base + at_ws if ws else 0, ws, _raw_stream(device.index) if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc, "ds_i8_quantize")
     got = []
     if rows:
         got.append(Int8Matrix._within(buf, base, 0, at_rs, r, c, ldr, device))
@@ -180,51 +177,65 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
     return got[0] if len(got) == 1 else tuple(got)
 
 
-def _out(out: torch.Tensor | None, m: int, n: int, dtype: torch.dtype, device) -> tuple[torch.Tensor, int, int]:
-    """The output, its type, the distance between its rows."""
-    if out is None:
-        return torch.empty((m, n), dtype=dtype, device=device), _dtype(dtype, "out"), n
+def _out(out: torch.Tensor, m: int, n: int, device) -> int:
+    """The distance between the rows of a given output."""
     if out.shape != (m, n) or out.device != device:
         raise ValueError(f"out: a matrix {(m, n)} on {device} expected, got {tuple(out.shape)} on {out.device}")
     ld, step = out.stride()
     if (n > 1 and step != 1) or (m > 1 and ld < n):
         raise ValueError("out: rows of consecutive entries expected")
-    return out, _dtype(out.dtype, "out"), (ld if m > 1 else n)
+    return ld if m > 1 else n
 
 
 def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """a b^T (+ bias): [a rows, b rows], the sums exact in 32-bit integers."""
-    if a.cols != b.cols:
-        raise ValueError(f"lengths differ: {a.cols} and {b.cols}")
-    device = a.device
-    bp = _vector(bias, b.rows, "bias")
-    if b.device != device or (bias is not None and bias.device != device):
-        raise ValueError("tensors on different devices")
-    out, odt, ldo = _out(out, a.rows, b.rows, out_dtype, device)
-    call, address = fast_call()
-    _check(call(address["ds_i8_matmul"], a.codes_ptr, a.ld, a.scale_ptr, b.codes_ptr, b.ld, b.scale_ptr, bp, a.rows, b.rows, a.cols,
-                out.data_ptr(), odt, ldo, _dev_status(device), _stream_of(device, stream)), "ds_i8_matmul")
+    if _call is None:
+        _load()
+    m, n, k, device = a.rows, b.rows, a.cols, a.device
+    if b.cols != k:
+        raise ValueError(f"lengths differ: {k} and {b.cols}")
+    if b.device != device:
+        raise ValueError(f"matrices on {device} and {b.device}")
+    bp = None if bias is None else _vector(bias, n, "bias", device)
+    if out is None:
+        out, ldo = _empty((m, n), dtype=out_dtype, device=device), n
+    else:
+        ldo = _out(out, m, n, device)
+    index = device.index
+    rc = _call(_matmul_at, a.codes_ptr, a.ld, a.scale_ptr, b.codes_ptr, b.ld, b.scale_ptr, bp, m, n, k, out.data_ptr(),
+               _dtype(out.dtype, "out"), ldo, _dev_status(index), _raw_stream(index) if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc, "ds_i8_matmul")
     return out
 
 
 def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """x W^T (+ bias) for weights quantised before: x [tokens, k] is quantised by rows on the way."""
+    if _call is None:
+        _load()
     dt = _dtype(x.dtype, "x")
     x, m, k, ld, device = _matrix(x, "x")
     n = w.rows
     if w.cols != k:
         raise ValueError(f"x has {k} columns, the weights {w.cols}")
-    bp = _vector(bias, n, "bias")
-    if w.device != device or (bias is not None and bias.device != device):
-        raise ValueError("tensors on different devices")
-    out, odt, ldo = _out(out, m, n, out_dtype or x.dtype, device)
-    call, address = fast_call()
-    size = load_library().ds_i8_linear_workspace(m, k, n)
-    ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
-    _check(call(address["ds_i8_linear"], x.data_ptr(), dt, m, k, ld, w.codes_ptr, w.ld, w.scale_ptr, bp, n, out.data_ptr(), odt, ldo,
-                None if ws is None else ws.data_ptr(), size, _dev_status(device), _stream_of(device, stream)), "ds_i8_linear")
+    if w.device != device:
+        raise ValueError(f"x on {device}, the weights on {w.device}")
+    bp = None if bias is None else _vector(bias, n, "bias", device)
+    if out is not None:
+        ldo, odt = _out(out, m, n, device), _dtype(out.dtype, "out")
+    elif out_dtype is None:
+        out, ldo, odt = x.new_empty((m, n)), n, dt
+    else:
+        out, ldo, odt = _empty((m, n), dtype=out_dtype, device=device), n, _dtype(out_dtype, "out")
+    size = _linear_ws(m, k, n)
+    ws = _empty(size, dtype=torch.uint8, device=device) if size else None
+    index = device.index
+    rc = _call(_linear_at, x.data_ptr(), dt, m, k, ld, w.codes_ptr, w.ld, w.scale_ptr, bp, n, out.data_ptr(), odt, ldo,
+               ws.data_ptr() if size else None, size, _dev_status(index), _raw_stream(index) if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc, "ds_i8_linear")
     return out
 
 
@@ -319,7 +330,7 @@ class OrthUpdate:
         xp = self._span(x, "x", (torch.float32,))
         _check(self.lib.ds_orth_update(self.handle, gp, _DTYPES[g.dtype], mp, None if out is None else out.data_ptr(),
                                        DS_F32 if out is None else _DTYPES[out.dtype], xp, gamma, decay,
-                                       _stream_of(self.device, stream)), "ds_orth_update")
+                                       _raw_stream(self.device.index) if stream is None else stream.cuda_stream), "ds_orth_update")
         return out
 
     def timed_out(self) -> bool:
