@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32
 #pragma unroll
     for (int k = 0; k < kRows; ++k) take(v[k], r0 + warp + 8 * k);
   } else {
-#pragma unroll 1
+#pragma unroll 4
     for (int k = 0; k < kRows; ++k) {
       const uint32_t r = r0 + warp + 8 * k;
       Vec<T> v;
@@ -276,6 +276,118 @@ __global__ void __launch_bounds__(256)
 #pragma unroll 4
   for (int k = 0; k < 16; ++k) {
     const uint32_t l = tid / 32 + 8 * k, w = tid % 32;
+    if (c0 + l < cols && r0 + 4 * w < ldqt) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
+  }
+}
+
+// Both readings in one launch, for matrices so small that launches are what they cost: a CTA looks its tile's rows and columns
+// through from end to end for their largest magnitudes (the matrix lies in L2; 512 x 768: 16 MB of reads in all), then encodes
+// the tile, 64 x 64.  512 x 768 in bf16: 7.6 us, and one launch for the host instead of three.
+// Warps 0..7 hold the tile and look through its rows, warps 8..15 through its columns.
+template <class T>
+__global__ void __launch_bounds__(512)
+    k_i8_small(const T* x, uint64_t ld, uint32_t rows, uint32_t cols, int8_t* q, uint64_t ldq, float* scale, int8_t* qt, uint64_t ldqt,
+               float* scale_t, float* col_sum) {
+  pdl_prologue();
+  constexpr int N = Vec<T>::kN, kLanes = 64 / N, kStep = 256 / kLanes;    // lanes across 64 columns; rows that eight warps take at once
+  __shared__ float rinv[64], cinv[64];
+  __shared__ uint32_t tops[kStep][64 + 1], turned[64][17];
+  __shared__ float part[kStep][64 + 1];
+  const uint32_t r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tid = threadIdx.x & 255, warp = tid >> 5, lane = tid & 31;
+  auto vec_at = [&](uint32_t r, uint32_t c) { return __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)r * ld + c)); };   // c < cols, a multiple of N
+  const uint32_t lc = tid % 16 * 4, lr = tid / 16 * 4, c = c0 + lc;        // 4 x 4 blocks of the tile
+  float f[4][4];
+  if (threadIdx.x < 256) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool in = r0 + lr + i < rows && c < cols;     // cols is a multiple of 4
+      const T* p = x + (uint64_t)(r0 + lr + i) * ld + c;
+      if constexpr (sizeof(T) == 4) {
+        const float4 v = in ? __ldg(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        f[i][0] = v.x, f[i][1] = v.y, f[i][2] = v.z, f[i][3] = v.w;
+      } else {
+        const uint2 v = in ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[i][j] = to_f32(reinterpret_cast<const T*>(&v)[j]);
+      }
+    }
+    uint32_t top[8] = {};      // eight rows a warp
+    if (q)
+      for (uint32_t k = lane * N; k < cols; k += 32 * N) {
+        Vec<T> v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i].raw = r0 + warp * 8 + i < rows ? vec_at(r0 + warp * 8 + i, k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int j = 0; j < N; ++j) top[i] = max(top[i], mag_bits(v[i].at(j)));
+      }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, top[i]);
+      if (lane == i && q) {
+        float s, inv;
+        scale_of(m, s, inv);
+        rinv[warp * 8 + i] = inv;
+        if (blockIdx.x == 0 && r0 + warp * 8 + i < rows) scale[r0 + warp * 8 + i] = s;
+      }
+    }
+  } else if (qt || col_sum) {
+    const uint32_t k = c0 + tid % kLanes * N, first = tid / kLanes;
+    uint32_t top[N] = {};
+    float sum[N] = {};
+    if (k < cols) {
+      for (uint32_t r = first; r < rows; r += 8 * kStep) {
+        Vec<T> v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i].raw = r + i * kStep < rows ? vec_at(r + i * kStep, k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) top[j] = max(top[j], mag_bits(v[i].at(j)));
+          sum[j] += ((v[0].at(j) + v[1].at(j)) + (v[2].at(j) + v[3].at(j))) + ((v[4].at(j) + v[5].at(j)) + (v[6].at(j) + v[7].at(j)));
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) tops[first][tid % kLanes * N + j] = top[j], part[first][tid % kLanes * N + j] = sum[j];
+    // the eight warps of the columns alone
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (tid < 64) {
+      uint32_t m = 0;
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < kStep; i += 4) {
+        m = max(max(m, tops[i][tid]), max(tops[i + 1][tid], max(tops[i + 2][tid], tops[i + 3][tid])));
+        t += (part[i][tid] + part[i + 1][tid]) + (part[i + 2][tid] + part[i + 3][tid]);
+      }
+      float s, inv;
+      scale_of(m, s, inv);
+      cinv[tid] = inv;
+      if (blockIdx.y == 0 && c0 + tid < cols) {
+        if (qt) scale_t[c0 + tid] = s;
+        if (col_sum) col_sum[c0 + tid] = t;
+      }
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 256) {
+    if (q) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r0 + lr + i < rows && c < ldq)
+          *reinterpret_cast<uint32_t*>(q + (uint64_t)(r0 + lr + i) * ldq + c) = codes4(f[i][0], f[i][1], f[i][2], f[i][3], rinv[lr + i]);
+    }
+    if (qt) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) turned[lc + j][lr / 4] = codes4(f[0][j], f[1][j], f[2][j], f[3][j], cinv[lc + j]);
+    }
+  }
+  if (!qt) return;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t l = threadIdx.x / 16 + 32 * k, w = threadIdx.x % 16;
     if (c0 + l < cols && r0 + 4 * w < ldqt) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
   }
 }
@@ -682,6 +794,14 @@ cudaError_t quantize(const T* x, uint32_t rows, uint32_t cols, uint64_t ld, int8
     } else {
       launch_pdl(k_i8_rows<T, false>, dim3(rows), dim3(256), st, x, ld, cols, q, ldq, scale);
     }
+    count_launches(1);
+    return cudaGetLastError();
+  }
+  // One launch where a CTA's reading stays under 400 KB and all CTAs' under 64 MB (1024 x 1024 in bf16, at both limits: 11 us
+  // either way on the device, and two launches less for the host); rows of whole vectors only.
+  const uint64_t reads = ((uint64_t)rows + cols) * 64 * sizeof(T), ctas = (uint64_t)((rows + 63) / 64) * ((cols + 63) / 64);
+  if (vec && cols % Vec<T>::kN == 0 && reads <= 400 * 1024 && reads * ctas <= (64u << 20)) {
+    launch_pdl(k_i8_small<T>, dim3((cols + 63) / 64, (rows + 63) / 64), dim3(512), st, x, ld, rows, cols, q, ldq, scale, qt, ldqt, scale_t, col_sum);
     count_launches(1);
     return cudaGetLastError();
   }
