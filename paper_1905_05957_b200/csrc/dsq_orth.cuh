@@ -48,8 +48,8 @@ struct OrthOut {
   float keep, rate;
 };
 
-// Matrices whose shorter side is at most 128 and whose longer side fits: one cluster of CTAs a matrix, everything in one launch
-// (dsq_orth_small.cu).  Returns the CTAs a matrix takes, 0 where it does not fit.
+// Matrices whose shorter side is at most 64 and whose longer side is not too long: one cluster of CTAs a matrix, everything in one launch
+// (dsq_orth_small.cu).  Returns the CTAs a matrix takes, 0 where the general form is taken.
 uint32_t orth_small_ctas(uint32_t m, uint32_t n, uint32_t batch);
 cudaError_t launch_orth_small(const ds_orth_config& c, uint32_t ctas, const Momentum& mo, int g_dtype, const OrthOut& o, cudaStream_t st);
 

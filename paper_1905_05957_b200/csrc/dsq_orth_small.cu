@@ -1,12 +1,13 @@
-// The orthogonalised update of small matrices in one launch: X is [m, n], m <= 128, and a cluster of CTAs keeps it in shared
+// The orthogonalised update of small matrices in one launch: X is [m, n], m <= 64, and a cluster of CTAs keeps it in shared
 // memory for all steps, each CTA a slice of columns.  Of a step  A = X X^T,  B = b A + c A A,  X = a X + B X  only A needs the
 // other slices: the CTAs' sums are added through distributed shared memory, every CTA a share of the rows, and handed to all;
 // B is computed by every CTA for itself.  The same goes for the norm.
 //
-// A launch of the general form costs 4 to 5 us whatever its size, and an update has seventeen of them; here four 64 x 576
-// matrices take the time of their sums alone.  Since the tensor cores are idle most of that time, the products are taken in
-// two halves of either operand (hi hi + hi lo + lo hi on 16-bit floats: 22 bits), which small matrices need: their roundings do
-// not average out.  The warp instruction m16n8k16 is used; the operands are far too small for tiles of 128 rows to pay.
+// A launch of the general form costs 3 to 4 us whatever its size, and an update has seventeen of them.  Here a step takes 4 us,
+// about a third of it products, a third the exchange of A and a third their latencies: 34 us for four 64 x 576, 62 in the general
+// form.  The products are taken in two halves of either operand (hi hi + hi lo + lo hi on 16-bit floats: 22 bits), which small
+// matrices need: their roundings do not average out.  The warp instruction m16n8k16 is used; a tile of the tensor core's own
+// instruction would be half empty.  (Shorter sides up to 128 were slower than the general form, 77 against 59 us for 128 x 128.)
 #include "dsq_mma.cuh"
 #include "dsq_orth.cuh"
 
@@ -16,6 +17,7 @@ namespace {
 
 constexpr int kSmallThreads = 512, kSmallWarps = kSmallThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int MP = 64;              // rows of X, those past its end zeros
 // (Loops here are unrolled no further than they are written: the whole kernel runs in some ten thousand cycles, and fetching its
 // instructions for the first time is a good part of them.  A form with everything unrolled took twice as long.)
 
@@ -57,7 +59,6 @@ __device__ __forceinline__ float2 join2(uint32_t hi, uint32_t lo) {
 
 // Shared memory of a CTA, in bytes: X hi, X lo [MP][w + 8] halves; A hi, A lo [MP][MP + 8]; and one block that is the CTA's share
 // of A in floats [MP][MP + 4], then B hi, B lo.  (Rows 16 bytes longer than a multiple of 32 spread ldmatrix over all banks.)
-template <int MP>
 struct SmallLayout {
   uint32_t w, pitch;      // columns of a slice (a multiple of 16), bytes between rows of X
   static constexpr uint32_t kPitchA = (MP + 8) * 2, kHalfA = MP * kPitchA, kPitchP = (MP + 4) * 4;
@@ -76,14 +77,14 @@ struct SmallArgs {
   float a, b, c, eps;
 };
 
-template <class T, int MP>
+template <class T>
 __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs p) {
   constexpr int kRowTiles = MP / 16, kHalves = kSmallWarps / kRowTiles, kCols = MP / kHalves, kTiles = kCols / 8;
-  constexpr int kChunkTiles = MP == 64 ? 4 : 8, kChunk = kHalves * kChunkTiles * 8;    // 128 columns at a time
+  constexpr int kChunkTiles = 4, kChunk = kHalves * kChunkTiles * 8;    // 128 columns at a time
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ double sums[kMaxCluster], warp_sum[kSmallWarps];
   pdl_prologue();
-  const SmallLayout<MP> L(p.w);
+  const SmallLayout L(p.w);
   const uint32_t base = smem_u32(dyn), xh = base, xl = base + L.x_half(), ah = base + L.at_a(), al = ah + L.kHalfA, ps = base + L.at_p(),
                  bh = ps, bl = ps + L.kHalfA;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -294,15 +295,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs
 
 uint32_t slice(uint32_t n, uint32_t ctas) { return ((n + ctas - 1) / ctas + 15) / 16 * 16; }
 constexpr uint32_t kSmallSmem = 225 * 1024;
-uint32_t small_bytes(uint32_t m, uint32_t w) { return m <= 64 ? SmallLayout<64>(w).bytes() : SmallLayout<128>(w).bytes(); }
-
-template <class T, int MP>
+template <class T>
 cudaError_t launch(const SmallArgs& a, uint32_t ctas, uint32_t batch, cudaStream_t st) {
-  allow_smem_for<k_orth_small<T, MP>>(kSmallSmem);
+  allow_smem_for<k_orth_small<T>>(kSmallSmem);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(ctas * batch);
   cfg.blockDim = dim3(kSmallThreads);
-  cfg.dynamicSmemBytes = SmallLayout<MP>(a.w).bytes();
+  cfg.dynamicSmemBytes = SmallLayout(a.w).bytes();
   cfg.stream = st;
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -312,7 +311,7 @@ cudaError_t launch(const SmallArgs& a, uint32_t ctas, uint32_t batch, cudaStream
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  (void)cudaLaunchKernelEx(&cfg, k_orth_small<T, MP>, a);
+  (void)cudaLaunchKernelEx(&cfg, k_orth_small<T>, a);
   count_launches(1);
   return cudaGetLastError();
 }
@@ -321,16 +320,19 @@ cudaError_t launch(const SmallArgs& a, uint32_t ctas, uint32_t batch, cudaStream
 
 namespace dsq {
 
+// Time in us, fitted to measurements: slices of 32, 64, 80, 128, 256, 512 columns took 21, 26, 34, 38, 58 and 98 for one wave of
+// clusters.  The general form takes 50 to 76 for m <= 64 (1 x 64 x 64: 52, 1 x 64 x 2048: 72, 40 x 64 x 576: 76).
 uint32_t orth_small_ctas(uint32_t m, uint32_t n, uint32_t batch) {
-  if (m > 128) return 0;
-  // slices of about 64 columns: narrower ones leave a CTA less work than the exchange costs
-  uint32_t c = 1;
-  while (c < kMaxCluster && n > 64 * c) c *= 2;
-  while (c < kMaxCluster && small_bytes(m, slice(n, c)) > kSmallSmem) c *= 2;
-  if (small_bytes(m, slice(n, c)) > kSmallSmem) return 0;
-  // many matrices fill the SMs with fewer CTAs each
-  while (c > 1 && (uint64_t)batch * c > (uint64_t)sm_count() && small_bytes(m, slice(n, c / 2)) <= kSmallSmem) c /= 2;
-  return c;
+  if (m > MP) return 0;
+  double least = 65;
+  uint32_t best = 0;
+  for (uint32_t c = 1; c <= kMaxCluster; c *= 2) {
+    const uint32_t w = slice(n, c), at_once = c == 1 ? (uint32_t)sm_count() : (uint32_t)cluster_count(c);
+    if (SmallLayout(w).bytes() > kSmallSmem || at_once == 0) continue;
+    const double t = (double)((batch + at_once - 1) / at_once) * (16 + 0.16 * w + (c > 1 ? 5 : 0));
+    if (t < least) least = t, best = c;
+  }
+  return best;
 }
 
 cudaError_t launch_orth_small(const ds_orth_config& c, uint32_t ctas, const Momentum& mo, int g_dtype, const OrthOut& o, cudaStream_t st) {
@@ -348,13 +350,9 @@ cudaError_t launch_orth_small(const ds_orth_config& c, uint32_t ctas, const Mome
   a.b = c.b;
   a.c = c.c;
   a.eps = c.eps;
-  if (a.m <= 64)
-    return g_dtype == DS_F32    ? launch<float, 64>(a, ctas, c.batch, st)
-           : g_dtype == DS_BF16 ? launch<__nv_bfloat16, 64>(a, ctas, c.batch, st)
-                                : launch<__half, 64>(a, ctas, c.batch, st);
-  return g_dtype == DS_F32    ? launch<float, 128>(a, ctas, c.batch, st)
-         : g_dtype == DS_BF16 ? launch<__nv_bfloat16, 128>(a, ctas, c.batch, st)
-                              : launch<__half, 128>(a, ctas, c.batch, st);
+  return g_dtype == DS_F32    ? launch<float>(a, ctas, c.batch, st)
+         : g_dtype == DS_BF16 ? launch<__nv_bfloat16>(a, ctas, c.batch, st)
+                              : launch<__half>(a, ctas, c.batch, st);
 }
 
 }  // namespace dsq
