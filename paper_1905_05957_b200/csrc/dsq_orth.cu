@@ -401,7 +401,7 @@ inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * t
 
 bool orth_config_ok(const ds_orth_config* c) {
   if (!c || c->rows < 1 || c->cols < 1 || c->batch < 1 || c->batch > 65535 || c->rows > (1u << 20) || c->cols > (1u << 20)) return false;
-  if (c->steps < 1 || c->steps > 32 || (c->flags & ~DS_ORTH_NESTEROV)) return false;
+  if (c->steps < 1 || c->steps > 32 || (c->flags & ~DS_ORTH_NESTEROV) || c->reserved) return false;
   if (c->stride && c->stride < (uint64_t)c->rows * c->cols) return false;
   for (float v : {c->a, c->b, c->c, c->momentum, c->eps, c->scale})
     if (!std::isfinite(v)) return false;
