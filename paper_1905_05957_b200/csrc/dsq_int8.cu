@@ -132,7 +132,9 @@ __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32
   pdl_prologue();
   constexpr int N = Vec<T>::kN, kRows = kAmaxRows / 8;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t c = (blockIdx.x * 32 + lane) * N, r0 = blockIdx.y * kAmaxRows;
+  // a lane's columns: a vector's, or (rows on no boundary) every 32nd, so that a warp reads consecutive entries
+  const uint32_t c0 = blockIdx.x * 32 * N, r0 = blockIdx.y * kAmaxRows;
+  auto col = [&](int i) { return c0 + (VEC ? lane * N + i : lane + 32 * i); };
   uint32_t top[N];
   float sum[N];
 #pragma unroll
@@ -152,25 +154,22 @@ __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32
       if (lane == 0 && r < rows && mine) atomicMax(row_top + r, mine);
     }
   };
-  if (VEC && (blockIdx.x + 1) * 32 * N <= cols && r0 + kAmaxRows <= rows) {   // inside: all loads together
-    Vec<T> v[kRows];
+  Vec<T> v[kRows];
+  if (VEC && c0 + 32 * N <= cols && r0 + kAmaxRows <= rows) {   // inside
 #pragma unroll
-    for (int k = 0; k < kRows; ++k) v[k].raw = __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)(r0 + warp + 8 * k) * ld + c));
-#pragma unroll
-    for (int k = 0; k < kRows; ++k) take(v[k], r0 + warp + 8 * k);
+    for (int k = 0; k < kRows; ++k) v[k].raw = __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)(r0 + warp + 8 * k) * ld + col(0)));
   } else {
-#pragma unroll 4
+#pragma unroll
     for (int k = 0; k < kRows; ++k) {
       const uint32_t r = r0 + warp + 8 * k;
-      Vec<T> v;
-      v.raw = make_uint4(0, 0, 0, 0);
-      if (r < rows)
+      v[k].raw = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (c + i < cols) v.set(i, x[(uint64_t)r * ld + c + i]);
-      take(v, r);
+      for (int i = 0; i < N; ++i)
+        if (r < rows && col(i) < cols) v[k].set(i, x[(uint64_t)r * ld + col(i)]);
     }
   }
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) take(v[k], r0 + warp + 8 * k);
   __shared__ uint32_t tops[8][32 * N];
   __shared__ float part[SUMS ? 8 : 1][SUMS ? 32 * N : 1];
 #pragma unroll
@@ -183,14 +182,14 @@ __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32
     uint32_t m = 0;
 #pragma unroll
     for (int w = 0; w < 8; ++w) m = max(m, tops[w][t]);
-    const uint32_t col = (blockIdx.x * 32 + t % 32) * N + t / 32;
-    if (col < cols) {
-      if (col_top && m) atomicMax(col_top + col, m);
+    const uint32_t at = c0 + (VEC ? t % 32 * N + t / 32 : t);
+    if (at < cols) {
+      if (col_top && m) atomicMax(col_top + at, m);
       if constexpr (SUMS) {
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) s += part[w][t];
-        sums[(uint64_t)blockIdx.y * cols + col] = s;
+        sums[(uint64_t)blockIdx.y * cols + at] = s;
       }
     }
   }
@@ -198,7 +197,7 @@ __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32
 
 // Second reading: the codes.  A tile is 128 x 128; a thread takes blocks of 4 rows x 8 columns, writes their rows straight and
 // their columns through shared memory, so that a column's 128 codes leave as one line.
-template <class T, bool VEC>
+template <class T>
 __global__ void __launch_bounds__(256)
     k_i8_codes(const T* x, uint64_t ld, uint32_t rows, uint32_t cols, const uint32_t* row_top, const uint32_t* col_top, const float* sums,
                int8_t* q, uint64_t ldq, float* scale, int8_t* qt, uint64_t ldqt, float* scale_t, float* col_sum) {
@@ -207,7 +206,7 @@ __global__ void __launch_bounds__(256)
   __shared__ float rinv[128], cinv[128];
   __shared__ uint32_t turned[128][33];
   const uint32_t r0 = blockIdx.y * 128, c0 = blockIdx.x * 128, tid = threadIdx.x;
-  const bool inside = VEC && r0 + 128 <= rows && c0 + 128 <= cols;
+  const bool inside = r0 + 128 <= rows && c0 + 128 <= cols;
   const uint32_t lc = tid % 16 * 8, c = c0 + lc;
   Vec<T> v[4][V];
   auto fetch = [&](int half) {
@@ -276,6 +275,72 @@ __global__ void __launch_bounds__(256)
 #pragma unroll 4
   for (int k = 0; k < 16; ++k) {
     const uint32_t l = tid / 32 + 8 * k, w = tid % 32;
+    if (c0 + l < cols && r0 + 4 * w < ldqt) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
+  }
+}
+
+// The same where rows start on no boundary of 16 bytes: tiles of 64 x 64, read entry by entry along the rows and handed to their
+// threads through shared memory (straight reads of 4 x 8 blocks took twice as long: 1999 x 1153 floats 9.2 us, now 6.1).
+template <class T>
+__global__ void __launch_bounds__(256)
+    k_i8_codes_odd(const T* x, uint64_t ld, uint32_t rows, uint32_t cols, const uint32_t* row_top, const uint32_t* col_top, const float* sums,
+                   int8_t* q, uint64_t ldq, float* scale, int8_t* qt, uint64_t ldqt, float* scale_t, float* col_sum) {
+  pdl_prologue();
+  __shared__ float rinv[64], cinv[64], tile[64][65];
+  __shared__ uint32_t turned[64][17];
+  const uint32_t r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tid = threadIdx.x;
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t r = r0 + tid / 64 + 4 * i, c = c0 + tid % 64;
+    v[i] = r < rows && c < cols ? to_f32(x[(uint64_t)r * ld + c]) : 0.f;
+  }
+  if (tid < 64) {
+    float s = 0.f, inv = 0.f;
+    if (q && r0 + tid < rows) {
+      scale_of(row_top[r0 + tid], s, inv);
+      if (blockIdx.x == 0) scale[r0 + tid] = s;
+    }
+    rinv[tid] = inv;
+  } else if (tid < 128) {
+    const uint32_t k = c0 + tid - 64;
+    float s = 0.f, inv = 0.f;
+    if (qt && k < cols) {
+      scale_of(col_top[k], s, inv);
+      if (blockIdx.y == 0) scale_t[k] = s;
+    }
+    cinv[tid - 64] = inv;
+  } else if (tid < 192) {
+    const uint32_t k = c0 + tid - 128;
+    if (col_sum && blockIdx.y == 0 && k < cols) {
+      float t = 0.f;
+#pragma unroll 4
+      for (uint32_t b = 0; b < (rows + kAmaxRows - 1) / kAmaxRows; ++b) t += sums[(uint64_t)b * cols + k];
+      col_sum[k] = t;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) tile[tid / 64 + 4 * i][tid % 64] = v[i];
+  __syncthreads();
+  const uint32_t lc = tid % 16 * 4, lr = tid / 16 * 4, c = c0 + lc;
+  float f[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[i][j] = tile[lr + i][lc + j];
+  if (q) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (r0 + lr + i < rows && c < ldq)
+        *reinterpret_cast<uint32_t*>(q + (uint64_t)(r0 + lr + i) * ldq + c) = codes4(f[i][0], f[i][1], f[i][2], f[i][3], rinv[lr + i]);
+  }
+  if (!qt) return;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) turned[lc + j][lr / 4] = codes4(f[0][j], f[1][j], f[2][j], f[3][j], cinv[lc + j]);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t l = tid / 16 + 16 * k, w = tid % 16;
     if (c0 + l < cols && r0 + 4 * w < ldqt) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
   }
 }
@@ -490,11 +555,14 @@ __global__ void __launch_bounds__(kThreads) k_i8_empty(T* out, uint64_t ld, uint
 // k is dealt to the instructions' places as it arrives: lane t of a group of four loads 16 consecutive codes of its rows and
 // tokens and feeds them as two instructions' worth.  The warps' sums meet in shared memory.
 //
-// Short inputs of up to 8 tokens are quantised within, by every CTA for itself, under the first loads of W (x stays in L2): a
-// decode step is then one launch.  Above kFewCodes codes of W a launch of TMA-fed tiles is faster than this one.
-constexpr uint32_t kFewFusedEntries = 16384;   // entries of x up to which it is quantised within
+// Short inputs are quantised within, by every CTA for itself, under the first loads of W (x stays in L2): a decode step is then
+// one launch, which spares the host more than it costs the device (16 tokens through 4096 x 4096: 9 us a call against 15).
+// Above kFewCodes codes of W a launch of TMA-fed tiles is faster than this one.
+constexpr uint32_t kFewFusedEntries = 16384, kFewFusedMost = 36864;   // entries of x up to which it is quantised within: by any
+                                                                      // number of CTAs, by as many as run at once
 constexpr uint32_t kFewMost = 16;              // tokens
 constexpr uint64_t kFewCodes = 48u << 20;
+constexpr size_t kFewSmem = 72 * 1024;         // codes of x in shared memory: 16 tokens in pitches of up to 64 bytes more than K
 
 struct FewParams {
   const void* x;          // tokens: values of type T, or codes
@@ -566,8 +634,8 @@ __global__ void __launch_bounds__(256, 2) k_i8_few(const FewParams p) {
   constexpr int kAhead = 4;
   extern __shared__ __align__(16) uint8_t xs[];     // the codes of tokens that are quantised here
   __shared__ int part[8][RB * 16][NT * 8 + 1];
-  __shared__ uint32_t tops[8];
-  __shared__ float scale[NT * 8], inverse[8];
+  __shared__ uint32_t tops[NT][8];
+  __shared__ float scale[NT * 8], inverse[NT * 8];
   pdl_prologue();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t row0 = blockIdx.x * (16 * RB);
@@ -597,40 +665,45 @@ __global__ void __launch_bounds__(256, 2) k_i8_few(const FewParams p) {
   for (int a = 0; a < kAhead; ++a) fetch(first + a, w[a], xc[a]);
 
   if constexpr (!kCodes) {
-    // scales: 8 / 2^ceil(log2 m) warps to a token
+    // scales: 8 / 2^ceil(log2 m) warps to a token, at least one
     const int shift = p.m <= 1 ? 3 : p.m <= 2 ? 2 : p.m <= 4 ? 1 : 0;
-    const uint32_t token = warp >> shift, share = warp & ((1 << shift) - 1), lanes = 32u << shift;
-    uint32_t top = 0;
-    if (token < p.m) {
-      const X* row = static_cast<const X*>(p.x) + token * p.ldx;
-      const uint32_t at = share * 32 + lane;
-      constexpr int N = Vec<X>::kN;
-      const uint32_t nv = p.vec ? p.k / N : 0;
-#pragma unroll 4
-      for (uint32_t v = at; v < nv; v += lanes) {
-        Vec<X> r;
-        r.raw = __ldg(reinterpret_cast<const uint4*>(row) + v);
+    const uint32_t share = warp & ((1 << shift) - 1), lanes = 32u << shift;
 #pragma unroll
-        for (int i = 0; i < N; ++i) top = max(top, mag_bits(r.at(i)));
-      }
+    for (int j = 0; j < NT; ++j) {
+      const uint32_t token = 8 * j + (warp >> shift);
+      uint32_t top = 0;
+      if (token < p.m) {
+        const X* row = static_cast<const X*>(p.x) + token * p.ldx;
+        const uint32_t at = share * 32 + lane;
+        constexpr int N = Vec<X>::kN;
+        const uint32_t nv = p.vec ? p.k / N : 0;
+#pragma unroll 4
+        for (uint32_t v = at; v < nv; v += lanes) {
+          Vec<X> r;
+          r.raw = __ldg(reinterpret_cast<const uint4*>(row) + v);
+#pragma unroll
+          for (int i = 0; i < N; ++i) top = max(top, mag_bits(r.at(i)));
+        }
 #pragma unroll 1
-      for (uint32_t k = nv * N + at; k < p.k; k += lanes) top = max(top, mag_bits(to_f32(row[k])));
+        for (uint32_t k = nv * N + at; k < p.k; k += lanes) top = max(top, mag_bits(to_f32(row[k])));
+      }
+      top = __reduce_max_sync(0xFFFFFFFFu, top);
+      if (lane == 0) tops[j][warp] = top;
     }
-    top = __reduce_max_sync(0xFFFFFFFFu, top);
-    if (lane == 0) tops[warp] = top;
     __syncthreads();
-    if (threadIdx.x < 8) {
-      const uint32_t tok = threadIdx.x;
+    if (threadIdx.x < 8 * NT) {
+      const uint32_t tok = threadIdx.x % 8, j = threadIdx.x / 8;
       uint32_t m = 0;
       for (uint32_t i = 0; i < (1u << shift); ++i)
-        if ((tok << shift) + i < 8) m = max(m, tops[(tok << shift) + i]);
+        if ((tok << shift) + i < 8) m = max(m, tops[j][(tok << shift) + i]);
       float s, v;
       scale_of(m, s, v);
-      scale[tok] = s;
-      inverse[tok] = v;
+      scale[threadIdx.x] = s;
+      inverse[threadIdx.x] = v;
     }
     __syncthreads();
     const uint32_t pieces = (p.k + 15) / 16;
+#pragma unroll 4
     for (uint32_t i = threadIdx.x; i < p.m * pieces; i += 256) {
       const uint32_t tok = i / pieces, k0 = (i - tok * pieces) * 16;
       *reinterpret_cast<uint4*>(xs + tok * pitch + k0) =
@@ -708,18 +781,28 @@ template <class X, class O, int NT>
 cudaError_t launch_few(const FewParams& p, cudaStream_t st) {
   // 32 rows a CTA halve what the tokens' codes cost; where that leaves SMs without a CTA, 16
   const size_t smem = sizeof(X) > 1 ? (size_t)p.m * few_pitch(p.k) : 0;
-  if ((p.n + 31) / 32 >= 2 * (uint32_t)sm_count())
-    launch_pdl_dyn(k_i8_few<X, O, NT, 2>, dim3((p.n + 31) / 32), dim3(256), smem, st, p);
-  else
-    launch_pdl_dyn(k_i8_few<X, O, NT, 1>, dim3((p.n + 15) / 16), dim3(256), smem, st, p);
-  count_launches(1);
-  return cudaGetLastError();
+  auto go = [&](auto kernel, uint32_t rows) {
+    launch_pdl_dyn(kernel, dim3((p.n + rows - 1) / rows), dim3(256), smem, st, p);
+    count_launches(1);
+    return cudaGetLastError();
+  };
+  if ((p.n + 31) / 32 >= 2 * (uint32_t)sm_count()) {
+    if (smem) allow_smem_for<k_i8_few<X, O, NT, 2>>(kFewSmem);
+    return go(k_i8_few<X, O, NT, 2>, 32);
+  }
+  if (smem) allow_smem_for<k_i8_few<X, O, NT, 1>>(kFewSmem);
+  return go(k_i8_few<X, O, NT, 1>, 16);
 }
-template <class X>
+template <class X, int NT>
 cudaError_t launch_few_fused(const FewParams& p, int out_dtype, cudaStream_t st) {
-  return out_dtype == DS_F32 ? launch_few<X, float, 1>(p, st) : out_dtype == DS_BF16 ? launch_few<X, __nv_bfloat16, 1>(p, st) : launch_few<X, __half, 1>(p, st);
+  return out_dtype == DS_F32    ? launch_few<X, float, NT>(p, st)
+         : out_dtype == DS_BF16 ? launch_few<X, __nv_bfloat16, NT>(p, st)
+                                : launch_few<X, __half, NT>(p, st);
 }
-inline bool few_fused(uint64_t rows, uint64_t n, uint64_t k) { return rows <= 8 && rows * k <= kFewFusedEntries && n * k <= kFewCodes; }
+inline bool few_fused(uint64_t rows, uint64_t n, uint64_t k) {
+  if (rows > kFewMost || n * k > kFewCodes) return false;
+  return rows * k <= kFewFusedEntries || (rows * k <= kFewFusedMost && (n + 15) / 16 <= 2 * (uint64_t)sm_count());
+}
 
 inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 inline bool aligned(const void* p, uint64_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -817,11 +900,11 @@ cudaError_t quantize(const T* x, uint32_t rows, uint32_t cols, uint64_t ld, int8
     vec ? amax(k_i8_amax<T, true, true>) : amax(k_i8_amax<T, false, true>);
   else
     vec ? amax(k_i8_amax<T, true, false>) : amax(k_i8_amax<T, false, false>);
-  auto codes = [&](auto kernel) {
-    launch_pdl(kernel, g2, dim3(256), st, x, ld, rows, cols, (const uint32_t*)rt, (const uint32_t*)ct, (const float*)sums, q, ldq, scale, qt, ldqt,
+  auto codes = [&](auto kernel, dim3 grid) {
+    launch_pdl(kernel, grid, dim3(256), st, x, ld, rows, cols, (const uint32_t*)rt, (const uint32_t*)ct, (const float*)sums, q, ldq, scale, qt, ldqt,
                scale_t, col_sum);
   };
-  vec ? codes(k_i8_codes<T, true>) : codes(k_i8_codes<T, false>);
+  vec ? codes(k_i8_codes<T>, g2) : codes(k_i8_codes_odd<T>, dim3((cols + 63) / 64, (rows + 63) / 64));
   count_launches(2);
   return cudaGetLastError();
 }
@@ -913,9 +996,13 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
     const FewParams p{x, ldx, nullptr, w, ldw, sw, bias, out, ldo, (uint32_t)rows, (uint32_t)n, (uint32_t)k,
                       aligned(x, 16) && ldx * size_of(dtype) % 16 == 0};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const cudaError_t e = dtype == DS_F32    ? launch_few_fused<float>(p, out_dtype, st)
-                          : dtype == DS_BF16 ? launch_few_fused<__nv_bfloat16>(p, out_dtype, st)
-                                             : launch_few_fused<__half>(p, out_dtype, st);
+    auto go = [&](auto tokens) {
+      constexpr int kGroups = decltype(tokens)::value;
+      return dtype == DS_F32    ? launch_few_fused<float, kGroups>(p, out_dtype, st)
+             : dtype == DS_BF16 ? launch_few_fused<__nv_bfloat16, kGroups>(p, out_dtype, st)
+                                : launch_few_fused<__half, kGroups>(p, out_dtype, st);
+    };
+    const cudaError_t e = rows <= 8 ? go(std::integral_constant<int, 1>()) : go(std::integral_constant<int, 2>());
     return e == cudaSuccess ? DS_OK : cuda_fail(e, "8-bit product");
   }
   if (!workspace) return DS_ERR_INVALID_ARG;
