@@ -36,13 +36,13 @@ __device__ __forceinline__ void scale_of(uint32_t amax_bits, float& s, float& in
 // round(v * inv) in the low byte: adding 1.5 * 2^23 rounds to the nearest whole number, ties to even, and leaves it in the low
 // bits (conversions run at a fraction of the rate of additions).  Of a line with inv = 0 the codes are masked: v may be inf or NaN.
 __device__ __forceinline__ uint32_t code_of(float v, float inv) { return __float_as_uint(__fadd_rn(__fmul_rn(v, inv), 12582912.f)); }
-__device__ __forceinline__ uint32_t mask_of(float inv) { return inv != 0.f ? 0xFFFFFFFFu : 0u; }
 __device__ __forceinline__ uint32_t mag_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
-  return pack4(code_of(a, inv), code_of(b, inv), code_of(c, inv), code_of(d, inv)) & mask_of(inv);
+  const uint32_t w = pack4(code_of(a, inv), code_of(b, inv), code_of(c, inv), code_of(d, inv));
+  return inv != 0.f ? w : 0u;
 }
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
@@ -139,21 +139,6 @@ __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32
   float sum[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) top[i] = 0, sum[i] = 0.f;
-  auto take = [&](const Vec<T>& v, uint32_t r) {
-    uint32_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float f = v.at(i);
-      const uint32_t b = mag_bits(f);
-      mine = max(mine, b);
-      top[i] = max(top[i], b);
-      if constexpr (SUMS) sum[i] += f;
-    }
-    if (row_top) {
-      mine = __reduce_max_sync(0xFFFFFFFFu, mine);
-      if (lane == 0 && r < rows && mine) atomicMax(row_top + r, mine);
-    }
-  };
   Vec<T> v[kRows];
   if (VEC && c0 + 32 * N <= cols && r0 + kAmaxRows <= rows) {   // inside
 #pragma unroll
@@ -168,8 +153,22 @@ __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32
         if (r < rows && col(i) < cols) v[k].set(i, x[(uint64_t)r * ld + col(i)]);
     }
   }
+  uint32_t row_max = 0;      // of row k in lane k: one atomic instruction for the warp's eight rows
 #pragma unroll
-  for (int k = 0; k < kRows; ++k) take(v[k], r0 + warp + 8 * k);
+  for (int k = 0; k < kRows; ++k) {
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float f = v[k].at(i);
+      const uint32_t b = mag_bits(f);
+      mine = max(mine, b);
+      top[i] = max(top[i], b);
+      if constexpr (SUMS) sum[i] += f;
+    }
+    mine = __reduce_max_sync(0xFFFFFFFFu, mine);
+    if (lane == k) row_max = mine;
+  }
+  if (row_top && row_max && r0 + warp + 8 * lane < rows) atomicMax(row_top + r0 + warp + 8 * lane, row_max);
   __shared__ uint32_t tops[8][32 * N];
   __shared__ float part[SUMS ? 8 : 1][SUMS ? 32 * N : 1];
 #pragma unroll
@@ -204,7 +203,8 @@ __global__ void __launch_bounds__(256)
   pdl_prologue();
   constexpr int N = Vec<T>::kN, V = 8 / N;     // vectors of 16 bytes in 8 columns
   __shared__ float rinv[128], cinv[128];
-  __shared__ uint32_t turned[128][33];
+  // a column's 32 words in pieces of 16 bytes, exchanged by the column's number: writes of a warp meet two to a bank, reads none
+  __shared__ __align__(16) uint32_t turned[128][32];
   const uint32_t r0 = blockIdx.y * 128, c0 = blockIdx.x * 128, tid = threadIdx.x;
   const bool inside = r0 + 128 <= rows && c0 + 128 <= cols;
   const uint32_t lc = tid % 16 * 8, c = c0 + lc;
@@ -267,15 +267,17 @@ __global__ void __launch_bounds__(256)
     }
     if (qt) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) turned[lc + j][lr / 4] = codes4(at(0, j), at(1, j), at(2, j), at(3, j), cinv[lc + j]);
+      for (int j = 0; j < 8; ++j) turned[lc + j][((lr / 16) ^ ((lc + j) / 8 & 7)) * 4 + lr / 4 % 4] = codes4(at(0, j), at(1, j), at(2, j), at(3, j), cinv[lc + j]);
     }
   }
   if (!qt) return;
   __syncthreads();
-#pragma unroll 4
-  for (int k = 0; k < 16; ++k) {
-    const uint32_t l = tid / 32 + 8 * k, w = tid % 32;
-    if (c0 + l < cols && r0 + 4 * w < ldqt) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t l = tid / 8 + 32 * k, piece = tid % 8;
+    if (c0 + l < cols && r0 + 16 * piece < ldqt)
+      *reinterpret_cast<uint4*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 16 * piece) =
+          *reinterpret_cast<const uint4*>(&turned[l][(piece ^ (l / 8 & 7)) * 4]);
   }
 }
 
@@ -616,7 +618,7 @@ __device__ __forceinline__ uint4 encode16(const T* row, uint32_t k0, uint32_t k,
   for (int h = 0; h < 2; ++h)
 #pragma unroll 1
     for (uint32_t i = k0 + 8 * h; i < k && i < k0 + 8 * h + 8; ++i)
-      v[h] |= (unsigned long long)(code_of(to_f32(row[i]), inv) & mask_of(inv) & 0xFFu) << (8 * (i & 7));
+      v[h] |= (unsigned long long)(inv != 0.f ? code_of(to_f32(row[i]), inv) & 0xFFu : 0u) << (8 * (i & 7));
   return make_uint4((uint32_t)v[0], (uint32_t)(v[0] >> 32), (uint32_t)v[1], (uint32_t)(v[1] >> 32));
 }
 
@@ -880,10 +882,10 @@ cudaError_t quantize(const T* x, uint32_t rows, uint32_t cols, uint64_t ld, int8
     count_launches(1);
     return cudaGetLastError();
   }
-  // One launch where a CTA's reading stays under 400 KB and all CTAs' under 64 MB (1024 x 1024 in bf16, at both limits: 11 us
-  // either way on the device, and two launches less for the host); rows of whole vectors only.
+  // One launch where a CTA's reading stays under 200 KB and all CTAs' under 64 MB (512 x 768 in bf16, 164 KB: 7.5 us; 768 x 768
+  // floats, 393 KB, would be 10 against 8); rows of whole vectors only.
   const uint64_t reads = ((uint64_t)rows + cols) * 64 * sizeof(T), ctas = (uint64_t)((rows + 63) / 64) * ((cols + 63) / 64);
-  if (vec && cols % Vec<T>::kN == 0 && reads <= 400 * 1024 && reads * ctas <= (64u << 20)) {
+  if (vec && cols % Vec<T>::kN == 0 && reads <= 200 * 1024 && reads * ctas <= (64u << 20)) {
     launch_pdl(k_i8_small<T>, dim3((cols + 63) / 64, (rows + 63) / 64), dim3(512), st, x, ld, rows, cols, q, ldq, scale, qt, ldqt, scale_t, col_sum);
     count_launches(1);
     return cudaGetLastError();
