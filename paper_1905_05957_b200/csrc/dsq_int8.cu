@@ -836,7 +836,7 @@ cudaError_t product(const int8_t* a, uint64_t lda, const float* sa, const int8_t
   // with rows that are not there; and where rows of out are on no boundary, since lanes then hold consecutive entries.
   const bool vec = aligned(out, 32) && ldo * sizeof(T) % 32 == 0 && aligned(sb, 16) && (!bias || aligned(bias, 16));
   if (m <= kTurnedMost || !vec) {
-    const MmaShape s{n, m, k, 1, 1, 0, dev_status};
+    const MmaShape s{n, m, k, 1, 1, 0, 0, dev_status};
     const EpiScaleTurned<T> epi{sa, sb, bias, out, ldo, n, m};
     const bool narrow = m <= 32;
     MmaPlan plan = plan_mma(s);
@@ -850,18 +850,18 @@ cudaError_t product(const int8_t* a, uint64_t lda, const float* sa, const int8_t
     cudaError_t e = make_tensor_map(&mw, kMmaI8, b, k, n, 1, ldb, ldb * n, 128, kMmaRows);
     if (e == cudaSuccess) e = make_tensor_map(&mx, kMmaI8, a, k, m, 1, lda, lda * m, 128, plan.box_rows());
     if (e != cudaSuccess) return e;
-    if (!narrow) return launch_mma<kMmaI8, false>(plan, mw, mx, s, epi, st);
-    return plan.parts > 1 ? launch_mma_split<kMmaI8, 32, false>(plan.parts, mw, mx, s, epi, st)
-                          : launch_mma_bn<kMmaI8, 32, false>(mw, mx, s, epi, st);
+    if (!narrow) return launch_mma<kMmaI8, kAlong, kAlong>(plan, mw, mx, s, epi, st);
+    return plan.parts > 1 ? launch_mma_split<kMmaI8, 32, kAlong, kAlong>(plan.parts, mw, mx, s, epi, st)
+                          : launch_mma_bn<kMmaI8, 32, kAlong, kAlong>(mw, mx, s, epi, st);
   }
-  const MmaShape s{m, n, k, 1, 1, 0, dev_status};
+  const MmaShape s{m, n, k, 1, 1, 0, 0, dev_status};
   const EpiScale<T> epi{sa, sb, bias, out, ldo, m, n};
   const MmaPlan plan = plan_mma(s);
   CUtensorMap ma, mb;
   cudaError_t e = make_tensor_map(&ma, kMmaI8, a, k, m, 1, lda, lda * m, 128, kMmaRows);
   if (e == cudaSuccess) e = make_tensor_map(&mb, kMmaI8, b, k, n, 1, ldb, ldb * n, 128, plan.box_rows());
   if (e != cudaSuccess) return e;
-  return launch_mma<kMmaI8, false>(plan, ma, mb, s, epi, st);
+  return launch_mma<kMmaI8, kAlong, kAlong>(plan, ma, mb, s, epi, st);
 }
 
 template <class T>

@@ -1,6 +1,6 @@
 // Matrix products on the fifth-generation tensor cores (tcgen05), shared by the orthogonalised update (16-bit
 // floating operands) and the 8-bit layer products: C = A B^T with A [M, K] and B [N, K], both laid out along K, or B
-// given as [K, N] (16-bit only).
+// given as [K, N] (16-bit only), or a symmetric operand of which half is there.
 //
 // One CTA per SM walks over 128 x BN tiles of C.  Warp 0 fetches operand tiles by TMA into a ring of stages (rows of 128
 // bytes, 128-byte swizzle), one thread of warp 1 issues the matrix instructions, and warps 4..11 read the finished
@@ -150,22 +150,48 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint
   return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)((lead >> 4) & 0x3FFFu) << 16) | ((uint64_t)((stride >> 4) & 0x3FFFu) << 32) |
          (1ull << 46) | (2ull << 61);
 }
-// Instruction descriptor: f16 x f16 -> f32, or s8 x s8 -> s32; M = 128.
-template <int KIND, int BN, bool B_ACROSS>
-__host__ __device__ constexpr uint32_t mma_idesc() {
-  const uint32_t types = KIND == kMmaF16 ? (1u << 4) : ((2u << 4) | (1u << 7) | (1u << 10));
-  return types | (B_ACROSS ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kMmaRows >> 4) << 24);
+// Instruction descriptor: f16 x f16 -> f32, or s8 x s8 -> s32; `rows` x `cols` of C; whether the operands lie across K.
+template <int KIND>
+__device__ __forceinline__ uint32_t mma_idesc(uint32_t rows, uint32_t cols, bool a_across, bool b_across) {
+  constexpr uint32_t types = KIND == kMmaF16 ? (1u << 4) : ((2u << 4) | (1u << 7) | (1u << 10));
+  return types | (a_across ? 1u << 15 : 0u) | (b_across ? 1u << 16 : 0u) | (cols >> 3 << 17) | (rows >> 4 << 24);
+}
+// The descriptor of instruction q (of four) of a step of 128 bytes of K.
+__device__ __forceinline__ uint64_t step_desc(uint32_t tile, int q, bool across) {
+  return across ? smem_desc(tile + 2048 * q, 64 * 128, 1024) : smem_desc(tile + 32 * q, 16, 1024);
 }
 
 // ---- the product ----------------------------------------------------------------------------------------
+
+// How an operand lies in memory.  kSym: a symmetric matrix of which blocks of 128 x 128 or 256 x 256 on and above the diagonal are
+// there (the diagonal ones whole): a piece below the diagonal is fetched from its mirror image and laid across K.  A tile's rows
+// of such an operand lie within one block: blocks are 256 wide where pairs or tiles of 256 columns read them, else 128, which
+// leaves less to compute below the diagonal.  (Writing the mirror images out instead cost 16 of 216 us of an update of twelve
+// 768 x 768.)
+enum MmaOperand : int { kAlong = 0, kAcross = 1, kSym = 2 };
 
 struct MmaShape {
   uint32_t m, n, k;        // C is [m, n] per matrix of the batch
   uint32_t batch;
   uint32_t elem;           // bytes of an operand's element
-  uint32_t sym;            // 1: C is symmetric; only 32 x 32 blocks on or above the diagonal are handed to the epilogue
+  uint32_t sym;            // 7 or 8: C is symmetric; only its blocks of 2^sym on or above the diagonal go to the epilogue (0: all)
+  uint32_t half;           // 7 or 8: blocks of 2^half of the kSym operands are there
   uint32_t* dev_status;
 };
+
+// Fetches a step of an operand: ROWS rows by 128 bytes of K, or their mirror image, 64 columns at a time.
+__device__ __forceinline__ bool mirrored(const MmaShape& s, uint32_t k, uint32_t row) { return k >> s.half < row >> s.half; }
+template <int MODE, int ROWS>
+__device__ __forceinline__ void load_operand(const MmaShape& s, uint32_t dst, const CUtensorMap* map, uint32_t k, uint32_t row, uint32_t b, uint32_t bar) {
+  if constexpr (MODE == kAlong) {
+    tma_load_3d(dst, map, (int)k, (int)row, (int)b, bar);
+  } else {
+    const bool across = MODE == kAcross || mirrored(s, k, row);
+#pragma unroll
+    for (int c = 0; c < ROWS; c += 64)
+      tma_load_3d(dst + c * 128, map, (int)(across ? row + c : k), (int)(across ? k : row + c), (int)b, bar);
+  }
+}
 
 // Epilogues.  A warp hands over blocks of 32 x 32 of C, a row to a lane:
 //   struct Pre;  Pre load(row, col0, batch) const;   what it reads from global memory for its row (row may be out of range)
@@ -327,21 +353,23 @@ struct TileWalk {
     nt = (s.n + bn - 1) / bn;
     if (sym) {
       per = 0;
-      for (uint32_t i = 0; i < mt; ++i) per += nt - i * kMmaRows / bn;
+      for (uint32_t i = 0; i < mt; ++i) per += nt - first(i);
     } else {
       per = mt * nt;
     }
     total = per * s.batch;
   }
+  // the first tile of tile row i that is wanted
+  __host__ __device__ uint32_t first(uint32_t i) const { return (i * kMmaRows >> sym << sym) / bn; }
   __host__ __device__ void at(uint32_t t, uint32_t& b, uint32_t& i, uint32_t& j) const {
     b = t / per;
     t -= b * per;
     if (sym) {
       i = 0;
       while (true) {
-        const uint32_t first = i * kMmaRows / bn, c = nt - first;
+        const uint32_t f = first(i), c = nt - f;
         if (t < c) {
-          j = first + t;
+          j = f + t;
           return;
         }
         t -= c;
@@ -356,7 +384,7 @@ struct TileWalk {
   }
 };
 
-template <int KIND, int BN, bool B_ACROSS, class Epi>
+template <int KIND, int BN, int A_MODE, int B_MODE, class Epi>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     k_mma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const __grid_constant__ Epi epi) {
   using T = MmaTile<BN, Epi>;
@@ -413,14 +441,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         const uint32_t dst = ring + stage * T::kStageBytes;
         if (one) {
           mbar_expect_tx(full + 8 * stage, T::kStageBytes);
-          tma_load_3d(dst, &map_a, (int)(kb * kBK), (int)(i * kMmaRows), (int)b, full + 8 * stage);
-          if constexpr (B_ACROSS) {
-#pragma unroll
-            for (int c = 0; c < BN / 64; ++c)
-              tma_load_3d(dst + kMmaRows * 128 + c * (kBK * 128), &map_b, (int)(j * BN + c * 64), (int)(kb * kBK), (int)b, full + 8 * stage);
-          } else {
-            tma_load_3d(dst + kMmaRows * 128, &map_b, (int)(kb * kBK), (int)(j * BN), (int)b, full + 8 * stage);
-          }
+          load_operand<A_MODE, kMmaRows>(shape, dst, &map_a, kb * kBK, i * kMmaRows, b, full + 8 * stage);
+          load_operand<B_MODE, BN>(shape, dst + kMmaRows * 128, &map_b, kb * kBK, j * BN, b, full + 8 * stage);
         }
         __syncwarp();
         ++issued;
@@ -442,10 +464,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     }
   } else if (warp == 1) {
     const bool one = elect_one();
-    constexpr uint32_t idesc = mma_idesc<KIND, BN, B_ACROSS>();
     uint32_t stage = 0, phase = 0, at = 0, aphase = 0;
     bool ok = true;
     for (uint32_t t = blockIdx.x; ok && t < walk.total; t += gridDim.x) {
+      uint32_t b = 0, i = 0, j = 0;
+      if constexpr (A_MODE == kSym || B_MODE == kSym) walk.at(t, b, i, j);
       if (!(ok = mbar_wait(tempty + 8 * at, aphase ^ 1, &gave_up))) break;
       tc_fence_after();
       const uint32_t d = tmem + at * BN;
@@ -454,12 +477,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tc_fence_after();
         if (one) {
           const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128;
+          const bool ta = A_MODE == kSym && mirrored(shape, kb * kBK, i * kMmaRows), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, kb * kBK, j * BN));
+          const uint32_t idesc = mma_idesc<KIND>(kMmaRows, BN, ta, tb);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {   // four instructions of 32 bytes of K
-            const uint64_t da = smem_desc(sa + 32 * q, 16, 1024);
-            const uint64_t db = B_ACROSS ? smem_desc(sb + 2048 * q, kBK * 128, 1024) : smem_desc(sb + 32 * q, 16, 1024);
-            tc_mma<KIND>(d, da, db, idesc, (kb | q) != 0);
-          }
+          for (int q = 0; q < 4; ++q)   // four instructions of 32 bytes of K
+            tc_mma<KIND>(d, step_desc(sa, q, ta), step_desc(sb, q, tb), idesc, (kb | q) != 0);
           tc_commit(empty + 8 * stage);
         }
         __syncwarp();
@@ -493,7 +515,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       const uint32_t row0 = i * kMmaRows + quarter * 32, col = j * BN;
       auto wanted = [&](int c) {
         const uint32_t col0 = col + 32 * c;
-        return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >= row0);
+        return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >> shape.sym >= row0 >> shape.sym);
       };
       if (!ew.tile(epi, (int)group, BN / 32, row0, col, b, tmem + at * BN + (quarter << 21), nk == 0, wanted,
                    [&] { return mbar_wait(tfull + 8 * at, aphase, &gave_up); }))
@@ -613,7 +635,7 @@ __device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t a_desc, ui
         : "memory");
 }
 
-template <int KIND, bool B_ACROSS, class Epi>
+template <int KIND, int A_MODE, int B_MODE, class Epi>
 __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
     k_mma_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const __grid_constant__ Epi epi) {
   constexpr int kPairStages = PairTile<Epi>::kStages;
@@ -677,14 +699,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
         const uint32_t dst = ring + stage * kPairStageBytes, bar = in_cta(full + 8 * stage, 0);
         if (one) {
           if (rank == 0) mbar_expect_tx(full + 8 * stage, 2 * (kMmaRows + mine) * 128);
-          tma_load_3d_pair(dst, &map_a, (int)(kb * kBK), (int)(row + rank * kMmaRows), (int)b, bar);
-          for (uint32_t c = 0; c < mine; c += 64) {
-            const uint32_t to = dst + kMmaRows * 128 + c * 128, n0 = col + rank * mine + c;
-            if constexpr (B_ACROSS)
-              tma_load_3d_pair(to, &map_b, (int)n0, (int)(kb * kBK), (int)b, bar);
-            else
-              tma_load_3d_pair(to, &map_b, (int)(kb * kBK), (int)n0, (int)b, bar);
+          const uint32_t k0 = kb * kBK, r0 = row + rank * kMmaRows, n0 = col + rank * mine;
+          if constexpr (A_MODE == kAlong) {
+            tma_load_3d_pair(dst, &map_a, (int)k0, (int)r0, (int)b, bar);
+          } else {
+            const bool across = mirrored(shape, k0, row);
+#pragma unroll
+            for (uint32_t c = 0; c < kMmaRows; c += 64)
+              tma_load_3d_pair(dst + c * 128, &map_a, (int)(across ? r0 + c : k0), (int)(across ? k0 : r0 + c), (int)b, bar);
           }
+          const bool across = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, col));
+          for (uint32_t c = 0; c < mine; c += 64)
+            tma_load_3d_pair(dst + (kMmaRows + c) * 128, &map_b, (int)(across ? n0 + c : k0), (int)(across ? k0 : n0 + c), (int)b, bar);
         }
         __syncwarp();
         ++issued;
@@ -706,15 +732,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
     }
   } else if (warp == 1 && rank == 0) {
     const bool one = elect_one();
-    constexpr uint32_t types = (KIND == kMmaF16 ? (1u << 4) : ((2u << 4) | (1u << 7) | (1u << 10))) | (B_ACROSS ? 1u << 16 : 0u) |
-                               ((uint32_t)(2 * kMmaRows >> 4) << 24);
     uint32_t stage = 0, phase = 0, at = 0, aphase = 0;
     bool ok = true;
     for (uint32_t t = pair; ok && t < walk.items; t += pairs) {
       uint32_t b, row, col, width;
       walk.at(t, b, row, col, width);
       if (skip(row, col, width)) continue;
-      const uint32_t idesc = types | (width >> 3 << 17);
       if (!(ok = mbar_wait(tempty + 8 * at, aphase ^ 1, &gave_up))) break;
       tc_fence_after();
       const uint32_t d = tmem + at * 256;
@@ -723,12 +746,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
         tc_fence_after();
         if (one) {
           const uint32_t sa = ring + stage * kPairStageBytes, sb = sa + kMmaRows * 128;
+          const bool ta = A_MODE == kSym && mirrored(shape, kb * kBK, row), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, kb * kBK, col));
+          const uint32_t idesc = mma_idesc<KIND>(2 * kMmaRows, width, ta, tb);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const uint64_t da = smem_desc(sa + 32 * q, 16, 1024);
-            const uint64_t db = B_ACROSS ? smem_desc(sb + 2048 * q, kBK * 128, 1024) : smem_desc(sb + 32 * q, 16, 1024);
-            tc_mma_pair<KIND>(d, da, db, idesc, (kb | q) != 0);
-          }
+          for (int q = 0; q < 4; ++q) tc_mma_pair<KIND>(d, step_desc(sa, q, ta), step_desc(sb, q, tb), idesc, (kb | q) != 0);
           tc_commit_pair(empty + 8 * stage);
         }
         __syncwarp();
@@ -762,7 +783,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
       const uint32_t row0 = row_t + rank * kMmaRows + quarter * 32;
       auto wanted = [&](int c) {
         const uint32_t col0 = col + 32 * c;
-        return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >= row0);
+        return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >> shape.sym >= row0 >> shape.sym);
       };
       if (!ew.tile(epi, (int)group, (int)(width >> 5), row0, col, b, tmem + at * 256 + (quarter << 21), false, wanted,
                    [&] { return mbar_wait(tfull + 8 * at, aphase, &gave_up); }))
@@ -790,7 +811,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
 // sums of it into the owner's shared memory (the ring, which is idle by then), and the owner adds them in the order of the
 // CTAs' ranks, so that results do not depend on timing.  512 x 512 x 4608 by single CTAs: 15.5 us of which 12 are the 72 steps
 // of K in a row; on a third of the SMs.
-template <int KIND, int BN, bool B_ACROSS, class Epi>
+template <int KIND, int BN, int A_MODE, int B_MODE, class Epi>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     k_mma_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const __grid_constant__ Epi epi,
                 const uint32_t parts) {
@@ -840,7 +861,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t row0 = ti * kMmaRows + quarter * 32, c_first = tj * BN;
   auto wanted = [&](int c) {
     const uint32_t col0 = c_first + 32 * c;
-    return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >= row0);
+    return row0 < shape.m && col0 < shape.n && (!shape.sym || col0 >> shape.sym >= row0 >> shape.sym);
   };
   auto owner = [&](int c) { return (uint32_t)(c * 4 + quarter) % parts; };
   // where in an owner's ring the sums of block (c, quarter) from CTA r lie: 4 KB
@@ -855,14 +876,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       const uint32_t dst = ring + stage * T::kStageBytes;
       if (one) {
         mbar_expect_tx(full + 8 * stage, T::kStageBytes);
-        tma_load_3d(dst, &map_a, (int)(kb * kBK), (int)(ti * kMmaRows), (int)b, full + 8 * stage);
-        if constexpr (B_ACROSS) {
-#pragma unroll
-          for (int c = 0; c < BN / 64; ++c)
-            tma_load_3d(dst + kMmaRows * 128 + c * (kBK * 128), &map_b, (int)(c_first + c * 64), (int)(kb * kBK), (int)b, full + 8 * stage);
-        } else {
-          tma_load_3d(dst + kMmaRows * 128, &map_b, (int)(kb * kBK), (int)c_first, (int)b, full + 8 * stage);
-        }
+        load_operand<A_MODE, kMmaRows>(shape, dst, &map_a, kb * kBK, ti * kMmaRows, b, full + 8 * stage);
+        load_operand<B_MODE, BN>(shape, dst + kMmaRows * 128, &map_b, kb * kBK, c_first, b, full + 8 * stage);
       }
       __syncwarp();
       ++issued;
@@ -883,19 +898,16 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     }
   } else if (warp == 1) {
     const bool one = elect_one();
-    constexpr uint32_t idesc = mma_idesc<KIND, BN, B_ACROSS>();
     uint32_t stage = 0, phase = 0;
     for (uint32_t kb = 0; kb < nk; ++kb) {
       if (!mbar_wait(full + 8 * stage, phase, &gave_up)) break;
       tc_fence_after();
       if (one) {
-        const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128;
+        const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128, k0 = (k_first + kb) * kBK;
+        const bool ta = A_MODE == kSym && mirrored(shape, k0, ti * kMmaRows), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, c_first));
+        const uint32_t idesc = mma_idesc<KIND>(kMmaRows, BN, ta, tb);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint64_t da = smem_desc(sa + 32 * q, 16, 1024);
-          const uint64_t db = B_ACROSS ? smem_desc(sb + 2048 * q, kBK * 128, 1024) : smem_desc(sb + 32 * q, 16, 1024);
-          tc_mma<KIND>(tmem, da, db, idesc, (kb | q) != 0);
-        }
+        for (int q = 0; q < 4; ++q) tc_mma<KIND>(tmem, step_desc(sa, q, ta), step_desc(sb, q, tb), idesc, (kb | q) != 0);
         tc_commit(empty + 8 * stage);
       }
       __syncwarp();
@@ -1025,11 +1037,12 @@ inline double pair_time(const MmaShape& s, int pairs) {
   if (w.items > w.whole) t += rounds > 0 ? (0.5 * main > epi ? 0.5 * main : epi) - 0.5 * epi : 0.5 * (main + epi);
   return t;
 }
-inline MmaPlan plan_mma(const MmaShape& s) {
+inline MmaPlan plan_mma(const MmaShape& s, bool b_sym = false) {   // b_sym: a tile of a symmetric B lies within one of its blocks
   const int sms = sm_count();
   MmaPlan p{false, 64, 1};
   double least = single_time(s, sms, 64);
   for (int bn : {128, 192, 256}) {
+    if (b_sym && bn == 192) continue;
     const double t = single_time(s, sms, bn);
     if (t < least) least = t, p = MmaPlan{false, bn, 1};
   }
@@ -1054,22 +1067,22 @@ inline void allow_smem_for(size_t bytes) {
     done.fetch_or(bit, std::memory_order_relaxed);
 }
 
-template <int KIND, int BN, bool B_ACROSS, class Epi>
+template <int KIND, int BN, int A_MODE, int B_MODE, class Epi>
 cudaError_t launch_mma_bn(const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
   const TileWalk w(s, BN);
   const uint32_t grid = w.total < (uint32_t)sm_count() ? w.total : (uint32_t)sm_count();
   if (!grid) return cudaSuccess;
-  allow_smem_for<k_mma<KIND, BN, B_ACROSS, Epi>>(MmaTile<BN, Epi>::kSmem);
-  launch_pdl_dyn(k_mma<KIND, BN, B_ACROSS, Epi>, dim3(grid), dim3(kMmaThreads), MmaTile<BN, Epi>::kSmem, st, a, b, s, epi);
+  allow_smem_for<k_mma<KIND, BN, A_MODE, B_MODE, Epi>>(MmaTile<BN, Epi>::kSmem);
+  launch_pdl_dyn(k_mma<KIND, BN, A_MODE, B_MODE, Epi>, dim3(grid), dim3(kMmaThreads), MmaTile<BN, Epi>::kSmem, st, a, b, s, epi);
   count_launches(1);
   return cudaGetLastError();
 }
 
-template <int KIND, int BN, bool B_ACROSS, class Epi>
+template <int KIND, int BN, int A_MODE, int B_MODE, class Epi>
 cudaError_t launch_mma_split(uint32_t parts, const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
   const TileWalk w(s, BN);
   if (!w.total) return cudaSuccess;
-  allow_smem_for<k_mma_split<KIND, BN, B_ACROSS, Epi>>(MmaTile<BN, Epi>::kSmem);
+  allow_smem_for<k_mma_split<KIND, BN, A_MODE, B_MODE, Epi>>(MmaTile<BN, Epi>::kSmem);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(w.total * parts);
   cfg.blockDim = dim3(kMmaThreads);
@@ -1083,30 +1096,34 @@ cudaError_t launch_mma_split(uint32_t parts, const CUtensorMap& a, const CUtenso
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  (void)cudaLaunchKernelEx(&cfg, k_mma_split<KIND, BN, B_ACROSS, Epi>, a, b, s, epi, parts);
+  (void)cudaLaunchKernelEx(&cfg, k_mma_split<KIND, BN, A_MODE, B_MODE, Epi>, a, b, s, epi, parts);
   count_launches(1);
   return cudaGetLastError();
 }
 
-template <int KIND, bool B_ACROSS, class Epi>
+template <int KIND, int A_MODE, int B_MODE, class Epi>
 cudaError_t launch_mma(const MmaPlan& plan, const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
   if (plan.pair) {
     const PairWalk w(s, pair_count());
     const uint32_t pairs = w.items < (uint32_t)pair_count() ? w.items : (uint32_t)pair_count();
     if (!pairs) return cudaSuccess;
-    allow_smem_for<k_mma_pair<KIND, B_ACROSS, Epi>>(PairTile<Epi>::kSmem);
-    launch_pdl_dyn(k_mma_pair<KIND, B_ACROSS, Epi>, dim3(2 * pairs), dim3(kMmaThreads), PairTile<Epi>::kSmem, st, a, b, s, epi);
+    allow_smem_for<k_mma_pair<KIND, A_MODE, B_MODE, Epi>>(PairTile<Epi>::kSmem);
+    launch_pdl_dyn(k_mma_pair<KIND, A_MODE, B_MODE, Epi>, dim3(2 * pairs), dim3(kMmaThreads), PairTile<Epi>::kSmem, st, a, b, s, epi);
     count_launches(1);
     return cudaGetLastError();
   }
   if (plan.parts > 1)
-    return plan.bn == 128 ? launch_mma_split<KIND, 128, B_ACROSS>(plan.parts, a, b, s, epi, st)
-                          : launch_mma_split<KIND, 64, B_ACROSS>(plan.parts, a, b, s, epi, st);
+    return plan.bn == 128 ? launch_mma_split<KIND, 128, A_MODE, B_MODE>(plan.parts, a, b, s, epi, st)
+                          : launch_mma_split<KIND, 64, A_MODE, B_MODE>(plan.parts, a, b, s, epi, st);
   switch (plan.bn) {
-    case 256: return launch_mma_bn<KIND, 256, B_ACROSS>(a, b, s, epi, st);
-    case 192: return launch_mma_bn<KIND, 192, B_ACROSS>(a, b, s, epi, st);
-    case 128: return launch_mma_bn<KIND, 128, B_ACROSS>(a, b, s, epi, st);
-    default: return launch_mma_bn<KIND, 64, B_ACROSS>(a, b, s, epi, st);
+    case 256: return launch_mma_bn<KIND, 256, A_MODE, B_MODE>(a, b, s, epi, st);
+    case 192:
+      if constexpr (B_MODE == kSym)
+        return cudaErrorInvalidValue;
+      else
+        return launch_mma_bn<KIND, 192, A_MODE, B_MODE>(a, b, s, epi, st);
+    case 128: return launch_mma_bn<KIND, 128, A_MODE, B_MODE>(a, b, s, epi, st);
+    default: return launch_mma_bn<KIND, 64, A_MODE, B_MODE>(a, b, s, epi, st);
   }
 }
 

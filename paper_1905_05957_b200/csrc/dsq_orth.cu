@@ -218,22 +218,12 @@ struct Half32 {   // 32 consecutive entries of a row, two to a word
   }
 };
 
-// A symmetric matrix in 16 bits without its diagonal, which is held apart.  A block goes out through shared memory; its mirror
-// image straight: lanes hold consecutive rows, so a column of the block is 64 consecutive bytes of the mirrored row.
+// A symmetric matrix in 16 bits without its diagonal, which is held apart; its blocks on and above the diagonal.
 struct SymOut {
   __half* off;
   float* diag;
   uint32_t m, ld;
   uint64_t stride, diag_stride;
-  __device__ __forceinline__ void put(const Half32& v, uint32_t row, uint32_t col0, uint32_t b, uint32_t block, int lane) const {
-    v.put(block, lane);
-    if (row < m && col0 > row) {
-      uint16_t* to = reinterpret_cast<uint16_t*>(off + b * stride + (uint64_t)col0 * ld + row);
-#pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (col0 + j < m) to[(uint64_t)j * ld] = (uint16_t)(v.w[j / 2] >> (16 * (j & 1)));
-    }
-  }
 };
 
 struct EpiGram {   // A = X X^T
@@ -241,7 +231,6 @@ struct EpiGram {   // A = X X^T
   struct Pre {};
   CUtensorMap a_blocks;
   SymOut a;
-  __device__ __forceinline__ const CUtensorMap* in(int) const { return nullptr; }
   __device__ __forceinline__ const CUtensorMap* out(int) const { return &a_blocks; }
   __device__ __forceinline__ Pre load(uint32_t, uint32_t, uint32_t) const { return {}; }
   __device__ __forceinline__ void apply(const Pre&, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b, uint32_t block, int lane) const {
@@ -255,7 +244,7 @@ struct EpiGram {   // A = X X^T
 #pragma unroll
     for (int j = 0; j < 16; ++j) v.set(j, s[2 * j], s[2 * j + 1]);
     if (row >= col0 && row < col0 + 32 && row < a.m) a.diag[b * a.diag_stride + row] = d * kDown;
-    a.put(v, row, col0, b, block, lane);
+    v.put(block, lane);
   }
 };
 
@@ -294,7 +283,7 @@ struct EpiPoly {   // B = b A + c A A, the accumulator being O O
     }
     if (row >= col0 && row < col0 + 32 && row < a.m)
       b.diag[z * a.diag_stride + row] = fmaf(c1, fmaf(d, kDown * kDown, p.d * p.d), b1 * p.d);
-    b.put(v, row, col0, z, block, lane);
+    v.put(block, lane);
   }
 };
 
@@ -421,7 +410,8 @@ struct ds_orth_ctx {
   uint32_t* dev_status;
   bool mapped;                    // the tensor maps below are made (on the first update: the driver makes them)
   MmaPlan p_gram, p_poly, p_x;
-  CUtensorMap x_rows[2], x_cols_gram[2], x_across[2], a_rows, a_cols, b_rows;
+  uint32_t half_a, half_b;        // A and B: log2 of the blocks of which half is there
+  CUtensorMap x_rows[2], x_cols_gram[2], x_across[2], a_sym, b_sym;
   CUtensorMap hi_blocks[2], lo_blocks[2], a_blocks, b_blocks;
 };
 
@@ -463,9 +453,12 @@ uint64_t orth_plan(ds_orth_ctx* h, uint8_t* ws) {
 
 cudaError_t orth_maps(ds_orth_ctx* h) {
   const uint32_t batch = h->cfg.batch;
-  h->p_gram = plan_mma({h->m, h->m, h->n, batch, 2, 1, nullptr});
-  h->p_poly = plan_mma({h->m, h->m, h->m, batch, 2, 1, nullptr});
-  h->p_x = plan_mma({h->m, h->n, h->m, batch, 2, 0, nullptr});
+  // from the last product to the first: how a product is taken says how much of its symmetric operand has to be there
+  h->p_x = plan_mma({h->m, h->n, h->m, batch, 2, 0, 0, nullptr});
+  h->half_b = h->p_x.pair ? 8 : 7;
+  h->p_poly = plan_mma({h->m, h->m, h->m, batch, 2, h->half_b, 0, nullptr}, true);
+  h->half_a = h->p_poly.pair || h->p_poly.bn > 128 ? 8 : 7;
+  h->p_gram = plan_mma({h->m, h->m, h->n, batch, 2, h->half_a, 0, nullptr});
   cudaError_t e = cudaSuccess;
   auto add = [&](CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t ld, uint64_t stride, uint32_t box_rows) {
     if (e == cudaSuccess) e = make_tensor_map(map, kMmaF16, base, cols, rows, batch, ld, stride, 64, box_rows);
@@ -475,9 +468,8 @@ cudaError_t orth_maps(ds_orth_ctx* h) {
     add(&h->x_cols_gram[i], h->hi[i], h->n, h->m, h->ldx, h->xs, h->p_gram.box_rows());
     add(&h->x_across[i], h->hi[i], h->n, h->m, h->ldx, h->xs, 64);
   }
-  add(&h->a_rows, h->a.off, h->m, h->m, h->ldm, h->ms, kMmaRows);
-  add(&h->a_cols, h->a.off, h->m, h->m, h->ldm, h->ms, h->p_poly.box_rows());
-  add(&h->b_rows, h->b.off, h->m, h->m, h->ldm, h->ms, kMmaRows);
+  add(&h->a_sym, h->a.off, h->m, h->m, h->ldm, h->ms, 64);
+  add(&h->b_sym, h->b.off, h->m, h->m, h->ldm, h->ms, 64);
   auto add_blocks = [&](CUtensorMap* map, const void* base, uint64_t cols, uint64_t ld, uint64_t stride) {
     if (e == cudaSuccess) e = make_tensor_map(map, kMmaF16, base, cols, h->m, batch, ld, stride, 32, 32, true);
   };
@@ -565,13 +557,13 @@ int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum
   cudaError_t e = g_dtype == DS_F32    ? launch_prepare<float>(h, mo, vec, st)
                   : g_dtype == DS_BF16 ? launch_prepare<__nv_bfloat16>(h, mo, vec, st)
                                        : launch_prepare<__half>(h, mo, vec, st);
-  const MmaShape gram{h->m, h->m, h->n, c.batch, 2, 1, h->dev_status}, poly{h->m, h->m, h->m, c.batch, 2, 1, h->dev_status},
-      full{h->m, h->n, h->m, c.batch, 2, 0, h->dev_status};
+  const MmaShape gram{h->m, h->m, h->n, c.batch, 2, h->half_a, 0, h->dev_status}, poly{h->m, h->m, h->m, c.batch, 2, h->half_b, h->half_a, h->dev_status},
+      full{h->m, h->n, h->m, c.batch, 2, 0, h->half_b, h->dev_status};
   int cur = 0;
   for (uint32_t s = 0; s < c.steps && e == cudaSuccess; ++s, cur ^= 1) {
-    e = launch_mma<kMmaF16, false>(h->p_gram, h->x_rows[cur], h->x_cols_gram[cur], gram, EpiGram{h->a_blocks, h->a}, st);
+    e = launch_mma<kMmaF16, kAlong, kAlong>(h->p_gram, h->x_rows[cur], h->x_cols_gram[cur], gram, EpiGram{h->a_blocks, h->a}, st);
     if (e == cudaSuccess)
-      e = launch_mma<kMmaF16, false>(h->p_poly, h->a_rows, h->a_cols, poly, EpiPoly{h->a_blocks, h->b_blocks, h->a, h->b, c.b, c.c}, st);
+      e = launch_mma<kMmaF16, kSym, kSym>(h->p_poly, h->a_sym, h->a_sym, poly, EpiPoly{h->a_blocks, h->b_blocks, h->a, h->b, c.b, c.c}, st);
     EpiX ex;
     memset(&ex, 0, sizeof ex);
     ex.blocks[0] = h->hi_blocks[cur];
@@ -589,7 +581,7 @@ int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum
       ex.tall = c.rows > c.cols;
       ex.vec = c.cols % 16 == 0 && (op & 31u) == 0 && (xp & 15u) == 0 && mo.stride % 4 == 0;
     }
-    if (e == cudaSuccess) e = launch_mma<kMmaF16, true>(h->p_x, h->b_rows, h->x_across[cur], full, ex, st);
+    if (e == cudaSuccess) e = launch_mma<kMmaF16, kSym, kAcross>(h->p_x, h->b_sym, h->x_across[cur], full, ex, st);
   }
   return e == cudaSuccess ? DS_OK : cuda_fail(e, "orthogonalised update");
 }
