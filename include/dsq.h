@@ -410,12 +410,12 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
  * for `batch` matrices [rows, cols], each row-major and contiguous, `stride` elements apart in g, buf and x (0: rows * cols),
  * so that they can be slices of the flat gradient and model of the step above; out is contiguous.  buf is float and updated
  * in place (NULL: u = g).  g: DS_F32, DS_BF16 or DS_F16; out: DS_F32 or DS_BF16.  buf and u are formed in 32 bits exactly as
- * written (each operation rounded); the products run on 16-bit floats with 32-bit sums: X is within about 1e-3 of exact
- * arithmetic (Frobenius norm, relative).  Singular values of X must stay below 8 (they do for the usual coefficients).  An
+ * written (each operation rounded); the products run on 16-bit floats with 32-bit sums: X is within 2e-3 of exact arithmetic
+ * (Frobenius norm, relative; 2e-4 to 5e-4 for gradients with a few strong directions, 1e-5 where the shorter side is at most 64).  Singular values of X must stay below 8 (they do for the usual coefficients).  An
  * update of zeros gives zeros; one that holds an inf or a NaN gives NaN.
  *
  * ds_orth_create: with workspace == NULL fills *workspace_bytes and returns DS_NEED_BUFFERS; else makes a handle on that
- * workspace (256-byte aligned, zero-filled once by the caller).  Host-only.  One handle on one stream at a time.
+ * workspace (256-byte aligned; it need not be cleared).  Host-only.  One handle on one stream at a time.
  */
 #define DS_ORTH_NESTEROV 0x1u
 typedef struct {

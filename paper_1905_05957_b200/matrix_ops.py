@@ -148,6 +148,9 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
     sums, in that order; one thing asked for is returned by itself, several as a tuple."""
     if not (rows or cols or col_sum):
         raise ValueError("nothing to compute")
+    if stream is not None:
+        with torch.cuda.stream(stream):      # what is allocated here belongs to the stream that uses it
+            return int8_quantize(x, rows, cols, col_sum)
     if _call is None:
         _load()
     dt = _dtype(x.dtype, "x")
@@ -164,7 +167,7 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
     base = buf.data_ptr()
     rc = _call(_quantize_at, x.data_ptr(), dt, r, c, ld, base if rows else 0, ldr, base + at_rs if rows else 0,
                base + at_c if cols else 0, ldc, base + at_cs if cols else 0, base + at_sum if col_sum else 0,
-               base + at_ws if ws else 0, ws, _raw_stream(device.index) if stream is None else stream.cuda_stream)
+               base + at_ws if ws else 0, ws, _raw_stream(device.index))
     if rc:
         _check(rc, "ds_i8_quantize")
     got = []
@@ -190,6 +193,9 @@ def _out(out: torch.Tensor, m: int, n: int, device) -> int:
 def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """a b^T (+ bias): [a rows, b rows], the sums exact in 32-bit integers."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return int8_matmul(a, b, bias, out_dtype, out)
     if _call is None:
         _load()
     m, n, k, device = a.rows, b.rows, a.cols, a.device
@@ -204,7 +210,7 @@ def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, 
         ldo = _out(out, m, n, device)
     index = device.index
     rc = _call(_matmul_at, a.codes_ptr, a.ld, a.scale_ptr, b.codes_ptr, b.ld, b.scale_ptr, bp, m, n, k, out.data_ptr(),
-               _dtype(out.dtype, "out"), ldo, _dev_status(index), _raw_stream(index) if stream is None else stream.cuda_stream)
+               _dtype(out.dtype, "out"), ldo, _dev_status(index), _raw_stream(index))
     if rc:
         _check(rc, "ds_i8_matmul")
     return out
@@ -213,6 +219,9 @@ def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, 
 def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """x W^T (+ bias) for weights quantised before: x [tokens, k] is quantised by rows on the way."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return int8_linear(x, w, bias, out_dtype, out)
     if _call is None:
         _load()
     dt = _dtype(x.dtype, "x")
@@ -233,7 +242,7 @@ def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None
     ws = _empty(size, dtype=torch.uint8, device=device) if size else None
     index = device.index
     rc = _call(_linear_at, x.data_ptr(), dt, m, k, ld, w.codes_ptr, w.ld, w.scale_ptr, bp, n, out.data_ptr(), odt, ldo,
-               ws.data_ptr() if size else None, size, _dev_status(index), _raw_stream(index) if stream is None else stream.cuda_stream)
+               ws.data_ptr() if size else None, size, _dev_status(index), _raw_stream(index))
     if rc:
         _check(rc, "ds_i8_linear")
     return out
@@ -297,9 +306,10 @@ class OrthUpdate:
         rc = self.lib.ds_orth_create(C.byref(self.cfg), None, C.byref(size), None, None)
         if rc != DS_NEED_BUFFERS:
             raise DsqError(rc, "ds_orth_create (size query)")
-        self.workspace = torch.zeros(size.value, dtype=torch.uint8, device=device)
+        self.workspace = torch.empty(size.value, dtype=torch.uint8, device=device)
         self.device = self.workspace.device
         self.dev_status = torch.zeros(4, dtype=torch.int32, device=device)
+        torch.cuda.synchronize(self.device)      # cleared before a product on any stream may set it
         h = C.c_void_p()
         _check(self.lib.ds_orth_create(C.byref(self.cfg), self.workspace.data_ptr(), C.byref(size), self.dev_status.data_ptr(),
                                        C.byref(h)), "ds_orth_create")
@@ -319,7 +329,11 @@ class OrthUpdate:
                out_dtype: torch.dtype | None = torch.bfloat16, x: torch.Tensor | None = None, gamma: float = 0.0, decay: float = 0.0,
                stream=None) -> torch.Tensor | None:
         """One update.  momentum (float32) is advanced in place.  Returns the orthogonalised update [batch, rows, cols] in
-        `out` or a new tensor of out_dtype (None: not wanted).  x (float32): also x = x (1 - gamma decay) - gamma scale update."""
+        `out` or a new tensor of out_dtype (None: not wanted).  x (float32): also x = x (1 - gamma decay) - gamma scale update.
+        One plan works on one stream at a time: its workspace holds the matrices between the products."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.update(g, momentum, out, out_dtype, x, gamma, decay)
         if out is None and out_dtype is not None:
             out = torch.empty(self.batch, self.rows, self.cols, dtype=out_dtype, device=self.device)
         if out is not None and (out.dtype not in (torch.float32, torch.bfloat16) or not out.is_contiguous()
@@ -330,7 +344,7 @@ class OrthUpdate:
         xp = self._span(x, "x", (torch.float32,))
         _check(self.lib.ds_orth_update(self.handle, gp, _DTYPES[g.dtype], mp, None if out is None else out.data_ptr(),
                                        DS_F32 if out is None else _DTYPES[out.dtype], xp, gamma, decay,
-                                       _raw_stream(self.device.index) if stream is None else stream.cuda_stream), "ds_orth_update")
+                                       _raw_stream(self.device.index)), "ds_orth_update")
         return out
 
     def timed_out(self) -> bool:

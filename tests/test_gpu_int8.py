@@ -260,6 +260,33 @@ def test_other_streams_and_many_calls_in_a_row():
     assert all(torch.equal(y, z) for r in got for y, z in zip(r, want))
 
 
+def test_a_given_stream_owns_what_the_call_allocates():
+    """Calls on a stream that is behind, while the current stream allocates and overwrites: the calls' workspaces and results must
+    not be handed to it."""
+    g = _gen(14)
+    x = torch.randn(300, 512, device="cuda", generator=g)
+    w0 = torch.randn(256, 512, device="cuda", generator=g)
+    dy = torch.randn(300, 256, device="cuda", generator=g)
+    plain = Int8Linear(w0)
+    want = plain.forward(x, training=True), *plain.backward(dy)[:2], plain.forward(x)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        busy = torch.randn(4096, 4096, device="cuda")
+        for _ in range(20):
+            busy = torch.sin(busy)
+    layer = Int8Linear(w0, stream=s)
+    y = layer.forward(x, training=True, stream=s)
+    dx, dw, _ = layer.backward(dy, stream=s)
+    z = layer.forward(x, stream=s)
+    for _ in range(50):
+        for n in (300 * 256, 300 * 512, 256 * 512, 200_000, 500_000):
+            torch.full((n,), -1, dtype=torch.uint8, device="cuda") if n % 2 else torch.full((n,), float("nan"), device="cuda")
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((y, dx, dw, z), want))
+
+
 def test_linear_in_a_captured_graph():
     g = _gen(6)
     w = int8_quantize(torch.randn(256, 512, device="cuda", generator=g))

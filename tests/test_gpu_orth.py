@@ -171,6 +171,23 @@ def test_another_stream():
     assert all(torch.equal(v, want) for v in got)
 
 
+@pytest.mark.parametrize("m,n", [(48, 100), (256, 320)])
+def test_in_a_captured_graph(m, n):
+    g, buf = _matrix(1, m, n, "low", 1), torch.zeros(1, m, n, device="cuda")
+    plan, out = OrthUpdate(m, n), torch.empty(1, m, n, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.update(g, buf, out=out)
+    want_buf = torch.zeros_like(buf)
+    other = OrthUpdate(m, n)
+    for t in range(3):
+        g.copy_(_matrix(1, m, n, "low", 5 + t))
+        graph.replay()
+        want = other.update(g, want_buf, out_dtype=F32)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(buf, want_buf)
+
+
 def test_refusals():
     for kw in (dict(rows=0, cols=4), dict(rows=4, cols=0), dict(rows=4, cols=4, batch=0), dict(rows=4, cols=4, steps=0),
                dict(rows=4, cols=4, steps=33), dict(rows=4, cols=4, momentum=float("nan")), dict(rows=4, cols=4, eps=-1.0),
