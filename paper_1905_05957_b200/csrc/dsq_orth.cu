@@ -457,7 +457,8 @@ cudaError_t orth_maps(ds_orth_ctx* h) {
   h->p_x = plan_mma({h->m, h->n, h->m, batch, 2, 0, 0, nullptr});
   h->half_b = h->p_x.pair ? 8 : 7;
   h->p_poly = plan_mma({h->m, h->m, h->m, batch, 2, h->half_b, 0, nullptr}, true);
-  h->half_a = h->p_poly.pair || h->p_poly.bn > 128 ? 8 : 7;
+  // (the epilogue of B = b A + c A A reads of A what it writes of B)
+  h->half_a = h->half_b == 8 || h->p_poly.pair || h->p_poly.bn > 128 ? 8 : 7;
   h->p_gram = plan_mma({h->m, h->m, h->n, batch, 2, h->half_a, 0, nullptr});
   cudaError_t e = cudaSuccess;
   auto add = [&](CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t ld, uint64_t stride, uint32_t box_rows) {

@@ -53,11 +53,25 @@ SIZES = [(1, 1), (1, 40), (7, 3), (16, 16), (31, 33), (64, 64), (64, 576), (65, 
 def test_update_against_64_bits(m, n, kind):
     g = _matrix(1, m, n, kind, m * 1000 + n) * 3e-3
     plan = OrthUpdate(m, n)
+    plan.workspace.fill_(0xFF)
     got = plan.update(g, out_dtype=F32)[0]
     assert _off(got, _exact(g[0])) < TOL
     assert torch.equal(plan.update(g, out_dtype=BF16)[0], got.to(BF16))
     assert torch.equal(plan.update(g, out_dtype=F32)[0], got)          # and the same again
     assert not plan.timed_out()
+
+
+@pytest.mark.parametrize("batch,m,n", [(12, 706, 1202), (1, 1344, 3964), (3, 947, 3707), (2, 2090, 1368), (1, 1250, 1250), (1, 2500, 2500), (6, 512, 512)])
+def test_larger_updates_in_every_form_of_product(batch, m, n):
+    """Sizes at which the three products of a step are taken in different forms (single CTAs, pairs, split), which say how much of
+    the symmetric matrices between them is written."""
+    g = _matrix(batch, m, n, "low", m)
+    plan = OrthUpdate(m, n, batch=batch)
+    plan.workspace.fill_(0xFF)                 # NaN in 16 bits: nothing that was not written may be read
+    got = plan.update(g, out_dtype=F32)
+    for i in range(batch):
+        assert _off(got[i], _exact(g[i])) < TOL
+    assert torch.equal(plan.update(g, out_dtype=F32), got) and not plan.timed_out()
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
