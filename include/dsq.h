@@ -377,7 +377,7 @@ typedef enum { DS_F32 = 0, DS_BF16 = 1, DS_F16 = 2 } ds_dtype;
  *   Each of (q, scale), (qt, scale_t), col_sum may be NULL; x is read once for the rows alone, else twice.  Rounding is to
  *   nearest even.  A line of zeros (or one whose scale would be subnormal) has scale 0 and codes 0; a line that holds an
  *   inf or a NaN has scale NaN and codes 0, so that products with it are NaN.  Codes between the line's end and the next
- *   multiple of 16 may be overwritten (with 0 by rows).  q, qt: 16-byte aligned, ldq and ldqt multiples of 16.
+ *   multiple of 16 are overwritten with 0, none beyond.  q, qt: 16-byte aligned, ldq and ldqt multiples of 16.
  *   workspace (16-byte aligned, ds_i8_quantize_workspace bytes) is needed unless q alone is asked for.
  * ds_i8_matmul:  out_mn = (sum_k a_mk b_nk) * sa_m * sb_n + bias_n  with a [m, k], b [n, k]; the sum is exact, the rest is
  *   done from left to right in 32 bits.  bias may be NULL.  out [m, n], `ldo` elements between rows, of type out_dtype.  k <= DS_I8_MAX_K, else DS_ERR_UNSUPPORTED.
@@ -413,7 +413,7 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
  * written (each operation rounded); the products run on 16-bit floats with 32-bit sums: X is within 2e-3 of exact arithmetic
  * (Frobenius norm, relative; typically 2e-4 to 8e-4; 1e-5 where the shorter side is at most
  * 64 and the longer not above about 2000, which take another form).  Singular values of X must stay below 8 (they do for the usual coefficients).  An
- * update of zeros gives zeros; one that holds an inf or a NaN gives NaN.
+ * update of zeros gives zeros (NaN if eps is 0); one that holds an inf or a NaN gives NaN.
  *
  * ds_orth_create: with workspace == NULL fills *workspace_bytes and returns DS_NEED_BUFFERS; else makes a handle on that
  * workspace (256-byte aligned; it need not be cleared).  Host-only.  One handle on one stream at a time.

