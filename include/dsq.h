@@ -412,7 +412,8 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
  * in place (NULL: u = g).  g: DS_F32, DS_BF16 or DS_F16; out: DS_F32 or DS_BF16.  buf and u are formed in 32 bits exactly as
  * written (each operation rounded); the products run on 16-bit floats with 32-bit sums: X is within 2e-3 of exact arithmetic
  * (Frobenius norm, relative; typically 2e-4 to 8e-4; 1e-5 where the shorter side is at most
- * 64 and the longer not above about 2000, which take another form).  Singular values of X must stay below 8 (they do for the usual coefficients).  An
+ * 64 and the longer at most 2048, which take another form).  Singular values of X must stay below 8 (they do for the usual
+ * coefficients).  An
  * update of zeros gives zeros (NaN if eps is 0); one that holds an inf or a NaN gives NaN.
  *
  * ds_orth_create: with workspace == NULL fills *workspace_bytes and returns DS_NEED_BUFFERS; else makes a handle on that

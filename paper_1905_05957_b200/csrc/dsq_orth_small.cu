@@ -320,11 +320,15 @@ cudaError_t launch(const SmallArgs& a, uint32_t ctas, uint32_t batch, cudaStream
 
 namespace dsq {
 
-// Time in us, fitted to measurements: slices of 32, 64, 80, 128, 256, 512 columns took 21, 26, 34, 38, 58 and 98 for one wave of
-// clusters.  The general form takes 50 to 76 for m <= 64 (1 x 64 x 64: 52, 1 x 64 x 2048: 72, 40 x 64 x 576: 76).
+// Matrices of up to 64 x 2048 take this form, as many CTAs each as the estimate finds best: slices of 32, 64, 80, 128, 256, 512
+// columns took 21, 26, 34, 38, 58 and 98 us for one wave of clusters.  Longer ones are faster in the general form (64 x 2048:
+// 58 here, 72 there; 64 x 3000: 78 and 79; 64 x 4096: 98 and 76).  The batch does not decide: a few matrices are faster here (16 of 64 x 576: 44 us, 63 there), many
+// about the same (400: 344 and 366; 2000 of 64 x 64: 368 and 313; 4000 of 16 x 16: 537 and 443), and these are the sizes that
+// need two halves: with the batch deciding, the same matrix came out a thousandfold less exact in a larger batch.
+constexpr uint32_t kSmallLength = 2048;
 uint32_t orth_small_ctas(uint32_t m, uint32_t n, uint32_t batch) {
-  if (m > MP) return 0;
-  double least = 65;
+  if (m > MP || n > kSmallLength) return 0;
+  double least = 1e30;
   uint32_t best = 0;
   for (uint32_t c = 1; c <= kMaxCluster; c *= 2) {
     const uint32_t w = slice(n, c), at_once = c == 1 ? (uint32_t)sm_count() : (uint32_t)cluster_count(c);
