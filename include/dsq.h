@@ -411,7 +411,7 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
  * so that they can be slices of the flat gradient and model of the step above; out is contiguous.  buf is float and updated
  * in place (NULL: u = g).  g: DS_F32, DS_BF16 or DS_F16; out: DS_F32 or DS_BF16.  buf and u are formed in 32 bits exactly as
  * written (each operation rounded); the products run on 16-bit floats with 32-bit sums: X is within 2e-3 of exact arithmetic
- * (Frobenius norm, relative; typically 2e-4 to 8e-4; 1e-5 where the shorter side is at most
+ * (Frobenius norm, relative; typically 2e-4 to 8e-4; with fewer than 8 rows or columns the roundings average out less: 4e-3; 1e-5 where the shorter side is at most
  * 64 and the longer at most 2048, which take another form).  Singular values of X must stay below 8 (they do for the usual
  * coefficients).  An
  * update of zeros gives zeros (NaN if eps is 0); one that holds an inf or a NaN gives NaN.
