@@ -410,9 +410,12 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
  * for `batch` matrices [rows, cols], each row-major and contiguous, `stride` elements apart in g, buf and x (0: rows * cols),
  * so that they can be slices of the flat gradient and model of the step above; out is contiguous.  buf is float and updated
  * in place (NULL: u = g).  g: DS_F32, DS_BF16 or DS_F16; out: DS_F32 or DS_BF16.  buf and u are formed in 32 bits exactly as
- * written (each operation rounded); the products run on 16-bit floats with 32-bit sums: X is within 2e-3 of exact arithmetic
- * (Frobenius norm, relative; typically 2e-4 to 8e-4; with fewer than 8 rows or columns the roundings average out less: 4e-3; 1e-5 where the shorter side is at most
- * 64 and the longer at most 2048, which take another form).  Singular values of X must stay below 8 (they do for the usual
+ * written (each operation rounded); the products run on 16-bit floats with 32-bit sums: X is within 1e-2 of exact arithmetic
+ * (Frobenius norm, relative, up to five steps of the usual coefficients) whatever u: typically 2e-4 to 1e-3, and up to 7e-3 where few
+ * rows of u are not zero or its entries are all alike, so that roundings do not average out.  Matrices whose shorter side is at most 64
+ * and whose longer side is at most 2048 take another form, which is as exact as 32-bit arithmetic: 1e-5, and up to 2e-4 where
+ * rows depend on one another.  Every step multiplies what roundings leave in directions where u is zero by a, in whatever
+ * arithmetic: more than eight steps of the usual coefficients are only for matrices of full rank.  Singular values of X must stay below 8 (they do for the usual
  * coefficients).  An
  * update of zeros gives zeros (NaN if eps is 0); one that holds an inf or a NaN gives NaN.
  *

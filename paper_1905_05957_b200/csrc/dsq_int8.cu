@@ -860,9 +860,9 @@ cudaError_t product(const int8_t* a, uint64_t lda, const float* sa, const int8_t
     cudaError_t e = make_tensor_map(&mw, kMmaI8, b, k, n, 1, ldb, ldb * n, 128, kMmaRows);
     if (e == cudaSuccess) e = make_tensor_map(&mx, kMmaI8, a, k, m, 1, lda, lda * m, 128, plan.box_rows());
     if (e != cudaSuccess) return e;
-    if (!narrow) return launch_mma<kMmaI8, kAlong, kAlong>(plan, mw, mx, s, epi, st);
-    return plan.parts > 1 ? launch_mma_split<kMmaI8, 32, kAlong, kAlong>(plan.parts, mw, mx, s, epi, st)
-                          : launch_mma_bn<kMmaI8, 32, kAlong, kAlong>(mw, mx, s, epi, st);
+    if (!narrow) return launch_mma<kMmaI8, kAlong, kAlong>(plan, mw, mx, mx, s, epi, st);
+    return plan.parts > 1 ? launch_mma_split<kMmaI8, 32, kAlong, kAlong>(plan.parts, mw, mx, mx, s, epi, st)
+                          : launch_mma_bn<kMmaI8, 32, kAlong, kAlong>(mw, mx, mx, s, epi, st);
   }
   const MmaShape s{m, n, k, 1, 1, 0, 0, dev_status};
   const EpiScale<T> epi{sa, sb, bias, out, ldo, m, n};
@@ -871,7 +871,7 @@ cudaError_t product(const int8_t* a, uint64_t lda, const float* sa, const int8_t
   cudaError_t e = make_tensor_map(&ma, kMmaI8, a, k, m, 1, lda, lda * m, 128, kMmaRows);
   if (e == cudaSuccess) e = make_tensor_map(&mb, kMmaI8, b, k, n, 1, ldb, ldb * n, 128, plan.box_rows());
   if (e != cudaSuccess) return e;
-  return launch_mma<kMmaI8, kAlong, kAlong>(plan, ma, mb, s, epi, st);
+  return launch_mma<kMmaI8, kAlong, kAlong>(plan, ma, mb, mb, s, epi, st);
 }
 
 template <class T>

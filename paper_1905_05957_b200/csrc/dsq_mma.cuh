@@ -177,6 +177,19 @@ struct MmaShape {
   uint32_t sym;            // 7 or 8: C is symmetric; only its blocks of 2^sym on or above the diagonal go to the epilogue (0: all)
   uint32_t half;           // 7 or 8: blocks of 2^half of the kSym operands are there
   uint32_t* dev_status;
+  uint32_t passes = 1;     // 2: C = A B2 + A B, B and B2 across K: K is gone through for B2 first, then for B
+};
+// Step kb of all passes as a step of K, and whether it belongs to B2.
+template <int B_MODE>
+struct PassStep {
+  uint32_t k;
+  bool second;
+  __device__ __forceinline__ PassStep(const MmaShape& s, uint32_t kb, uint32_t steps) : k(kb), second(false) {
+    if (B_MODE == kAcross && s.passes > 1) {
+      second = kb < steps;
+      k = second ? kb : kb - steps;
+    }
+  }
 };
 
 // Fetches a step of an operand: ROWS rows by 128 bytes of K, or their mirror image, 64 columns at a time.
@@ -386,7 +399,8 @@ struct TileWalk {
 
 template <int KIND, int BN, int A_MODE, int B_MODE, class Epi>
 __global__ void __launch_bounds__(kMmaThreads, 1)
-    k_mma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const __grid_constant__ Epi epi) {
+    k_mma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_b2, const MmaShape shape,
+          const __grid_constant__ Epi epi) {
   using T = MmaTile<BN, Epi>;
   constexpr int kBK = KIND == kMmaF16 ? 64 : 128;    // elements of K per stage: 128 bytes
   extern __shared__ uint8_t dyn[];
@@ -401,6 +415,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   if (threadIdx.x == 0) {
     tma_prefetch_map(&map_a);
     tma_prefetch_map(&map_b);
+    if (B_MODE == kAcross && shape.passes > 1) tma_prefetch_map(&map_b2);
     for (int i = 0; i < T::kStages; ++i) {
       mbar_init(full + 8 * i, 1);
       mbar_init(empty + 8 * i, 1);
@@ -427,7 +442,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   asm volatile("fence.proxy.async.global;" ::: "memory");   // what earlier kernels stored is about to be read by TMA
 
   const TileWalk walk(shape, BN);
-  const uint32_t nk = (shape.k + kBK - 1) / kBK;
+  const uint32_t steps = (shape.k + kBK - 1) / kBK, nk = B_MODE == kAcross ? steps * shape.passes : steps;
 
   if (warp == 0) {
     const bool one = elect_one();
@@ -441,8 +456,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         const uint32_t dst = ring + stage * T::kStageBytes;
         if (one) {
           mbar_expect_tx(full + 8 * stage, T::kStageBytes);
-          load_operand<A_MODE, kMmaRows>(shape, dst, &map_a, kb * kBK, i * kMmaRows, b, full + 8 * stage);
-          load_operand<B_MODE, BN>(shape, dst + kMmaRows * 128, &map_b, kb * kBK, j * BN, b, full + 8 * stage);
+          const PassStep<B_MODE> at(shape, kb, steps);
+          load_operand<A_MODE, kMmaRows>(shape, dst, &map_a, at.k * kBK, i * kMmaRows, b, full + 8 * stage);
+          load_operand<B_MODE, BN>(shape, dst + kMmaRows * 128, at.second ? &map_b2 : &map_b, at.k * kBK, j * BN, b, full + 8 * stage);
         }
         __syncwarp();
         ++issued;
@@ -477,7 +493,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tc_fence_after();
         if (one) {
           const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128;
-          const bool ta = A_MODE == kSym && mirrored(shape, kb * kBK, i * kMmaRows), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, kb * kBK, j * BN));
+          const uint32_t k0 = PassStep<B_MODE>(shape, kb, steps).k * kBK;
+          const bool ta = A_MODE == kSym && mirrored(shape, k0, i * kMmaRows), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, j * BN));
           const uint32_t idesc = mma_idesc<KIND>(kMmaRows, BN, ta, tb);
 #pragma unroll
           for (int q = 0; q < 4; ++q)   // four instructions of 32 bytes of K
@@ -637,7 +654,8 @@ __device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t a_desc, ui
 
 template <int KIND, int A_MODE, int B_MODE, class Epi>
 __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
-    k_mma_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const __grid_constant__ Epi epi) {
+    k_mma_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_b2, const MmaShape shape,
+               const __grid_constant__ Epi epi) {
   constexpr int kPairStages = PairTile<Epi>::kStages;
   constexpr int kBK = KIND == kMmaF16 ? 64 : 128;
   extern __shared__ uint8_t dyn[];
@@ -653,6 +671,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
   if (threadIdx.x == 0) {
     tma_prefetch_map(&map_a);
     tma_prefetch_map(&map_b);
+    if (B_MODE == kAcross && shape.passes > 1) tma_prefetch_map(&map_b2);
     for (int i = 0; i < kPairStages; ++i) {
       mbar_init(full + 8 * i, 1);
       mbar_init(empty + 8 * i, 1);
@@ -681,7 +700,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
 
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const PairWalk walk(shape, pairs);
-  const uint32_t nk = (shape.k + kBK - 1) / kBK;
+  const uint32_t steps = (shape.k + kBK - 1) / kBK, nk = B_MODE == kAcross ? steps * shape.passes : steps;
   // an item of which nothing is wanted (outside C, or below the diagonal): every role passes over it
   auto skip = [&](uint32_t row, uint32_t col, uint32_t width) { return col >= shape.n || (shape.sym && col + width <= row); };
 
@@ -699,7 +718,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
         const uint32_t dst = ring + stage * kPairStageBytes, bar = in_cta(full + 8 * stage, 0);
         if (one) {
           if (rank == 0) mbar_expect_tx(full + 8 * stage, 2 * (kMmaRows + mine) * 128);
-          const uint32_t k0 = kb * kBK, r0 = row + rank * kMmaRows, n0 = col + rank * mine;
+          const PassStep<B_MODE> at(shape, kb, steps);
+          const uint32_t k0 = at.k * kBK, r0 = row + rank * kMmaRows, n0 = col + rank * mine;
           if constexpr (A_MODE == kAlong) {
             tma_load_3d_pair(dst, &map_a, (int)k0, (int)r0, (int)b, bar);
           } else {
@@ -710,7 +730,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
           }
           const bool across = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, col));
           for (uint32_t c = 0; c < mine; c += 64)
-            tma_load_3d_pair(dst + (kMmaRows + c) * 128, &map_b, (int)(across ? n0 + c : k0), (int)(across ? k0 : n0 + c), (int)b, bar);
+            tma_load_3d_pair(dst + (kMmaRows + c) * 128, at.second ? &map_b2 : &map_b, (int)(across ? n0 + c : k0), (int)(across ? k0 : n0 + c), (int)b, bar);
         }
         __syncwarp();
         ++issued;
@@ -746,7 +766,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
         tc_fence_after();
         if (one) {
           const uint32_t sa = ring + stage * kPairStageBytes, sb = sa + kMmaRows * 128;
-          const bool ta = A_MODE == kSym && mirrored(shape, kb * kBK, row), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, kb * kBK, col));
+          const uint32_t k0 = PassStep<B_MODE>(shape, kb, steps).k * kBK;
+          const bool ta = A_MODE == kSym && mirrored(shape, k0, row), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, col));
           const uint32_t idesc = mma_idesc<KIND>(2 * kMmaRows, width, ta, tb);
 #pragma unroll
           for (int q = 0; q < 4; ++q) tc_mma_pair<KIND>(d, step_desc(sa, q, ta), step_desc(sb, q, tb), idesc, (kb | q) != 0);
@@ -813,7 +834,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
 // of K in a row; on a third of the SMs.
 template <int KIND, int BN, int A_MODE, int B_MODE, class Epi>
 __global__ void __launch_bounds__(kMmaThreads, 1)
-    k_mma_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MmaShape shape, const __grid_constant__ Epi epi,
+    k_mma_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_b2, const MmaShape shape,
+                const __grid_constant__ Epi epi,
                 const uint32_t parts) {
   using T = MmaTile<BN, Epi>;
   constexpr int kBK = KIND == kMmaF16 ? 64 : 128;
@@ -832,6 +854,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   if (threadIdx.x == 0) {
     tma_prefetch_map(&map_a);
     tma_prefetch_map(&map_b);
+    if (B_MODE == kAcross && shape.passes > 1) tma_prefetch_map(&map_b2);
     for (int i = 0; i < T::kStages; ++i) {
       mbar_init(full + 8 * i, 1);
       mbar_init(empty + 8 * i, 1);
@@ -854,7 +877,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const TileWalk walk(shape, BN);
   uint32_t b, ti, tj;
   walk.at(blockIdx.x / parts, b, ti, tj);
-  const uint32_t nk_all = (shape.k + kBK - 1) / kBK, share = (nk_all + parts - 1) / parts;
+  const uint32_t steps = (shape.k + kBK - 1) / kBK, nk_all = B_MODE == kAcross ? steps * shape.passes : steps, share = (nk_all + parts - 1) / parts;
   const uint32_t k_first = min(rank * share, nk_all), nk = min(share, nk_all - k_first);
 
   const uint32_t quarter = warp & 3, group = (warp - 4) >> 2;   // epilogue warps
@@ -876,8 +899,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       const uint32_t dst = ring + stage * T::kStageBytes;
       if (one) {
         mbar_expect_tx(full + 8 * stage, T::kStageBytes);
-        load_operand<A_MODE, kMmaRows>(shape, dst, &map_a, kb * kBK, ti * kMmaRows, b, full + 8 * stage);
-        load_operand<B_MODE, BN>(shape, dst + kMmaRows * 128, &map_b, kb * kBK, c_first, b, full + 8 * stage);
+        const PassStep<B_MODE> at(shape, kb, steps);
+        load_operand<A_MODE, kMmaRows>(shape, dst, &map_a, at.k * kBK, ti * kMmaRows, b, full + 8 * stage);
+        load_operand<B_MODE, BN>(shape, dst + kMmaRows * 128, at.second ? &map_b2 : &map_b, at.k * kBK, c_first, b, full + 8 * stage);
       }
       __syncwarp();
       ++issued;
@@ -903,7 +927,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       if (!mbar_wait(full + 8 * stage, phase, &gave_up)) break;
       tc_fence_after();
       if (one) {
-        const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128, k0 = (k_first + kb) * kBK;
+        const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128, k0 = PassStep<B_MODE>(shape, k_first + kb, steps).k * kBK;
         const bool ta = A_MODE == kSym && mirrored(shape, k0, ti * kMmaRows), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, c_first));
         const uint32_t idesc = mma_idesc<KIND>(kMmaRows, BN, ta, tb);
 #pragma unroll
@@ -1019,19 +1043,20 @@ inline double step_time(int bn, double busy) {
 inline double rounds_time(double rounds, double main, double epilogue) {
   return rounds <= 0 ? 0 : main + (rounds - 1) * (main > epilogue ? main : epilogue) + epilogue;
 }
+inline double k_steps(const MmaShape& s) { return s.passes * (s.k * (double)s.elem / 128); }
 inline double single_time(const MmaShape& s, int sms, int bn) {
   const TileWalk w(s, bn);
-  return 4 + rounds_time((double)((w.total + sms - 1) / sms), step_time(bn, (double)w.total / sms) * (s.k * (double)s.elem / 128),
+  return 4 + rounds_time((double)((w.total + sms - 1) / sms), step_time(bn, (double)w.total / sms) * k_steps(s),
                          kTileEpilogue * bn / 64);
 }
 inline double split_time(const MmaShape& s, int sms, int bn, uint32_t parts) {
   const TileWalk w(s, bn);
   if (w.total > (uint32_t)cluster_count(parts) || bn > 128) return 1e300;   // one round: a CTA keeps one tile
-  return 8 + step_time(bn, (double)w.total * parts / sms) * (s.k * (double)s.elem / 128) / parts + kTileEpilogue * bn / 64;
+  return 8 + step_time(bn, (double)w.total * parts / sms) * k_steps(s) / parts + kTileEpilogue * bn / 64;
 }
 inline double pair_time(const MmaShape& s, int pairs) {
   const PairWalk w(s, pairs);
-  const double rounds = w.whole / pairs + (w.whole % pairs != 0), steps = s.k * (double)s.elem / 128, epi = 4 * kTileEpilogue;
+  const double rounds = w.whole / pairs + (w.whole % pairs != 0), steps = k_steps(s), epi = 4 * kTileEpilogue;
   const double main = 0.40 * steps;
   double t = 6 + rounds_time(rounds, main, epi);
   if (w.items > w.whole) t += rounds > 0 ? (0.5 * main > epi ? 0.5 * main : epi) - 0.5 * epi : 0.5 * (main + epi);
@@ -1068,18 +1093,18 @@ inline void allow_smem_for(size_t bytes) {
 }
 
 template <int KIND, int BN, int A_MODE, int B_MODE, class Epi>
-cudaError_t launch_mma_bn(const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
+cudaError_t launch_mma_bn(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b2, const MmaShape& s, const Epi& epi, cudaStream_t st) {
   const TileWalk w(s, BN);
   const uint32_t grid = w.total < (uint32_t)sm_count() ? w.total : (uint32_t)sm_count();
   if (!grid) return cudaSuccess;
   allow_smem_for<k_mma<KIND, BN, A_MODE, B_MODE, Epi>>(MmaTile<BN, Epi>::kSmem);
-  launch_pdl_dyn(k_mma<KIND, BN, A_MODE, B_MODE, Epi>, dim3(grid), dim3(kMmaThreads), MmaTile<BN, Epi>::kSmem, st, a, b, s, epi);
+  launch_pdl_dyn(k_mma<KIND, BN, A_MODE, B_MODE, Epi>, dim3(grid), dim3(kMmaThreads), MmaTile<BN, Epi>::kSmem, st, a, b, b2, s, epi);
   count_launches(1);
   return cudaGetLastError();
 }
 
 template <int KIND, int BN, int A_MODE, int B_MODE, class Epi>
-cudaError_t launch_mma_split(uint32_t parts, const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
+cudaError_t launch_mma_split(uint32_t parts, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b2, const MmaShape& s, const Epi& epi, cudaStream_t st) {
   const TileWalk w(s, BN);
   if (!w.total) return cudaSuccess;
   allow_smem_for<k_mma_split<KIND, BN, A_MODE, B_MODE, Epi>>(MmaTile<BN, Epi>::kSmem);
@@ -1096,34 +1121,34 @@ cudaError_t launch_mma_split(uint32_t parts, const CUtensorMap& a, const CUtenso
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  (void)cudaLaunchKernelEx(&cfg, k_mma_split<KIND, BN, A_MODE, B_MODE, Epi>, a, b, s, epi, parts);
+  (void)cudaLaunchKernelEx(&cfg, k_mma_split<KIND, BN, A_MODE, B_MODE, Epi>, a, b, b2, s, epi, parts);
   count_launches(1);
   return cudaGetLastError();
 }
 
 template <int KIND, int A_MODE, int B_MODE, class Epi>
-cudaError_t launch_mma(const MmaPlan& plan, const CUtensorMap& a, const CUtensorMap& b, const MmaShape& s, const Epi& epi, cudaStream_t st) {
+cudaError_t launch_mma(const MmaPlan& plan, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b2, const MmaShape& s, const Epi& epi, cudaStream_t st) {
   if (plan.pair) {
     const PairWalk w(s, pair_count());
     const uint32_t pairs = w.items < (uint32_t)pair_count() ? w.items : (uint32_t)pair_count();
     if (!pairs) return cudaSuccess;
     allow_smem_for<k_mma_pair<KIND, A_MODE, B_MODE, Epi>>(PairTile<Epi>::kSmem);
-    launch_pdl_dyn(k_mma_pair<KIND, A_MODE, B_MODE, Epi>, dim3(2 * pairs), dim3(kMmaThreads), PairTile<Epi>::kSmem, st, a, b, s, epi);
+    launch_pdl_dyn(k_mma_pair<KIND, A_MODE, B_MODE, Epi>, dim3(2 * pairs), dim3(kMmaThreads), PairTile<Epi>::kSmem, st, a, b, b2, s, epi);
     count_launches(1);
     return cudaGetLastError();
   }
   if (plan.parts > 1)
-    return plan.bn == 128 ? launch_mma_split<KIND, 128, A_MODE, B_MODE>(plan.parts, a, b, s, epi, st)
-                          : launch_mma_split<KIND, 64, A_MODE, B_MODE>(plan.parts, a, b, s, epi, st);
+    return plan.bn == 128 ? launch_mma_split<KIND, 128, A_MODE, B_MODE>(plan.parts, a, b, b2, s, epi, st)
+                          : launch_mma_split<KIND, 64, A_MODE, B_MODE>(plan.parts, a, b, b2, s, epi, st);
   switch (plan.bn) {
-    case 256: return launch_mma_bn<KIND, 256, A_MODE, B_MODE>(a, b, s, epi, st);
+    case 256: return launch_mma_bn<KIND, 256, A_MODE, B_MODE>(a, b, b2, s, epi, st);
     case 192:
       if constexpr (B_MODE == kSym)
         return cudaErrorInvalidValue;
       else
-        return launch_mma_bn<KIND, 192, A_MODE, B_MODE>(a, b, s, epi, st);
-    case 128: return launch_mma_bn<KIND, 128, A_MODE, B_MODE>(a, b, s, epi, st);
-    default: return launch_mma_bn<KIND, 64, A_MODE, B_MODE>(a, b, s, epi, st);
+        return launch_mma_bn<KIND, 192, A_MODE, B_MODE>(a, b, b2, s, epi, st);
+    case 128: return launch_mma_bn<KIND, 128, A_MODE, B_MODE>(a, b, b2, s, epi, st);
+    default: return launch_mma_bn<KIND, 64, A_MODE, B_MODE>(a, b, b2, s, epi, st);
   }
 }
 

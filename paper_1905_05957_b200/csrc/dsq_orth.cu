@@ -8,11 +8,18 @@
 // would be eight times as large) and add up in 32 bits.  The entries of X, A and B are bounded (|X| <= 1.3, |A| <= 1.5, |B| <= 8 for
 // the usual coefficients), so they are held times 2^10, which keeps small entries out of the subnormals.  Two things
 // would otherwise lose bits that later steps multiply by a = 3.4 each:
-//  - X is carried in two halves (hi + lo, 22 bits).  The term aX takes both; the products take hi.  With hi alone, updates
-//    whose energy sits in few directions came out 0.6 % to 2 % off; with both, 0.02 % to 0.05 %.
+//  - X is carried in two halves (hi + lo, 22 bits), of which aX takes both.  With hi alone, updates whose energy sits in few
+//    directions came out 0.6 % to 2 % off.
 //  - The diagonals of A and B, which hold most of their size when rows are nearly orthogonal, stay in 32 bits: A = D + O and
 //    B = E + F with F off-diagonal:  F = b O + c (O O)_off + c (d_i + d_j) O_ij,  E_ii = b d_i + c d_i^2 + c (O O)_ii,
-//    X = (a + E) X + F X.  Row scalings cost nothing in the epilogues.  (0.1 % to 0.2 % off without it on such inputs.)
+//    X = a X + E X + F X.  Row scalings cost nothing in the epilogues.  (0.1 % to 0.2 % off without it on such inputs.)
+//  - E and F have to take the same X while errors can still grow.  B maps the left null space of X to zero, but only as E + F: with E (hi + lo)
+//    + F hi something of the size of lo stays in directions where X is zero, and each later step multiplies it by a.  (In
+//    all five steps: updates of 2 live rows of rank 1 were 4 % off, the gradient of one sample 4 %.)  So the first two steps take E hi + F hi,
+//    which leaves out B lo where X is not zero, and that does not grow; the last two take E (hi + lo) + F hi, whose errors have one step left
+//    to grow in; those between take both halves in both terms, F lo by a second pass over K.
+// What is left is 0.02 % to 0.1 % of ordinary updates; at most 0.7 % where few rows are not zero or all entries are alike, so that the
+// roundings of O and F are alike too (the worst of 1500 such inputs, and of 30000 under the same roundings emulated; median 0.1 %).
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -297,6 +304,7 @@ struct EpiX {   // X = (a + E) X + F X
   uint64_t diag_stride;
   uint32_t m, n;
   float a1;
+  int e_hi;                         // E multiplies the high half of X alone
   int last;                         // the last step writes:
   OrthOut to;                       //   in the orientation of the gradient
   int tall, vec;
@@ -304,7 +312,7 @@ struct EpiX {   // X = (a + E) X + F X
   __device__ __forceinline__ const CUtensorMap* out(int i) const { return last ? nullptr : next + i; }
   __device__ __forceinline__ Pre load(uint32_t row, uint32_t, uint32_t b) const { return {row < m ? diag[b * diag_stride + row] : 0.f}; }
   __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t b, uint32_t block, int lane) const {
-    const float f = a1 + p.e;
+    const float f = e_hi ? a1 : a1 + p.e, f_hi = e_hi ? p.e : 0.f;
     float v[32];
     Half32 h, l;
     h.get(block, lane);
@@ -312,8 +320,8 @@ struct EpiX {   // X = (a + E) X + F X
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       const float2 x = h.two(j), y = l.two(j);
-      v[2 * j] = fmaf(f, x.x + y.x, __uint_as_float(acc[2 * j]) * kDown);
-      v[2 * j + 1] = fmaf(f, x.y + y.y, __uint_as_float(acc[2 * j + 1]) * kDown);
+      v[2 * j] = fmaf(f, x.x + y.x, fmaf(f_hi, x.x, __uint_as_float(acc[2 * j]) * kDown));
+      v[2 * j + 1] = fmaf(f, x.y + y.y, fmaf(f_hi, x.y, __uint_as_float(acc[2 * j + 1]) * kDown));
     }
     if (!last) {
 #pragma unroll
@@ -388,6 +396,10 @@ struct EpiX {   // X = (a + E) X + F X
 
 inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
+// Which halves of X step s takes in E X and in F X (file header).
+enum HalvesTaken { kEhiFhi, kEbothFboth, kEbothFhi };
+inline HalvesTaken halves_of(uint32_t s, uint32_t steps) { return s + 2 >= steps ? kEbothFhi : s < 2 ? kEhiFhi : kEbothFboth; }
+
 bool orth_config_ok(const ds_orth_config* c) {
   if (!c || c->rows < 1 || c->cols < 1 || c->batch < 1 || c->batch > 65535 || c->rows > (1u << 20) || c->cols > (1u << 20)) return false;
   if (c->steps < 1 || c->steps > 32 || (c->flags & ~DS_ORTH_NESTEROV) || c->reserved) return false;
@@ -411,7 +423,7 @@ struct ds_orth_ctx {
   bool mapped;                    // the tensor maps below are made (on the first update: the driver makes them)
   MmaPlan p_gram, p_poly, p_x;
   uint32_t half_a, half_b;        // A and B: log2 of the blocks of which half is there
-  CUtensorMap x_rows[2], x_cols_gram[2], x_across[2], a_sym, b_sym;
+  CUtensorMap x_rows[2], x_cols_gram[2], x_across[2], lo_across[2], a_sym, b_sym;
   CUtensorMap hi_blocks[2], lo_blocks[2], a_blocks, b_blocks;
 };
 
@@ -468,6 +480,7 @@ cudaError_t orth_maps(ds_orth_ctx* h) {
     add(&h->x_rows[i], h->hi[i], h->n, h->m, h->ldx, h->xs, kMmaRows);
     add(&h->x_cols_gram[i], h->hi[i], h->n, h->m, h->ldx, h->xs, h->p_gram.box_rows());
     add(&h->x_across[i], h->hi[i], h->n, h->m, h->ldx, h->xs, 64);
+    add(&h->lo_across[i], h->lo[i], h->n, h->m, h->ldx, h->xs, 64);
   }
   add(&h->a_sym, h->a.off, h->m, h->m, h->ldm, h->ms, 64);
   add(&h->b_sym, h->b.off, h->m, h->m, h->ldm, h->ms, 64);
@@ -558,13 +571,13 @@ int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum
   cudaError_t e = g_dtype == DS_F32    ? launch_prepare<float>(h, mo, vec, st)
                   : g_dtype == DS_BF16 ? launch_prepare<__nv_bfloat16>(h, mo, vec, st)
                                        : launch_prepare<__half>(h, mo, vec, st);
-  const MmaShape gram{h->m, h->m, h->n, c.batch, 2, h->half_a, 0, h->dev_status}, poly{h->m, h->m, h->m, c.batch, 2, h->half_b, h->half_a, h->dev_status},
-      full{h->m, h->n, h->m, c.batch, 2, 0, h->half_b, h->dev_status};
+  const MmaShape gram{h->m, h->m, h->n, c.batch, 2, h->half_a, 0, h->dev_status}, poly{h->m, h->m, h->m, c.batch, 2, h->half_b, h->half_a, h->dev_status};
+  MmaShape full{h->m, h->n, h->m, c.batch, 2, 0, h->half_b, h->dev_status};
   int cur = 0;
   for (uint32_t s = 0; s < c.steps && e == cudaSuccess; ++s, cur ^= 1) {
-    e = launch_mma<kMmaF16, kAlong, kAlong>(h->p_gram, h->x_rows[cur], h->x_cols_gram[cur], gram, EpiGram{h->a_blocks, h->a}, st);
+    e = launch_mma<kMmaF16, kAlong, kAlong>(h->p_gram, h->x_rows[cur], h->x_cols_gram[cur], h->x_cols_gram[cur], gram, EpiGram{h->a_blocks, h->a}, st);
     if (e == cudaSuccess)
-      e = launch_mma<kMmaF16, kSym, kSym>(h->p_poly, h->a_sym, h->a_sym, poly, EpiPoly{h->a_blocks, h->b_blocks, h->a, h->b, c.b, c.c}, st);
+      e = launch_mma<kMmaF16, kSym, kSym>(h->p_poly, h->a_sym, h->a_sym, h->a_sym, poly, EpiPoly{h->a_blocks, h->b_blocks, h->a, h->b, c.b, c.c}, st);
     EpiX ex;
     memset(&ex, 0, sizeof ex);
     ex.blocks[0] = h->hi_blocks[cur];
@@ -582,7 +595,10 @@ int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum
       ex.tall = c.rows > c.cols;
       ex.vec = c.cols % 16 == 0 && (op & 31u) == 0 && (xp & 15u) == 0 && mo.stride % 4 == 0;
     }
-    if (e == cudaSuccess) e = launch_mma<kMmaF16, kSym, kAcross>(h->p_x, h->b_sym, h->x_across[cur], full, ex, st);
+    const HalvesTaken taken = halves_of(s, c.steps);
+    ex.e_hi = taken == kEhiFhi;
+    full.passes = taken == kEbothFboth ? 2 : 1;
+    if (e == cudaSuccess) e = launch_mma<kMmaF16, kSym, kAcross>(h->p_x, h->b_sym, h->x_across[cur], h->lo_across[cur], full, ex, st);
   }
   return e == cudaSuccess ? DS_OK : cuda_fail(e, "orthogonalised update");
 }
