@@ -415,9 +415,9 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
  * rows of u are not zero or its entries are all alike, so that roundings do not average out.  Matrices whose shorter side is at most 64
  * and whose longer side is at most 2048 take another form, which is as exact as 32-bit arithmetic: 1e-5, and up to 2e-4 where
  * rows depend on one another.  Every step multiplies what roundings leave in directions where u is zero by a, in whatever
- * arithmetic: more than eight steps of the usual coefficients are only for matrices of full rank.  Singular values of X must stay below 8 (they do for the usual
- * coefficients).  An
- * update of zeros gives zeros (NaN if eps is 0); one that holds an inf or a NaN gives NaN.
+ * arithmetic: more than eight steps of the usual coefficients are only for matrices of full rank.  A, B and X are held in 16 bits: singular
+ * values s of X must stay below 8 and |b s^2 + c s^4| below 64 in every step (s below 2.6 for the usual coefficients, which keep it
+ * below 1.3), else the update is inf or NaN; ds_orth_create does not check the coefficients for it.  An update of zeros gives zeros (NaN if eps is 0); one that holds an inf or a NaN gives NaN.
  *
  * ds_orth_create: with workspace == NULL fills *workspace_bytes and returns DS_NEED_BUFFERS; else makes a handle on that
  * workspace (256-byte aligned; it need not be cleared).  Host-only.  One handle on one stream at a time.

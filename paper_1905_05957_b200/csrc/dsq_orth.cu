@@ -6,7 +6,7 @@
 //
 // Numbers.  Products run on 16-bit floats with 11 bits of significand (same rate as the 8-bit-significand format, whose error
 // would be eight times as large) and add up in 32 bits.  The entries of X, A and B are bounded (|X| <= 1.3, |A| <= 1.5, |B| <= 8 for
-// the usual coefficients), so they are held times 2^10, which keeps small entries out of the subnormals.  Two things
+// the usual coefficients), so they are held times 2^10, which keeps small entries out of the subnormals; entries from 64 on are inf.  Three things
 // would otherwise lose bits that later steps multiply by a = 3.4 each:
 //  - X is carried in two halves (hi + lo, 22 bits), of which aX takes both.  With hi alone, updates whose energy sits in few
 //    directions came out 0.6 % to 2 % off.

@@ -104,3 +104,18 @@ def test_fewer_steps(steps):
                                                  (48, 48, 8, 2, 1e-4), (1024, 16, 300, 1, 0)])
 def test_small_matrices_of_low_rank(m, n, live, rank, noise):
     _check(_few_rows(m, n, live, rank, noise, m + n), TOL_SMALL)
+
+
+@pytest.mark.parametrize("m,n,tol", [(128, 300, TOL), (48, 100, TOL_SMALL)])
+@pytest.mark.parametrize("coef,steps,largest,b_largest", [((1.98, 0.0, 0.0), 4, 7.77, 0), ((1.72, 0.0, 1.0), 2, 2.73, 55)])
+def test_coefficients_near_the_documented_limits(m, n, tol, coef, steps, largest, b_largest):
+    """Equal entries: the one singular value is 1 at first.  The first coefficients take it to 7.76 before the last step (A up to 60.3), the
+    second to 2.72, where B is 54.7; results are finite and as exact as elsewhere."""
+    s = 1.0
+    for _ in range(steps - 1):
+        s *= coef[0] + coef[1] * s ** 2 + coef[2] * s ** 4
+    assert 0.99 * largest < s < largest < 8 and coef[1] * s ** 2 + coef[2] * s ** 4 <= b_largest < 64
+    u = torch.ones(m, n, device="cuda")
+    got = OrthUpdate(m, n, steps=steps, coef=coef).update(u, out_dtype=F32)[0]
+    assert torch.isfinite(got).all()
+    assert _off(got, _exact(u, steps, coef)) < tol
