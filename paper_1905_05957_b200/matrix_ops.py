@@ -319,6 +319,7 @@ class OrthUpdate:
         self.workspace = torch.empty(size.value, dtype=torch.uint8, device=device)
         self.device = self.workspace.device
         self.dev_status = torch.zeros(4, dtype=torch.int32, device=device)
+        self._last_stream = _raw_stream(self.device.index)     # where the allocator takes both to be in use
         torch.cuda.synchronize(self.device)      # cleared before a product on any stream may set it
         h = C.c_void_p()
         _check(self.lib.ds_orth_create(C.byref(self.cfg), self.workspace.data_ptr(), C.byref(size), self.dev_status.data_ptr(),
@@ -340,7 +341,8 @@ class OrthUpdate:
                stream=None) -> torch.Tensor | None:
         """One update.  momentum (float32) is advanced in place.  Returns the orthogonalised update [batch, rows, cols] in
         `out` or a new tensor of out_dtype (None: not wanted).  x (float32): also x = x (1 - gamma decay) - gamma scale update.
-        One plan works on one stream at a time: its workspace holds the matrices between the products."""
+        One plan works on one stream at a time: its workspace holds the matrices between the products.  Tensors that the caller
+        allocated on another stream follow PyTorch's rules (record_stream), the plan's own memory needs nothing."""
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.update(g, momentum, out, out_dtype, x, gamma, decay)
@@ -355,9 +357,14 @@ class OrthUpdate:
         gp = self._span(g, "g", tuple(_DTYPES))
         mp = self._span(momentum, "momentum", (torch.float32,))
         xp = self._span(x, "x", (torch.float32,))
+        raw = _raw_stream(self.device.index)
+        if raw != self._last_stream:             # a plan that is dropped before this stream has run keeps its memory until it has
+            used = torch.cuda.current_stream(self.device)
+            self.workspace.record_stream(used)
+            self.dev_status.record_stream(used)
+            self._last_stream = raw
         _check(self.lib.ds_orth_update(self.handle, gp, _DTYPES[g.dtype], mp, None if out is None else out.data_ptr(),
-                                       DS_F32 if out is None else _DTYPES[out.dtype], xp, gamma, decay,
-                                       _raw_stream(self.device.index)), "ds_orth_update")
+                                       DS_F32 if out is None else _DTYPES[out.dtype], xp, gamma, decay, raw), "ds_orth_update")
         return out
 
     def timed_out(self) -> bool:
