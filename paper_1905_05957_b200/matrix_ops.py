@@ -91,7 +91,7 @@ class Int8Matrix:
     """Codes [rows, cols] (int8) with one float32 scale per row: row r stands for codes[r] * scale[r].
     Rows must start on 16-byte boundaries (int8_quantize gives such; pack() copies into such)."""
 
-    __slots__ = ("rows", "cols", "ld", "device", "codes_ptr", "scale_ptr", "_codes", "_scale")
+    __slots__ = ("rows", "cols", "ld", "device", "codes_ptr", "scale_ptr", "_codes", "_scale", "stream")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor):
         if codes.dtype is not torch.int8 or not codes.is_cuda:
@@ -103,16 +103,25 @@ class Int8Matrix:
         self.rows, self.cols, self.device = r, c, codes.device
         self.ld = ld if r > 1 else (c + 15) // 16 * 16
         self._codes, self._scale = codes, scale
+        self.stream = _raw_stream(codes.device.index)      # the last one on which the allocator takes the memory to be in use
         self.codes_ptr, self.scale_ptr = codes.data_ptr(), _vector(scale, r, "scale", self.device)
 
     @classmethod
-    def _within(cls, buf: torch.Tensor, base: int, at: int, scale_at: int, rows: int, cols: int, ld: int, device) -> "Int8Matrix":
+    def _within(cls, buf: torch.Tensor, base: int, at: int, scale_at: int, rows: int, cols: int, ld: int, device, stream: int) -> "Int8Matrix":
         """Codes and scales at two offsets of one byte buffer whose address is `base`; views are made when asked for."""
         m = cls.__new__(cls)
         m.rows, m.cols, m.ld, m.device = rows, cols, ld, device
-        m.codes_ptr, m.scale_ptr = base + at, base + scale_at
+        m.codes_ptr, m.scale_ptr, m.stream = base + at, base + scale_at, stream
         m._codes, m._scale = (buf, at), (buf, scale_at)
         return m
+
+    def used_on(self, stream: int):
+        """Tells the allocator of the current stream, on which the matrix is about to be used: dropped before that has run, its memory is
+        kept until it has."""
+        current = torch.cuda.current_stream(self.device)
+        for t in (self._codes, self._scale):
+            (t[0] if isinstance(t, tuple) else t).record_stream(current)
+        self.stream = stream
 
     @property
     def codes(self) -> torch.Tensor:
@@ -169,16 +178,17 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
     ws = _quantize_ws(r, c, 1 if col_sum else 0) if cols or col_sum else 0
     buf = _empty(at_ws + ws + 16, dtype=torch.uint8, device=device)
     base = buf.data_ptr()
+    raw = _raw_stream(device.index)
     rc = _call(_quantize_at, x.data_ptr(), dt, r, c, ld, base if rows else 0, ldr, base + at_rs if rows else 0,
                base + at_c if cols else 0, ldc, base + at_cs if cols else 0, base + at_sum if col_sum else 0,
-               base + at_ws if ws else 0, ws, _raw_stream(device.index))
+               base + at_ws if ws else 0, ws, raw)
     if rc:
         _check(rc, "ds_i8_quantize")
     got = []
     if rows:
-        got.append(Int8Matrix._within(buf, base, 0, at_rs, r, c, ldr, device))
+        got.append(Int8Matrix._within(buf, base, 0, at_rs, r, c, ldr, device, raw))
     if cols:
-        got.append(Int8Matrix._within(buf, base, at_c, at_cs, c, r, ldc, device))
+        got.append(Int8Matrix._within(buf, base, at_c, at_cs, c, r, ldc, device, raw))
     if col_sum:
         got.append(buf[at_sum:at_sum + 4 * c].view(torch.float32))
     return got[0] if len(got) == 1 else tuple(got)
@@ -216,8 +226,13 @@ def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, 
     else:
         ldo = _out(out, m, n, device)
     index = device.index
+    raw = _raw_stream(index)
+    if a.stream != raw:
+        a.used_on(raw)
+    if b.stream != raw:
+        b.used_on(raw)
     rc = _call(_matmul_at, a.codes_ptr, a.ld, a.scale_ptr, b.codes_ptr, b.ld, b.scale_ptr, bp, m, n, k, out.data_ptr(),
-               _dtype(out.dtype, "out"), ldo, _dev_status(index), _raw_stream(index))
+               _dtype(out.dtype, "out"), ldo, _dev_status(index), raw)
     if rc:
         _check(rc, "ds_i8_matmul")
     return out
@@ -251,8 +266,11 @@ def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None
     size = _linear_ws(m, k, n)
     ws = _empty(size, dtype=torch.uint8, device=device) if size else None
     index = device.index
+    raw = _raw_stream(index)
+    if w.stream != raw:
+        w.used_on(raw)
     rc = _call(_linear_at, x.data_ptr(), dt, m, k, ld, w.codes_ptr, w.ld, w.scale_ptr, bp, n, out.data_ptr(), odt, ldo,
-               ws.data_ptr() if size else None, size, _dev_status(index), _raw_stream(index))
+               ws.data_ptr() if size else None, size, _dev_status(index), raw)
     if rc:
         _check(rc, "ds_i8_linear")
     return out

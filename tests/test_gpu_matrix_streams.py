@@ -3,7 +3,7 @@ not be handed out again until it has."""
 import pytest
 import torch
 
-from paper_1905_05957_b200 import OrthUpdate
+from paper_1905_05957_b200 import Int8Linear, Int8Matrix, OrthUpdate, int8_linear, int8_matmul, int8_quantize
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +48,46 @@ def test_a_plan_dropped_before_its_stream_has_run(m, n):
     _overwrite(sizes)
     torch.cuda.synchronize()
     assert torch.equal(out, want[0]) and torch.equal(buf, want_buf) and torch.equal(x, want_x)
+
+
+def _weights(n, k, seed):
+    return torch.randn(n, k, device="cuda", generator=_gen(seed))
+
+
+@pytest.mark.parametrize("m", [1, 40, 300])
+@pytest.mark.parametrize("made", ["quantised", "packed"])
+def test_codes_dropped_before_their_stream_has_run(m, made):
+    """Weights and tokens quantised on the current stream, used on another and dropped."""
+    x, w = _weights(m, 512, 1), _weights(256, 512, 2)
+
+    def make(v):
+        q = int8_quantize(v)
+        return Int8Matrix.pack(q.codes, q.scale) if made == "packed" else q
+
+    want = int8_linear(x, make(w)), int8_matmul(make(x), make(w))
+    y, z = torch.empty_like(want[0]), torch.empty_like(want[1])
+    torch.cuda.synchronize()
+    a, b, c = make(x), make(w), make(w)
+    s = _behind()
+    int8_linear(x, b, out=y, stream=s)
+    int8_matmul(a, c, out=z, stream=s)
+    del a, b, c
+    _overwrite([256 * 512 + 4 * 256 + 16, 256 * 512, 4 * 256, m * 512 + 4 * 304 + 16, m * 512, 4 * m, 16])
+    torch.cuda.synchronize()
+    assert torch.equal(y, want[0]) and torch.equal(z, want[1])
+
+
+def test_a_layer_dropped_before_its_stream_has_run():
+    x, w, dy = _weights(300, 512, 1), _weights(256, 512, 2), _weights(300, 256, 3)
+    layer = Int8Linear(w)
+    layer.forward(x, training=True)
+    want = layer.backward(dy)[1]
+    dw = torch.empty_like(want)
+    layer.forward(x, training=True)      # codes of x and W on the current stream, the backward pass on another
+    torch.cuda.synchronize()
+    s = _behind()
+    layer.backward(dy, dw=dw, stream=s)
+    del layer
+    _overwrite([300 * 512 + 512 * 304 + 4 * 816 + 16, 256 * 512 * 2 + 4 * 768 + 16, 300 * 512, 256 * 512])
+    torch.cuda.synchronize()
+    assert torch.equal(dw, want)
