@@ -1076,7 +1076,8 @@ inline MmaPlan plan_mma(const MmaShape& s, bool b_sym = false) {   // b_sym: a t
       const double t = split_time(s, sms, bn, parts);
       if (t < least) least = t, p = MmaPlan{false, bn, parts};
     }
-  if (pair_time(s, pair_count()) < least) p = MmaPlan{true, 256, 1};
+  const int pairs = pair_count();      // 0: no device that could be asked; the launch then says what is wrong
+  if (pairs > 0 && pair_time(s, pairs) < least) p = MmaPlan{true, 256, 1};
   return p;
 }
 

@@ -1,6 +1,9 @@
 """Host-side checks of the matrix operators' C ABI that need no GPU: struct sizes, workspace sizes, and refusals, which come
 before anything is launched."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -109,3 +112,27 @@ def test_orth_plans(lib):
         bad = b.ds_orth_config.from_buffer_copy(cfg)
         setattr(bad, field, value)
         assert lib.ds_orth_create(C.byref(bad), None, C.byref(size), None, None) == b.DS_ERR_INVALID_ARG, field
+
+
+def test_a_host_without_a_device_gets_a_status():
+    """In a process of its own that sees no device: calls of every form end with the CUDA error as their status."""
+    code = """
+import ctypes as C
+from paper_1905_05957_b200 import binding as b
+lib, P = b.load_library(), 0x10000
+for m, n, k in ((4, 64, 64), (40, 64, 64), (100, 64, 64), (100, 64, 0), (5000, 5000, 256)):
+    print(lib.ds_i8_matmul(P, 256, P, P, 256, P, None, m, n, k, P, 0, n, P, None))
+for rows in (2, 100):
+    print(lib.ds_i8_linear(P, 0, rows, 64, 64, P, 64, P, None, 64, P, 0, 64, P, 1 << 20, P, None))
+print(lib.ds_i8_quantize(P, 0, 8, 64, 64, P, 64, P, P, 16, P, None, P, 1 << 20, None))
+for m, n in ((48, 100), (300, 500), (4096, 4096)):
+    cfg = b.ds_orth_config(m, n, 1, 5, 3.4445, -4.775, 2.0315, 0.95, 1e-7, 1.0, 1, 0, 0)
+    size, h = C.c_size_t(0), C.c_void_p()
+    assert lib.ds_orth_create(C.byref(cfg), None, C.byref(size), None, None) == b.DS_NEED_BUFFERS
+    assert lib.ds_orth_create(C.byref(cfg), P, C.byref(size), P, C.byref(h)) == b.DS_OK
+    print(lib.ds_orth_update(h, P, 0, None, P, 0, None, 0.0, 0.0, None))
+"""
+    env = dict(os.environ, CUDA_VISIBLE_DEVICES="", PYTHONPATH=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    got = subprocess.run([sys.executable, "-c", code], env=env, capture_output=True, text=True)
+    assert got.returncode == 0, got.stderr[-500:]
+    assert [int(v) for v in got.stdout.split()] == [b.DS_ERR_CUDA] * 11
