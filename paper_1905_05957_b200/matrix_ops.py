@@ -70,9 +70,13 @@ def _vector(v: torch.Tensor | None, n: int, what: str, device) -> int | None:
 _status: dict = {}     # device index -> (word in which products report waits that ran out, its address)
 
 
-def _dev_status(index: int) -> int:
+def _dev_status(index: int) -> int | None:
+    """The address of the device's status word, made when codes or products are first asked for.  None while a graph is captured on a
+    device that has none yet: it cannot be made then, and the captured products report nothing."""
     entry = _status.get(index)
     if entry is None:
+        if torch.cuda.is_current_stream_capturing():
+            return None
         word = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", index))
         torch.cuda.synchronize(index)          # cleared before any stream's product may set it
         entry = _status[index] = (word, word.data_ptr())
@@ -80,7 +84,8 @@ def _dev_status(index: int) -> int:
 
 
 def device_status(device: str | torch.device = "cuda") -> int:
-    """DS_DEV_* flags of the matrix operators on a device; 0 unless one of them failed.  Waits for the device."""
+    """DS_DEV_* flags of the matrix operators on a device; 0 unless one of them failed.  (Products captured into a graph before any
+    call of these operators on the device do not report.)  Waits for the device."""
     device = torch.device(device)
     index = torch.cuda.current_device() if device.index is None else device.index
     _dev_status(index)
@@ -178,6 +183,8 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
     ws = _quantize_ws(r, c, 1 if col_sum else 0) if cols or col_sum else 0
     buf = _empty(at_ws + ws + 16, dtype=torch.uint8, device=device)
     base = buf.data_ptr()
+    if device.index not in _status:
+        _dev_status(device.index)
     raw = _raw_stream(device.index)
     rc = _call(_quantize_at, x.data_ptr(), dt, r, c, ld, base if rows else 0, ldr, base + at_rs if rows else 0,
                base + at_c if cols else 0, ldc, base + at_cs if cols else 0, base + at_sum if col_sum else 0,
