@@ -105,11 +105,12 @@ class Int8Matrix:
         ld, step = codes.stride()
         if c > 1 and step != 1:
             raise ValueError("codes: a row-major int8 matrix expected")
-        self.rows, self.cols, self.device = r, c, codes.device
+        device = codes.device
+        self.rows, self.cols, self.device = r, c, device
         self.ld = ld if r > 1 else (c + 15) // 16 * 16
         self._codes, self._scale = codes, scale
-        self.stream = _raw_stream(codes.device.index)      # the last one on which the allocator takes the memory to be in use
-        self.codes_ptr, self.scale_ptr = codes.data_ptr(), _vector(scale, r, "scale", self.device)
+        self.stream = _raw_stream(device.index)      # the last one on which the allocator takes the memory to be in use
+        self.codes_ptr, self.scale_ptr = codes.data_ptr(), _vector(scale, r, "scale", device)
 
     @classmethod
     def _within(cls, buf: torch.Tensor, base: int, at: int, scale_at: int, rows: int, cols: int, ld: int, device, stream: int) -> "Int8Matrix":
@@ -170,7 +171,8 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
         _load()
     dt = _dtype(x.dtype, "x")
     x, r, c, ld, device = _matrix(x, "x")
-    if device.index != _current():           # the library works on the current device
+    index = device.index
+    if index != _current():                  # the library works on the current device
         with torch.cuda.device(device):
             return int8_quantize(x, rows, cols, col_sum)
     # one buffer: codes, scales, sums, and at its end what only the call itself uses
@@ -183,9 +185,9 @@ def int8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, col_su
     ws = _quantize_ws(r, c, 1 if col_sum else 0) if cols or col_sum else 0
     buf = _empty(at_ws + ws + 16, dtype=torch.uint8, device=device)
     base = buf.data_ptr()
-    if device.index not in _status:
-        _dev_status(device.index)
-    raw = _raw_stream(device.index)
+    if index not in _status:
+        _dev_status(index)
+    raw = _raw_stream(index)
     rc = _call(_quantize_at, x.data_ptr(), dt, r, c, ld, base if rows else 0, ldr, base + at_rs if rows else 0,
                base + at_c if cols else 0, ldc, base + at_cs if cols else 0, base + at_sum if col_sum else 0,
                base + at_ws if ws else 0, ws, raw)
@@ -224,7 +226,8 @@ def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, 
         raise ValueError(f"lengths differ: {k} and {b.cols}")
     if b.device != device:
         raise ValueError(f"matrices on {device} and {b.device}")
-    if device.index != _current():
+    index = device.index
+    if index != _current():
         with torch.cuda.device(device):
             return int8_matmul(a, b, bias, out_dtype, out)
     bp = None if bias is None else _vector(bias, n, "bias", device)
@@ -232,7 +235,6 @@ def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, 
         out, ldo = _empty((m, n), dtype=out_dtype, device=device), n
     else:
         ldo = _out(out, m, n, device)
-    index = device.index
     raw = _raw_stream(index)
     if a.stream != raw:
         a.used_on(raw)
@@ -260,7 +262,8 @@ def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None
         raise ValueError(f"x has {k} columns, the weights {w.cols}")
     if w.device != device:
         raise ValueError(f"x on {device}, the weights on {w.device}")
-    if device.index != _current():
+    index = device.index
+    if index != _current():
         with torch.cuda.device(device):
             return int8_linear(x, w, bias, out_dtype, out)
     bp = None if bias is None else _vector(bias, n, "bias", device)
@@ -272,7 +275,6 @@ def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None
         out, ldo, odt = _empty((m, n), dtype=out_dtype, device=device), n, _dtype(out_dtype, "out")
     size = _linear_ws(m, k, n)
     ws = _empty(size, dtype=torch.uint8, device=device) if size else None
-    index = device.index
     raw = _raw_stream(index)
     if w.stream != raw:
         w.used_on(raw)
