@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(256) k_i8_rows(const T* x, uint64_t ld, uint32
 #pragma unroll
     for (int k = 0; k < kKeep; ++k) {
       const uint32_t v = threadIdx.x + k * blockDim.x;
-      keep[k].raw = v < nv ? __ldg(reinterpret_cast<const uint4*>(row) + v) : make_uint4(0, 0, 0, 0);
+      keep[k].raw = v < nv ? ld_plain(reinterpret_cast<const uint4*>(row) + v) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int k = 0; k < kKeep; ++k)
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(256) k_i8_amax(const T* x, uint64_t ld, uint32
   Vec<T> v[kRows];
   if (VEC && c0 + 32 * N <= cols && r0 + kAmaxRows <= rows) {   // inside
 #pragma unroll
-    for (int k = 0; k < kRows; ++k) v[k].raw = __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)(r0 + warp + 8 * k) * ld + col(0)));
+    for (int k = 0; k < kRows; ++k) v[k].raw = ld_plain(reinterpret_cast<const uint4*>(x + (uint64_t)(r0 + warp + 8 * k) * ld + col(0)));
   } else {
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[i][j].raw = __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)(r + i) * ld + c) + j);
+        for (int j = 0; j < V; ++j) v[i][j].raw = ld_plain(reinterpret_cast<const uint4*>(x + (uint64_t)(r + i) * ld + c) + j);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(512)
   __shared__ uint32_t tops[kStep][64 + 1], turned[64][17];
   __shared__ float part[kStep][64 + 1];
   const uint32_t r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tid = threadIdx.x & 255, warp = tid >> 5, lane = tid & 31;
-  auto vec_at = [&](uint32_t r, uint32_t c) { return __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)r * ld + c)); };   // c < cols, a multiple of N
+  auto vec_at = [&](uint32_t r, uint32_t c) { return ld_plain(reinterpret_cast<const uint4*>(x + (uint64_t)r * ld + c)); };   // c < cols, a multiple of N
   const uint32_t lc = tid % 16 * 4, lr = tid / 16 * 4, c = c0 + lc;        // 4 x 4 blocks of the tile
   float f[4][4];
   if (threadIdx.x < 256) {
@@ -380,10 +380,10 @@ __global__ void __launch_bounds__(512)
       const bool in = r0 + lr + i < rows && c < cols;     // cols is a multiple of 4
       const T* p = x + (uint64_t)(r0 + lr + i) * ld + c;
       if constexpr (sizeof(T) == 4) {
-        const float4 v = in ? __ldg(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 v = in ? ld_plain(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
         f[i][0] = v.x, f[i][1] = v.y, f[i][2] = v.z, f[i][3] = v.w;
       } else {
-        const uint2 v = in ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
+        const uint2 v = in ? ld_plain(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[i][j] = to_f32(reinterpret_cast<const T*>(&v)[j]);
       }
@@ -499,32 +499,35 @@ struct EpiScale {
   T* out;
   uint64_t ld;
   uint32_t m, n;
-  __device__ __forceinline__ Pre load(uint32_t row, uint32_t, uint32_t) const { return {row < m ? __ldg(sa + row) : 0.f}; }
+  __device__ __forceinline__ Pre load(uint32_t row, uint32_t, uint32_t) const { return {row < m ? ld_plain(sa + row) : 0.f}; }
   __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t) const {
     if (row >= m) return;
     T* o = out + row * ld + col0;
     if (col0 + 32 <= n) {
+      uint32_t piece[sizeof(T)][8];      // all of them before the first store: loads are not moved ahead of stores
 #pragma unroll
-      for (int i = 0; i < 32; i += 32 / sizeof(T)) {
-        uint32_t piece[8];
-#pragma unroll
-        for (int j = 0; j < 32 / (int)sizeof(T); j += 4) {
-          const float4 s = __ldg(reinterpret_cast<const float4*>(sb + col0 + i + j));
-          float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (bias) c = __ldg(reinterpret_cast<const float4*>(bias + col0 + i + j));
-          const float v0 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j], p.s), s.x), c.x);
-          const float v1 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j + 1], p.s), s.y), c.y);
-          const float v2 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j + 2], p.s), s.z), c.z);
-          const float v3 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + j + 3], p.s), s.w), c.w);
-          pack4f<T>(piece + j * sizeof(T) / 4, v0, v1, v2, v3);
-        }
-        st_b32(o + i, piece);
+      for (int i = 0; i < 32; i += 4) {
+        const float4 s = ld_plain(reinterpret_cast<const float4*>(sb + col0 + i));
+        float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (bias) c = ld_plain(reinterpret_cast<const float4*>(bias + col0 + i));
+        const float v0 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i], p.s), s.x), c.x);
+        const float v1 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + 1], p.s), s.y), c.y);
+        const float v2 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + 2], p.s), s.z), c.z);
+        const float v3 = __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[i + 3], p.s), s.w), c.w);
+        pack4f<T>(&piece[i * sizeof(T) / 32][i * sizeof(T) / 4 % 8], v0, v1, v2, v3);
       }
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T); ++i) st_b32(o + 32 / sizeof(T) * i, piece[i]);
     } else {
+      float s[32], c[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        s[j] = col0 + j < n ? ld_plain(sb + col0 + j) : 0.f;
+        c[j] = bias && col0 + j < n ? ld_plain(bias + col0 + j) : 0.f;
+      }
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        if (col0 + j < n)
-          store1(o + j, __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[j], p.s), __ldg(sb + col0 + j)), bias ? __ldg(bias + col0 + j) : 0.f));
+        if (col0 + j < n) store1(o + j, __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[j], p.s), s[j]), c[j]));
     }
   }
 };
@@ -535,21 +538,23 @@ template <class T>
 struct EpiScaleTurned {
   static constexpr int kIn = 0, kOut = 0;
   struct Pre {
-    float s, c;
+    float s, c, token;             // of this lane's channel, and the scale of token col0 + lane
   };
   const float *sa, *sb, *bias;   // of tokens, of channels
   T* out;
   uint64_t ld;
   uint32_t m, n;                 // channels, tokens
-  __device__ __forceinline__ Pre load(uint32_t row, uint32_t, uint32_t) const {
-    return row < m ? Pre{__ldg(sb + row), bias ? __ldg(bias + row) : 0.f} : Pre{0.f, 0.f};
+  __device__ __forceinline__ Pre load(uint32_t row, uint32_t col0, uint32_t) const {
+    const uint32_t token = col0 + (row & 31);
+    return {row < m ? ld_plain(sb + row) : 0.f, row < m && bias ? ld_plain(bias + row) : 0.f, token < n ? ld_plain(sa + token) : 0.f};
   }
   __device__ __forceinline__ void apply(const Pre& p, const uint32_t (&acc)[32], uint32_t row, uint32_t col0, uint32_t) const {
-    if (row >= m) return;
     T* o = out + col0 * ld + row;
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (col0 + j < n) store1(o + j * ld, __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[j], __ldg(sa + col0 + j)), p.s), p.c));
+    for (int j = 0; j < 32; ++j) {
+      const float s = __shfl_sync(0xFFFFFFFFu, p.token, j);
+      if (row < m && col0 + j < n) store1(o + j * ld, __fadd_rn(__fmul_rn(__fmul_rn((float)(int)acc[j], s), p.s), p.c));
+    }
   }
 };
 
@@ -592,7 +597,7 @@ struct FewParams {
 // 16 codes from k0 on; behind the end of a row nothing is read and zeros stand.  (The end is rare: kept small, since the
 // loops' length in instructions counts where a warp lives for a few microseconds.)
 __device__ __forceinline__ uint4 load_codes16(const int8_t* row, uint32_t k0, uint32_t k) {
-  if (k0 + 16 <= k) return __ldg(reinterpret_cast<const uint4*>(row + k0));
+  if (k0 + 16 <= k) return ld_plain(reinterpret_cast<const uint4*>(row + k0));
   unsigned long long v[2] = {0, 0};
 #pragma unroll
   for (int h = 0; h < 2; ++h)
@@ -615,7 +620,7 @@ __device__ __forceinline__ uint4 encode16(const T* row, uint32_t k0, uint32_t k,
 #pragma unroll
     for (int i = 0; i < 16 / Vec<T>::kN; ++i) {
       Vec<T> v;
-      v.raw = __ldg(reinterpret_cast<const uint4*>(row + k0) + i);
+      v.raw = ld_plain(reinterpret_cast<const uint4*>(row + k0) + i);
 #pragma unroll
       for (int j = 0; j < Vec<T>::kN / 4; ++j)
         w[i * (Vec<T>::kN / 4) + j] =
@@ -667,10 +672,10 @@ __global__ void __launch_bounds__(256, 2) k_i8_few(const FewParams p) {
     if (c >= end) return;
     const uint32_t k0 = c * 64 + t * 16;
 #pragma unroll
-    for (int i = 0; i < 2 * RB; ++i) to[i] = __ldg(reinterpret_cast<const uint4*>(wrow[i] + k0));
+    for (int i = 0; i < 2 * RB; ++i) to[i] = ld_plain(reinterpret_cast<const uint4*>(wrow[i] + k0));
     if constexpr (kCodes) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) xt[j] = __ldg(reinterpret_cast<const uint4*>(xrow[j] + k0));
+      for (int j = 0; j < NT; ++j) xt[j] = ld_plain(reinterpret_cast<const uint4*>(xrow[j] + k0));
     }
   };
 #pragma unroll
@@ -692,7 +697,7 @@ __global__ void __launch_bounds__(256, 2) k_i8_few(const FewParams p) {
 #pragma unroll 4
         for (uint32_t v = at; v < nv; v += lanes) {
           Vec<X> r;
-          r.raw = __ldg(reinterpret_cast<const uint4*>(row) + v);
+          r.raw = ld_plain(reinterpret_cast<const uint4*>(row) + v);
 #pragma unroll
           for (int i = 0; i < N; ++i) top = max(top, mag_bits(r.at(i)));
         }
@@ -785,7 +790,7 @@ __global__ void __launch_bounds__(256, 2) k_i8_few(const FewParams p) {
     for (int q = 0; q < 8; ++q) s += part[q][r][token];
     if (row < p.n)
       store1(static_cast<O*>(p.out) + token * p.ldo + row,
-             __fadd_rn(__fmul_rn(__fmul_rn((float)s, scale[token]), __ldg(p.sw + row)), p.bias ? __ldg(p.bias + row) : 0.f));
+             __fadd_rn(__fmul_rn(__fmul_rn((float)s, scale[token]), ld_plain(p.sw + row)), p.bias ? ld_plain(p.bias + row) : 0.f));
   }
 }
 

@@ -139,8 +139,8 @@ __global__ void __launch_bounds__(kThreads) k_orth_split(const Momentum mo, uint
   // the norm's parts are asked for before the tile, and added in the same order in every CTA
   static_assert(kNormCtas == 2 * kThreads, "two parts a thread");
   double sum = 0, second = 0;
-  if (threadIdx.x < parts) sum = __ldg(partial + (uint64_t)b * kNormCtas + threadIdx.x);
-  if (threadIdx.x + kThreads < parts) second = __ldg(partial + (uint64_t)b * kNormCtas + threadIdx.x + kThreads);
+  if (threadIdx.x < parts) sum = ld_plain(partial + (uint64_t)b * kNormCtas + threadIdx.x);
+  if (threadIdx.x + kThreads < parts) second = ld_plain(partial + (uint64_t)b * kNormCtas + threadIdx.x + kThreads);
   float gv[4][4], bv[4][4], v[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -273,7 +273,7 @@ struct EpiPoly {   // B = b A + c A A, the accumulator being O O
     float d = 0.f;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const float4 t = __ldg(dj + q);
+      const float4 t = ld_plain(dj + q);
       const float2 o0 = v.two(2 * q), o1 = v.two(2 * q + 1);
       const float dd[4] = {t.x, t.y, t.z, t.w}, o[4] = {o0.x, o0.y, o1.x, o1.y};
       float e[4];
