@@ -170,12 +170,12 @@ __global__ void __launch_bounds__(kThreads) k_orth_split(const Momentum mo, uint
   sum = 0;
 #pragma unroll
   for (int i = 0; i < kThreads / 32; ++i) sum += warp_sum[i];
-  const float f = kUp / ((float)sqrt(sum) + eps);
+  const NormFactor f(sum, eps);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t lr = threadIdx.x / 16 + 16 * i, lc = threadIdx.x % 16 * 4, r = r0 + lr, c = c0 + lc;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[i][j] = __fmul_rn(buf ? mo.direction(gv[i][j], bv[i][j]) : gv[i][j], f);
+    for (int j = 0; j < 4; ++j) v[i][j] = f(buf ? mo.direction(gv[i][j], bv[i][j]) : gv[i][j]);
     if constexpr (TALL) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) tile[lr][lc + j] = v[i][j];

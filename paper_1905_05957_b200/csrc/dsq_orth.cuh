@@ -25,6 +25,25 @@ __device__ __forceinline__ void load4(float (&o)[4], const T16* p) {
   for (int i = 0; i < 4; ++i) o[i] = to_f32(e[i]);
 }
 
+// X kUp = (u first) then.  The sum of squares is in 64 bits; where the norm or kUp / norm would leave 32 bits, u is brought into
+// range by a power of two.  (A norm of 0 without eps, or one that is not a number, makes X NaN.)
+struct NormFactor {
+  float first, then;
+  __device__ __forceinline__ NormFactor(double sum, float eps) : then(1.f) {
+    const double root = sqrt(sum);
+    const float norm = (float)root + eps;
+    first = kUp / norm;
+    if (!(norm > 1e-30f && norm < 1e30f)) {
+      const double wide = root + (double)eps;
+      if (wide > 0 && wide < 1e60) {
+        first = wide < 1 ? 0x1p100f : 0x1p-100f;
+        then = (float)((double)kUp / (wide * (double)first));
+      }
+    }
+  }
+  __device__ __forceinline__ float operator()(float u) const { return __fmul_rn(__fmul_rn(u, first), then); }
+};
+
 struct Momentum {
   const void* g;
   float* buf;        // NULL: u = g

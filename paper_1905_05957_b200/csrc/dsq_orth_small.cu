@@ -146,9 +146,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_orth_small(const SmallArgs
   cluster_sync();
   double norm2 = 0;
   for (uint32_t i = 0; i < ctas; ++i) norm2 += sums[i];
-  const float scale = kUp / ((float)sqrt(norm2) + p.eps);
+  const NormFactor scale(norm2, p.eps);
   visit(load, [&](int q, uint64_t, uint32_t at_x) {
-    const float v = __fmul_rn(buf ? p.mo.direction(gv[q], bv[q]) : gv[q], scale);
+    const float v = scale(buf ? p.mo.direction(gv[q], bv[q]) : gv[q]);
     const __half h = __float2half_rn(v);
     *reinterpret_cast<__half*>(dyn + at_x) = h;
     *reinterpret_cast<__half*>(dyn + L.x_half() + at_x) = __float2half_rn(v - __half2float(h));

@@ -119,3 +119,15 @@ def test_coefficients_near_the_documented_limits(m, n, tol, coef, steps, largest
     got = OrthUpdate(m, n, steps=steps, coef=coef).update(u, out_dtype=F32)[0]
     assert torch.isfinite(got).all()
     assert _off(got, _exact(u, steps, coef)) < tol
+
+
+@pytest.mark.parametrize("m,n", [(80, 120), (300, 140), (40, 72)])
+@pytest.mark.parametrize("sigma,eps", [(1e-44, 0.0), (1e-41, 0.0), (1e-38, 0.0), (1e-36, 0.0), (2e36, 0.0), (5e37, 0.0), (5e37, 1e-7)])
+def test_norms_outside_32_bits(m, n, sigma, eps):
+    """1024 / norm passes the largest float below a norm of 3e-36, the norm itself from 3.4e38 on; the entries are finite and so is the
+    update.  Tolerance: that of ordinary inputs, 2e-3."""
+    g = torch.randn(m, n, device="cuda", generator=_gen(m)) + 0.2
+    g = g.clamp(-5, 5) * sigma
+    assert torch.isfinite(g).all() and (g != 0).any()
+    got = OrthUpdate(m, n, eps=eps).update(g, out_dtype=F32)[0]
+    assert _off(got, _exact(g, eps=eps)) < 2e-3
