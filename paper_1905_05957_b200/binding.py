@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import importlib.util
 import os
+import sysconfig
 
 import torch
 
@@ -15,6 +16,7 @@ from .workloads import Q, Workload
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "csrc", "libdsq.so")
+CALL_LIB = os.path.join(_HERE, "csrc", "dsq_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 DS_OK, DS_NEED_BUFFERS = 0, 1
 DS_ERR_INVALID_ARG, DS_ERR_ALIGN, DS_ERR_BUFFER_TOO_SMALL = -1, -2, -3
@@ -123,18 +125,20 @@ _call = None
 
 def fast_call():
     """(call, addresses): call(addresses[name], *integers) calls a function of the ABI whose arguments are all pointers or
-    integers, without ctypes (csrc/dsq_call.c)."""
+    integers, without ctypes (csrc/dsq_call.c); through ctypes where that extension was not built for this interpreter."""
     global _call
     if _call is None:
         lib = load_library()
-        path = os.path.join(_HERE, "csrc", "dsq_call.so")
-        spec = importlib.util.spec_from_file_location("dsq_call", path)
-        if not os.path.exists(path) or spec is None:
-            raise RuntimeError(f"{path} is missing: run `python -m paper_1905_05957_b200.build`")
-        module = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(module)
-        _call = module.call, {name: C.cast(getattr(lib, name), C.c_void_p).value
-                              for name in ("ds_i8_quantize", "ds_i8_matmul", "ds_i8_linear")}
+        functions = [getattr(lib, name) for name in ("ds_i8_quantize", "ds_i8_matmul", "ds_i8_linear")]
+        address = {f.__name__: C.cast(f, C.c_void_p).value for f in functions}
+        if os.path.exists(CALL_LIB):
+            spec = importlib.util.spec_from_file_location("dsq_call", CALL_LIB)
+            module = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(module)
+            _call = module.call, address
+        else:
+            at = {address[f.__name__]: f for f in functions}
+            _call = (lambda where, *args: at[where](*args)), address
     return _call
 
 

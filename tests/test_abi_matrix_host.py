@@ -136,3 +136,25 @@ for m, n in ((48, 100), (300, 500), (4096, 4096)):
     got = subprocess.run([sys.executable, "-c", code], env=env, capture_output=True, text=True)
     assert got.returncode == 0, got.stderr[-500:]
     assert [int(v) for v in got.stdout.split()] == [b.DS_ERR_CUDA] * 11
+
+
+def test_a_host_without_a_c_compiler(lib, tmp_path, monkeypatch):
+    """The library is built without the extension, and the calls go through ctypes to the same functions."""
+    missing = str(tmp_path / "dsq_call.so")
+    monkeypatch.setattr(libbuild, "CALL_LIB", missing)
+    monkeypatch.setenv("CC", str(tmp_path / "no-such-compiler"))
+    assert libbuild.build_call() is None and libbuild.build() == libbuild.LIB
+    monkeypatch.setattr(libbuild.sysconfig, "get_paths", lambda: {"include": str(tmp_path)})      # no Python.h
+    monkeypatch.setenv("CC", "gcc")
+    assert libbuild.build_call() is None and libbuild.build() == libbuild.LIB and not os.path.exists(missing)
+    monkeypatch.setattr(b, "CALL_LIB", missing)
+    monkeypatch.setattr(b, "_call", None)
+    call, address = b.fast_call()
+    assert call(address["ds_i8_matmul"], P, 64, P, P, 64, P, None, 0, 5, 64, P, 1, 5, P, None) == b.DS_OK
+    assert call(address["ds_i8_matmul"], P, 64, P, P, 64, P, None, 4, 5, 64, P, 9, 5, P, None) == b.DS_ERR_INVALID_ARG
+    assert call(address["ds_i8_linear"], P, 0, 0, 64, 64, P, 64, P, None, 5, P, 0, 5, 0, 0, P, 0) == b.DS_OK
+    assert call(address["ds_i8_quantize"], P, 3, 8, 64, 64, P, 64, P, 0, 0, 0, 0, 0, 0, 0) == b.DS_ERR_INVALID_ARG
+
+
+def test_the_extension_names_its_interpreter():
+    assert os.path.basename(libbuild.CALL_LIB) == "dsq_call" + libbuild.sysconfig.get_config_var("EXT_SUFFIX")
