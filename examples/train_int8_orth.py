@@ -15,7 +15,7 @@ import sys
 import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
-from paper_1905_05957_b200 import DoubleSqueeze, Int8Linear, OrthUpdate, Q  # noqa: E402
+from paper_1905_05957_b200 import DoubleSqueeze, Int8Linear, OrthUpdate, Q, device_status  # noqa: E402
 
 
 def train(steps: int = 60, workers: int = 4, batch: int = 256, width: int = 192, rate: float = 0.03, seed: int = 0) -> list[float]:
@@ -70,6 +70,8 @@ def train(steps: int = 60, workers: int = 4, batch: int = 256, width: int = 192,
         losses.append(total / workers)
     losses = [float(v) for v in losses]
     step.close()
+    if device_status() or any(plan.timed_out() for plan in plans):      # a product that gave up waiting leaves wrong numbers
+        raise RuntimeError("a matrix product timed out on the device")
     return losses
 
 

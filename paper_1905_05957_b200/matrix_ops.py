@@ -89,6 +89,7 @@ def device_status(device: str | torch.device = "cuda") -> int:
     device = torch.device(device)
     index = torch.cuda.current_device() if device.index is None else device.index
     _dev_status(index)
+    torch.cuda.synchronize(index)              # products on other streams, too
     return int(_status[index][0].item())
 
 
@@ -396,6 +397,7 @@ class OrthUpdate:
 
     def timed_out(self) -> bool:
         """Whether a product of this plan ever gave up waiting (DS_DEV_MMA_TIMEOUT).  Waits for the device."""
+        torch.cuda.synchronize(self.device)
         return bool(int(self.dev_status[0].item()) & DS_DEV_MMA_TIMEOUT)
 
     def close(self):

@@ -3,7 +3,8 @@ not be handed out again until it has."""
 import pytest
 import torch
 
-from paper_1905_05957_b200 import Int8Linear, Int8Matrix, OrthUpdate, int8_linear, int8_matmul, int8_quantize
+from paper_1905_05957_b200 import Int8Linear, Int8Matrix, OrthUpdate, int8_linear, int8_matmul, int8_quantize, matrix_ops
+from paper_1905_05957_b200.matrix_ops import device_status
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +92,22 @@ def test_a_layer_dropped_before_its_stream_has_run():
     _overwrite([300 * 512 + 512 * 304 + 4 * 816 + 16, 256 * 512 * 2 + 4 * 768 + 16, 300 * 512, 256 * 512])
     torch.cuda.synchronize()
     assert torch.equal(dw, want)
+
+
+def test_status_of_products_on_other_streams():
+    """What a product on a stream that is behind reports is seen: here the words are set as such a product would set them."""
+    plan = OrthUpdate(8, 16)
+    assert device_status() == 0 and not plan.timed_out()
+    word = matrix_ops._status[torch.cuda.current_device()][0]
+    s = _behind()
+    with torch.cuda.stream(s):
+        word.fill_(2)
+        plan.dev_status[:1].fill_(2)
+    seen = device_status(), plan.timed_out()
+    torch.cuda.synchronize()
+    word.zero_()
+    assert seen == (2, True)
+    s = _behind()
+    with torch.cuda.stream(s):
+        plan.dev_status[:1].fill_(0)
+    assert not plan.timed_out() and device_status() == 0
