@@ -1005,11 +1005,13 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
   if (k == 0)
     return dtype_ok(dtype) ? ds_i8_matmul(nullptr, 0, sw, nullptr, 0, sw, bias, rows, n, 0, out, out_dtype, ldo, dev_status, cuda_stream)
                            : DS_ERR_INVALID_ARG;
+  // all refusals come before the first launch
+  if (!dtype_ok(dtype) || !dtype_ok(out_dtype) || n > kMaxLen || ldx < k || ldo < n || !x || !sw || !out) return DS_ERR_INVALID_ARG;
+  int rc = check_codes(w, ldw, k);
+  if (rc != DS_OK) return rc;
+  if (!aligned(x, size_of(dtype)) || !aligned(sw, 4) || !aligned(bias, 4) || !aligned(out, size_of(out_dtype)) || !aligned(dev_status, 4))
+    return DS_ERR_ALIGN;
   if (few_fused(rows, n, k)) {
-    if (!dtype_ok(dtype) || !dtype_ok(out_dtype) || n > kMaxLen || ldx < k || ldo < n || !x || !sw || !out) return DS_ERR_INVALID_ARG;
-    const int rc = check_codes(w, ldw, k);
-    if (rc != DS_OK) return rc;
-    if (!aligned(x, size_of(dtype)) || !aligned(sw, 4) || !aligned(bias, 4) || !aligned(out, size_of(out_dtype))) return DS_ERR_ALIGN;
     const FewParams p{x, ldx, nullptr, w, ldw, sw, bias, out, ldo, (uint32_t)rows, (uint32_t)n, (uint32_t)k,
                       aligned(x, 16) && ldx * size_of(dtype) % 16 == 0};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -1028,7 +1030,7 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
   const uint64_t ldq = round_up(k, 16);
   float* s = static_cast<float*>(workspace);
   int8_t* q = static_cast<int8_t*>(workspace) + 4 * round_up(rows, 64);
-  const int rc = ds_i8_quantize(x, dtype, rows, k, ldx, q, ldq, s, nullptr, 0, nullptr, nullptr, nullptr, 0, cuda_stream);
+  rc = ds_i8_quantize(x, dtype, rows, k, ldx, q, ldq, s, nullptr, 0, nullptr, nullptr, nullptr, 0, cuda_stream);
   if (rc != DS_OK) return rc;
   return ds_i8_matmul(q, ldq, s, w, ldw, sw, bias, rows, n, k, out, out_dtype, ldo, dev_status, cuda_stream);
 }

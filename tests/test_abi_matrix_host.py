@@ -158,3 +158,18 @@ def test_a_host_without_a_c_compiler(lib, tmp_path, monkeypatch):
 
 def test_the_extension_names_its_interpreter():
     assert os.path.basename(libbuild.CALL_LIB) == "dsq_call" + libbuild.sysconfig.get_config_var("EXT_SUFFIX")
+
+
+@pytest.mark.parametrize("rows", [2, 64])
+def test_linear_refuses_before_it_launches(lib, rows):
+    """Both forms: a refusal of the product's arguments comes before the quantiser is launched (without a device: before its launch fails)."""
+    def linear(**kw):
+        a = dict(x=P, dtype=0, rows=rows, k=64, ldx=64, w=P, ldw=64, sw=P, bias=None, n=5, out=P, odt=0, ldo=5, ws=P, size=1 << 20, status=P)
+        a.update(kw)
+        return lib.ds_i8_linear(*a.values(), None)
+
+    for kw in (dict(x=None), dict(w=None), dict(sw=None), dict(out=None), dict(ldx=32), dict(ldw=48), dict(ldo=4), dict(dtype=5), dict(odt=5),
+               dict(n=(1 << 30) + 1, ldo=1 << 31)):
+        assert linear(**kw) == b.DS_ERR_INVALID_ARG, kw
+    for kw in (dict(w=P + 8), dict(ldw=72), dict(x=P + 2), dict(out=P + 2), dict(sw=P + 1), dict(bias=P + 2), dict(status=P + 1)):
+        assert linear(**kw) == b.DS_ERR_ALIGN, kw
