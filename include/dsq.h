@@ -378,9 +378,12 @@ typedef enum { DS_F32 = 0, DS_BF16 = 1, DS_F16 = 2 } ds_dtype;
  *   nearest even.  A line of zeros (or one whose scale would be subnormal) has scale 0 and codes 0; a line that holds an
  *   inf or a NaN has scale NaN and codes 0, so that products with it are NaN.  Codes between the line's end and the next
  *   multiple of 16 are overwritten with 0, none beyond.  q, qt: 16-byte aligned, ldq and ldqt multiples of 16.
+ *   With codes by columns or sums: at most 4194240 rows, else DS_ERR_UNSUPPORTED.
  *   workspace (16-byte aligned, ds_i8_quantize_workspace bytes) is needed unless q alone is asked for.
- * ds_i8_matmul:  out_mn = (sum_k a_mk b_nk) * sa_m * sb_n + bias_n  with a [m, k], b [n, k]; the sum is exact, the rest is
- *   done from left to right in 32 bits.  bias may be NULL.  out [m, n], `ldo` elements between rows, of type out_dtype.  k <= DS_I8_MAX_K, else DS_ERR_UNSUPPORTED.
+ * ds_i8_matmul:  out_mn = (sum_k a_mk b_nk) * sa_m * sb_n + bias_n  with a [m, k], b [n, k]; codes from -127 to 127; the sum is
+ *   exact, the rest is done from left to right in 32 bits.  (Codes of -128, which the quantiser does not make, overflow where all
+ *   k = DS_I8_MAX_K of either line are such.)  bias may be NULL.  out [m, n], `ldo` elements between rows, of type out_dtype.
+ *   k <= DS_I8_MAX_K, else DS_ERR_UNSUPPORTED.
  *   k = 0 gives the bias.
  * ds_i8_linear:  the two together for a linear layer whose weights w [n, k] were quantised before (rows = output
  *   channels): x [rows, k] is quantised by rows into the workspace (ds_i8_linear_workspace bytes, 16-byte aligned;
@@ -417,7 +420,8 @@ int ds_i8_linear(const void* x, int dtype, uint64_t rows, uint64_t k, uint64_t l
  * rows depend on one another.  Every step multiplies what roundings leave in directions where u is zero by a, in whatever
  * arithmetic: more than eight steps of the usual coefficients are only for matrices of full rank.  A, B and X are held in 16 bits: singular
  * values s of X must stay below 8 and |b s^2 + c s^4| below 64 in every step (s below 2.6 for the usual coefficients, which keep it
- * below 1.3), else the update is inf or NaN; ds_orth_create does not check the coefficients for it.  An update of zeros gives zeros (NaN if eps is 0); one that holds an inf or a NaN gives NaN.
+ * below 1.3), else the update is inf or NaN; ds_orth_create does not check the coefficients for it.  An update of zeros
+ * gives zeros (NaN if eps is 0); one that holds an inf or a NaN gives NaN.
  *
  * ds_orth_create: with workspace == NULL fills *workspace_bytes and returns DS_NEED_BUFFERS; else makes a handle on that
  * workspace (256-byte aligned; it need not be cleared).  Host-only.  One handle on one stream at a time.

@@ -1,6 +1,9 @@
 """Operators on matrices beside the DoubleSqueeze step: layer products in 8-bit integers, whose gradients the workers
 compress, and the orthogonalised update that moves the model by what comes back.  Argument marshalling over the C ABI
 (include/dsq.h); PyTorch supplies memory and streams.
+
+The calls stand outside autograd, like the rest of the package: a result carries no gradient, whatever its arguments require.
+Int8Linear.backward gives a layer's gradients.
 """
 from __future__ import annotations
 
@@ -94,7 +97,7 @@ def device_status(device: str | torch.device = "cuda") -> int:
 
 
 class Int8Matrix:
-    """Codes [rows, cols] (int8) with one float32 scale per row: row r stands for codes[r] * scale[r].
+    """Codes [rows, cols] (int8, from -127 to 127) with one float32 scale per row: row r stands for codes[r] * scale[r].
     Rows must start on 16-byte boundaries (int8_quantize gives such; pack() copies into such)."""
 
     __slots__ = ("rows", "cols", "ld", "device", "codes_ptr", "scale_ptr", "_codes", "_scale", "stream")
@@ -250,7 +253,7 @@ def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, 
 
 def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
-    """x W^T (+ bias) for weights quantised before: x [tokens, k] is quantised by rows on the way."""
+    """x W^T (+ bias) for weights quantised before: x [tokens, k] is quantised by rows on the way.  No gradient flows back through it."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return int8_linear(x, w, bias, out_dtype, out)
@@ -290,7 +293,7 @@ class Int8Linear:
     """A linear layer y = x W^T (+ bias) whose three products run in 8-bit integers.
 
     W [out, in] (float32, bfloat16 or float16) is quantised by rows for the forward product and by columns for the gradient
-    of the inputs; call set_weight() after every change of W.  forward(x, training=True) keeps the column codes of x (one byte
+    of the inputs; call set_weight() after every change of W.  The bias is float32.  forward(x, training=True) keeps the column codes of x (one byte
     an entry) for the gradient of the weights."""
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor | None = None, training: bool = True, stream=None):
