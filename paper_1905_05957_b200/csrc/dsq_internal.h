@@ -50,10 +50,11 @@ inline void launch_pdl(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t
   (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
-// The same with `smem` bytes of dynamic shared memory (beyond the 48 KB a kernel gets by default the caller has raised the
-// kernel's limit).
+// The same with `smem` bytes of dynamic shared memory (beyond the 48 KB a kernel gets by default the
+// limit is raised first; that call only sets a number on the host).
 template <typename... P, typename... A>
-inline void launch_pdl_dyn(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
+inline void launch_pdl_smem(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
+  if (smem > 48 * 1024) (void)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = block;

@@ -1088,6 +1088,22 @@ inline MmaPlan plan_mma(const MmaShape& s, bool b_sym = false) {   // b_sym: a t
   return p;
 }
 
+// launch_pdl with `smem` bytes of dynamic shared memory; beyond the 48 KB that a kernel gets by default allow_smem_for has raised its limit.
+template <typename... P, typename... A>
+inline void launch_pdl_dyn(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // Shared memory beyond 48 KB is asked for once per kernel and device.
 template <auto KERNEL>
 inline void allow_smem_for(size_t bytes) {
