@@ -49,13 +49,13 @@ HEADLINE = 5                 # the largest one that fits one GPU
 # (a multi-pass capture must stay small) is scaled by the entries one launch processes: the
 # traffic of a streaming kernel grows in proportion.
 NCU_CAPTURES = {
-    "sign1": ("k_chunked<SIGN1, WORKER, 4, 256>", 748182272 + 331582464, 8 * 11_689_512, "3e80faecea9d3b0a"),
-    "qsgd": ("k_chunked<QSGD, WORKER, 2, 256>", 1073773000 + 630182144, 8 * 16_777_216, "3e80faecea9d3b0a"),
+    "sign1": ("k_chunked<SIGN1, WORKER, 4, 256>", 748286976 + 330969856, 8 * 11_689_512, "d3d9d8b17436cd39"),
+    "qsgd": ("k_chunked<QSGD, WORKER, 2, 256>", 1073782784 + 629218816, 8 * 16_777_216, "d3d9d8b17436cd39"),
     # the first kernel of the top-k worker pass alone (v read once, written once); the selection that follows it
     # moves a few percent of that
-    "topk": ("k_topk_pass1<WORKER>", 537251328 + 221441280, 16 * 4_194_304, "8493784d4c9f8058"),
-    "clip": ("k_clip<WORKER, 16>", 748323328 + 508980736, 8 * 11_689_512, "ccfe82e0a4de6e6b"),
-    "rsparse": ("k_rsparse<WORKER>", 748263680 + 333547008, 8 * 11_689_512, "ccfe82e0a4de6e6b"),
+    "topk": ("k_topk_pass1<WORKER>", 537271040 + 222255104, 16 * 4_194_304, "879da170ce59d806"),
+    "clip": ("k_clip<WORKER, 16>", 748474112 + 508574208, 8 * 11_689_512, "ed3a8b1fc2f54b30"),
+    "rsparse": ("k_rsparse<WORKER>", 748261120 + 329410304, 8 * 11_689_512, "ed3a8b1fc2f54b30"),
 }
 KERNEL_SOURCES = {  # files whose change invalidates the captured counters
     "sign1": ("dsq_chunked.cuh", "dsq_common.cuh", "dsq_internal.h"),

@@ -23,6 +23,13 @@ __device__ __forceinline__ void pdl_prologue() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// A load of what an earlier launch may have written.  Not the read-only path (ld.global.nc): that one asks its data to be constant for the
+// kernel's life, and under programmatic dependent launch a kernel is resident, waiting, while the launches before it write.
+template <class T>
+__device__ __forceinline__ T ld_plain(const T* p) {
+  return *p;
+}
+
 enum Src : int {
   SRC_WORKER = 0,        // v = g[row] + delta_w[row]
   SRC_SRV_IDENTITY = 1,  // v = (sum_i c_i) * inv_n + delta_s
@@ -204,14 +211,14 @@ __device__ __forceinline__ void src_load_tile(const SrcParams& p, uint32_t row, 
           wreg[j] = 0;
           sreg[j] = 0.f;
           if (wi < p.n && word < nw)
-            wreg[j] = __ldg(reinterpret_cast<const uint32_t*>(p.wp + wi * p.wp_stride + p.wp_off[kSgn]) + word);
+            wreg[j] = ld_plain(reinterpret_cast<const uint32_t*>(p.wp + wi * p.wp_stride + p.wp_off[kSgn]) + word);
           if constexpr (SRC == SRC_SRV_TERNARY) {
             zreg[j] = 0;
             if (wi < p.n && word < nw)
-              zreg[j] = __ldg(reinterpret_cast<const uint32_t*>(p.wp + wi * p.wp_stride + p.wp_off[1]) + word);
+              zreg[j] = ld_plain(reinterpret_cast<const uint32_t*>(p.wp + wi * p.wp_stride + p.wp_off[1]) + word);
           }
           if (lane < 8 && i0 + lane < p.n && e0 < p.d)
-            sreg[j] = __ldg(reinterpret_cast<const float*>(p.wp + (i0 + lane) * p.wp_stride + p.wp_off[kScl]) +
+            sreg[j] = ld_plain(reinterpret_cast<const float*>(p.wp + (i0 + lane) * p.wp_stride + p.wp_off[kScl]) +
                             (e0 >> p.w_log2_chunk));
           if constexpr (SRC == SRC_SRV_QSGD) {
 #pragma unroll
@@ -311,7 +318,7 @@ __device__ __forceinline__ void src_load_tile(const SrcParams& p, uint32_t row, 
           for (int u = 0; u < 8; ++u) {
             const uint32_t* off = reinterpret_cast<const uint32_t*>(p.wp + (uint64_t)(i0 + u) * p.wp_stride + p.wp_off[1]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) o[j][u] = (i0 + u < p.n && cnt[j]) ? __ldg(off + (e[j] >> p.w_log2_chunk)) : 0xFFFFFFFFu;
+            for (int j = 0; j < V; ++j) o[j][u] = (i0 + u < p.n && cnt[j]) ? ld_plain(off + (e[j] >> p.w_log2_chunk)) : 0xFFFFFFFFu;
           }
 #pragma unroll
           for (int u = 0; u < 8; ++u) {
@@ -321,7 +328,7 @@ __device__ __forceinline__ void src_load_tile(const SrcParams& p, uint32_t row, 
               // the filler 0xFFFFFFFF is no draw (draws are at most S - 1); a survivor past the end of a ragged
               // last float4 reads its slot, which holds +0, and is dropped by the masking of v below anyway
               const bool mine = o[j][u] <= smask && ((((uint32_t)e[j] ^ o[j][u]) & smask & ~3u) == 0u);
-              c[j][u] = mine ? __ldg(val + (e[j] >> p.w_log2_keep)) : 0.f;
+              c[j][u] = mine ? ld_plain(val + (e[j] >> p.w_log2_keep)) : 0.f;
             }
           }
 #pragma unroll
@@ -345,7 +352,7 @@ __device__ __forceinline__ void src_load_tile(const SrcParams& p, uint32_t row, 
           for (int u = 0; u < 4; ++u) {
             const uint32_t* off = reinterpret_cast<const uint32_t*>(p.wp + (uint64_t)(i0 + u) * p.wp_stride + p.wp_off[1]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) o[j][u] = (i0 + u < p.n && cnt[j]) ? __ldg(off + (e[j] >> p.w_log2_chunk)) : 0xFFFFFFFFu;
+            for (int j = 0; j < V; ++j) o[j][u] = (i0 + u < p.n && cnt[j]) ? ld_plain(off + (e[j] >> p.w_log2_chunk)) : 0xFFFFFFFFu;
           }
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
@@ -356,7 +363,7 @@ __device__ __forceinline__ void src_load_tile(const SrcParams& p, uint32_t row, 
 #pragma unroll
               for (int k = 0; k < 4; ++k)
                 if ((uint32_t)k < cnt[j] && (((uint32_t)e[j] + k) & smask) == o[j][u])   // never true for the filler 0xFFFFFFFF
-                  comp(c[j][u], k) = __ldg(val + ((e[j] + k) >> p.w_log2_keep));
+                  comp(c[j][u], k) = ld_plain(val + ((e[j] + k) >> p.w_log2_keep));
             }
           }
 #pragma unroll

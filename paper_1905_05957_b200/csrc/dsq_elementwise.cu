@@ -170,7 +170,7 @@ k_rsparse(const SrcParams src, const RsparseParams rp, float* delta_out, uint64_
     for (int j = 0; j < V; ++j) {
       ee[j] = (q0 + (uint64_t)j * kThreads + threadIdx.x) * 4;
       cc[j] = ee[j] < src.d ? (uint32_t)min((uint64_t)4, src.d - ee[j]) : 0u;
-      oo[j] = cc[j] ? __ldg(off + (ee[j] >> rp.log2_chunk)) : 0u;  // the chunk's draw, made by k_rsparse_draw
+      oo[j] = cc[j] ? ld_plain(off + (ee[j] >> rp.log2_chunk)) : 0u;  // the chunk's draw, made by k_rsparse_draw
       xx[j] = (x && cc[j]) ? load_row4(x, ee[j], cc[j], 1) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     src_load_tile<SRC, V>(src, row, ee, cc, vv);
@@ -231,22 +231,22 @@ __global__ void __launch_bounds__(kThreads) k_apply_dense(const PayloadView pv, 
     if (pv.op == DS_Q_IDENTITY) {
       C = load_row4(reinterpret_cast<const float*>(pv.base + pv.off[0]), e, cnt, 1);
     } else if (pv.op == DS_Q_SIGN1) {
-      const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(pv.base + pv.off[0]) + (e >> 5)) >> (uint32_t)(e & 31);
-      const float s = __ldg(reinterpret_cast<const float*>(pv.base + pv.off[1]) + (e >> pv.log2_chunk));
+      const uint32_t w = ld_plain(reinterpret_cast<const uint32_t*>(pv.base + pv.off[0]) + (e >> 5)) >> (uint32_t)(e & 31);
+      const float s = ld_plain(reinterpret_cast<const float*>(pv.base + pv.off[1]) + (e >> pv.log2_chunk));
       C = make_float4(signed_by_bit(s, w, 0), signed_by_bit(s, w, 1), signed_by_bit(s, w, 2), signed_by_bit(s, w, 3));
     } else if (pv.op == DS_Q_TERNARY) {
-      const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(pv.base + pv.off[0]) + (e >> 5)) >> (uint32_t)(e & 31);
-      const uint32_t z = __ldg(reinterpret_cast<const uint32_t*>(pv.base + pv.off[1]) + (e >> 5)) >> (uint32_t)(e & 31);
-      const float s = __ldg(reinterpret_cast<const float*>(pv.base + pv.off[2]));
+      const uint32_t w = ld_plain(reinterpret_cast<const uint32_t*>(pv.base + pv.off[0]) + (e >> 5)) >> (uint32_t)(e & 31);
+      const uint32_t z = ld_plain(reinterpret_cast<const uint32_t*>(pv.base + pv.off[1]) + (e >> 5)) >> (uint32_t)(e & 31);
+      const float s = ld_plain(reinterpret_cast<const float*>(pv.base + pv.off[2]));
       C = make_float4((z & 1u) ? signed_by_bit(s, w, 0) : 0.f, (z & 2u) ? signed_by_bit(s, w, 1) : 0.f,
                       (z & 4u) ? signed_by_bit(s, w, 2) : 0.f, (z & 8u) ? signed_by_bit(s, w, 3) : 0.f);
     } else if (pv.op == DS_Q_RSPARSE) {
-      const uint32_t o = __ldg(reinterpret_cast<const uint32_t*>(pv.base + pv.off[1]) + (e >> pv.log2_chunk));
+      const uint32_t o = ld_plain(reinterpret_cast<const uint32_t*>(pv.base + pv.off[1]) + (e >> pv.log2_chunk));
       const float* val = reinterpret_cast<const float*>(pv.base + pv.off[0]);
       C = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if ((uint32_t)k < cnt && (((uint32_t)e + k) & ((1u << pv.log2_keep) - 1u)) == o) comp(C, k) = __ldg(val + ((e + k) >> pv.log2_keep));
+        if ((uint32_t)k < cnt && (((uint32_t)e + k) & ((1u << pv.log2_keep) - 1u)) == o) comp(C, k) = ld_plain(val + ((e + k) >> pv.log2_keep));
     } else if (pv.op == DS_Q_CLIP) {
       uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -257,8 +257,8 @@ __global__ void __launch_bounds__(kThreads) k_apply_dense(const PayloadView pv, 
       C = make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
     } else {  // DS_Q_QSGD
       const uint32_t lv = __ldcs(reinterpret_cast<const uint32_t*>(pv.base + pv.off[0] + e));
-      const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(pv.base + pv.off[1]) + (e >> 5)) >> (uint32_t)(e & 31);
-      const float q = __ldg(reinterpret_cast<const float*>(pv.base + pv.off[2]) + (e >> pv.log2_chunk));
+      const uint32_t w = ld_plain(reinterpret_cast<const uint32_t*>(pv.base + pv.off[1]) + (e >> 5)) >> (uint32_t)(e & 31);
+      const float q = ld_plain(reinterpret_cast<const float*>(pv.base + pv.off[2]) + (e >> pv.log2_chunk));
       C = make_float4(signed_by_bit(__fmul_rn(byte_to_float(lv, 0), q), w, 0),
                       signed_by_bit(__fmul_rn(byte_to_float(lv, 1), q), w, 1),
                       signed_by_bit(__fmul_rn(byte_to_float(lv, 2), q), w, 2),
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kThreads) k_apply_dense(const PayloadView pv, 
 }
 
 // Sparse payload: only the k listed entries of x change (the others would subtract gamma * 0).
-__global__ void __launch_bounds__(kThreads) k_apply_sparse(const uint32_t* __restrict__ idx, const float* __restrict__ val,
+__global__ void __launch_bounds__(kThreads) k_apply_sparse(const uint32_t* idx, const float* val,
                                                            uint64_t k, float* x, float gamma) {
   pdl_prologue();
   for (uint64_t m = (uint64_t)blockIdx.x * kThreads + threadIdx.x; m < k; m += (uint64_t)gridDim.x * kThreads) {
@@ -304,7 +304,7 @@ cudaError_t launch_apply(const PayloadView& pv, float* x, uint64_t d, float gamm
 // the finished slice is written out whole -- the accumulator needs no clearing beforehand.
 constexpr uint32_t kAccSpan = kSparseSpan;
 
-__global__ void __launch_bounds__(kThreads) k_sparse_offsets(const uint8_t* __restrict__ wp, uint64_t stride, uint64_t off_idx,
+__global__ void __launch_bounds__(kThreads) k_sparse_offsets(const uint8_t* wp, uint64_t stride, uint64_t off_idx,
                                                              uint64_t k, uint64_t nspan, uint32_t* off) {
   pdl_prologue();
   const uint32_t i = blockIdx.y;
@@ -319,9 +319,9 @@ __global__ void __launch_bounds__(kThreads) k_sparse_offsets(const uint8_t* __re
   }
 }
 
-__global__ void __launch_bounds__(kThreads) k_sparse_accumulate(const uint8_t* __restrict__ wp, uint64_t stride,
+__global__ void __launch_bounds__(kThreads) k_sparse_accumulate(const uint8_t* wp, uint64_t stride,
                                                                 uint64_t off_idx, uint64_t off_val, uint32_t n, uint64_t d,
-                                                                uint64_t nspan, const uint32_t* __restrict__ off,
+                                                                uint64_t nspan, const uint32_t* off,
                                                                 float* acc) {
   pdl_prologue();
   __shared__ float s_acc[kAccSpan];

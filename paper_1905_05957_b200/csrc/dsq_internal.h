@@ -50,24 +50,6 @@ inline void launch_pdl(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t
   (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
-// The same with `smem` bytes of dynamic shared memory (beyond the 48 KB a kernel gets by default the
-// limit is raised first; that call only sets a number on the host).
-template <typename... P, typename... A>
-inline void launch_pdl_smem(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
-  if (smem > 48 * 1024) (void)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
-}
-
 // Destination of a chunk-wise operator (SIGN1 or QSGD).
 struct ChunkParams {
   uint32_t* out_bits;        // sign words, row stride bits_stride (in words)

@@ -24,13 +24,6 @@ constexpr long long kWaitCycles = 2000000000ll;   // about one second
 
 enum MmaKind : int { kMmaF16 = 0, kMmaI8 = 1 };
 
-// A load of what an earlier launch may have written.  Not the read-only path (ld.global.nc): that one asks its data to be constant for the
-// kernel's life, and under programmatic dependent launch a kernel is resident, waiting, while the launches before it write.
-template <class T>
-__device__ __forceinline__ T ld_plain(const T* p) {
-  return *p;
-}
-
 // ---- PTX ------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
