@@ -6,8 +6,8 @@
 // A launch of the general form costs 3 to 4 us whatever its size, and an update has seventeen of them.  Here a step takes 4 us,
 // about a third of it products, a third the exchange of A and a third their latencies: 34 us for four 64 x 576, 62 in the general
 // form.  The products are taken in two halves of either operand (hi hi + hi lo + lo hi on 16-bit floats: 22 bits), which small
-// matrices need: their roundings do not average out.  The warp instruction m16n8k16 is used; a tile of the tensor core's own
-// instruction would be half empty.  (Shorter sides up to 128 were slower than the general form, 77 against 59 us for 128 x 128.)
+// matrices need: their roundings do not average out.  The warp instruction m16n8k16 is used, fed from shared memory without
+// descriptors, barriers and tensor memory.  The tensor core's own instruction has a tile of 64 rows too; it was not tried here.  (Shorter sides up to 128 were slower than the general form, 77 against 59 us for 128 x 128.)
 #include "dsq_mma.cuh"
 #include "dsq_orth.cuh"
 
