@@ -387,7 +387,7 @@ typedef enum { DS_F32 = 0, DS_BF16 = 1, DS_F16 = 2 } ds_dtype;
  *   k = 0 gives the bias.
  * ds_i8_linear:  the two together for a linear layer whose weights w [n, k] were quantised before (rows = output
  *   channels): x [rows, k] is quantised by rows into the workspace (ds_i8_linear_workspace bytes, 16-byte aligned;
- *   none where that is 0: a few short rows, which are one launch).
+ *   none where that is 0: a few short rows, which are one launch).  out may not overlap x.
  * Training takes the same calls: forward  a = rows of x, b = rows of W;  gradient of inputs  a = rows of dY, b = columns
  *   of W (qt);  gradient of weights  a = columns of dY, b = columns of x.
  */

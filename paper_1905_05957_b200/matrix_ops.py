@@ -253,7 +253,8 @@ def int8_matmul(a: Int8Matrix, b: Int8Matrix, bias: torch.Tensor | None = None, 
 
 def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
-    """x W^T (+ bias) for weights quantised before: x [tokens, k] is quantised by rows on the way.  No gradient flows back through it."""
+    """x W^T (+ bias) for weights quantised before: x [tokens, k] is quantised by rows on the way.  No gradient flows back through it.
+    `out` may not overlap x."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return int8_linear(x, w, bias, out_dtype, out)
@@ -273,6 +274,10 @@ def int8_linear(x: torch.Tensor, w: Int8Matrix, bias: torch.Tensor | None = None
     bp = None if bias is None else _vector(bias, n, "bias", device)
     if out is not None:
         ldo, odt = _out(out, m, n, device), _dtype(out.dtype, "out")
+        if m and n and k:      # with few tokens some blocks still read x when others store
+            first, last = x.data_ptr(), x.data_ptr() + ((m - 1) * ld + k) * x.element_size()
+            if out.data_ptr() < last and first < out.data_ptr() + ((m - 1) * ldo + n) * out.element_size():
+                raise ValueError("out: overlaps x")
     elif out_dtype is None:
         out, ldo, odt = x.new_empty((m, n)), n, dt
     else:

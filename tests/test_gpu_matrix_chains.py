@@ -84,3 +84,16 @@ def test_quantise_multiply_and_update_in_a_row(m, n):
     want = run(torch.cuda.synchronize)
     for _ in range(5):
         assert all(torch.equal(a, b) for a, b in zip(run(lambda: None), want))
+
+
+@pytest.mark.parametrize("m", [1, 16, 100])
+def test_an_output_over_its_input_is_refused(m):
+    w = int8_quantize(_randn(256, 256, seed=1))
+    store = torch.zeros(2 * m + 1, 256, device="cuda")
+    x = store[:m]
+    for out in (x, store[m - 1:2 * m - 1], x.view(torch.bfloat16)[:, :256]):
+        with pytest.raises(ValueError, match="overlap"):
+            int8_linear(x, w, out=out)
+    x.copy_(_randn(m, 256, seed=2))
+    assert torch.equal(int8_linear(x, w, out=store[m:2 * m]), int8_linear(x, w))          # right behind it is not over it
+    assert (store[2 * m:] == 0).all()
