@@ -445,6 +445,124 @@ int ds_orth_update(ds_orth_handle h, const void* g, int g_dtype, float* momentum
                    float decay, void* cuda_stream);
 int ds_orth_destroy(ds_orth_handle h);
 
+/*
+ * ---- Layers in 16-bit floats, and what stands between layers ----
+ *
+ * Arguments come as structures whose members are all 64 bits wide: pointers, uint64_t and double.  Device memory and workspaces are the caller's.
+ * Matrices are rows of consecutive entries, `ld` entries apart (of a single row it is not read).  Outputs may not share memory with inputs or with one another, except
+ * where an entry says so; the rows of two matrices that lie side by side in wider rows of one pitch do not.  Refusals come before anything is launched.
+ *
+ * ds_f16_matmul: products of 16-bit matrices (bf16 or fp16, both operands of one type), sums and epilogue in 32 bits:
+ *     z_mn = sum_k a_mk b_nk + bias_n,     out_mn = act(z_mn) + residual_mn
+ *   layout DS_F16_FORWARD  a [m, k], b [n, k]   a layer's forward product: a = x, b = W
+ *          DS_F16_INPUTS   a [m, k], b [k, n]   the gradient of its inputs: a = dz, b = W
+ *          DS_F16_WEIGHTS  a [k, m], b [k, n]   the gradient of its weights: a = dz, b = x
+ *   bias (float), residual and z (of the operands' type) may be NULL.  out_dtype: the operands' or DS_F32; out is rounded once from 32 bits, and so is z,
+ *   which training keeps.  The residual may be out itself.  Operands that do not start on 16-byte boundaries or whose rows do not are copied into the
+ *   workspace (ds_f16_matmul_workspace bytes, 16-byte aligned; 0 where none are) by a launch of their own.  k = 0 gives act(bias) + residual.
+ *   The order of a sum depends on the sizes and the device, not on timing.
+ * ds_f16_slope: dz = dy act'(z) (in 16 bits) and / or sum_n = the column sums of dy act'(z) before it is rounded, in a fixed order.  z as the forward
+ *   product left it (NULL for DS_ACT_NONE).  dz may be dy or z itself.  workspace: ds_f16_slope_workspace bytes where sums are asked for.  At most 4194240 rows.
+ * ds_f16_pack: a copy of x as 16-bit floats on 16-byte rows (ldo a multiple of 8; entries from cols up to ldo become 0).
+ */
+typedef enum { DS_ACT_NONE = 0, DS_ACT_RELU = 1, DS_ACT_GELU = 2, DS_ACT_GELU_TANH = 3, DS_ACT_SILU = 4 } ds_activation;
+#define DS_F16_FORWARD 0u
+#define DS_F16_INPUTS 1u
+#define DS_F16_WEIGHTS 2u
+typedef struct {
+  uint64_t dtype, layout, m, n, k;
+  const void* a;
+  uint64_t lda;
+  const void* b;
+  uint64_t ldb;
+  const float* bias;
+  uint64_t activation;
+  const void* residual;
+  uint64_t ldr;
+  void* z;
+  uint64_t ldz;
+  void* out;
+  uint64_t out_dtype, ldo;
+  void* workspace;
+  uint64_t workspace_bytes;
+  uint32_t* dev_status;
+} ds_f16_product;
+uint64_t ds_f16_matmul_workspace(const ds_f16_product* p);
+int ds_f16_matmul(const ds_f16_product* p, void* cuda_stream);
+typedef struct {
+  uint64_t dtype, rows, cols;
+  const void* dy;
+  uint64_t lddy;
+  const void* z;
+  uint64_t ldz, activation;
+  void* dz;
+  uint64_t lddz;
+  void* sum;
+  uint64_t sum_dtype;
+  void* workspace;
+  uint64_t workspace_bytes;
+} ds_f16_slope_args;
+uint64_t ds_f16_slope_workspace(uint64_t rows, uint64_t cols);
+int ds_f16_slope(const ds_f16_slope_args* p, void* cuda_stream);
+int ds_f16_pack(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* out, int out_dtype, uint64_t ldo, void* cuda_stream);
+
+/*
+ * Norms around a residual connection, row by row in 32 bits:
+ *     u = post(y)          if post_w:  (y - mean) r post_w + post_b,  r = 1 / sqrt(mean((y - mean)^2) + eps);  DS_NORM_RMS: mean = 0
+ *     u = gate u           if gate: [groups, cols]; the rows are `groups` runs of rows / groups
+ *     u = D(u)             if threshold: dropout as below, of the rows' entries
+ *     h = residual_scale x + u      (u alone without x)
+ *     n = pre(h)           if pre_w, of h before it is rounded
+ *   y, n, dn, dy have `dtype`; x, h, dh, dx have `stream_dtype`: the same, or DS_F32.  Weights, biases, gates and their gradients are float.
+ *   ds_norm_forward writes h and / or n, and for the backward pass stats ([rows, 4] floats, 16-byte aligned; may be NULL).  h and n may each be x or y itself, of one type and pitch.
+ *   ds_norm_backward: from dh and / or dn (the gradients of h and n) those of x, y and the parameters; each is wanted where its pointer is not NULL.  y, x and the
+ *   parameters as the forward pass had them, stats as it left them.  dx and dy may be one of the inputs of their type and pitch.  workspace: ds_norm_backward_workspace bytes, 16-byte aligned.
+ *   Rows that hold an inf or a NaN are NaN and their parameters' gradients with them; other rows are not touched by them.
+ *   cols <= DS_NORM_MAX_COLS, else DS_ERR_UNSUPPORTED.
+ */
+#define DS_NORM_MAX_COLS 32768u
+#define DS_NORM_RMS 0u
+#define DS_NORM_LAYER 1u
+typedef struct {
+  uint64_t dtype, stream_dtype, rows, cols, norm;
+  const void* y;
+  uint64_t ldy;
+  const void* x;
+  uint64_t ldx;
+  const float *post_w, *post_b, *gate;
+  uint64_t groups;
+  const float *pre_w, *pre_b;
+  double residual_scale, eps;
+  uint64_t threshold, seed, layer, step;
+  float* stats;
+  void* h;
+  uint64_t ldh;
+  void* n;
+  uint64_t ldn;
+  const void* dh;
+  uint64_t lddh;
+  const void* dn;
+  uint64_t lddn;
+  void* dx;
+  uint64_t lddx;
+  void* dy;
+  uint64_t lddy;
+  float *d_post_w, *d_post_b, *d_gate, *d_pre_w, *d_pre_b;
+  void* workspace;
+  uint64_t workspace_bytes;
+} ds_norm_args;
+int ds_norm_forward(const ds_norm_args* p, void* cuda_stream);
+uint64_t ds_norm_backward_workspace(const ds_norm_args* p);
+int ds_norm_backward(const ds_norm_args* p, void* cuda_stream);
+
+/*
+ * Dropout with a mask that is drawn, not stored:  out = keep ? x * 65536 / (65536 - threshold) : 0, in 32 bits, rounded once.
+ *   Entry c of row r is kept iff half c mod 8 (the low half of word 0 first) of Philox4x32-10 with counter (c / 8, r, layer, step) and key (low word of seed, high word of
+ *   seed xor 0x44524F50) is at least threshold (probability times 65536; at most 65535).  The gradient is the same call on the gradient.  out may be x itself.
+ */
+int ds_dropout(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ldx, void* out, uint64_t ldo, uint32_t threshold, uint64_t seed, uint32_t layer,
+               uint32_t step, void* cuda_stream);
+
 /* Text of the most recent CUDA error seen by this thread's calls ("" if none). */
 const char* ds_last_error(void);
 

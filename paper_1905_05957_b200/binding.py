@@ -31,11 +31,17 @@ EXPORTS = ("ds_get_layout", "ds_create", "ds_worker_compress", "ds_server_aggreg
            "ds_server_aggregate_compress_slice", "ds_apply_update_slice", "ds_server_topk_slice_begin",
            "ds_server_topk_slice_digit", "ds_server_topk_slice_emit", "ds_apply_update_sparse_range",
            "ds_i8_quantize_workspace", "ds_i8_quantize", "ds_i8_matmul", "ds_i8_linear_workspace", "ds_i8_linear",
-           "ds_orth_create", "ds_orth_update", "ds_orth_destroy")
+           "ds_orth_create", "ds_orth_update", "ds_orth_destroy",
+           "ds_f16_matmul_workspace", "ds_f16_matmul", "ds_f16_slope_workspace", "ds_f16_slope", "ds_f16_pack",
+           "ds_norm_forward", "ds_norm_backward_workspace", "ds_norm_backward", "ds_dropout")
 DS_DEV_MMA_TIMEOUT = 2
 DS_F32, DS_BF16, DS_F16 = 0, 1, 2
 DS_I8_MAX_K = 131072
 DS_ORTH_NESTEROV = 1
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+DS_F16_FORWARD, DS_F16_INPUTS, DS_F16_WEIGHTS = 0, 1, 2
+DS_NORM_MAX_COLS = 32768
+DS_NORM_RMS, DS_NORM_LAYER = 0, 1
 DS_SLICE_ALIGN = 8192
 
 
@@ -66,6 +72,27 @@ class ds_orth_config(C.Structure):
     _fields_ = [("rows", C.c_uint32), ("cols", C.c_uint32), ("batch", C.c_uint32), ("steps", C.c_uint32),
                 ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("momentum", C.c_float), ("eps", C.c_float),
                 ("scale", C.c_float), ("flags", C.c_uint32), ("reserved", C.c_uint32), ("stride", C.c_uint64)]
+
+
+def _words(*names):
+    return [(n, C.c_uint64) for n in names]
+
+
+class ds_f16_product(C.Structure):
+    _fields_ = _words("dtype", "layout", "m", "n", "k", "a", "lda", "b", "ldb", "bias", "activation", "residual", "ldr", "z", "ldz", "out",
+                      "out_dtype", "ldo", "workspace", "workspace_bytes", "dev_status")
+
+
+class ds_f16_slope_args(C.Structure):
+    _fields_ = _words("dtype", "rows", "cols", "dy", "lddy", "z", "ldz", "activation", "dz", "lddz", "sum", "sum_dtype", "workspace",
+                      "workspace_bytes")
+
+
+class ds_norm_args(C.Structure):
+    _fields_ = (_words("dtype", "stream_dtype", "rows", "cols", "norm", "y", "ldy", "x", "ldx", "post_w", "post_b", "gate", "groups", "pre_w", "pre_b")
+                + [("residual_scale", C.c_double), ("eps", C.c_double)]
+                + _words("threshold", "seed", "layer", "step", "stats", "h", "ldh", "n", "ldn", "dh", "lddh", "dn", "lddn", "dx", "lddx", "dy", "lddy",
+                         "d_post_w", "d_post_b", "d_gate", "d_pre_w", "d_pre_b", "workspace", "workspace_bytes"))
 
 
 class DsqError(RuntimeError):
@@ -111,8 +138,17 @@ def load_library() -> C.CDLL:
     L.ds_orth_create.argtypes = [C.POINTER(ds_orth_config), vp, C.POINTER(size), vp, C.POINTER(vp)]
     L.ds_orth_update.argtypes = [vp, vp, C.c_int, vp, vp, C.c_int, vp, C.c_float, C.c_float, vp]
     L.ds_orth_destroy.argtypes = [vp]
+    L.ds_f16_matmul_workspace.argtypes = [C.POINTER(ds_f16_product)]
+    L.ds_f16_matmul.argtypes = [C.POINTER(ds_f16_product), vp]
+    L.ds_f16_slope_workspace.argtypes = [u64, u64]
+    L.ds_f16_slope.argtypes = [C.POINTER(ds_f16_slope_args), vp]
+    L.ds_f16_pack.argtypes = [vp, C.c_int, u64, u64, u64, vp, C.c_int, u64, vp]
+    L.ds_norm_forward.argtypes = L.ds_norm_backward.argtypes = [C.POINTER(ds_norm_args), vp]
+    L.ds_norm_backward_workspace.argtypes = [C.POINTER(ds_norm_args)]
+    L.ds_dropout.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, u32, u64, u32, u32, vp]
     for name in EXPORTS:
         getattr(L, name).restype = C.c_int
+    L.ds_f16_matmul_workspace.restype = L.ds_f16_slope_workspace.restype = L.ds_norm_backward_workspace.restype = u64
     L.ds_i8_quantize_workspace.restype = L.ds_i8_linear_workspace.restype = u64
     L.ds_last_error.restype = C.c_char_p
     L.ds_kernel_launches.restype = C.c_uint64
@@ -121,6 +157,18 @@ def load_library() -> C.CDLL:
 
 
 _call = None
+_STRUCT_CALLS = {"ds_f16_matmul": ds_f16_product, "ds_f16_slope": ds_f16_slope_args, "ds_norm_forward": ds_norm_args, "ds_norm_backward": ds_norm_args}
+_struct_call = None
+
+
+def _extension():
+    """The module that csrc/dsq_call.c builds for this interpreter, or None."""
+    if not os.path.exists(CALL_LIB):
+        return None
+    spec = importlib.util.spec_from_file_location("dsq_call", CALL_LIB)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
 
 
 def fast_call():
@@ -129,17 +177,35 @@ def fast_call():
     global _call
     if _call is None:
         lib = load_library()
-        functions = [getattr(lib, name) for name in ("ds_i8_quantize", "ds_i8_matmul", "ds_i8_linear")]
+        functions = [getattr(lib, name) for name in ("ds_i8_quantize", "ds_i8_matmul", "ds_i8_linear", "ds_f16_pack", "ds_dropout")]
         address = {f.__name__: C.cast(f, C.c_void_p).value for f in functions}
-        if os.path.exists(CALL_LIB):
-            spec = importlib.util.spec_from_file_location("dsq_call", CALL_LIB)
-            module = importlib.util.module_from_spec(spec)
-            spec.loader.exec_module(module)
+        module = _extension()
+        if module is not None:
             _call = module.call, address
         else:
             at = {address[f.__name__]: f for f in functions}
             _call = (lambda where, *args: at[where](*args)), address
     return _call
+
+
+def fast_struct_call():
+    """(call, addresses): call(addresses[name], stream, *members) calls a function of the ABI that takes a structure of 64-bit members and a
+    stream, by the same two ways."""
+    global _struct_call
+    if _struct_call is None:
+        lib = load_library()
+        address = {name: C.cast(getattr(lib, name), C.c_void_p).value for name in _STRUCT_CALLS}
+        module = _extension()
+        if module is not None and hasattr(module, "call_struct"):
+            _struct_call = module.call_struct, address
+        else:
+            at = {address[name]: (getattr(lib, name), kind) for name, kind in _STRUCT_CALLS.items()}
+
+            def call(where, stream, *members):
+                function, kind = at[where]
+                return function(C.byref(kind(*(0 if v is None else v for v in members))), stream)
+            _struct_call = call, address
+    return _struct_call
 
 
 def _qspec(q: Q) -> ds_qspec:

@@ -16,8 +16,10 @@ CALL_SRC = os.path.join(CSRC, "dsq_call.c")
 CALL_LIB = os.path.join(CSRC, "dsq_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["dsq_api.cu", "dsq_chunked.cu", "dsq_chunked_sign.cu", "dsq_chunked_sign_l2.cu", "dsq_chunked_qsgd.cu", "dsq_chunked_qsgd_window.cu",
            "dsq_elementwise.cu", "dsq_topk.cu", "dsq_static.cu", "dsq_whole.cu",
-           "dsq_mma.cu", "dsq_orth.cu", "dsq_orth_small.cu", "dsq_int8.cu"]
-HEADERS = ["dsq_common.cuh", "dsq_chunked.cuh", "dsq_mma.cuh", "dsq_orth.cuh", "dsq_internal.h", os.path.join("..", "..", "include", "dsq.h")]
+           "dsq_mma.cu", "dsq_orth.cu", "dsq_orth_small.cu", "dsq_int8.cu",
+           "dsq_linear16.cu", "dsq_product16_forward.cu", "dsq_product16_forward_z.cu", "dsq_product16_gradient.cu", "dsq_product16_floats.cu",
+           "dsq_product16_turned.cu", "dsq_norm.cu", "dsq_dropout.cu"]
+HEADERS = ["dsq_common.cuh", "dsq_chunked.cuh", "dsq_mma.cuh", "dsq_orth.cuh", "dsq_product16.cuh", "dsq_dropout.cuh", "dsq_rows8.cuh", "dsq_internal.h", os.path.join("..", "..", "include", "dsq.h")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

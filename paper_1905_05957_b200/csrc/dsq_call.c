@@ -4,10 +4,14 @@
  * call(address, a, b, ...) -> int: calls a function of the ABI whose arguments are all pointers or integers.  Every argument is
  * passed as 64 bits, which the x86-64 and AArch64 calling conventions pass in the same places as narrower integers; None is
  * NULL.  The caller vouches for the address and the number of arguments.
+ *
+ * call_struct(address, stream, a, b, ...) -> int: calls a function of the ABI that takes a structure whose members are all 64 bits
+ * wide, given one by one (a Python float becomes a double), and a stream.
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
+#include <string.h>
 
 #define MOST 18
 typedef uint64_t u;
@@ -34,6 +38,35 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLong(rc);
 }
 
-static PyMethodDef methods[] = {{"call", (PyCFunction)(void*)call, METH_FASTCALL, "call(address, *integers) -> int"}, {NULL, NULL, 0, NULL}};
+#define MOST_MEMBERS 64
+
+static PyObject* call_struct(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  u a[MOST_MEMBERS] = {0}, head[2] = {0};
+  (void)self;
+  if (n < 3 || n > MOST_MEMBERS + 2) {
+    PyErr_SetString(PyExc_TypeError, "an address, a stream and 1 to 64 members expected");
+    return NULL;
+  }
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    u* to = i < 2 ? head + i : a + (i - 2);
+    if (args[i] == Py_None) continue;
+    if (PyFloat_CheckExact(args[i])) {
+      const double v = PyFloat_AS_DOUBLE(args[i]);
+      memcpy(to, &v, sizeof v);
+      continue;
+    }
+    *to = (u)PyLong_AsUnsignedLongLongMask(args[i]);
+    if (*to == (u)-1 && PyErr_Occurred()) return NULL;
+  }
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((int (*)(const u*, u))head[0])(a, head[1]);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+static PyMethodDef methods[] = {{"call", (PyCFunction)(void*)call, METH_FASTCALL, "call(address, *integers) -> int"},
+                                {"call_struct", (PyCFunction)(void*)call_struct, METH_FASTCALL, "call_struct(address, stream, *members) -> int"},
+                                {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "dsq_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit_dsq_call(void) { return PyModule_Create(&module); }

@@ -1,0 +1,540 @@
+// A linear layer in 16-bit floats: its products (dsq_product16.cuh), the form for a few tokens, the gradient through the
+// activation, and copies onto 16-byte rows.
+#include <type_traits>
+
+#include "dsq_product16.cuh"
+
+using namespace dsq;
+
+namespace {
+
+inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
+inline bool aligned(const void* p, uint64_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+inline bool half_ok(uint64_t t) { return t == DS_BF16 || t == DS_F16; }
+inline bool dtype_ok(uint64_t t) { return t == DS_F32 || t == DS_BF16 || t == DS_F16; }
+inline uint32_t size_of(uint64_t dtype) { return dtype == DS_F32 ? 4 : 2; }
+constexpr uint64_t kMaxLen = 1ull << 30;
+
+// Whether the rows of two matrices share memory: `rows` of `bytes` bytes, `ld` apart.  Rows that lie side by side in wider ones
+// (columns of one buffer) do not.
+struct Span {
+  uintptr_t p;
+  uint64_t rows, bytes, ld;
+};
+inline Span span(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t size) {
+  return {reinterpret_cast<uintptr_t>(p), rows, cols * size, ld * size};
+}
+inline bool overlap(const Span& a, const Span& b) {
+  if (!a.p || !b.p || !a.rows || !b.rows || !a.bytes || !b.bytes) return false;
+  if (a.p >= b.p + (b.rows - 1) * b.ld + b.bytes || b.p >= a.p + (a.rows - 1) * a.ld + a.bytes) return false;
+  if (a.ld != b.ld || !a.ld) return true;
+  const uint64_t off = a.p >= b.p ? (a.p - b.p) % a.ld : (a.ld - (b.p - a.p) % a.ld) % a.ld;      // of a's row within b's rows
+  return off < b.bytes || off + a.bytes > a.ld;
+}
+
+// ---- copies onto 16-byte rows ---------------------------------------------------------------------------
+// Bound by memory; a thread takes eight entries of a row.  Entries behind a row's end become 0.
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_f16_pack(const T* x, uint64_t ld, uint32_t cols, int from_bf16, uint16_t* out, uint64_t ldo, int bf16, int vec) {
+  pdl_prologue();
+  const uint32_t c = (blockIdx.x * kThreads + threadIdx.x) * 8;
+  if (c >= ldo) return;
+  const uint64_t r = blockIdx.y + (uint64_t)gridDim.y * blockIdx.z;
+  const T* row = x + r * ld;
+  uint32_t w[4];
+  if constexpr (sizeof(T) == 4) {
+    float v[8];
+    if (vec && c + 8 <= cols) {
+      const float4 a = ld_plain(reinterpret_cast<const float4*>(row + c)), b = ld_plain(reinterpret_cast<const float4*>(row + c) + 1);
+      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? ld_plain(row + c + j) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = halves_of(v[2 * j], v[2 * j + 1], bf16);
+  } else {
+    uint16_t h[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = c + j < cols ? ld_plain(row + c + j) : (uint16_t)0;
+    if (from_bf16 == bf16) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = h[2 * j] | (uint32_t)h[2 * j + 1] << 16;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = halves_of(from_half(h[2 * j], from_bf16), from_half(h[2 * j + 1], from_bf16), bf16);
+    }
+  }
+  *reinterpret_cast<uint4*>(out + r * ldo + c) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+cudaError_t pack(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* out, int out_dtype, uint64_t ldo, cudaStream_t st) {
+  const uint64_t gx = (ldo + 8 * kThreads - 1) / (8 * kThreads), full = rows < 32768 ? rows : 32768;
+  for (uint64_t r0 = 0; r0 < rows;) {      // rows in two dimensions of the grid, a last launch for what is left of them
+    const uint64_t gz = (rows - r0) / full ? ((rows - r0) / full < 32768 ? (rows - r0) / full : 32768) : 1, gy = (rows - r0) < full ? rows - r0 : full;
+    const dim3 grid((uint32_t)gx, (uint32_t)gy, (uint32_t)gz);
+    uint16_t* to = static_cast<uint16_t*>(out) + r0 * ldo;
+    if (dtype == DS_F32) {
+      const float* from = static_cast<const float*>(x) + r0 * ld;
+      launch_pdl(k_f16_pack<float>, grid, dim3(kThreads), st, from, ld, (uint32_t)cols, 0, to, ldo, (int)(out_dtype == DS_BF16),
+                 (int)(aligned(x, 16) && ld % 4 == 0));
+    } else {
+      const uint16_t* from = static_cast<const uint16_t*>(x) + r0 * ld;
+      launch_pdl(k_f16_pack<uint16_t>, grid, dim3(kThreads), st, from, ld, (uint32_t)cols, (int)(dtype == DS_BF16), to, ldo,
+                 (int)(out_dtype == DS_BF16), 0);
+    }
+    count_launches(1);
+    r0 += gy * gz;
+  }
+  return cudaGetLastError();
+}
+
+// ---- an empty sum: act(bias) + residual -----------------------------------------------------------------
+__global__ void __launch_bounds__(kThreads) k_f16_empty(const Out16 o) {
+  pdl_prologue();
+  const uint64_t r = blockIdx.x;
+  for (uint32_t c = threadIdx.x; c < o.n; c += kThreads) {
+    float v = o.bias ? o.bias[c] : 0.f;
+    if (o.z) o.z[r * o.ldz + c] = half_of(v, o.bf16);
+    with_act(o.act, [&](auto a) { v = act_of<decltype(a)::value>(v); });
+    if (o.residual) v += from_half(o.residual[r * o.ldr + c], o.bf16);
+    if (o.f32)
+      static_cast<float*>(o.out)[r * o.ldo + c] = v;
+    else
+      static_cast<uint16_t*>(o.out)[r * o.ldo + c] = half_of(v, o.bf16);
+  }
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------------
+// The weights' bytes are all that counts.  A CTA takes 16 or 32 rows of W; each of its eight warps has an eighth of K, which it
+// reads in chunks of 32 entries a row, four chunks ahead, straight into the registers of m16n8k16 instructions (tokens are the
+// 8 columns; the warp instruction is enough, the loop waits for memory).  K is dealt to the instructions' places as it arrives:
+// lane t of a group of four loads 8 consecutive entries of its rows and tokens and feeds them as two instructions' worth.
+// The warps' sums meet in shared memory and are added in the order of the warps.
+constexpr uint32_t kFewMost = 16;
+
+struct FewParams16 {
+  const uint16_t *x, *w;
+  uint64_t ldx, ldw;
+  uint32_t k;
+  Out16 o;
+};
+
+// 8 entries from k0 on; behind the end of a row nothing is read and zeros stand.
+__device__ __forceinline__ uint4 load_halves8(const uint16_t* row, uint32_t k0, uint32_t k) {
+  if (k0 + 8 <= k) return ld_plain(reinterpret_cast<const uint4*>(row + k0));
+  uint32_t v[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    if (k0 + 2 * h < k) v[h] = row[k0 + 2 * h];
+    if (k0 + 2 * h + 1 < k) v[h] |= (uint32_t)row[k0 + 2 * h + 1] << 16;
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+template <bool BF16>
+__device__ __forceinline__ void mma_half(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (BF16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// NT: groups of 8 tokens, RB: blocks of 16 rows of W.
+template <bool BF16, int NT, int RB>
+__global__ void __launch_bounds__(256, 2) k_f16_few(const FewParams16 p) {
+  constexpr int kAhead = 4;
+  __shared__ float part[8][RB * 16][NT * 8 + 1];
+  pdl_prologue();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t row0 = blockIdx.x * (16 * RB);
+  const uint32_t chunks = p.k / 32, per = (chunks + 7) / 8;
+  const uint32_t first = min(warp * per, chunks), end = min(first + per, chunks);
+  const uint16_t *wrow[2 * RB], *xrow[NT];      // rows and tokens past the end: one that is there, not stored
+#pragma unroll
+  for (int i = 0; i < 2 * RB; ++i) wrow[i] = p.w + (uint64_t)min(row0 + g + 8 * i, p.o.n - 1) * p.ldw;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) xrow[j] = p.x + min(8u * j + g, p.o.m - 1) * p.ldx;
+  uint4 w[kAhead][2 * RB], xc[kAhead][NT];
+  auto fetch = [&](uint32_t c, uint4 (&to)[2 * RB], uint4 (&xt)[NT]) {
+    if (c >= end) return;
+    const uint32_t k0 = c * 32 + t * 8;
+#pragma unroll
+    for (int i = 0; i < 2 * RB; ++i) to[i] = ld_plain(reinterpret_cast<const uint4*>(wrow[i] + k0));
+#pragma unroll
+    for (int j = 0; j < NT; ++j) xt[j] = ld_plain(reinterpret_cast<const uint4*>(xrow[j] + k0));
+  };
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a) fetch(first + a, w[a], xc[a]);
+  float acc[RB][NT][4];
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[r][j][i] = 0.f;
+  auto multiply = [&](const uint4 (&wc)[2 * RB], const uint4 (&x)[NT]) {
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      const uint4 lo = wc[2 * r], hi = wc[2 * r + 1];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        mma_half<BF16>(acc[r][j], lo.x, hi.x, lo.y, hi.y, x[j].x, x[j].y);
+        mma_half<BF16>(acc[r][j], lo.z, hi.z, lo.w, hi.w, x[j].z, x[j].w);
+      }
+    }
+  };
+  for (uint32_t c0 = first; c0 < end; c0 += kAhead) {
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const uint32_t c = c0 + a;
+      if (c >= end) break;
+      multiply(w[a], xc[a]);
+      fetch(c + kAhead, w[a], xc[a]);
+    }
+  }
+  if (warp == 7 && (p.k & 31)) {      // the rest of K
+    const uint32_t k0 = chunks * 32 + t * 8;
+    uint4 we[2 * RB], xe[NT];
+#pragma unroll
+    for (int i = 0; i < 2 * RB; ++i) we[i] = load_halves8(wrow[i], k0, p.k);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) xe[j] = load_halves8(xrow[j], k0, p.k);
+    multiply(we, xe);
+  }
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) part[warp][16 * r + g + 8 * (i >> 1)][8 * j + 2 * t + (i & 1)] = acc[r][j][i];
+  __syncthreads();
+  const Out16& o = p.o;
+  for (uint32_t at = threadIdx.x; at < RB * 16 * o.m; at += 256) {
+    const uint32_t token = at / (RB * 16), r = at % (RB * 16), row = row0 + r;
+    if (row >= o.n) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v += part[q][r][token];
+    if (o.bias) v += ld_plain(o.bias + row);
+    if (o.z) o.z[token * o.ldz + row] = half_of(v, BF16);
+    with_act(o.act, [&](auto a) { v = act_of<decltype(a)::value>(v); });
+    if (o.residual) v += from_half(ld_plain(o.residual + token * o.ldr + row), BF16);
+    if (o.f32)
+      static_cast<float*>(o.out)[token * o.ldo + row] = v;
+    else
+      static_cast<uint16_t*>(o.out)[token * o.ldo + row] = half_of(v, BF16);
+  }
+}
+
+template <bool BF16, int NT>
+cudaError_t launch_few16(const FewParams16& p, cudaStream_t st) {
+  if ((p.o.n + 31) / 32 >= 2 * (uint32_t)sm_count())
+    launch_pdl(k_f16_few<BF16, NT, 2>, dim3((p.o.n + 31) / 32), dim3(256), st, p);
+  else
+    launch_pdl(k_f16_few<BF16, NT, 1>, dim3((p.o.n + 15) / 16), dim3(256), st, p);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+// ---- the gradient through the activation ----------------------------------------------------------------
+// dz = dy act'(z) in 16 bits and, from what is not yet rounded, the column sums of each block of kSumRows rows; a second kernel adds
+// the blocks in their order.  Bound by memory.  A warp reads 8 entries a lane of a row; a CTA's warps take every eighth row.
+constexpr uint32_t kSumRows = 64;
+
+template <bool VEC>
+__global__ void __launch_bounds__(256) k_f16_slope(const uint16_t* dy, uint64_t lddy, const uint16_t* z, uint64_t ldz, int act, int bf16, uint16_t* dz,
+                                                   uint64_t lddz, uint32_t rows, uint32_t cols, float* sums) {
+  __shared__ float part[8][256 + 8];
+  pdl_prologue();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t c = blockIdx.x * 256 + lane * 8, r0 = blockIdx.y * kSumRows;
+  float s[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s[j] = 0.f;
+  if (c < cols) {
+    const bool whole = VEC && c + 8 <= cols;
+    auto get = [&](const uint16_t* row, uint32_t (&w)[4]) {
+      if (whole) {
+        const uint4 v = ld_plain(reinterpret_cast<const uint4*>(row + c));
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[j] = c + 2 * j < cols ? ld_plain(row + c + 2 * j) : 0u;
+          if (c + 2 * j + 1 < cols) w[j] |= (uint32_t)ld_plain(row + c + 2 * j + 1) << 16;
+        }
+      }
+    };
+    constexpr uint32_t kBatch = 4;      // rows in flight
+    for (uint32_t i = 0; i < kSumRows / 8; i += kBatch) {
+      uint32_t g[kBatch][4], q[kBatch][4];
+#pragma unroll
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        const uint64_t r = r0 + warp + 8 * (i + b);
+        if (r < rows) {
+          get(dy + r * lddy, g[b]);
+          if (z) get(z + r * ldz, q[b]);
+        }
+      }
+#pragma unroll
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        const uint64_t r = r0 + warp + 8 * (i + b);
+        if (r >= rows) break;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = half_at(g[b][j / 2], j & 1, bf16);
+        with_act(act, [&](auto a) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] *= slope_of<decltype(a)::value>(half_at(q[b][j / 2], j & 1, bf16));
+        });
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += v[j];
+        if (dz) {
+          uint16_t* to = dz + r * lddz + c;
+          if (whole)
+            *reinterpret_cast<uint4*>(to) = make_uint4(halves_of(v[0], v[1], bf16), halves_of(v[2], v[3], bf16), halves_of(v[4], v[5], bf16), halves_of(v[6], v[7], bf16));
+          else
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (c + j < cols) to[j] = half_of(v[j], bf16);
+        }
+      }
+    }
+  }
+  if (!sums) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) part[warp][lane * 8 + j] = s[j];
+  __syncthreads();
+  const uint32_t col = blockIdx.x * 256 + threadIdx.x;
+  if (col >= cols) return;
+  float v = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) v += part[w][threadIdx.x];
+  sums[(uint64_t)blockIdx.y * cols + col] = v;
+}
+
+__global__ void __launch_bounds__(256) k_f16_sums(const float* sums, uint32_t blocks, uint32_t cols, void* out, int f32, int bf16) {
+  __shared__ float part[8][32];
+  pdl_prologue();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t col = blockIdx.x * 32 + lane;
+  float v = 0.f;
+  if (col < cols)
+    for (uint32_t b = warp; b < blocks; b += 8) v += ld_plain(sums + (uint64_t)b * cols + col);
+  part[warp][lane] = v;
+  __syncthreads();
+  if (warp || col >= cols) return;
+  v = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) v += part[w][lane];
+  if (f32)
+    static_cast<float*>(out)[col] = v;
+  else
+    static_cast<uint16_t*>(out)[col] = half_of(v, bf16);
+}
+
+// ---- host side ------------------------------------------------------------------------------------------
+
+struct Shape16 {
+  uint64_t rows_a, cols_a, rows_b, cols_b;      // as they lie in memory
+  bool copy_a, copy_b;
+  uint64_t bytes_a, bytes_b;
+};
+Shape16 shape_of(const ds_f16_product* p) {
+  Shape16 s;
+  const bool a_across = p->layout == DS_F16_WEIGHTS, b_across = p->layout != DS_F16_FORWARD;
+  s.rows_a = a_across ? p->k : p->m, s.cols_a = a_across ? p->m : p->k;
+  s.rows_b = b_across ? p->k : p->n, s.cols_b = b_across ? p->n : p->k;
+  // a single row has no pitch
+  s.copy_a = !aligned(p->a, 16) || (s.rows_a > 1 && p->lda % 8);
+  s.copy_b = !aligned(p->b, 16) || (s.rows_b > 1 && p->ldb % 8);
+  s.bytes_a = s.copy_a ? round_up(s.rows_a * round_up(s.cols_a, 8) * 2, 256) : 0;
+  s.bytes_b = s.copy_b ? round_up(s.rows_b * round_up(s.cols_b, 8) * 2, 256) : 0;
+  return s;
+}
+
+// CTAs that share a tile's K, for few tokens: as many as run at once with at least four steps each.
+inline uint32_t few_parts(uint32_t tiles, uint32_t k) {
+  uint32_t p = 1;
+  while (p < 8 && tiles <= (uint32_t)cluster_count(2 * p) && (k + 63) / 64 >= 8 * p) p *= 2;
+  return p;
+}
+
+constexpr uint32_t kTurnedMost = 64;
+
+cudaError_t multiply(const ds_f16_product* p, const Out16& o, Operand16 a, Operand16 b, cudaStream_t st) {
+  const uint32_t m = o.m, n = o.n, k = (uint32_t)p->k;
+  if (!a.across && !b.across && m <= kFewMost) {
+    const FewParams16 f{static_cast<const uint16_t*>(a.p), static_cast<const uint16_t*>(b.p), a.ld, b.ld, k, o};
+    if (o.bf16) return m <= 8 ? launch_few16<true, 1>(f, st) : launch_few16<true, 2>(f, st);
+    return m <= 8 ? launch_few16<false, 1>(f, st) : launch_few16<false, 2>(f, st);
+  }
+  const MmaShape s{m, n, k, 1, 2, 0, 0, p->dev_status, 1, (uint32_t)o.bf16};
+  const bool bare = !o.residual && !o.z && !o.bias && !o.act;
+  const bool blocks = !o.f32 && aligned(o.out, 16) && o.ldo % 8 == 0 && (!o.residual || (aligned(o.residual, 16) && o.ldr % 8 == 0)) &&
+                      (!o.z || (aligned(o.z, 16) && o.ldz % 8 == 0)) && (p->layout == DS_F16_FORWARD || bare);
+  const bool floats = o.f32 && bare && aligned(o.out, 32) && o.ldo % 8 == 0;
+  if (m <= kTurnedMost || !(blocks || floats)) {
+    const MmaShape t{n, m, k, 1, 2, 0, 0, p->dev_status, 1, (uint32_t)o.bf16};
+    MmaPlan plan = plan_mma(t);
+    if (m <= 32 && !a.across && !b.across) {
+      plan.pair = false;
+      plan.bn = 32;
+      plan.parts = few_parts(TileWalk(t, 32).total, k);
+    }
+    return product16_turned(plan, b, a, t, EpiTurned{o}, st);
+  }
+  const MmaPlan plan = plan_mma(s);
+  if (floats) return product16_floats(plan, a, b, s, EpiFloats{static_cast<float*>(o.out), o.ldo, m, n}, st);
+  auto maps = [&](auto& epi) {
+    cudaError_t e = make_tensor_map(&epi.map_y, kMmaHalf, o.out, n, m, 1, o.ldo, o.ldo * m, 32, 32, true);
+    if (e == cudaSuccess && o.residual) e = make_tensor_map(&epi.map_r, kMmaHalf, o.residual, n, m, 1, o.ldr, o.ldr * m, 32, 32, true);
+    if (e == cudaSuccess && o.z) e = make_tensor_map(&epi.map_z, kMmaHalf, o.z, n, m, 1, o.ldz, o.ldz * m, 32, 32, true);
+    epi.o = o;
+    epi.bias_vec = aligned(o.bias, 16);
+    return e;
+  };
+  if (o.z) {
+    EpiBlocks<2> epi{};
+    const cudaError_t e = maps(epi);
+    return e != cudaSuccess ? e : product16_forward_z(plan, a, b, s, epi, st);
+  }
+  EpiBlocks<1> epi{};
+  const cudaError_t e = maps(epi);
+  if (e != cudaSuccess) return e;
+  return p->layout == DS_F16_FORWARD ? product16_forward(plan, a, b, s, epi, st) : product16_gradient(plan, a, b, s, epi, st);
+}
+
+int check_product(const ds_f16_product* p) {
+  if (!p || !half_ok(p->dtype) || p->layout > DS_F16_WEIGHTS || p->activation > DS_ACT_SILU) return DS_ERR_INVALID_ARG;
+  if (p->out_dtype != DS_F32 && p->out_dtype != p->dtype) return DS_ERR_INVALID_ARG;
+  if (p->m > kMaxLen || p->n > kMaxLen || p->k > kMaxLen) return DS_ERR_INVALID_ARG;
+  return DS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ds_f16_pack(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* out, int out_dtype, uint64_t ldo, void* cuda_stream) {
+  if (!dtype_ok(dtype) || !half_ok(out_dtype) || rows > kMaxLen || cols > kMaxLen || ldo > kMaxLen + 8) return DS_ERR_INVALID_ARG;
+  if (rows == 0 || cols == 0) return DS_OK;
+  if (!x || !out || (ld < cols && rows > 1) || ldo < cols) return DS_ERR_INVALID_ARG;
+  if (!aligned(x, size_of(dtype)) || !aligned(out, 16) || ldo % 8) return DS_ERR_ALIGN;
+  if (overlap(span(x, rows, cols, ld, size_of(dtype)), span(out, rows, ldo, ldo, 2))) return DS_ERR_INVALID_ARG;
+  const cudaError_t e = pack(x, dtype, rows, cols, ld, out, out_dtype, ldo, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? DS_OK : cuda_fail(e, "16-bit copy");
+}
+
+uint64_t ds_f16_matmul_workspace(const ds_f16_product* p) {
+  if (check_product(p) != DS_OK || !p->m || !p->n || !p->k) return 0;
+  const Shape16 s = shape_of(p);
+  return s.bytes_a + s.bytes_b;
+}
+
+int ds_f16_matmul(const ds_f16_product* p, void* cuda_stream) {
+  const int rc = check_product(p);
+  if (rc != DS_OK) return rc;
+  if (p->m == 0 || p->n == 0) return DS_OK;
+  if (!p->out || (p->m > 1 && p->ldo < p->n)) return DS_ERR_INVALID_ARG;
+  if ((p->residual && p->m > 1 && p->ldr < p->n) || (p->z && p->m > 1 && p->ldz < p->n)) return DS_ERR_INVALID_ARG;
+  if (!aligned(p->out, size_of(p->out_dtype)) || !aligned(p->bias, 4) || !aligned(p->residual, 2) || !aligned(p->z, 2) || !aligned(p->dev_status, 4))
+    return DS_ERR_ALIGN;
+  const Shape16 s = shape_of(p);
+  const Span out = span(p->out, p->m, p->n, p->ldo, size_of(p->out_dtype)), z = span(p->z, p->m, p->n, p->ldz, 2),
+             res = span(p->residual, p->m, p->n, p->ldr, 2), bias = span(p->bias, 1, p->n, p->n, 4);
+  // the residual may be added to in place
+  const bool in_place = p->residual == p->out && p->ldr == p->ldo && p->out_dtype != DS_F32;
+  if (overlap(out, z) || overlap(res, z) || (!in_place && overlap(out, res)) || overlap(out, bias) || overlap(z, bias)) return DS_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const Out16 o{p->bias, static_cast<const uint16_t*>(p->residual), static_cast<uint16_t*>(p->z), p->out, p->ldr, p->ldz, p->ldo, (uint32_t)p->m, (uint32_t)p->n,
+                (int)p->activation, p->dtype == DS_BF16, p->out_dtype == DS_F32};
+  cudaError_t e = cudaSuccess;
+  if (p->k == 0) {
+    launch_pdl(k_f16_empty, dim3(o.m), dim3(kThreads), st, o);
+    count_launches(1);
+    e = cudaGetLastError();
+    return e == cudaSuccess ? DS_OK : cuda_fail(e, "16-bit product");
+  }
+  if (!p->a || !p->b || (s.rows_a > 1 && p->lda < s.cols_a) || (s.rows_b > 1 && p->ldb < s.cols_b)) return DS_ERR_INVALID_ARG;
+  if (!aligned(p->a, 2) || !aligned(p->b, 2)) return DS_ERR_ALIGN;
+  const Span sa = span(p->a, s.rows_a, s.cols_a, p->lda, 2), sb = span(p->b, s.rows_b, s.cols_b, p->ldb, 2);
+  if (overlap(out, sa) || overlap(out, sb) || overlap(z, sa) || overlap(z, sb)) return DS_ERR_INVALID_ARG;
+  if (s.bytes_a + s.bytes_b) {
+    if (!p->workspace) return DS_ERR_INVALID_ARG;
+    if (!aligned(p->workspace, 16)) return DS_ERR_ALIGN;
+    if (p->workspace_bytes < s.bytes_a + s.bytes_b) return DS_ERR_BUFFER_TOO_SMALL;
+    const Span ws = span(p->workspace, 1, s.bytes_a + s.bytes_b, s.bytes_a + s.bytes_b, 1);
+    if (overlap(ws, sa) || overlap(ws, sb) || overlap(ws, out) || overlap(ws, z) || overlap(ws, res) || overlap(ws, bias)) return DS_ERR_INVALID_ARG;
+  }
+  const bool a_across = p->layout == DS_F16_WEIGHTS, b_across = p->layout != DS_F16_FORWARD;
+  // a single row's pitch is the caller's word for nothing: one that a tensor map takes
+  Operand16 a{p->a, s.rows_a > 1 ? p->lda : round_up(s.cols_a, 8), o.m, a_across}, b{p->b, s.rows_b > 1 ? p->ldb : round_up(s.cols_b, 8), o.n, b_across};
+  uint8_t* ws = static_cast<uint8_t*>(p->workspace);
+  if (s.copy_a) {
+    const uint64_t ld = round_up(s.cols_a, 8);
+    e = pack(p->a, (int)p->dtype, s.rows_a, s.cols_a, p->lda, ws, (int)p->dtype, ld, st);
+    a.p = ws, a.ld = ld;
+  }
+  if (e == cudaSuccess && s.copy_b) {
+    const uint64_t ld = round_up(s.cols_b, 8);
+    e = pack(p->b, (int)p->dtype, s.rows_b, s.cols_b, p->ldb, ws + s.bytes_a, (int)p->dtype, ld, st);
+    b.p = ws + s.bytes_a, b.ld = ld;
+  }
+  if (e == cudaSuccess) e = multiply(p, o, a, b, st);
+  return e == cudaSuccess ? DS_OK : cuda_fail(e, "16-bit product");
+}
+
+uint64_t ds_f16_slope_workspace(uint64_t rows, uint64_t cols) { return 4 * ((rows + kSumRows - 1) / kSumRows) * cols; }
+
+int ds_f16_slope(const ds_f16_slope_args* p, void* cuda_stream) {
+  if (!p || !half_ok(p->dtype) || p->activation > DS_ACT_SILU || p->rows > kMaxLen || p->cols > kMaxLen) return DS_ERR_INVALID_ARG;
+  if (p->sum && p->sum_dtype != DS_F32 && p->sum_dtype != p->dtype) return DS_ERR_INVALID_ARG;
+  if (p->cols == 0) return DS_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (!aligned(p->sum, p->sum ? size_of(p->sum_dtype) : 1)) return DS_ERR_ALIGN;
+  if (p->rows == 0) {
+    const cudaError_t e = p->sum ? cudaMemsetAsync(p->sum, 0, size_of(p->sum_dtype) * p->cols, st) : cudaSuccess;
+    return e == cudaSuccess ? DS_OK : cuda_fail(e, "clearing sums");
+  }
+  if (!p->dy || (p->activation != DS_ACT_NONE) != (p->z != nullptr) || (!p->dz && !p->sum)) return DS_ERR_INVALID_ARG;
+  if (p->rows > 1 && (p->lddy < p->cols || (p->z && p->ldz < p->cols) || (p->dz && p->lddz < p->cols))) return DS_ERR_INVALID_ARG;
+  if (!aligned(p->dy, 2) || !aligned(p->z, 2) || !aligned(p->dz, 2)) return DS_ERR_ALIGN;
+  const uint64_t blocks = (p->rows + kSumRows - 1) / kSumRows;
+  if (blocks > 65535) return DS_ERR_UNSUPPORTED;
+  const Span dy = span(p->dy, p->rows, p->cols, p->lddy, 2), z = span(p->z, p->rows, p->cols, p->ldz, 2), dz = span(p->dz, p->rows, p->cols, p->lddz, 2),
+             sum = span(p->sum, 1, p->cols, p->cols, p->sum ? size_of(p->sum_dtype) : 0);
+  // in place over dy or z, entry by entry
+  if ((overlap(dz, dy) && !(p->dz == p->dy && p->lddz == p->lddy)) || (overlap(dz, z) && !(p->dz == p->z && p->lddz == p->ldz)) || overlap(sum, dz) ||
+      overlap(sum, dy) || overlap(sum, z))
+    return DS_ERR_INVALID_ARG;
+  float* sums = nullptr;
+  if (p->sum) {
+    if (!p->workspace) return DS_ERR_INVALID_ARG;
+    if (!aligned(p->workspace, 16)) return DS_ERR_ALIGN;
+    if (p->workspace_bytes < ds_f16_slope_workspace(p->rows, p->cols)) return DS_ERR_BUFFER_TOO_SMALL;
+    const Span ws = span(p->workspace, 1, ds_f16_slope_workspace(p->rows, p->cols), ds_f16_slope_workspace(p->rows, p->cols), 1);
+    if (overlap(ws, dy) || overlap(ws, z) || overlap(ws, dz) || overlap(ws, sum)) return DS_ERR_INVALID_ARG;
+    sums = static_cast<float*>(p->workspace);
+  }
+  auto vec16 = [&](const void* q, uint64_t ld) { return !q || (aligned(q, 16) && (p->rows == 1 || ld % 8 == 0)); };
+  const bool vec = vec16(p->dy, p->lddy) && vec16(p->z, p->ldz) && vec16(p->dz, p->lddz);
+  const dim3 grid((uint32_t)((p->cols + 255) / 256), (uint32_t)blocks);
+  launch_pdl(vec ? k_f16_slope<true> : k_f16_slope<false>, grid, dim3(256), st, static_cast<const uint16_t*>(p->dy), p->lddy, static_cast<const uint16_t*>(p->z), p->ldz,
+             (int)p->activation, (int)(p->dtype == DS_BF16), static_cast<uint16_t*>(p->dz), p->lddz, (uint32_t)p->rows, (uint32_t)p->cols, sums);
+  count_launches(1);
+  if (p->sum) {
+    launch_pdl(k_f16_sums, dim3((uint32_t)((p->cols + 31) / 32)), dim3(256), st, (const float*)sums, (uint32_t)blocks, (uint32_t)p->cols, p->sum,
+               (int)(p->sum_dtype == DS_F32), (int)(p->dtype == DS_BF16));
+    count_launches(1);
+  }
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? DS_OK : cuda_fail(e, "gradient through the activation");
+}
+
+}  // extern "C"

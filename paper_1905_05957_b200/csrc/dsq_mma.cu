@@ -71,12 +71,12 @@ cudaError_t make_tensor_map(CUtensorMap* map, int kind, const void* base, uint64
                             uint64_t batch_stride, uint32_t box_cols, uint32_t box_rows, bool block) {
   const EncodeFn fn = encoder();
   if (!fn) return cudaErrorNotSupported;
-  const uint64_t size = kind == kMmaF16 ? 2 : 1;
+  const uint64_t size = kind != kMmaI8 ? 2 : 1;
   const cuuint64_t dims[3] = {cols, rows, batch};
   const cuuint64_t strides[2] = {ld * size, batch_stride * size};   // bytes, of the second and the third dimension
   const cuuint32_t box[3] = {box_cols, box_rows, 1};
   const cuuint32_t step[3] = {1, 1, 1};
-  const CUresult r = fn(map, kind == kMmaF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 3,
+  const CUresult r = fn(map, kind != kMmaI8 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 3,
                         const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                         block ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;

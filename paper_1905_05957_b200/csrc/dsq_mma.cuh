@@ -22,7 +22,7 @@ constexpr int kMmaThreads = 384;          // 4 warps of plumbing, 8 of epilogue
 constexpr int kMmaRows = 128;             // rows of a tile: the lanes of tensor memory
 constexpr long long kWaitCycles = 2000000000ll;   // about one second
 
-enum MmaKind : int { kMmaF16 = 0, kMmaI8 = 1 };
+enum MmaKind : int { kMmaF16 = 0, kMmaI8 = 1, kMmaHalf = 2 };   // kMmaHalf: fp16 or bf16, which of the two the shape says
 
 // ---- PTX ------------------------------------------------------------------------------------------------
 
@@ -85,7 +85,7 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
 }
 template <int KIND>
 __device__ __forceinline__ void tc_mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  if constexpr (KIND == kMmaF16)
+  if constexpr (KIND != kMmaI8)
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
@@ -150,10 +150,12 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint
   return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)((lead >> 4) & 0x3FFFu) << 16) | ((uint64_t)((stride >> 4) & 0x3FFFu) << 32) |
          (1ull << 46) | (2ull << 61);
 }
-// Instruction descriptor: f16 x f16 -> f32, or s8 x s8 -> s32; `rows` x `cols` of C; whether the operands lie across K.
+// Instruction descriptor: f16 x f16 -> f32, bf16 x bf16 -> f32 (kMmaHalf with `bf16`), or s8 x s8 -> s32; `rows` x `cols` of C; whether
+// the operands lie across K.
 template <int KIND>
-__device__ __forceinline__ uint32_t mma_idesc(uint32_t rows, uint32_t cols, bool a_across, bool b_across) {
-  constexpr uint32_t types = KIND == kMmaF16 ? (1u << 4) : ((2u << 4) | (1u << 7) | (1u << 10));
+__device__ __forceinline__ uint32_t mma_idesc(uint32_t rows, uint32_t cols, bool a_across, bool b_across, bool bf16) {
+  uint32_t types = KIND != kMmaI8 ? (1u << 4) : ((2u << 4) | (1u << 7) | (1u << 10));
+  if (KIND == kMmaHalf && bf16) types |= (1u << 7) | (1u << 10);
   return types | (a_across ? 1u << 15 : 0u) | (b_across ? 1u << 16 : 0u) | (cols >> 3 << 17) | (rows >> 4 << 24);
 }
 // The descriptor of instruction q (of four) of a step of 128 bytes of K.
@@ -178,6 +180,7 @@ struct MmaShape {
   uint32_t half;           // 7 or 8: blocks of 2^half of the kSym operands are there
   uint32_t* dev_status;
   uint32_t passes = 1;     // 2: C = A B2 + A B, B and B2 across K: K is gone through for B2 first, then for B
+  uint32_t bf16 = 0;       // kMmaHalf: the operands are bf16, else fp16
 };
 // Step kb of all passes as a step of K, and whether it belongs to B2.
 template <int B_MODE>
@@ -212,7 +215,7 @@ __device__ __forceinline__ void load_operand(const MmaShape& s, uint32_t dst, co
 // and, with kIn or kOut above 0, blocks of 32 x 32 halves that pass through shared memory: kIn of them are fetched by TMA, two
 // blocks ahead, and kOut are stored by TMA.  A row read or written straight from a lane touches 32 lines an instruction; that
 // alone was most of the epilogue of X = a X + B X (1536 x 4608 x 512: 17.6 us, 7.1 without reads and writes).
-//   const CUtensorMap* in(i) const;  const CUtensorMap* out(i) const;     (out: NULL where nothing is stored)
+//   const CUtensorMap* in(i) const;  const CUtensorMap* out(i) const;     (NULL where nothing is read or stored)
 //   void apply(pre, acc, row, col0, batch, smem) const;                   smem: this lane's row of the first block (see row_chunk)
 constexpr uint32_t kBlockBytes = 2048;     // 32 rows of 64 bytes, 64-byte swizzle
 // The 16-byte piece q of a lane's row: pieces are exchanged within a row by the row's number, as TMA lays them.
@@ -249,8 +252,13 @@ struct EpilogueWarp {
   volatile int* gave_up;
 
   __device__ __forceinline__ uint32_t at(uint32_t which) const { return slots + which * Staged<Epi>::kSlot; }
+  static __device__ __forceinline__ bool reads(const Epi& epi) {
+    if constexpr (Epi::kIn > 0) return epi.in(0) != nullptr;
+    return false;
+  }
   __device__ __forceinline__ void fetch(const Epi& epi, uint32_t which, uint32_t row0, uint32_t col0, uint32_t b) {
     if constexpr (Epi::kIn > 0) {
+      if (!epi.in(0)) return;
       if (lane == 0) {
         asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");    // what this slot last held has left it
         mbar_expect_tx(bars + 8 * which, Epi::kIn * kBlockBytes);
@@ -275,7 +283,7 @@ struct EpilogueWarp {
     return finish(epi, pre, acc, row0, col0, b);
   }
   __device__ __forceinline__ bool finish(const Epi& epi, const typename Epi::Pre& pre, const uint32_t (&acc)[32], uint32_t row0, uint32_t col0, uint32_t b) {
-    if constexpr (Epi::kIn > 0) {
+    if (Epi::kIn > 0 && reads(epi)) {
       if (!mbar_wait(bars + 8 * slot, (phases >> slot) & 1, gave_up)) return false;
       phases ^= 1u << slot;
     } else if constexpr (Epi::kOut > 0) {
@@ -309,8 +317,8 @@ struct EpilogueWarp {
     }
   }
   // What is still on its way into this warp's slots when it gives up lands first (`fetched`: loads asked for and not waited for).
-  __device__ __forceinline__ void abandon(int fetched) {
-    if constexpr (Epi::kIn > 0) {
+  __device__ __forceinline__ void abandon(const Epi& epi, int fetched) {
+    if (Epi::kIn > 0 && reads(epi)) {
       for (int i = 0; i < fetched; ++i) {
         const uint32_t which = (slot + i) & 1;
         const long long t0 = clock64();
@@ -336,7 +344,7 @@ struct EpilogueWarp {
     }
     if (cn < blocks) fetch(epi, slot ^ 1, row0, col + 32 * cn, b);
     if (!ready()) {
-      abandon((c < blocks) + (cn < blocks));
+      abandon(epi, (c < blocks) + (cn < blocks));
       return false;
     }
     tc_fence_after();
@@ -346,7 +354,7 @@ struct EpilogueWarp {
       typename Epi::Pre after{};
       if (!block(epi, pre, tmem_at + 32 * c, empty, row0, col + 32 * c, b,
                  [&] { if (cn < blocks) after = epi.load(row0 + lane, col + 32 * cn, b); })) {
-        abandon(1 + (cn < blocks));
+        abandon(epi, 1 + (cn < blocks));
         return false;
       }
       if (nn < blocks) fetch(epi, used, row0, col + 32 * nn, b);
@@ -402,7 +410,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     k_mma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_b2, const MmaShape shape,
           const __grid_constant__ Epi epi) {
   using T = MmaTile<BN, Epi>;
-  constexpr int kBK = KIND == kMmaF16 ? 64 : 128;    // elements of K per stage: 128 bytes
+  constexpr int kBK = KIND != kMmaI8 ? 64 : 128;    // elements of K per stage: 128 bytes
   extern __shared__ uint8_t dyn[];
   __shared__ uint64_t bars[2 * T::kStages + 5 + 16];
   __shared__ uint32_t tmem_slot;
@@ -494,8 +502,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         if (one) {
           const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128;
           const uint32_t k0 = PassStep<B_MODE>(shape, kb, steps).k * kBK;
-          const bool ta = A_MODE == kSym && mirrored(shape, k0, i * kMmaRows), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, j * BN));
-          const uint32_t idesc = mma_idesc<KIND>(kMmaRows, BN, ta, tb);
+          const bool ta = A_MODE == kAcross || (A_MODE == kSym && mirrored(shape, k0, i * kMmaRows)), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, j * BN));
+          const uint32_t idesc = mma_idesc<KIND>(kMmaRows, BN, ta, tb, shape.bf16);
 #pragma unroll
           for (int q = 0; q < 4; ++q)   // four instructions of 32 bytes of K
             tc_mma<KIND>(d, step_desc(sa, q, ta), step_desc(sb, q, tb), idesc, (kb | q) != 0);
@@ -638,7 +646,7 @@ __device__ __forceinline__ void tc_commit_pair(uint32_t bar) {   // arrives at t
 }
 template <int KIND>
 __device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  if constexpr (KIND == kMmaF16)
+  if constexpr (KIND != kMmaI8)
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
@@ -657,7 +665,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
     k_mma_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_b2, const MmaShape shape,
                const __grid_constant__ Epi epi) {
   constexpr int kPairStages = PairTile<Epi>::kStages;
-  constexpr int kBK = KIND == kMmaF16 ? 64 : 128;
+  constexpr int kBK = KIND != kMmaI8 ? 64 : 128;
   extern __shared__ uint8_t dyn[];
   __shared__ uint64_t bars[2 * kPairStages + 5 + 16];
   __shared__ uint32_t tmem_slot;
@@ -723,7 +731,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
           if constexpr (A_MODE == kAlong) {
             tma_load_3d_pair(dst, &map_a, (int)k0, (int)r0, (int)b, bar);
           } else {
-            const bool across = mirrored(shape, k0, row);
+            const bool across = A_MODE == kAcross || mirrored(shape, k0, row);
 #pragma unroll
             for (uint32_t c = 0; c < kMmaRows; c += 64)
               tma_load_3d_pair(dst + c * 128, &map_a, (int)(across ? r0 + c : k0), (int)(across ? k0 : r0 + c), (int)b, bar);
@@ -767,8 +775,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) __cluster_dims__(2, 1, 1)
         if (one) {
           const uint32_t sa = ring + stage * kPairStageBytes, sb = sa + kMmaRows * 128;
           const uint32_t k0 = PassStep<B_MODE>(shape, kb, steps).k * kBK;
-          const bool ta = A_MODE == kSym && mirrored(shape, k0, row), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, col));
-          const uint32_t idesc = mma_idesc<KIND>(2 * kMmaRows, width, ta, tb);
+          const bool ta = A_MODE == kAcross || (A_MODE == kSym && mirrored(shape, k0, row)), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, col));
+          const uint32_t idesc = mma_idesc<KIND>(2 * kMmaRows, width, ta, tb, shape.bf16);
 #pragma unroll
           for (int q = 0; q < 4; ++q) tc_mma_pair<KIND>(d, step_desc(sa, q, ta), step_desc(sb, q, tb), idesc, (kb | q) != 0);
           tc_commit_pair(empty + 8 * stage);
@@ -838,7 +846,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
                 const __grid_constant__ Epi epi,
                 const uint32_t parts) {
   using T = MmaTile<BN, Epi>;
-  constexpr int kBK = KIND == kMmaF16 ? 64 : 128;
+  constexpr int kBK = KIND != kMmaI8 ? 64 : 128;
   constexpr int kTmem = BN < 32 ? 32 : BN == 192 ? 256 : BN;
   constexpr int kBlocks = BN / 32;
   extern __shared__ uint8_t dyn[];
@@ -928,8 +936,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       tc_fence_after();
       if (one) {
         const uint32_t sa = ring + stage * T::kStageBytes, sb = sa + kMmaRows * 128, k0 = PassStep<B_MODE>(shape, k_first + kb, steps).k * kBK;
-        const bool ta = A_MODE == kSym && mirrored(shape, k0, ti * kMmaRows), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, c_first));
-        const uint32_t idesc = mma_idesc<KIND>(kMmaRows, BN, ta, tb);
+        const bool ta = A_MODE == kAcross || (A_MODE == kSym && mirrored(shape, k0, ti * kMmaRows)), tb = B_MODE == kAcross || (B_MODE == kSym && mirrored(shape, k0, c_first));
+        const uint32_t idesc = mma_idesc<KIND>(kMmaRows, BN, ta, tb, shape.bf16);
 #pragma unroll
         for (int q = 0; q < 4; ++q) tc_mma<KIND>(tmem, step_desc(sa, q, ta), step_desc(sb, q, tb), idesc, (kb | q) != 0);
         tc_commit(empty + 8 * stage);
@@ -992,7 +1000,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         }
       }
       if (!ew.finish(epi, pre, acc, row0, c_first + 32 * c, b)) {
-        ew.abandon(1);
+        ew.abandon(epi, 1);
         break;
       }
     }
