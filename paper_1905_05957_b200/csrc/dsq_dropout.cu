@@ -7,16 +7,24 @@ using namespace dsq;
 
 namespace {
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) k_dropout(const T* x, uint64_t ldx, T* out, uint64_t ldo, uint32_t rows, uint32_t cols, int vec, const Drop drop) {
+// A warp has 256 neighbouring entries of a row, blockDim.x / 32 warps side by side, blockDim.y rows at once; two rows in flight a thread.
+template <class T, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_dropout(const T* x, uint64_t ldx, T* out, uint64_t ldo, uint32_t rows, uint32_t cols, const Drop drop) {
   pdl_prologue();
-  const uint32_t c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
-  if (c >= cols) return;
-  for (uint32_t row = blockIdx.y * blockDim.y + threadIdx.y; row < rows; row += gridDim.y * blockDim.y) {
-    float v[8];
-    load8<T>(x, row * ldx, c, cols, vec, v);
-    drop8(drop, drop.threshold ? kept8(drop, row, c) : 0xFFu, v);
-    store8<T>(out, row * ldo, c, cols, vec, v);
+  const uint32_t c = (blockIdx.x * blockDim.x + threadIdx.x) * 8, step = gridDim.y * blockDim.y;
+  const int lane = threadIdx.x & 31;
+  if (c - 8 * lane >= cols) return;
+  for (uint32_t row = blockIdx.y * blockDim.y + threadIdx.y; row < rows; row += 2 * step) {
+    const bool two = row + step < rows;
+    float v[8], u[8];
+    load_row8<VEC>(x + row * ldx, c, cols, lane, v);
+    if (two) load_row8<VEC>(x + (row + step) * ldx, c, cols, lane, u);
+    if (drop.threshold) drop8(drop, draw8(drop, row, c), v);
+    store_row8<VEC>(out + row * ldo, c, cols, lane, v);
+    if (two) {
+      if (drop.threshold) drop8(drop, draw8(drop, row + step, c), u);
+      store_row8<VEC>(out + (row + step) * ldo, c, cols, lane, u);
+    }
   }
 }
 
@@ -24,13 +32,12 @@ inline bool aligned(const void* p, uint64_t to) { return (reinterpret_cast<uintp
 
 template <class T>
 cudaError_t launch(const void* x, uint64_t ldx, void* out, uint64_t ldo, uint32_t rows, uint32_t cols, const Drop& drop, cudaStream_t st) {
-  const uint32_t pieces = (cols + 7) / 8;
-  uint32_t tx = 1;
-  while (tx < kThreads && tx < pieces) tx *= 2;
-  const uint32_t ty = kThreads / tx, gy = (rows + ty - 1) / ty;
-  const int vec = aligned(x, 16) && aligned(out, 16) && (rows == 1 || (ldx * sizeof(T) % 16 == 0 && ldo * sizeof(T) % 16 == 0));
-  launch_pdl(k_dropout<T>, dim3((pieces + tx - 1) / tx, gy < 32768 ? gy : 32768), dim3(tx, ty), st, static_cast<const T*>(x), ldx, static_cast<T*>(out), ldo, rows, cols,
-             vec, drop);
+  const uint32_t warps = (cols + 255) / 256;
+  const uint32_t tx = 32 * (warps < 8 ? warps : 8), ty = kThreads / tx, gx = (warps * 32 + tx - 1) / tx;
+  const bool vec = cols % 8 == 0 && rows_on_boundary(x, ldx, rows, sizeof(T)) && rows_on_boundary(out, ldo, rows, sizeof(T));
+  const uint32_t gy = (rows + ty - 1) / ty;
+  launch_pdl(vec ? k_dropout<T, true> : k_dropout<T, false>, dim3(gx, gy < 32768 ? gy : 32768), dim3(tx, ty), st, static_cast<const T*>(x), ldx, static_cast<T*>(out), ldo,
+             rows, cols, drop);
   count_launches(1);
   return cudaGetLastError();
 }

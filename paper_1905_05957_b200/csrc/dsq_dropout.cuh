@@ -18,19 +18,16 @@ inline Drop make_drop(uint32_t threshold, uint64_t seed, uint32_t layer, uint32_
   return {philox_key_schedule((uint32_t)seed, (uint32_t)(seed >> 32) ^ kDropKey), threshold, layer, step, (float)(65536.0 / (65536.0 - threshold))};
 }
 
-// Bit j: entry c + j of the row is kept (c a multiple of 8).
-__device__ __forceinline__ uint32_t kept8(const Drop& d, uint32_t row, uint32_t c) {
-  const uint4 r = philox4x32_10(make_uint4(c >> 3, row, d.layer, d.step), d.keys);
-  const uint32_t top = d.threshold << 16;
-  uint32_t m = 0;
-  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+// The random words of entries c .. c + 7 of a row (c a multiple of 8).
+__device__ __forceinline__ uint4 draw8(const Drop& d, uint32_t row, uint32_t c) { return philox4x32_10(make_uint4(c >> 3, row, d.layer, d.step), d.keys); }
+// An entry's half in the upper half of a word against the threshold there: the lower half below it makes no difference.
+__device__ __forceinline__ void drop8(const Drop& d, const uint4& r, float (&v)[8]) {
+  const uint32_t top = d.threshold << 16, w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m |= (uint32_t)(w[i] << 16 >= top) << (2 * i) | (uint32_t)(w[i] >= top) << (2 * i + 1);
-  return m;
-}
-__device__ __forceinline__ void drop8(const Drop& d, uint32_t kept, float (&v)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = kept >> j & 1 ? v[j] * d.scale : 0.f;
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = w[i] << 16 >= top ? v[2 * i] * d.scale : 0.f;
+    v[2 * i + 1] = w[i] >= top ? v[2 * i + 1] * d.scale : 0.f;
+  }
 }
 
 }  // namespace dsq

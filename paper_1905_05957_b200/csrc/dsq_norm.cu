@@ -7,386 +7,555 @@
 // statistics that the forward pass left, and what parameters get is summed by CTAs that each take a run of rows, a thread
 // its eight columns, and added up in the CTAs' order: nothing depends on timing.
 #include "dsq_dropout.cuh"
+#include "dsq_mma.cuh"
 #include "dsq_rows8.cuh"
 
 using namespace dsq;
 
 namespace {
 
+// A matrix: its rows are `pitch` bytes apart (a 32-bit number, so that an address is one multiplication).
+struct Rows {
+  const uint8_t* p;              // or NULL
+  uint32_t pitch;
+  __device__ __forceinline__ const uint8_t* at(uint32_t row) const { return p + (uint64_t)row * pitch; }
+  template <class T>
+  __device__ __forceinline__ T* out(uint32_t row) const { return reinterpret_cast<T*>(const_cast<uint8_t*>(at(row))); }
+  __device__ __forceinline__ uint32_t shift(uint32_t row) const { return ((uint32_t)reinterpret_cast<uintptr_t>(p) + row * pitch) & 15; }
+};
 struct NormParams {
-  const void* y;
-  const void* x;                 // or NULL
-  uint64_t ldy, ldx;
+  Rows y, x;
   const float *post_w, *post_b, *gate, *pre_w, *pre_b;      // or NULL
   float residual_scale, eps;
   uint32_t rows, cols, group_rows;      // rows that share a gate
   int layer;                     // layer norms, else RMS
   Drop drop;
   float4* stats;                 // per row: mean and 1/size of y, of h; or NULL
-  // forward
-  void *h, *n;                   // or NULL
-  uint64_t ldh, ldn;
-  // backward
-  const void *dh, *dn;           // or NULL
-  void *dx, *dy;                 // or NULL
-  uint64_t lddh, lddn, lddx, lddy;
-  float *gate_part;              // sums of every unit of rows (of every gate, where a gate's rows are one unit)
-  float *part;                   // sums of every CTA: [grid][kinds][cols]
-  uint32_t units, unit_rows, units_per_group;
+  Rows h, n;                     // forward
+  Rows dh, dn, dx, dy;           // backward
+  float *gate_part;              // sums of every unit of rows (of every gate, where a gate's rows are one unit); or NULL
+  float *part;                   // sums of every CTA: [teams][kinds][cols]
   uint32_t kinds;                // vectors in `part`
   int at_post_w, at_post_b, at_pre_w, at_pre_b;      // their places, or -1
-  int vec;                       // all matrices on 16-byte rows
-  int wvec;                      // all vectors on 16-byte boundaries, and cols a multiple of 4
+  // both: runs of rows with one gate, and how rows are dealt out
+  uint32_t units, unit_rows, units_per_group;
+  uint32_t size;                 // CTAs of a cluster
+  int vec;                       // every row starts on a 16-byte boundary, and cols is a multiple of 8
 };
 
+// ---- how rows are dealt out -----------------------------------------------------------------------------
+// A thread has eight columns.  blockDim.x threads (whole warps, up to 512) have a row, or, above 4096 columns, each CTA of a cluster its share of one; blockDim.y
+// slices of a CTA have rows of their own and go at their own pace.  Units (runs of rows that share a gate) go to teams (CTAs or clusters) in turn, the rows of a unit to
+// slices in turn.
+constexpr uint32_t kNormCols = 4096, kNormThreads = 512;
+
+struct RowWalk {
+  uint32_t unit, row, last;      // row >= last: no more in this unit;  unit >= units: no more at all
+  __device__ __forceinline__ void enter(const NormParams& p, uint32_t u) {
+    unit = u;
+    row = last = 0;
+    if (u >= p.units) return;
+    const uint32_t group = u / p.units_per_group, end = min((group + 1) * p.group_rows, p.rows);
+    const uint32_t first = group * p.group_rows + (u - group * p.units_per_group) * p.unit_rows;
+    last = min(first + p.unit_rows, end);
+    row = first + threadIdx.y;
+  }
+  // to the first unit from u on that has a row for this slice
+  __device__ __forceinline__ void find(const NormParams& p, uint32_t u, uint32_t teams) {
+    enter(p, u);
+    while (row >= last && unit < p.units) enter(p, unit + teams);
+  }
+};
+// ---- rows on their way ----------------------------------------------------------------------------------
+// Each warp copies its 256 columns of the rows to come into shared memory, DEPTH - 1 rows ahead: nothing but the warp itself waits for them, and no
+// registers are held.  A row's granules lie as they do in memory, so rows may start anywhere.
+template <class T>
+constexpr uint32_t kWarpBytes = 32 * 16 * (sizeof(T) / 2) + 16;      // 256 entries, and the granule behind them
+
+// `part`: the warp's part of the row, of which `left` entries are there.
+template <bool VEC, class T>
+__device__ __forceinline__ void fetch_row(uint32_t to, const uint8_t* part, int left, int lane) {
+  constexpr int G = sizeof(T) / 2;
+  const uint32_t shift = VEC ? 0 : shift_of(part);
+  const uint8_t* at = part - shift;
+  const int bytes = left * (int)sizeof(T) + (int)shift;      // up to the row's end
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int i = 16 * (lane + 32 * g);
+    if (i < bytes) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i), "l"(at + i) : "memory");
+  }
+  if (!VEC && shift && lane == 0 && bytes > 512 * G)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * G), "l"(at + 512 * G) : "memory");
+}
+// This lane's eight entries of a row that has arrived; those behind the row's end are 0 (VEC: where nothing arrives, the ring holds zeros).
+template <bool VEC, class T>
+__device__ __forceinline__ void read_row8(uint32_t from, uint32_t shift, int left, int lane, float (&v)[8]) {
+  constexpr int N = kWords<T>;
+  const uint32_t at = from + lane * 4 * N;
+  uint32_t w[N + 4];
+#pragma unroll
+  for (int g = 0; g < N / 4; ++g)
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * g]), "=r"(w[4 * g + 1]), "=r"(w[4 * g + 2]), "=r"(w[4 * g + 3]) : "r"(at + 16 * g) : "memory");
+  if constexpr (!VEC) {
+    if (shift) {
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[N]), "=r"(w[N + 1]), "=r"(w[N + 2]), "=r"(w[N + 3]) : "r"(at + 4 * N) : "memory");
+      take_from<N>(w, shift);
+    }
+  }
+  unpack8<T>(w, v);
+  if (!VEC && left < 8)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j >= left) v[j] = 0.f;
+}
+template <int PENDING>
+__device__ __forceinline__ void wait_rows() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
+  __syncwarp();      // every lane's copies have landed, and every lane is done with the row before
+}
+__device__ __forceinline__ void commit_rows() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
+// VEC: pieces that no row reaches stay zero.
+template <bool VEC>
+__device__ __forceinline__ void clear_ring(uint8_t* ring, uint32_t bytes) {
+  if constexpr (VEC) {
+    for (uint32_t i = (threadIdx.y * blockDim.x + threadIdx.x) * 16; i < bytes; i += blockDim.x * blockDim.y * 16)
+      *reinterpret_cast<uint4*>(ring + i) = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+  }
+}
+
+// Eight entries of a vector of parameters; `none` where there is no vector, 0 behind its end.
+__device__ __forceinline__ void load_param8(const float* p, uint32_t c, uint32_t cols, float none, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? p ? ld_plain(p + c + j) : none : 0.f;
+}
+
 // ---- sums over the threads of a row ---------------------------------------------------------------------
-// blockDim.x threads (whole warps) have a row, blockDim.y rows are in hand.  K values at once, one barrier: the two halves of `red` take turns.
-constexpr int kMostWarps = 32;
-template <int K>
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+struct SumSpace {
+  float warp[2][16][2];      // of each warp; the two halves take turns, so that one barrier is enough
+  float cta[2][8][2];        // of each CTA of a cluster
+};
 struct RowSum {
-  float (*red)[kMostWarps][K];      // [2]
+  SumSpace* space;
+  uint32_t rank, size;
   int turn = 0;
+  template <int K>
   __device__ __forceinline__ void operator()(float (&v)[K]) {
 #pragma unroll
     for (int o = 16; o; o >>= 1)
 #pragma unroll
       for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
     const int warps = blockDim.x >> 5;
-    if (warps == 1) return;
-    const int warp = threadIdx.x >> 5, first = threadIdx.y * warps;
+    if (warps == 1 && size == 1) return;
+    const int first = threadIdx.y * warps;
     if ((threadIdx.x & 31) == 0)
 #pragma unroll
-      for (int k = 0; k < K; ++k) red[turn][first + warp][k] = v[k];
-    __syncthreads();
+      for (int k = 0; k < K; ++k) space->warp[turn][first + (threadIdx.x >> 5)][k] = v[k];
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + threadIdx.y), "r"(blockDim.x) : "memory");      // this slice alone
+    const int l = threadIdx.x & 15;
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = 0.f;
-    for (int w = 0; w < warps; ++w)
+    for (int k = 0; k < K; ++k) v[k] = l < warps ? space->warp[turn][first + l][k] : 0.f;
 #pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += red[turn][first + w][k];
+    for (int o = 8; o; o >>= 1)
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+    if (size > 1) {      // one slice here
+      if (threadIdx.x < size) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          uint32_t to;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&space->cta[turn][rank][k])), "r"(threadIdx.x));
+          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v[k]) : "memory");
+        }
+      }
+      cluster_barrier();
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] = 0.f;
+      for (uint32_t r = 0; r < size; ++r)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] += space->cta[turn][r][k];
+    }
     turn ^= 1;
   }
 };
 
-// ---- forward --------------------------------------------------------------------------------------------
-// A row to blockDim.x threads, NV pieces of eight columns a thread.
-template <class X, class Y, int NV>
-__global__ void __launch_bounds__(1024) k_norm_forward(const NormParams p) {
-  __shared__ float red[2][kMostWarps][1];
-  pdl_prologue();
-  const uint32_t row = blockIdx.x * blockDim.y + threadIdx.y;
-  const bool live = row < p.rows;      // every thread stays for the barriers
-  RowSum<1> sum{red};
-  const float inv = 1.f / (float)p.cols;
-  float v[NV][8];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const uint32_t c = (threadIdx.x + i * blockDim.x) * 8;
-    if (live && c < p.cols)
-      load8<Y>(p.y, row * p.ldy, c, p.cols, p.vec, v[i]);
-    else
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-  }
-  // mean and 1 / size of the rows in v
-  auto statistics = [&](float& mean, float& r) {
-    mean = 0.f;
-    if (p.layer) {
-      float s[1] = {0.f};
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] += v[i][j];
-      sum(s);
-      mean = s[0] * inv;
+// What both passes begin with.
+struct Place {
+  uint32_t rank, team, teams, c, c_warp;
+  int lane, warp, left, left_warp;      // entries of a row from this thread's and this warp's first on
+  __device__ __forceinline__ Place(const NormParams& p) {
+    rank = 0;
+    if (p.size > 1) {
+      asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+      cluster_barrier();      // the others are there before their shared memory is written
     }
-    float q[1] = {0.f};
+    team = blockIdx.x / p.size, teams = gridDim.x / p.size;
+    c = (rank * blockDim.x + threadIdx.x) * 8;
+    lane = threadIdx.x & 31;
+    c_warp = c - 8 * lane;
+    left = entries_left(c, p.cols), left_warp = entries_left(c_warp, p.cols);
+    warp = threadIdx.y * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  }
+};
+
+// ---- forward --------------------------------------------------------------------------------------------
+// FULL: layer norms or biases.  Parameters stay in registers.  A slice has two rows in hand, whose sums share their barriers.
+template <class X, class Y>
+struct ForwardRing {
+  static constexpr int kDepth = 3;                                             // pairs of rows
+  static constexpr uint32_t kRow = kWarpBytes<X> + kWarpBytes<Y>, kWarp = 2 * kRow;      // a warp's part of a row, of a pair
+};
+template <class X, class Y, bool FULL, bool VEC>
+__global__ void __launch_bounds__(kNormThreads, 1) k_norm_forward(const NormParams p) {
+  using R = ForwardRing<X, Y>;
+  extern __shared__ __align__(16) uint8_t ring[];      // [depth][warps][2][y | x]
+  __shared__ SumSpace space;
+  pdl_prologue();
+  const Place at(p);
+  RowSum sum{&space, at.rank, p.size};
+  const uint32_t warps = (blockDim.x >> 5) * blockDim.y, slot_bytes = warps * R::kWarp;
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + at.warp * R::kWarp;
+  const float inv = 1.f / (float)p.cols;
+  clear_ring<VEC>(ring, R::kDepth * slot_bytes);
+  RowWalk ahead, now;
+  uint32_t put = 0, get = 0;
+  ahead.find(p, at.team, at.teams);
+  auto fetch = [&] {
+    if (ahead.unit < p.units) {
+      const uint32_t to = mine + put * slot_bytes;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const uint32_t c = (threadIdx.x + i * blockDim.x) * 8;
-      if (c + 8 <= p.cols) {
+      for (int i = 0; i < 2; ++i)
+        if (ahead.row + i * blockDim.y < ahead.last) {
+          const uint32_t row = ahead.row + i * blockDim.y;
+          fetch_row<VEC, Y>(to + i * R::kRow, p.y.at(row) + at.c_warp * sizeof(Y), at.left_warp, at.lane);
+          if (p.x.p) fetch_row<VEC, X>(to + i * R::kRow + kWarpBytes<Y>, p.x.at(row) + at.c_warp * sizeof(X), at.left_warp, at.lane);
+        }
+      ahead.row += 2 * blockDim.y;
+      if (ahead.row >= ahead.last) ahead.find(p, ahead.unit + at.teams, at.teams);
+    }
+    commit_rows();
+    if (++put == R::kDepth) put = 0;
+  };
+#pragma unroll
+  for (int i = 0; i < R::kDepth - 1; ++i) fetch();
+
+  // parameters: u = hat gw + gb;  n = hat w2 + b2
+  float gw[8], gb[8], w2[8], b2[8];
+  uint32_t group = 0xFFFFFFFFu;
+  load_param8(p.pre_w, at.c, p.cols, 0.f, w2);
+  if constexpr (FULL) load_param8(p.pre_b, at.c, p.cols, 0.f, b2);
+
+  // mean and 1 / size of the two rows
+  auto statistics = [&](const float (&v)[2][8], float (&mean)[2], float (&r)[2]) {
+    mean[0] = mean[1] = 0.f;
+    float q[2] = {0.f, 0.f};
+    if (FULL && p.layer) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mean[i] += v[i][j];
+      sum(mean);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        mean[i] *= inv;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float d = v[i][j] - mean;
-          q[0] = __fmaf_rn(d, d, q[0]);
+          const float d = VEC || j < at.left ? v[i][j] - mean[i] : 0.f;
+          q[i] = __fmaf_rn(d, d, q[i]);
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float d = c + j < p.cols ? v[i][j] - mean : 0.f;
-          q[0] = __fmaf_rn(d, d, q[0]);
-        }
+        if (VEC && at.left <= 0) q[i] = 0.f;      // columns that are not there
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[i] = __fmaf_rn(v[i][j], v[i][j], q[i]);
     }
     sum(q);
-    r = 1.f / sqrtf(__fmaf_rn(q[0], inv, p.eps));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r[i] = rsqrtf(__fmaf_rn(q[i], inv, p.eps));      // good to 2 units of 2^-23
   };
-  float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (p.post_w) statistics(st.x, st.y);
-  const float* gate = p.gate ? p.gate + (uint64_t)(row / p.group_rows) * p.cols : nullptr;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const uint32_t c = (threadIdx.x + i * blockDim.x) * 8;
-    if (!live || c >= p.cols) continue;
-    float t[8];
-    if (p.post_w) {
-      load8<float>(p.post_w, 0, c, p.cols, p.wvec, t);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - st.x) * st.y * t[j];
-      if (p.post_b) {
-        load8<float>(p.post_b, 0, c, p.cols, p.wvec, t);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] += t[j];
-      }
-    }
-    if (gate) {
-      load8<float>(gate, 0, c, p.cols, p.wvec, t);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] *= t[j];
-    }
-    if (p.drop.threshold) drop8(p.drop, kept8(p.drop, row, c), v[i]);
-    if (p.x) {
-      load8<X>(p.x, row * p.ldx, c, p.cols, p.vec, t);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = __fmaf_rn(p.residual_scale, t[j], v[i][j]);
-    }
-    if (p.h) store8<X>(p.h, row * p.ldh, c, p.cols, p.vec, v[i]);
-  }
-  if (p.pre_w) {
-    statistics(st.z, st.w);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const uint32_t c = (threadIdx.x + i * blockDim.x) * 8;
-      if (!live || c >= p.cols) continue;
+  for (now.find(p, at.team, at.teams); now.unit < p.units; now.find(p, now.unit + at.teams, at.teams)) {
+    const uint32_t g = now.unit / p.units_per_group;
+    if (g != group) {
       float t[8];
-      load8<float>(p.pre_w, 0, c, p.cols, p.wvec, t);
+      load_param8(p.post_w, at.c, p.cols, 1.f, gw);
+      if constexpr (FULL) load_param8(p.post_b, at.c, p.cols, 0.f, gb);
+      if (p.gate) {
+        load_param8(p.gate + (uint64_t)g * p.cols, at.c, p.cols, 1.f, t);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - st.z) * st.w * t[j];
-      if (p.pre_b) {
-        load8<float>(p.pre_b, 0, c, p.cols, p.wvec, t);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] += t[j];
+        for (int j = 0; j < 8; ++j) {
+          gw[j] *= t[j];
+          if constexpr (FULL) gb[j] *= t[j];
+        }
       }
-      store8<Y>(p.n, row * p.ldn, c, p.cols, p.vec, v[i]);
+      group = g;
+    }
+    for (; now.row < now.last; now.row += 2 * blockDim.y) {
+      wait_rows<R::kDepth - 2>();
+      fetch();
+      const uint32_t from = mine + get * slot_bytes;
+      if (++get == R::kDepth) get = 0;
+      const bool two = now.row + blockDim.y < now.last;      // else the second row is what the ring held: worked on, not stored
+      const uint32_t row[2] = {now.row, two ? now.row + blockDim.y : now.row};
+      float v[2][8], m1[2] = {0.f, 0.f}, r1[2] = {0.f, 0.f}, m2[2] = {0.f, 0.f}, r2[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) read_row8<VEC, Y>(from + i * R::kRow, VEC ? 0 : p.y.shift(row[i]), at.left, at.lane, v[i]);
+      if (p.post_w) {
+        statistics(v, m1, r1);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = (FULL ? v[i][j] - m1[i] : v[i][j]) * r1[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = FULL ? __fmaf_rn(v[i][j], gw[j], gb[j]) : v[i][j] * gw[j];
+        if (p.drop.threshold) drop8(p.drop, draw8(p.drop, row[i], at.c), v[i]);
+        if (p.x.p) {
+          float t[8];
+          read_row8<VEC, X>(from + i * R::kRow + kWarpBytes<Y>, VEC ? 0 : p.x.shift(row[i]), at.left, at.lane, t);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = __fmaf_rn(p.residual_scale, t[j], v[i][j]);
+        }
+        if (p.h.p && (!i || two)) store_row8<VEC>(p.h.out<X>(row[i]), at.c, p.cols, at.lane, v[i]);
+      }
+      if (p.pre_w) {
+        statistics(v, m2, r2);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            v[i][j] = (FULL ? v[i][j] - m2[i] : v[i][j]) * r2[i];
+            v[i][j] = FULL ? __fmaf_rn(v[i][j], w2[j], b2[j]) : v[i][j] * w2[j];
+          }
+          if (!i || two) store_row8<VEC>(p.n.out<Y>(row[i]), at.c, p.cols, at.lane, v[i]);
+        }
+      }
+      if (p.stats && threadIdx.x == 0 && at.rank == 0) {
+        p.stats[row[0]] = make_float4(m1[0], r1[0], m2[0], r2[0]);
+        if (two) p.stats[row[1]] = make_float4(m1[1], r1[1], m2[1], r2[1]);
+      }
     }
   }
-  if (live && p.stats && threadIdx.x == 0) p.stats[row] = st;
+  if (p.size > 1) cluster_barrier();      // no CTA's shared memory goes away under a neighbour's store
 }
 
 // ---- backward -------------------------------------------------------------------------------------------
 //   d = dh + J_pre^T dn;   dx = a d;   q = g D(d);   dy = J_post^T q
 //   J^T t = r (w t - mean(w t) - hat mean(w t hat)), the second term for layer norms alone
-// A thread has eight columns, blockDim.x threads a part of a row: a whole one, or, above kBackCols columns, its share in a cluster of
-// CTAs, which exchange their sums through distributed shared memory.  blockDim.y rows are in hand at once.
-constexpr uint32_t kBackCols = 4096, kBackThreads = 512;
-
-template <int K>
-struct ClusterSum {
-  float (*red)[kMostWarps][K];
-  float (*peer)[8][K];              // [2][rank]
-  int turn = 0;
-  uint32_t rank, size;
-  __device__ __forceinline__ void operator()(float (&v)[K]) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1)
-#pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
-    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, first = threadIdx.y * warps;
-    if (warps > 1 || size > 1) {
-      if ((threadIdx.x & 31) == 0)
-#pragma unroll
-        for (int k = 0; k < K; ++k) red[turn][first + warp][k] = v[k];
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < K; ++k) v[k] = 0.f;
-      for (int w = 0; w < warps; ++w)
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[k] += red[turn][first + w][k];
-    }
-    if (size > 1) {                 // blockDim.y is 1 here
-      if (threadIdx.x < size) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          uint32_t to;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&peer[turn][rank][k])), "r"(threadIdx.x));
-          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v[k]) : "memory");
-        }
-      }
-      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-#pragma unroll
-      for (int k = 0; k < K; ++k) v[k] = 0.f;
-      for (uint32_t r = 0; r < size; ++r)
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[k] += peer[turn][r][k];
-    }
-    turn ^= 1;
-  }
-};
-
+// A thread sums  A = sum D(d) hat1,  B = sum D(d)  over the rows of a unit, from which the gradients of gate, post weight and bias follow
+// (w1 A + b1 B, g A, g B), and  C = sum dn hat2,  E = sum dn  over all of its rows.
 template <class X, class Y>
-__global__ void __launch_bounds__(kBackThreads, 1) k_norm_backward(const NormParams p, const uint32_t size) {
-  __shared__ float red[2][kMostWarps][2], peer[2][8][2];
-  extern __shared__ float flush[];      // [blockDim.y][blockDim.x * 8]
+struct BackwardRing {
+  static constexpr uint32_t kWarp = 2 * kWarpBytes<X> + 2 * kWarpBytes<Y>;      // y, x, dn, dh
+  static constexpr int kDepth = sizeof(X) + sizeof(Y) == 8 ? 2 : sizeof(X) + sizeof(Y) == 6 ? 3 : 4;
+};
+template <class X, class Y, bool FULL, bool VEC>
+__global__ void __launch_bounds__(kNormThreads, 1) k_norm_backward(const NormParams p) {
+  using R = BackwardRing<X, Y>;
+  extern __shared__ __align__(16) uint8_t ring[];      // [depth][warps][y | x | dn | dh], then sums of the post norm's gradients [2][8][threads], then [threads][8]
+  __shared__ SumSpace space;
   pdl_prologue();
-  uint32_t rank = 0;
-  if (size > 1) {
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // the others are there before their shared memory is written
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  }
-  ClusterSum<2> sum{red, peer, 0, rank, size};
-  const uint32_t width = blockDim.x * 8, c0 = rank * width, c = c0 + threadIdx.x * 8, team = blockIdx.x / size, teams = gridDim.x / size;
+  const Place at(p);
+  RowSum sum{&space, at.rank, p.size};
+  const uint32_t threads = blockDim.x * blockDim.y, warps = threads >> 5, slot_bytes = warps * R::kWarp, tid = threadIdx.y * blockDim.x + threadIdx.x;
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + at.warp * R::kWarp;
+  float* post = reinterpret_cast<float*>(ring + R::kDepth * slot_bytes) + tid;      // a thread's own, `threads` apart
+  float* flush = reinterpret_cast<float*>(ring + R::kDepth * slot_bytes) + 16 * threads;
   const float inv = 1.f / (float)p.cols;
-  const bool mine = c < p.cols;
-  float s_gate[8], s_post_w[8], s_post_b[8], s_pre_w[8], s_pre_b[8];
+  constexpr uint32_t kAtX = kWarpBytes<Y>, kAtDn = kAtX + kWarpBytes<X>, kAtDh = kAtDn + kWarpBytes<Y>;
+  clear_ring<VEC>(ring, R::kDepth * slot_bytes);
+  RowWalk ahead, now;
+  uint32_t put = 0, get = 0;
+  ahead.find(p, at.team, at.teams);
+  auto fetch = [&] {
+    if (ahead.unit < p.units) {
+      const uint32_t to = mine + put * slot_bytes, row = ahead.row;
+      fetch_row<VEC, Y>(to, p.y.at(row) + at.c_warp * sizeof(Y), at.left_warp, at.lane);
+      if (p.x.p) fetch_row<VEC, X>(to + kAtX, p.x.at(row) + at.c_warp * sizeof(X), at.left_warp, at.lane);
+      if (p.dn.p) fetch_row<VEC, Y>(to + kAtDn, p.dn.at(row) + at.c_warp * sizeof(Y), at.left_warp, at.lane);
+      if (p.dh.p) fetch_row<VEC, X>(to + kAtDh, p.dh.at(row) + at.c_warp * sizeof(X), at.left_warp, at.lane);
+      ahead.row += blockDim.y;
+      if (ahead.row >= ahead.last) ahead.find(p, ahead.unit + at.teams, at.teams);
+    }
+    commit_rows();
+    if (++put == R::kDepth) put = 0;
+  };
 #pragma unroll
-  for (int j = 0; j < 8; ++j) s_gate[j] = s_post_w[j] = s_post_b[j] = s_pre_w[j] = s_pre_b[j] = 0.f;
+  for (int i = 0; i < R::kDepth - 1; ++i) fetch();
 
-  // this CTA's sums of one kind, over the rows that were in hand side by side, into a vector
-  auto flush_to = [&](float (&s)[8], float* to) {
-    if (blockDim.y == 1) {
-      if (mine)
+  float w2[8], gw[8], gb[8], s_a[8], s_b[8], s_c[8], s_e[8];
+  load_param8(p.pre_w, at.c, p.cols, 0.f, w2);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < p.cols) to[c + j] = s[j];
+  for (int j = 0; j < 8; ++j) {
+    s_a[j] = s_b[j] = s_c[j] = s_e[j] = 0.f;
+    post[j * threads] = post[(8 + j) * threads] = 0.f;
+  }
+  // what the slices summed of one kind, into a vector
+  auto flush_to = [&](const float (&s)[8], float* to) {
+    const uint32_t width = blockDim.x * 8, c0 = at.rank * width;
+    if (blockDim.y == 1) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (at.c + j < p.cols) to[at.c + j] = s[j];
     } else {
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < 8; ++j) flush[threadIdx.y * width + threadIdx.x * 8 + j] = s[j];
       __syncthreads();
-      for (uint32_t k = threadIdx.y * blockDim.x + threadIdx.x; k < width; k += blockDim.x * blockDim.y) {
+      for (uint32_t k = tid; k < width; k += threads) {
         float v = 0.f;
-        for (uint32_t y = 0; y < blockDim.y; ++y) v += flush[y * width + k];
+        for (uint32_t i = 0; i < blockDim.y; ++i) v += flush[i * width + k];
         if (c0 + k < p.cols) to[c0 + k] = v;
       }
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = 0.f;
   };
 
-  for (uint32_t u = team; u < p.units; u += teams) {
-    const uint32_t group = u / p.units_per_group, r_end = min((group + 1) * p.group_rows, p.rows);
-    const uint32_t first = group * p.group_rows + (u - group * p.units_per_group) * p.unit_rows, last = min(first + p.unit_rows, r_end);
-    for (uint32_t r0 = first; r0 < last; r0 += blockDim.y) {
-      const uint32_t row = r0 + threadIdx.y;
-      const bool live = row < last && mine;
-      float hat1[8], d[8], t[8];
-      float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-      float x[8];
-      if (live) {
-        if (p.stats) st = ld_plain(p.stats + row);
-        load8<Y>(p.y, row * p.ldy, c, p.cols, p.vec, hat1);
-        if (p.x) load8<X>(p.x, row * p.ldx, c, p.cols, p.vec, x);
-      }
-      if (!live)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) hat1[j] = 0.f;
-      if (!live || !p.x)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = 0.f;
-      if (live && p.dh)
-        load8<X>(p.dh, row * p.lddh, c, p.cols, p.vec, d);
-      else
-#pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = 0.f;
-      if (live && p.dn)
-        load8<Y>(p.dn, row * p.lddn, c, p.cols, p.vec, t);
-      else
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = 0.f;
-      // forward again: v = post(y)
-      float v[8], w1[8];
-      const uint32_t kept = p.drop.threshold ? kept8(p.drop, row, c) : 0u;
-      if (p.post_w) {
-        if (live)
-          load8<float>(p.post_w, 0, c, p.cols, p.wvec, w1);
-        else
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w1[j] = 0.f;
+  uint32_t group = 0xFFFFFFFFu;
+  for (uint32_t u = at.team; u < p.units; u += at.teams) {
+    const uint32_t g = u / p.units_per_group;
+    if (g != group) {
+      float t[8];
+      load_param8(p.post_w, at.c, p.cols, 1.f, gw);
+      if constexpr (FULL) load_param8(p.post_b, at.c, p.cols, 0.f, gb);
+      if (p.gate) {
+        load_param8(p.gate + (uint64_t)g * p.cols, at.c, p.cols, 1.f, t);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          hat1[j] = (hat1[j] - st.x) * st.y;
-          v[j] = hat1[j] * w1[j];
+          gw[j] *= t[j];
+          if constexpr (FULL) gb[j] *= t[j];
         }
-        if (p.post_b && live) {
-          float b[8];
-          load8<float>(p.post_b, 0, c, p.cols, p.wvec, b);
+      }
+      group = g;
+    }
+    now.enter(p, u);
+    float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (p.stats && now.row < now.last) st = ld_plain(p.stats + now.row);
+    for (; now.row < now.last; now.row += blockDim.y) {
+      float4 st_next = st;
+      if (p.stats && now.row + blockDim.y < now.last) st_next = ld_plain(p.stats + now.row + blockDim.y);
+      wait_rows<R::kDepth - 2>();
+      fetch();
+      const uint32_t from = mine + get * slot_bytes, row = now.row;
+      if (++get == R::kDepth) get = 0;
+      float hat1[8], d[8];
+      read_row8<VEC, Y>(from, VEC ? 0 : p.y.shift(row), at.left, at.lane, hat1);
+      if (p.post_w) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] += b[j];
-        }
+        for (int j = 0; j < 8; ++j) hat1[j] = (FULL ? hat1[j] - st.x : hat1[j]) * st.y;
+      }
+      uint4 draw = make_uint4(0, 0, 0, 0);
+      if (p.drop.threshold) draw = draw8(p.drop, row, at.c);
+      if (p.dh.p) {
+        read_row8<VEC, X>(from + kAtDh, VEC ? 0 : p.dh.shift(row), at.left, at.lane, d);
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = hat1[j];
+        for (int j = 0; j < 8; ++j) d[j] = 0.f;
       }
-      float g[8];
-      if (p.gate && live)
-        load8<float>(p.gate + (uint64_t)group * p.cols, 0, c, p.cols, p.wvec, g);
-      else
+      if (p.dn.p) {
+        float hat2[8], t[8], s[FULL ? 2 : 1];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = 1.f;
-      if (p.pre_w) {
-        float hat2[8], w2[8], s[2] = {0.f, 0.f};
-        if (live)
-          load8<float>(p.pre_w, 0, c, p.cols, p.wvec, w2);
-        else
+        for (int j = 0; j < 8; ++j) hat2[j] = FULL ? __fmaf_rn(hat1[j], gw[j], gb[j]) : hat1[j] * gw[j];
+        if (p.drop.threshold) drop8(p.drop, draw, hat2);
+        if (p.x.p) {
+          read_row8<VEC, X>(from + kAtX, VEC ? 0 : p.x.shift(row), at.left, at.lane, t);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) w2[j] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) hat2[j] = v[j] * g[j];
-        if (p.drop.threshold) drop8(p.drop, kept, hat2);
+          for (int j = 0; j < 8; ++j) hat2[j] = __fmaf_rn(p.residual_scale, t[j], hat2[j]);
+        }
+        read_row8<VEC, Y>(from + kAtDn, VEC ? 0 : p.dn.shift(row), at.left, at.lane, t);
+        s[0] = 0.f;
+        if constexpr (FULL) s[1] = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          hat2[j] = (__fmaf_rn(p.residual_scale, x[j], hat2[j]) - st.z) * st.w;
-          s_pre_w[j] = __fmaf_rn(t[j], hat2[j], s_pre_w[j]);
-          s_pre_b[j] += t[j];
+          hat2[j] = (FULL ? hat2[j] - st.z : hat2[j]) * st.w;
+          s_c[j] = __fmaf_rn(t[j], hat2[j], s_c[j]);
+          if constexpr (FULL) s_e[j] += t[j];
           t[j] *= w2[j];
-          s[0] += t[j];
-          s[1] = __fmaf_rn(t[j], hat2[j], s[1]);
+          s[0] = __fmaf_rn(t[j], hat2[j], s[0]);
+          if constexpr (FULL) s[1] += t[j];
         }
         sum(s);
-        const float m = p.layer ? s[0] * inv : 0.f, k = s[1] * inv;
+        const float k = s[0] * inv;
+        float m = 0.f;
+        if constexpr (FULL) m = p.layer ? s[1] * inv : 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = __fmaf_rn(st.w, t[j] - m - hat2[j] * k, d[j]);
+        for (int j = 0; j < 8; ++j) d[j] = __fmaf_rn(st.w, __fmaf_rn(-hat2[j], k, FULL ? t[j] - m : t[j]), d[j]);
       }
-      if (live && p.dx) {
+      if (p.dx.p) {
+        float t[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) t[j] = p.residual_scale * d[j];
-        store8<X>(p.dx, row * p.lddx, c, p.cols, p.vec, t);
+        store_row8<VEC>(p.dx.out<X>(row), at.c, p.cols, at.lane, t);
       }
-      if (p.drop.threshold) drop8(p.drop, kept, d);
+      if (p.drop.threshold) drop8(p.drop, draw, d);
+      float s[FULL ? 2 : 1];
+      s[0] = 0.f;
+      if constexpr (FULL) s[1] = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        s_gate[j] = __fmaf_rn(d[j], v[j], s_gate[j]);
-        d[j] *= g[j];
+        s_a[j] = __fmaf_rn(d[j], hat1[j], s_a[j]);
+        if constexpr (FULL) s_b[j] += d[j];
+        d[j] *= gw[j];
+        s[0] = __fmaf_rn(d[j], hat1[j], s[0]);
+        if constexpr (FULL) s[1] += d[j];
       }
       if (p.post_w) {
-        float s[2] = {0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          s_post_w[j] = __fmaf_rn(d[j], hat1[j], s_post_w[j]);
-          s_post_b[j] += d[j];
-          d[j] *= w1[j];
-          s[0] += d[j];
-          s[1] = __fmaf_rn(d[j], hat1[j], s[1]);
-        }
         sum(s);
-        const float m = p.layer ? s[0] * inv : 0.f, k = s[1] * inv;
+        const float k = s[0] * inv;
+        float m = 0.f;
+        if constexpr (FULL) m = p.layer ? s[1] * inv : 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = st.y * (d[j] - m - hat1[j] * k);
+        for (int j = 0; j < 8; ++j) d[j] = st.y * __fmaf_rn(-hat1[j], k, FULL ? d[j] - m : d[j]);
       }
-      if (live && p.dy) store8<Y>(p.dy, row * p.lddy, c, p.cols, p.vec, d);
+      if (p.dy.p) store_row8<VEC>(p.dy.out<Y>(row), at.c, p.cols, at.lane, d);
+      st = st_next;
     }
-    if (p.gate_part) flush_to(s_gate, p.gate_part + (uint64_t)u * p.cols);
+    if (p.gate_part) {
+      float t[8], w[8];
+      load_param8(p.post_w, at.c, p.cols, 1.f, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = w[j] * s_a[j];
+      if constexpr (FULL) {
+        load_param8(p.post_b, at.c, p.cols, 0.f, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = __fmaf_rn(w[j], s_b[j], t[j]);
+      }
+      flush_to(t, p.gate_part + (uint64_t)u * p.cols);
+    }
+    if (p.at_post_w >= 0) {
+      float t[8];
+      load_param8(p.gate ? p.gate + (uint64_t)g * p.cols : nullptr, at.c, p.cols, 1.f, t);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        post[j * threads] = __fmaf_rn(t[j], s_a[j], post[j * threads]);
+        if constexpr (FULL) post[(8 + j) * threads] = __fmaf_rn(t[j], s_b[j], post[(8 + j) * threads]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s_a[j] = s_b[j] = 0.f;
   }
-  float* part = p.part + (uint64_t)team * p.kinds * p.cols;
-  if (p.at_post_w >= 0) flush_to(s_post_w, part + (uint64_t)p.at_post_w * p.cols);
-  if (p.at_post_b >= 0) flush_to(s_post_b, part + (uint64_t)p.at_post_b * p.cols);
-  if (p.at_pre_w >= 0) flush_to(s_pre_w, part + (uint64_t)p.at_pre_w * p.cols);
-  if (p.at_pre_b >= 0) flush_to(s_pre_b, part + (uint64_t)p.at_pre_b * p.cols);
-  if (size > 1) {      // no CTA's shared memory goes away under a neighbour's store
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  float* part = p.part + (uint64_t)at.team * p.kinds * p.cols;
+  if (p.at_post_w >= 0) {
+    float t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = post[j * threads];
+    flush_to(t, part + (uint64_t)p.at_post_w * p.cols);
+    if (FULL && p.at_post_b >= 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = post[(8 + j) * threads];
+      flush_to(t, part + (uint64_t)p.at_post_b * p.cols);
+    }
   }
+  if (p.at_pre_w >= 0) flush_to(s_c, part + (uint64_t)p.at_pre_w * p.cols);
+  if (FULL && p.at_pre_b >= 0) flush_to(s_e, part + (uint64_t)p.at_pre_b * p.cols);
+  if (p.size > 1) cluster_barrier();      // no CTA's shared memory goes away under a neighbour's store
 }
 
 // The CTAs' sums, added in their order: out[v] = sum_i in[v * stride_v + i * stride_i].
@@ -424,64 +593,53 @@ inline bool aligned(const void* p, uint64_t to) { return (reinterpret_cast<uintp
 inline uint32_t size_of(uint64_t dtype) { return dtype == DS_F32 ? 4 : 2; }
 constexpr uint64_t kMaxRows = 1ull << 30;
 
-int sms() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 148;
-  return n;
-}
-
-// How the backward pass is cut.
-struct BackPlan {
+// How a pass is cut.
+struct NormPlan {
   uint32_t size;              // CTAs of a cluster
-  uint32_t tx, ty;            // threads of a row (or of its share), rows in hand
+  uint32_t tx, ty;            // threads of a row (or of its share), slices
   uint32_t units, unit_rows, units_per_group, teams;
   uint64_t gate_bytes, part_bytes;
 };
-BackPlan back_plan(const ds_norm_args* p) {
-  BackPlan b;
+NormPlan norm_plan(const ds_norm_args* p) {
+  NormPlan b;
   const uint64_t cols = p->cols, groups = p->groups ? p->groups : 1, group_rows = p->rows / groups;
   b.size = 1;
-  while (b.size * (uint64_t)kBackCols < cols) b.size *= 2;
+  while (b.size * (uint64_t)kNormCols < cols) b.size *= 2;
   const uint32_t pieces = (uint32_t)((cols + 8 * b.size - 1) / (8 * b.size));
   b.tx = (uint32_t)round_up(pieces, 32);
-  b.ty = b.size > 1 ? 1 : kBackThreads / b.tx;
-  if (b.ty > group_rows) b.ty = group_rows ? (uint32_t)group_rows : 1;
-  const uint64_t want = (uint64_t)sms() / b.size;      // teams that run at once
-  // a group's rows are cut where there are fewer groups than teams, into units of at least one row a slice
-  uint64_t per = groups >= want ? 1 : (want + groups - 1) / groups;
+  b.ty = b.size > 1 ? 1 : kNormThreads / b.tx;
+  // as many teams as run at once (one CTA an SM); with few rows a team has fewer slices, so that all of the device works
+  const uint64_t want = b.size > 1 ? (cluster_count(b.size) ? cluster_count(b.size) : 1) : sm_count();
+  while (b.ty > 1 && p->rows < want * b.ty) --b.ty;
+  // Units of a group: so many that the team with most rows has fewest (units go to teams in turn); tried for one to four units a team.
   const uint64_t most = (group_rows + b.ty - 1) / b.ty;
-  if (per > most) per = most ? most : 1;
-  b.unit_rows = (uint32_t)round_up((group_rows + per - 1) / per, b.ty);
-  if (!b.unit_rows) b.unit_rows = 1;
-  b.units_per_group = group_rows ? (uint32_t)((group_rows + b.unit_rows - 1) / b.unit_rows) : 1;
+  uint64_t least = ~0ull;
+  for (uint64_t k = 1; k <= 4; ++k) {
+    uint64_t per = k * want / groups;
+    per = per < 1 ? 1 : per > most ? most : per;
+    const uint64_t rows = round_up((group_rows + per - 1) / per, b.ty), units = (group_rows + rows - 1) / rows, cost = (units * groups + want - 1) / want * (rows / b.ty);
+    if (cost < least) {
+      least = cost;
+      b.unit_rows = (uint32_t)rows;
+      b.units_per_group = (uint32_t)units;
+    }
+  }
   b.units = (uint32_t)(b.units_per_group * groups);
   b.teams = b.units < want ? b.units : (uint32_t)want;
-  const uint32_t kinds = (p->d_post_w != nullptr) + (p->d_post_b != nullptr) + (p->d_pre_w != nullptr) + (p->d_pre_b != nullptr);
+  const uint32_t kinds = (p->d_post_w != nullptr || p->d_post_b != nullptr) + (p->d_post_b != nullptr) + (p->d_pre_w != nullptr) + (p->d_pre_b != nullptr);
   b.gate_bytes = p->d_gate && b.units_per_group > 1 ? round_up(4ull * b.units * cols, 256) : 0;
   b.part_bytes = 4ull * b.teams * kinds * cols;
   return b;
 }
 
-template <class X, class Y>
-cudaError_t forward(const NormParams& q, cudaStream_t st) {
-  const uint32_t pieces = (q.cols + 7) / 8;
-  auto go = [&](auto kernel, uint32_t nv) {
-    const uint32_t tx = (uint32_t)round_up((pieces + nv - 1) / nv, 32), ty = tx >= 256 ? 1 : 256 / tx;
-    launch_pdl(kernel, dim3((q.rows + ty - 1) / ty), dim3(tx, ty), st, q);
-    count_launches(1);
-    return cudaGetLastError();
-  };
-  if (pieces <= 512) return go(k_norm_forward<X, Y, 1>, 1);
-  if (pieces <= 1024) return go(k_norm_forward<X, Y, 2>, 2);
-  return go(k_norm_forward<X, Y, 4>, 4);
-}
-
-template <class X, class Y>
-cudaError_t backward(const NormParams& q, const BackPlan& b, cudaStream_t st) {
+template <auto KERNEL>
+cudaError_t launch(NormParams q, const NormPlan& b, uint32_t smem, uint32_t most, cudaStream_t st) {
+  allow_smem_for<KERNEL>(most);
+  q.units = b.units, q.unit_rows = b.unit_rows, q.units_per_group = b.units_per_group, q.size = b.size;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(b.teams * b.size);
   cfg.blockDim = dim3(b.tx, b.ty);
-  cfg.dynamicSmemBytes = b.ty > 1 ? b.tx * b.ty * 32 : 0;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -491,9 +649,26 @@ cudaError_t backward(const NormParams& q, const BackPlan& b, cudaStream_t st) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = b.size > 1 ? 2 : 1;
-  (void)cudaLaunchKernelEx(&cfg, k_norm_backward<X, Y>, q, b.size);
+  (void)cudaLaunchKernelEx(&cfg, KERNEL, q);
   count_launches(1);
   return cudaGetLastError();
+}
+inline bool full(const NormParams& q) { return q.layer || q.post_b || q.pre_b; }
+template <class X, class Y>
+cudaError_t forward(const NormParams& q, const NormPlan& b, cudaStream_t st) {
+  using R = ForwardRing<X, Y>;
+  constexpr uint32_t kThread = R::kDepth * R::kWarp / 32;      // bytes a thread
+  const uint32_t smem = b.tx * b.ty * kThread, most = kNormThreads * kThread;
+  if (q.vec) return full(q) ? launch<k_norm_forward<X, Y, true, true>>(q, b, smem, most, st) : launch<k_norm_forward<X, Y, false, true>>(q, b, smem, most, st);
+  return full(q) ? launch<k_norm_forward<X, Y, true, false>>(q, b, smem, most, st) : launch<k_norm_forward<X, Y, false, false>>(q, b, smem, most, st);
+}
+template <class X, class Y>
+cudaError_t backward(const NormParams& q, const NormPlan& b, cudaStream_t st) {
+  using R = BackwardRing<X, Y>;
+  constexpr uint32_t kThread = R::kDepth * R::kWarp / 32 + 64 + 32;
+  const uint32_t smem = b.tx * b.ty * kThread, most = kNormThreads * kThread;
+  if (q.vec) return full(q) ? launch<k_norm_backward<X, Y, true, true>>(q, b, smem, most, st) : launch<k_norm_backward<X, Y, false, true>>(q, b, smem, most, st);
+  return full(q) ? launch<k_norm_backward<X, Y, true, false>>(q, b, smem, most, st) : launch<k_norm_backward<X, Y, false, false>>(q, b, smem, most, st);
 }
 
 template <class F>
@@ -533,6 +708,11 @@ int check(const ds_norm_args* p, bool back) {
   if (!p->y) return DS_ERR_INVALID_ARG;
   const bool many = p->rows > 1;
   auto narrow = [&](const void* q, uint64_t ld) { return many && q && ld < p->cols; };
+  // rows 2^30 entries apart at most: addresses are made with 32-bit pitches
+  auto far = [&](const void* q, uint64_t ld) { return many && q && ld >= 1ull << 30; };
+  if (far(p->y, p->ldy) || far(p->x, p->ldx) || (!back && (far(p->h, p->ldh) || far(p->n, p->ldn))) ||
+      (back && (far(p->dh, p->lddh) || far(p->dn, p->lddn) || far(p->dx, p->lddx) || far(p->dy, p->lddy))))
+    return DS_ERR_UNSUPPORTED;
   if (narrow(p->y, p->ldy) || narrow(p->x, p->ldx)) return DS_ERR_INVALID_ARG;
   if (!back) {
     if (narrow(p->h, p->ldh) || narrow(p->n, p->ldn)) return DS_ERR_INVALID_ARG;
@@ -547,23 +727,24 @@ int check(const ds_norm_args* p, bool back) {
   return DS_OK;
 }
 
-NormParams params(const ds_norm_args* p) {
+NormParams params(const ds_norm_args* p, bool back) {
   NormParams q{};
-  q.y = p->y, q.x = p->x, q.ldy = p->ldy, q.ldx = p->ldx;
   q.post_w = p->post_w, q.post_b = p->post_b, q.gate = p->gate, q.pre_w = p->pre_w, q.pre_b = p->pre_b;
   q.residual_scale = (float)p->residual_scale, q.eps = (float)p->eps;
   q.rows = (uint32_t)p->rows, q.cols = (uint32_t)p->cols, q.group_rows = (uint32_t)(p->rows / (p->groups ? p->groups : 1));
   q.layer = p->norm == DS_NORM_LAYER;
   q.drop = make_drop((uint32_t)p->threshold, p->seed, (uint32_t)p->layer, (uint32_t)p->step);
   q.stats = reinterpret_cast<float4*>(p->stats);
-  bool vec = true;
-  auto see = [&](const void* m, uint64_t ld, uint32_t size) { vec = vec && (!m || (aligned(m, 16) && (p->rows == 1 || ld * size % 16 == 0))); };
   const uint32_t sy = size_of(p->dtype), sx = size_of(p->stream_dtype);
-  see(p->y, p->ldy, sy), see(p->x, p->ldx, sx), see(p->h, p->ldh, sx), see(p->n, p->ldn, sy);
-  see(p->dh, p->lddh, sx), see(p->dn, p->lddn, sy), see(p->dx, p->lddx, sx), see(p->dy, p->lddy, sy);
-  q.vec = vec;
-  q.wvec = aligned(p->post_w, 16) && aligned(p->post_b, 16) && aligned(p->gate, 16) && aligned(p->pre_w, 16) && aligned(p->pre_b, 16) &&
-           (p->groups <= 1 || p->cols % 4 == 0);
+  auto rows = [&](const void* m, uint64_t ld, uint32_t size) { return Rows{static_cast<const uint8_t*>(m), p->rows > 1 ? (uint32_t)(ld * size) : 0}; };
+  q.y = rows(p->y, p->ldy, sy), q.x = rows(p->x, p->ldx, sx);
+  if (back)
+    q.dh = rows(p->dh, p->lddh, sx), q.dn = rows(p->dn, p->lddn, sy), q.dx = rows(p->dx, p->lddx, sx), q.dy = rows(p->dy, p->lddy, sy);
+  else
+    q.h = rows(p->h, p->ldh, sx), q.n = rows(p->n, p->ldn, sy);
+  auto on = [&](const void* m, uint64_t ld, uint32_t size) { return rows_on_boundary(m, ld, p->rows, size); };
+  q.vec = p->cols % 8 == 0 && on(p->y, p->ldy, sy) && on(p->x, p->ldx, sx) && on(p->h, p->ldh, sx) && on(p->n, p->ldn, sy) && on(p->dh, p->lddh, sx) &&
+          on(p->dn, p->lddn, sy) && on(p->dx, p->lddx, sx) && on(p->dy, p->lddy, sy);
   return q;
 }
 
@@ -583,15 +764,15 @@ int ds_norm_forward(const ds_norm_args* p, void* cuda_stream) {
       (overlap(n, x) && !over(p->n, p->ldn, sy, p->x, p->ldx, sx)) || (overlap(n, y) && !over(p->n, p->ldn, sy, p->y, p->ldy, sy)) || overlap(h, n) ||
       overlap(stats, h) || overlap(stats, n) || overlap(stats, x) || overlap(stats, y))
     return DS_ERR_INVALID_ARG;
-  NormParams q = params(p);
-  q.h = p->h, q.ldh = p->ldh, q.n = p->n, q.ldn = p->ldn;
-  const cudaError_t e = by_types(p, [&](auto sx_, auto sy_) { return forward<decltype(sx_), decltype(sy_)>(q, static_cast<cudaStream_t>(cuda_stream)); });
+  const NormParams q = params(p, false);
+  const NormPlan b = norm_plan(p);
+  const cudaError_t e = by_types(p, [&](auto sx_, auto sy_) { return forward<decltype(sx_), decltype(sy_)>(q, b, static_cast<cudaStream_t>(cuda_stream)); });
   return e == cudaSuccess ? DS_OK : cuda_fail(e, "norms around a residual connection");
 }
 
 uint64_t ds_norm_backward_workspace(const ds_norm_args* p) {
   if (check(p, true) != DS_OK || p->rows == 0) return 0;
-  const BackPlan b = back_plan(p);
+  const NormPlan b = norm_plan(p);
   return b.gate_bytes + b.part_bytes;
 }
 
@@ -609,7 +790,7 @@ int ds_norm_backward(const ds_norm_args* p, void* cuda_stream) {
     return DS_OK;
   }
   const uint32_t sy = size_of(p->dtype), sx = size_of(p->stream_dtype);
-  const BackPlan b = back_plan(p);
+  const NormPlan b = norm_plan(p);
   const uint64_t ws = b.gate_bytes + b.part_bytes;
   if (ws) {
     if (!p->workspace) return DS_ERR_INVALID_ARG;
@@ -643,10 +824,7 @@ int ds_norm_backward(const ds_norm_args* p, void* cuda_stream) {
     for (int j = 0; j < 5; ++j)
       if (overlap(small[i], region(weights[j], 1, j == 4 ? p->groups * p->cols : p->cols, 0, 4))) return DS_ERR_INVALID_ARG;
   }
-  NormParams q = params(p);
-  q.dh = p->dh, q.dn = p->dn, q.dx = p->dx, q.dy = p->dy;
-  q.lddh = p->lddh, q.lddn = p->lddn, q.lddx = p->lddx, q.lddy = p->lddy;
-  q.units = b.units, q.unit_rows = b.unit_rows, q.units_per_group = b.units_per_group;
+  NormParams q = params(p, true);
   uint8_t* space_p = static_cast<uint8_t*>(p->workspace);
   q.gate_part = !p->d_gate ? nullptr : b.gate_bytes ? reinterpret_cast<float*>(space_p) : p->d_gate;
   q.at_post_w = q.at_post_b = q.at_pre_w = q.at_pre_b = -1;
@@ -657,7 +835,7 @@ int ds_norm_backward(const ds_norm_args* p, void* cuda_stream) {
   float* outs_p[4] = {p->d_post_w, p->d_post_b, p->d_pre_w, p->d_pre_b};
   int* places[4] = {&q.at_post_w, &q.at_post_b, &q.at_pre_w, &q.at_pre_b};
   for (int i = 0; i < 4; ++i)
-    if (outs_p[i]) *places[i] = kinds++;
+    if (outs_p[i] || (i == 0 && p->d_post_b)) *places[i] = kinds++;      // the bias's sums come with the weight's
   q.kinds = (uint32_t)kinds;
   q.part = part;
   for (int i = 0; i < 4; ++i)

@@ -1,4 +1,7 @@
-// Eight neighbouring entries of a row, as floats.
+// Eight neighbouring entries of a row, as floats: rows may start anywhere.  Memory is read and written in whole 16-byte granules; a warp holds 256 neighbouring
+// entries, eight a lane, and where a row starts `shift` bytes behind a boundary a lane takes what it lacks from the granule behind its own, or hands over
+// the end of its own to the next lane.  (Entry by entry, a warp's 2-byte accesses touch every sector eight times: dropout of 16384 x 8191 in bf16 took 314 us
+// so, and 120 with 8192 columns.)  A granule is read only if it holds an entry of the row; what else it holds is dropped.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -21,13 +24,15 @@ __device__ __forceinline__ T from_float(float v) {
   else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(v);
   else return __float2bfloat16_rn(v);
 }
+// Words of eight entries.
 template <class T>
-__device__ __forceinline__ void unpack8(const uint4 (&q)[sizeof(T) / 2], float (&v)[8]) {
+constexpr int kWords = 2 * sizeof(T);
+template <class T>
+__device__ __forceinline__ void unpack8(const uint32_t* w, float (&v)[8]) {
   if constexpr (sizeof(T) == 4) {
-    v[0] = __uint_as_float(q[0].x), v[1] = __uint_as_float(q[0].y), v[2] = __uint_as_float(q[0].z), v[3] = __uint_as_float(q[0].w);
-    v[4] = __uint_as_float(q[1].x), v[5] = __uint_as_float(q[1].y), v[6] = __uint_as_float(q[1].z), v[7] = __uint_as_float(q[1].w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
   } else {
-    const uint32_t w[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (std::is_same<T, __nv_bfloat16>::value) {
@@ -39,38 +44,142 @@ __device__ __forceinline__ void unpack8(const uint4 (&q)[sizeof(T) / 2], float (
     }
   }
 }
-// Entries behind the row's end are 0.
 template <class T>
-__device__ __forceinline__ void load8(const void* base, uint64_t at, uint32_t c, uint32_t cols, bool vec, float (&v)[8]) {
-  const T* p = static_cast<const T*>(base) + at + c;
-  if (vec && c + 8 <= cols) {
-    uint4 q[sizeof(T) / 2];
+__device__ __forceinline__ void pack8(const float (&v)[8], uint32_t* w) {
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = ld_plain(reinterpret_cast<const uint4*>(p) + i);
-    unpack8<T>(q, v);
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? to_float(ld_plain(p + j)) : 0.f;
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      } else {
+        const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+    }
   }
 }
-template <class T>
-__device__ __forceinline__ void store8(void* base, uint64_t at, uint32_t c, uint32_t cols, bool vec, const float (&v)[8]) {
-  T* p = static_cast<T*>(base) + at + c;
-  if (vec && c + 8 <= cols) {
-    if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      T t[8];
+
+// w[0..N): the bytes from `shift` on (0..15, a multiple of the entries' size).
+template <int N>
+__device__ __forceinline__ void take_from(uint32_t (&w)[N + 4], uint32_t shift) {
+  if (shift & 8)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[j] = from_float<T>(v[j]);
-      *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(t);
+    for (int i = 0; i < N + 2; ++i) w[i] = w[i + 2];
+  if (shift & 4)
+#pragma unroll
+    for (int i = 0; i < N + 1; ++i) w[i] = w[i + 1];
+  if (shift & 2)
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+}
+
+__device__ __forceinline__ uint32_t shift_of(const void* row) { return (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15); }
+
+// Entries from c on, not counted far: so that bytes fit into 32 bits.
+__device__ __forceinline__ int entries_left(uint32_t c, uint32_t cols) {
+  const int left = (int)(cols - c);
+  return left < 4096 ? left : 4096;
+}
+
+// Entries c .. c + 7 of a row of `cols`, lane l of a whole warp those 8 l behind lane 0's.  Entries behind the row's end are 0.
+// VEC: every row starts on a 16-byte boundary and cols is a multiple of 8.
+template <bool VEC, class T>
+__device__ __forceinline__ void load_row8(const T* row, uint32_t c, uint32_t cols, int lane, float (&v)[8]) {
+  constexpr int N = kWords<T>;
+  uint32_t w[N + 4];
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = 0;
+  const uint32_t shift = VEC ? 0 : shift_of(row);
+  const uint8_t* at = reinterpret_cast<const uint8_t*>(row + c) - shift;
+  // the granules that hold something of this row
+  const int bytes = VEC ? (c < cols ? 4 * N : 0) : entries_left(c, cols) * (int)sizeof(T) + (int)shift;
+#pragma unroll
+  for (int g = 0; g < N / 4; ++g)
+    if (16 * g < bytes) {
+      const uint4 q = ld_plain(reinterpret_cast<const uint4*>(at) + g);
+      w[4 * g] = q.x, w[4 * g + 1] = q.y, w[4 * g + 2] = q.z, w[4 * g + 3] = q.w;
     }
-  } else {
+  if (!VEC && shift) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[N + i] = __shfl_down_sync(0xFFFFFFFFu, w[i], 1);
+    if (lane == 31 && 4 * N < bytes) {
+      const uint4 q = ld_plain(reinterpret_cast<const uint4*>(at) + N / 4);
+      w[N] = q.x, w[N + 1] = q.y, w[N + 2] = q.z, w[N + 3] = q.w;
+    }
+    take_from<N>(w, shift);
+  }
+  unpack8<T>(w, v);
+  if (!VEC && c + 8 > cols)
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (c + j < cols) p[j] = from_float<T>(v[j]);
+      if (c + j >= cols) v[j] = 0.f;
+}
+
+// The other way round.  The whole warp calls it, lanes behind the row's end, too.
+template <bool VEC, class T>
+__device__ __forceinline__ void store_row8(T* row, uint32_t c, uint32_t cols, int lane, const float (&v)[8]) {
+  constexpr int N = kWords<T>, kEach = 16 / sizeof(T);
+  uint32_t w[N + 4];
+  if constexpr (VEC) {
+    if (c >= cols) return;
+    pack8<T>(v, w);
+#pragma unroll
+    for (int g = 0; g < N / 4; ++g) reinterpret_cast<uint4*>(row + c)[g] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+    return;
   }
+  const uint32_t shift = shift_of(row);
+  const int left = entries_left(c, cols) * (int)sizeof(T);      // bytes of the row from entry c on
+  if (!shift) {
+    pack8<T>(v, w);
+    uint4* to = reinterpret_cast<uint4*>(row + c);
+#pragma unroll
+    for (int g = 0; g < N / 4; ++g)
+      if (16 * (g + 1) <= left) {
+        to[g] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+      } else if (16 * g < left) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+          if (c + g * kEach + j < cols) row[c + g * kEach + j] = from_float<T>(v[g * kEach + j]);
+      }
+    return;
+  }
+  // granule g holds `shift` bytes of what comes before it (of the lane before, for the first one), then this lane's
+  pack8<T>(v, w + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xFFFFFFFFu, w[N + i], 1);
+  const uint32_t last[4] = {w[N], w[N + 1], w[N + 2], w[N + 3]};      // this lane's own last 16 bytes
+  take_from<N>(w, 16 - shift);
+  uint8_t* at = reinterpret_cast<uint8_t*>(row + c) - shift;
+  const int s = (int)shift;
+  auto put = [&](int i, uint32_t word, int byte) {      // the entry at byte i of the granules
+    if constexpr (sizeof(T) == 4)
+      *reinterpret_cast<uint32_t*>(at + i) = word;
+    else
+      *reinterpret_cast<uint16_t*>(at + i) = (uint16_t)(byte ? word >> 16 : word);
+  };
+#pragma unroll
+  for (int g = 0; g < N / 4; ++g) {
+    if ((g || lane) && 16 * (g + 1) - s <= left) {
+      reinterpret_cast<uint4*>(at)[g] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+    } else if (16 * g - s < left) {      // the row's end, or what begins a warp
+#pragma unroll
+      for (int i = 16 * g; i < 16 * g + 16; i += sizeof(T))
+        if (i - s < left && (lane || i >= s)) put(i, w[i / 4], i & 2);
+    }
+  }
+  if (lane == 31)      // what this lane would hand over
+#pragma unroll
+    for (int i = 0; i < 16; i += sizeof(T))
+      if (i >= 16 - s && 4 * N - 16 + i < left) put(4 * N - 16 + i + s, last[i / 4], i & 2);
+}
+
+// Whether rows of a matrix start on 16-byte boundaries (or it is not there).
+inline bool rows_on_boundary(const void* p, uint64_t ld, uint64_t rows, uint32_t size) {
+  return !p || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && (rows <= 1 || ld * size % 16 == 0));
 }
 
 }  // namespace dsq
