@@ -3,6 +3,7 @@
 #include <type_traits>
 
 #include "dsq_product16.cuh"
+#include "dsq_rows8.cuh"
 
 using namespace dsq;
 
@@ -33,60 +34,36 @@ inline bool overlap(const Span& a, const Span& b) {
 }
 
 // ---- copies onto 16-byte rows ---------------------------------------------------------------------------
-// Bound by memory; a thread takes eight entries of a row.  Entries behind a row's end become 0.
-template <class T>
-__global__ void __launch_bounds__(kThreads) k_f16_pack(const T* x, uint64_t ld, uint32_t cols, int from_bf16, uint16_t* out, uint64_t ldo, int bf16, int vec) {
+// Bound by memory; a lane takes eight entries of a row.  Entries behind a row's end become 0.
+template <class T, class O>
+__global__ void __launch_bounds__(kThreads) k_f16_pack(const T* x, uint64_t ld, uint32_t rows, uint32_t cols, O* out, uint64_t ldo) {
   pdl_prologue();
-  const uint32_t c = (blockIdx.x * kThreads + threadIdx.x) * 8;
-  if (c >= ldo) return;
-  const uint64_t r = blockIdx.y + (uint64_t)gridDim.y * blockIdx.z;
-  const T* row = x + r * ld;
-  uint32_t w[4];
-  if constexpr (sizeof(T) == 4) {
+  const uint32_t c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  const int lane = threadIdx.x & 31;
+  if (c - 8 * lane >= ldo) return;
+  for (uint32_t r = blockIdx.y * blockDim.y + threadIdx.y; r < rows; r += gridDim.y * blockDim.y) {
     float v[8];
-    if (vec && c + 8 <= cols) {
-      const float4 a = ld_plain(reinterpret_cast<const float4*>(row + c)), b = ld_plain(reinterpret_cast<const float4*>(row + c) + 1);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? ld_plain(row + c + j) : 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = halves_of(v[2 * j], v[2 * j + 1], bf16);
-  } else {
-    uint16_t h[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = c + j < cols ? ld_plain(row + c + j) : (uint16_t)0;
-    if (from_bf16 == bf16) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = h[2 * j] | (uint32_t)h[2 * j + 1] << 16;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = halves_of(from_half(h[2 * j], from_bf16), from_half(h[2 * j + 1], from_bf16), bf16);
-    }
+    load_row8<false>(x + r * ld, c, cols, lane, v);
+    store_row8<true>(out + r * ldo, c, (uint32_t)ldo, lane, v);
   }
-  *reinterpret_cast<uint4*>(out + r * ldo + c) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-cudaError_t pack(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* out, int out_dtype, uint64_t ldo, cudaStream_t st) {
-  const uint64_t gx = (ldo + 8 * kThreads - 1) / (8 * kThreads), full = rows < 32768 ? rows : 32768;
-  for (uint64_t r0 = 0; r0 < rows;) {      // rows in two dimensions of the grid, a last launch for what is left of them
-    const uint64_t gz = (rows - r0) / full ? ((rows - r0) / full < 32768 ? (rows - r0) / full : 32768) : 1, gy = (rows - r0) < full ? rows - r0 : full;
-    const dim3 grid((uint32_t)gx, (uint32_t)gy, (uint32_t)gz);
-    uint16_t* to = static_cast<uint16_t*>(out) + r0 * ldo;
-    if (dtype == DS_F32) {
-      const float* from = static_cast<const float*>(x) + r0 * ld;
-      launch_pdl(k_f16_pack<float>, grid, dim3(kThreads), st, from, ld, (uint32_t)cols, 0, to, ldo, (int)(out_dtype == DS_BF16),
-                 (int)(aligned(x, 16) && ld % 4 == 0));
-    } else {
-      const uint16_t* from = static_cast<const uint16_t*>(x) + r0 * ld;
-      launch_pdl(k_f16_pack<uint16_t>, grid, dim3(kThreads), st, from, ld, (uint32_t)cols, (int)(dtype == DS_BF16), to, ldo,
-                 (int)(out_dtype == DS_BF16), 0);
-    }
-    count_launches(1);
-    r0 += gy * gz;
-  }
+template <class T, class O>
+cudaError_t pack_as(const void* x, uint64_t rows, uint64_t cols, uint64_t ld, void* out, uint64_t ldo, cudaStream_t st) {
+  const uint32_t warps = (uint32_t)((ldo + 255) / 256), tx = 32 * (warps < 8 ? warps : 8), ty = kThreads / tx, gy = (uint32_t)((rows + ty - 1) / ty);
+  launch_pdl(k_f16_pack<T, O>, dim3((warps * 32 + tx - 1) / tx, gy < 32768 ? gy : 32768), dim3(tx, ty), st, static_cast<const T*>(x), ld, (uint32_t)rows, (uint32_t)cols,
+             static_cast<O*>(out), ldo);
+  count_launches(1);
   return cudaGetLastError();
+}
+cudaError_t pack(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* out, int out_dtype, uint64_t ldo, cudaStream_t st) {
+  using B = __nv_bfloat16;
+  using H = __half;
+  if (out_dtype == DS_BF16)
+    return dtype == DS_F32 ? pack_as<float, B>(x, rows, cols, ld, out, ldo, st) : dtype == DS_BF16 ? pack_as<B, B>(x, rows, cols, ld, out, ldo, st)
+                                                                                                  : pack_as<H, B>(x, rows, cols, ld, out, ldo, st);
+  return dtype == DS_F32 ? pack_as<float, H>(x, rows, cols, ld, out, ldo, st) : dtype == DS_BF16 ? pack_as<B, H>(x, rows, cols, ld, out, ldo, st)
+                                                                                                : pack_as<H, H>(x, rows, cols, ld, out, ldo, st);
 }
 
 // ---- an empty sum: act(bias) + residual -----------------------------------------------------------------
@@ -243,67 +220,43 @@ cudaError_t launch_few16(const FewParams16& p, cudaStream_t st) {
 
 // ---- the gradient through the activation ----------------------------------------------------------------
 // dz = dy act'(z) in 16 bits and, from what is not yet rounded, the column sums of each block of kSumRows rows; a second kernel adds
-// the blocks in their order.  Bound by memory.  A warp reads 8 entries a lane of a row; a CTA's warps take every eighth row.
+// the blocks in their order.  Bound by memory.  A lane has eight columns; a CTA's eight warps take every eighth row, four at a time.
 constexpr uint32_t kSumRows = 64;
 
-template <bool VEC>
-__global__ void __launch_bounds__(256) k_f16_slope(const uint16_t* dy, uint64_t lddy, const uint16_t* z, uint64_t ldz, int act, int bf16, uint16_t* dz,
-                                                   uint64_t lddz, uint32_t rows, uint32_t cols, float* sums) {
-  __shared__ float part[8][256 + 8];
+template <class T, int ACT, bool VEC>
+__global__ void __launch_bounds__(256) k_f16_slope(const T* dy, uint64_t lddy, const T* z, uint64_t ldz, T* dz, uint64_t lddz, uint32_t rows, uint32_t cols, float* sums) {
+  __shared__ float part[8][256];
   pdl_prologue();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t c = blockIdx.x * 256 + lane * 8, r0 = blockIdx.y * kSumRows;
+  const uint32_t c = blockIdx.x * 256 + lane * 8, r0 = blockIdx.y * kSumRows + warp;
   float s[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) s[j] = 0.f;
-  if (c < cols) {
-    const bool whole = VEC && c + 8 <= cols;
-    auto get = [&](const uint16_t* row, uint32_t (&w)[4]) {
-      if (whole) {
-        const uint4 v = ld_plain(reinterpret_cast<const uint4*>(row + c));
-        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  constexpr uint32_t kBatch = 4;      // rows in flight
+#pragma unroll 1
+  for (uint32_t i = 0; i < kSumRows; i += 8 * kBatch) {
+    float g[kBatch][8], q[kBatch][8];
+#pragma unroll
+    for (uint32_t b = 0; b < kBatch; ++b) {
+      const uint64_t r = r0 + i + 8 * b;
+      if (r < rows) {
+        load_row8<VEC>(dy + r * lddy, c, cols, lane, g[b]);
+        if constexpr (ACT != DS_ACT_NONE) load_row8<VEC>(z + r * ldz, c, cols, lane, q[b]);
       } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          w[j] = c + 2 * j < cols ? ld_plain(row + c + 2 * j) : 0u;
-          if (c + 2 * j + 1 < cols) w[j] |= (uint32_t)ld_plain(row + c + 2 * j + 1) << 16;
-        }
+        for (int j = 0; j < 8; ++j) g[b][j] = q[b][j] = 0.f;
       }
-    };
-    constexpr uint32_t kBatch = 4;      // rows in flight
-    for (uint32_t i = 0; i < kSumRows / 8; i += kBatch) {
-      uint32_t g[kBatch][4], q[kBatch][4];
+    }
 #pragma unroll
-      for (uint32_t b = 0; b < kBatch; ++b) {
-        const uint64_t r = r0 + warp + 8 * (i + b);
-        if (r < rows) {
-          get(dy + r * lddy, g[b]);
-          if (z) get(z + r * ldz, q[b]);
-        }
+    for (uint32_t b = 0; b < kBatch; ++b) {
+      const uint64_t r = r0 + i + 8 * b;
+      if (r >= rows) break;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (ACT != DS_ACT_NONE) g[b][j] *= slope_of<ACT>(q[b][j]);
+        s[j] += g[b][j];
       }
-#pragma unroll
-      for (uint32_t b = 0; b < kBatch; ++b) {
-        const uint64_t r = r0 + warp + 8 * (i + b);
-        if (r >= rows) break;
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = half_at(g[b][j / 2], j & 1, bf16);
-        with_act(act, [&](auto a) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] *= slope_of<decltype(a)::value>(half_at(q[b][j / 2], j & 1, bf16));
-        });
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] += v[j];
-        if (dz) {
-          uint16_t* to = dz + r * lddz + c;
-          if (whole)
-            *reinterpret_cast<uint4*>(to) = make_uint4(halves_of(v[0], v[1], bf16), halves_of(v[2], v[3], bf16), halves_of(v[4], v[5], bf16), halves_of(v[6], v[7], bf16));
-          else
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (c + j < cols) to[j] = half_of(v[j], bf16);
-        }
-      }
+      if (dz) store_row8<VEC>(dz + r * lddz, c, cols, lane, g[b]);
     }
   }
   if (!sums) return;
@@ -318,14 +271,40 @@ __global__ void __launch_bounds__(256) k_f16_slope(const uint16_t* dy, uint64_t 
   sums[(uint64_t)blockIdx.y * cols + col] = v;
 }
 
+template <class T>
+void launch_slope(const ds_f16_slope_args* p, float* sums, bool vec, dim3 grid, cudaStream_t st) {
+  auto go = [&](auto kernel) {
+    launch_pdl(kernel, grid, dim3(256), st, static_cast<const T*>(p->dy), p->lddy, static_cast<const T*>(p->z), p->ldz, static_cast<T*>(p->dz), p->lddz, (uint32_t)p->rows,
+               (uint32_t)p->cols, sums);
+  };
+  auto by = [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    vec ? go(k_f16_slope<T, ACT, true>) : go(k_f16_slope<T, ACT, false>);
+  };
+  switch (p->activation) {
+    case DS_ACT_NONE: return by(std::integral_constant<int, DS_ACT_NONE>());
+    case DS_ACT_RELU: return by(std::integral_constant<int, DS_ACT_RELU>());
+    case DS_ACT_GELU: return by(std::integral_constant<int, DS_ACT_GELU>());
+    case DS_ACT_GELU_TANH: return by(std::integral_constant<int, DS_ACT_GELU_TANH>());
+    default: return by(std::integral_constant<int, DS_ACT_SILU>());
+  }
+}
+
 __global__ void __launch_bounds__(256) k_f16_sums(const float* sums, uint32_t blocks, uint32_t cols, void* out, int f32, int bf16) {
   __shared__ float part[8][32];
   pdl_prologue();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t col = blockIdx.x * 32 + lane;
   float v = 0.f;
+  constexpr int kBatch = 8;      // loads in flight
   if (col < cols)
-    for (uint32_t b = warp; b < blocks; b += 8) v += ld_plain(sums + (uint64_t)b * cols + col);
+    for (uint32_t i = warp; i < blocks; i += 8 * kBatch) {
+      float t[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) t[b] = i + 8 * b < blocks ? ld_plain(sums + (uint64_t)(i + 8 * b) * cols + col) : 0.f;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) v += t[b];
+    }
   part[warp][lane] = v;
   __syncthreads();
   if (warp || col >= cols) return;
@@ -522,11 +501,13 @@ int ds_f16_slope(const ds_f16_slope_args* p, void* cuda_stream) {
     if (overlap(ws, dy) || overlap(ws, z) || overlap(ws, dz) || overlap(ws, sum)) return DS_ERR_INVALID_ARG;
     sums = static_cast<float*>(p->workspace);
   }
-  auto vec16 = [&](const void* q, uint64_t ld) { return !q || (aligned(q, 16) && (p->rows == 1 || ld % 8 == 0)); };
-  const bool vec = vec16(p->dy, p->lddy) && vec16(p->z, p->ldz) && vec16(p->dz, p->lddz);
+  auto on = [&](const void* q, uint64_t ld) { return rows_on_boundary(q, ld, p->rows, 2); };
+  const bool vec = p->cols % 8 == 0 && on(p->dy, p->lddy) && on(p->z, p->ldz) && on(p->dz, p->lddz);
   const dim3 grid((uint32_t)((p->cols + 255) / 256), (uint32_t)blocks);
-  launch_pdl(vec ? k_f16_slope<true> : k_f16_slope<false>, grid, dim3(256), st, static_cast<const uint16_t*>(p->dy), p->lddy, static_cast<const uint16_t*>(p->z), p->ldz,
-             (int)p->activation, (int)(p->dtype == DS_BF16), static_cast<uint16_t*>(p->dz), p->lddz, (uint32_t)p->rows, (uint32_t)p->cols, sums);
+  if (p->dtype == DS_BF16)
+    launch_slope<__nv_bfloat16>(p, sums, vec, grid, st);
+  else
+    launch_slope<__half>(p, sums, vec, grid, st);
   count_launches(1);
   if (p->sum) {
     launch_pdl(k_f16_sums, dim3((uint32_t)((p->cols + 31) / 32)), dim3(256), st, (const float*)sums, (uint32_t)blocks, (uint32_t)p->cols, p->sum,

@@ -68,7 +68,8 @@ struct RowWalk {
 };
 // ---- rows on their way ----------------------------------------------------------------------------------
 // Each warp copies its 256 columns of the rows to come into shared memory, DEPTH - 1 rows ahead: nothing but the warp itself waits for them, and no
-// registers are held.  A row's granules lie as they do in memory, so rows may start anywhere.
+// registers are held.  Whole granules are copied as they lie, so rows may start anywhere.  (A lane's two granules of floats apart, so that
+// reading them meets no bank conflicts, made the copies slow: 16384 x 4096 backward 217 to 276 us.)
 template <class T>
 constexpr uint32_t kWarpBytes = 32 * 16 * (sizeof(T) / 2) + 16;      // 256 entries, and the granule behind them
 
@@ -81,8 +82,8 @@ __device__ __forceinline__ void fetch_row(uint32_t to, const uint8_t* part, int 
   const int bytes = left * (int)sizeof(T) + (int)shift;      // up to the row's end
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    const int i = 16 * (lane + 32 * g);
-    if (i < bytes) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i), "l"(at + i) : "memory");
+    const int i = lane + 32 * g;
+    if (16 * i < bytes) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16 * i), "l"(at + 16 * i) : "memory");
   }
   if (!VEC && shift && lane == 0 && bytes > 512 * G)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * G), "l"(at + 512 * G) : "memory");
@@ -91,14 +92,14 @@ __device__ __forceinline__ void fetch_row(uint32_t to, const uint8_t* part, int 
 template <bool VEC, class T>
 __device__ __forceinline__ void read_row8(uint32_t from, uint32_t shift, int left, int lane, float (&v)[8]) {
   constexpr int N = kWords<T>;
-  const uint32_t at = from + lane * 4 * N;
+  constexpr int G = N / 4;
   uint32_t w[N + 4];
 #pragma unroll
-  for (int g = 0; g < N / 4; ++g)
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * g]), "=r"(w[4 * g + 1]), "=r"(w[4 * g + 2]), "=r"(w[4 * g + 3]) : "r"(at + 16 * g) : "memory");
+  for (int g = 0; g < G; ++g)
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * g]), "=r"(w[4 * g + 1]), "=r"(w[4 * g + 2]), "=r"(w[4 * g + 3]) : "r"(from + 16 * (G * lane + g)) : "memory");
   if constexpr (!VEC) {
     if (shift) {
-      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[N]), "=r"(w[N + 1]), "=r"(w[N + 2]), "=r"(w[N + 3]) : "r"(at + 4 * N) : "memory");
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[N]), "=r"(w[N + 1]), "=r"(w[N + 2]), "=r"(w[N + 3]) : "r"(from + 16 * (G * lane + G)) : "memory");
       take_from<N>(w, shift);
     }
   }
@@ -117,8 +118,8 @@ __device__ __forceinline__ void commit_rows() { asm volatile("cp.async.commit_gr
 
 // VEC: pieces that no row reaches stay zero.
 template <bool VEC>
-__device__ __forceinline__ void clear_ring(uint8_t* ring, uint32_t bytes) {
-  if constexpr (VEC) {
+__device__ __forceinline__ void clear_ring(const NormParams& p, uint8_t* ring, uint32_t bytes) {
+  if (VEC && p.cols != blockDim.x * 8 * p.size) {
     for (uint32_t i = (threadIdx.y * blockDim.x + threadIdx.x) * 16; i < bytes; i += blockDim.x * blockDim.y * 16)
       *reinterpret_cast<uint4*>(ring + i) = make_uint4(0, 0, 0, 0);
     __syncthreads();
@@ -128,7 +129,14 @@ __device__ __forceinline__ void clear_ring(uint8_t* ring, uint32_t bytes) {
 // Eight entries of a vector of parameters; `none` where there is no vector, 0 behind its end.
 __device__ __forceinline__ void load_param8(const float* p, uint32_t c, uint32_t cols, float none, float (&v)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? p ? ld_plain(p + c + j) : none : 0.f;
+  for (int j = 0; j < 8; ++j) v[j] = none;
+  if (p && c + 8 <= cols && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    const float4 a = ld_plain(reinterpret_cast<const float4*>(p + c)), b = ld_plain(reinterpret_cast<const float4*>(p + c) + 1);
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  } else if (p || c + 8 > cols) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? p ? ld_plain(p + c + j) : none : 0.f;
+  }
 }
 
 // ---- sums over the threads of a row ---------------------------------------------------------------------
@@ -137,8 +145,8 @@ __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 struct SumSpace {
-  float warp[2][16][2];      // of each warp; the two halves take turns, so that one barrier is enough
-  float cta[2][8][2];        // of each CTA of a cluster
+  float warp[2][16][3];      // of each warp; the two halves take turns, so that one barrier is enough
+  float cta[2][8][3];        // of each CTA of a cluster
 };
 struct RowSum {
   SumSpace* space;
@@ -221,7 +229,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_forward(const NormPara
   const uint32_t warps = (blockDim.x >> 5) * blockDim.y, slot_bytes = warps * R::kWarp;
   const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + at.warp * R::kWarp;
   const float inv = 1.f / (float)p.cols;
-  clear_ring<VEC>(ring, R::kDepth * slot_bytes);
+  clear_ring<VEC>(p, ring, R::kDepth * slot_bytes);
   RowWalk ahead, now;
   uint32_t put = 0, get = 0;
   ahead.find(p, at.team, at.teams);
@@ -371,7 +379,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_backward(const NormPar
   float* flush = reinterpret_cast<float*>(ring + R::kDepth * slot_bytes) + 16 * threads;
   const float inv = 1.f / (float)p.cols;
   constexpr uint32_t kAtX = kWarpBytes<Y>, kAtDn = kAtX + kWarpBytes<X>, kAtDh = kAtDn + kWarpBytes<Y>;
-  clear_ring<VEC>(ring, R::kDepth * slot_bytes);
+  clear_ring<VEC>(p, ring, R::kDepth * slot_bytes);
   RowWalk ahead, now;
   uint32_t put = 0, get = 0;
   ahead.find(p, at.team, at.teams);
@@ -459,19 +467,24 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_backward(const NormPar
 #pragma unroll
         for (int j = 0; j < 8; ++j) d[j] = 0.f;
       }
-      if (p.dn.p) {
-        float hat2[8], t[8], s[FULL ? 2 : 1];
+      // RMS norms have one exchange of sums: with u = D(hat1 gw), the pre norm's  S = sum t hat2,  the post norm's sum is
+      // sum u (dh + r2 t) - r2 S / cols sum u hat2.
+      float hat2[8], t[8], s[3] = {0.f, 0.f, 0.f};
+      if (p.dn.p || !FULL) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) hat2[j] = FULL ? __fmaf_rn(hat1[j], gw[j], gb[j]) : hat1[j] * gw[j];
         if (p.drop.threshold) drop8(p.drop, draw, hat2);
+      }
+      if (p.dn.p) {
+        float u[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = hat2[j];
         if (p.x.p) {
           read_row8<VEC, X>(from + kAtX, VEC ? 0 : p.x.shift(row), at.left, at.lane, t);
 #pragma unroll
           for (int j = 0; j < 8; ++j) hat2[j] = __fmaf_rn(p.residual_scale, t[j], hat2[j]);
         }
         read_row8<VEC, Y>(from + kAtDn, VEC ? 0 : p.dn.shift(row), at.left, at.lane, t);
-        s[0] = 0.f;
-        if constexpr (FULL) s[1] = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           hat2[j] = (FULL ? hat2[j] - st.z : hat2[j]) * st.w;
@@ -479,40 +492,62 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_backward(const NormPar
           if constexpr (FULL) s_e[j] += t[j];
           t[j] *= w2[j];
           s[0] = __fmaf_rn(t[j], hat2[j], s[0]);
-          if constexpr (FULL) s[1] += t[j];
+          if constexpr (FULL) {
+            s[1] += t[j];
+          } else {
+            d[j] = __fmaf_rn(st.w, t[j], d[j]);
+            s[1] = __fmaf_rn(u[j], d[j], s[1]);
+            s[2] = __fmaf_rn(u[j], hat2[j], s[2]);
+          }
         }
-        sum(s);
-        const float k = s[0] * inv;
-        float m = 0.f;
-        if constexpr (FULL) m = p.layer ? s[1] * inv : 0.f;
+      } else if constexpr (!FULL) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = __fmaf_rn(st.w, __fmaf_rn(-hat2[j], k, FULL ? t[j] - m : t[j]), d[j]);
+        for (int j = 0; j < 8; ++j) s[1] = __fmaf_rn(hat2[j], d[j], s[1]);
+      }
+      if constexpr (FULL) {
+        if (p.dn.p) {
+          sum(*reinterpret_cast<float(*)[2]>(s));
+          const float k = s[0] * inv, m = p.layer ? s[1] * inv : 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d[j] = __fmaf_rn(st.w, __fmaf_rn(-hat2[j], k, t[j] - m), d[j]);
+        }
+      } else {
+        if (p.post_w)
+          sum(s);
+        else
+          sum(*reinterpret_cast<float(*)[1]>(s));
+        if (p.dn.p) {
+          const float k = st.w * s[0] * inv;
+          s[1] = __fmaf_rn(-k, s[2], s[1]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d[j] = __fmaf_rn(-hat2[j], k, d[j]);
+        }
       }
       if (p.dx.p) {
-        float t[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) t[j] = p.residual_scale * d[j];
         store_row8<VEC>(p.dx.out<X>(row), at.c, p.cols, at.lane, t);
       }
       if (p.drop.threshold) drop8(p.drop, draw, d);
-      float s[FULL ? 2 : 1];
-      s[0] = 0.f;
-      if constexpr (FULL) s[1] = 0.f;
+      if constexpr (FULL) s[0] = s[1] = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         s_a[j] = __fmaf_rn(d[j], hat1[j], s_a[j]);
         if constexpr (FULL) s_b[j] += d[j];
         d[j] *= gw[j];
-        s[0] = __fmaf_rn(d[j], hat1[j], s[0]);
-        if constexpr (FULL) s[1] += d[j];
+        if constexpr (FULL) s[0] = __fmaf_rn(d[j], hat1[j], s[0]), s[1] += d[j];
       }
       if (p.post_w) {
-        sum(s);
-        const float k = s[0] * inv;
-        float m = 0.f;
-        if constexpr (FULL) m = p.layer ? s[1] * inv : 0.f;
+        if constexpr (FULL) {
+          sum(*reinterpret_cast<float(*)[2]>(s));
+          const float k = s[0] * inv, m = p.layer ? s[1] * inv : 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = st.y * __fmaf_rn(-hat1[j], k, FULL ? d[j] - m : d[j]);
+          for (int j = 0; j < 8; ++j) d[j] = st.y * __fmaf_rn(-hat1[j], k, d[j] - m);
+        } else {
+          const float k = s[1] * inv;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d[j] = st.y * __fmaf_rn(-hat1[j], k, d[j]);
+        }
       }
       if (p.dy.p) store_row8<VEC>(p.dy.out<Y>(row), at.c, p.cols, at.lane, d);
       st = st_next;
@@ -575,8 +610,15 @@ __global__ void __launch_bounds__(256) k_norm_sums(const SumsParams p) {
   while (v >= p.vectors[kind]) v -= p.vectors[kind++];
   const float* in = p.in[kind] + (uint64_t)v * p.count[kind] * p.step[kind];
   float s = 0.f;
+  constexpr int kBatch = 10;      // loads in flight
   if (col < p.cols)
-    for (uint32_t i = warp; i < p.count[kind]; i += 8) s += ld_plain(in + i * p.step[kind] + col);
+    for (uint32_t i = warp; i < p.count[kind]; i += 8 * kBatch) {
+      float t[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) t[b] = i + 8 * b < p.count[kind] ? ld_plain(in + (i + 8 * b) * p.step[kind] + col) : 0.f;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) s += t[b];
+    }
   part[warp][lane] = s;
   __syncthreads();
   if (warp || col >= p.cols) return;

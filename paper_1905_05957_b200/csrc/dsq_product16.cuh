@@ -35,16 +35,42 @@ __device__ __forceinline__ float from_half(uint16_t w, bool bf16) {
   return bf16 ? __uint_as_float((uint32_t)w << 16) : __half2float(__ushort_as_half(w));
 }
 
-// 1 / (1 + exp(-v)): __expf and __fdividef are good to a few units of 2^-22 here, results are rounded to 2^-9 or 2^-12.
-__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
-constexpr float kSqrtHalf = 0.70710678f, kSqrt2OverPi = 0.79788456f, kGeluCubic = 0.044715f, kInvSqrt2Pi = 0.39894228f;
+// Powers of two and reciprocals by the special function unit, good to a few units of 2^-23; numbers below 2^-126 count as 0.
+__device__ __forceinline__ float exp2_of(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float reciprocal(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+constexpr float kLog2E = 1.44269504f, kSqrtHalf = 0.70710678f, kSqrt2OverPi = 0.79788456f, kGeluCubic = 0.044715f, kInvSqrt2Pi = 0.39894228f;
+// 1 / (1 + exp(-v)) of v = scaled / log2(e)
+__device__ __forceinline__ float sigmoid2(float scaled) { return reciprocal(1.f + exp2_of(-scaled)); }
+// The normal distribution's Phi(z), and exp(-z^2 / 2): Phi(-|z|) = exp(-z^2 / 2) P(t) / 2 with t = 1 / (1 + 0.3275911 |z| / sqrt 2) and a P of five terms
+// (Hastings, in Abramowitz and Stegun 7.1.26: off by 7.5e-8 at most here, and no cancellation for negative z).  An unrolled run of 32 values is a
+// third of the instructions that erff takes, which an epilogue fetches once a block.
+__device__ __forceinline__ float phi_of(float z, float& e) {
+  const float t = reciprocal(__fmaf_rn(0.3275911f * kSqrtHalf, fabsf(z), 1.f));
+  e = exp2_of(z * z * (-0.5f * kLog2E));
+  float q = __fmaf_rn(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+  q = __fmaf_rn(t, q, 0.5f * 1.421413741f);
+  q = __fmaf_rn(t, q, 0.5f * -0.284496736f);
+  q = __fmaf_rn(t, q, 0.5f * 0.254829592f) * t * e;
+  return z < 0.f ? q : 1.f - q;
+}
 
 template <int ACT>
 __device__ __forceinline__ float act_of(float z) {
   if constexpr (ACT == DS_ACT_RELU) return z < 0.f ? 0.f : z;
-  if constexpr (ACT == DS_ACT_GELU) return 0.5f * z * (1.f + erff(z * kSqrtHalf));
-  if constexpr (ACT == DS_ACT_GELU_TANH) return z * sigmoid(2.f * kSqrt2OverPi * __fmaf_rn(kGeluCubic * z * z, z, z));   // (1 + tanh u) / 2 = sigmoid(2 u)
-  if constexpr (ACT == DS_ACT_SILU) return z * sigmoid(z);
+  if constexpr (ACT == DS_ACT_GELU) {
+    float e;
+    return z * phi_of(z, e);
+  }
+  if constexpr (ACT == DS_ACT_GELU_TANH) return z * sigmoid2(2.f * kSqrt2OverPi * kLog2E * __fmaf_rn(kGeluCubic * z * z, z, z));   // (1 + tanh u) / 2 = sigmoid(2 u)
+  if constexpr (ACT == DS_ACT_SILU) return z * sigmoid2(kLog2E * z);
   return z;
 }
 // act'(z).  Beyond |z| = 100 the slopes are 0 and 1 in 32 bits; kept there so that no inf meets a zero.
@@ -52,13 +78,17 @@ template <int ACT>
 __device__ __forceinline__ float slope_of(float z) {
   if constexpr (ACT == DS_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
   const float c = fabsf(z) > 100.f ? copysignf(100.f, z) : z;
-  if constexpr (ACT == DS_ACT_GELU) return __fmaf_rn(c * kInvSqrt2Pi, __expf(-0.5f * c * c), 0.5f * (1.f + erff(c * kSqrtHalf)));
+  if constexpr (ACT == DS_ACT_GELU) {
+    float e;
+    const float p = phi_of(c, e);
+    return __fmaf_rn(c * kInvSqrt2Pi, e, p);
+  }
   if constexpr (ACT == DS_ACT_GELU_TANH) {
-    const float s = sigmoid(2.f * kSqrt2OverPi * __fmaf_rn(kGeluCubic * c * c, c, c));
+    const float s = sigmoid2(2.f * kSqrt2OverPi * kLog2E * __fmaf_rn(kGeluCubic * c * c, c, c));
     return __fmaf_rn(c * s * (1.f - s), 2.f * kSqrt2OverPi * __fmaf_rn(3.f * kGeluCubic * c, c, 1.f), s);
   }
   if constexpr (ACT == DS_ACT_SILU) {
-    const float s = sigmoid(c);
+    const float s = sigmoid2(kLog2E * c);
     return s * __fmaf_rn(c, 1.f - s, 1.f);
   }
   return 1.f;

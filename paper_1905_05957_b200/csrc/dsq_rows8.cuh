@@ -127,6 +127,12 @@ __device__ __forceinline__ void store_row8(T* row, uint32_t c, uint32_t cols, in
   if constexpr (VEC) {
     if (c >= cols) return;
     pack8<T>(v, w);
+    if (sizeof(T) == 4 && (reinterpret_cast<uintptr_t>(row) & 16) == 0) {      // a whole sector at once
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + c), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[N - 4]), "r"(w[N - 3]),
+                   "r"(w[N - 2]), "r"(w[N - 1])
+                   : "memory");
+      return;
+    }
 #pragma unroll
     for (int g = 0; g < N / 4; ++g) reinterpret_cast<uint4*>(row + c)[g] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
     return;
