@@ -88,7 +88,9 @@ __global__ void __launch_bounds__(kThreads) k_f16_empty(const Out16 o) {
 // 8 columns; the warp instruction is enough, the loop waits for memory).  K is dealt to the instructions' places as it arrives:
 // lane t of a group of four loads 8 consecutive entries of its rows and tokens and feeds them as two instructions' worth.
 // The warps' sums meet in shared memory and are added in the order of the warps.
-constexpr uint32_t kFewMost = 16;
+constexpr uint32_t kFewMost = 16, kFewGroup = 8;
+// With more than one group of tokens and this many entries of W, a launch of TMA-fed tiles is faster (16 x 4096 -> 16384: 29 and 25 us; 16 x 11008 -> 4096: 19 and 21).
+constexpr uint64_t kFewEntries = 48u << 20;
 
 struct FewParams16 {
   const uint16_t *x, *w;
@@ -210,7 +212,8 @@ __global__ void __launch_bounds__(256, 2) k_f16_few(const FewParams16 p) {
 
 template <bool BF16, int NT>
 cudaError_t launch_few16(const FewParams16& p, cudaStream_t st) {
-  if ((p.o.n + 31) / 32 >= 2 * (uint32_t)sm_count())
+  // 16 rows a CTA while one round of CTAs (three an SM) takes them all, else 32 (1 x 2048 -> 8192: 8.1 and 7.2 us; -> 2048: 4.4 and 4.9)
+  if ((p.o.n + 15) / 16 > 3 * (uint32_t)sm_count())
     launch_pdl(k_f16_few<BF16, NT, 2>, dim3((p.o.n + 31) / 32), dim3(256), st, p);
   else
     launch_pdl(k_f16_few<BF16, NT, 1>, dim3((p.o.n + 15) / 16), dim3(256), st, p);
@@ -224,7 +227,7 @@ cudaError_t launch_few16(const FewParams16& p, cudaStream_t st) {
 constexpr uint32_t kSumRows = 64;
 
 template <class T, int ACT, bool VEC>
-__global__ void __launch_bounds__(256) k_f16_slope(const T* dy, uint64_t lddy, const T* z, uint64_t ldz, T* dz, uint64_t lddz, uint32_t rows, uint32_t cols, float* sums) {
+__global__ void __launch_bounds__(256, VEC ? 4 : 2) k_f16_slope(const T* dy, uint64_t lddy, const T* z, uint64_t ldz, T* dz, uint64_t lddz, uint32_t rows, uint32_t cols, float* sums) {
   __shared__ float part[8][256];
   pdl_prologue();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -235,28 +238,28 @@ __global__ void __launch_bounds__(256) k_f16_slope(const T* dy, uint64_t lddy, c
   constexpr uint32_t kBatch = 4;      // rows in flight
 #pragma unroll 1
   for (uint32_t i = 0; i < kSumRows; i += 8 * kBatch) {
-    float g[kBatch][8], q[kBatch][8];
+    uint32_t g[kBatch][kWords<T> + 4], q[kBatch][kWords<T> + 4];
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
       const uint64_t r = r0 + i + 8 * b;
       if (r < rows) {
-        load_row8<VEC>(dy + r * lddy, c, cols, lane, g[b]);
-        if constexpr (ACT != DS_ACT_NONE) load_row8<VEC>(z + r * ldz, c, cols, lane, q[b]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) g[b][j] = q[b][j] = 0.f;
+        load_words8<VEC>(dy + r * lddy, c, cols, lane, g[b]);
+        if constexpr (ACT != DS_ACT_NONE) load_words8<VEC>(z + r * ldz, c, cols, lane, q[b]);
       }
     }
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
       const uint64_t r = r0 + i + 8 * b;
       if (r >= rows) break;
+      float v[8], t[8];
+      entries8<VEC, T>(g[b], c, cols, v);
+      if constexpr (ACT != DS_ACT_NONE) entries8<VEC, T>(q[b], c, cols, t);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if constexpr (ACT != DS_ACT_NONE) g[b][j] *= slope_of<ACT>(q[b][j]);
-        s[j] += g[b][j];
+        if constexpr (ACT != DS_ACT_NONE) v[j] *= slope_of<ACT>(t[j]);
+        s[j] += v[j];
       }
-      if (dz) store_row8<VEC>(dz + r * lddz, c, cols, lane, g[b]);
+      if (dz) store_row8<VEC>(dz + r * lddz, c, cols, lane, v);
     }
   }
   if (!sums) return;
@@ -348,10 +351,10 @@ constexpr uint32_t kTurnedMost = 64;
 
 cudaError_t multiply(const ds_f16_product* p, const Out16& o, Operand16 a, Operand16 b, cudaStream_t st) {
   const uint32_t m = o.m, n = o.n, k = (uint32_t)p->k;
-  if (!a.across && !b.across && m <= kFewMost) {
+  if (!a.across && !b.across && (m <= kFewGroup || (m <= kFewMost && (uint64_t)n * k <= kFewEntries))) {
     const FewParams16 f{static_cast<const uint16_t*>(a.p), static_cast<const uint16_t*>(b.p), a.ld, b.ld, k, o};
-    if (o.bf16) return m <= 8 ? launch_few16<true, 1>(f, st) : launch_few16<true, 2>(f, st);
-    return m <= 8 ? launch_few16<false, 1>(f, st) : launch_few16<false, 2>(f, st);
+    if (o.bf16) return m <= kFewGroup ? launch_few16<true, 1>(f, st) : launch_few16<true, 2>(f, st);
+    return m <= kFewGroup ? launch_few16<false, 1>(f, st) : launch_few16<false, 2>(f, st);
   }
   const MmaShape s{m, n, k, 1, 2, 0, 0, p->dev_status, 1, (uint32_t)o.bf16};
   const bool bare = !o.residual && !o.z && !o.bias && !o.act;

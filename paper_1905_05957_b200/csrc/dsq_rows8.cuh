@@ -63,18 +63,20 @@ __device__ __forceinline__ void pack8(const float (&v)[8], uint32_t* w) {
   }
 }
 
-// w[0..N): the bytes from `shift` on (0..15, a multiple of the entries' size).
-template <int N>
+// w[0..N): the bytes from `shift` on (0..15, a multiple of the entries' size).  LONG: and in w[N..N + 4) what follows, zeros behind the last word.
+template <int N, bool LONG = false>
 __device__ __forceinline__ void take_from(uint32_t (&w)[N + 4], uint32_t shift) {
+  constexpr int L = LONG ? N + 4 : N;
+  auto at = [&](int i) { return i < N + 4 ? w[i] : 0u; };
   if (shift & 8)
 #pragma unroll
-    for (int i = 0; i < N + 2; ++i) w[i] = w[i + 2];
+    for (int i = 0; i < (LONG ? L : N + 2); ++i) w[i] = at(i + 2);
   if (shift & 4)
 #pragma unroll
-    for (int i = 0; i < N + 1; ++i) w[i] = w[i + 1];
+    for (int i = 0; i < (LONG ? L : N + 1); ++i) w[i] = at(i + 1);
   if (shift & 2)
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    for (int i = 0; i < L; ++i) w[i] = __funnelshift_r(w[i], at(i + 1), 16);
 }
 
 __device__ __forceinline__ uint32_t shift_of(const void* row) { return (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15); }
@@ -86,11 +88,10 @@ __device__ __forceinline__ int entries_left(uint32_t c, uint32_t cols) {
 }
 
 // Entries c .. c + 7 of a row of `cols`, lane l of a whole warp those 8 l behind lane 0's.  Entries behind the row's end are 0.
-// VEC: every row starts on a 16-byte boundary and cols is a multiple of 8.
+// VEC: every row starts on a 16-byte boundary and cols is a multiple of 8.  First as words, for loads that run ahead of their use.
 template <bool VEC, class T>
-__device__ __forceinline__ void load_row8(const T* row, uint32_t c, uint32_t cols, int lane, float (&v)[8]) {
+__device__ __forceinline__ void load_words8(const T* row, uint32_t c, uint32_t cols, int lane, uint32_t (&w)[kWords<T> + 4]) {
   constexpr int N = kWords<T>;
-  uint32_t w[N + 4];
 #pragma unroll
   for (int i = 0; i < N; ++i) w[i] = 0;
   const uint32_t shift = VEC ? 0 : shift_of(row);
@@ -112,11 +113,36 @@ __device__ __forceinline__ void load_row8(const T* row, uint32_t c, uint32_t col
     }
     take_from<N>(w, shift);
   }
+}
+template <bool VEC, class T>
+__device__ __forceinline__ void entries8(const uint32_t* w, uint32_t c, uint32_t cols, float (&v)[8]) {
   unpack8<T>(w, v);
   if (!VEC && c + 8 > cols)
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (c + j >= cols) v[j] = 0.f;
+}
+template <bool VEC, class T>
+__device__ __forceinline__ void load_row8(const T* row, uint32_t c, uint32_t cols, int lane, float (&v)[8]) {
+  uint32_t w[kWords<T> + 4];
+  load_words8<VEC>(row, c, cols, lane, w);
+  entries8<VEC, T>(w, c, cols, v);
+}
+
+// Eight entries to where they fit whole: a boundary of 16 bytes, for floats of 32 if `at` is on one.
+template <class T>
+__device__ __forceinline__ void store_piece8(T* at, const float (&v)[8]) {
+  constexpr int N = kWords<T>;
+  uint32_t w[N];
+  pack8<T>(v, w);
+  if (sizeof(T) == 4 && (reinterpret_cast<uintptr_t>(at) & 16) == 0) {      // a whole sector at once
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[N - 4]), "r"(w[N - 3]), "r"(w[N - 2]),
+                 "r"(w[N - 1])
+                 : "memory");
+    return;
+  }
+#pragma unroll
+  for (int g = 0; g < N / 4; ++g) reinterpret_cast<uint4*>(at)[g] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
 }
 
 // The other way round.  The whole warp calls it, lanes behind the row's end, too.
@@ -125,16 +151,7 @@ __device__ __forceinline__ void store_row8(T* row, uint32_t c, uint32_t cols, in
   constexpr int N = kWords<T>, kEach = 16 / sizeof(T);
   uint32_t w[N + 4];
   if constexpr (VEC) {
-    if (c >= cols) return;
-    pack8<T>(v, w);
-    if (sizeof(T) == 4 && (reinterpret_cast<uintptr_t>(row) & 16) == 0) {      // a whole sector at once
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + c), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[N - 4]), "r"(w[N - 3]),
-                   "r"(w[N - 2]), "r"(w[N - 1])
-                   : "memory");
-      return;
-    }
-#pragma unroll
-    for (int g = 0; g < N / 4; ++g) reinterpret_cast<uint4*>(row + c)[g] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+    if (c < cols) store_piece8(row + c, v);
     return;
   }
   const uint32_t shift = shift_of(row);
@@ -157,8 +174,7 @@ __device__ __forceinline__ void store_row8(T* row, uint32_t c, uint32_t cols, in
   pack8<T>(v, w + 4);
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xFFFFFFFFu, w[N + i], 1);
-  const uint32_t last[4] = {w[N], w[N + 1], w[N + 2], w[N + 3]};      // this lane's own last 16 bytes
-  take_from<N>(w, 16 - shift);
+  take_from<N, true>(w, 16 - shift);      // w[N..]: what this lane hands over
   uint8_t* at = reinterpret_cast<uint8_t*>(row + c) - shift;
   const int s = (int)shift;
   auto put = [&](int i, uint32_t word, int byte) {      // the entry at byte i of the granules
@@ -167,20 +183,27 @@ __device__ __forceinline__ void store_row8(T* row, uint32_t c, uint32_t cols, in
     else
       *reinterpret_cast<uint16_t*>(at + i) = (uint16_t)(byte ? word >> 16 : word);
   };
+  const bool ends = left - 8 * (31 - lane) * (int)sizeof(T) < 4 * N;      // the row ends before or within the last lane's entries
 #pragma unroll
   for (int g = 0; g < N / 4; ++g) {
-    if ((g || lane) && 16 * (g + 1) - s <= left) {
+    if ((g || lane) && (!ends || 16 * (g + 1) - s <= left)) {
       reinterpret_cast<uint4*>(at)[g] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
-    } else if (16 * g - s < left) {      // the row's end, or what begins a warp
+    } else if (ends && 16 * g - s < left) {      // the row's end, or what begins a warp
 #pragma unroll
       for (int i = 16 * g; i < 16 * g + 16; i += sizeof(T))
         if (i - s < left && (lane || i >= s)) put(i, w[i / 4], i & 2);
     }
   }
-  if (lane == 31)      // what this lane would hand over
+  if (!ends && (lane == 0 || lane == 31)) {      // the first lane's own part of its first granule, and what the last lane would hand over
+    const int from = lane ? 4 * N : 0;
 #pragma unroll
     for (int i = 0; i < 16; i += sizeof(T))
-      if (i >= 16 - s && 4 * N - 16 + i < left) put(4 * N - 16 + i + s, last[i / 4], i & 2);
+      if (lane ? i < s : i >= s) put(from + i, lane ? w[N + i / 4] : w[i / 4], i & 2);
+  }
+  if (ends && lane == 31)
+#pragma unroll
+    for (int i = 0; i < 16; i += sizeof(T))
+      if (i < s && 4 * N + i - s < left) put(4 * N + i, w[N + i / 4], i & 2);
 }
 
 // Whether rows of a matrix start on 16-byte boundaries (or it is not there).
