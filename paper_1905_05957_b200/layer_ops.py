@@ -15,7 +15,7 @@ import torch
 from . import matrix_ops as _m
 from .binding import (ACTIVATIONS, DS_F16_FORWARD, DS_F16_INPUTS, DS_F16_WEIGHTS, DS_F32, DS_NORM_LAYER, DS_NORM_MAX_COLS, DS_NORM_RMS,
                       ds_f16_product, ds_norm_args, fast_call, fast_struct_call, load_library)
-from .matrix_ops import _DTYPES, _check, _current, _dev_status, _empty, _matrix, _out, _raw_stream, _vector
+from .matrix_ops import _DTYPES, _check, _current, _dev_status, _raw_stream, _status
 
 _HALVES = {torch.bfloat16: _DTYPES[torch.bfloat16], torch.float16: _DTYPES[torch.float16]}
 _NORMS = {"rms": DS_NORM_RMS, "layer": DS_NORM_LAYER}
@@ -45,14 +45,49 @@ def _activation(name: str) -> int:
     return code
 
 
-def _like(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, device, what: str) -> tuple[torch.Tensor, int]:
-    """t as rows of consecutive entries, and the distance between them; it has to be [rows, cols] of dtype on device."""
+def _rows(t: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int, int]:
+    """t as rows of consecutive entries; rows, columns, the distance between rows, the device's index."""
+    shape, index = t.shape, t.get_device()
+    if index < 0:
+        raise ValueError(f"{what}: a CUDA tensor expected: there is no CPU path")
+    if len(shape) != 2:
+        raise ValueError(f"{what}: a matrix expected, got {len(shape)} dimensions")
+    r, c = shape
+    ld, step = t.stride()
+    if (c > 1 and step != 1) or (r > 1 and ld < c):
+        t, ld = t.contiguous(), c
+    return t, r, c, (ld if r > 1 else c), index
+
+
+def _like(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, index: int, what: str) -> tuple[torch.Tensor, int]:
+    """t as rows of consecutive entries, and the distance between them; it has to be [rows, cols] of dtype on that device."""
     if t.dtype is not dtype:
         raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
-    if t.shape != (rows, cols) or t.device != device:
-        raise ValueError(f"{what}: a matrix {(rows, cols)} on {device} expected, got {tuple(t.shape)} on {t.device}")
-    t, _, _, ld, _ = _matrix(t, what)
-    return t, ld
+    if t.shape != (rows, cols) or t.get_device() != index:
+        raise ValueError(f"{what}: a matrix {(rows, cols)} on cuda:{index} expected, got {tuple(t.shape)} on {t.device}")
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
+        return t.contiguous(), cols
+    return t, (ld if rows > 1 else cols)
+
+
+def _given(out: torch.Tensor, rows: int, cols: int, index: int, what: str) -> int:
+    """The distance between the rows of a given output."""
+    if out.shape != (rows, cols) or out.get_device() != index:
+        raise ValueError(f"{what}: a matrix {(rows, cols)} on cuda:{index} expected, got {tuple(out.shape)} on {out.device}")
+    ld, step = out.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
+        raise ValueError(f"{what}: rows of consecutive entries expected")
+    return ld if rows > 1 else cols
+
+
+def _floats(v: torch.Tensor, n: int, index: int, what: str) -> int:
+    """The address of n contiguous float32 values on that device."""
+    if v.dtype is not torch.float32 or v.shape != (n,) or not v.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous float32 values expected, got {v.dtype} {tuple(v.shape)}")
+    if v.get_device() != index:
+        raise ValueError(f"{what}: on {v.device}, the others on cuda:{index}")
+    return v.data_ptr()
 
 
 def _on_boundary(p: int, ld: int, rows: int) -> bool:
@@ -63,7 +98,7 @@ def _packed(x: torch.Tensor, ld: int, dtype: torch.dtype, index: int) -> tuple[t
     """A copy of a matrix in 16 bits, on 16-byte rows."""
     r, c = x.shape
     pitch = max(8, (c + 7) // 8 * 8)
-    out = _empty((r, pitch), dtype=dtype, device=x.device)
+    out = x.new_empty((r, pitch), dtype=dtype)
     rc = _call(_pack_at, x.data_ptr(), _m._dtype(x.dtype, "x"), r, c, ld, out.data_ptr(), _half(dtype, "dtype"), pitch, _raw_stream(index))
     if rc:
         _check(rc, "ds_f16_pack")
@@ -71,15 +106,18 @@ def _packed(x: torch.Tensor, ld: int, dtype: torch.dtype, index: int) -> tuple[t
 
 
 def _product(layout: int, dt: int, m: int, n: int, k: int, a: int, lda: int, b: int, ldb: int, bias, act: int, res, ldr: int, z, ldz: int, out: int, odt: int,
-             ldo: int, index: int, device):
-    rows_a, rows_b = (k if layout == DS_F16_WEIGHTS else m), (n if layout == DS_F16_FORWARD else k)
-    ws, size = None, 0
-    if not (_on_boundary(a, lda, rows_a) and _on_boundary(b, ldb, rows_b)):
+             ldo: int, index: int, raw: int, like: torch.Tensor):
+    ws = address = None
+    size = 0
+    if (a | b) & 15 or (lda | ldb) & 7:      # perhaps an operand has to be copied
         args = ds_f16_product(dt, layout, m, n, k, a, lda, b, ldb, 0, 0, 0, 0, 0, 0, out, odt, ldo, 0, 0, 0)
         size = load_library().ds_f16_matmul_workspace(C.byref(args))
-        ws = _empty(size, dtype=torch.uint8, device=device)
-    rc = _struct(_matmul_at, _raw_stream(index), dt, layout, m, n, k, a, lda, b, ldb, bias, act, res, ldr, z, ldz, out, odt, ldo,
-                 ws.data_ptr() if size else None, size, _dev_status(index))
+        if size:
+            ws = like.new_empty(size // 2)
+            address = ws.data_ptr()
+    status = _status.get(index)
+    rc = _struct(_matmul_at, raw, dt, layout, m, n, k, a, lda, b, ldb, bias, act, res, ldr, z, ldz, out, odt, ldo, address, size,
+                 status[1] if status else _dev_status(index))
     if rc:
         _check(rc, "ds_f16_matmul")
 
@@ -99,33 +137,36 @@ def linear16(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None,
 def _forward(x, w, bias, act, residual, out_dtype, out, keep_z):
     if _struct is None:
         _load()
-    dt = _half(x.dtype, "x")
-    x, m, k, ldx, device = _matrix(x, "x")
+    dtype = x.dtype
+    dt = _HALVES.get(dtype)
+    if dt is None:
+        _half(dtype, "x")
+    x, m, k, ldx, index = _rows(x, "x")
     n = w.shape[0]
-    w, ldw = _like(w, n, k, x.dtype, device, "w")
-    index = device.index
+    w, ldw = _like(w, n, k, dtype, index, "w")
     if index != _current():                  # the library works on the current device
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             return _forward(x, w, bias, act, residual, out_dtype, out, keep_z)
-    bp = None if bias is None else _vector(bias, n, "bias", device)
+    bp = None if bias is None else _floats(bias, n, index, "bias")
     rp, ldr = None, 0
     if residual is not None:
-        residual, ldr = _like(residual, m, n, x.dtype, device, "residual")
+        residual, ldr = _like(residual, m, n, dtype, index, "residual")
         rp = residual.data_ptr()
     if out is not None:
-        ldo, odt = _out(out, m, n, device), _DTYPES.get(out.dtype)
+        ldo, odt = _given(out, m, n, index, "out"), _DTYPES.get(out.dtype)
+    elif out_dtype is None:
+        out, ldo, odt = x.new_empty((m, n)), n, dt
     else:
-        out = _empty((m, n), dtype=out_dtype or x.dtype, device=device)
-        ldo, odt = n, _DTYPES.get(out.dtype)
+        out, ldo, odt = x.new_empty((m, n), dtype=out_dtype), n, _DTYPES.get(out_dtype)
     if odt != dt and odt != DS_F32:
-        raise TypeError(f"out: {x.dtype} or float32 expected, got {out.dtype}")
-    z, ldz = None, 0
+        raise TypeError(f"out: {dtype} or float32 expected, got {out.dtype}")
+    z, zp, ldz = None, None, 0
     if keep_z:
         ldz = (n + 7) // 8 * 8
-        z = _empty((m, ldz), dtype=x.dtype, device=device)[:, :n]
+        z = x.new_empty((m, ldz))
+        zp = z.data_ptr()
     if m and n:
-        _product(DS_F16_FORWARD, dt, m, n, k, x.data_ptr(), ldx, w.data_ptr(), ldw, bp, act, rp, ldr, None if z is None else z.data_ptr(), ldz, out.data_ptr(),
-                 odt, ldo, index, device)
+        _product(DS_F16_FORWARD, dt, m, n, k, x.data_ptr(), ldx, w.data_ptr(), ldw, bp, act, rp, ldr, zp, ldz, out.data_ptr(), odt, ldo, index, _raw_stream(index), x)
     return out, z
 
 
@@ -148,53 +189,55 @@ class Linear16:
         if _struct is None:
             _load()
         _m._dtype(weight.dtype, "weight")
-        weight, r, _, ld, device = _matrix(weight, "weight")
+        weight, r, _, ld, index = _rows(weight, "weight")
         dtype = self._dtype or (torch.bfloat16 if weight.dtype is torch.float32 else weight.dtype)
         _half(dtype, "dtype")
         if self.bias is not None:
-            _vector(self.bias, r, "bias", device)
-        if device.index != _current():
-            with torch.cuda.device(device):
+            _floats(self.bias, r, index, "bias")
+        if index != _current():
+            with torch.cuda.device(index):
                 return self.set_weight(weight)
         if weight.dtype is not dtype or not _on_boundary(weight.data_ptr(), ld, r):
-            weight, ld = _packed(weight, ld, dtype, device.index)
-        self.weight, self._device = weight, device
+            weight, ld = _packed(weight, ld, dtype, index)
+        self.weight, self._index = weight, index
         self._x = self._z = None
-        self._stream = self._saved_on = _raw_stream(device.index)      # where the allocator takes the tensors to be in use
+        self._stream = self._saved_on = _raw_stream(index)      # where the allocator takes the tensors to be in use
 
     def _used(self, saved: bool):
         """Tells the allocator of the current stream: dropped before that has run, the layer's memory is kept until it has."""
-        raw = _raw_stream(self._device.index)
+        raw = _raw_stream(self._index)
         if raw != self._stream:
-            self.weight.record_stream(torch.cuda.current_stream(self._device))
+            self.weight.record_stream(torch.cuda.current_stream(self._index))
             if self.bias is not None:
-                self.bias.record_stream(torch.cuda.current_stream(self._device))
+                self.bias.record_stream(torch.cuda.current_stream(self._index))
             self._stream = raw
         if saved and raw != self._saved_on:
             for t in (self._x, self._z):
                 if t is not None:
-                    t.record_stream(torch.cuda.current_stream(self._device))
+                    t.record_stream(torch.cuda.current_stream(self._index))
             self._saved_on = raw
+        return raw
 
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None, training: bool = False, out_dtype: torch.dtype | None = None,
                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.forward(x, residual, training, out_dtype, out)
-        if x.device != self._device:
-            raise ValueError(f"x on {x.device}, the weights on {self._device}")
-        if self._device.index != _current():
-            with torch.cuda.device(self._device):
+        index = self._index
+        if x.get_device() != index:
+            raise ValueError(f"x on {x.device}, the weights on cuda:{index}")
+        if index != _current():
+            with torch.cuda.device(index):
                 return self.forward(x, residual, training, out_dtype, out)
-        self._used(False)
-        if training:
-            _half(x.dtype, "x")
-            x, m, k, ldx, _ = _matrix(x, "x")
-            if m and k and not _on_boundary(x.data_ptr(), ldx, m):      # once, for this product and for the gradient of the weights
-                x = _packed(x, ldx, x.dtype, self._device.index)[0]
-        y, z = _forward(x, self.weight, self.bias, self._act, residual, out_dtype, out, training and self._act != 0)
-        if training:
-            self._x, self._z, self._saved_on = x, z, _raw_stream(self._device.index)
+        raw = self._used(False)
+        if not training:
+            return _forward(x, self.weight, self.bias, self._act, residual, out_dtype, out, False)[0]
+        _half(x.dtype, "x")
+        x, m, k, ldx, _ = _rows(x, "x")
+        if m and k and not _on_boundary(x.data_ptr(), ldx, m):      # once, for this product and for the gradient of the weights
+            x = _packed(x, ldx, x.dtype, index)[0]
+        y, z = _forward(x, self.weight, self.bias, self._act, residual, out_dtype, out, self._act != 0)
+        self._x, self._z, self._saved_on = x, z, raw
         return y
 
     def backward(self, dy: torch.Tensor, grad_dtype: torch.dtype | None = None, dw: torch.Tensor | None = None, db: torch.Tensor | None = None,
@@ -207,52 +250,53 @@ class Linear16:
                 return self.backward(dy, grad_dtype, dw, db, need_dx)
         if self._x is None:
             raise RuntimeError("backward needs a forward with training=True before it")
-        x, z, device = self._x, self._z, self._device
-        index, dt = device.index, _HALVES[x.dtype]
+        x, z, index, act = self._x, self._z, self._index, self._act
+        dtype = x.dtype
+        dt = _HALVES[dtype]
         if index != _current():
-            with torch.cuda.device(device):
+            with torch.cuda.device(index):
                 return self.backward(dy, grad_dtype, dw, db, need_dx)
         (m, k), n = x.shape, self.weight.shape[0]
-        dy, lddy = _like(dy, m, n, x.dtype, device, "dy")
-        grad_dtype = grad_dtype or x.dtype
+        dy, lddy = _like(dy, m, n, dtype, index, "dy")
+        grad_dtype = grad_dtype or dtype
         if dw is None:
-            dw, ldo = _empty((n, k), dtype=grad_dtype, device=device), k
+            dw, ldo = x.new_empty((n, k), dtype=grad_dtype), k
         else:
-            ldo = _out(dw, n, k, device)
+            ldo = _given(dw, n, k, index, "dw")
         if self.bias is None:
             db = None
         elif db is None:
-            db = _empty(n, dtype=grad_dtype, device=device)
-        elif db.shape != (n,) or db.device != device or not db.is_contiguous():
-            raise ValueError(f"db: {n} contiguous values on {device} expected, got {tuple(db.shape)} on {db.device}")
+            db = x.new_empty(n, dtype=grad_dtype)
+        elif db.shape != (n,) or db.get_device() != index or not db.is_contiguous():
+            raise ValueError(f"db: {n} contiguous values on cuda:{index} expected, got {tuple(db.shape)} on {db.device}")
         for g, what in ((dw, "dw"), (db, "db")):
-            if g is not None and g.dtype is not x.dtype and g.dtype is not torch.float32:
-                raise TypeError(f"{what}: {x.dtype} or float32 expected, got {g.dtype}")
-        self._used(True)
-        raw = _raw_stream(index)
-        dz, lddz = dy, lddy
-        if self._act or db is not None:
+            if g is not None and g.dtype is not dtype and g.dtype is not torch.float32:
+                raise TypeError(f"{what}: {dtype} or float32 expected, got {g.dtype}")
+        raw = self._used(True)
+        dz, lddz, buf = dy.data_ptr(), lddy, None
+        if act or db is not None:
+            # dz, and behind it what the sums need
+            ldn = (n + 7) // 8 * 8
+            at = 2 * m * ldn if act else 0
             size = load_library().ds_f16_slope_workspace(m, n) if db is not None else 0
-            ws = _empty(size, dtype=torch.uint8, device=device) if size else None
-            if self._act:
-                lddz = (n + 7) // 8 * 8
-                dz = _empty((m, lddz), dtype=x.dtype, device=device)[:, :n]
-            rc = _struct(_slope_at, raw, dt, m, n, dy.data_ptr(), lddy, None if z is None else z.data_ptr(), 0 if z is None else z.stride(0), self._act,
-                         dz.data_ptr() if self._act else None, lddz, None if db is None else db.data_ptr(), 0 if db is None else _DTYPES[db.dtype],
-                         ws.data_ptr() if size else None, size)
+            buf = x.new_empty((at + size + 1) // 2 + 8)
+            base = buf.data_ptr()
+            rc = _struct(_slope_at, raw, dt, m, n, dz, lddy, None if z is None else z.data_ptr(), ldn, act, base if act else None, ldn,
+                         None if db is None else db.data_ptr(), 0 if db is None else _DTYPES[db.dtype], base + at if size else None, size)
             if rc:
                 _check(rc, "ds_f16_slope")
-        if need_dx and m and n and not _on_boundary(dz.data_ptr(), lddz, m):      # once, for both products
-            dz, lddz = _packed(dz, lddz, x.dtype, index)
+            if act:
+                dz, lddz = base, ldn
+        if need_dx and m and n and not _on_boundary(dz, lddz, m):      # once, for both products
+            buf, lddz = _packed(dy, lddz, dtype, index)
+            dz = buf.data_ptr()
         dx = None
         if need_dx:
-            dx = _empty((m, k), dtype=x.dtype, device=device)
+            dx = x.new_empty((m, k))
             if m and k:
-                _product(DS_F16_INPUTS, dt, m, k, n, dz.data_ptr(), lddz, self.weight.data_ptr(), self.weight.stride(0), None, 0, None, 0, None, 0, dx.data_ptr(), dt, k,
-                         index, device)
+                _product(DS_F16_INPUTS, dt, m, k, n, dz, lddz, self.weight.data_ptr(), self.weight.stride(0), None, 0, None, 0, None, 0, dx.data_ptr(), dt, k, index, raw, x)
         if n and k:
-            _product(DS_F16_WEIGHTS, dt, n, k, m, dz.data_ptr(), lddz, x.data_ptr(), x.stride(0), None, 0, None, 0, None, 0, dw.data_ptr(), _DTYPES[dw.dtype], ldo, index,
-                     device)
+            _product(DS_F16_WEIGHTS, dt, n, k, m, dz, lddz, x.data_ptr(), x.stride(0), None, 0, None, 0, None, 0, dw.data_ptr(), _DTYPES[dw.dtype], ldo, index, raw, x)
         return dx, dw, db
 
 
@@ -281,17 +325,16 @@ def dropout(x: torch.Tensor, p: float, seed: int, step: int = 0, layer: int = 0,
     if _struct is None:
         _load()
     dt = _m._dtype(x.dtype, "x")
-    x, r, c, ld, device = _matrix(x, "x")
-    index = device.index
+    x, r, c, ld, index = _rows(x, "x")
     if index != _current():
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             return dropout(x, p, seed, step, layer, out)
     if out is None:
-        out, ldo = _empty((r, c), dtype=x.dtype, device=device), c
+        out, ldo = x.new_empty((r, c)), c
     elif out.dtype is not x.dtype:
         raise TypeError(f"out: {x.dtype} expected, got {out.dtype}")
     else:
-        ldo = _out(out, r, c, device)
+        ldo = _given(out, r, c, index, "out")
     rc = _call(_dropout_at, x.data_ptr(), dt, r, c, ld, out.data_ptr(), ldo, _threshold(p), seed & 0xFFFFFFFFFFFFFFFF, _word(layer, "layer"), _word(step, "step"),
                _raw_stream(index))
     if rc:
@@ -321,34 +364,34 @@ class ResidualNorm:
         self._norm, self._scale, self._eps = _NORMS[norm], float(residual_scale), float(eps)
         self._drop = (_threshold(p), seed & 0xFFFFFFFFFFFFFFFF, _word(layer, "layer"))
         self._tensors = {"post_weight": post_weight, "post_bias": post_bias, "gate": gate, "pre_weight": pre_weight, "pre_bias": pre_bias}
-        given = [t for t in self._tensors.values() if t is not None]
-        self.cols = given[0].shape[-1] if given else None
-        self._device = device = given[0].device if given else None
-        if given and not given[0].is_cuda:
-            raise ValueError("parameters: CUDA tensors expected: there is no CPU path")
-        self._groups = 0
-        if gate is not None:
-            if gate.dim() == 2:
-                self._groups = gate.shape[0]
-            elif gate.dim() == 1:
-                self._groups = 1
-            if not self._groups:
-                raise ValueError(f"gate: [cols] or [groups, cols] expected, got {tuple(gate.shape)}")
-        at = {name: None if t is None else _vector(t.reshape(-1) if name == "gate" and t.is_contiguous() else t,
-                                                   self.cols * self._groups if name == "gate" else self.cols, name, device) for name, t in self._tensors.items()}
-        self._params = (at["post_weight"], at["post_bias"], at["gate"], self._groups, at["pre_weight"], at["pre_bias"], self._scale, self._eps, *self._drop)
-        self._stream = None if device is None else _raw_stream(device.index)
-        self._saved = None
+        self.cols = self._index = None
+        self._groups, at = 0, []
+        for name, t in self._tensors.items():
+            if t is None:
+                at.append(None)
+                continue
+            if self.cols is None:
+                self.cols, self._index = t.shape[-1] if t.dim() else 0, t.get_device()
+                if self._index < 0:
+                    raise ValueError(f"{name}: a CUDA tensor expected: there is no CPU path")
+            if name == "gate":
+                if not 1 <= t.dim() <= 2 or t.shape[-1] != self.cols or not t.numel() or t.dtype is not torch.float32 or not t.is_contiguous() or t.get_device() != self._index:
+                    raise ValueError(f"gate: [cols] or [groups, cols] contiguous float32 values beside the others expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+                self._groups = t.shape[0] if t.dim() == 2 else 1
+                at.append(t.data_ptr())
+            else:
+                at.append(_floats(t, self.cols, self._index, name))
+        self._params = (at[0], at[1], at[2], self._groups, at[3], at[4], self._scale, self._eps, *self._drop)
+        self._stream = None if self._index is None else _raw_stream(self._index)
+        self._saved, self._workspaces = None, {}
 
-    def _used(self, saved=()):
+    def _used(self, raw: int, index: int, saved=()):
         """Tells the allocator of the current stream, on which parameters and what is kept are about to be used."""
-        device = self._device if self._device is not None else saved[0].device
-        raw = _raw_stream(device.index)
         if raw != self._stream:
             if self._stream is not None:
                 for t in (*self._tensors.values(), *saved):
                     if t is not None:
-                        t.record_stream(torch.cuda.current_stream(device))
+                        t.record_stream(torch.cuda.current_stream(index))
             self._stream = raw
 
     def forward(self, y: torch.Tensor, x: torch.Tensor | None = None, step: int = 0, training: bool = False, need_h: bool = True, h: torch.Tensor | None = None,
@@ -360,64 +403,68 @@ class ResidualNorm:
                 return self.forward(y, x, step, training, need_h, h, n)
         if _struct is None:
             _load()
-        dt = _m._dtype(y.dtype, "y")
-        y, rows, cols, ldy, device = _matrix(y, "y")
-        index = device.index
-        if self.cols is not None and (cols != self.cols or device != self._device):
-            raise ValueError(f"y: rows of {self.cols} on {self._device} expected, got {cols} on {device}")
+        dtype = y.dtype
+        dt = _DTYPES.get(dtype)
+        if dt is None:
+            _m._dtype(dtype, "y")
+        y, rows, cols, ldy, index = _rows(y, "y")
+        if cols != self.cols and self.cols is not None or index != self._index and self._index is not None:
+            raise ValueError(f"y: rows of {self.cols} on cuda:{self._index} expected, got {cols} on cuda:{index}")
         if not 0 < cols <= DS_NORM_MAX_COLS:
             raise ValueError(f"y: rows of 1 to {DS_NORM_MAX_COLS} entries expected, got {cols}")
         if self._groups and rows % self._groups:
             raise ValueError(f"y: {rows} rows are not {self._groups} equal runs")
         if index != _current():
-            with torch.cuda.device(device):
+            with torch.cuda.device(index):
                 return self.forward(y, x, step, training, need_h, h, n)
-        xp, ldx, sdt, stype = None, 0, dt, y.dtype
+        xp, ldx, sdt, stype = None, 0, dt, dtype
         if x is not None:
-            if x.dtype is not y.dtype and x.dtype is not torch.float32:
-                raise TypeError(f"x: {y.dtype} or float32 expected, got {x.dtype}")
-            x, ldx = _like(x, rows, cols, x.dtype, device, "x")
-            xp, stype = x.data_ptr(), x.dtype
-            sdt = _DTYPES[stype]
+            stype = x.dtype
+            if stype is not dtype and stype is not torch.float32:
+                raise TypeError(f"x: {dtype} or float32 expected, got {stype}")
+            x, ldx = _like(x, rows, cols, stype, index, "x")
+            xp, sdt = x.data_ptr(), _DTYPES[stype]
         pre = self._params[4] is not None
-        if not need_h and not pre:
-            raise ValueError("nothing to compute")
+        hp, ldh = None, 0
         if h is not None:
             if x is None and h.dtype is torch.float32:
                 stype, sdt = torch.float32, DS_F32
             if h.dtype is not stype:
                 raise TypeError(f"h: {stype} expected, got {h.dtype}")
-            ldh = _out(h, rows, cols, device)
+            ldh = _given(h, rows, cols, index, "h")
+            hp = h.data_ptr()
         elif need_h:
-            h, ldh = _empty((rows, cols), dtype=stype, device=device), cols
-        else:
-            ldh = 0
-        ldn = 0
+            h, ldh = (y if x is None else x).new_empty((rows, cols)), cols
+            hp = h.data_ptr()
+        elif not pre:
+            raise ValueError("nothing to compute")
+        np_, ldn = None, 0
         if not pre:
             if n is not None:
                 raise ValueError("n: there is no pre norm")
-        elif n is not None:
-            if n.dtype is not y.dtype:
-                raise TypeError(f"n: {y.dtype} expected, got {n.dtype}")
-            ldn = _out(n, rows, cols, device)
         else:
-            n, ldn = _empty((rows, cols), dtype=y.dtype, device=device), cols
-        if self._device is not None:
-            self._used()
-        stats = None
+            if n is None:
+                n, ldn = y.new_empty((rows, cols)), cols
+            elif n.dtype is not dtype:
+                raise TypeError(f"n: {dtype} expected, got {n.dtype}")
+            else:
+                ldn = _given(n, rows, cols, index, "n")
+            np_ = n.data_ptr()
+        raw = _raw_stream(index)
+        if raw != self._stream:
+            self._used(raw, index)
+        stats = sp = None
+        yp = y.data_ptr()
         if training:
-            stats = _empty((rows, 4), dtype=torch.float32, device=device)
-            for o in (h, n):
-                if o is not None and rows and any(i is not None and i.data_ptr() == o.data_ptr() for i in (x, y)):
-                    raise ValueError("a training forward may not write over its inputs")
-        rc = _struct(_norm_at, _raw_stream(index), dt, sdt, rows, cols, self._norm, y.data_ptr(), ldy, xp, ldx, *self._params, _word(step, "step"),
-                     None if stats is None else stats.data_ptr(), None if h is None else h.data_ptr(), ldh, None if n is None else n.data_ptr(), ldn)
+            stats = y.new_empty((rows, 4), dtype=torch.float32)
+            sp = stats.data_ptr()
+            if rows and (hp in (xp, yp) and hp or np_ in (xp, yp) and np_):
+                raise ValueError("a training forward may not write over its inputs")
+        rc = _struct(_norm_at, raw, dt, sdt, rows, cols, self._norm, yp, ldy, xp, ldx, *self._params, _word(step, "step"), sp, hp, ldh, np_, ldn)
         if rc:
             _check(rc, "ds_norm_forward")
         if training:
             self._saved = (y, ldy, x, ldx, stats, step, stype)
-            if self._device is None:
-                self._stream = _raw_stream(index)
         return h, n
 
     def backward(self, dh: torch.Tensor | None = None, dn: torch.Tensor | None = None, need_dx: bool = True, out: dict | None = None, stream=None):
@@ -429,47 +476,54 @@ class ResidualNorm:
         if self._saved is None:
             raise RuntimeError("backward needs a forward with training=True before it")
         y, ldy, x, ldx, stats, step, stype = self._saved
-        (rows, cols), device = y.shape, y.device
-        index = device.index
+        (rows, cols), dtype, index = y.shape, y.dtype, y.get_device()
         if index != _current():
-            with torch.cuda.device(device):
+            with torch.cuda.device(index):
                 return self.backward(dh, dn, need_dx, out)
         if dh is None and dn is None:
             raise ValueError("the gradient of h or of n expected")
         dhp = dnp = None
         lddh = lddn = 0
         if dh is not None:
-            dh, lddh = _like(dh, rows, cols, stype, device, "dh")
+            dh, lddh = _like(dh, rows, cols, stype, index, "dh")
             dhp = dh.data_ptr()
         if dn is not None:
             if self._params[4] is None:
                 raise ValueError("dn: there is no pre norm")
-            dn, lddn = _like(dn, rows, cols, y.dtype, device, "dn")
+            dn, lddn = _like(dn, rows, cols, dtype, index, "dn")
             dnp = dn.data_ptr()
-        out = out or {}
-        unknown = [k for k in out if self._tensors.get(k) is None]
-        if unknown:
-            raise ValueError(f"out: no parameter {', '.join(map(str, unknown))}")
         grads, at = {}, []
         for name, t in self._tensors.items():
             if t is None:
+                if out and name in out:
+                    raise ValueError(f"out: there is no {name}")
                 at.append(None)
                 continue
-            g = out.get(name)
+            g = out.get(name) if out else None
             if g is None:
-                g = _empty(t.shape, dtype=torch.float32, device=device)
-            elif g.dtype is not torch.float32 or g.shape != t.shape or g.device != device or not g.is_contiguous():
-                raise ValueError(f"out[{name!r}]: contiguous float32 values {tuple(t.shape)} on {device} expected")
+                g = stats.new_empty(t.shape)
+            elif g.dtype is not torch.float32 or g.shape != t.shape or g.get_device() != index or not g.is_contiguous():
+                raise ValueError(f"out[{name!r}]: contiguous float32 values {tuple(t.shape)} on cuda:{index} expected")
             grads[name] = g
             at.append(g.data_ptr())
-        self._used((y, x, stats))
-        dy = _empty((rows, cols), dtype=y.dtype, device=device)
-        dx = _empty((rows, cols), dtype=stype, device=device) if x is not None and need_dx else None
-        members = [_DTYPES[y.dtype], _DTYPES[stype], rows, cols, self._norm, y.data_ptr(), ldy, None if x is None else x.data_ptr(), ldx, *self._params, step, stats.data_ptr(),
+        if out and any(name not in self._tensors for name in out):
+            raise ValueError(f"out: parameters are {', '.join(self._tensors)}")
+        raw = _raw_stream(index)
+        if raw != self._stream:
+            self._used(raw, index, (y, x, stats))
+        dy, dx = y.new_empty((rows, cols)), None
+        if x is not None and need_dx:
+            dx = x.new_empty((rows, cols))
+        members = [_DTYPES[dtype], _DTYPES[stype], rows, cols, self._norm, y.data_ptr(), ldy, None if x is None else x.data_ptr(), ldx, *self._params, step, stats.data_ptr(),
                    None, 0, None, 0, dhp, lddh, dnp, lddn, None if dx is None else dx.data_ptr(), cols, dy.data_ptr(), cols, *at]
-        size = load_library().ds_norm_backward_workspace(C.byref(ds_norm_args(*(0 if v is None else v for v in members))))
-        ws = _empty(size, dtype=torch.uint8, device=device) if size else None
-        rc = _struct(_norm_back_at, _raw_stream(index), *members, ws.data_ptr() if size else None, size)
+        size = self._workspaces.get((rows, cols))
+        if size is None:
+            size = load_library().ds_norm_backward_workspace(C.byref(ds_norm_args(*(0 if v is None else v for v in members))))
+        ws = stats.new_empty((size + 3) // 4) if size else None
+        rc = _struct(_norm_back_at, raw, *members, ws.data_ptr() if size else None, size)
         if rc:
             _check(rc, "ds_norm_backward")
+        if len(self._workspaces) > 64:
+            self._workspaces.clear()
+        self._workspaces[rows, cols] = size      # of the parameters' gradients; the others need none
         return dy, dx, grads
