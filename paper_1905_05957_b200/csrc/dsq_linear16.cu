@@ -322,6 +322,10 @@ __global__ void __launch_bounds__(256) k_f16_sums(const float* sums, uint32_t bl
 
 // ---- host side ------------------------------------------------------------------------------------------
 
+// Entries that rows of copied operands are a multiple of: whole lines of 128 bytes.  (Rows on other boundaries of 16 bytes span a line more in every step of K:
+// 4096 x 4096 x 4104 takes 114 us so, and 88 on lines.)
+constexpr uint64_t kLine = 64;
+
 struct Shape16 {
   uint64_t rows_a, cols_a, rows_b, cols_b;      // as they lie in memory
   bool copy_a, copy_b;
@@ -335,8 +339,8 @@ Shape16 shape_of(const ds_f16_product* p) {
   // a single row has no pitch
   s.copy_a = !aligned(p->a, 16) || (s.rows_a > 1 && p->lda % 8);
   s.copy_b = !aligned(p->b, 16) || (s.rows_b > 1 && p->ldb % 8);
-  s.bytes_a = s.copy_a ? round_up(s.rows_a * round_up(s.cols_a, 8) * 2, 256) : 0;
-  s.bytes_b = s.copy_b ? round_up(s.rows_b * round_up(s.cols_b, 8) * 2, 256) : 0;
+  s.bytes_a = s.copy_a ? round_up(s.rows_a * round_up(s.cols_a, kLine) * 2, 256) : 0;
+  s.bytes_b = s.copy_b ? round_up(s.rows_b * round_up(s.cols_b, kLine) * 2, 256) : 0;
   return s;
 }
 
@@ -459,12 +463,12 @@ int ds_f16_matmul(const ds_f16_product* p, void* cuda_stream) {
   Operand16 a{p->a, s.rows_a > 1 ? p->lda : round_up(s.cols_a, 8), o.m, a_across}, b{p->b, s.rows_b > 1 ? p->ldb : round_up(s.cols_b, 8), o.n, b_across};
   uint8_t* ws = static_cast<uint8_t*>(p->workspace);
   if (s.copy_a) {
-    const uint64_t ld = round_up(s.cols_a, 8);
+    const uint64_t ld = round_up(s.cols_a, kLine);
     e = pack(p->a, (int)p->dtype, s.rows_a, s.cols_a, p->lda, ws, (int)p->dtype, ld, st);
     a.p = ws, a.ld = ld;
   }
   if (e == cudaSuccess && s.copy_b) {
-    const uint64_t ld = round_up(s.cols_b, 8);
+    const uint64_t ld = round_up(s.cols_b, kLine);
     e = pack(p->b, (int)p->dtype, s.rows_b, s.cols_b, p->ldb, ws + s.bytes_a, (int)p->dtype, ld, st);
     b.p = ws + s.bytes_a, b.ld = ld;
   }

@@ -70,7 +70,7 @@ def test_product_workspace(lib):
         return lib.ds_f16_matmul_workspace(C.byref(_args(b.ds_f16_product, PRODUCT, **kw)))
     assert size() == 0 and size(k=63, lda=64, ldb=64) == 0
     assert size(lda=65) == 40 * 64 * 2 and size(b=P + 2) == 24 * 64 * 2 and size(a=P + 2, ldb=65) == 64 * 64 * 2
-    assert size(layout=2, lda=41) == 64 * 40 * 2 and size(layout=1, ldb=25) == 64 * 24 * 2
+    assert size(layout=2, lda=41) == 64 * 64 * 2 and size(layout=1, ldb=25) == 64 * 64 * 2      # rows of whole lines
     assert size(m=1, lda=7) == 0                                                      # a single row has no pitch
     assert lib.ds_f16_matmul(None, None) == INVALID and lib.ds_f16_matmul_workspace(None) == 0
 
