@@ -409,10 +409,14 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_backward(const NormPar
   // what the slices summed of one kind, into a vector
   auto flush_to = [&](const float (&s)[8], float* to) {
     const uint32_t width = blockDim.x * 8, c0 = at.rank * width;
-    if (blockDim.y == 1) {
+    if (blockDim.y == 1) {      // (entry by entry, a warp's stores touch 32 sectors each: a single row of 4096 took 7.9 us)
+      if (at.c + 8 <= p.cols && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+        store_piece8(to + at.c, s);
+      } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (at.c + j < p.cols) to[at.c + j] = s[j];
+        for (int j = 0; j < 8; ++j)
+          if (at.c + j < p.cols) to[at.c + j] = s[j];
+      }
     } else {
       __syncthreads();
 #pragma unroll
@@ -601,8 +605,10 @@ struct SumsParams {
   uint32_t count[5], vectors[5];      // vectors: of this kind (gates: one a group), `count` steps apart
   uint32_t cols;
 };
-__global__ void __launch_bounds__(256) k_norm_sums(const SumsParams p) {
-  __shared__ float part[8][32];
+constexpr int kSumThreads = 512;
+__global__ void __launch_bounds__(kSumThreads) k_norm_sums(const SumsParams p) {
+  constexpr int kWarps = kSumThreads / 32, kBatch = 10;      // loads in flight: those of 160 CTAs' sums at once
+  __shared__ float part[kWarps][32];
   pdl_prologue();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t col = blockIdx.x * 32 + lane;
@@ -610,12 +616,11 @@ __global__ void __launch_bounds__(256) k_norm_sums(const SumsParams p) {
   while (v >= p.vectors[kind]) v -= p.vectors[kind++];
   const float* in = p.in[kind] + (uint64_t)v * p.count[kind] * p.step[kind];
   float s = 0.f;
-  constexpr int kBatch = 10;      // loads in flight
   if (col < p.cols)
-    for (uint32_t i = warp; i < p.count[kind]; i += 8 * kBatch) {
+    for (uint32_t i = warp; i < p.count[kind]; i += kWarps * kBatch) {
       float t[kBatch];
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) t[b] = i + 8 * b < p.count[kind] ? ld_plain(in + (i + 8 * b) * p.step[kind] + col) : 0.f;
+      for (int b = 0; b < kBatch; ++b) t[b] = i + kWarps * b < p.count[kind] ? ld_plain(in + (i + kWarps * b) * p.step[kind] + col) : 0.f;
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) s += t[b];
     }
@@ -624,7 +629,7 @@ __global__ void __launch_bounds__(256) k_norm_sums(const SumsParams p) {
   if (warp || col >= p.cols) return;
   s = 0.f;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) s += part[w][lane];
+  for (int w = 0; w < kWarps; ++w) s += part[w][lane];
   p.out[kind][(uint64_t)v * p.cols + col] = s;
 }
 
@@ -893,7 +898,7 @@ int ds_norm_backward(const ds_norm_args* p, void* cuda_stream) {
   s.cols = (uint32_t)p->cols;
   cudaError_t e = by_types(p, [&](auto sx_, auto sy_) { return backward<decltype(sx_), decltype(sy_)>(q, b, st); });
   if (e == cudaSuccess && vectors) {
-    launch_pdl(k_norm_sums, dim3((uint32_t)((p->cols + 31) / 32), vectors), dim3(256), st, s);
+    launch_pdl(k_norm_sums, dim3((uint32_t)((p->cols + 31) / 32), vectors), dim3(kSumThreads), st, s);
     count_launches(1);
     e = cudaGetLastError();
   }
