@@ -145,8 +145,8 @@ __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 struct SumSpace {
-  float warp[2][16][3];      // of each warp; the two halves take turns, so that one barrier is enough
-  float cta[2][8][3];        // of each CTA of a cluster
+  float warp[2][16][4];      // of each warp; the two halves take turns, so that one barrier is enough
+  float cta[2][8][4];        // of each CTA of a cluster
 };
 struct RowSum {
   SumSpace* space;
@@ -212,16 +212,22 @@ struct Place {
 };
 
 // ---- forward --------------------------------------------------------------------------------------------
-// FULL: layer norms or biases.  Parameters stay in registers.  A slice has two rows in hand, whose sums share their barriers.
-template <class X, class Y>
+// FULL: layer norms or biases.  Parameters stay in registers.  A slice has ROWS rows in hand, whose sums share their barriers: a row takes mostly
+// the time from its first addition to its sums (16384 x 4096 in bf16, RMS norms before and after: 100 us by two rows, 96 by four; 8192 x 8192: 199 and 151; layer norms
+// 144 by two, 139 by three, 174 by four, which no longer fit into the registers; floats fill shared memory with two).
+template <class X, class Y, bool FULL>
+constexpr int kRowsInHand = sizeof(X) + sizeof(Y) == 8 ? 2 : FULL ? 3 : 4;
+template <class X, class Y, int ROWS>
 struct ForwardRing {
-  static constexpr int kDepth = 3;                                             // pairs of rows
-  static constexpr uint32_t kRow = kWarpBytes<X> + kWarpBytes<Y>, kWarp = 2 * kRow;      // a warp's part of a row, of a pair
+  static constexpr uint32_t kRow = kWarpBytes<X> + kWarpBytes<Y>, kWarp = ROWS * kRow;      // a warp's part of a row, and of the rows in hand
+  static constexpr int kDepth = 16 * kWarp * 3 <= 220 * 1024 ? 3 : 2;
+  static constexpr uint32_t kThread = kDepth * kWarp / 32;                                  // bytes a thread
 };
-template <class X, class Y, bool FULL, bool VEC>
+template <class X, class Y, bool FULL, bool VEC, int ROWS>
 __global__ void __launch_bounds__(kNormThreads, 1) k_norm_forward(const NormParams p) {
-  using R = ForwardRing<X, Y>;
-  extern __shared__ __align__(16) uint8_t ring[];      // [depth][warps][2][y | x]
+  using R = ForwardRing<X, Y, ROWS>;
+  constexpr int kRows = ROWS;
+  extern __shared__ __align__(16) uint8_t ring[];      // [depth][warps][rows][y | x]
   __shared__ SumSpace space;
   pdl_prologue();
   const Place at(p);
@@ -237,13 +243,14 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_forward(const NormPara
     if (ahead.unit < p.units) {
       const uint32_t to = mine + put * slot_bytes;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (ahead.row + i * blockDim.y < ahead.last) {
-          const uint32_t row = ahead.row + i * blockDim.y;
+      for (int i = 0; i < kRows; ++i) {
+        const uint32_t row = ahead.row + i * blockDim.y;
+        if (row < ahead.last) {
           fetch_row<VEC, Y>(to + i * R::kRow, p.y.at(row) + at.c_warp * sizeof(Y), at.left_warp, at.lane);
           if (p.x.p) fetch_row<VEC, X>(to + i * R::kRow + kWarpBytes<Y>, p.x.at(row) + at.c_warp * sizeof(X), at.left_warp, at.lane);
         }
-      ahead.row += 2 * blockDim.y;
+      }
+      ahead.row += kRows * blockDim.y;
       if (ahead.row >= ahead.last) ahead.find(p, ahead.unit + at.teams, at.teams);
     }
     commit_rows();
@@ -258,18 +265,19 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_forward(const NormPara
   load_param8(p.pre_w, at.c, p.cols, 0.f, w2);
   if constexpr (FULL) load_param8(p.pre_b, at.c, p.cols, 0.f, b2);
 
-  // mean and 1 / size of the two rows
-  auto statistics = [&](const float (&v)[2][8], float (&mean)[2], float (&r)[2]) {
-    mean[0] = mean[1] = 0.f;
-    float q[2] = {0.f, 0.f};
+  // mean and 1 / size of the rows
+  auto statistics = [&](const float (&v)[kRows][8], float (&mean)[kRows], float (&r)[kRows]) {
+    float q[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) mean[i] = q[i] = 0.f;
     if (FULL && p.layer) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < kRows; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) mean[i] += v[i][j];
       sum(mean);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kRows; ++i) {
         mean[i] *= inv;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -280,13 +288,13 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_forward(const NormPara
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < kRows; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) q[i] = __fmaf_rn(v[i][j], v[i][j], q[i]);
     }
     sum(q);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) r[i] = rsqrtf(__fmaf_rn(q[i], inv, p.eps));      // good to 2 units of 2^-23
+    for (int i = 0; i < kRows; ++i) r[i] = rsqrtf(__fmaf_rn(q[i], inv, p.eps));      // good to 2 units of 2^-23
   };
   for (now.find(p, at.team, at.teams); now.unit < p.units; now.find(p, now.unit + at.teams, at.teams)) {
     const uint32_t g = now.unit / p.units_per_group;
@@ -304,51 +312,53 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_forward(const NormPara
       }
       group = g;
     }
-    for (; now.row < now.last; now.row += 2 * blockDim.y) {
+    for (; now.row < now.last; now.row += kRows * blockDim.y) {
       wait_rows<R::kDepth - 2>();
       fetch();
       const uint32_t from = mine + get * slot_bytes;
       if (++get == R::kDepth) get = 0;
-      const bool two = now.row + blockDim.y < now.last;      // else the second row is what the ring held: worked on, not stored
-      const uint32_t row[2] = {now.row, two ? now.row + blockDim.y : now.row};
-      float v[2][8], m1[2] = {0.f, 0.f}, r1[2] = {0.f, 0.f}, m2[2] = {0.f, 0.f}, r2[2] = {0.f, 0.f};
+      // rows that are not there are what the ring held: worked on, not stored
+      auto there = [&](int i) { return !i || now.row + i * blockDim.y < now.last; };
+      auto row = [&](int i) { return now.row + i * blockDim.y; };
+      float v[kRows][8], mean[kRows], r[kRows];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) read_row8<VEC, Y>(from + i * R::kRow, VEC ? 0 : p.y.shift(row[i]), at.left, at.lane, v[i]);
+      for (int i = 0; i < kRows; ++i) read_row8<VEC, Y>(from + i * R::kRow, VEC ? 0 : p.y.shift(row(i)), at.left, at.lane, v[i]);
+      float2* st = reinterpret_cast<float2*>(p.stats);
+      const bool notes = st && threadIdx.x == 0 && at.rank == 0;
       if (p.post_w) {
-        statistics(v, m1, r1);
+        statistics(v, mean, r);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kRows; ++i) {
+          if (notes && there(i)) st[2 * row(i)] = make_float2(mean[i], r[i]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[i][j] = (FULL ? v[i][j] - m1[i] : v[i][j]) * r1[i];
+          for (int j = 0; j < 8; ++j) v[i][j] = (FULL ? v[i][j] - mean[i] : v[i][j]) * r[i];
+        }
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kRows; ++i) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = FULL ? __fmaf_rn(v[i][j], gw[j], gb[j]) : v[i][j] * gw[j];
-        if (p.drop.threshold) drop8(p.drop, draw8(p.drop, row[i], at.c), v[i]);
+        if (p.drop.threshold) drop8(p.drop, draw8(p.drop, row(i), at.c), v[i]);
         if (p.x.p) {
           float t[8];
-          read_row8<VEC, X>(from + i * R::kRow + kWarpBytes<Y>, VEC ? 0 : p.x.shift(row[i]), at.left, at.lane, t);
+          read_row8<VEC, X>(from + i * R::kRow + kWarpBytes<Y>, VEC ? 0 : p.x.shift(row(i)), at.left, at.lane, t);
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[i][j] = __fmaf_rn(p.residual_scale, t[j], v[i][j]);
         }
-        if (p.h.p && (!i || two)) store_row8<VEC>(p.h.out<X>(row[i]), at.c, p.cols, at.lane, v[i]);
+        if (p.h.p && there(i)) store_row8<VEC>(p.h.out<X>(row(i)), at.c, p.cols, at.lane, v[i]);
       }
       if (p.pre_w) {
-        statistics(v, m2, r2);
+        statistics(v, mean, r);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kRows; ++i) {
+          if (notes && there(i)) st[2 * row(i) + 1] = make_float2(mean[i], r[i]);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            v[i][j] = (FULL ? v[i][j] - m2[i] : v[i][j]) * r2[i];
+            v[i][j] = (FULL ? v[i][j] - mean[i] : v[i][j]) * r[i];
             v[i][j] = FULL ? __fmaf_rn(v[i][j], w2[j], b2[j]) : v[i][j] * w2[j];
           }
-          if (!i || two) store_row8<VEC>(p.n.out<Y>(row[i]), at.c, p.cols, at.lane, v[i]);
+          if (there(i)) store_row8<VEC>(p.n.out<Y>(row(i)), at.c, p.cols, at.lane, v[i]);
         }
-      }
-      if (p.stats && threadIdx.x == 0 && at.rank == 0) {
-        p.stats[row[0]] = make_float4(m1[0], r1[0], m2[0], r2[0]);
-        if (two) p.stats[row[1]] = make_float4(m1[1], r1[1], m2[1], r2[1]);
       }
     }
   }
@@ -701,13 +711,18 @@ cudaError_t launch(NormParams q, const NormPlan& b, uint32_t smem, uint32_t most
   return cudaGetLastError();
 }
 inline bool full(const NormParams& q) { return q.layer || q.post_b || q.pre_b; }
+template <class X, class Y, bool FULL, int ROWS>
+cudaError_t forward_by(const NormParams& q, const NormPlan& b, cudaStream_t st) {
+  constexpr uint32_t kThread = ForwardRing<X, Y, ROWS>::kThread;
+  const uint32_t smem = b.tx * b.ty * kThread, most = kNormThreads * kThread;
+  return q.vec ? launch<k_norm_forward<X, Y, FULL, true, ROWS>>(q, b, smem, most, st) : launch<k_norm_forward<X, Y, FULL, false, ROWS>>(q, b, smem, most, st);
+}
 template <class X, class Y>
 cudaError_t forward(const NormParams& q, const NormPlan& b, cudaStream_t st) {
-  using R = ForwardRing<X, Y>;
-  constexpr uint32_t kThread = R::kDepth * R::kWarp / 32;      // bytes a thread
-  const uint32_t smem = b.tx * b.ty * kThread, most = kNormThreads * kThread;
-  if (q.vec) return full(q) ? launch<k_norm_forward<X, Y, true, true>>(q, b, smem, most, st) : launch<k_norm_forward<X, Y, false, true>>(q, b, smem, most, st);
-  return full(q) ? launch<k_norm_forward<X, Y, true, false>>(q, b, smem, most, st) : launch<k_norm_forward<X, Y, false, false>>(q, b, smem, most, st);
+  // two rows a slice at most, one after the other: rows that are not there would only cost time (1 x 4096: 4.5 us by four rows, 3.1 by one)
+  const bool single = b.unit_rows <= 2 * b.ty && b.units <= b.teams;
+  if (full(q)) return single ? forward_by<X, Y, true, 1>(q, b, st) : forward_by<X, Y, true, kRowsInHand<X, Y, true>>(q, b, st);
+  return single ? forward_by<X, Y, false, 1>(q, b, st) : forward_by<X, Y, false, kRowsInHand<X, Y, false>>(q, b, st);
 }
 template <class X, class Y>
 cudaError_t backward(const NormParams& q, const NormPlan& b, cudaStream_t st) {
