@@ -158,6 +158,7 @@ def load_library() -> C.CDLL:
 
 _call = None
 _STRUCT_CALLS = {"ds_f16_matmul": ds_f16_product, "ds_f16_slope": ds_f16_slope_args, "ds_norm_forward": ds_norm_args, "ds_norm_backward": ds_norm_args}
+_STRUCT_SIZES = {"ds_f16_matmul_workspace": ds_f16_product, "ds_norm_backward_workspace": ds_norm_args}
 _struct_call = None
 
 
@@ -189,22 +190,27 @@ def fast_call():
 
 
 def fast_struct_call():
-    """(call, addresses): call(addresses[name], stream, *members) calls a function of the ABI that takes a structure of 64-bit members and a
-    stream, by the same two ways."""
+    """(call, size, addresses): call(addresses[name], stream, *members) calls a function of the ABI that takes a structure of 64-bit members and a
+    stream, size(addresses[name], *members) one that takes such a structure and returns a size (members left out are 0), by the same two ways."""
     global _struct_call
     if _struct_call is None:
         lib = load_library()
-        address = {name: C.cast(getattr(lib, name), C.c_void_p).value for name in _STRUCT_CALLS}
+        kinds = {**_STRUCT_CALLS, **_STRUCT_SIZES}
+        address = {name: C.cast(getattr(lib, name), C.c_void_p).value for name in kinds}
         module = _extension()
-        if module is not None and hasattr(module, "call_struct"):
-            _struct_call = module.call_struct, address
+        if module is not None and hasattr(module, "size_struct"):
+            _struct_call = module.call_struct, module.size_struct, address
         else:
-            at = {address[name]: (getattr(lib, name), kind) for name, kind in _STRUCT_CALLS.items()}
+            at = {address[name]: (getattr(lib, name), kind) for name, kind in kinds.items()}
 
             def call(where, stream, *members):
                 function, kind = at[where]
                 return function(C.byref(kind(*(0 if v is None else v for v in members))), stream)
-            _struct_call = call, address
+
+            def size(where, *members):
+                function, kind = at[where]
+                return function(C.byref(kind(*(0 if v is None else v for v in members))))
+            _struct_call = call, size, address
     return _struct_call
 
 

@@ -6,7 +6,8 @@
  * NULL.  The caller vouches for the address and the number of arguments.
  *
  * call_struct(address, stream, a, b, ...) -> int: calls a function of the ABI that takes a structure whose members are all 64 bits
- * wide, given one by one (a Python float becomes a double), and a stream.
+ * wide, given one by one (a Python float becomes a double), and a stream.  size_struct(address, a, b, ...) -> int: one that takes such a
+ * structure alone and returns a size of 64 bits; members that are not given are 0.
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -40,6 +41,20 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 
 #define MOST_MEMBERS 64
 
+static int members(u* to, PyObject* const* args, Py_ssize_t n) {
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (args[i] == Py_None) continue;
+    if (PyFloat_CheckExact(args[i])) {
+      const double v = PyFloat_AS_DOUBLE(args[i]);
+      memcpy(to + i, &v, sizeof v);
+      continue;
+    }
+    to[i] = (u)PyLong_AsUnsignedLongLongMask(args[i]);
+    if (to[i] == (u)-1 && PyErr_Occurred()) return 0;
+  }
+  return 1;
+}
+
 static PyObject* call_struct(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   u a[MOST_MEMBERS] = {0}, head[2] = {0};
   (void)self;
@@ -47,17 +62,7 @@ static PyObject* call_struct(PyObject* self, PyObject* const* args, Py_ssize_t n
     PyErr_SetString(PyExc_TypeError, "an address, a stream and 1 to 64 members expected");
     return NULL;
   }
-  for (Py_ssize_t i = 0; i < n; ++i) {
-    u* to = i < 2 ? head + i : a + (i - 2);
-    if (args[i] == Py_None) continue;
-    if (PyFloat_CheckExact(args[i])) {
-      const double v = PyFloat_AS_DOUBLE(args[i]);
-      memcpy(to, &v, sizeof v);
-      continue;
-    }
-    *to = (u)PyLong_AsUnsignedLongLongMask(args[i]);
-    if (*to == (u)-1 && PyErr_Occurred()) return NULL;
-  }
+  if (!members(head, args, 2) || !members(a, args + 2, n - 2)) return NULL;
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = ((int (*)(const u*, u))head[0])(a, head[1]);
@@ -65,8 +70,20 @@ static PyObject* call_struct(PyObject* self, PyObject* const* args, Py_ssize_t n
   return PyLong_FromLong(rc);
 }
 
+static PyObject* size_struct(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  u a[MOST_MEMBERS] = {0}, f = 0;
+  (void)self;
+  if (n < 2 || n > MOST_MEMBERS + 1) {
+    PyErr_SetString(PyExc_TypeError, "an address and 1 to 64 members expected");
+    return NULL;
+  }
+  if (!members(&f, args, 1) || !members(a, args + 1, n - 1)) return NULL;
+  return PyLong_FromUnsignedLongLong(((u (*)(const u*))f)(a));
+}
+
 static PyMethodDef methods[] = {{"call", (PyCFunction)(void*)call, METH_FASTCALL, "call(address, *integers) -> int"},
                                 {"call_struct", (PyCFunction)(void*)call_struct, METH_FASTCALL, "call_struct(address, stream, *members) -> int"},
+                                {"size_struct", (PyCFunction)(void*)size_struct, METH_FASTCALL, "size_struct(address, *members) -> int"},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "dsq_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit_dsq_call(void) { return PyModule_Create(&module); }

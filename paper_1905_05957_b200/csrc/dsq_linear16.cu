@@ -123,8 +123,21 @@ __device__ __forceinline__ void mma_half(float (&c)[4], uint32_t a0, uint32_t a1
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// NT: groups of 8 tokens, RB: blocks of 16 rows of W.
-template <bool BF16, int NT, int RB>
+// The same of a row that starts anywhere; the granules are read that hold something of the row.
+__device__ __forceinline__ uint4 load_halves8_anywhere(const uint16_t* row, uint32_t k0, uint32_t k) {
+  if (k0 + 8 > k) return load_halves8(row, k0, k);      // entry by entry
+  const uint32_t shift = shift_of(row);
+  const uint4* at = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row + k0) - shift);
+  const uint4 a = ld_plain(at);
+  if (!shift) return a;
+  const uint4 b = ld_plain(at + 1);
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  take_from<4>(w, shift);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// NT: groups of 8 tokens, RB: blocks of 16 rows of W.  XVEC: tokens start on 16-byte boundaries (those of W always do).
+template <bool BF16, int NT, int RB, bool XVEC>
 __global__ void __launch_bounds__(256, 2) k_f16_few(const FewParams16 p) {
   constexpr int kAhead = 4;
   __shared__ float part[8][RB * 16][NT * 8 + 1];
@@ -145,7 +158,7 @@ __global__ void __launch_bounds__(256, 2) k_f16_few(const FewParams16 p) {
 #pragma unroll
     for (int i = 0; i < 2 * RB; ++i) to[i] = ld_plain(reinterpret_cast<const uint4*>(wrow[i] + k0));
 #pragma unroll
-    for (int j = 0; j < NT; ++j) xt[j] = ld_plain(reinterpret_cast<const uint4*>(xrow[j] + k0));
+    for (int j = 0; j < NT; ++j) xt[j] = XVEC ? ld_plain(reinterpret_cast<const uint4*>(xrow[j] + k0)) : load_halves8_anywhere(xrow[j], k0, p.k);
   };
 #pragma unroll
   for (int a = 0; a < kAhead; ++a) fetch(first + a, w[a], xc[a]);
@@ -182,7 +195,7 @@ __global__ void __launch_bounds__(256, 2) k_f16_few(const FewParams16 p) {
 #pragma unroll
     for (int i = 0; i < 2 * RB; ++i) we[i] = load_halves8(wrow[i], k0, p.k);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) xe[j] = load_halves8(xrow[j], k0, p.k);
+    for (int j = 0; j < NT; ++j) xe[j] = XVEC ? load_halves8(xrow[j], k0, p.k) : load_halves8_anywhere(xrow[j], k0, p.k);
     multiply(we, xe);
   }
 #pragma unroll
@@ -210,15 +223,19 @@ __global__ void __launch_bounds__(256, 2) k_f16_few(const FewParams16 p) {
   }
 }
 
-template <bool BF16, int NT>
+template <bool BF16, int NT, bool XVEC>
 cudaError_t launch_few16(const FewParams16& p, cudaStream_t st) {
   // 16 rows a CTA while one round of CTAs (three an SM) takes them all, else 32 (1 x 2048 -> 8192: 8.1 and 7.2 us; -> 2048: 4.4 and 4.9)
   if ((p.o.n + 15) / 16 > 3 * (uint32_t)sm_count())
-    launch_pdl(k_f16_few<BF16, NT, 2>, dim3((p.o.n + 31) / 32), dim3(256), st, p);
+    launch_pdl(k_f16_few<BF16, NT, 2, XVEC>, dim3((p.o.n + 31) / 32), dim3(256), st, p);
   else
-    launch_pdl(k_f16_few<BF16, NT, 1>, dim3((p.o.n + 15) / 16), dim3(256), st, p);
+    launch_pdl(k_f16_few<BF16, NT, 1, XVEC>, dim3((p.o.n + 15) / 16), dim3(256), st, p);
   count_launches(1);
   return cudaGetLastError();
+}
+template <bool BF16, int NT>
+cudaError_t launch_few16(const FewParams16& p, cudaStream_t st) {
+  return rows_on_boundary(p.x, p.ldx, p.o.m, 2) ? launch_few16<BF16, NT, true>(p, st) : launch_few16<BF16, NT, false>(p, st);
 }
 
 // ---- the gradient through the activation ----------------------------------------------------------------
@@ -331,13 +348,17 @@ struct Shape16 {
   bool copy_a, copy_b;
   uint64_t bytes_a, bytes_b;
 };
+// Few tokens are multiplied by k_f16_few.
+bool few_tokens(const ds_f16_product* p) {
+  return p->layout == DS_F16_FORWARD && (p->m <= kFewGroup || (p->m <= kFewMost && p->n * p->k <= kFewEntries));
+}
 Shape16 shape_of(const ds_f16_product* p) {
   Shape16 s;
   const bool a_across = p->layout == DS_F16_WEIGHTS, b_across = p->layout != DS_F16_FORWARD;
   s.rows_a = a_across ? p->k : p->m, s.cols_a = a_across ? p->m : p->k;
   s.rows_b = b_across ? p->k : p->n, s.cols_b = b_across ? p->n : p->k;
   // a single row has no pitch
-  s.copy_a = !aligned(p->a, 16) || (s.rows_a > 1 && p->lda % 8);
+  s.copy_a = !few_tokens(p) && (!aligned(p->a, 16) || (s.rows_a > 1 && p->lda % 8));
   s.copy_b = !aligned(p->b, 16) || (s.rows_b > 1 && p->ldb % 8);
   s.bytes_a = s.copy_a ? round_up(s.rows_a * round_up(s.cols_a, kLine) * 2, 256) : 0;
   s.bytes_b = s.copy_b ? round_up(s.rows_b * round_up(s.cols_b, kLine) * 2, 256) : 0;
@@ -355,7 +376,7 @@ constexpr uint32_t kTurnedMost = 64;
 
 cudaError_t multiply(const ds_f16_product* p, const Out16& o, Operand16 a, Operand16 b, cudaStream_t st) {
   const uint32_t m = o.m, n = o.n, k = (uint32_t)p->k;
-  if (!a.across && !b.across && (m <= kFewGroup || (m <= kFewMost && (uint64_t)n * k <= kFewEntries))) {
+  if (few_tokens(p)) {
     const FewParams16 f{static_cast<const uint16_t*>(a.p), static_cast<const uint16_t*>(b.p), a.ld, b.ld, k, o};
     if (o.bf16) return m <= kFewGroup ? launch_few16<true, 1>(f, st) : launch_few16<true, 2>(f, st);
     return m <= kFewGroup ? launch_few16<false, 1>(f, st) : launch_few16<false, 2>(f, st);

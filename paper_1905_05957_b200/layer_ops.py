@@ -7,26 +7,27 @@ kept by reference: the inputs of a training forward may not be changed before it
 """
 from __future__ import annotations
 
-import ctypes as C
 import math
 
 import torch
 
 from . import matrix_ops as _m
 from .binding import (ACTIVATIONS, DS_F16_FORWARD, DS_F16_INPUTS, DS_F16_WEIGHTS, DS_F32, DS_NORM_LAYER, DS_NORM_MAX_COLS, DS_NORM_RMS,
-                      ds_f16_product, ds_norm_args, fast_call, fast_struct_call, load_library)
+                      fast_call, fast_struct_call, load_library)
 from .matrix_ops import _DTYPES, _check, _current, _dev_status, _raw_stream, _status
 
 _HALVES = {torch.bfloat16: _DTYPES[torch.bfloat16], torch.float16: _DTYPES[torch.float16]}
 _NORMS = {"rms": DS_NORM_RMS, "layer": DS_NORM_LAYER}
-_call = _struct = _matmul_at = _slope_at = _pack_at = _norm_at = _norm_back_at = _dropout_at = None
+_like_of = torch.empty_like
+_call = _struct = _size = _matmul_at = _matmul_ws = _slope_at = _slope_ws = _pack_at = _norm_at = _norm_back_at = _norm_back_ws = _dropout_at = None
 
 
 def _load():
     """Looks the library's functions up once."""
-    global _call, _struct, _matmul_at, _slope_at, _pack_at, _norm_at, _norm_back_at, _dropout_at
-    _struct, at = fast_struct_call()
+    global _call, _struct, _size, _matmul_at, _matmul_ws, _slope_at, _slope_ws, _pack_at, _norm_at, _norm_back_at, _norm_back_ws, _dropout_at
+    _struct, _size, at = fast_struct_call()
     _matmul_at, _slope_at, _norm_at, _norm_back_at = (at[n] for n in ("ds_f16_matmul", "ds_f16_slope", "ds_norm_forward", "ds_norm_backward"))
+    _matmul_ws, _norm_back_ws, _slope_ws = at["ds_f16_matmul_workspace"], at["ds_norm_backward_workspace"], load_library().ds_f16_slope_workspace
     _call, at = fast_call()
     _pack_at, _dropout_at = at["ds_f16_pack"], at["ds_dropout"]
 
@@ -116,8 +117,7 @@ def _product(layout: int, dt: int, m: int, n: int, k: int, a: int, lda: int, b: 
     ws = address = None
     size = 0
     if (a | b) & 15 or (lda | ldb) & 7:      # perhaps an operand has to be copied
-        args = ds_f16_product(dt, layout, m, n, k, a, lda, b, ldb, 0, 0, 0, 0, 0, 0, out, odt, ldo, 0, 0, 0)
-        size = load_library().ds_f16_matmul_workspace(C.byref(args))
+        size = _size(_matmul_ws, dt, layout, m, n, k, a, lda, b, ldb, bias, act, res, ldr, z, ldz, out, odt, ldo)
         if size:
             ws = like.new_empty(size // 2)
             address = ws.data_ptr()
@@ -161,7 +161,7 @@ def _forward(x, w, bias, act, residual, out_dtype, out, keep_z):
     if out is not None:
         ldo, odt = _given(out, m, n, index, "out"), _DTYPES.get(out.dtype)
     elif out_dtype is None:
-        out, ldo, odt = x.new_empty((m, n)), n, dt
+        out, ldo, odt = (x.new_empty((m, n)) if residual is None else _like_of(residual)), n, dt
     else:
         out, ldo, odt = x.new_empty((m, n), dtype=out_dtype), n, _DTYPES.get(out_dtype)
     if odt != dt and odt != DS_F32:
@@ -284,7 +284,7 @@ class Linear16:
             # dz, and behind it what the sums need
             ldn = _pitch(n)
             at = 2 * m * ldn if act else 0
-            size = load_library().ds_f16_slope_workspace(m, n) if db is not None else 0
+            size = _slope_ws(m, n) if db is not None else 0
             buf = x.new_empty((at + size + 1) // 2 + 8)
             base = buf.data_ptr()
             rc = _struct(_slope_at, raw, dt, m, n, dz, lddy, None if z is None else z.data_ptr(), ldn, act, base if act else None, ldn,
@@ -298,7 +298,7 @@ class Linear16:
             dz = buf.data_ptr()
         dx = None
         if need_dx:
-            dx = x.new_empty((m, k))
+            dx = _like_of(x)
             if m and k:
                 _product(DS_F16_INPUTS, dt, m, k, n, dz, lddz, self.weight.data_ptr(), self.weight.stride(0), None, 0, None, 0, None, 0, dx.data_ptr(), dt, k, index, raw, x)
         if n and k:
@@ -336,7 +336,7 @@ def dropout(x: torch.Tensor, p: float, seed: int, step: int = 0, layer: int = 0,
         with torch.cuda.device(index):
             return dropout(x, p, seed, step, layer, out)
     if out is None:
-        out, ldo = x.new_empty((r, c)), c
+        out, ldo = _like_of(x), c
     elif out.dtype is not x.dtype:
         raise TypeError(f"out: {x.dtype} expected, got {out.dtype}")
     else:
@@ -389,7 +389,7 @@ class ResidualNorm:
                 at.append(_floats(t, self.cols, self._index, name))
         self._params = (at[0], at[1], at[2], self._groups, at[3], at[4], self._scale, self._eps, *self._drop)
         self._stream = None if self._index is None else _raw_stream(self._index)
-        self._saved, self._workspaces = None, {}
+        self._saved = None
 
     def _used(self, raw: int, index: int, saved=()):
         """Tells the allocator of the current stream, on which parameters and what is kept are about to be used."""
@@ -440,7 +440,7 @@ class ResidualNorm:
             ldh = _given(h, rows, cols, index, "h")
             hp = h.data_ptr()
         elif need_h:
-            h, ldh = (y if x is None else x).new_empty((rows, cols)), cols
+            h, ldh = _like_of(y if x is None else x), cols
             hp = h.data_ptr()
         elif not pre:
             raise ValueError("nothing to compute")
@@ -450,7 +450,7 @@ class ResidualNorm:
                 raise ValueError("n: there is no pre norm")
         else:
             if n is None:
-                n, ldn = y.new_empty((rows, cols)), cols
+                n, ldn = _like_of(y), cols
             elif n.dtype is not dtype:
                 raise TypeError(f"n: {dtype} expected, got {n.dtype}")
             else:
@@ -507,7 +507,7 @@ class ResidualNorm:
                 continue
             g = out.get(name) if out else None
             if g is None:
-                g = stats.new_empty(t.shape)
+                g = _like_of(t)
             elif g.dtype is not torch.float32 or g.shape != t.shape or g.get_device() != index or not g.is_contiguous():
                 raise ValueError(f"out[{name!r}]: contiguous float32 values {tuple(t.shape)} on cuda:{index} expected")
             grads[name] = g
@@ -517,19 +517,14 @@ class ResidualNorm:
         raw = _raw_stream(index)
         if raw != self._stream:
             self._used(raw, index, (y, x, stats))
-        dy, dx = y.new_empty((rows, cols)), None
+        dy, dx = _like_of(y), None
         if x is not None and need_dx:
-            dx = x.new_empty((rows, cols))
+            dx = _like_of(x)
         members = [_DTYPES[dtype], _DTYPES[stype], rows, cols, self._norm, y.data_ptr(), ldy, None if x is None else x.data_ptr(), ldx, *self._params, step, stats.data_ptr(),
                    None, 0, None, 0, dhp, lddh, dnp, lddn, None if dx is None else dx.data_ptr(), cols, dy.data_ptr(), cols, *at]
-        size = self._workspaces.get((rows, cols))
-        if size is None:
-            size = load_library().ds_norm_backward_workspace(C.byref(ds_norm_args(*(0 if v is None else v for v in members))))
+        size = _size(_norm_back_ws, *members)
         ws = stats.new_empty((size + 3) // 4) if size else None
         rc = _struct(_norm_back_at, raw, *members, ws.data_ptr() if size else None, size)
         if rc:
             _check(rc, "ds_norm_backward")
-        if len(self._workspaces) > 64:
-            self._workspaces.clear()
-        self._workspaces[rows, cols] = size      # of the parameters' gradients; the others need none
         return dy, dx, grads

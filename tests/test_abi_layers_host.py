@@ -28,7 +28,7 @@ def test_structures_agree_with_the_header(name, kind):
 
 
 def test_struct_calls(lib):
-    call, at = b.fast_struct_call()
+    call, size, at = b.fast_struct_call()
     zero = [0] * len(b.ds_norm_args._fields_)
     assert call(at["ds_norm_forward"], None, *zero) == INVALID                          # no columns
     zero[3] = 8
@@ -36,7 +36,14 @@ def test_struct_calls(lib):
     assert call(at["ds_norm_forward"], None, *zero) == b.DS_OK                          # no rows
     zero[16] = -1.0
     assert call(at["ds_norm_forward"], None, *zero) == INVALID                          # floats arrive as doubles
+    product = list(PRODUCT.values())
+    product[6] = 65
+    assert size(at["ds_f16_matmul_workspace"], *product) == 40 * 64 * 2 and size(at["ds_f16_matmul_workspace"], 1) == 0
+    assert size(at["ds_norm_backward_workspace"], *zero) == 0
     if getattr(call, "__name__", "") == "call_struct":
+        for bad in ((), (1,), (at["ds_f16_matmul_workspace"], "x")):
+            with pytest.raises(TypeError):
+                size(*bad)
         for bad in ((), (1, 2), (1, 2, *range(65)), (at["ds_norm_forward"], None, "x")):
             with pytest.raises(TypeError):
                 call(*bad)
@@ -72,6 +79,8 @@ def test_product_workspace(lib):
     assert size(lda=65) == 40 * 64 * 2 and size(b=P + 2) == 24 * 64 * 2 and size(a=P + 2, ldb=65) == 64 * 64 * 2
     assert size(layout=2, lda=41) == 64 * 64 * 2 and size(layout=1, ldb=25) == 64 * 64 * 2      # rows of whole lines
     assert size(m=1, lda=7) == 0                                                      # a single row has no pitch
+    assert size(m=9, lda=65) == size(m=16, a=P + 2) == 0 and size(m=18, lda=65) == 18 * 64 * 2      # few tokens are read where they lie
+    assert size(m=9, ldb=65) == 24 * 64 * 2
     assert lib.ds_f16_matmul(None, None) == INVALID and lib.ds_f16_matmul_workspace(None) == 0
 
 
