@@ -462,7 +462,7 @@ int ds_orth_destroy(ds_orth_handle h);
  *   workspace (ds_f16_matmul_workspace bytes, 16-byte aligned; 0 where none are) by a launch of their own; a few tokens are read where they lie.  k = 0 gives act(bias) + residual.
  *   The order of a sum depends on the sizes and the device, not on timing.
  * ds_f16_slope: dz = dy act'(z) (in 16 bits) and / or sum_n = the column sums of dy act'(z) before it is rounded, in a fixed order.  z as the forward
- *   product left it (NULL for DS_ACT_NONE).  dz may be dy or z itself.  workspace: ds_f16_slope_workspace bytes where sums are asked for.  At most 4194240 rows.
+ *   product left it (NULL for DS_ACT_NONE).  dz may be dy or z itself.  workspace: ds_f16_slope_workspace bytes where sums are asked for.  At most 2097120 rows.
  * ds_f16_pack: a copy of x as 16-bit floats on 16-byte rows (ldo a multiple of 8; entries from cols up to ldo become 0).
  */
 typedef enum { DS_ACT_NONE = 0, DS_ACT_RELU = 1, DS_ACT_GELU = 2, DS_ACT_GELU_TANH = 3, DS_ACT_SILU = 4 } ds_activation;

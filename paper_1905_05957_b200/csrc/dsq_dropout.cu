@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(kThreads) k_dropout(const T* x, uint64_t ldx, 
       const uint32_t row = first + b * step;
       if (row >= rows) break;
       float v[8];
-      entries8<VEC, T>(w[b], c, cols, v);
+      entries8<VEC>(x + row * ldx, w[b], c, cols, lane, v);
       if (drop.threshold) drop8(drop, draw8(drop, row, c), v);
       store_row8<VEC>(out + row * ldo, c, cols, lane, v);
     }

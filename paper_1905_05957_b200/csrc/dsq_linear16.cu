@@ -241,10 +241,11 @@ cudaError_t launch_few16(const FewParams16& p, cudaStream_t st) {
 // ---- the gradient through the activation ----------------------------------------------------------------
 // dz = dy act'(z) in 16 bits and, from what is not yet rounded, the column sums of each block of kSumRows rows; a second kernel adds
 // the blocks in their order.  Bound by memory.  A lane has eight columns; a CTA's eight warps take every eighth row, four at a time.
-constexpr uint32_t kSumRows = 64;
+constexpr uint32_t kSumRows = 32;
 
-template <class T, int ACT, bool VEC>
-__global__ void __launch_bounds__(256, VEC ? 4 : 2) k_f16_slope(const T* dy, uint64_t lddy, const T* z, uint64_t ldz, T* dz, uint64_t lddz, uint32_t rows, uint32_t cols, float* sums) {
+// DY, Z: how the rows of dy, and of z and dz lie (what this package's layers keep starts on boundaries, a gradient may not).
+template <class T, int ACT, int DY, int Z>
+__global__ void __launch_bounds__(256, DY ? 4 : 3) k_f16_slope(const T* dy, uint64_t lddy, const T* z, uint64_t ldz, T* dz, uint64_t lddz, uint32_t rows, uint32_t cols, float* sums) {
   __shared__ float part[8][256];
   pdl_prologue();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -260,8 +261,8 @@ __global__ void __launch_bounds__(256, VEC ? 4 : 2) k_f16_slope(const T* dy, uin
     for (uint32_t b = 0; b < kBatch; ++b) {
       const uint64_t r = r0 + i + 8 * b;
       if (r < rows) {
-        load_words8<VEC>(dy + r * lddy, c, cols, lane, g[b]);
-        if constexpr (ACT != DS_ACT_NONE) load_words8<VEC>(z + r * ldz, c, cols, lane, q[b]);
+        load_words8<DY>(dy + r * lddy, c, cols, lane, g[b]);
+        if constexpr (ACT != DS_ACT_NONE) load_words8<Z>(z + r * ldz, c, cols, lane, q[b]);
       }
     }
 #pragma unroll
@@ -269,14 +270,14 @@ __global__ void __launch_bounds__(256, VEC ? 4 : 2) k_f16_slope(const T* dy, uin
       const uint64_t r = r0 + i + 8 * b;
       if (r >= rows) break;
       float v[8], t[8];
-      entries8<VEC, T>(g[b], c, cols, v);
-      if constexpr (ACT != DS_ACT_NONE) entries8<VEC, T>(q[b], c, cols, t);
+      entries8<DY>(dy + r * lddy, g[b], c, cols, lane, v);
+      if constexpr (ACT != DS_ACT_NONE) entries8<Z>(z + r * ldz, q[b], c, cols, lane, t);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if constexpr (ACT != DS_ACT_NONE) v[j] *= slope_of<ACT>(t[j]);
         s[j] += v[j];
       }
-      if (dz) store_row8<VEC>(dz + r * lddz, c, cols, lane, v);
+      if (dz) store_row8<Z>(dz + r * lddz, c, cols, lane, v);
     }
   }
   if (!sums) return;
@@ -292,14 +293,16 @@ __global__ void __launch_bounds__(256, VEC ? 4 : 2) k_f16_slope(const T* dy, uin
 }
 
 template <class T>
-void launch_slope(const ds_f16_slope_args* p, float* sums, bool vec, dim3 grid, cudaStream_t st) {
+void launch_slope(const ds_f16_slope_args* p, float* sums, dim3 grid, cudaStream_t st) {
+  auto on = [&](const void* q, uint64_t ld) { return rows_on_boundary(q, ld, p->rows, 2); };
+  const bool z = on(p->z, p->ldz) && on(p->dz, p->lddz), all = z && p->cols % 8 == 0 && on(p->dy, p->lddy);
   auto go = [&](auto kernel) {
     launch_pdl(kernel, grid, dim3(256), st, static_cast<const T*>(p->dy), p->lddy, static_cast<const T*>(p->z), p->ldz, static_cast<T*>(p->dz), p->lddz, (uint32_t)p->rows,
                (uint32_t)p->cols, sums);
   };
   auto by = [&](auto act) {
     constexpr int ACT = decltype(act)::value;
-    vec ? go(k_f16_slope<T, ACT, true>) : go(k_f16_slope<T, ACT, false>);
+    all ? go(k_f16_slope<T, ACT, kWhole, kWhole>) : z ? go(k_f16_slope<T, ACT, kAnywhere, kAligned>) : go(k_f16_slope<T, ACT, kAnywhere, kAnywhere>);
   };
   switch (p->activation) {
     case DS_ACT_NONE: return by(std::integral_constant<int, DS_ACT_NONE>());
@@ -310,18 +313,19 @@ void launch_slope(const ds_f16_slope_args* p, float* sums, bool vec, dim3 grid, 
   }
 }
 
-__global__ void __launch_bounds__(256) k_f16_sums(const float* sums, uint32_t blocks, uint32_t cols, void* out, int f32, int bf16) {
-  __shared__ float part[8][32];
+constexpr int kSumThreads = 512;
+__global__ void __launch_bounds__(kSumThreads) k_f16_sums(const float* sums, uint32_t blocks, uint32_t cols, void* out, int f32, int bf16) {
+  constexpr int kWarps = kSumThreads / 32, kBatch = 8;      // loads in flight
+  __shared__ float part[kWarps][32];
   pdl_prologue();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t col = blockIdx.x * 32 + lane;
   float v = 0.f;
-  constexpr int kBatch = 8;      // loads in flight
   if (col < cols)
-    for (uint32_t i = warp; i < blocks; i += 8 * kBatch) {
+    for (uint32_t i = warp; i < blocks; i += kWarps * kBatch) {
       float t[kBatch];
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) t[b] = i + 8 * b < blocks ? ld_plain(sums + (uint64_t)(i + 8 * b) * cols + col) : 0.f;
+      for (int b = 0; b < kBatch; ++b) t[b] = i + kWarps * b < blocks ? ld_plain(sums + (uint64_t)(i + kWarps * b) * cols + col) : 0.f;
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) v += t[b];
     }
@@ -330,7 +334,7 @@ __global__ void __launch_bounds__(256) k_f16_sums(const float* sums, uint32_t bl
   if (warp || col >= cols) return;
   v = 0.f;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) v += part[w][lane];
+  for (int w = 0; w < kWarps; ++w) v += part[w][lane];
   if (f32)
     static_cast<float*>(out)[col] = v;
   else
@@ -529,16 +533,14 @@ int ds_f16_slope(const ds_f16_slope_args* p, void* cuda_stream) {
     if (overlap(ws, dy) || overlap(ws, z) || overlap(ws, dz) || overlap(ws, sum)) return DS_ERR_INVALID_ARG;
     sums = static_cast<float*>(p->workspace);
   }
-  auto on = [&](const void* q, uint64_t ld) { return rows_on_boundary(q, ld, p->rows, 2); };
-  const bool vec = p->cols % 8 == 0 && on(p->dy, p->lddy) && on(p->z, p->ldz) && on(p->dz, p->lddz);
   const dim3 grid((uint32_t)((p->cols + 255) / 256), (uint32_t)blocks);
   if (p->dtype == DS_BF16)
-    launch_slope<__nv_bfloat16>(p, sums, vec, grid, st);
+    launch_slope<__nv_bfloat16>(p, sums, grid, st);
   else
-    launch_slope<__half>(p, sums, vec, grid, st);
+    launch_slope<__half>(p, sums, grid, st);
   count_launches(1);
   if (p->sum) {
-    launch_pdl(k_f16_sums, dim3((uint32_t)((p->cols + 31) / 32)), dim3(256), st, (const float*)sums, (uint32_t)blocks, (uint32_t)p->cols, p->sum,
+    launch_pdl(k_f16_sums, dim3((uint32_t)((p->cols + 31) / 32)), dim3(kSumThreads), st, (const float*)sums, (uint32_t)blocks, (uint32_t)p->cols, p->sum,
                (int)(p->sum_dtype == DS_F32), (int)(p->dtype == DS_BF16));
     count_launches(1);
   }

@@ -88,8 +88,10 @@ __device__ __forceinline__ int entries_left(uint32_t c, uint32_t cols) {
 }
 
 // Entries c .. c + 7 of a row of `cols`, lane l of a whole warp those 8 l behind lane 0's.  Entries behind the row's end are 0.
-// VEC: every row starts on a 16-byte boundary and cols is a multiple of 8.  First as words, for loads that run ahead of their use.
-template <bool VEC, class T>
+// VEC: kWhole (true): every row starts on a 16-byte boundary and cols is a multiple of 8; kAligned: rows start so; else anywhere.  First as words, for loads that run ahead of
+// their use: nothing in them waits (a lane's exchange with the next one does).
+constexpr int kAnywhere = 0, kWhole = 1, kAligned = 2;
+template <int VEC, class T>
 __device__ __forceinline__ void load_words8(const T* row, uint32_t c, uint32_t cols, int lane, uint32_t (&w)[kWords<T> + 4]) {
   constexpr int N = kWords<T>;
 #pragma unroll
@@ -97,36 +99,44 @@ __device__ __forceinline__ void load_words8(const T* row, uint32_t c, uint32_t c
   const uint32_t shift = VEC ? 0 : shift_of(row);
   const uint8_t* at = reinterpret_cast<const uint8_t*>(row + c) - shift;
   // the granules that hold something of this row
-  const int bytes = VEC ? (c < cols ? 4 * N : 0) : entries_left(c, cols) * (int)sizeof(T) + (int)shift;
+  const int bytes = VEC == kWhole ? (c < cols ? 4 * N : 0) : entries_left(c, cols) * (int)sizeof(T) + (int)shift;
 #pragma unroll
   for (int g = 0; g < N / 4; ++g)
     if (16 * g < bytes) {
       const uint4 q = ld_plain(reinterpret_cast<const uint4*>(at) + g);
       w[4 * g] = q.x, w[4 * g + 1] = q.y, w[4 * g + 2] = q.z, w[4 * g + 3] = q.w;
     }
-  if (!VEC && shift) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[N + i] = __shfl_down_sync(0xFFFFFFFFu, w[i], 1);
-    if (lane == 31 && 4 * N < bytes) {
-      const uint4 q = ld_plain(reinterpret_cast<const uint4*>(at) + N / 4);
-      w[N] = q.x, w[N + 1] = q.y, w[N + 2] = q.z, w[N + 3] = q.w;
-    }
-    take_from<N>(w, shift);
+  if (!VEC && lane == 31 && shift && 4 * N < bytes) {
+    const uint4 q = ld_plain(reinterpret_cast<const uint4*>(at) + N / 4);
+    w[N] = q.x, w[N + 1] = q.y, w[N + 2] = q.z, w[N + 3] = q.w;
   }
 }
-template <bool VEC, class T>
-__device__ __forceinline__ void entries8(const uint32_t* w, uint32_t c, uint32_t cols, float (&v)[8]) {
+// Then as floats: the whole warp together.
+template <int VEC, class T>
+__device__ __forceinline__ void entries8(const T* row, uint32_t (&w)[kWords<T> + 4], uint32_t c, uint32_t cols, int lane, float (&v)[8]) {
+  constexpr int N = kWords<T>;
+  if constexpr (VEC == kAnywhere) {
+    const uint32_t shift = shift_of(row);
+    if (shift) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t next = __shfl_down_sync(0xFFFFFFFFu, w[i], 1);
+        if (lane != 31) w[N + i] = next;
+      }
+      take_from<N>(w, shift);
+    }
+  }
   unpack8<T>(w, v);
-  if (!VEC && c + 8 > cols)
+  if (VEC != kWhole && c + 8 > cols)
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (c + j >= cols) v[j] = 0.f;
 }
-template <bool VEC, class T>
+template <int VEC, class T>
 __device__ __forceinline__ void load_row8(const T* row, uint32_t c, uint32_t cols, int lane, float (&v)[8]) {
   uint32_t w[kWords<T> + 4];
   load_words8<VEC>(row, c, cols, lane, w);
-  entries8<VEC, T>(w, c, cols, v);
+  entries8<VEC>(row, w, c, cols, lane, v);
 }
 
 // Eight entries to where they fit whole: a boundary of 16 bytes, for floats of 32 if `at` is on one.
@@ -146,17 +156,17 @@ __device__ __forceinline__ void store_piece8(T* at, const float (&v)[8]) {
 }
 
 // The other way round.  The whole warp calls it, lanes behind the row's end, too.
-template <bool VEC, class T>
+template <int VEC, class T>
 __device__ __forceinline__ void store_row8(T* row, uint32_t c, uint32_t cols, int lane, const float (&v)[8]) {
   constexpr int N = kWords<T>, kEach = 16 / sizeof(T);
   uint32_t w[N + 4];
-  if constexpr (VEC) {
+  if constexpr (VEC == kWhole) {
     if (c < cols) store_piece8(row + c, v);
     return;
   }
-  const uint32_t shift = shift_of(row);
+  const uint32_t shift = VEC ? 0 : shift_of(row);
   const int left = entries_left(c, cols) * (int)sizeof(T);      // bytes of the row from entry c on
-  if (!shift) {
+  if (VEC || !shift) {
     pack8<T>(v, w);
     uint4* to = reinterpret_cast<uint4*>(row + c);
 #pragma unroll
