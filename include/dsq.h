@@ -58,6 +58,7 @@ typedef enum {
  * full histogram after a missing or wrong prediction ("full": v is read three times).  Both routes
  * give the same result; the counters are for tests and tuning.  Word 3 is reserved. */
 #define DS_DEV_MMA_TIMEOUT 0x2u       /* a tensor-core product gave up waiting (about a second): its outputs are not valid */
+#define DS_DEV_NORM_TIMEOUT 0x4u      /* a norm of more than 4096 columns gave up waiting for its row's other parts: its outputs are not valid */
 #define DS_DEV_WORD_FLAGS 0
 #define DS_DEV_WORD_TOPK_PREDICTED 1
 #define DS_DEV_WORD_TOPK_FULL 2
@@ -518,7 +519,7 @@ int ds_f16_pack(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t
  *   ds_norm_backward: from dh and / or dn (the gradients of h and n) those of x, y and the parameters; each is wanted where its pointer is not NULL.  y, x and the
  *   parameters as the forward pass had them, stats as it left them.  dx and dy may be one of the inputs of their type and pitch.  workspace: ds_norm_backward_workspace bytes, 16-byte aligned.
  *   Rows that hold an inf or a NaN are NaN and their parameters' gradients with them; other rows are not touched by them.
- *   cols <= DS_NORM_MAX_COLS, else DS_ERR_UNSUPPORTED.
+ *   cols <= DS_NORM_MAX_COLS, rows less than 2^30 entries apart, else DS_ERR_UNSUPPORTED.  dev_status may be NULL (DS_DEV_NORM_TIMEOUT).
  */
 #define DS_NORM_MAX_COLS 32768u
 #define DS_NORM_RMS 0u
@@ -548,6 +549,7 @@ typedef struct {
   void* dy;
   uint64_t lddy;
   float *d_post_w, *d_post_b, *d_gate, *d_pre_w, *d_pre_b;
+  uint32_t* dev_status;
   void* workspace;
   uint64_t workspace_bytes;
 } ds_norm_args;

@@ -35,6 +35,7 @@ EXPORTS = ("ds_get_layout", "ds_create", "ds_worker_compress", "ds_server_aggreg
            "ds_f16_matmul_workspace", "ds_f16_matmul", "ds_f16_slope_workspace", "ds_f16_slope", "ds_f16_pack",
            "ds_norm_forward", "ds_norm_backward_workspace", "ds_norm_backward", "ds_dropout")
 DS_DEV_MMA_TIMEOUT = 2
+DS_DEV_NORM_TIMEOUT = 4
 DS_F32, DS_BF16, DS_F16 = 0, 1, 2
 DS_I8_MAX_K = 131072
 DS_ORTH_NESTEROV = 1
@@ -92,7 +93,7 @@ class ds_norm_args(C.Structure):
     _fields_ = (_words("dtype", "stream_dtype", "rows", "cols", "norm", "y", "ldy", "x", "ldx", "post_w", "post_b", "gate", "groups", "pre_w", "pre_b")
                 + [("residual_scale", C.c_double), ("eps", C.c_double)]
                 + _words("threshold", "seed", "layer", "step", "stats", "h", "ldh", "n", "ldn", "dh", "lddh", "dn", "lddn", "dx", "lddx", "dy", "lddy",
-                         "d_post_w", "d_post_b", "d_gate", "d_pre_w", "d_pre_b", "workspace", "workspace_bytes"))
+                         "d_post_w", "d_post_b", "d_gate", "d_pre_w", "d_pre_b", "dev_status", "workspace", "workspace_bytes"))
 
 
 class DsqError(RuntimeError):

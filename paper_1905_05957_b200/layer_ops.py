@@ -19,6 +19,8 @@ from .matrix_ops import _DTYPES, _check, _current, _dev_status, _raw_stream, _st
 _HALVES = {torch.bfloat16: _DTYPES[torch.bfloat16], torch.float16: _DTYPES[torch.float16]}
 _NORMS = {"rms": DS_NORM_RMS, "layer": DS_NORM_LAYER}
 _like_of = torch.empty_like
+_WIDE = 4096                 # columns above which a row's parts wait for one another
+_NOTHING = (None,) * 13      # the members of ds_norm_args that the forward pass does not read
 _call = _struct = _size = _matmul_at = _matmul_ws = _slope_at = _slope_ws = _pack_at = _norm_at = _norm_back_at = _norm_back_ws = _dropout_at = None
 
 
@@ -389,16 +391,15 @@ class ResidualNorm:
                 at.append(_floats(t, self.cols, self._index, name))
         self._params = (at[0], at[1], at[2], self._groups, at[3], at[4], self._scale, self._eps, *self._drop)
         self._stream = None if self._index is None else _raw_stream(self._index)
-        self._saved = None
+        self._saved = self._saved_on = None
 
-    def _used(self, raw: int, index: int, saved=()):
-        """Tells the allocator of the current stream, on which parameters and what is kept are about to be used."""
-        if raw != self._stream:
-            if self._stream is not None:
-                for t in (*self._tensors.values(), *saved):
-                    if t is not None:
-                        t.record_stream(torch.cuda.current_stream(index))
-            self._stream = raw
+    def _used(self, raw: int, index: int):
+        """Tells the allocator of the current stream, on which the parameters are about to be used."""
+        if self._stream is not None:
+            for t in self._tensors.values():
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream(index))
+        self._stream = raw
 
     def forward(self, y: torch.Tensor, x: torch.Tensor | None = None, step: int = 0, training: bool = False, need_h: bool = True, h: torch.Tensor | None = None,
                 n: torch.Tensor | None = None, stream=None):
@@ -460,17 +461,18 @@ class ResidualNorm:
         if raw != self._stream:
             self._used(raw, index)
         stats = sp = None
-        yp = y.data_ptr()
+        yp, status = y.data_ptr(), _status.get(index)
         if training:
             stats = y.new_empty((rows, 4), dtype=torch.float32)
             sp = stats.data_ptr()
             if rows and (hp in (xp, yp) and hp or np_ in (xp, yp) and np_):
                 raise ValueError("a training forward may not write over its inputs")
-        rc = _struct(_norm_at, raw, dt, sdt, rows, cols, self._norm, yp, ldy, xp, ldx, *self._params, _word(step, "step"), sp, hp, ldh, np_, ldn)
+        rc = _struct(_norm_at, raw, dt, sdt, rows, cols, self._norm, yp, ldy, xp, ldx, *self._params, _word(step, "step"), sp, hp, ldh, np_, ldn,
+                     *_NOTHING, (status[1] if status else _dev_status(index)) if cols > _WIDE else None)
         if rc:
             _check(rc, "ds_norm_forward")
         if training:
-            self._saved = (y, ldy, x, ldx, stats, step, stype)
+            self._saved, self._saved_on = (y, ldy, x, ldx, stats, step, stype), raw
         return h, n
 
     def backward(self, dh: torch.Tensor | None = None, dn: torch.Tensor | None = None, need_dx: bool = True, out: dict | None = None, stream=None):
@@ -516,12 +518,18 @@ class ResidualNorm:
             raise ValueError(f"out: parameters are {', '.join(self._tensors)}")
         raw = _raw_stream(index)
         if raw != self._stream:
-            self._used(raw, index, (y, x, stats))
+            self._used(raw, index)
+        if raw != self._saved_on:             # what was kept is dropped at the earliest when this stream is done with it
+            for t in (y, x, stats):
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream(index))
+            self._saved_on = raw
         dy, dx = _like_of(y), None
         if x is not None and need_dx:
             dx = _like_of(x)
         members = [_DTYPES[dtype], _DTYPES[stype], rows, cols, self._norm, y.data_ptr(), ldy, None if x is None else x.data_ptr(), ldx, *self._params, step, stats.data_ptr(),
-                   None, 0, None, 0, dhp, lddh, dnp, lddn, None if dx is None else dx.data_ptr(), cols, dy.data_ptr(), cols, *at]
+                   None, 0, None, 0, dhp, lddh, dnp, lddn, None if dx is None else dx.data_ptr(), cols, dy.data_ptr(), cols, *at,
+                   _dev_status(index) if cols > _WIDE else None]
         size = _size(_norm_back_ws, *members)
         ws = stats.new_empty((size + 3) // 4) if size else None
         rc = _struct(_norm_back_at, raw, *members, ws.data_ptr() if size else None, size)

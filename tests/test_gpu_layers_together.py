@@ -187,6 +187,20 @@ def test_streams():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, ref))
         del junk
+    # kept here, used on the side stream for something else in between: what was kept is this stream's all the same
+    want = ref[2]
+    for _ in range(3):
+        _, joint = make()
+        side.wait_stream(torch.cuda.current_stream())
+        joint.forward(dy, stream=side)
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        got = joint.backward(dy, stream=side)[0]
+        del joint
+        junk = [torch.full((700, 512), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(20)]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        del junk
     for stream in (None, sides[1]):
         y = linear16(x, w.to(torch.bfloat16), stream=stream)
         z = dropout(x, 0.5, 1, stream=stream)
