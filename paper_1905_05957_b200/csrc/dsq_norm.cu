@@ -141,9 +141,9 @@ __device__ __forceinline__ void load_param8(const float* p, uint32_t c, uint32_t
 }
 
 // ---- sums over the threads of a row ---------------------------------------------------------------------
-struct SumSpace {
-  float warp[2][16][4];      // of each warp; the two halves take turns, so that one barrier is enough
-  float cta[2][8][4];        // of each CTA of a cluster, written by the CTAs themselves
+struct alignas(16) SumSpace {
+  float warp[2][8][8][16];      // of each slice's values by its warps (0 where there is no warp); the two halves take turns, so that one barrier is enough
+  float cta[2][8][8];           // of each CTA of a cluster, written by the CTAs themselves
   uint64_t arrived[2];       // their bytes
   int gave_up;
 };
@@ -153,37 +153,77 @@ struct RowSum {
   SumSpace* space;
   uint32_t sums = 0;      // so many before: which half is next, and its barrier's phase
   __device__ __forceinline__ void begin(uint32_t size) {
-    if (size == 1) return;
-    if (threadIdx.x == 0 && threadIdx.y == 0) {
+    float* zero = &space->warp[0][0][0][0];
+    for (uint32_t i = threadIdx.y * blockDim.x + threadIdx.x; i < sizeof(space->warp) / 4; i += blockDim.x * blockDim.y) zero[i] = 0.f;
+    if (size > 1 && threadIdx.x == 0 && threadIdx.y == 0) {
       mbar_init(smem_u32(&space->arrived[0]), 1);
       mbar_init(smem_u32(&space->arrived[1]), 1);
       space->gave_up = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    cluster_sync();      // the others are there, and their barriers, before anything is sent
+    if (size > 1) cluster_sync();      // the others are there, and their barriers, before anything is sent
   }
+  // K values at once.  One or two are added lane by lane.  Of more, lanes halve them between one another as they add (P / 2, P / 4, ... exchanges and then one each, where P
+  // sums one by one would be five each): lanes of a group of 32 / P end with one of the sums, join it across the warps and hand it round.  Fewer instructions, a
+  // longer way: four values 96 to 91 us (16384 x 4096 forward), two 160 to 174 (65536 x 768 backward, layer norms).
   template <int K>
   __device__ __forceinline__ void operator()(float (&v)[K], uint32_t size) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1)
-#pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
-    const int warps = blockDim.x >> 5;
-    if (warps == 1 && size == 1) return;
+    static_assert(K <= 8, "");
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const uint32_t turn = sums & 1;
-    const int first = threadIdx.y * warps;
-    if ((threadIdx.x & 31) == 0)
+    const bool joined = warps > 1 || size > 1;
+    auto& space_of = space->warp[turn][threadIdx.y];      // [value][warp]
+    auto wait = [] { asm volatile("bar.sync %0, %1;" ::"r"(1 + threadIdx.y), "r"(blockDim.x) : "memory"); };      // for this slice alone
+    if constexpr (K <= 2) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) space->warp[turn][first + (threadIdx.x >> 5)][k] = v[k];
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + threadIdx.y), "r"(blockDim.x) : "memory");      // this slice alone
-    const int l = threadIdx.x & 15;
+      for (int o = 16; o; o >>= 1)
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = l < warps ? space->warp[turn][first + l][k] : 0.f;
+        for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+      if (joined) {
+        if (lane == 0)
 #pragma unroll
-    for (int o = 8; o; o >>= 1)
+          for (int k = 0; k < K; ++k) space_of[k][threadIdx.x >> 5] = v[k];
+        wait();
 #pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+        for (int k = 0; k < K; ++k) v[k] = space_of[k][lane & 15];
+#pragma unroll
+        for (int o = 8; o; o >>= 1)
+#pragma unroll
+          for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+      }
+    } else {
+      constexpr int P = K <= 4 ? 4 : 8, G = 32 / P;
+      float w[P];
+#pragma unroll
+      for (int k = 0; k < P; ++k) w[k] = k < K ? v[k] : 0.f;
+#pragma unroll
+      for (int half = P / 2, off = 16; half; half /= 2, off /= 2)
+#pragma unroll
+        for (int i = 0; i < half; ++i) {
+          const bool up = lane & off;
+          const float mine = up ? w[i + half] : w[i], other = up ? w[i] : w[i + half];
+          w[i] = mine + __shfl_xor_sync(0xFFFFFFFFu, other, off);
+        }
+#pragma unroll
+      for (int off = G / 2; off; off /= 2) w[0] += __shfl_xor_sync(0xFFFFFFFFu, w[0], off);
+      if (joined) {
+        if ((lane & (G - 1)) == 0) space_of[lane / G][threadIdx.x >> 5] = w[0];
+        wait();
+        if constexpr (P == 8) {
+          const float4 q = *reinterpret_cast<const float4*>(&space_of[lane / G][4 * (lane & (G - 1))]);
+          w[0] = (q.x + q.y) + (q.z + q.w);
+        } else {
+          const float2 q = *reinterpret_cast<const float2*>(&space_of[lane / G][2 * (lane & (G - 1))]);
+          w[0] = q.x + q.y;
+        }
+#pragma unroll
+        for (int o = G / 2; o; o /= 2) w[0] += __shfl_xor_sync(0xFFFFFFFFu, w[0], o);
+      }
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] = __shfl_sync(0xFFFFFFFFu, w[0], k * G);
+    }
+    if (!joined) return;
     if (size > 1) {      // one slice here
       const uint32_t bar = smem_u32(&space->arrived[turn]);
       if (threadIdx.x == 0) mbar_expect_tx(bar, size * K * 4);
