@@ -166,7 +166,7 @@ struct RowSum {
   }
   // K values at once.  One or two are added lane by lane.  Of more, lanes halve them between one another as they add (P / 2, P / 4, ... exchanges and then one each, where P
   // sums one by one would be five each): lanes of a group of 32 / P end with one of the sums, join it across the warps and hand it round.  Fewer instructions, a
-  // longer way: four values 96 to 91 us (16384 x 4096 forward), two 160 to 174 (65536 x 768 backward, layer norms).
+  // longer way: four values 96 to 91 us (16384 x 4096 forward), two 168 to 174 (65536 x 768 backward, layer norms).
   template <int K>
   __device__ __forceinline__ void operator()(float (&v)[K], uint32_t size) {
     static_assert(K <= 8, "");
@@ -541,18 +541,25 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_backward(const NormPar
 #pragma unroll
         for (int j = 0; j < 8; ++j) d[j] = 0.f;
       }
-      // RMS norms have one exchange of sums: with u = D(hat1 gw), the pre norm's  S = sum t hat2,  the post norm's sum is
-      // sum u (dh + r2 t) - r2 S / cols sum u hat2.
-      float hat2[8], t[8], s[3] = {0.f, 0.f, 0.f};
-      if (p.dn.p || !FULL) {
+      // One exchange of sums for both norms.  With  e = dh + r2 w2 dn,  q = D(g w1),  S = mean(w2 dn hat2)  and  M = mean(w2 dn)  (layer norms)
+      // the gradient of h is  d = e - r2 (M + S hat2),  and what the post norm takes the mean of follows from sums that need neither S nor M:
+      //   sum q d = sum q e - r2 M sum q - r2 S sum q hat2,     sum q hat1 d = sum q hat1 e - r2 M sum q hat1 - r2 S sum q hat1 hat2
+      float hat2[8], q[8], s[FULL ? 8 : 3];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) hat2[j] = FULL ? __fmaf_rn(hat1[j], gw[j], gb[j]) : hat1[j] * gw[j];
-        if (p.drop.threshold) drop8(p.drop, draw, hat2);
-      }
+      for (int i = 0; i < (FULL ? 8 : 3); ++i) s[i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = FULL ? gw[j] : hat1[j] * gw[j];      // (RMS norms: q hat1)
+      if (p.drop.threshold && (!FULL || p.post_w)) drop8(p.drop, draw, q);
       if (p.dn.p) {
-        float u[8];
+        float t[8];
+        if constexpr (FULL) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = hat2[j];
+          for (int j = 0; j < 8; ++j) hat2[j] = __fmaf_rn(hat1[j], gw[j], gb[j]);
+          if (p.drop.threshold) drop8(p.drop, draw, hat2);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) hat2[j] = q[j];
+        }
         if (p.x.p) {
           read_row8<VEC, X>(from + kAtX, VEC ? 0 : p.x.shift(row), at.left, at.lane, t);
 #pragma unroll
@@ -566,62 +573,64 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_backward(const NormPar
           if constexpr (FULL) s_e[j] += t[j];
           t[j] *= w2[j];
           s[0] = __fmaf_rn(t[j], hat2[j], s[0]);
-          if constexpr (FULL) {
-            s[1] += t[j];
-          } else {
-            d[j] = __fmaf_rn(st.w, t[j], d[j]);
-            s[1] = __fmaf_rn(u[j], d[j], s[1]);
-            s[2] = __fmaf_rn(u[j], hat2[j], s[2]);
-          }
-        }
-      } else if constexpr (!FULL) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[1] = __fmaf_rn(hat2[j], d[j], s[1]);
-      }
-      if constexpr (FULL) {
-        if (p.dn.p) {
-          sum(*reinterpret_cast<float(*)[2]>(s));
-          const float k = s[0] * inv, m = p.layer ? s[1] * inv : 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) d[j] = __fmaf_rn(st.w, __fmaf_rn(-hat2[j], k, t[j] - m), d[j]);
+          if constexpr (FULL) s[1] += t[j];
+          d[j] = __fmaf_rn(st.w, t[j], d[j]);
         }
       } else {
-        if (p.post_w)
-          sum(s);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) hat2[j] = 0.f;
+      }
+      float k1 = 0.f, m1 = 0.f;
+      if (p.post_w) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (FULL) {
+            s[2] = __fmaf_rn(q[j], d[j], s[2]);
+            s[3] += q[j];
+            s[4] = __fmaf_rn(q[j], hat2[j], s[4]);
+            const float u = q[j] * hat1[j];
+            s[5] = __fmaf_rn(u, d[j], s[5]);
+            s[6] += u;
+            s[7] = __fmaf_rn(u, hat2[j], s[7]);
+          } else {
+            s[1] = __fmaf_rn(q[j], d[j], s[1]);
+            s[2] = __fmaf_rn(q[j], hat2[j], s[2]);
+          }
+        }
+        sum(s);
+      } else if (p.dn.p) {
+        if constexpr (FULL)
+          sum(*reinterpret_cast<float(*)[2]>(s));
         else
           sum(*reinterpret_cast<float(*)[1]>(s));
-        if (p.dn.p) {
-          const float k = st.w * s[0] * inv;
-          s[1] = __fmaf_rn(-k, s[2], s[1]);
+      }
+      const float k = st.w * s[0] * inv;
+      if constexpr (FULL) {
+        const float m = p.layer ? st.w * s[1] * inv : 0.f;
+        m1 = p.layer ? __fmaf_rn(-k, s[4], __fmaf_rn(-m, s[3], s[2])) * inv : 0.f;
+        k1 = __fmaf_rn(-k, s[7], __fmaf_rn(-m, s[6], s[5])) * inv;
+        if (p.dn.p)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d[j] = __fmaf_rn(-hat2[j], k, d[j] - m);
+      } else {
+        k1 = __fmaf_rn(-k, s[2], s[1]) * inv;
+        if (p.dn.p)
 #pragma unroll
           for (int j = 0; j < 8; ++j) d[j] = __fmaf_rn(-hat2[j], k, d[j]);
-        }
       }
       if (p.dx.p) {
+        float t[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) t[j] = p.residual_scale * d[j];
         store_row8<VEC>(p.dx.out<X>(row), at.c, p.cols, at.lane, t);
       }
       if (p.drop.threshold) drop8(p.drop, draw, d);
-      if constexpr (FULL) s[0] = s[1] = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         s_a[j] = __fmaf_rn(d[j], hat1[j], s_a[j]);
         if constexpr (FULL) s_b[j] += d[j];
         d[j] *= gw[j];
-        if constexpr (FULL) s[0] = __fmaf_rn(d[j], hat1[j], s[0]), s[1] += d[j];
-      }
-      if (p.post_w) {
-        if constexpr (FULL) {
-          sum(*reinterpret_cast<float(*)[2]>(s));
-          const float k = s[0] * inv, m = p.layer ? s[1] * inv : 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) d[j] = st.y * __fmaf_rn(-hat1[j], k, d[j] - m);
-        } else {
-          const float k = s[1] * inv;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) d[j] = st.y * __fmaf_rn(-hat1[j], k, d[j]);
-        }
+        if (p.post_w) d[j] = st.y * __fmaf_rn(-hat1[j], k1, FULL ? d[j] - m1 : d[j]);
       }
       if (p.dy.p) store_row8<VEC>(p.dy.out<Y>(row), at.c, p.cols, at.lane, d);
       st = st_next;
