@@ -103,15 +103,14 @@ def _pitch(cols: int) -> int:
     return (cols + 63) // 64 * 64 or 64
 
 
-def _packed(x: torch.Tensor, ld: int, dtype: torch.dtype, index: int) -> tuple[torch.Tensor, int]:
-    """A copy of a matrix in 16 bits, on rows of whole lines."""
-    r, c = x.shape
+def _packed(x: torch.Tensor, r: int, c: int, ld: int, dtype: torch.dtype, index: int) -> tuple[torch.Tensor, int]:
+    """A copy of a matrix in 16 bits, on rows of whole lines: [rows, pitch], and the pitch."""
     pitch = _pitch(c)
     out = x.new_empty((r, pitch), dtype=dtype)
-    rc = _call(_pack_at, x.data_ptr(), _m._dtype(x.dtype, "x"), r, c, ld, out.data_ptr(), _half(dtype, "dtype"), pitch, _raw_stream(index))
+    rc = _call(_pack_at, x.data_ptr(), _DTYPES[x.dtype], r, c, ld, out.data_ptr(), _HALVES[dtype], pitch, _raw_stream(index))
     if rc:
         _check(rc, "ds_f16_pack")
-    return out[:, :c], pitch
+    return out, pitch
 
 
 def _product(layout: int, dt: int, m: int, n: int, k: int, a: int, lda: int, b: int, ldb: int, bias, act: int, res, ldr: int, z, ldz: int, out: int, odt: int,
@@ -139,22 +138,28 @@ def linear16(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None,
     if stream is not None:
         with torch.cuda.stream(stream):      # what is allocated here belongs to the stream that uses it
             return linear16(x, w, bias, activation, residual, out_dtype, out)
-    return _forward(x, w, bias, _activation(activation), residual, out_dtype, out, False)[0]
+    return _forward(x, w, bias, _activation(activation), residual, out_dtype, out)
 
 
-def _forward(x, w, bias, act, residual, out_dtype, out, keep_z):
+def _forward(x, w, bias, act, residual, out_dtype, out):
     if _struct is None:
         _load()
     dtype = x.dtype
-    dt = _HALVES.get(dtype)
-    if dt is None:
+    if dtype not in _HALVES:
         _half(dtype, "x")
     x, m, k, ldx, index = _rows(x, "x")
     n = w.shape[0]
     w, ldw = _like(w, n, k, dtype, index, "w")
     if index != _current():                  # the library works on the current device
         with torch.cuda.device(index):
-            return _forward(x, w, bias, act, residual, out_dtype, out, keep_z)
+            return _forward(x, w, bias, act, residual, out_dtype, out)
+    return _multiply(x, m, k, ldx, w, n, ldw, bias, act, residual, out_dtype, out, False, index, _raw_stream(index))[0]
+
+
+def _multiply(x, m, k, ldx, w, n, ldw, bias, act, residual, out_dtype, out, keep_z, index, raw):
+    """out and z of x and w whose first entries are those of [m, k] and [n, k] matrices of one type."""
+    dtype = x.dtype
+    dt = _HALVES[dtype]
     bp = None if bias is None else _floats(bias, n, index, "bias")
     rp, ldr = None, 0
     if residual is not None:
@@ -174,7 +179,7 @@ def _forward(x, w, bias, act, residual, out_dtype, out, keep_z):
         z = x.new_empty((m, ldz))
         zp = z.data_ptr()
     if m and n:
-        _product(DS_F16_FORWARD, dt, m, n, k, x.data_ptr(), ldx, w.data_ptr(), ldw, bp, act, rp, ldr, zp, ldz, out.data_ptr(), odt, ldo, index, _raw_stream(index), x)
+        _product(DS_F16_FORWARD, dt, m, n, k, x.data_ptr(), ldx, w.data_ptr(), ldw, bp, act, rp, ldr, zp, ldz, out.data_ptr(), odt, ldo, index, raw, x)
     return out, z
 
 
@@ -196,26 +201,35 @@ class Linear16:
                 return self.set_weight(weight)
         if _struct is None:
             _load()
-        _m._dtype(weight.dtype, "weight")
-        weight, r, _, ld, index = _rows(weight, "weight")
+        if weight.dtype not in _DTYPES:
+            _m._dtype(weight.dtype, "weight")
+        weight, r, c, ld, index = _rows(weight, "weight")
         dtype = self._dtype or (torch.bfloat16 if weight.dtype is torch.float32 else weight.dtype)
-        _half(dtype, "dtype")
+        if dtype not in _HALVES:
+            _half(dtype, "dtype")
         if self.bias is not None:
             _floats(self.bias, r, index, "bias")
         if index != _current():
             with torch.cuda.device(index):
                 return self.set_weight(weight)
         if weight.dtype is not dtype or not _on_boundary(weight.data_ptr(), ld, r):
-            weight, ld = _packed(weight, ld, dtype, index)
-        self.weight, self._index = weight, index
+            weight, ld = _packed(weight, r, c, ld, dtype, index)
+        # the weights, perhaps on longer rows, and what backward() reads: x, likewise, and z
+        self._w, self._ldw, self.shape, self._index = weight, ld, torch.Size((r, c)), index
         self._x = self._z = None
+        self._rows_of_x = self._ldx = 0
         self._stream = self._saved_on = _raw_stream(index)      # where the allocator takes the tensors to be in use
+
+    @property
+    def weight(self) -> torch.Tensor:
+        """The weights as the products read them."""
+        return self._w[:, :self.shape[1]]
 
     def _used(self, saved: bool):
         """Tells the allocator of the current stream: dropped before that has run, the layer's memory is kept until it has."""
         raw = _raw_stream(self._index)
         if raw != self._stream:
-            self.weight.record_stream(torch.cuda.current_stream(self._index))
+            self._w.record_stream(torch.cuda.current_stream(self._index))
             if self.bias is not None:
                 self.bias.record_stream(torch.cuda.current_stream(self._index))
             self._stream = raw
@@ -237,15 +251,18 @@ class Linear16:
         if index != _current():
             with torch.cuda.device(index):
                 return self.forward(x, residual, training, out_dtype, out)
-        raw = self._used(False)
-        if not training:
-            return _forward(x, self.weight, self.bias, self._act, residual, out_dtype, out, False)[0]
-        _half(x.dtype, "x")
-        x, m, k, ldx, _ = _rows(x, "x")
-        if m and k and not _on_boundary(x.data_ptr(), ldx, m):      # once, for this product and for the gradient of the weights
-            x = _packed(x, ldx, x.dtype, index)[0]
-        y, z = _forward(x, self.weight, self.bias, self._act, residual, out_dtype, out, self._act != 0)
-        self._x, self._z, self._saved_on = x, z, raw
+        raw, w, (n, k) = self._used(False), self._w, self.shape
+        dtype = w.dtype
+        if x.dtype is not dtype:
+            raise TypeError(f"x: {dtype} expected, got {x.dtype}")
+        x, m, c, ldx, _ = _rows(x, "x")
+        if c != k:
+            raise ValueError(f"x has {c} columns, the weights {k}")
+        if training and m and k and not _on_boundary(x.data_ptr(), ldx, m):      # once, for this product and for the gradient of the weights
+            x, ldx = _packed(x, m, k, ldx, dtype, index)
+        y, z = _multiply(x, m, k, ldx, w, n, self._ldw, self.bias, self._act, residual, out_dtype, out, training and self._act != 0, index, raw)
+        if training:
+            self._x, self._rows_of_x, self._ldx, self._z, self._saved_on = x, m, ldx, z, raw
         return y
 
     def backward(self, dy: torch.Tensor, grad_dtype: torch.dtype | None = None, dw: torch.Tensor | None = None, db: torch.Tensor | None = None,
@@ -264,7 +281,7 @@ class Linear16:
         if index != _current():
             with torch.cuda.device(index):
                 return self.backward(dy, grad_dtype, dw, db, need_dx)
-        (m, k), n = x.shape, self.weight.shape[0]
+        m, (n, k) = self._rows_of_x, self.shape
         dy, lddy = _like(dy, m, n, dtype, index, "dy")
         grad_dtype = grad_dtype or dtype
         if dw is None:
@@ -296,15 +313,15 @@ class Linear16:
             if act:
                 dz, lddz = base, ldn
         if need_dx and m and n and not _on_boundary(dz, lddz, m):      # once, for both products
-            buf, lddz = _packed(dy, lddz, dtype, index)
+            buf, lddz = _packed(dy, m, n, lddz, dtype, index)
             dz = buf.data_ptr()
         dx = None
         if need_dx:
-            dx = _like_of(x)
+            dx = x.new_empty((m, k))
             if m and k:
-                _product(DS_F16_INPUTS, dt, m, k, n, dz, lddz, self.weight.data_ptr(), self.weight.stride(0), None, 0, None, 0, None, 0, dx.data_ptr(), dt, k, index, raw, x)
+                _product(DS_F16_INPUTS, dt, m, k, n, dz, lddz, self._w.data_ptr(), self._ldw, None, 0, None, 0, None, 0, dx.data_ptr(), dt, k, index, raw, x)
         if n and k:
-            _product(DS_F16_WEIGHTS, dt, n, k, m, dz, lddz, x.data_ptr(), x.stride(0), None, 0, None, 0, None, 0, dw.data_ptr(), _DTYPES[dw.dtype], ldo, index, raw, x)
+            _product(DS_F16_WEIGHTS, dt, n, k, m, dz, lddz, x.data_ptr(), self._ldx, None, 0, None, 0, None, 0, dw.data_ptr(), _DTYPES[dw.dtype], ldo, index, raw, x)
         return dx, dw, db
 
 
