@@ -1,5 +1,5 @@
 // Dropout by itself, of activations or of their gradients: y = keep ? x * scale : 0 with the mask of dsq_dropout.cuh.  Bound by memory
-// where entries have 32 bits, near the generator's rate in 16 (twenty 32 x 32-bit products for eight entries).
+// where entries have 32 bits (16384 x 8192: 158 us, 6.8 TB/s), near the generator's rate in 16 (twenty 32 x 32-bit products for eight entries: 91 us, 5.9 TB/s).
 #include "dsq_dropout.cuh"
 #include "dsq_mma.cuh"
 #include "dsq_rows8.cuh"

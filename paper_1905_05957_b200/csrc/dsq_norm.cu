@@ -6,6 +6,10 @@
 // registers; backward, h is computed again from x and y (which costs no byte more than reading it would) with the norms'
 // statistics that the forward pass left, and what parameters get is summed by CTAs that each take a run of rows, a thread
 // its eight columns, and added up in the CTAs' order: nothing depends on timing.
+//
+// What bounds it (16384 x 4096, RMS norms before and after, bf16): forward 91 us, 5.9 TB/s, and backward 164 us, 4.9 TB/s, of a copy's 6.5; parameters and
+// sums take the registers of one CTA an SM (128 a thread), and what is left over is the latency of a row's exchanges of sums and the issue of instructions (53 and 60 % of the cycles).
+// Layer norms have an exchange more each and twice the sums: 127 and 221 us.  One CTA a row that read the parameters again took 143 and 514.
 #include "dsq_dropout.cuh"
 #include "dsq_mma.cuh"
 #include "dsq_rows8.cuh"
@@ -67,6 +71,7 @@ struct RowWalk {
     while (row >= last && unit < p.units) enter(p, unit + teams);
   }
 };
+
 // ---- rows on their way ----------------------------------------------------------------------------------
 // Each warp copies its 256 columns of the rows to come into shared memory, DEPTH - 1 rows ahead: nothing but the warp itself waits for them, and no
 // registers are held.  Whole granules are copied as they lie, so rows may start anywhere.  (A lane's two granules of floats apart, so that
