@@ -389,7 +389,8 @@ cudaError_t multiply(const ds_f16_product* p, const Out16& o, Operand16 a, Opera
   }
   const MmaShape s{m, n, k, 1, 2, 0, 0, p->dev_status, 1, (uint32_t)o.bf16};
   const bool bare = !o.residual && !o.z && !o.bias && !o.act;
-  const bool blocks = !o.f32 && aligned(o.out, 16) && o.ldo % 8 == 0 && (!o.residual || (aligned(o.residual, 16) && o.ldr % 8 == 0)) &&
+  // (rows that end inside 16 bytes: a block's store would write the rest of them, which is not the matrix's)
+  const bool blocks = !o.f32 && n % 8 == 0 && aligned(o.out, 16) && o.ldo % 8 == 0 && (!o.residual || (aligned(o.residual, 16) && o.ldr % 8 == 0)) &&
                       (!o.z || (aligned(o.z, 16) && o.ldz % 8 == 0)) && (p->layout == DS_F16_FORWARD || bare);
   const bool floats = o.f32 && bare && aligned(o.out, 32) && o.ldo % 8 == 0;
   if (m <= kTurnedMost || !(blocks || floats)) {

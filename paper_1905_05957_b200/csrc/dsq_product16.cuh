@@ -120,8 +120,8 @@ struct Out16 {
 
 // ---- epilogues ------------------------------------------------------------------------------------------
 
-// Rows of residual, z and out start on 16-byte boundaries and out has 16 bits: blocks of 32 x 32 pass through shared memory
-// by TMA.  OUTS 2: z leaves, too.
+// Rows of residual, z and out start and end on 16-byte boundaries and out has 16 bits: blocks of 32 x 32 pass through shared memory
+// by TMA (whose stores leave out rows and columns outside the matrix, but columns 16 bytes at a time).  OUTS 2: z leaves, too.
 template <int OUTS>
 struct EpiBlocks {
   static constexpr int kIn = 1, kOut = OUTS;

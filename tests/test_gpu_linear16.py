@@ -93,6 +93,37 @@ def test_rows_within_wider_rows(m, k, n, pad, offset):
     assert torch.equal(dx, (dy.double() @ w.double()).to(dtype))
 
 
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("m", [2, 12, 40, 100, 700])
+@pytest.mark.parametrize("n", [1, 7, 31, 66, 129, 250, 255, 1001, 1004])
+def test_rows_that_end_inside_16_bytes(m, n, dtype):
+    """Operands and outputs whose rows start on 16-byte boundaries and end anywhere: what lies behind them is not read into sums (NaN) and not written."""
+    def padded(*shape, fill=float("nan"), dt=dtype, seed=None):
+        r, c = shape
+        buf = torch.full((r, (c + 7) // 8 * 8 + 8), fill, dtype=dt, device="cuda")
+        if seed is not None:
+            buf[:, :c] = _whole(shape, seed, dt)
+        return buf[:, :c], buf
+    (x, _), (w, _), (r, _), (dy, _) = padded(m, 37, seed=1), padded(n, 37, seed=2), padded(m, n, seed=3), padded(m, n, seed=4)
+    z = x.double() @ w.double().T
+    for dt in (dtype, torch.float32):
+        out, buf = padded(m, n, fill=7.0, dt=dt)
+        linear16(x, w, residual=r, out=out)
+        assert torch.equal(out, (z + r.double()).to(dt)) and bool((buf[:, n:] == 7.0).all())
+    layer = Linear16(w, activation="relu")
+    assert torch.equal(layer.forward(x, training=True), torch.relu(z).to(dtype))
+    dz = dy.double() * (z > 0)
+    for dt in (dtype, torch.float32):
+        dw, buf = padded(n, 37, fill=7.0, dt=dt)
+        dx, _, _ = layer.backward(dy, dw=dw)
+        assert torch.equal(dx, (dz @ w.double()).to(dtype)) and torch.equal(dw, (dz.T @ x.double()).to(dt)) and bool((buf[:, 37:] == 7.0).all())
+    layer = Linear16(dy.t().contiguous())          # gradients of weights whose rows end inside 16 bytes, on rows that do not
+    layer.forward(r.t().contiguous()[:, :m], training=True)
+    got, buf = padded(n, m, fill=7.0)
+    layer.backward(_whole((n, n), 5, dtype), dw=got)
+    assert bool((buf[:, m:] == 7.0).all())
+
+
 def test_columns_of_one_buffer():
     buf = _whole((70, 96), 1, torch.bfloat16)
     x, w = buf[:, :32], _whole((64, 32), 2, torch.bfloat16)
