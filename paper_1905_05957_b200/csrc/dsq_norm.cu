@@ -609,9 +609,9 @@ __global__ void __launch_bounds__(kNormThreads, 1) k_norm_backward(const NormPar
         else
           sum(*reinterpret_cast<float(*)[1]>(s));
       }
-      const float k = st.w * s[0] * inv;
+      const float r2 = p.dn.p ? st.w * inv : 0.f, k = r2 * s[0];      // without a pre norm its statistics are not there
       if constexpr (FULL) {
-        const float m = p.layer ? st.w * s[1] * inv : 0.f;
+        const float m = p.layer ? r2 * s[1] : 0.f;
         m1 = p.layer ? __fmaf_rn(-k, s[4], __fmaf_rn(-m, s[3], s[2])) * inv : 0.f;
         k1 = __fmaf_rn(-k, s[7], __fmaf_rn(-m, s[6], s[5])) * inv;
         if (p.dn.p)

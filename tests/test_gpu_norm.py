@@ -301,6 +301,28 @@ def test_rows_of_zeros_and_large_means():
     assert float((dy - 1000).abs().max()) < 1e-2 and not g["pre_weight"].any()      # 1 / sqrt(eps)
 
 
+@pytest.mark.parametrize("biases", [False, True])
+@pytest.mark.parametrize("post,pre", [(True, False), (False, True), (False, False)])
+def test_statistics_of_norms_that_are_not_there(post, pre, biases):
+    """Memory that the forward pass leaves as it was has no part in the gradients."""
+    rows, cols = 37, 200
+    for norm in ("rms", "layer"):
+        params = _params(cols, norm, post, pre, 1, biases)
+        op = ResidualNorm(norm, **params)
+        y, x, dh, dn = (_normal((rows, cols), s) for s in (1, 2, 3, 4))
+        got = []
+        for poison in (0.0, float("nan"), float("inf")):
+            junk = [torch.full((rows, 4), poison, device="cuda") for _ in range(64)]      # what is given back next is one of these
+            del junk
+            op.forward(y, x, training=True)
+            for given in ((dh, dn) if pre else (dh,), (dh,)):
+                dy, dx, g = op.backward(*given)
+                got.append([dy, dx, *g.values()])
+        for i in range(2):
+            assert all(bool(t.isfinite().all()) for t in got[i])
+            assert all(torch.equal(a, b) for other in got[i + 2::2] for a, b in zip(got[i], other))
+
+
 def test_no_rows():
     params = _params(64, "rms", True, True, 2, False)
     op = ResidualNorm("rms", **params)
