@@ -121,8 +121,7 @@ extern "C" int ds_dropout(const void* x, int dtype, uint64_t rows, uint64_t cols
   const uint32_t size = dtype == DS_F32 ? 4 : 2;
   if (!aligned(x, size) || !aligned(out, size)) return DS_ERR_ALIGN;
   // over its input only entry by entry
-  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(out);
-  if (a < b + ((rows - 1) * ldo + cols) * size && b < a + ((rows - 1) * ldx + cols) * size && !(a == b && (ldx == ldo || rows == 1))) return DS_ERR_INVALID_ARG;
+  if (overlap(span(x, rows, cols, ldx, size), span(out, rows, cols, ldo, size)) && !(x == out && (ldx == ldo || rows == 1))) return DS_ERR_INVALID_ARG;
   const Drop drop = make_drop(threshold, seed, layer, step);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = dtype == DS_F32    ? launch<float>(x, ldx, out, ldo, (uint32_t)rows, (uint32_t)cols, drop, st)

@@ -16,23 +16,6 @@ inline bool dtype_ok(uint64_t t) { return t == DS_F32 || t == DS_BF16 || t == DS
 inline uint32_t size_of(uint64_t dtype) { return dtype == DS_F32 ? 4 : 2; }
 constexpr uint64_t kMaxLen = 1ull << 30;
 
-// Whether the rows of two matrices share memory: `rows` of `bytes` bytes, `ld` apart.  Rows that lie side by side in wider ones
-// (columns of one buffer) do not.
-struct Span {
-  uintptr_t p;
-  uint64_t rows, bytes, ld;
-};
-inline Span span(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t size) {
-  return {reinterpret_cast<uintptr_t>(p), rows, cols * size, ld * size};
-}
-inline bool overlap(const Span& a, const Span& b) {
-  if (!a.p || !b.p || !a.rows || !b.rows || !a.bytes || !b.bytes) return false;
-  if (a.p >= b.p + (b.rows - 1) * b.ld + b.bytes || b.p >= a.p + (a.rows - 1) * a.ld + a.bytes) return false;
-  if (a.ld != b.ld || !a.ld) return true;
-  const uint64_t off = a.p >= b.p ? (a.p - b.p) % a.ld : (a.ld - (b.p - a.p) % a.ld) % a.ld;      // of a's row within b's rows
-  return off < b.bytes || off + a.bytes > a.ld;
-}
-
 // ---- copies onto 16-byte rows ---------------------------------------------------------------------------
 // Bound by memory; a lane takes eight entries of a row.  Entries behind a row's end become 0.
 template <class T, class O>

@@ -816,15 +816,6 @@ cudaError_t by_types(const ds_norm_args* p, F&& f) {
   return p->stream_dtype == DS_F32 ? f(float(), H()) : f(H(), H());
 }
 
-struct Region {
-  uintptr_t p;
-  uint64_t bytes;
-};
-inline Region region(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t size) {
-  return {reinterpret_cast<uintptr_t>(p), p && rows && cols ? ((rows - 1) * ld + cols) * size : 0};
-}
-inline bool overlap(const Region& a, const Region& b) { return a.bytes && b.bytes && a.p < b.p + b.bytes && b.p < a.p + a.bytes; }
-
 int check(const ds_norm_args* p, bool back) {
   if (!p || p->dtype > DS_F16 || (p->stream_dtype != p->dtype && p->stream_dtype != DS_F32) || p->norm > DS_NORM_LAYER) return DS_ERR_INVALID_ARG;
   if (p->rows > kMaxRows || p->cols == 0) return DS_ERR_INVALID_ARG;
@@ -893,8 +884,8 @@ int ds_norm_forward(const ds_norm_args* p, void* cuda_stream) {
   const int rc = check(p, false);
   if (rc != DS_OK || p->rows == 0) return rc;
   const uint32_t sy = size_of(p->dtype), sx = size_of(p->stream_dtype);
-  const Region y = region(p->y, p->rows, p->cols, p->ldy, sy), x = region(p->x, p->rows, p->cols, p->ldx, sx), h = region(p->h, p->rows, p->cols, p->ldh, sx),
-               n = region(p->n, p->rows, p->cols, p->ldn, sy), stats = region(p->stats, 1, 4 * p->rows, 0, 4);
+  const Span y = span(p->y, p->rows, p->cols, p->ldy, sy), x = span(p->x, p->rows, p->cols, p->ldx, sx), h = span(p->h, p->rows, p->cols, p->ldh, sx),
+               n = span(p->n, p->rows, p->cols, p->ldn, sy), stats = span(p->stats, 1, 4 * p->rows, 0, 4);
   // a thread reads its entries of x and y before it writes the same ones of h; n comes after them all
   auto over = [&](const void* a, uint64_t lda, uint32_t sa, const void* b, uint64_t ldb, uint32_t sb) { return a == b && sa == sb && (lda == ldb || p->rows == 1); };
   if ((overlap(h, x) && !over(p->h, p->ldh, sx, p->x, p->ldx, sx)) || (overlap(h, y) && !over(p->h, p->ldh, sx, p->y, p->ldy, sy)) ||
@@ -934,10 +925,10 @@ int ds_norm_backward(const ds_norm_args* p, void* cuda_stream) {
     if (!aligned(p->workspace, 16)) return DS_ERR_ALIGN;
     if (p->workspace_bytes < ws) return DS_ERR_BUFFER_TOO_SMALL;
   }
-  const Region in[] = {region(p->y, p->rows, p->cols, p->ldy, sy), region(p->x, p->rows, p->cols, p->ldx, sx), region(p->dh, p->rows, p->cols, p->lddh, sx),
-                       region(p->dn, p->rows, p->cols, p->lddn, sy), region(p->stats, 1, 4 * p->rows, 0, 4)};
-  const struct { Region r; const void* p; uint64_t ld; uint32_t size; } to[] = {{region(p->dx, p->rows, p->cols, p->lddx, sx), p->dx, p->lddx, sx},
-                                                                                {region(p->dy, p->rows, p->cols, p->lddy, sy), p->dy, p->lddy, sy}};
+  const Span in[] = {span(p->y, p->rows, p->cols, p->ldy, sy), span(p->x, p->rows, p->cols, p->ldx, sx), span(p->dh, p->rows, p->cols, p->lddh, sx),
+                       span(p->dn, p->rows, p->cols, p->lddn, sy), span(p->stats, 1, 4 * p->rows, 0, 4)};
+  const struct { Span r; const void* p; uint64_t ld; uint32_t size; } to[] = {{span(p->dx, p->rows, p->cols, p->lddx, sx), p->dx, p->lddx, sx},
+                                                                                {span(p->dy, p->rows, p->cols, p->lddy, sy), p->dy, p->lddy, sy}};
   const struct { const void* p; uint64_t ld; uint32_t size; } from[] = {{p->y, p->ldy, sy}, {p->x, p->ldx, sx}, {p->dh, p->lddh, sx}, {p->dn, p->lddn, sy}};
   for (auto& t : to) {      // over an input only entry by entry
     for (int i = 0; i < 4; ++i)
@@ -945,11 +936,11 @@ int ds_norm_backward(const ds_norm_args* p, void* cuda_stream) {
     if (overlap(t.r, in[4])) return DS_ERR_INVALID_ARG;
   }
   if (overlap(to[0].r, to[1].r)) return DS_ERR_INVALID_ARG;
-  const Region space = region(p->workspace, 1, ws, 0, 1);
+  const Span space = span(p->workspace, 1, ws, 0, 1);
   const float* weights[] = {p->post_w, p->post_b, p->pre_w, p->pre_b, p->gate};
-  Region small[6];
+  Span small[6];
   int n = 0;
-  for (auto& o : outs) small[n++] = region(o.to, 1, o.n, 0, 4);
+  for (auto& o : outs) small[n++] = span(o.to, 1, o.n, 0, 4);
   small[n++] = space;
   for (int i = 0; i < n; ++i) {
     for (int j = 0; j < i; ++j)
@@ -959,7 +950,7 @@ int ds_norm_backward(const ds_norm_args* p, void* cuda_stream) {
     for (auto& t : to)
       if (overlap(small[i], t.r)) return DS_ERR_INVALID_ARG;
     for (int j = 0; j < 5; ++j)
-      if (overlap(small[i], region(weights[j], 1, j == 4 ? p->groups * p->cols : p->cols, 0, 4))) return DS_ERR_INVALID_ARG;
+      if (overlap(small[i], span(weights[j], 1, j == 4 ? p->groups * p->cols : p->cols, 0, 4))) return DS_ERR_INVALID_ARG;
   }
   NormParams q = params(p, true);
   uint8_t* space_p = static_cast<uint8_t*>(p->workspace);

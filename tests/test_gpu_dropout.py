@@ -114,3 +114,17 @@ def test_refusals():
         dropout(x[0], 0.1, 1)
     with pytest.raises(DsqError):
         dropout(x[:9], 0.1, 1, out=x[1:])      # over its input, a row off
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(5, 8), (33, 131), (300, 2056)])
+def test_columns_of_one_buffer(rows, cols, dtype):
+    """Input and output side by side in wider rows; what does share memory is refused."""
+    buf = torch.zeros(rows, 2 * cols, device="cuda", dtype=dtype)
+    x, out = buf[:, :cols], buf[:, cols:]
+    x.copy_(_x(rows, cols, dtype))
+    want = dropout(x.clone(), 0.3, 5)
+    dropout(x, 0.3, 5, out=out)
+    assert torch.equal(out, want) and torch.equal(x, _x(rows, cols, dtype))
+    with pytest.raises(DsqError):
+        dropout(x, 0.3, 5, out=buf[:, cols - 1:2 * cols - 1])

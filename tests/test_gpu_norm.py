@@ -323,6 +323,21 @@ def test_statistics_of_norms_that_are_not_there(post, pre, biases):
             assert all(torch.equal(a, b) for other in got[i + 2::2] for a, b in zip(got[i], other))
 
 
+@pytest.mark.parametrize("rows,cols", [(5, 8), (33, 200), (7, 333), (3, 4100)])
+def test_columns_of_one_buffer(rows, cols):
+    """Inputs and outputs side by side in wider rows; what does share memory is refused."""
+    buf = torch.zeros(rows, 4 * cols, device="cuda")
+    y, x, h, n = (buf[:, i * cols:(i + 1) * cols] for i in range(4))
+    y.copy_(_normal((rows, cols), 1))
+    x.copy_(_normal((rows, cols), 2))
+    op = ResidualNorm("layer", **_params(cols, "layer", True, True, 1, True))
+    want = op.forward(y.clone(), x.clone())
+    op.forward(y, x, h=h, n=n)
+    assert torch.equal(h, want[0]) and torch.equal(n, want[1])
+    with pytest.raises(DsqError):
+        op.forward(y, x, h=h, n=buf[:, 3 * cols - 1:4 * cols - 1])
+
+
 def test_no_rows():
     params = _params(64, "rms", True, True, 2, False)
     op = ResidualNorm("rms", **params)
