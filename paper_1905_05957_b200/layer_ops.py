@@ -25,13 +25,14 @@ _call = _struct = _size = _matmul_at = _matmul_ws = _slope_at = _slope_ws = _pac
 
 
 def _load():
-    """Looks the library's functions up once."""
+    """Looks the library's functions up once.  _struct comes last: who sees it, on whichever thread, sees the others."""
     global _call, _struct, _size, _matmul_at, _matmul_ws, _slope_at, _slope_ws, _pack_at, _norm_at, _norm_back_at, _norm_back_ws, _dropout_at
-    _struct, _size, at = fast_struct_call()
+    struct, _size, at = fast_struct_call()
     _matmul_at, _slope_at, _norm_at, _norm_back_at = (at[n] for n in ("ds_f16_matmul", "ds_f16_slope", "ds_norm_forward", "ds_norm_backward"))
     _matmul_ws, _norm_back_ws, _slope_ws = at["ds_f16_matmul_workspace"], at["ds_norm_backward_workspace"], load_library().ds_f16_slope_workspace
     _call, at = fast_call()
     _pack_at, _dropout_at = at["ds_f16_pack"], at["ds_dropout"]
+    _struct = struct
 
 
 def _half(t: torch.dtype, what: str) -> int:

@@ -49,6 +49,17 @@ def test_struct_calls(lib):
                 call(*bad)
 
 
+def test_a_second_thread_sees_all_functions_or_none(lib, monkeypatch):
+    from paper_1905_05957_b200 import layer_ops
+    seen = []
+    for name in ("fast_struct_call", "fast_call"):
+        real = getattr(b, name)
+        monkeypatch.setattr(layer_ops, name, lambda real=real: (seen.append(layer_ops._struct), real())[1])
+    monkeypatch.setattr(layer_ops, "_struct", None)
+    layer_ops._load()
+    assert seen == [None, None] and layer_ops._struct is not None and layer_ops._dropout_at is not None
+
+
 def _args(kind, values, **kw):
     values = {**values, **kw}
     return kind(**{k: v for k, v in values.items() if v is not None})
