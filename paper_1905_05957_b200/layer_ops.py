@@ -375,8 +375,8 @@ class ResidualNorm:
 
     the stream and the input of the next.  post and pre are RMS ("rms") or layer norms ("layer") over a row, each there if it has a weight, with an optional bias;
     gate [cols] or [groups, cols] multiplies rows by entry (the rows are `groups` equal runs: one for each sequence, say); D is dropout with probability p, drawn as
-    dropout() draws it.  All parameters are float32 and are used where they lie; the arithmetic is in 32 bits, h and n are rounded once.  y and n have one type
-    (float32, bfloat16, float16), x and h the same or float32."""
+    dropout() draws it.  All parameters are float32 and are used where they lie at each call (a tensor may get other storage between two of them, of the same length and on the same
+    device); the arithmetic is in 32 bits, h and n are rounded once.  y and n have one type (float32, bfloat16, float16), x and h the same or float32."""
 
     def __init__(self, norm: str = "rms", post_weight: torch.Tensor | None = None, post_bias: torch.Tensor | None = None, gate: torch.Tensor | None = None,
                  pre_weight: torch.Tensor | None = None, pre_bias: torch.Tensor | None = None, residual_scale: float = 1.0, eps: float = 1e-5, p: float = 0.0,
@@ -388,28 +388,33 @@ class ResidualNorm:
         if not eps >= 0:
             raise ValueError(f"eps: not below 0 expected, got {eps}")
         self._norm, self._scale, self._eps = _NORMS[norm], float(residual_scale), float(eps)
-        self._drop = (_threshold(p), seed & 0xFFFFFFFFFFFFFFFF, _word(layer, "layer"))
+        self._rest = (self._scale, self._eps, _threshold(p), seed & 0xFFFFFFFFFFFFFFFF, _word(layer, "layer"))
         self._tensors = {"post_weight": post_weight, "post_bias": post_bias, "gate": gate, "pre_weight": pre_weight, "pre_bias": pre_bias}
         self.cols = self._index = None
-        self._groups, at = 0, []
         for name, t in self._tensors.items():
-            if t is None:
-                at.append(None)
-                continue
-            if self.cols is None:
+            if t is not None:
                 self.cols, self._index = t.shape[-1] if t.dim() else 0, t.get_device()
                 if self._index < 0:
                     raise ValueError(f"{name}: a CUDA tensor expected: there is no CPU path")
-            if name == "gate":
-                if not 1 <= t.dim() <= 2 or t.shape[-1] != self.cols or not t.numel() or t.dtype is not torch.float32 or not t.is_contiguous() or t.get_device() != self._index:
-                    raise ValueError(f"gate: [cols] or [groups, cols] contiguous float32 values beside the others expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
-                self._groups = t.shape[0] if t.dim() == 2 else 1
-                at.append(t.data_ptr())
-            else:
-                at.append(_floats(t, self.cols, self._index, name))
-        self._params = (at[0], at[1], at[2], self._groups, at[3], at[4], self._scale, self._eps, *self._drop)
+                break
+        self._members()
         self._stream = None if self._index is None else _raw_stream(self._index)
         self._saved = self._saved_on = None
+
+    def _members(self) -> tuple:
+        """The members of ds_norm_args from post_w to layer.  The parameters are looked at in every call: their storage may be another since the last one."""
+        at, groups, cols, index = [], 0, self.cols, self._index
+        for name, t in self._tensors.items():
+            if t is None:
+                at.append(None)
+            elif name == "gate":
+                if not 1 <= t.dim() <= 2 or t.shape[-1] != cols or not t.numel() or t.dtype is not torch.float32 or not t.is_contiguous() or t.get_device() != index:
+                    raise ValueError(f"gate: [cols] or [groups, cols] contiguous float32 values beside the others expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+                groups = t.shape[0] if t.dim() == 2 else 1
+                at.append(t.data_ptr())
+            else:
+                at.append(_floats(t, cols, index, name))
+        return (at[0], at[1], at[2], groups, at[3], at[4], *self._rest)
 
     def _used(self, raw: int, index: int):
         """Tells the allocator of the current stream, on which the parameters are about to be used."""
@@ -437,11 +442,12 @@ class ResidualNorm:
             raise ValueError(f"y: rows of {self.cols} on cuda:{self._index} expected, got {cols} on cuda:{index}")
         if not 0 < cols <= DS_NORM_MAX_COLS:
             raise ValueError(f"y: rows of 1 to {DS_NORM_MAX_COLS} entries expected, got {cols}")
-        if self._groups and rows % self._groups:
-            raise ValueError(f"y: {rows} rows are not {self._groups} equal runs")
         if index != _current():
             with torch.cuda.device(index):
                 return self.forward(y, x, step, training, need_h, h, n)
+        params = self._members()
+        if params[3] and rows % params[3]:
+            raise ValueError(f"y: {rows} rows are not {params[3]} equal runs")
         xp, ldx, sdt, stype = None, 0, dt, dtype
         if x is not None:
             stype = x.dtype
@@ -449,7 +455,7 @@ class ResidualNorm:
                 raise TypeError(f"x: {dtype} or float32 expected, got {stype}")
             x, ldx = _like(x, rows, cols, stype, index, "x")
             xp, sdt = x.data_ptr(), _DTYPES[stype]
-        pre = self._params[4] is not None
+        pre = params[4] is not None
         hp, ldh = None, 0
         if h is not None:
             if x is None and h.dtype is torch.float32:
@@ -485,7 +491,7 @@ class ResidualNorm:
             sp = stats.data_ptr()
             if rows and (hp in (xp, yp) and hp or np_ in (xp, yp) and np_):
                 raise ValueError("a training forward may not write over its inputs")
-        rc = _struct(_norm_at, raw, dt, sdt, rows, cols, self._norm, yp, ldy, xp, ldx, *self._params, _word(step, "step"), sp, hp, ldh, np_, ldn,
+        rc = _struct(_norm_at, raw, dt, sdt, rows, cols, self._norm, yp, ldy, xp, ldx, *params, _word(step, "step"), sp, hp, ldh, np_, ldn,
                      *_NOTHING, (status[1] if status else _dev_status(index)) if cols > _WIDE else None)
         if rc:
             _check(rc, "ds_norm_forward")
@@ -508,13 +514,16 @@ class ResidualNorm:
                 return self.backward(dh, dn, need_dx, out)
         if dh is None and dn is None:
             raise ValueError("the gradient of h or of n expected")
+        params = self._members()
+        if params[3] and rows % params[3]:
+            raise ValueError(f"gate: {rows} rows are not {params[3]} equal runs")
         dhp = dnp = None
         lddh = lddn = 0
         if dh is not None:
             dh, lddh = _like(dh, rows, cols, stype, index, "dh")
             dhp = dh.data_ptr()
         if dn is not None:
-            if self._params[4] is None:
+            if params[4] is None:
                 raise ValueError("dn: there is no pre norm")
             dn, lddn = _like(dn, rows, cols, dtype, index, "dn")
             dnp = dn.data_ptr()
@@ -545,7 +554,7 @@ class ResidualNorm:
         dy, dx = _like_of(y), None
         if x is not None and need_dx:
             dx = _like_of(x)
-        members = [_DTYPES[dtype], _DTYPES[stype], rows, cols, self._norm, y.data_ptr(), ldy, None if x is None else x.data_ptr(), ldx, *self._params, step, stats.data_ptr(),
+        members = [_DTYPES[dtype], _DTYPES[stype], rows, cols, self._norm, y.data_ptr(), ldy, None if x is None else x.data_ptr(), ldx, *params, step, stats.data_ptr(),
                    None, 0, None, 0, dhp, lddh, dnp, lddn, None if dx is None else dx.data_ptr(), cols, dy.data_ptr(), cols, *at,
                    _dev_status(index) if cols > _WIDE else None]
         size = _size(_norm_back_ws, *members)

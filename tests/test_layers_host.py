@@ -1,0 +1,139 @@
+"""What the layers and joints hand to the library and tell the allocator, on a host without a device: tensors that have an address, a type and a place but no memory,
+and calls that are noted instead of made."""
+import types
+
+import pytest
+import torch
+
+from paper_1905_05957_b200 import layer_ops
+from paper_1905_05957_b200.layer_ops import Linear16, ResidualNorm
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+class Tensor:
+    """Rows of consecutive entries at an address of their own."""
+    last = 0x10000
+
+    def __init__(self, *shape, dtype=F32, index=0, owner="caller"):
+        self.shape, self.dtype, self.index, self.owner = torch.Size(shape), dtype, index, owner
+        self.used_on = set()
+        self.renew()
+
+    def renew(self):
+        """Other storage for the same tensor."""
+        Tensor.last += 1 << 24
+        self.address, self.used_on = Tensor.last, set()
+
+    device = property(lambda self: f"cuda:{self.index}")
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def stride(self):
+        return tuple(self.shape[i + 1:].numel() for i in range(len(self.shape)))
+
+    def get_device(self):
+        return self.index
+
+    def is_contiguous(self):
+        return True
+
+    def contiguous(self):
+        return self
+
+    def data_ptr(self):
+        return self.address
+
+    def detach(self):
+        view = Tensor(*self.shape, dtype=self.dtype, index=self.index, owner=self.owner)
+        view.address, view.used_on = self.address, self.used_on      # one storage
+        return view
+
+    def new_empty(self, shape, dtype=None):
+        return Tensor(*((shape,) if isinstance(shape, int) else shape), dtype=dtype or self.dtype, index=self.index, owner="package")
+
+    def record_stream(self, stream):
+        self.used_on.add(stream.name)
+
+
+@pytest.fixture
+def host(monkeypatch):
+    """.calls: (address of the function, stream, members...);  .on(stream): what follows runs there."""
+    h = types.SimpleNamespace(calls=[], stream=0)
+
+    def note(where, stream, *members):
+        h.calls.append((where, stream, members))
+        return 0
+
+    def note_call(where, *args):
+        h.calls.append((where, args[-1], args[:-1]))
+        return 0
+    for name, value in dict(_struct=note, _call=note_call, _size=lambda *a: 0, _slope_ws=lambda r, c: 0, _raw_stream=lambda index: h.stream, _current=lambda: 0,
+                            _status={0: (None, 0)}, _matmul_at="matmul", _slope_at="slope", _pack_at="pack", _norm_at="forward", _norm_back_at="backward",
+                            _like_of=lambda t: Tensor(*t.shape, dtype=t.dtype, index=t.index, owner="package")).items():
+        monkeypatch.setattr(layer_ops, name, value)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda index=None: types.SimpleNamespace(name=h.stream, cuda_stream=h.stream))
+
+    def on(stream):
+        h.stream = stream
+    h.on = on
+    return h
+
+
+def _addresses(call):
+    return [m for m in call[2] if isinstance(m, int) and m > 1 << 24]
+
+
+PARAMETERS = ("post_weight", "post_bias", "gate", "pre_weight", "pre_bias")
+
+
+@pytest.mark.parametrize("name", PARAMETERS)
+def test_a_joint_reads_a_parameter_where_it_is_now(host, name):
+    params = {k: Tensor(64) for k in PARAMETERS}
+    op, y, x = ResidualNorm("layer", **params), Tensor(6, 64), Tensor(6, 64)
+    old = params[name].address
+    op.forward(y, x, training=True)
+    op.backward(x)
+    assert all(old in _addresses(c) for c in host.calls)
+    params[name].renew()
+    del host.calls[:]
+    op.forward(y, x, training=True)
+    op.backward(x)
+    assert len(host.calls) == 2
+    assert all(old not in _addresses(c) and params[name].address in _addresses(c) for c in host.calls)
+
+
+@pytest.mark.parametrize("name", PARAMETERS)
+@pytest.mark.parametrize("change", [dict(shape=torch.Size((60,))), dict(dtype=BF16), dict(index=1)], ids=str)
+def test_a_joint_refuses_a_parameter_that_no_longer_fits(host, name, change):
+    """Its kernels would read, and write gradients, past what is there."""
+    params = {k: Tensor(64) for k in PARAMETERS}
+    op, y = ResidualNorm("layer", **params), Tensor(6, 64)
+    op.forward(y, training=True)
+    for k, v in change.items():
+        setattr(params[name], k, v)
+    del host.calls[:]
+    with pytest.raises(ValueError):
+        op.forward(y)
+    with pytest.raises(ValueError):
+        op.backward(y)
+    assert not host.calls
+
+
+def test_a_joint_counts_the_gates_that_are_there(host):
+    gate = Tensor(2, 64)
+    op, y = ResidualNorm("rms", gate=gate), Tensor(6, 64)
+    op.forward(y, training=True)
+    gate.shape = torch.Size((4, 64))
+    with pytest.raises(ValueError):
+        op.forward(y)                       # six rows are not four runs
+    with pytest.raises(ValueError):
+        op.backward(y)
+    gate.shape = torch.Size((3, 64))
+    del host.calls[:]
+    op.forward(y)
+    assert 3 in host.calls[0][2]
