@@ -188,7 +188,7 @@ class Linear16:
     """A linear layer y = act(x W^T + bias) + residual in 16-bit floats.
 
     W [out, in]: bfloat16 or float16, used where it lies if its rows start on 16-byte boundaries, else copied; or float32 (a slice of a model of the step),
-    copied as `dtype` (bfloat16 unless given).  Call set_weight() after every change of W.  The bias is float32.  forward(x, training=True) keeps x and, with an activation,
+    copied as `dtype` (bfloat16 unless given).  Call set_weight() after every change of W (the layer keeps the memory that W had then, even if W gets other).  The bias is float32.  forward(x, training=True) keeps x and, with an activation,
     x W^T + bias in 16 bits for the gradients."""
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor | None = None, activation: str = "none", dtype: torch.dtype | None = None, stream=None):
@@ -215,6 +215,8 @@ class Linear16:
                 return self.set_weight(weight)
         if weight.dtype is not dtype or not _on_boundary(weight.data_ptr(), ld, r):
             weight, ld = _packed(weight, r, c, ld, dtype, index)
+        else:
+            weight = weight.detach()             # its memory as it is now, whatever becomes of the caller's tensor
         # the weights, perhaps on longer rows, and what backward() reads: x, likewise, and z
         self._w, self._ldw, self.shape, self._index = weight, ld, torch.Size((r, c)), index
         self._x = self._z = None

@@ -137,3 +137,18 @@ def test_a_joint_counts_the_gates_that_are_there(host):
     del host.calls[:]
     op.forward(y)
     assert 3 in host.calls[0][2]
+
+
+def test_a_layer_keeps_the_weights_that_it_was_given(host):
+    """Until set_weight(): a tensor that has other memory or another shape since then is not read by the sizes that it had."""
+    w, x = Tensor(48, 64, dtype=BF16), Tensor(100, 64, dtype=BF16)
+    layer, old = Linear16(w), w.address
+    w.renew()
+    w.shape, w.index = torch.Size((10, 64)), 1
+    layer.forward(x, training=True)
+    layer.backward(Tensor(100, 48, dtype=BF16))
+    assert all(w.address not in _addresses(c) for c in host.calls) and old in _addresses(host.calls[0])
+    w.index = 0
+    layer.set_weight(w)
+    del host.calls[:]
+    assert layer.forward(x).shape == (100, 10) and w.address in _addresses(host.calls[0])
