@@ -261,8 +261,11 @@ class Linear16:
         x, m, c, ldx, _ = _rows(x, "x")
         if c != k:
             raise ValueError(f"x has {c} columns, the weights {k}")
-        if training and m and k and not _on_boundary(x.data_ptr(), ldx, m):      # once, for this product and for the gradient of the weights
-            x, ldx = _packed(x, m, k, ldx, dtype, index)
+        if training:
+            if m and k and not _on_boundary(x.data_ptr(), ldx, m):      # once, for this product and for the gradient of the weights
+                x, ldx = _packed(x, m, k, ldx, dtype, index)
+            else:
+                x = x.detach()                   # its memory as it is now, whatever becomes of the caller's tensor
         y, z = _multiply(x, m, k, ldx, w, n, self._ldw, self.bias, self._act, residual, out_dtype, out, training and self._act != 0, index, raw)
         if training:
             self._x, self._rows_of_x, self._ldx, self._z, self._saved_on = x, m, ldx, z, raw
@@ -498,7 +501,8 @@ class ResidualNorm:
         if rc:
             _check(rc, "ds_norm_forward")
         if training:
-            self._saved, self._saved_on = (y, ldy, x, ldx, stats, step, stype), raw
+            # the memory of y and x as it is now, whatever becomes of the caller's tensors
+            self._saved, self._saved_on = (y.detach(), ldy, None if x is None else x.detach(), ldx, stats, step, stype), raw
         return h, n
 
     def backward(self, dh: torch.Tensor | None = None, dn: torch.Tensor | None = None, need_dx: bool = True, out: dict | None = None, stream=None):

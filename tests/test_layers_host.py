@@ -152,3 +152,20 @@ def test_a_layer_keeps_the_weights_that_it_was_given(host):
     layer.set_weight(w)
     del host.calls[:]
     assert layer.forward(x).shape == (100, 10) and w.address in _addresses(host.calls[0])
+
+
+def test_what_backward_reads_is_what_forward_read(host):
+    """Its memory is kept, with the sizes that it had: the caller's tensors may get other."""
+    layer, op = Linear16(Tensor(48, 64, dtype=BF16)), ResidualNorm("rms", pre_weight=Tensor(64))
+    x, y, r = Tensor(100, 64, dtype=BF16), Tensor(100, 64, dtype=BF16), Tensor(100, 64)
+    layer.forward(x, training=True)
+    op.forward(y, r, training=True)
+    old = [t.address for t in (x, y, r)]
+    for t in (x, y, r):
+        t.renew()
+        t.shape = torch.Size((1, 8))
+    del host.calls[:]
+    layer.backward(Tensor(100, 48, dtype=BF16))
+    dy, dx, _ = op.backward(Tensor(100, 64))
+    seen = {a for c in host.calls for a in _addresses(c)}
+    assert seen >= set(old) and not seen & {x.address, y.address, r.address} and dy.shape == dx.shape == (100, 64)
