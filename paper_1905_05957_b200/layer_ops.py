@@ -104,6 +104,17 @@ def _pitch(cols: int) -> int:
     return (cols + 63) // 64 * 64 or 64
 
 
+_streams: dict = {}          # (device index, handle) -> the stream
+
+
+def _stream_of(index: int, raw: int) -> torch.cuda.Stream:
+    """The current stream, whose handle is raw."""
+    stream = _streams.get((index, raw))
+    if stream is None:
+        stream = _streams[index, raw] = torch.cuda.current_stream(index)
+    return stream
+
+
 def _packed(x: torch.Tensor, r: int, c: int, ld: int, dtype: torch.dtype, index: int) -> tuple[torch.Tensor, int]:
     """A copy of a matrix in 16 bits, on rows of whole lines: [rows, pitch], and the pitch."""
     pitch = _pitch(c)
@@ -213,7 +224,8 @@ class Linear16:
         if index != _current():
             with torch.cuda.device(index):
                 return self.set_weight(weight)
-        if weight.dtype is not dtype or not _on_boundary(weight.data_ptr(), ld, r):
+        packed = weight.dtype is not dtype or not _on_boundary(weight.data_ptr(), ld, r)
+        if packed:
             weight, ld = _packed(weight, r, c, ld, dtype, index)
         else:
             weight = weight.detach()             # its memory as it is now, whatever becomes of the caller's tensor
@@ -221,7 +233,9 @@ class Linear16:
         self._w, self._ldw, self.shape, self._index = weight, ld, torch.Size((r, c)), index
         self._x = self._z = None
         self._rows_of_x = self._ldx = 0
-        self._stream = self._saved_on = _raw_stream(index)      # where the allocator takes the tensors to be in use
+        # where the allocator takes the tensors to be in use; the caller's may belong to any stream
+        self._saved_on = _raw_stream(index)
+        self._stream = self._saved_on if packed else None
 
     @property
     def weight(self) -> torch.Tensor:
@@ -230,16 +244,15 @@ class Linear16:
 
     def _used(self, saved: bool):
         """Tells the allocator of the current stream: dropped before that has run, the layer's memory is kept until it has."""
-        raw = _raw_stream(self._index)
+        index = self._index
+        raw = _raw_stream(index)
         if raw != self._stream:
-            self._w.record_stream(torch.cuda.current_stream(self._index))
-            if self.bias is not None:
-                self.bias.record_stream(torch.cuda.current_stream(self._index))
+            self._w.record_stream(_stream_of(index, raw))
             self._stream = raw
         if saved and raw != self._saved_on:
             for t in (self._x, self._z):
                 if t is not None:
-                    t.record_stream(torch.cuda.current_stream(self._index))
+                    t.record_stream(_stream_of(index, raw))
             self._saved_on = raw
         return raw
 
@@ -266,7 +279,10 @@ class Linear16:
                 x, ldx = _packed(x, m, k, ldx, dtype, index)
             else:
                 x = x.detach()                   # its memory as it is now, whatever becomes of the caller's tensor
+                x.record_stream(_stream_of(index, raw))
         y, z = _multiply(x, m, k, ldx, w, n, self._ldw, self.bias, self._act, residual, out_dtype, out, training and self._act != 0, index, raw)
+        if self.bias is not None:
+            self.bias.record_stream(_stream_of(index, raw))
         if training:
             self._x, self._rows_of_x, self._ldx, self._z, self._saved_on = x, m, ldx, z, raw
         return y
@@ -403,7 +419,6 @@ class ResidualNorm:
                     raise ValueError(f"{name}: a CUDA tensor expected: there is no CPU path")
                 break
         self._members()
-        self._stream = None if self._index is None else _raw_stream(self._index)
         self._saved = self._saved_on = None
 
     def _members(self) -> tuple:
@@ -422,12 +437,10 @@ class ResidualNorm:
         return (at[0], at[1], at[2], groups, at[3], at[4], *self._rest)
 
     def _used(self, raw: int, index: int):
-        """Tells the allocator of the current stream, on which the parameters are about to be used."""
-        if self._stream is not None:
-            for t in self._tensors.values():
-                if t is not None:
-                    t.record_stream(torch.cuda.current_stream(index))
-        self._stream = raw
+        """Tells the allocator of the current stream, on which the parameters are used: they may belong to any, and their storage may be another than at the last call."""
+        for t in self._tensors.values():
+            if t is not None:
+                t.record_stream(_stream_of(index, raw))
 
     def forward(self, y: torch.Tensor, x: torch.Tensor | None = None, step: int = 0, training: bool = False, need_h: bool = True, h: torch.Tensor | None = None,
                 n: torch.Tensor | None = None, stream=None):
@@ -487,8 +500,7 @@ class ResidualNorm:
                 ldn = _given(n, rows, cols, index, "n")
             np_ = n.data_ptr()
         raw = _raw_stream(index)
-        if raw != self._stream:
-            self._used(raw, index)
+        self._used(raw, index)
         stats = sp = None
         yp, status = y.data_ptr(), _status.get(index)
         if training:
@@ -502,7 +514,11 @@ class ResidualNorm:
             _check(rc, "ds_norm_forward")
         if training:
             # the memory of y and x as it is now, whatever becomes of the caller's tensors
-            self._saved, self._saved_on = (y.detach(), ldy, None if x is None else x.detach(), ldx, stats, step, stype), raw
+            y, x = y.detach(), None if x is None else x.detach()
+            for t in (y, x):
+                if t is not None:
+                    t.record_stream(_stream_of(index, raw))
+            self._saved, self._saved_on = (y, ldy, x, ldx, stats, step, stype), raw
         return h, n
 
     def backward(self, dh: torch.Tensor | None = None, dn: torch.Tensor | None = None, need_dx: bool = True, out: dict | None = None, stream=None):
@@ -550,12 +566,11 @@ class ResidualNorm:
         if out and any(name not in self._tensors for name in out):
             raise ValueError(f"out: parameters are {', '.join(self._tensors)}")
         raw = _raw_stream(index)
-        if raw != self._stream:
-            self._used(raw, index)
+        self._used(raw, index)
         if raw != self._saved_on:             # what was kept is dropped at the earliest when this stream is done with it
             for t in (y, x, stats):
                 if t is not None:
-                    t.record_stream(torch.cuda.current_stream(index))
+                    t.record_stream(_stream_of(index, raw))
             self._saved_on = raw
         dy, dx = _like_of(y), None
         if x is not None and need_dx:

@@ -1,8 +1,8 @@
-"""Memory that layers and joints use without owning it: parameters whose storage is replaced between calls."""
+"""Memory that layers and joints use without owning it: parameters whose storage is replaced between calls, and tensors that belong to another stream than the one that uses them."""
 import pytest
 import torch
 
-from paper_1905_05957_b200 import ResidualNorm
+from paper_1905_05957_b200 import Linear16, ResidualNorm
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,42 @@ def test_a_joint_whose_parameters_get_other_storage(groups):
         op.forward(y, x)
     with pytest.raises(ValueError):
         op.backward(dh, dn)
+
+
+@pytest.mark.parametrize("dropped", ["object", "next forward"])
+def test_tensors_of_another_stream(dropped):
+    """Weights, parameters and inputs that belong to the main stream, all used on a late side stream alone, then dropped here: what is allocated here next must not be theirs."""
+    rows, width = 600, 512
+    x, dy = _normal(rows, width, seed=1, dtype=torch.bfloat16), _normal(rows, width, seed=2, dtype=torch.bfloat16)
+    w, v = _normal(width, width, seed=3, dtype=torch.bfloat16, scale=width ** -0.5), 1 + _normal(width, seed=4, scale=0.1)
+
+    def make(stream):
+        with torch.cuda.stream(torch.cuda.current_stream() if stream is None else stream):
+            layer, joint = Linear16(own[0], own[1], "gelu"), ResidualNorm("layer", post_weight=own[2], pre_weight=own[3])
+            return layer, joint, layer.forward(own[4], training=True), *joint.forward(own[5], own[6], training=True)
+
+    def copies():
+        return [t.clone() for t in (w, v, v, v, x, x, dy)]
+    own = copies()
+    layer, joint, *want = make(None)
+    want += [*layer.backward(dy), *joint.backward(dy, dy)[:2]]
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        own = copies()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        layer, joint, *got = make(side)
+        with torch.cuda.stream(side):
+            got += [*layer.backward(dy), *joint.backward(dy, dy)[:2]]
+            if dropped == "next forward":
+                layer.forward(x, training=True)
+                joint.forward(x, dy, training=True)
+        del own
+        if dropped == "object":
+            del layer, joint
+        junk = [torch.full((rows, width), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(20)]
+        junk += [torch.full((width,), float("nan"), device="cuda") for _ in range(20)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del junk

@@ -76,6 +76,7 @@ def host(monkeypatch):
                             _status={0: (None, 0)}, _matmul_at="matmul", _slope_at="slope", _pack_at="pack", _norm_at="forward", _norm_back_at="backward",
                             _like_of=lambda t: Tensor(*t.shape, dtype=t.dtype, index=t.index, owner="package")).items():
         monkeypatch.setattr(layer_ops, name, value)
+    monkeypatch.setattr(layer_ops, "_streams", {}, raising=False)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda index=None: types.SimpleNamespace(name=h.stream, cuda_stream=h.stream))
 
     def on(stream):
@@ -169,3 +170,42 @@ def test_what_backward_reads_is_what_forward_read(host):
     dy, dx, _ = op.backward(Tensor(100, 64))
     seen = {a for c in host.calls for a in _addresses(c)}
     assert seen >= set(old) and not seen & {x.address, y.address, r.address} and dy.shape == dx.shape == (100, 64)
+
+
+def test_the_allocator_is_told_where_a_layer_uses_what_it_was_given(host):
+    """Memory that belongs to another stream, used on one stream alone and dropped: the tensors may belong to any stream, so it is told of that one."""
+    host.on(7)
+    w, b, x = Tensor(48, 64, dtype=BF16), Tensor(48), Tensor(100, 64, dtype=BF16)
+    layer = Linear16(w, b, "gelu")
+    layer.forward(x, training=True)
+    layer.backward(Tensor(100, 48, dtype=BF16))
+    assert w.used_on == b.used_on == x.used_on == {7}
+    layer.bias = other = Tensor(48)
+    layer.forward(x)
+    assert other.used_on == {7}
+    host.on(8)
+    layer.forward(x)
+    assert w.used_on == b.used_on | {8} == other.used_on and x.used_on == {7}      # x: no training, the caller's alone
+    layer.backward(Tensor(100, 48, dtype=BF16))
+    assert x.used_on == {7, 8}
+    host.on(9)
+    layer = Linear16(Tensor(48, 64), b)           # the weights are a copy of this stream's own
+    layer.forward(x)
+    assert b.used_on == {7, 9}
+
+
+def test_the_allocator_is_told_where_a_joint_uses_what_it_was_given(host):
+    host.on(7)
+    params = {k: Tensor(64) for k in PARAMETERS}
+    op, y, x = ResidualNorm("layer", **params), Tensor(6, 64), Tensor(6, 64)
+    op.forward(y, x)
+    assert all(t.used_on == {7} for t in params.values()) and not y.used_on and not x.used_on
+    op.forward(y, x, training=True)
+    assert y.used_on == x.used_on == {7}
+    host.on(8)
+    op.backward(x)
+    assert all(t.used_on == {7, 8} for t in (y, x, *params.values()))
+    for t in params.values():
+        t.renew()
+    op.backward(x)                                # other storage, the stream of the last call
+    assert all(t.used_on == {8} for t in params.values())
