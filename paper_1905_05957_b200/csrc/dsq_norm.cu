@@ -854,6 +854,14 @@ int check(const ds_norm_args* p, bool back) {
   return DS_OK;
 }
 
+struct Parameters {
+  Span all[5];
+};
+Parameters parameters(const ds_norm_args* p) {
+  auto vector = [&](const float* v, uint64_t n) { return span(v, 1, n, 0, 4); };
+  return {{vector(p->post_w, p->cols), vector(p->post_b, p->cols), vector(p->pre_w, p->cols), vector(p->pre_b, p->cols), vector(p->gate, p->groups * p->cols)}};
+}
+
 NormParams params(const ds_norm_args* p, bool back) {
   NormParams q{};
   q.post_w = p->post_w, q.post_b = p->post_b, q.gate = p->gate, q.pre_w = p->pre_w, q.pre_b = p->pre_b;
@@ -892,6 +900,8 @@ int ds_norm_forward(const ds_norm_args* p, void* cuda_stream) {
       (overlap(n, x) && !over(p->n, p->ldn, sy, p->x, p->ldx, sx)) || (overlap(n, y) && !over(p->n, p->ldn, sy, p->y, p->ldy, sy)) || overlap(h, n) ||
       overlap(stats, h) || overlap(stats, n) || overlap(stats, x) || overlap(stats, y))
     return DS_ERR_INVALID_ARG;
+  for (const Span& v : parameters(p).all)      // read by every CTA, whenever it comes to them
+    if (overlap(h, v) || overlap(n, v) || overlap(stats, v)) return DS_ERR_INVALID_ARG;
   const NormParams q = params(p, false);
   const NormPlan b = norm_plan(p);
   const cudaError_t e = by_types(p, [&](auto sx_, auto sy_) { return forward<decltype(sx_), decltype(sy_)>(q, b, static_cast<cudaStream_t>(cuda_stream)); });
@@ -937,7 +947,10 @@ int ds_norm_backward(const ds_norm_args* p, void* cuda_stream) {
   }
   if (overlap(to[0].r, to[1].r)) return DS_ERR_INVALID_ARG;
   const Span space = span(p->workspace, 1, ws, 0, 1);
-  const float* weights[] = {p->post_w, p->post_b, p->pre_w, p->pre_b, p->gate};
+  const Parameters weights = parameters(p);
+  for (auto& t : to)
+    for (const Span& v : weights.all)
+      if (overlap(t.r, v)) return DS_ERR_INVALID_ARG;
   Span small[6];
   int n = 0;
   for (auto& o : outs) small[n++] = span(o.to, 1, o.n, 0, 4);
@@ -949,8 +962,8 @@ int ds_norm_backward(const ds_norm_args* p, void* cuda_stream) {
       if (overlap(small[i], r)) return DS_ERR_INVALID_ARG;
     for (auto& t : to)
       if (overlap(small[i], t.r)) return DS_ERR_INVALID_ARG;
-    for (int j = 0; j < 5; ++j)
-      if (overlap(small[i], span(weights[j], 1, j == 4 ? p->groups * p->cols : p->cols, 0, 4))) return DS_ERR_INVALID_ARG;
+    for (const Span& v : weights.all)
+      if (overlap(small[i], v)) return DS_ERR_INVALID_ARG;
   }
   NormParams q = params(p, true);
   uint8_t* space_p = static_cast<uint8_t*>(p->workspace);

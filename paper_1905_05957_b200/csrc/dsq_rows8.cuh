@@ -13,7 +13,7 @@
 namespace dsq {
 
 // Whether the rows of two matrices share memory: `rows` of `bytes` bytes, `ld` apart.  Rows that lie side by side in wider ones
-// (columns of one buffer) do not.
+// (columns of one buffer) do not, nor does a single row (whose ld is not read) between wider ones.
 struct Span {
   uintptr_t p;
   uint64_t rows, bytes, ld;
@@ -22,11 +22,12 @@ inline Span span(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, uint3
   return {reinterpret_cast<uintptr_t>(p), rows, cols * size, ld * size};
 }
 inline bool overlap(const Span& a, const Span& b) {
+  if (b.rows == 1 && a.rows != 1) return overlap(b, a);
   if (!a.p || !b.p || !a.rows || !b.rows || !a.bytes || !b.bytes) return false;
   if (a.p >= b.p + (b.rows - 1) * b.ld + b.bytes || b.p >= a.p + (a.rows - 1) * a.ld + a.bytes) return false;
-  if (a.ld != b.ld || !a.ld) return true;
-  const uint64_t off = a.p >= b.p ? (a.p - b.p) % a.ld : (a.ld - (b.p - a.p) % a.ld) % a.ld;      // of a's row within b's rows
-  return off < b.bytes || off + a.bytes > a.ld;
+  if (b.rows == 1 || !b.ld || (a.rows != 1 && a.ld != b.ld)) return true;
+  const uint64_t off = a.p >= b.p ? (a.p - b.p) % b.ld : (b.ld - (b.p - a.p) % b.ld) % b.ld;      // of a's row within b's rows
+  return off < b.bytes || off + a.bytes > b.ld;
 }
 
 template <class T>

@@ -147,6 +147,19 @@ def test_backward_refusals(lib, kw, code):
     assert lib.ds_norm_backward(C.byref(_args(b.ds_norm_args, BACKWARD, **kw)), None) == code
 
 
+VECTORS = dict(post_w=20 * FAR, post_b=21 * FAR, gate=22 * FAR, pre_w=23 * FAR, pre_b=24 * FAR)
+
+
+@pytest.mark.parametrize("name", VECTORS)
+def test_outputs_over_parameters_are_refused(lib, name):
+    """CTAs read them at times of their own: an output there would be read by some of them."""
+    at = VECTORS[name] + 4 * 16
+    for out in ("h", "n", "stats"):
+        assert lib.ds_norm_forward(C.byref(_args(b.ds_norm_args, FORWARD, **VECTORS, **{out: at})), None) == INVALID
+    for out in ("dx", "dy"):
+        assert lib.ds_norm_backward(C.byref(_args(b.ds_norm_args, BACKWARD, **VECTORS, **{out: at})), None) == INVALID
+
+
 def test_backward_workspace(lib):
     """Sums of each CTA, for each parameter whose gradient is wanted, and of each unit of a gate's rows; none that nothing asks for."""
     def size(**kw):

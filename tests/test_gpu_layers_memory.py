@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_1905_05957_b200 import Linear16, ResidualNorm
+from paper_1905_05957_b200 import DsqError, Linear16, ResidualNorm
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +76,19 @@ def test_tensors_of_another_stream(dropped):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         del junk
+
+
+def test_parameters_between_wider_rows():
+    """A vector in the columns that the rows of an output leave free shares no memory with it; one in its rows does."""
+    rows, cols = 9, 64
+    buf = torch.zeros(rows, 2 * cols, device="cuda")
+    h, w = buf[:, :cols], buf[3, cols:]
+    w.copy_(1 + _normal(cols, seed=1))
+    y, x = _normal(rows, cols, seed=2), _normal(rows, cols, seed=3)
+    want = ResidualNorm("layer", post_weight=w.clone()).forward(y, x)[0]
+    op = ResidualNorm("layer", post_weight=w)
+    op.forward(y, x, h=h)
+    assert torch.equal(h, want)
+    for at in (0, 5, cols - 1):
+        with pytest.raises(DsqError):
+            ResidualNorm("layer", post_weight=buf[3, at:at + cols]).forward(y, x, h=h)
