@@ -446,7 +446,7 @@ int ds_f16_matmul(const ds_f16_product* p, void* cuda_stream) {
   const Span out = span(p->out, p->m, p->n, p->ldo, size_of(p->out_dtype)), z = span(p->z, p->m, p->n, p->ldz, 2),
              res = span(p->residual, p->m, p->n, p->ldr, 2), bias = span(p->bias, 1, p->n, p->n, 4);
   // the residual may be added to in place
-  const bool in_place = p->residual == p->out && p->ldr == p->ldo && p->out_dtype != DS_F32;
+  const bool in_place = p->residual == p->out && (p->ldr == p->ldo || p->m == 1) && p->out_dtype != DS_F32;
   if (overlap(out, z) || overlap(res, z) || (!in_place && overlap(out, res)) || overlap(out, bias) || overlap(z, bias)) return DS_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const Out16 o{p->bias, static_cast<const uint16_t*>(p->residual), static_cast<uint16_t*>(p->z), p->out, p->ldr, p->ldz, p->ldo, (uint32_t)p->m, (uint32_t)p->n,
@@ -507,8 +507,8 @@ int ds_f16_slope(const ds_f16_slope_args* p, void* cuda_stream) {
   const Span dy = span(p->dy, p->rows, p->cols, p->lddy, 2), z = span(p->z, p->rows, p->cols, p->ldz, 2), dz = span(p->dz, p->rows, p->cols, p->lddz, 2),
              sum = span(p->sum, 1, p->cols, p->cols, p->sum ? size_of(p->sum_dtype) : 0);
   // in place over dy or z, entry by entry
-  if ((overlap(dz, dy) && !(p->dz == p->dy && p->lddz == p->lddy)) || (overlap(dz, z) && !(p->dz == p->z && p->lddz == p->ldz)) || overlap(sum, dz) ||
-      overlap(sum, dy) || overlap(sum, z))
+  auto itself = [&](const void* q, uint64_t ld) { return p->dz == q && (p->lddz == ld || p->rows == 1); };
+  if ((overlap(dz, dy) && !itself(p->dy, p->lddy)) || (overlap(dz, z) && !itself(p->z, p->ldz)) || overlap(sum, dz) || overlap(sum, dy) || overlap(sum, z))
     return DS_ERR_INVALID_ARG;
   float* sums = nullptr;
   if (p->sum) {

@@ -147,6 +147,16 @@ def test_backward_refusals(lib, kw, code):
     assert lib.ds_norm_backward(C.byref(_args(b.ds_norm_args, BACKWARD, **kw)), None) == code
 
 
+def test_the_pitch_of_a_single_row_is_not_read(lib):
+    """In place over the residual, dy or z whatever it is: what is refused is the misaligned address that is looked at after that."""
+    one = dict(m=1, residual=FAR, ldr=7, ldo=24, a=P + 1)
+    assert lib.ds_f16_matmul(C.byref(_args(b.ds_f16_product, PRODUCT, **one)), None) == ALIGN
+    assert lib.ds_f16_matmul(C.byref(_args(b.ds_f16_product, PRODUCT, **dict(one, residual=FAR + 16))), None) == INVALID
+    for kw in (dict(dz=P, lddz=7), dict(dz=FAR, lddz=0)):
+        assert lib.ds_f16_slope(C.byref(_args(b.ds_f16_slope_args, SLOPE, rows=1, workspace=4 * FAR + 8, **kw)), None) == ALIGN
+    assert lib.ds_f16_slope(C.byref(_args(b.ds_f16_slope_args, SLOPE, rows=1, workspace=4 * FAR + 8, dz=P + 64)), None) == INVALID
+
+
 VECTORS = dict(post_w=20 * FAR, post_b=21 * FAR, gate=22 * FAR, pre_w=23 * FAR, pre_b=24 * FAR)
 
 

@@ -1,8 +1,10 @@
 """Memory that layers and joints use without owning it: parameters whose storage is replaced between calls, and tensors that belong to another stream than the one that uses them."""
+import ctypes as C
+
 import pytest
 import torch
 
-from paper_1905_05957_b200 import DsqError, Linear16, ResidualNorm
+from paper_1905_05957_b200 import DsqError, Linear16, ResidualNorm, binding, linear16
 
 pytestmark = pytest.mark.gpu
 
@@ -76,6 +78,25 @@ def test_tensors_of_another_stream(dropped):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         del junk
+
+
+def test_single_rows_in_place_whatever_their_pitches():
+    """Through the C ABI, which takes pitches that the Python calls work out: of one row they mean nothing."""
+    lib = binding.load_library()
+    x, w, r = (_normal(*s, seed=i, dtype=torch.bfloat16) for i, s in enumerate(((1, 64), (48, 64), (1, 48))))
+    want, out = linear16(x, w, residual=r), r.clone()
+    p = binding.ds_f16_product(dtype=binding.DS_BF16, m=1, n=48, k=64, a=x.data_ptr(), lda=3, b=w.data_ptr(), ldb=64, residual=out.data_ptr(), ldr=5, out=out.data_ptr(),
+                               out_dtype=binding.DS_BF16, ldo=9)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.ds_f16_matmul(C.byref(p), stream) == binding.DS_OK
+    assert torch.equal(out, want)
+    dy, z = _normal(1, 48, seed=3, dtype=torch.bfloat16), _normal(1, 48, seed=4, dtype=torch.bfloat16)
+    want = torch.where(z > 0, dy, torch.zeros_like(dy))
+    for over in (dy.clone(), z.clone()):
+        given = [over if torch.equal(over, t) else t for t in (dy, z)]
+        p = binding.ds_f16_slope_args(dtype=binding.DS_BF16, rows=1, cols=48, dy=given[0].data_ptr(), lddy=2, z=given[1].data_ptr(), ldz=3, activation=1, dz=over.data_ptr(), lddz=5)
+        assert lib.ds_f16_slope(C.byref(p), stream) == binding.DS_OK
+        assert torch.equal(over, want)
 
 
 def test_parameters_between_wider_rows():
