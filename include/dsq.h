@@ -518,7 +518,9 @@ int ds_f16_pack(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t
  *   ds_norm_forward writes h and / or n, and for the backward pass stats ([rows, 4] floats, 16-byte aligned; may be NULL).  h and n may each be x or y itself, of one type and pitch.
  *   ds_norm_backward: from dh and / or dn (the gradients of h and n) those of x, y and the parameters; each is wanted where its pointer is not NULL.  y, x and the
  *   parameters as the forward pass had them, stats as it left them.  dx and dy may be one of the inputs of their type and pitch.  workspace: ds_norm_backward_workspace bytes, 16-byte aligned.
- *   Rows that hold an inf or a NaN are NaN and their parameters' gradients with them; other rows are not touched by them.
+ *   Infs and NaNs go through these formulas and stay in their rows; in gradients of parameters they reach the columns of which a term is one.  A NaN makes a normalised row NaN, and so does
+ *   an inf in a layer norm.  In an RMS norm an inf makes r 0: its own entry becomes NaN, the others 0 (post_b, pre_b); the gradient of what is normalised is NaN all along the row.  Finite
+ *   rows whose squares (of layer norms: about the mean) sum to more than 32 bits hold, 3.4e38, have r = 0 as well and come out as 0.  Without a norm an entry touches itself alone.
  *   cols <= DS_NORM_MAX_COLS, rows less than 2^30 entries apart, else DS_ERR_UNSUPPORTED.  dev_status may be NULL (DS_DEV_NORM_TIMEOUT).
  */
 #define DS_NORM_MAX_COLS 32768u

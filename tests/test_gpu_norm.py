@@ -286,6 +286,61 @@ def test_rows_do_not_touch_one_another():
     assert bool(got[1][7].isnan().all()) and bool(got[1][9].isnan().all()) and bool(got[2][11].isnan().all())
 
 
+def _formula(y, x, params, norm, eps=1e-5):
+    """h and n by the formulas in 32 bits, with what they make of infs and NaNs."""
+    def normed(v, which):
+        c = v - v.mean(1, keepdim=True) if norm == "layer" else v
+        return c * (c.square().mean(1, keepdim=True) + eps).rsqrt() * params[which + "_weight"] + params.get(which + "_bias", 0.0)
+    h = x + (normed(y, "post") if "post_weight" in params else y) * params["gate"]
+    return h, normed(h, "pre") if "pre_weight" in params else None
+
+
+@pytest.mark.parametrize("biases", [False, True])
+@pytest.mark.parametrize("post,pre", [(True, True), (True, False), (False, True), (False, False)])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_what_infs_nans_and_large_rows_become(norm, post, pre, biases):
+    """Each follows the formulas, in its row, and in the parameters' gradients in the columns of which a term is one; other rows are as they were."""
+    rows, cols = 24, 300
+    params = _params(cols, norm, post, pre, 1, biases)
+    y, x, dh = (_normal((rows, cols), s) for s in (1, 2, 3))
+    dn = _normal((rows, cols), 4) if pre else None
+    op = ResidualNorm(norm, **params)
+    clean = [t for t in (*op.forward(y, x, training=True), *op.backward(dh, dn)[:2]) if t is not None]
+    y[3, 100], y[5, 7], x[8, 299], x[10, 0] = float("nan"), float("inf"), float("-inf"), float("nan")
+    y[12], x[13] = 1e19 * torch.sign(y[12]) * (1 + y[12].abs()), 1e19 * torch.sign(x[13]) * (1 + x[13].abs())      # squares sum to 3e40 and more
+    touched = [3, 5, 8, 10, 12, 13]
+    h, n = op.forward(y, x, training=True)
+    for got, want in zip((h, n), _formula(y, x, params, norm)):
+        if got is None:
+            continue
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+        ok = want.isfinite()
+        assert bool(((got - want).abs()[ok] <= 2.0 ** -14 * (1 + want.abs()[ok])).all())
+    dy, dx, grads = op.backward(dh, dn)
+    rest = [r for r in range(rows) if r not in touched]
+    assert all(torch.equal(a[rest], b[rest]) for a, b in zip([t for t in (h, n, dy, dx) if t is not None], clean))
+    if post:
+        assert bool(dy[3].isnan().all()) and bool(dy[5].isnan().all()) and bool(h[12].isfinite().all())
+        assert bool(grads["post_weight"].isnan().all())
+        if norm == "rms":      # the finite entries of a row with an inf are 0
+            assert bool(h[5, :7].eq(x[5, :7]).all()) != biases
+    if not post and not pre:
+        assert int(h.isnan().sum()) == 2 and int(h.isinf().sum()) == 2 and bool(dy.isfinite().all()) and int((~grads["gate"].isfinite()).sum()) == 2
+
+
+def test_gradients_of_an_rms_norm_with_an_inf():
+    """The finite entries of its row are 0 and add 0: one column alone is NaN."""
+    w = torch.ones(300, device="cuda")
+    y, dh = _normal((24, 300), 1), _normal((24, 300), 2)
+    y[5, 7] = float("inf")
+    op = ResidualNorm("rms", post_weight=w)
+    op.forward(y, training=True)
+    assert op.backward(dh)[2]["post_weight"].isnan().nonzero().flatten().tolist() == [7]
+    op = ResidualNorm("rms", pre_weight=w)
+    op.forward(y, training=True)
+    assert op.backward(dn=dh)[2]["pre_weight"].isnan().nonzero().flatten().tolist() == [7]
+
+
 def test_rows_of_zeros_and_large_means():
     op = ResidualNorm("layer", post_weight=torch.ones(512, device="cuda"), eps=1e-5)
     y = torch.zeros(4, 512, device="cuda")
