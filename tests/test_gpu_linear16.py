@@ -183,6 +183,34 @@ def test_gradients_agree_with_differences(act):
         assert abs(float((grad.double() * way).sum()) - want) <= float(terms) * 2.0 ** -9      # halves of fp16: z, dz and dx rounded by 2^-11 each
 
 
+@pytest.mark.parametrize("m,n", [(1, 1000), (12, 1000), (40, 1000), (200, 1000), (200, 1001)])      # the forms of the product
+@pytest.mark.parametrize("dtype", HALVES)
+def test_gelu_to_a_fraction_of_itself(m, n, dtype):
+    """Down the negative tail, too, where gelu is small: z comes as the bias and is exact.  Phi is good to 2^-19 (its fit 2^-22.9, a reciprocal and a power of two a few units of 2^-23, a
+    dozen operations of 2^-24), and z^2 / 2 in the exponent is off by two roundings and a constant's, 2^-23 of itself."""
+    z = torch.linspace(-12.9, 9.0, n, device="cuda")
+    z8 = z.double()
+    want = 0.5 * z8 * torch.erfc(-z8 * 0.5 ** 0.5)
+    off = want.abs() * (2.0 ** -19 + z8.square() * 2.0 ** -24)
+    x, w = torch.zeros(m, 64, dtype=dtype, device="cuda"), torch.zeros(n, 64, dtype=dtype, device="cuda")
+    assert bool(((linear16(x, w, z, "gelu", out_dtype=torch.float32).double() - want).abs() <= off).all())
+    tiny = 2.0 ** -25 if dtype is torch.float16 else 0.0
+    assert bool(((linear16(x, w, z, "gelu").double() - want).abs() <= 1.001 * off + torch.finfo(dtype).eps / 2 * want.abs() + tiny).all())
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+def test_the_slope_of_gelu_to_a_fraction_of_its_terms(dtype):
+    """Phi(z) + z phi(z), as the gradient of the bias of a single token in 32 bits; the same errors of either term.  z is kept in 16 bits: whole multiples of 2^-4 are exact."""
+    z = torch.arange(-206, 144, device="cuda").float() / 16
+    n = z.numel()
+    layer = Linear16(torch.zeros(n, 64, dtype=dtype, device="cuda"), z, "gelu")
+    layer.forward(torch.zeros(1, 64, dtype=dtype, device="cuda"), training=True)
+    _, _, db = layer.backward(torch.ones(1, n, dtype=dtype, device="cuda"), grad_dtype=torch.float32)
+    z8 = z.double()
+    phi, tail = 0.5 * torch.erfc(-z8 * 0.5 ** 0.5), z8 * torch.exp(-0.5 * z8.square()) * (2 * torch.pi) ** -0.5
+    assert bool(((db.double() - (phi + tail)).abs() <= (phi + tail.abs()) * (2.0 ** -19 + z8.square() * 2.0 ** -24)).all())
+
+
 @pytest.mark.parametrize("act", ["none", "gelu", "silu", "relu", "gelu_tanh"])
 @pytest.mark.parametrize("m", [4, 40, 200])
 def test_no_inner_entries(act, m):
