@@ -20,6 +20,7 @@ _HALVES = {torch.bfloat16: _DTYPES[torch.bfloat16], torch.float16: _DTYPES[torch
 _NORMS = {"rms": DS_NORM_RMS, "layer": DS_NORM_LAYER}
 _like_of = torch.empty_like
 _WIDE = 4096                 # columns above which a row's parts wait for one another
+_SLOPE_ROWS = 2097120        # rows that the gradient through an activation, or a bias's, takes at most
 _NOTHING = (None,) * 13      # the members of ds_norm_args that the forward pass does not read
 _call = _struct = _size = _matmul_at = _matmul_ws = _slope_at = _slope_ws = _pack_at = _norm_at = _norm_back_at = _norm_back_ws = _dropout_at = None
 
@@ -200,7 +201,7 @@ class Linear16:
 
     W [out, in]: bfloat16 or float16, used where it lies if its rows start on 16-byte boundaries, else copied; or float32 (a slice of a model of the step),
     copied as `dtype` (bfloat16 unless given).  Call set_weight() after every change of W (the layer keeps the memory that W had then, even if W gets other).  The bias is float32.  forward(x, training=True) keeps x and, with an activation,
-    x W^T + bias in 16 bits for the gradients."""
+    x W^T + bias in 16 bits for the gradients; with an activation or a bias it takes up to 2097120 tokens."""
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor | None = None, activation: str = "none", dtype: torch.dtype | None = None, stream=None):
         self.activation, self._act = activation, _activation(activation)
@@ -274,6 +275,8 @@ class Linear16:
         x, m, c, ldx, _ = _rows(x, "x")
         if c != k:
             raise ValueError(f"x has {c} columns, the weights {k}")
+        if training and m > _SLOPE_ROWS and (self._act or self.bias is not None):
+            raise ValueError(f"x: at most {_SLOPE_ROWS} rows expected in training with an activation or a bias, got {m}")
         if training:
             if m and k and not _on_boundary(x.data_ptr(), ldx, m):      # once, for this product and for the gradient of the weights
                 x, ldx = _packed(x, m, k, ldx, dtype, index)

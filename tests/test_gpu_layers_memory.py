@@ -113,3 +113,16 @@ def test_parameters_between_wider_rows():
     for at in (0, 5, cols - 1):
         with pytest.raises(DsqError):
             ResidualNorm("layer", post_weight=buf[3, at:at + cols]).forward(y, x, h=h)
+
+
+def test_as_many_tokens_as_a_layer_trains_on():
+    """Whole numbers whose sums are exact."""
+    m = 2097120
+    x, w = torch.ones(m, 8, dtype=torch.bfloat16, device="cuda"), torch.ones(16, 8, dtype=torch.bfloat16, device="cuda")
+    x[-1] = 2
+    layer = Linear16(w, torch.zeros(16, device="cuda"), "relu")
+    assert bool((layer.forward(x, training=True)[-1] == 16).all())
+    dx, dw, db = layer.backward(x.repeat(1, 2), grad_dtype=torch.float32)
+    assert bool((dx[:-1] == 16).all()) and bool((dx[-1] == 32).all()) and bool((dw == m - 1 + 4).all()) and bool((db == m - 1 + 2).all())
+    with pytest.raises(ValueError):
+        layer.forward(torch.ones(m + 1, 8, dtype=torch.bfloat16, device="cuda"), training=True)

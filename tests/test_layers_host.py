@@ -209,3 +209,17 @@ def test_the_allocator_is_told_where_a_joint_uses_what_it_was_given(host):
         t.renew()
     op.backward(x)                                # other storage, the stream of the last call
     assert all(t.used_on == {8} for t in params.values())
+
+
+def test_more_tokens_than_backward_takes_are_refused_forward(host):
+    """2097120, where the column sums and slopes are taken; nothing is launched."""
+    w, b = Tensor(16, 8, dtype=BF16), Tensor(16)
+    x = Tensor(2097121, 8, dtype=BF16)
+    for layer in (Linear16(w, b), Linear16(w, activation="relu")):
+        with pytest.raises(ValueError):
+            layer.forward(x, training=True)
+        assert not host.calls
+        layer.forward(x)
+        layer.forward(Tensor(2097120, 8, dtype=BF16), training=True)
+        del host.calls[:]
+    Linear16(w).forward(x, training=True)
