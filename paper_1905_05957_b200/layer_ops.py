@@ -14,7 +14,7 @@ import torch
 from . import matrix_ops as _m
 from .binding import (ACTIVATIONS, DS_F16_FORWARD, DS_F16_INPUTS, DS_F16_WEIGHTS, DS_F32, DS_NORM_LAYER, DS_NORM_MAX_COLS, DS_NORM_RMS,
                       fast_call, fast_struct_call, load_library)
-from .matrix_ops import _DTYPES, _check, _current, _dev_status, _raw_stream, _status
+from .matrix_ops import _DTYPES, _check, _current, _dev_status, _raw_stream, _status, _stream_of
 
 _HALVES = {torch.bfloat16: _DTYPES[torch.bfloat16], torch.float16: _DTYPES[torch.float16]}
 _NORMS = {"rms": DS_NORM_RMS, "layer": DS_NORM_LAYER}
@@ -103,17 +103,6 @@ def _pitch(cols: int) -> int:
     """Entries between the rows of what the products' operands are copied to: whole lines of 128 bytes (rows that start on other boundaries of 16 bytes span a line more:
     4096 x 4096 x 4104 takes 114 us so, and 88 on lines)."""
     return (cols + 63) // 64 * 64 or 64
-
-
-_streams: dict = {}          # (device index, handle) -> the stream
-
-
-def _stream_of(index: int, raw: int) -> torch.cuda.Stream:
-    """The current stream, whose handle is raw."""
-    stream = _streams.get((index, raw))
-    if stream is None:
-        stream = _streams[index, raw] = torch.cuda.current_stream(index)
-    return stream
 
 
 def _packed(x: torch.Tensor, r: int, c: int, ld: int, dtype: torch.dtype, index: int) -> tuple[torch.Tensor, int]:

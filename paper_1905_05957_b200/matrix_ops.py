@@ -70,6 +70,17 @@ def _vector(v: torch.Tensor | None, n: int, what: str, device) -> int | None:
     return v.data_ptr()
 
 
+_streams: dict = {}    # (device index, handle) -> the stream
+
+
+def _stream_of(index: int, raw: int) -> torch.cuda.Stream:
+    """The current stream, whose handle is raw."""
+    stream = _streams.get((index, raw))
+    if stream is None:
+        stream = _streams[index, raw] = torch.cuda.current_stream(index)
+    return stream
+
+
 _status: dict = {}     # device index -> (word in which products report waits that ran out, its address)
 
 
@@ -113,7 +124,7 @@ class Int8Matrix:
         self.rows, self.cols, self.device = r, c, device
         self.ld = ld if r > 1 else (c + 15) // 16 * 16
         self._codes, self._scale = codes, scale
-        self.stream = _raw_stream(device.index)      # the last one on which the allocator takes the memory to be in use
+        self.stream = None                           # the last one on which the allocator takes the memory to be in use: the caller's may belong to any
         self.codes_ptr, self.scale_ptr = codes.data_ptr(), _vector(scale, r, "scale", device)
 
     @classmethod
@@ -128,7 +139,7 @@ class Int8Matrix:
     def used_on(self, stream: int):
         """Tells the allocator of the current stream, on which the matrix is about to be used: dropped before that has run, its memory is
         kept until it has."""
-        current = torch.cuda.current_stream(self.device)
+        current = _stream_of(self.device.index, stream)
         for t in (self._codes, self._scale):
             (t[0] if isinstance(t, tuple) else t).record_stream(current)
         self.stream = stream
@@ -312,11 +323,20 @@ class Int8Linear:
             self.by_rows, self.by_cols = int8_quantize(weight, stream=stream), None
         self._x_cols = None
 
+    def _bias_used(self, stream):
+        """Tells the allocator of the stream on which the bias, which may belong to any, was used."""
+        if self.bias is not None:
+            index = self.by_rows.device.index
+            self.bias.record_stream(stream if stream is not None else _stream_of(index, _raw_stream(index)))
+
     def forward(self, x: torch.Tensor, training: bool = False, out_dtype: torch.dtype | None = None, stream=None) -> torch.Tensor:
         if not training:
-            return int8_linear(x, self.by_rows, self.bias, out_dtype, stream=stream)
-        rows, self._x_cols = int8_quantize(x, rows=True, cols=True, stream=stream)
-        return int8_matmul(rows, self.by_rows, self.bias, out_dtype or x.dtype, stream=stream)
+            y = int8_linear(x, self.by_rows, self.bias, out_dtype, stream=stream)
+        else:
+            rows, self._x_cols = int8_quantize(x, rows=True, cols=True, stream=stream)
+            y = int8_matmul(rows, self.by_rows, self.bias, out_dtype or x.dtype, stream=stream)
+        self._bias_used(stream)
+        return y
 
     def backward(self, dy: torch.Tensor, dx_dtype: torch.dtype | None = None, dw_dtype: torch.dtype = torch.float32,
                  dw: torch.Tensor | None = None, stream=None):

@@ -5,7 +5,7 @@ import types
 import pytest
 import torch
 
-from paper_1905_05957_b200 import layer_ops
+from paper_1905_05957_b200 import Int8Linear, Int8Matrix, int8_matmul, layer_ops, matrix_ops
 from paper_1905_05957_b200.layer_ops import Linear16, ResidualNorm
 
 F32, BF16 = torch.float32, torch.bfloat16
@@ -25,7 +25,8 @@ class Tensor:
         Tensor.last += 1 << 24
         self.address, self.used_on = Tensor.last, set()
 
-    device = property(lambda self: f"cuda:{self.index}")
+    device = property(lambda self: torch.device("cuda", self.index))
+    is_cuda = True
 
     def dim(self):
         return len(self.shape)
@@ -76,7 +77,10 @@ def host(monkeypatch):
                             _status={0: (None, 0)}, _matmul_at="matmul", _slope_at="slope", _pack_at="pack", _norm_at="forward", _norm_back_at="backward",
                             _like_of=lambda t: Tensor(*t.shape, dtype=t.dtype, index=t.index, owner="package")).items():
         monkeypatch.setattr(layer_ops, name, value)
-    monkeypatch.setattr(layer_ops, "_streams", {}, raising=False)
+    for name, value in dict(_call=note_call, _linear_ws=lambda *a: 0, _quantize_ws=lambda *a: 0, _raw_stream=lambda index: h.stream, _current=lambda: 0, _status={0: (None, 0)}, _streams={},
+                            _linear_at="linear", _quantize_at="quantize", _matmul_at="matmul",
+                            _empty=lambda *shape, dtype, device: Tensor(*(shape[0] if isinstance(shape[0], tuple) else shape), dtype=dtype, owner="package")).items():
+        monkeypatch.setattr(matrix_ops, name, value, raising=name != "_streams")
     monkeypatch.setattr(torch.cuda, "current_stream", lambda index=None: types.SimpleNamespace(name=h.stream, cuda_stream=h.stream))
 
     def on(stream):
@@ -223,3 +227,21 @@ def test_more_tokens_than_backward_takes_are_refused_forward(host):
         layer.forward(Tensor(2097120, 8, dtype=BF16), training=True)
         del host.calls[:]
     Linear16(w).forward(x, training=True)
+
+
+def test_the_allocator_is_told_where_8_bit_matrices_and_biases_are_used(host):
+    """As above; codes that the package made belong to the stream that made them."""
+    host.on(7)
+    codes, scale = Tensor(32, 64, dtype=torch.int8), Tensor(32)
+    m = Int8Matrix(codes, scale)
+    int8_matmul(m, m)
+    assert codes.used_on == scale.used_on == {7}
+    host.on(8)
+    int8_matmul(m, m)
+    assert codes.used_on == scale.used_on == {7, 8}
+    b, x = Tensor(48), Tensor(16, 64, dtype=BF16)
+    layer = Int8Linear(Tensor(48, 64), b)
+    layer.forward(x)
+    host.on(9)
+    layer.forward(x, training=True)
+    assert b.used_on == {8, 9} and layer.by_rows._codes[0].used_on == {9}
