@@ -1,5 +1,6 @@
 // A linear layer in 16-bit floats: its products (dsq_product16.cuh), the form for a few tokens, the gradient through the
 // activation, and copies onto 16-byte rows.
+#include <atomic>
 #include <type_traits>
 
 #include "dsq_product16.cuh"
@@ -206,10 +207,35 @@ __global__ void __launch_bounds__(256, 2) k_f16_few(const FewParams16 p) {
   }
 }
 
+// CTAs of a form that an SM holds, asked for once a device.
+template <auto KERNEL>
+uint32_t ctas_an_sm() {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<int> known[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 2;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (!n) {
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, KERNEL, 256, 0) != cudaSuccess || n < 1) {
+      (void)cudaGetLastError();
+      return 2;
+    }
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  return (uint32_t)n;
+}
+// What an SM goes through: rounds of CTAs, each taking as long as it has rows of W.
+template <bool BF16, int NT, int RB, bool XVEC>
+uint32_t few_cost(uint32_t n) {
+  const uint32_t rows = ctas_an_sm<k_f16_few<BF16, NT, RB, XVEC>>() * 16 * RB, round = rows * (uint32_t)sm_count();
+  return (n + round - 1) / round * rows;
+}
+
 template <bool BF16, int NT, bool XVEC>
 cudaError_t launch_few16(const FewParams16& p, cudaStream_t st) {
-  // 16 rows a CTA while one round of CTAs (three an SM) takes them all, else 32 (1 x 2048 -> 8192: 8.1 and 7.2 us; -> 2048: 4.4 and 4.9)
-  if ((p.o.n + 15) / 16 > 3 * (uint32_t)sm_count())
+  // 16 or 32 rows a CTA, by the rounds that they take (16 and 32, K = 4096, 148 SMs.  Up to 8 tokens three CTAs an SM and two: -> 7104 10.3 and 10.9 us, -> 7680 13.7 and 11.5,
+  // -> 11008 16.2 and 17.6, -> 16384 23.1 and 21.7.  9 to 16 tokens, two and two: -> 4608 8.7 and 12.6, -> 6144 14.0 and 13.1, -> 11008 20.7 and 23.2)
+  if (few_cost<BF16, NT, 2, XVEC>(p.o.n) <= few_cost<BF16, NT, 1, XVEC>(p.o.n))
     launch_pdl(k_f16_few<BF16, NT, 2, XVEC>, dim3((p.o.n + 31) / 32), dim3(256), st, p);
   else
     launch_pdl(k_f16_few<BF16, NT, 1, XVEC>, dim3((p.o.n + 15) / 16), dim3(256), st, p);

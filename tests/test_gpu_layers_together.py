@@ -241,3 +241,20 @@ def test_more_than_2_31_entries():
     tall[-1] = 3
     out = linear16(tall, torch.ones(cols, 16, dtype=torch.bfloat16, device="cuda"))
     assert bool((out[-1] == 48).all()) and bool((out[-2] == 16).all()) and bool((out[0] == 16).all()) and bool((out[rows // 2] == 16).all())
+
+
+@pytest.mark.parametrize("odd", [0, 1])
+@pytest.mark.parametrize("m", [1, 8, 9, 16, 17, 32])
+@pytest.mark.parametrize("k,n", [(64, 300), (520, 4736), (512, 4752), (264, 7104), (520, 7120), (1032, 9472), (512, 9504), (256, 11008), (2056, 640), (2048, 2048), (1024, 4096), (8200, 2368),
+                                 (8200, 2384), (16400, 136)])
+def test_few_tokens_by_every_form(m, k, n, odd):
+    """Sizes on either side of where another form takes over on 148 SMs; tokens on 16-byte boundaries and not.  Whole numbers: exact."""
+    gen = torch.Generator(device="cuda").manual_seed(m + n)
+    x, w = (torch.randint(-2, 3, s, device="cuda", generator=gen).to(torch.bfloat16) for s in ((m, k + odd), (n, k)))
+    x, b = x[:, odd:], torch.randint(-9, 10, (n,), device="cuda", generator=gen).float()
+    z = x.double() @ w.double().T + b
+    assert torch.equal(linear16(x, w, b, "relu", out_dtype=torch.float32), torch.relu(z).float())
+    layer = Linear16(w, b, "relu")
+    assert torch.equal(layer.forward(x, training=True), torch.relu(z).to(torch.bfloat16))
+    dy = torch.randint(-2, 3, (m, n), device="cuda", generator=gen).to(torch.bfloat16)
+    assert torch.equal(layer.backward(dy, grad_dtype=torch.float32, need_dx=False)[2], (dy.double() * (z > 0)).sum(0).float())
