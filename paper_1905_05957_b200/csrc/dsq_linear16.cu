@@ -73,8 +73,6 @@ __global__ void __launch_bounds__(kThreads) k_f16_empty(const Out16 o) {
 // lane t of a group of four loads 8 consecutive entries of its rows and tokens and feeds them as two instructions' worth.
 // The warps' sums meet in shared memory and are added in the order of the warps.
 constexpr uint32_t kFewMost = 16, kFewGroup = 8;
-// With more than one group of tokens and this many entries of W, a launch of TMA-fed tiles is faster (16 x 4096 -> 16384: 29 and 25 us; 16 x 11008 -> 4096: 19 and 21).
-constexpr uint64_t kFewEntries = 48u << 20;
 
 struct FewParams16 {
   const uint16_t *x, *w;
@@ -363,9 +361,14 @@ struct Shape16 {
   bool copy_a, copy_b;
   uint64_t bytes_a, bytes_b;
 };
-// Few tokens are multiplied by k_f16_few.
+// Few tokens are multiplied by k_f16_few, but where TMA-fed tiles are faster: two groups of tokens and more rows of W than two CTAs an SM with 32 rows each take in a round (9 tokens, K = 4096,
+// 148 SMs: -> 9472 15.7 and, by tiles, 17.2 us, -> 9504 18.6 and 16.5, -> 16384 26.9 and 24.6), or long rows and no more CTAs than SMs, so that a warp's eighth of K takes
+// longer than memory does (8 tokens -> 1024: K = 8192 10.0 and 10.3, 10240 12.1 and 10.8, 16384 18.4 and 13.0; K = 12288 -> 2048 17.4 and 14.9, -> 4096 19.0 and 20.7).
+constexpr uint64_t kFewLong = 8192;
 bool few_tokens(const ds_f16_product* p) {
-  return p->layout == DS_F16_FORWARD && (p->m <= kFewGroup || (p->m <= kFewMost && p->n * p->k <= kFewEntries));
+  const uint64_t sms = (uint64_t)sm_count();
+  if (p->layout != DS_F16_FORWARD || p->m > kFewMost || (p->k > kFewLong && p->n <= 16 * sms)) return false;
+  return p->m <= kFewGroup || p->n <= 2 * 32 * sms;
 }
 Shape16 shape_of(const ds_f16_product* p) {
   Shape16 s;
