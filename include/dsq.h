@@ -460,7 +460,7 @@ int ds_orth_destroy(ds_orth_handle h);
  *          DS_F16_WEIGHTS  a [k, m], b [k, n]   the gradient of its weights: a = dz, b = x
  *   bias (float), residual and z (of the operands' type) may be NULL.  out_dtype: the operands' or DS_F32; out is rounded once from 32 bits, and so is z,
  *   which training keeps.  The residual may be out itself.  Operands that do not start on 16-byte boundaries or whose rows do not are copied into the
- *   workspace (ds_f16_matmul_workspace bytes, 16-byte aligned; 0 where none are) by a launch of their own; a few tokens are read where they lie.  k = 0 gives act(bias) + residual.
+ *   workspace (ds_f16_matmul_workspace bytes, 16-byte aligned; 0 where none are) by a launch of their own; a few tokens in short rows are read where they lie.  k = 0 gives act(bias) + residual.
  *   The order of a sum depends on the sizes and the device, not on timing.
  * ds_f16_slope: dz = dy act'(z) (in 16 bits) and / or sum_n = the column sums of dy act'(z) before it is rounded, in a fixed order.  z as the forward
  *   product left it (NULL for DS_ACT_NONE).  dz may be dy or z itself.  workspace: ds_f16_slope_workspace bytes where sums are asked for.  At most 2097120 rows.

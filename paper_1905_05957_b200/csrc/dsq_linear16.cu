@@ -370,13 +370,16 @@ bool few_tokens(const ds_f16_product* p) {
   if (p->layout != DS_F16_FORWARD || p->m > kFewMost || (p->k > kFewLong && p->n <= 16 * sms)) return false;
   return p->m <= kFewGroup || p->n <= 2 * 32 * sms;
 }
+// Tokens on no boundary are read where they lie while rows are shorter than this, and copied else (a launch of its own and, in Python, memory for it): 8 tokens, K -> 2048, K = 512: 3.0 and,
+// copied, 3.7 us, 2048: 6.7 and 5.8, 8192: 21.9 and 13.5; 16 tokens: 3.8 and 3.9, 9.5 and 6.3, 33.7 and 14.4.
+constexpr uint64_t kFewWhereTheyLie = 2048;
 Shape16 shape_of(const ds_f16_product* p) {
   Shape16 s;
   const bool a_across = p->layout == DS_F16_WEIGHTS, b_across = p->layout != DS_F16_FORWARD;
   s.rows_a = a_across ? p->k : p->m, s.cols_a = a_across ? p->m : p->k;
   s.rows_b = b_across ? p->k : p->n, s.cols_b = b_across ? p->n : p->k;
   // a single row has no pitch
-  s.copy_a = !few_tokens(p) && (!aligned(p->a, 16) || (s.rows_a > 1 && p->lda % 8));
+  s.copy_a = (!few_tokens(p) || p->k >= kFewWhereTheyLie) && (!aligned(p->a, 16) || (s.rows_a > 1 && p->lda % 8));
   s.copy_b = !aligned(p->b, 16) || (s.rows_b > 1 && p->ldb % 8);
   s.bytes_a = s.copy_a ? round_up(s.rows_a * round_up(s.cols_a, kLine) * 2, 256) : 0;
   s.bytes_b = s.copy_b ? round_up(s.rows_b * round_up(s.cols_b, kLine) * 2, 256) : 0;

@@ -95,6 +95,15 @@ def test_product_workspace(lib):
     assert lib.ds_f16_matmul(None, None) == INVALID and lib.ds_f16_matmul_workspace(None) == 0
 
 
+def test_product_workspace_of_few_tokens(lib):
+    """Short rows are read where they lie, long ones are copied; two groups of tokens only where CTAs take W in a round."""
+    def size(**kw):
+        return lib.ds_f16_matmul_workspace(C.byref(_args(b.ds_f16_product, PRODUCT, **{**dict(m=8, k=2040, lda=2041, ldb=2040), **kw})))
+    assert size() == size(m=16) == size(m=1, a=P + 2) == 0
+    assert size(k=2048, lda=2049, ldb=2048) == 8 * 2048 * 2 and size(m=1, k=2048, a=P + 2, ldb=2048) == 2048 * 2 and size(m=8, k=2048, lda=2048, ldb=2048) == 0
+    assert size(m=16, n=1 << 20) == 16 * 2048 * 2 and size(m=8, n=1 << 20) == 0
+
+
 SLOPE = dict(dtype=1, rows=100, cols=64, dy=P, lddy=64, z=FAR, ldz=64, activation=2, dz=2 * FAR, lddz=64, sum=3 * FAR, sum_dtype=0, workspace=4 * FAR, workspace_bytes=1 << 20)
 
 
