@@ -394,6 +394,10 @@ inline uint32_t few_parts(uint32_t tiles, uint32_t k) {
 }
 
 constexpr uint32_t kTurnedMost = 64;
+// Up to 32 tokens have tiles of 32 columns where four CTAs or more share one's K (which plan_mma's times do not know; 17 tokens by 32 columns and by its plan: 2048 -> 2048 7.9 and 9.1 us,
+// 2048 -> 4096 8.7 and 9.1, 4096 -> 1024 8.7 and 8.7); with shorter rows, or fewer CTAs a tile, its plan is as good or better (1024 -> 4096 7.6 and 6.4, 512 -> 1024 5.8 and 4.3, 2048 -> 8192
+// 10.6 and 10.0).
+constexpr uint32_t kNarrow = 32, kNarrowK = 1536;
 
 cudaError_t multiply(const ds_f16_product* p, const Out16& o, Operand16 a, Operand16 b, cudaStream_t st) {
   const uint32_t m = o.m, n = o.n, k = (uint32_t)p->k;
@@ -411,10 +415,13 @@ cudaError_t multiply(const ds_f16_product* p, const Out16& o, Operand16 a, Opera
   if (m <= kTurnedMost || !(blocks || floats)) {
     const MmaShape t{n, m, k, 1, 2, 0, 0, p->dev_status, 1, (uint32_t)o.bf16};
     MmaPlan plan = plan_mma(t);
-    if (m <= 32 && !a.across && !b.across) {
-      plan.pair = false;
-      plan.bn = 32;
-      plan.parts = few_parts(TileWalk(t, 32).total, k);
+    if (m <= kNarrow && k >= kNarrowK && !a.across && !b.across) {
+      const uint32_t parts = few_parts(TileWalk(t, 32).total, k);
+      if (parts >= 4) {
+        plan.pair = false;
+        plan.bn = 32;
+        plan.parts = parts;
+      }
     }
     return product16_turned(plan, b, a, t, EpiTurned{o}, st);
   }
