@@ -386,18 +386,19 @@ Shape16 shape_of(const ds_f16_product* p) {
   return s;
 }
 
-// CTAs that share a tile's K, for few tokens: as many as run at once with at least four steps each.
+// CTAs that share a tile's K, for few tokens: as many as run at once with at least four steps each, if that spares a tile 18 steps, which is what the exchange of their sums costs
+// (17 tokens, split and not: 1536 -> 1536, 18 spared, 7.1 and 7.6 us; 2048 -> 6144, 16, 9.7 and 9.3; 1024 -> 4096, 12, 7.5 and 6.3; 4096 -> 6144, 32, 13.6 and 14.9).
 inline uint32_t few_parts(uint32_t tiles, uint32_t k) {
+  const uint32_t steps = (k + 63) / 64;
   uint32_t p = 1;
-  while (p < 8 && tiles <= (uint32_t)cluster_count(2 * p) && (k + 63) / 64 >= 8 * p) p *= 2;
-  return p;
+  while (p < 8 && tiles <= (uint32_t)cluster_count(2 * p) && steps >= 8 * p) p *= 2;
+  return steps * (p - 1) >= 18 * p ? p : 1;
 }
 
 constexpr uint32_t kTurnedMost = 64;
-// Up to 32 tokens have tiles of 32 columns where four CTAs or more share one's K (which plan_mma's times do not know; 17 tokens by 32 columns and by its plan: 2048 -> 2048 7.9 and 9.1 us,
-// 2048 -> 4096 8.7 and 9.1, 4096 -> 1024 8.7 and 8.7); with shorter rows, or fewer CTAs a tile, its plan is as good or better (1024 -> 4096 7.6 and 6.4, 512 -> 1024 5.8 and 4.3, 2048 -> 8192
-// 10.6 and 10.0).
-constexpr uint32_t kNarrow = 32, kNarrowK = 1536;
+// Up to 32 tokens have tiles of 32 columns, which plan_mma's times do not know: as good as its plan, and better where that is 64 columns and tokens are fewer than 16
+// (10 tokens, 4096 -> 16384 24.5 and 28.3 us, 2048 -> 8192 9.6 and 11.4; 17 tokens 9.7 and 10.6, 4096 -> 8192 15.6 and 15.4).
+constexpr uint32_t kNarrow = 32;
 
 cudaError_t multiply(const ds_f16_product* p, const Out16& o, Operand16 a, Operand16 b, cudaStream_t st) {
   const uint32_t m = o.m, n = o.n, k = (uint32_t)p->k;
@@ -415,13 +416,10 @@ cudaError_t multiply(const ds_f16_product* p, const Out16& o, Operand16 a, Opera
   if (m <= kTurnedMost || !(blocks || floats)) {
     const MmaShape t{n, m, k, 1, 2, 0, 0, p->dev_status, 1, (uint32_t)o.bf16};
     MmaPlan plan = plan_mma(t);
-    if (m <= kNarrow && k >= kNarrowK && !a.across && !b.across) {
-      const uint32_t parts = few_parts(TileWalk(t, 32).total, k);
-      if (parts >= 4) {
-        plan.pair = false;
-        plan.bn = 32;
-        plan.parts = parts;
-      }
+    if (m <= kNarrow && !a.across && !b.across) {
+      plan.pair = false;
+      plan.bn = 32;
+      plan.parts = few_parts(TileWalk(t, 32).total, k);
     }
     return product16_turned(plan, b, a, t, EpiTurned{o}, st);
   }

@@ -10,7 +10,8 @@ cudaError_t product16_turned(const MmaPlan& plan, const Operand16& a, const Oper
   cudaError_t e = operand_map(&ma, a, s.k, kMmaRows);
   if (e == cudaSuccess) e = operand_map(&mb, b, s.k, 32);
   if (e != cudaSuccess) return e;
-  return launch_mma_split<kMmaHalf, 32, kAlong, kAlong>(plan.parts, ma, mb, mb, s, epi, st);      // (32 columns are planned with several parts alone)
+  return plan.parts > 1 ? launch_mma_split<kMmaHalf, 32, kAlong, kAlong>(plan.parts, ma, mb, mb, s, epi, st)
+                        : launch_mma_bn<kMmaHalf, 32, kAlong, kAlong>(ma, mb, mb, s, epi, st);
 }
 
 }  // namespace dsq
