@@ -194,8 +194,16 @@ class Linear16:
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor | None = None, activation: str = "none", dtype: torch.dtype | None = None, stream=None):
         self.activation, self._act = activation, _activation(activation)
-        self.bias, self._dtype = bias, dtype
+        self._bias, self._dtype = bias, dtype
         self.set_weight(weight, stream)
+
+    @property
+    def bias(self) -> torch.Tensor | None:
+        return self._bias
+
+    @bias.setter
+    def bias(self, bias: torch.Tensor | None):
+        self._bias, self._bias_on = bias, {}
 
     def set_weight(self, weight: torch.Tensor, stream=None):
         if stream is not None:
@@ -214,8 +222,7 @@ class Linear16:
         if index != _current():
             with torch.cuda.device(index):
                 return self.set_weight(weight)
-        packed = weight.dtype is not dtype or not _on_boundary(weight.data_ptr(), ld, r)
-        if packed:
+        if weight.dtype is not dtype or not _on_boundary(weight.data_ptr(), ld, r):
             weight, ld = _packed(weight, r, c, ld, dtype, index)
         else:
             weight = weight.detach()             # its memory as it is now, whatever becomes of the caller's tensor
@@ -223,27 +230,20 @@ class Linear16:
         self._w, self._ldw, self.shape, self._index = weight, ld, torch.Size((r, c)), index
         self._x = self._z = None
         self._rows_of_x = self._ldx = 0
-        # where the allocator takes the tensors to be in use; the caller's may belong to any stream
-        self._saved_on = _raw_stream(index)
-        self._stream = self._saved_on if packed else None
+        # the streams on which the allocator takes the tensors to be in use, by their handles; the caller's may belong to any
+        self._on, self._saved_on, self._bias_on = set(), set(), {}      # (the bias's address with each: it may get other storage)
 
     @property
     def weight(self) -> torch.Tensor:
         """The weights as the products read them."""
         return self._w[:, :self.shape[1]]
 
-    def _used(self, saved: bool):
-        """Tells the allocator of the current stream: dropped before that has run, the layer's memory is kept until it has."""
-        index = self._index
-        raw = _raw_stream(index)
-        if raw != self._stream:
-            self._w.record_stream(_stream_of(index, raw))
-            self._stream = raw
-        if saved and raw != self._saved_on:
-            for t in (self._x, self._z):
-                if t is not None:
-                    t.record_stream(_stream_of(index, raw))
-            self._saved_on = raw
+    def _used(self) -> int:
+        """The current stream's handle.  Tells the allocator of a stream that uses the weights for the first time: dropped before it has run, their memory is kept until it has."""
+        raw = _raw_stream(self._index)
+        if raw not in self._on:
+            self._w.record_stream(_stream_of(self._index, raw))
+            self._on.add(raw)
         return raw
 
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None, training: bool = False, out_dtype: torch.dtype | None = None,
@@ -257,7 +257,7 @@ class Linear16:
         if index != _current():
             with torch.cuda.device(index):
                 return self.forward(x, residual, training, out_dtype, out)
-        raw, w, (n, k) = self._used(False), self._w, self.shape
+        raw, w, (n, k) = self._used(), self._w, self.shape
         dtype = w.dtype
         if x.dtype is not dtype:
             raise TypeError(f"x: {dtype} expected, got {x.dtype}")
@@ -270,13 +270,13 @@ class Linear16:
             if m and k and not _on_boundary(x.data_ptr(), ldx, m):      # once, for this product and for the gradient of the weights
                 x, ldx = _packed(x, m, k, ldx, dtype, index)
             else:
-                x = x.detach()                   # its memory as it is now, whatever becomes of the caller's tensor
                 x.record_stream(_stream_of(index, raw))
-        y, z = _multiply(x, m, k, ldx, w, n, self._ldw, self.bias, self._act, residual, out_dtype, out, training and self._act != 0, index, raw)
-        if self.bias is not None:
-            self.bias.record_stream(_stream_of(index, raw))
+        y, z = _multiply(x, m, k, ldx, w, n, self._ldw, self._bias, self._act, residual, out_dtype, out, training and self._act != 0, index, raw)
+        if self._bias is not None and self._bias_on.get(raw) != self._bias.data_ptr():
+            self._bias.record_stream(_stream_of(index, raw))
+            self._bias_on[raw] = self._bias.data_ptr()
         if training:
-            self._x, self._rows_of_x, self._ldx, self._z, self._saved_on = x, m, ldx, z, raw
+            self._x, self._rows_of_x, self._ldx, self._z, self._saved_on, self._x_was = x, m, ldx, z, {raw}, (x.data_ptr(), x.shape)
         return y
 
     def backward(self, dy: torch.Tensor, grad_dtype: torch.dtype | None = None, dw: torch.Tensor | None = None, db: torch.Tensor | None = None,
@@ -290,8 +290,10 @@ class Linear16:
         if self._x is None:
             raise RuntimeError("backward needs a forward with training=True before it")
         x, z, index, act = self._x, self._z, self._index, self._act
-        dtype = x.dtype
+        dtype = self._w.dtype
         dt = _HALVES[dtype]
+        if (x.data_ptr(), x.shape) != self._x_was or x.dtype is not dtype:
+            raise RuntimeError("x has other memory than in the training forward")
         if index != _current():
             with torch.cuda.device(index):
                 return self.backward(dy, grad_dtype, dw, db, need_dx)
@@ -311,7 +313,12 @@ class Linear16:
         for g, what in ((dw, "dw"), (db, "db")):
             if g is not None and g.dtype is not dtype and g.dtype is not torch.float32:
                 raise TypeError(f"{what}: {dtype} or float32 expected, got {g.dtype}")
-        raw = self._used(True)
+        raw = self._used()
+        if raw not in self._saved_on:
+            for t in (x, z):
+                if t is not None:
+                    t.record_stream(_stream_of(index, raw))
+            self._saved_on.add(raw)
         dz, lddz, buf = dy.data_ptr(), lddy, None
         if act or db is not None:
             # dz, and behind it what the sums need
@@ -402,37 +409,43 @@ class ResidualNorm:
             raise ValueError(f"eps: not below 0 expected, got {eps}")
         self._norm, self._scale, self._eps = _NORMS[norm], float(residual_scale), float(eps)
         self._rest = (self._scale, self._eps, _threshold(p), seed & 0xFFFFFFFFFFFFFFFF, _word(layer, "layer"))
+        self._saved = None
+        # the streams on which the allocator takes the parameters and what backward() reads to be in use, by their handles, and the parameters' addresses there
+        self._on, self._saved_on, self._seen = set(), set(), None
         self._tensors = {"post_weight": post_weight, "post_bias": post_bias, "gate": gate, "pre_weight": pre_weight, "pre_bias": pre_bias}
+        self._given = [p for p in ((0, "post_weight", post_weight), (1, "post_bias", post_bias), (2, "gate", gate), (3, "pre_weight", pre_weight), (4, "pre_bias", pre_bias))
+                       if p[2] is not None]
         self.cols = self._index = None
-        for name, t in self._tensors.items():
-            if t is not None:
-                self.cols, self._index = t.shape[-1] if t.dim() else 0, t.get_device()
-                if self._index < 0:
-                    raise ValueError(f"{name}: a CUDA tensor expected: there is no CPU path")
-                break
-        self._members()
-        self._saved = self._saved_on = None
+        if self._given:
+            _, name, t = self._given[0]
+            self.cols, self._index = t.shape[-1] if t.dim() else 0, t.get_device()
+            if self._index < 0:
+                raise ValueError(f"{name}: a CUDA tensor expected: there is no CPU path")
+            self._members()
 
     def _members(self) -> tuple:
         """The members of ds_norm_args from post_w to layer.  The parameters are looked at in every call: their storage may be another since the last one."""
-        at, groups, cols, index = [], 0, self.cols, self._index
-        for name, t in self._tensors.items():
-            if t is None:
-                at.append(None)
-            elif name == "gate":
+        at, groups, cols, index = [None] * 5, 0, self.cols, self._index
+        for i, name, t in self._given:
+            if i == 2:
                 if not 1 <= t.dim() <= 2 or t.shape[-1] != cols or not t.numel() or t.dtype is not torch.float32 or not t.is_contiguous() or t.get_device() != index:
                     raise ValueError(f"gate: [cols] or [groups, cols] contiguous float32 values beside the others expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
                 groups = t.shape[0] if t.dim() == 2 else 1
-                at.append(t.data_ptr())
+                at[2] = t.data_ptr()
             else:
-                at.append(_floats(t, cols, index, name))
+                at[i] = _floats(t, cols, index, name)
         return (at[0], at[1], at[2], groups, at[3], at[4], *self._rest)
 
-    def _used(self, raw: int, index: int):
-        """Tells the allocator of the current stream, on which the parameters are used: they may belong to any, and their storage may be another than at the last call."""
-        for t in self._tensors.values():
-            if t is not None:
+    def _used(self, index: int, members: tuple) -> int:
+        """The current stream's handle.  Tells the allocator of a stream that uses the parameters, or those of another storage, for the first time."""
+        raw = _raw_stream(index)
+        if raw not in self._on or members != self._seen:
+            if members != self._seen:
+                self._on, self._seen = set(), members
+            for _, _, t in self._given:
                 t.record_stream(_stream_of(index, raw))
+            self._on.add(raw)
+        return raw
 
     def forward(self, y: torch.Tensor, x: torch.Tensor | None = None, step: int = 0, training: bool = False, need_h: bool = True, h: torch.Tensor | None = None,
                 n: torch.Tensor | None = None, stream=None):
@@ -491,8 +504,7 @@ class ResidualNorm:
             else:
                 ldn = _given(n, rows, cols, index, "n")
             np_ = n.data_ptr()
-        raw = _raw_stream(index)
-        self._used(raw, index)
+        raw = self._used(index, params)
         stats = sp = None
         yp, status = y.data_ptr(), _status.get(index)
         if training:
@@ -505,12 +517,10 @@ class ResidualNorm:
         if rc:
             _check(rc, "ds_norm_forward")
         if training:
-            # the memory of y and x as it is now, whatever becomes of the caller's tensors
-            y, x = y.detach(), None if x is None else x.detach()
-            for t in (y, x):
-                if t is not None:
-                    t.record_stream(_stream_of(index, raw))
-            self._saved, self._saved_on = (y, ldy, x, ldx, stats, step, stype), raw
+            y.record_stream(_stream_of(index, raw))
+            if x is not None:
+                x.record_stream(_stream_of(index, raw))
+            self._saved, self._saved_on = (y, ldy, x, ldx, stats, step, stype, yp, xp, y.shape, dtype), {raw}
         return h, n
 
     def backward(self, dh: torch.Tensor | None = None, dn: torch.Tensor | None = None, need_dx: bool = True, out: dict | None = None, stream=None):
@@ -521,8 +531,10 @@ class ResidualNorm:
                 return self.backward(dh, dn, need_dx, out)
         if self._saved is None:
             raise RuntimeError("backward needs a forward with training=True before it")
-        y, ldy, x, ldx, stats, step, stype = self._saved
-        (rows, cols), dtype, index = y.shape, y.dtype, y.get_device()
+        y, ldy, x, ldx, stats, step, stype, yp, xp, shape, dtype = self._saved
+        (rows, cols), index = shape, stats.get_device()
+        if y.data_ptr() != yp or y.shape != shape or y.dtype is not dtype or x is not None and (x.data_ptr() != xp or x.shape != shape or x.dtype is not stype):
+            raise RuntimeError("y or x has other memory than in the training forward")
         if index != _current():
             with torch.cuda.device(index):
                 return self.backward(dh, dn, need_dx, out)
@@ -557,17 +569,16 @@ class ResidualNorm:
             at.append(g.data_ptr())
         if out and any(name not in self._tensors for name in out):
             raise ValueError(f"out: parameters are {', '.join(self._tensors)}")
-        raw = _raw_stream(index)
-        self._used(raw, index)
-        if raw != self._saved_on:             # what was kept is dropped at the earliest when this stream is done with it
+        raw = self._used(index, params)
+        if raw not in self._saved_on:         # what was kept is dropped at the earliest when this stream is done with it
             for t in (y, x, stats):
                 if t is not None:
                     t.record_stream(_stream_of(index, raw))
-            self._saved_on = raw
+            self._saved_on.add(raw)
         dy, dx = _like_of(y), None
         if x is not None and need_dx:
             dx = _like_of(x)
-        members = [_DTYPES[dtype], _DTYPES[stype], rows, cols, self._norm, y.data_ptr(), ldy, None if x is None else x.data_ptr(), ldx, *params, step, stats.data_ptr(),
+        members = [_DTYPES[dtype], _DTYPES[stype], rows, cols, self._norm, yp, ldy, xp, ldx, *params, step, stats.data_ptr(),
                    None, 0, None, 0, dhp, lddh, dnp, lddn, None if dx is None else dx.data_ptr(), cols, dy.data_ptr(), cols, *at,
                    _dev_status(index) if cols > _WIDE else None]
         size = _size(_norm_back_ws, *members)

@@ -313,8 +313,16 @@ class Int8Linear:
     an entry) for the gradient of the weights."""
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor | None = None, training: bool = True, stream=None):
-        self.bias = bias
+        self._bias, self._on = bias, {}
         self.set_weight(weight, training, stream)
+
+    @property
+    def bias(self) -> torch.Tensor | None:
+        return self._bias
+
+    @bias.setter
+    def bias(self, bias: torch.Tensor | None):
+        self._bias, self._on = bias, {}
 
     def set_weight(self, weight: torch.Tensor, training: bool = True, stream=None):
         if training:
@@ -323,20 +331,17 @@ class Int8Linear:
             self.by_rows, self.by_cols = int8_quantize(weight, stream=stream), None
         self._x_cols = None
 
-    def _bias_used(self, stream):
-        """Tells the allocator of the stream on which the bias, which may belong to any, was used."""
-        if self.bias is not None:
-            index = self.by_rows.device.index
-            self.bias.record_stream(stream if stream is not None else _stream_of(index, _raw_stream(index)))
-
     def forward(self, x: torch.Tensor, training: bool = False, out_dtype: torch.dtype | None = None, stream=None) -> torch.Tensor:
+        if self._bias is not None:
+            index = self.by_rows.device.index
+            raw = _raw_stream(index) if stream is None else stream.cuda_stream
+            if self._on.get(raw) != self._bias.data_ptr():      # the allocator is told of a stream that uses the bias, which may belong to any, for the first time
+                self._bias.record_stream(_stream_of(index, raw) if stream is None else stream)
+                self._on[raw] = self._bias.data_ptr()
         if not training:
-            y = int8_linear(x, self.by_rows, self.bias, out_dtype, stream=stream)
-        else:
-            rows, self._x_cols = int8_quantize(x, rows=True, cols=True, stream=stream)
-            y = int8_matmul(rows, self.by_rows, self.bias, out_dtype or x.dtype, stream=stream)
-        self._bias_used(stream)
-        return y
+            return int8_linear(x, self.by_rows, self._bias, out_dtype, stream=stream)
+        rows, self._x_cols = int8_quantize(x, rows=True, cols=True, stream=stream)
+        return int8_matmul(rows, self.by_rows, self._bias, out_dtype or x.dtype, stream=stream)
 
     def backward(self, dy: torch.Tensor, dx_dtype: torch.dtype | None = None, dw_dtype: torch.dtype = torch.float32,
                  dw: torch.Tensor | None = None, stream=None):

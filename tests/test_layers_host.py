@@ -25,8 +25,8 @@ class Tensor:
         Tensor.last += 1 << 24
         self.address, self.used_on = Tensor.last, set()
 
-    device = property(lambda self: torch.device("cuda", self.index))
-    is_cuda = True
+    device = property(lambda self: torch.device("cuda", self.index) if self.index >= 0 else torch.device("cpu"))
+    is_cuda = property(lambda self: self.index >= 0)
 
     def dim(self):
         return len(self.shape)
@@ -58,6 +58,8 @@ class Tensor:
         return Tensor(*((shape,) if isinstance(shape, int) else shape), dtype=dtype or self.dtype, index=self.index, owner="package")
 
     def record_stream(self, stream):
+        if self.index < 0:
+            raise NotImplementedError("record_stream on the host")
         self.used_on.add(stream.name)
 
 
@@ -159,25 +161,28 @@ def test_a_layer_keeps_the_weights_that_it_was_given(host):
     assert layer.forward(x).shape == (100, 10) and w.address in _addresses(host.calls[0])
 
 
-def test_what_backward_reads_is_what_forward_read(host):
-    """Its memory is kept, with the sizes that it had: the caller's tensors may get other."""
+@pytest.mark.parametrize("change", [dict(shape=torch.Size((1, 8))), dict(shape=torch.Size((100, 60))), dict(dtype=torch.float16), dict()], ids=str)
+@pytest.mark.parametrize("which", ["x", "y", "r"])
+def test_backward_reads_what_forward_read(host, which, change):
+    """Inputs that have other memory, sizes or types since then are refused."""
     layer, op = Linear16(Tensor(48, 64, dtype=BF16)), ResidualNorm("rms", pre_weight=Tensor(64))
-    x, y, r = Tensor(100, 64, dtype=BF16), Tensor(100, 64, dtype=BF16), Tensor(100, 64)
-    layer.forward(x, training=True)
-    op.forward(y, r, training=True)
-    old = [t.address for t in (x, y, r)]
-    for t in (x, y, r):
-        t.renew()
-        t.shape = torch.Size((1, 8))
-    del host.calls[:]
+    given = dict(x=Tensor(100, 64, dtype=BF16), y=Tensor(100, 64, dtype=BF16), r=Tensor(100, 64))
+    layer.forward(given["x"], training=True)
+    op.forward(given["y"], given["r"], training=True)
     layer.backward(Tensor(100, 48, dtype=BF16))
-    dy, dx, _ = op.backward(Tensor(100, 64))
-    seen = {a for c in host.calls for a in _addresses(c)}
-    assert seen >= set(old) and not seen & {x.address, y.address, r.address} and dy.shape == dx.shape == (100, 64)
+    op.backward(Tensor(100, 64))
+    del host.calls[:]
+    for k, v in change.items():
+        setattr(given[which], k, v)
+    if not change:
+        given[which].renew()
+    with pytest.raises(RuntimeError):
+        layer.backward(Tensor(100, 48, dtype=BF16)) if which == "x" else op.backward(Tensor(100, 64))
+    assert not host.calls
 
 
 def test_the_allocator_is_told_where_a_layer_uses_what_it_was_given(host):
-    """Memory that belongs to another stream, used on one stream alone and dropped: the tensors may belong to any stream, so it is told of that one."""
+    """Memory that belongs to another stream, used on one stream alone: the tensors may belong to any stream, so it is told of that one."""
     host.on(7)
     w, b, x = Tensor(48, 64, dtype=BF16), Tensor(48), Tensor(100, 64, dtype=BF16)
     layer = Linear16(w, b, "gelu")
@@ -186,16 +191,22 @@ def test_the_allocator_is_told_where_a_layer_uses_what_it_was_given(host):
     assert w.used_on == b.used_on == x.used_on == {7}
     layer.bias = other = Tensor(48)
     layer.forward(x)
+    other.renew()                                 # other storage, the stream of the last call
+    layer.forward(x)
     assert other.used_on == {7}
     host.on(8)
     layer.forward(x)
-    assert w.used_on == b.used_on | {8} == other.used_on and x.used_on == {7}      # x: no training, the caller's alone
+    assert w.used_on == other.used_on == {7, 8} and x.used_on == {7}      # x: no training, the caller's alone
     layer.backward(Tensor(100, 48, dtype=BF16))
-    assert x.used_on == {7, 8}
+    assert x.used_on == layer._z.used_on | {7} == {7, 8}
     host.on(9)
-    layer = Linear16(Tensor(48, 64), b)           # the weights are a copy of this stream's own
+    layer = Linear16(w, b)
     layer.forward(x)
-    assert b.used_on == {7, 9}
+    layer.set_weight(Tensor(48, 64, dtype=BF16))
+    assert w.used_on == {7, 8, 9} and b.used_on == {7, 9}
+    layer.bias.index = -1                         # on the host: refused as ever
+    with pytest.raises(ValueError):
+        layer.forward(x)
 
 
 def test_the_allocator_is_told_where_a_joint_uses_what_it_was_given(host):
@@ -208,11 +219,14 @@ def test_the_allocator_is_told_where_a_joint_uses_what_it_was_given(host):
     assert y.used_on == x.used_on == {7}
     host.on(8)
     op.backward(x)
-    assert all(t.used_on == {7, 8} for t in (y, x, *params.values()))
+    assert all(t.used_on == {7, 8} for t in (y, x, *params.values())) and op._saved[4].used_on == {8}
     for t in params.values():
-        t.renew()
-    op.backward(x)                                # other storage, the stream of the last call
+        t.renew()                                 # other storage, the stream of the last call
+    op.backward(x)
     assert all(t.used_on == {8} for t in params.values())
+    host.on(7)
+    op.forward(y, x)
+    assert all(t.used_on == {7, 8} for t in params.values())
 
 
 def test_more_tokens_than_backward_takes_are_refused_forward(host):
@@ -239,9 +253,14 @@ def test_the_allocator_is_told_where_8_bit_matrices_and_biases_are_used(host):
     host.on(8)
     int8_matmul(m, m)
     assert codes.used_on == scale.used_on == {7, 8}
-    b, x = Tensor(48), Tensor(16, 64, dtype=BF16)
+    b, other, x = Tensor(48), Tensor(48), Tensor(16, 64, dtype=BF16)
     layer = Int8Linear(Tensor(48, 64), b)
     layer.forward(x)
     host.on(9)
     layer.forward(x, training=True)
-    assert b.used_on == {8, 9} and layer.by_rows._codes[0].used_on == {9}
+    assert layer.by_rows._codes[0].used_on == {9}
+    layer.bias = other
+    layer.forward(x)
+    other.renew()                                 # other storage, the stream of the last call
+    layer.forward(x)
+    assert b.used_on == {8, 9} and other.used_on == {9}
