@@ -18,7 +18,7 @@ from .matrix_ops import _DTYPES, _check, _current, _dev_status, _raw_stream, _st
 
 _HALVES = {torch.bfloat16: _DTYPES[torch.bfloat16], torch.float16: _DTYPES[torch.float16]}
 _NORMS = {"rms": DS_NORM_RMS, "layer": DS_NORM_LAYER}
-_like_of = torch.empty_like
+_like_of, _F32 = torch.empty_like, torch.float32
 _WIDE = 4096                 # columns above which a row's parts wait for one another
 _SLOPE_ROWS = 2097120        # rows that the gradient through an activation, or a bias's, takes at most
 _NOTHING = (None,) * 13      # the members of ds_norm_args that the forward pass does not read
@@ -88,7 +88,7 @@ def _given(out: torch.Tensor, rows: int, cols: int, index: int, what: str) -> in
 
 def _floats(v: torch.Tensor, n: int, index: int, what: str) -> int:
     """The address of n contiguous float32 values on that device."""
-    if v.dtype is not torch.float32 or v.shape != (n,) or not v.is_contiguous():
+    if v.dtype is not _F32 or v.shape != (n,) or not v.is_contiguous():
         raise ValueError(f"{what}: {n} contiguous float32 values expected, got {v.dtype} {tuple(v.shape)}")
     if v.get_device() != index:
         raise ValueError(f"{what}: on {v.device}, the others on cuda:{index}")
@@ -409,9 +409,7 @@ class ResidualNorm:
             raise ValueError(f"eps: not below 0 expected, got {eps}")
         self._norm, self._scale, self._eps = _NORMS[norm], float(residual_scale), float(eps)
         self._rest = (self._scale, self._eps, _threshold(p), seed & 0xFFFFFFFFFFFFFFFF, _word(layer, "layer"))
-        self._saved = None
-        # the streams on which the allocator takes the parameters and what backward() reads to be in use, by their handles, and the parameters' addresses there
-        self._on, self._saved_on, self._seen = set(), set(), None
+        self._saved, self._saved_on = None, set()      # what backward() reads, and the streams that use it
         self._tensors = {"post_weight": post_weight, "post_bias": post_bias, "gate": gate, "pre_weight": pre_weight, "pre_bias": pre_bias}
         self._given = [p for p in ((0, "post_weight", post_weight), (1, "post_bias", post_bias), (2, "gate", gate), (3, "pre_weight", pre_weight), (4, "pre_bias", pre_bias))
                        if p[2] is not None]
@@ -421,31 +419,40 @@ class ResidualNorm:
             self.cols, self._index = t.shape[-1] if t.dim() else 0, t.get_device()
             if self._index < 0:
                 raise ValueError(f"{name}: a CUDA tensor expected: there is no CPU path")
-            self._members()
+        self._look()
 
     def _members(self) -> tuple:
         """The members of ds_norm_args from post_w to layer.  The parameters are looked at in every call: their storage may be another since the last one."""
+        index = self._index
+        for t, at, shape in self._seen:
+            if t.data_ptr() != at or t.shape != shape or t.dtype is not _F32 or not t.is_contiguous() or t.get_device() != index:
+                return self._look()
+        return self._at
+
+    def _look(self) -> tuple:
         at, groups, cols, index = [None] * 5, 0, self.cols, self._index
         for i, name, t in self._given:
             if i == 2:
-                if not 1 <= t.dim() <= 2 or t.shape[-1] != cols or not t.numel() or t.dtype is not torch.float32 or not t.is_contiguous() or t.get_device() != index:
+                if not 1 <= t.dim() <= 2 or t.shape[-1] != cols or not t.numel() or t.dtype is not _F32 or not t.is_contiguous() or t.get_device() != index:
                     raise ValueError(f"gate: [cols] or [groups, cols] contiguous float32 values beside the others expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
                 groups = t.shape[0] if t.dim() == 2 else 1
                 at[2] = t.data_ptr()
             else:
                 at[i] = _floats(t, cols, index, name)
-        return (at[0], at[1], at[2], groups, at[3], at[4], *self._rest)
+        self._seen = [(t, at[i], t.shape) for i, _, t in self._given]
+        self._on = set()                         # the streams on which the allocator takes these parameters to be in use, by their handles: they may belong to any
+        self._at = (at[0], at[1], at[2], groups, at[3], at[4], *self._rest)
+        return self._at
 
-    def _used(self, index: int, members: tuple) -> int:
-        """The current stream's handle.  Tells the allocator of a stream that uses the parameters, or those of another storage, for the first time."""
+    def _used(self, index: int) -> tuple[int, torch.cuda.Stream]:
+        """The current stream and its handle.  Tells the allocator of one that uses the parameters for the first time: dropped before it has run, their memory is kept until it has."""
         raw = _raw_stream(index)
-        if raw not in self._on or members != self._seen:
-            if members != self._seen:
-                self._on, self._seen = set(), members
-            for _, _, t in self._given:
-                t.record_stream(_stream_of(index, raw))
+        stream = _stream_of(index, raw)
+        if raw not in self._on:
+            for t, _, _ in self._seen:
+                t.record_stream(stream)
             self._on.add(raw)
-        return raw
+        return raw, stream
 
     def forward(self, y: torch.Tensor, x: torch.Tensor | None = None, step: int = 0, training: bool = False, need_h: bool = True, h: torch.Tensor | None = None,
                 n: torch.Tensor | None = None, stream=None):
@@ -504,7 +511,7 @@ class ResidualNorm:
             else:
                 ldn = _given(n, rows, cols, index, "n")
             np_ = n.data_ptr()
-        raw = self._used(index, params)
+        raw, current = self._used(index)
         stats = sp = None
         yp, status = y.data_ptr(), _status.get(index)
         if training:
@@ -517,9 +524,9 @@ class ResidualNorm:
         if rc:
             _check(rc, "ds_norm_forward")
         if training:
-            y.record_stream(_stream_of(index, raw))
+            y.record_stream(current)
             if x is not None:
-                x.record_stream(_stream_of(index, raw))
+                x.record_stream(current)
             self._saved, self._saved_on = (y, ldy, x, ldx, stats, step, stype, yp, xp, y.shape, dtype), {raw}
         return h, n
 
@@ -569,11 +576,11 @@ class ResidualNorm:
             at.append(g.data_ptr())
         if out and any(name not in self._tensors for name in out):
             raise ValueError(f"out: parameters are {', '.join(self._tensors)}")
-        raw = self._used(index, params)
+        raw, current = self._used(index)
         if raw not in self._saved_on:         # what was kept is dropped at the earliest when this stream is done with it
             for t in (y, x, stats):
                 if t is not None:
-                    t.record_stream(_stream_of(index, raw))
+                    t.record_stream(current)
             self._saved_on.add(raw)
         dy, dx = _like_of(y), None
         if x is not None and need_dx:
