@@ -411,8 +411,8 @@ class ResidualNorm:
         self._rest = (self._scale, self._eps, _threshold(p), seed & 0xFFFFFFFFFFFFFFFF, _word(layer, "layer"))
         self._saved, self._saved_on = None, set()      # what backward() reads, and the streams that use it
         self._tensors = {"post_weight": post_weight, "post_bias": post_bias, "gate": gate, "pre_weight": pre_weight, "pre_bias": pre_bias}
-        self._given = [p for p in ((0, "post_weight", post_weight), (1, "post_bias", post_bias), (2, "gate", gate), (3, "pre_weight", pre_weight), (4, "pre_bias", pre_bias))
-                       if p[2] is not None]
+        self._given = [v for v in ((0, "post_weight", post_weight), (1, "post_bias", post_bias), (2, "gate", gate), (3, "pre_weight", pre_weight), (4, "pre_bias", pre_bias))
+                       if v[2] is not None]
         self.cols = self._index = None
         if self._given:
             _, name, t = self._given[0]

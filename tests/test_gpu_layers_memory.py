@@ -1,5 +1,8 @@
 """Memory that layers and joints use without owning it: parameters whose storage is replaced between calls, and tensors that belong to another stream than the one that uses them."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -126,3 +129,28 @@ def test_as_many_tokens_as_a_layer_trains_on():
     assert bool((dx[:-1] == 16).all()) and bool((dx[-1] == 32).all()) and bool((dw == m - 1 + 4).all()) and bool((db == m - 1 + 2).all())
     with pytest.raises(ValueError):
         layer.forward(torch.ones(m + 1, 8, dtype=torch.bfloat16, device="cuda"), training=True)
+
+
+FIRST = """
+import sys
+import torch
+from paper_1905_05957_b200 import ResidualNorm, linear16
+x, w = (torch.ones(s, 2048, device="cuda", dtype=torch.bfloat16) for s in (int(sys.argv[1]), 6144))
+norm = torch.ones(2048, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    y = linear16(x, w)
+    n = ResidualNorm("rms", pre_weight=norm).forward(x)[1]
+y.zero_()
+graph.replay()
+torch.cuda.synchronize()
+assert bool((y == 2048).all()) and bool((n == 1).all())
+"""
+
+
+@pytest.mark.parametrize("tokens", [1, 12])
+def test_a_process_whose_first_call_is_captured(tokens):
+    """What is asked of the device once, how many CTAs an SM holds among it, may be asked while a graph is captured."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", FIRST, str(tokens)], cwd=root, check=True, timeout=300)
