@@ -9,7 +9,7 @@
 //
 // What bounds it (16384 x 4096, RMS norms before and after, bf16): forward 91 us, 5.9 TB/s, and backward 164 us, 4.9 TB/s, of a copy's 6.5; parameters and
 // sums take the registers of one CTA an SM (128 a thread), and what is left over is the latency of a row's exchanges of sums and the issue of instructions (53 and 60 % of the cycles).
-// Layer norms have an exchange more each and twice the sums: 127 and 221 us.  One CTA a row that read the parameters again took 143 and 514.
+// Layer norms have an exchange more each forward, and backward one exchange of eight sums instead of three: 127 and 221 us.  One CTA a row that read the parameters again took 143 and 514.
 #include "dsq_dropout.cuh"
 #include "dsq_mma.cuh"
 #include "dsq_rows8.cuh"
