@@ -460,7 +460,8 @@ int ds_orth_destroy(ds_orth_handle h);
  *          DS_F16_WEIGHTS  a [k, m], b [k, n]   the gradient of its weights: a = dz, b = x
  *   bias (float), residual and z (of the operands' type) may be NULL.  out_dtype: the operands' or DS_F32; out is rounded once from 32 bits, and so is z,
  *   which training keeps.  The residual may be out itself.  Operands that do not start on 16-byte boundaries or whose rows do not are copied into the
- *   workspace (ds_f16_matmul_workspace bytes, 16-byte aligned; 0 where none are) by a launch of their own; a few tokens in short rows are read where they lie.  k = 0 gives act(bias) + residual.
+ *   workspace (ds_f16_matmul_workspace bytes, 16-byte aligned; 0 where none are) by a launch of their own; a few tokens in short rows are read where they lie.  k = 0
+ *   gives act(bias) + residual.
  *   The order of a sum depends on the sizes and the device, not on timing.
  * ds_f16_slope: dz = dy act'(z) (in 16 bits) and / or sum_n = the column sums of dy act'(z) before it is rounded, in a fixed order.  z as the forward
  *   product left it (NULL for DS_ACT_NONE).  dz may be dy or z itself.  workspace: ds_f16_slope_workspace bytes where sums are asked for.  At most 2097120 rows.
@@ -517,10 +518,12 @@ int ds_f16_pack(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t
  *   y, n, dn, dy have `dtype`; x, h, dh, dx have `stream_dtype`: the same, or DS_F32.  Weights, biases, gates and their gradients are float.
  *   ds_norm_forward writes h and / or n, and for the backward pass stats ([rows, 4] floats, 16-byte aligned; may be NULL).  h and n may each be x or y itself, of one type and pitch.
  *   ds_norm_backward: from dh and / or dn (the gradients of h and n) those of x, y and the parameters; each is wanted where its pointer is not NULL.  y, x and the
- *   parameters as the forward pass had them, stats as it left them.  dx and dy may be one of the inputs of their type and pitch.  workspace: ds_norm_backward_workspace bytes, 16-byte aligned.
- *   Infs and NaNs go through these formulas and stay in their rows; in gradients of parameters they reach the columns of which a term is one.  A NaN makes a normalised row NaN, and so does
- *   an inf in a layer norm.  In an RMS norm an inf makes r 0: its own entry becomes NaN, the others 0 (post_b, pre_b); the gradient of what is normalised is NaN all along the row.  Finite
- *   rows whose squares (of layer norms: about the mean) sum to more than 32 bits hold, 3.4e38, have r = 0 as well and come out as 0.  Without a norm an entry touches itself alone.
+ *   parameters as the forward pass had them, stats as it left them.  dx and dy may be one of the inputs of their type and pitch.  workspace: ds_norm_backward_workspace
+ *   bytes, 16-byte aligned.
+ *   Infs and NaNs go through these formulas and stay in their rows; in gradients of parameters they reach the columns of which a term is one.  A NaN makes a normalised
+ *   row NaN, and so does an inf in a layer norm.  In an RMS norm an inf makes r 0: its own entry becomes NaN, the others 0 (post_b, pre_b); the gradient of what is
+ *   normalised is NaN all along the row.  Finite rows whose squares (of layer norms: about the mean) sum to more than 32 bits hold, 3.4e38, have r = 0 as well and come
+ *   out as 0.  Without a norm an entry touches itself alone.
  *   cols <= DS_NORM_MAX_COLS, rows less than 2^30 entries apart, else DS_ERR_UNSUPPORTED.  dev_status may be NULL (DS_DEV_NORM_TIMEOUT).
  */
 #define DS_NORM_MAX_COLS 32768u

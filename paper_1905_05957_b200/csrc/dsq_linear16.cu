@@ -247,7 +247,8 @@ cudaError_t launch_few16(const FewParams16& p, cudaStream_t st) {
 
 // ---- the gradient through the activation ----------------------------------------------------------------
 // dz = dy act'(z) in 16 bits and, from what is not yet rounded, the column sums of each block of kSumRows rows; a second kernel adds
-// the blocks in their order.  Bound by memory (4096 x 4096 in bf16, gelu: 20 us, 5.1 TB/s).  A lane has eight columns; a CTA's eight warps take every eighth row, four at a time.
+// the blocks in their order.  Bound by memory (4096 x 4096 in bf16: silu 17 us, 5.9 TB/s; gelu, whose instructions count, 23 us, 4.5 TB/s).  A lane has eight columns; a
+// CTA's eight warps take every eighth row, four at a time.
 // dz is rounded to 16 bits, since the operands of the matrix instructions that follow have as many, and z was kept so: half a step each, which leaves the gradients 1.4 times
 // as far from exact ones as their own rounding does.
 constexpr uint32_t kSumRows = 32;
@@ -361,17 +362,18 @@ struct Shape16 {
   bool copy_a, copy_b;
   uint64_t bytes_a, bytes_b;
 };
-// Few tokens are multiplied by k_f16_few, but where TMA-fed tiles are faster: two groups of tokens and more rows of W than two CTAs an SM with 32 rows each take in a round (9 tokens, K = 4096,
-// 148 SMs: -> 9472 15.7 and, by tiles, 17.2 us, -> 9504 18.6 and 16.5, -> 16384 26.9 and 24.6), or long rows and no more CTAs than SMs, so that a warp's eighth of K takes
-// longer than memory does (8 tokens -> 1024: K = 8192 10.0 and 10.3, 10240 12.1 and 10.8, 16384 18.4 and 13.0; K = 12288 -> 2048 17.4 and 14.9, -> 4096 19.0 and 20.7).
+// Few tokens are multiplied by k_f16_few, but where TMA-fed tiles are faster: two groups of tokens and more rows of W than two CTAs an SM with 32 rows each take in a
+// round (9 tokens, K = 4096, 148 SMs: -> 9472 15.7 and, by tiles, 17.2 us, -> 9504 18.6 and 16.5, -> 16384 26.9 and 24.6), or long rows and no more CTAs than SMs, so
+// that a warp's eighth of K takes longer than memory does (8 tokens -> 1024: K = 8192 10.0 and 10.3, 10240 12.1 and 10.8, 16384 18.4 and 13.0; K = 12288 -> 2048 17.4 and
+// 14.9, -> 4096 19.0 and 20.7).
 constexpr uint64_t kFewLong = 8192;
 bool few_tokens(const ds_f16_product* p) {
   const uint64_t sms = (uint64_t)sm_count();
   if (p->layout != DS_F16_FORWARD || p->m > kFewMost || (p->k > kFewLong && p->n <= 16 * sms)) return false;
   return p->m <= kFewGroup || p->n <= 2 * 32 * sms;
 }
-// Tokens on no boundary are read where they lie while rows are shorter than this, and copied else (a launch of its own and, in Python, memory for it): 8 tokens, K -> 2048, K = 512: 3.0 and,
-// copied, 3.7 us, 2048: 6.7 and 5.8, 8192: 21.9 and 13.5; 16 tokens: 3.8 and 3.9, 9.5 and 6.3, 33.7 and 14.4.
+// Tokens on no boundary are read where they lie while rows are shorter than this, and copied else (a launch of its own and, in Python, memory for it): 8 tokens, K ->
+// 2048, K = 512: 3.0 and, copied, 3.7 us, 2048: 6.7 and 5.8, 8192: 21.9 and 13.5; 16 tokens: 3.8 and 3.9, 9.5 and 6.3, 33.7 and 14.4.
 constexpr uint64_t kFewWhereTheyLie = 2048;
 Shape16 shape_of(const ds_f16_product* p) {
   Shape16 s;

@@ -50,9 +50,10 @@ constexpr float kLog2E = 1.44269504f, kSqrtHalf = 0.70710678f, kSqrt2OverPi = 0.
 // 1 / (1 + exp(-v)) of v = scaled / log2(e)
 __device__ __forceinline__ float sigmoid2(float scaled) { return reciprocal(1.f + exp2_of(-scaled)); }
 // The normal distribution's Phi(z), and exp(-z^2 / 2): Phi(-|z|) = exp(-z^2 / 2) t P(t) with t = 1 / (1 + 0.3 |z|) and a P of eight terms, fitted for this so that the largest
-// relative error over 0 <= |z| <= 13.3 (where the power of two ends) is least: 1.3e-7.  Evaluated as below it is 2^-20 for |z| up to 4 and grows with the rounding of z^2, to 2^-17 at 13: no
-// cancellation for negative z.  (Five terms of a polynomial with a bounded absolute error were off by 0.16 % of Phi at -5 and 1 % at -8.)  An unrolled run of 32 values is
-// what an epilogue fetches once a block, so that erff's length costs more than its work (4096^3 in training, forward: 107 us by erff, 98 by five terms, 101 by these).
+// relative error over 0 <= |z| <= 13.3 (where the power of two ends) is least: 1.3e-7.  Evaluated as below it is 2^-20 for |z| up to 4 and grows with the rounding of
+// z^2, to 2^-17 at 13: no cancellation for negative z.  (Five terms of a polynomial with a bounded absolute error were off by 0.16 % of Phi at -5 and 1 % at -8.)  An
+// unrolled run of 32 values is what an epilogue fetches once a block, so that erff's length costs more than its work (4096^3 in training, forward: 107 us by erff, 98 by
+// five terms, 101 by these).
 __device__ __forceinline__ float phi_of(float z, float& e) {
   const float t = reciprocal(__fmaf_rn(0.3f, fabsf(z), 1.f));
   e = exp2_of(z * z * (-0.5f * kLog2E));

@@ -189,8 +189,9 @@ class Linear16:
     """A linear layer y = act(x W^T + bias) + residual in 16-bit floats.
 
     W [out, in]: bfloat16 or float16, used where it lies if its rows start on 16-byte boundaries, else copied; or float32 (a slice of a model of the step),
-    copied as `dtype` (bfloat16 unless given).  Call set_weight() after every change of W (the layer keeps the memory that W had then, even if W gets other).  The bias is float32.  forward(x, training=True) keeps x and, with an activation,
-    x W^T + bias in 16 bits for the gradients; with an activation or a bias it takes up to 2097120 tokens."""
+    copied as `dtype` (bfloat16 unless given).  Call set_weight() after every change of W (the layer keeps the memory that W had then, even if W gets other).
+    The bias is float32.  forward(x, training=True) keeps x and, with an activation, x W^T + bias in 16 bits for the gradients; with an activation or a bias
+    it takes up to 2097120 tokens."""
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor | None = None, activation: str = "none", dtype: torch.dtype | None = None, stream=None):
         self.activation, self._act = activation, _activation(activation)
@@ -239,7 +240,8 @@ class Linear16:
         return self._w[:, :self.shape[1]]
 
     def _used(self) -> int:
-        """The current stream's handle.  Tells the allocator of a stream that uses the weights for the first time: dropped before it has run, their memory is kept until it has."""
+        """The current stream's handle.  Tells the allocator of a stream that uses the weights for the first time: dropped before it has run, their memory is
+        kept until it has."""
         raw = _raw_stream(self._index)
         if raw not in self._on:
             self._w.record_stream(_stream_of(self._index, raw))
@@ -445,7 +447,8 @@ class ResidualNorm:
         return self._at
 
     def _used(self, index: int) -> tuple[int, torch.cuda.Stream]:
-        """The current stream and its handle.  Tells the allocator of one that uses the parameters for the first time: dropped before it has run, their memory is kept until it has."""
+        """The current stream's handle, and the stream.  Tells the allocator of one that uses the parameters for the first time: dropped before it has run,
+        their memory is kept until it has."""
         raw = _raw_stream(index)
         stream = _stream_of(index, raw)
         if raw not in self._on:

@@ -332,16 +332,18 @@ class Int8Linear:
         self._x_cols = None
 
     def forward(self, x: torch.Tensor, training: bool = False, out_dtype: torch.dtype | None = None, stream=None) -> torch.Tensor:
+        if not training:
+            y = int8_linear(x, self.by_rows, self._bias, out_dtype, stream=stream)
+        else:
+            rows, self._x_cols = int8_quantize(x, rows=True, cols=True, stream=stream)
+            y = int8_matmul(rows, self.by_rows, self._bias, out_dtype or x.dtype, stream=stream)
         if self._bias is not None:
             index = self.by_rows.device.index
             raw = _raw_stream(index) if stream is None else stream.cuda_stream
             if self._on.get(raw) != self._bias.data_ptr():      # the allocator is told of a stream that uses the bias, which may belong to any, for the first time
                 self._bias.record_stream(_stream_of(index, raw) if stream is None else stream)
                 self._on[raw] = self._bias.data_ptr()
-        if not training:
-            return int8_linear(x, self.by_rows, self._bias, out_dtype, stream=stream)
-        rows, self._x_cols = int8_quantize(x, rows=True, cols=True, stream=stream)
-        return int8_matmul(rows, self.by_rows, self._bias, out_dtype or x.dtype, stream=stream)
+        return y
 
     def backward(self, dy: torch.Tensor, dx_dtype: torch.dtype | None = None, dw_dtype: torch.dtype = torch.float32,
                  dw: torch.Tensor | None = None, stream=None):

@@ -264,3 +264,7 @@ def test_the_allocator_is_told_where_8_bit_matrices_and_biases_are_used(host):
     other.renew()                                 # other storage, the stream of the last call
     layer.forward(x)
     assert b.used_on == {8, 9} and other.used_on == {9}
+    other.index = -1                              # on the host: refused as ever
+    for training in (False, True):
+        with pytest.raises(ValueError):
+            layer.forward(x, training=training)
